@@ -1,7 +1,7 @@
 """Cases that measure the 8-bit linear operators and the token log probabilities.
 
   product        Y = diag(x_scale) (Xc - 128) (Wc - zero)^T diag(w_scale): 8-bit token codes times 8- or 4-bit channel codes
-  logprobs       log probability of each row's given token, the row's log normaliser and entropy, its k likeliest tokens
+  logprobs       log probability of each row's given token, the row's maximum, log sum and entropy, its k likeliest tokens
   logprobs_grad  the gradient of those numbers with respect to the logits
   checkpoint     activations to 8-bit codes with one power-of-two scale per 32 of a token's values, and back
   weight_grad    dW = dY^T X from the 8-bit codes of X
@@ -160,8 +160,9 @@ def prepare(case, seed):
         s["targets"] = torch.where(rows % 16 == 15, torch.full_like(y, -100), y)  # the separators of packed sequences are not scored
         if kind == "logprobs_grad":
             v = s["logits"].float()
-            s["lse"] = torch.logsumexp(v, dim=1)
-            lp = v - s["lse"][:, None]
+            top = v.amax(dim=1)  # what the forward call gave: the row's maximum and the log of its sum
+            s["norm"] = torch.stack([top, torch.log(torch.exp(v - top[:, None]).sum(dim=1))], dim=1)
+            lp = v - s["norm"][:, :1] - s["norm"][:, 1:]
             s["entropy"] = -torch.where(torch.isfinite(lp), lp.exp() * lp, torch.zeros_like(lp)).sum(dim=1)
             s["d_logprob"] = -torch.rand(T, generator=g, device="cuda") / T
             s["d_entropy"] = 0.01 * torch.randn(T, generator=g, device="cuda") / T
@@ -186,7 +187,7 @@ def _buffers(s):
         s["out"] = new(T, c["m"], dtype=_DT[c["y"]])
         s["ws"] = rq.workspace(rq.realq_int8_product_workspace_size(T, c["n"], c["m"], c["w_bits"]))
     elif c["kind"] == "logprobs":
-        s["out"] = {"logprob": new(T), "lse": new(T), "entropy": new(T)}
+        s["out"] = {"logprob": new(T), "norm": new(T, 2), "entropy": new(T)}
         if c["k"]:
             s["out"] |= {"top_ids": new(T, c["k"], dtype=torch.int64), "top_logprob": new(T, c["k"])}
     elif c["kind"] == "logprobs_grad":
@@ -212,7 +213,7 @@ def _own_run(s):
     elif kind == "logprobs":
         rq.realq_token_logprobs(s["logits"], s["targets"], **out)
     elif kind == "logprobs_grad":
-        rq.realq_token_logprobs_grad(s["logits"], s["targets"], s["lse"], out, d_logprob=s["d_logprob"], entropy=s["entropy"], d_entropy=s["d_entropy"],
+        rq.realq_token_logprobs_grad(s["logits"], s["targets"], s["norm"], out, d_logprob=s["d_logprob"], entropy=s["entropy"], d_entropy=s["d_entropy"],
                                      top_ids=s["top_ids"], d_top=s["d_top"])
     elif kind == "checkpoint":
         rq.realq_checkpoint_pack(s["x"], s["codes"], s["byte"])
@@ -253,17 +254,17 @@ def _plain_run(s):
         top = v.amax(dim=1, keepdim=True)
         e = torch.exp(v - top)
         total = e.sum(dim=1, keepdim=True)
-        lse = top + torch.log(total)
-        lp = v - lse
+        log_sum = torch.log(total)
+        lp = v - top - log_sum
         entropy = -torch.where(e > 0, e / total * lp, torch.zeros_like(lp)).sum(dim=1)
-        out = {"logprob": torch.where(scored, lp.gather(1, at)[:, 0], torch.zeros_like(entropy)), "lse": lse[:, 0], "entropy": entropy}
+        out = {"logprob": torch.where(scored, lp.gather(1, at)[:, 0], torch.zeros_like(entropy)), "norm": torch.cat([top, log_sum], dim=1), "entropy": entropy}
         if c["k"]:
             ids = 2 ** 32 - 1 - torch.topk(_top_keys(v), c["k"], dim=1).values % 2 ** 32
             best = v.gather(1, ids)
             out["top_ids"] = torch.where(torch.isfinite(best), ids, torch.full_like(ids, -1))
-            out["top_logprob"] = best - lse
+            out["top_logprob"] = best - top - log_sum
         return out
-    lp = v - s["lse"][:, None]
+    lp = v - s["norm"][:, :1] - s["norm"][:, 1:]
     p = torch.exp(lp)
     g = torch.where(scored, s["d_logprob"], torch.zeros_like(s["d_logprob"]))
     d = torch.where(p > 0, -p * s["d_entropy"][:, None] * (lp + s["entropy"][:, None]), torch.zeros_like(p))
@@ -282,9 +283,9 @@ def work(case):
         w = m * n if c["w_bits"] == 8 else m * ((n + 1) // 2)
         return {"bytes": T * n + w + 4 * T + 4 * m + (m if c["zeros"] else 0) + T * m * _SZ[c["y"]], "flops": 2 * T * n * m}
     if kind == "logprobs":
-        return {"bytes": T * (c["V"] * _SZ[c["logits"]] + 8 + 12 + 12 * c["k"]), "flops": 6 * T * c["V"]}
+        return {"bytes": T * (c["V"] * _SZ[c["logits"]] + 8 + 16 + 12 * c["k"]), "flops": 6 * T * c["V"]}
     if kind == "logprobs_grad":
-        return {"bytes": T * (2 * c["V"] * _SZ[c["logits"]] + 8 + 16 + 12 * c["k"]), "flops": 6 * T * c["V"]}
+        return {"bytes": T * (2 * c["V"] * _SZ[c["logits"]] + 8 + 20 + 12 * c["k"]), "flops": 6 * T * c["V"]}
     if kind == "checkpoint":  # values in, codes and scales out, and back again
         return {"bytes": 2 * T * (c["n"] * (_SZ[c["x"]] + 1) + -(-c["n"] // BLOCK)), "flops": 4 * T * c["n"]}
     n, m = c["n"], c["m"]
@@ -330,7 +331,9 @@ def exact(case, seed):
         mine = torch.zeros_like(v)
         rows = torch.nonzero(y >= 0)[:, 0]
         if kind == "logprobs":
-            one = {"logprob": torch.zeros(len(y), dtype=torch.float64, device="cuda"), "lse": torch.logsumexp(v, dim=1), "entropy": -plogp.sum(dim=1)}
+            one = {"logprob": torch.zeros(len(y), dtype=torch.float64, device="cuda"), "entropy": -plogp.sum(dim=1)}
+            top = v.max(dim=1).values
+            one["norm"] = torch.stack([top, torch.logsumexp(v, dim=1) - top], dim=1)
             one["logprob"][rows] = logp[rows, y[rows]]
             if c["k"]:
                 by = torch.sort(v, dim=1, descending=True, stable=True)
