@@ -247,6 +247,100 @@ realq_status_t realq_quantize_activations(realq_stream_t stream, int64_t T, int6
                                           realq_dtype_t x_dtype, int bits, float a_clip, void *X_q, uint8_t *codes,
                                           float *scale);
 
+/* ---- 8-bit linear operators ----
+ * A quantized module run on its codes, the model's output scored, and a
+ * module's inputs kept in 8 bits for its weight gradient.  The paper has no
+ * counterpart for these; its settings supply the codes (Sec. 5,
+ * "Weight-Activation Quantization") and its perplexities and Fisher
+ * pre-computation the uses. */
+
+/* realq_int8_product: Y = X̂ Ŵᵀ from the codes of both,
+ *   Y[t][i] = x_scale[t] w_scale[i] sum_j (X_codes[t][j] - 128) (w_ij - z_i),
+ * the sum a whole number (exact below 2^24 in magnitude; above, accumulated
+ * in fp32), times x_scale[t], times w_scale[i] in fp32, rounded once to
+ * y_dtype.
+ *   X_codes  T x n bytes and x_scale (T floats): the codes and scales of
+ *            realq_quantize_activations with bits = 8 (zero point 128).
+ *   W_codes  w_bits = 8: m x n bytes (those of realq_quantize_activations on
+ *            the weight's rows, for instance); w_bits = 4: m x ceil(n/2)
+ *            bytes, even column in the low nibble, as the sweep writes them.
+ *   w_scale  m floats, one per output channel (the sweep's with group_size =
+ *            0); w_zero m bytes, or NULL for 2^(w_bits - 1).
+ *   Y        T x m, y_dtype.
+ *   ws       realq_int8_product_workspace_size(T, n, m, w_bits) bytes,
+ *            256-byte aligned; the first word is the status that
+ *            realq_workspace_status reads (REALQ_ERR_TIMEOUT: Y holds NaN
+ *            where a bounded wait gave up).
+ * Any alignment of the codes.  n at most REALQ_INT8_PRODUCT_MAX_N, T and m
+ * below 2^30.  T = 0 is a no-op.  Asynchronous. */
+#define REALQ_INT8_PRODUCT_MAX_N 131071
+size_t realq_int8_product_workspace_size(int64_t T, int64_t n, int64_t m, int w_bits);
+realq_status_t realq_int8_product(realq_stream_t stream, int64_t T, int64_t n, int64_t m, const uint8_t *X_codes,
+                                  const float *x_scale, const uint8_t *W_codes, int w_bits, const float *w_scale,
+                                  const uint8_t *w_zero, void *Y, realq_dtype_t y_dtype, void *ws, size_t ws_bytes);
+
+/* realq_token_logprobs: for each of T rows of V logits (row stride ld >= V
+ * elements, dtype), with p = softmax of the row,
+ *   logprob[t]      log p at targets[t]; 0 for a negative target (a position
+ *                   that is not scored), NaN for one >= V
+ *   norm[2t], [2t+1]  the row's maximum and log sum_j e^(x_j - maximum)
+ *                   (their sum is the log normaliser; realq_token_logprobs_grad
+ *                   takes both, which keeps p exact where the maximum is large)
+ *   entropy[t]      -sum p log p
+ *   top_ids, top_logprob  T x k: the k likeliest tokens, equal logits by the
+ *                   lower index, and their log probabilities; -1 and -inf
+ *                   where fewer than k logits are above -inf
+ * Masked logits may be -inf or the type's lowest value.  A row of nothing but
+ * -inf has maximum -inf, log sum 0, entropy 0, logprob -inf and no top tokens;
+ * one holding a NaN or +inf gets NaN and ids -1.  logprob, norm, entropy and
+ * top_logprob may each be NULL; targets only with logprob NULL; k in
+ * [0, REALQ_TOP_MAX], top_ids NULL only with k = 0.  fp32 sums.  T = 0 is a
+ * no-op.  Asynchronous; no workspace.
+ *
+ * realq_token_logprobs_grad: d_logits (row stride ld_d, dtype) =
+ *   d_logprob[t] d logprob[t] / d x + d_entropy[t] d entropy[t] / d x
+ *   + sum_i d_top[t][i] d top_logprob[t][i] / d x,
+ * with the forward call's norm, entropy and top_ids (an id of -1 takes no
+ * part).  d_logprob, d_entropy (with entropy) and d_top (with top_ids and
+ * k > 0) may each be absent (NULL, or k = 0).  Rows of nothing but -inf get
+ * zeros.  d_logits may be logits (with ld_d = ld). */
+#define REALQ_TOP_MAX 32
+realq_status_t realq_token_logprobs(realq_stream_t stream, int64_t T, int64_t V, int64_t ld, const void *logits,
+                                    realq_dtype_t dtype, const int64_t *targets, float *logprob, float *norm,
+                                    float *entropy, int k, int64_t *top_ids, float *top_logprob);
+realq_status_t realq_token_logprobs_grad(realq_stream_t stream, int64_t T, int64_t V, int64_t ld, const void *logits,
+                                         realq_dtype_t dtype, const int64_t *targets, const float *norm,
+                                         const float *d_logprob, const float *entropy, const float *d_entropy, int k,
+                                         const int64_t *top_ids, const float *d_top, int64_t ld_d, void *d_logits);
+
+/* Activation checkpoints in 8 bits.  realq_checkpoint_pack keeps X (T x n,
+ * x_dtype) as signed codes (T x n bytes) and one scale byte per 32 consecutive
+ * values of a token (T x ceil(n/32) bytes; a row's last block may be shorter):
+ *   byte b = the biased fp32 exponent of the block's largest magnitude,
+ *   code q = clamp(rint(x 2^(133 - b)), -127, 127), value q 2^(b - 133):
+ * a power-of-two step between 1/128 and 1/64 of the block's largest
+ * magnitude, an error of at most half a step (one step where the code is
+ * clamped).  A block holding an infinity or a NaN gets b = 255, codes 0, and
+ * reads back as NaN.  realq_checkpoint_unpack writes the values as x_dtype;
+ * they are bf16 numbers, so neither type rounds them.
+ *
+ * realq_checkpoint_weight_grad: the weight gradient of Y = X Wᵀ (W m x n) with
+ * X read from its checkpoint, dW (m x n fp32) = dYᵀ X̂, added to dW when
+ * accumulate != 0.  dY: T x m, dy_dtype, 16-byte aligned.  Products are exact,
+ * sums fp32; a fixed order of summation (bitwise repeatable).  ws:
+ * realq_checkpoint_weight_grad_workspace_size(T, m, n, dy_dtype) bytes,
+ * 256-byte aligned; its first word is the status that realq_workspace_status
+ * reads (REALQ_ERR_TIMEOUT: NaN where a bounded wait gave up).  T = 0 leaves
+ * or clears dW.  Asynchronous. */
+realq_status_t realq_checkpoint_pack(realq_stream_t stream, int64_t T, int64_t n, const void *X, realq_dtype_t x_dtype,
+                                     int8_t *codes, uint8_t *exps);
+realq_status_t realq_checkpoint_unpack(realq_stream_t stream, int64_t T, int64_t n, const int8_t *codes,
+                                       const uint8_t *exps, void *X, realq_dtype_t x_dtype);
+size_t realq_checkpoint_weight_grad_workspace_size(int64_t T, int64_t m, int64_t n, realq_dtype_t dy_dtype);
+realq_status_t realq_checkpoint_weight_grad(realq_stream_t stream, int64_t T, int64_t m, int64_t n, const void *dY,
+                                            realq_dtype_t dy_dtype, const int8_t *codes, const uint8_t *exps, float *dW,
+                                            int accumulate, void *ws, size_t ws_bytes);
+
 /* Saliency-weighted Hessians of the coarse stage (Sec. 3.3 Eq.
  * saliency_hessian, used by Alg. 1 for every row group g; N_g = 4 in the
  * paper), and the Hessian-side saliency clipping of the appendix.

@@ -21,7 +21,9 @@ __all__ = [
     "realq_hessian_accumulate", "realq_hessian_workspace_size", "realq_hessian_prepare",
     "realq_prepare_workspace_size", "realq_hessian_prepare_noalloc",
     "realq_hessian_prepare_deferred", "realq_prepare_status", "Graph", "realq_graph_begin", "realq_graph_end", "realq_scale_moment", "realq_quantize_layer",
-    "realq_quantize_activations", "realq_saliency_clip", "realq_hessian_weighted_workspace_size",
+    "realq_quantize_activations", "realq_int8_product_workspace_size", "realq_int8_product", "realq_token_logprobs",
+    "realq_token_logprobs_grad", "realq_checkpoint_pack", "realq_checkpoint_unpack",
+    "realq_checkpoint_weight_grad_workspace_size", "realq_checkpoint_weight_grad", "realq_saliency_clip", "realq_hessian_weighted_workspace_size",
     "realq_hessian_accumulate_weighted", "realq_hessian_prepare_scaled", "realq_quantize_layer_grouped",
     "realq_quantize_grouped_workspace_size", "realq_quantize_layer_minibatch",
     "realq_quantize_minibatch_workspace_size", "realq_quantize_tokens_workspace_size", "realq_quantize_layer_tokens",
@@ -106,6 +108,15 @@ _SIGS = {
     "realq_graph_destroy": ([_vp], None),
     "realq_scale_moment": ([_vp, _i64, _i64, _vp, _vp], _int),
     "realq_quantize_activations": ([_vp, _i64, _i64, _vp, _int, _int, _f32, _vp, _vp, _vp], _int),
+    "realq_int8_product_workspace_size": ([_i64, _i64, _i64, _int], _sz),
+    "realq_int8_product": ([_vp, _i64, _i64, _i64, _vp, _vp, _vp, _int, _vp, _vp, _vp, _int, _vp, _sz], _int),
+    "realq_token_logprobs": ([_vp, _i64, _i64, _i64, _vp, _int, _vp, _vp, _vp, _vp, _int, _vp, _vp], _int),
+    "realq_token_logprobs_grad": ([_vp, _i64, _i64, _i64, _vp, _int, _vp, _vp, _vp, _vp, _vp, _int, _vp, _vp, _i64,
+                                   _vp], _int),
+    "realq_checkpoint_pack": ([_vp, _i64, _i64, _vp, _int, _vp, _vp], _int),
+    "realq_checkpoint_unpack": ([_vp, _i64, _i64, _vp, _vp, _vp, _int], _int),
+    "realq_checkpoint_weight_grad_workspace_size": ([_i64, _i64, _i64, _int], _sz),
+    "realq_checkpoint_weight_grad": ([_vp, _i64, _i64, _i64, _vp, _int, _vp, _vp, _vp, _int, _vp, _sz], _int),
     "realq_saliency_clip": ([_vp, _i64, _int, _vp, _f64, _vp, _vp], _int),
     "realq_hessian_weighted_workspace_size": ([_i64, _i64], _sz),
     "realq_hessian_accumulate_weighted": ([_vp, _i64, _i64, _vp, _int, _vp, _vp, _vp, _vp, _sz], _int),
@@ -371,6 +382,130 @@ def realq_quantize_activations(X: torch.Tensor, bits: int = 4, a_clip: float = 0
     _check(lib().realq_quantize_activations(_stream(stream), T, n, _ptr(X), _dtype(X), bits, a_clip, _ptr(X_q),
                                             _ptr(codes), _ptr(scale)))
     return X_q
+
+
+# ------------------------------------------------- 8-bit linear operators ---
+TOP_MAX = 32
+
+
+def _rows(t: torch.Tensor, name: str):
+    """Address and row stride of a matrix whose rows may lie apart."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError(f"{name}: expected a matrix with contiguous, non-overlapping rows")
+    if not t.is_cuda:
+        raise ValueError("expected a CUDA tensor")
+    return ctypes.c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+def realq_int8_product_workspace_size(T: int, n: int, m: int, w_bits: int = 8) -> int:
+    return int(lib().realq_int8_product_workspace_size(T, n, m, w_bits))
+
+
+def realq_int8_product(X_codes: torch.Tensor, x_scale: torch.Tensor, W_codes: torch.Tensor, w_scale: torch.Tensor,
+                       Y: torch.Tensor, w_bits: int = 8, w_zero: Optional[torch.Tensor] = None,
+                       ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Y = diag(x_scale) (X_codes - 128) (W_codes - w_zero)^T diag(w_scale): 8-bit
+    token codes (T x n) times 8-bit (m x n) or packed 4-bit (m x ceil(n/2))
+    channel codes.  w_zero None: 2^(w_bits - 1)."""
+    T, n = X_codes.shape
+    m = W_codes.shape[0]
+    _need(X_codes, torch.uint8, (T, n), "X_codes")
+    _need(W_codes, torch.uint8, (m, n if w_bits == 8 else (n + 1) // 2), "W_codes")
+    _need(x_scale, torch.float32, (T,), "x_scale")
+    _need(w_scale, torch.float32, (m,), "w_scale")
+    _need(w_zero, torch.uint8, (m,), "w_zero")
+    _need(Y, Y.dtype, (T, m), "Y")
+    wp, wb = _ws(ws)
+    _check(lib().realq_int8_product(_stream(stream), T, n, m, _ptr(X_codes), _ptr(x_scale), _ptr(W_codes), w_bits,
+                                    _ptr(w_scale), _ptr(w_zero), _ptr(Y), _dtype(Y), wp, wb))
+    return Y
+
+
+def realq_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor],
+                         logprob: Optional[torch.Tensor] = None, norm: Optional[torch.Tensor] = None,
+                         entropy: Optional[torch.Tensor] = None, top_ids: Optional[torch.Tensor] = None,
+                         top_logprob: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Log probabilities of the targets (int64; negative: not scored) in rows of
+    logits, the rows' (maximum, log sum), entropies and likeliest tokens, each
+    written where its output is given.  Rows of logits may lie apart."""
+    T, V = logits.shape
+    p, ld = _rows(logits, "logits")
+    k = 0 if top_ids is None else top_ids.shape[1]
+    if top_logprob is not None and top_ids is None:
+        raise ValueError("top_logprob needs top_ids")
+    _need(targets, torch.int64, (T,), "targets")
+    _need(logprob, torch.float32, (T,), "logprob")
+    _need(norm, torch.float32, (T, 2), "norm")
+    _need(entropy, torch.float32, (T,), "entropy")
+    _need(top_ids, torch.int64, (T, k), "top_ids")
+    _need(top_logprob, torch.float32, (T, k), "top_logprob")
+    _check(lib().realq_token_logprobs(_stream(stream), T, V, ld, p, _dtype(logits), _ptr(targets), _ptr(logprob),
+                                      _ptr(norm), _ptr(entropy), k, _ptr(top_ids), _ptr(top_logprob)))
+
+
+def realq_token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Tensor], norm: torch.Tensor,
+                              d_logits: torch.Tensor, d_logprob: Optional[torch.Tensor] = None,
+                              entropy: Optional[torch.Tensor] = None, d_entropy: Optional[torch.Tensor] = None,
+                              top_ids: Optional[torch.Tensor] = None, d_top: Optional[torch.Tensor] = None,
+                              stream=None) -> torch.Tensor:
+    """d_logits from the gradients of realq_token_logprobs' outputs that are
+    given; d_logits may be logits."""
+    T, V = logits.shape
+    p, ld = _rows(logits, "logits")
+    if d_logits.dtype != logits.dtype or d_logits.shape != logits.shape:
+        raise ValueError("d_logits must match logits")
+    pd, ldd = _rows(d_logits, "d_logits")
+    k = 0 if d_top is None else d_top.shape[1]
+    _need(targets, torch.int64, (T,), "targets")
+    _need(norm, torch.float32, (T, 2), "norm")
+    _need(d_logprob, torch.float32, (T,), "d_logprob")
+    _need(entropy, torch.float32, (T,), "entropy")
+    _need(d_entropy, torch.float32, (T,), "d_entropy")
+    _need(d_top, torch.float32, (T, k), "d_top")
+    if k:
+        _need(top_ids, torch.int64, (T, k), "top_ids")
+    _check(lib().realq_token_logprobs_grad(_stream(stream), T, V, ld, p, _dtype(logits), _ptr(targets), _ptr(norm),
+                                           _ptr(d_logprob), _ptr(entropy), _ptr(d_entropy), k,
+                                           _ptr(top_ids) if k else None, _ptr(d_top) if k else None, ldd, pd))
+    return d_logits
+
+
+def realq_checkpoint_pack(X: torch.Tensor, codes: torch.Tensor, exps: torch.Tensor, stream=None) -> None:
+    """Keep X (T x n) as 8-bit codes with a power-of-two scale byte per 32 values
+    of a token: codes int8 T x n, exps uint8 T x ceil(n/32)."""
+    T, n = X.shape
+    _need(codes, torch.int8, (T, n), "codes")
+    _need(exps, torch.uint8, (T, (n + 31) // 32), "exps")
+    _check(lib().realq_checkpoint_pack(_stream(stream), T, n, _ptr(X), _dtype(X), _ptr(codes), _ptr(exps)))
+
+
+def realq_checkpoint_unpack(codes: torch.Tensor, exps: torch.Tensor, X: torch.Tensor, stream=None) -> torch.Tensor:
+    T, n = codes.shape
+    _need(codes, torch.int8, (T, n), "codes")
+    _need(exps, torch.uint8, (T, (n + 31) // 32), "exps")
+    _need(X, X.dtype, (T, n), "X")
+    _check(lib().realq_checkpoint_unpack(_stream(stream), T, n, _ptr(codes), _ptr(exps), _ptr(X), _dtype(X)))
+    return X
+
+
+def realq_checkpoint_weight_grad_workspace_size(T: int, m: int, n: int, dy_dtype=torch.bfloat16) -> int:
+    dt = REALQ_BF16 if dy_dtype == torch.bfloat16 else REALQ_F32
+    return int(lib().realq_checkpoint_weight_grad_workspace_size(T, m, n, dt))
+
+
+def realq_checkpoint_weight_grad(dY: torch.Tensor, codes: torch.Tensor, exps: torch.Tensor, dW: torch.Tensor,
+                                 accumulate: bool = False, ws: Optional[torch.Tensor] = None,
+                                 stream=None) -> torch.Tensor:
+    """dW (fp32) = dY^T X (added to dW with accumulate), X read from its 8-bit checkpoint."""
+    T, m = dY.shape
+    n = codes.shape[1]
+    _need(codes, torch.int8, (T, n), "codes")
+    _need(exps, torch.uint8, (T, (n + 31) // 32), "exps")
+    _need(dW, torch.float32, (m, n), "dW")
+    wp, wb = _ws(ws)
+    _check(lib().realq_checkpoint_weight_grad(_stream(stream), T, m, n, _ptr(dY), _dtype(dY), _ptr(codes), _ptr(exps),
+                                              _ptr(dW), int(bool(accumulate)), wp, wb))
+    return dW
 
 
 def realq_saliency_clip(S: torch.Tensor, pct: float = 0.99, S_out: Optional[torch.Tensor] = None,

@@ -355,6 +355,112 @@ realq_status_t realq_quantize_activations(realq_stream_t stream, int64_t T, int6
     return act_quant(S(stream), T, n, X, x_dtype, bits, a_clip, X_q, codes, scale);
 }
 
+// ------------------------------------------------ 8-bit linear operators ---
+size_t realq_int8_product_workspace_size(int64_t T, int64_t n, int64_t m, int w_bits) {
+    return T > 0 && n > 0 && m > 0 && (w_bits == 4 || w_bits == 8) ? int8_product_ws_bytes(T, n, m, w_bits, num_sms()) : 0;
+}
+
+realq_status_t realq_int8_product(realq_stream_t stream, int64_t T, int64_t n, int64_t m, const uint8_t *X_codes,
+                                  const float *x_scale, const uint8_t *W_codes, int w_bits, const float *w_scale,
+                                  const uint8_t *w_zero, void *Y, realq_dtype_t y_dtype, void *ws, size_t ws_bytes) {
+    if (T < 0 || n <= 0 || m <= 0) return fail(REALQ_ERR_INVALID_ARG, "int8_product: n, m > 0 and T >= 0 required");
+    if (w_bits != 4 && w_bits != 8) return fail(REALQ_ERR_INVALID_ARG, "int8_product: w_bits must be 4 or 8 (got %d)", w_bits);
+    if (!valid_dtype(y_dtype)) return fail(REALQ_ERR_INVALID_ARG, "int8_product: bad y_dtype");
+    if (T == 0) return REALQ_OK;
+    if (!X_codes || !x_scale || !W_codes || !w_scale || !Y) return fail(REALQ_ERR_INVALID_ARG, "int8_product: NULL argument");
+    if (reinterpret_cast<uintptr_t>(Y) % (y_dtype == REALQ_BF16 ? 2 : 4))
+        return fail(REALQ_ERR_INVALID_ARG, "int8_product: Y is not aligned to its type");
+    if (n > REALQ_INT8_PRODUCT_MAX_N || m >= (1ll << 30) || T >= (1ll << 30))
+        return fail(REALQ_ERR_UNSUPPORTED, "int8_product: n at most %d, m and T below 2^30", REALQ_INT8_PRODUCT_MAX_N);
+    REALQ_TRY(check_ws(ws, ws_bytes, int8_product_ws_bytes(T, n, m, w_bits, num_sms()), "int8_product"));
+    return int8_product(S(stream), T, n, m, X_codes, x_scale, W_codes, w_bits, w_scale, w_zero, Y, y_dtype, ws, num_sms());
+}
+
+realq_status_t realq_token_logprobs(realq_stream_t stream, int64_t T, int64_t V, int64_t ld, const void *logits,
+                                    realq_dtype_t dtype, const int64_t *targets, float *logprob, float *norm,
+                                    float *entropy, int k, int64_t *top_ids, float *top_logprob) {
+    if (T < 0 || V <= 0 || ld < V) return fail(REALQ_ERR_INVALID_ARG, "token_logprobs: V > 0, ld >= V, T >= 0 required");
+    if (!valid_dtype(dtype)) return fail(REALQ_ERR_INVALID_ARG, "token_logprobs: bad dtype");
+    if (k < 0 || k > REALQ_TOP_MAX) return fail(REALQ_ERR_INVALID_ARG, "token_logprobs: k must be in [0, %d]", REALQ_TOP_MAX);
+    if (T == 0) return REALQ_OK;
+    if (!logits || (logprob && !targets) || (k > 0 && !top_ids))
+        return fail(REALQ_ERR_INVALID_ARG, "token_logprobs: NULL logits, targets or top_ids");
+    if (reinterpret_cast<uintptr_t>(logits) % (dtype == REALQ_BF16 ? 2 : 4))
+        return fail(REALQ_ERR_INVALID_ARG, "token_logprobs: logits not aligned to their type");
+    if (V > INT32_MAX - 65536 || T > INT32_MAX / 8) return fail(REALQ_ERR_UNSUPPORTED, "token_logprobs: too many rows or columns");
+    return token_logprobs(S(stream), T, V, ld, logits, dtype, targets, logprob, norm, entropy, k, top_ids, top_logprob,
+                          num_sms());
+}
+
+realq_status_t realq_token_logprobs_grad(realq_stream_t stream, int64_t T, int64_t V, int64_t ld, const void *logits,
+                                         realq_dtype_t dtype, const int64_t *targets, const float *norm,
+                                         const float *d_logprob, const float *entropy, const float *d_entropy, int k,
+                                         const int64_t *top_ids, const float *d_top, int64_t ld_d, void *d_logits) {
+    if (T < 0 || V <= 0 || ld < V || ld_d < V)
+        return fail(REALQ_ERR_INVALID_ARG, "token_logprobs_grad: V > 0, ld and ld_d >= V, T >= 0 required");
+    if (!valid_dtype(dtype)) return fail(REALQ_ERR_INVALID_ARG, "token_logprobs_grad: bad dtype");
+    if (k < 0 || k > REALQ_TOP_MAX)
+        return fail(REALQ_ERR_INVALID_ARG, "token_logprobs_grad: k must be in [0, %d]", REALQ_TOP_MAX);
+    if (T == 0) return REALQ_OK;
+    if (!logits || !norm || !d_logits) return fail(REALQ_ERR_INVALID_ARG, "token_logprobs_grad: NULL logits, norm or d_logits");
+    if ((d_logprob && !targets) || (d_entropy && !entropy) || (k > 0 && (!top_ids || !d_top)))
+        return fail(REALQ_ERR_INVALID_ARG, "token_logprobs_grad: a gradient without its targets, entropy or top_ids");
+    const uintptr_t es = dtype == REALQ_BF16 ? 2 : 4;
+    if (reinterpret_cast<uintptr_t>(logits) % es || reinterpret_cast<uintptr_t>(d_logits) % es)
+        return fail(REALQ_ERR_INVALID_ARG, "token_logprobs_grad: logits not aligned to their type");
+    if (d_logits == logits && ld_d != ld)
+        return fail(REALQ_ERR_INVALID_ARG, "token_logprobs_grad: in place, ld_d must be ld");
+    if (V > INT32_MAX - 65536 || T > INT32_MAX / ((V + 4095) / 4096))
+        return fail(REALQ_ERR_UNSUPPORTED, "token_logprobs_grad: too many rows or columns");
+    return token_logprobs_grad(S(stream), T, V, ld, logits, dtype, targets, norm, d_logprob, entropy, d_entropy, k,
+                               top_ids, d_top, ld_d, d_logits);
+}
+
+static realq_status_t check_checkpoint(const char *who, int64_t T, int64_t n, const void *X, realq_dtype_t x_dtype,
+                                       const void *codes, const void *exps) {
+    if (T < 0 || n <= 0) return fail(REALQ_ERR_INVALID_ARG, "%s: n > 0, T >= 0 required", who);
+    if (!valid_dtype(x_dtype)) return fail(REALQ_ERR_INVALID_ARG, "%s: bad dtype", who);
+    if (T > 0 && (!X || !codes || !exps)) return fail(REALQ_ERR_INVALID_ARG, "%s: NULL argument", who);
+    if (reinterpret_cast<uintptr_t>(X) % (x_dtype == REALQ_BF16 ? 2 : 4))
+        return fail(REALQ_ERR_INVALID_ARG, "%s: values not aligned to their type", who);
+    if (T > (int64_t)INT32_MAX / ((n + 31) / 32) * 8) return fail(REALQ_ERR_UNSUPPORTED, "%s: too many values", who);
+    return REALQ_OK;
+}
+
+realq_status_t realq_checkpoint_pack(realq_stream_t stream, int64_t T, int64_t n, const void *X, realq_dtype_t x_dtype,
+                                     int8_t *codes, uint8_t *exps) {
+    REALQ_TRY(check_checkpoint("checkpoint_pack", T, n, X, x_dtype, codes, exps));
+    return T == 0 ? REALQ_OK : checkpoint_pack(S(stream), T, n, X, x_dtype, codes, exps);
+}
+
+realq_status_t realq_checkpoint_unpack(realq_stream_t stream, int64_t T, int64_t n, const int8_t *codes,
+                                       const uint8_t *exps, void *X, realq_dtype_t x_dtype) {
+    REALQ_TRY(check_checkpoint("checkpoint_unpack", T, n, X, x_dtype, codes, exps));
+    return T == 0 ? REALQ_OK : checkpoint_unpack(S(stream), T, n, codes, exps, X, x_dtype);
+}
+
+size_t realq_checkpoint_weight_grad_workspace_size(int64_t T, int64_t m, int64_t n, realq_dtype_t dy_dtype) {
+    return T > 0 && n > 0 && m > 0 && valid_dtype(dy_dtype) ? checkpoint_grad_ws_bytes(T, m, n, dy_dtype, num_sms()) : 0;
+}
+
+realq_status_t realq_checkpoint_weight_grad(realq_stream_t stream, int64_t T, int64_t m, int64_t n, const void *dY,
+                                            realq_dtype_t dy_dtype, const int8_t *codes, const uint8_t *exps, float *dW,
+                                            int accumulate, void *ws, size_t ws_bytes) {
+    if (m <= 0) return fail(REALQ_ERR_INVALID_ARG, "checkpoint_weight_grad: m > 0 required");
+    REALQ_TRY(check_checkpoint("checkpoint_weight_grad", T, n, dY, dy_dtype, codes, exps));
+    if (!dW) return fail(REALQ_ERR_INVALID_ARG, "checkpoint_weight_grad: NULL dW");
+    if (T == 0) {   // an empty sum
+        if (!accumulate) REALQ_CUDA_TRY(cudaMemsetAsync(dW, 0, (size_t)m * n * sizeof(float), S(stream)));
+        return REALQ_OK;
+    }
+    if (reinterpret_cast<uintptr_t>(dY) % 16)
+        return fail(REALQ_ERR_INVALID_ARG, "checkpoint_weight_grad: dY must be 16-byte aligned");
+    if (m >= (1ll << 30) || n >= (1ll << 30) || T >= (1ll << 29))
+        return fail(REALQ_ERR_UNSUPPORTED, "checkpoint_weight_grad: m, n below 2^30 and T below 2^29");
+    REALQ_TRY(check_ws(ws, ws_bytes, checkpoint_grad_ws_bytes(T, m, n, dy_dtype, num_sms()), "checkpoint_weight_grad"));
+    return checkpoint_grad(S(stream), T, m, n, dY, dy_dtype, codes, exps, dW, accumulate, ws, num_sms());
+}
+
 realq_status_t realq_saliency_clip(realq_stream_t stream, int64_t T, int n_groups, const float *sal, double pct,
                                    float *sal_out, float *clip_out) {
     if (T <= 0 || n_groups <= 0 || !sal || !clip_out) return fail(REALQ_ERR_INVALID_ARG, "saliency_clip: bad argument");

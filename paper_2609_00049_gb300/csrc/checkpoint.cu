@@ -1,0 +1,189 @@
+// Activation checkpoints in 8 bits: a layer's inputs X (T x n) kept for the
+// backward pass as signed 8-bit codes with one power-of-two scale for each 32
+// consecutive values of a token (the last block of a row may be shorter).
+//
+//   byte  b = biased fp32 exponent of the block's largest magnitude
+//   code  q = clamp(rint(x 2^(133 - b)), -127, 127)
+//   value x̂ = q 2^(b - 133)
+//
+// so the largest magnitude lies in [64, 128) steps, a value is off by at most
+// half a step (a whole one where rounding would reach 128), and q with its
+// sign fits bf16's eight significant bits: x̂ is a bf16 number and the
+// products formed from it need no further rounding.  A block holding an
+// infinity or a NaN gets byte 255 and reads back as NaN.
+//
+// Both directions read and write each byte once and are bound by HBM.  A
+// thread owns eight values (one 16-byte load of bf16, two of fp32) and four
+// neighbouring lanes share a block, so its maximum takes two shuffles;
+// widths that are not a multiple of 32 and unaligned rows take a warp per
+// block, one value to a lane.
+#include "kernels.cuh"
+
+namespace realq {
+namespace {
+
+constexpr unsigned FULL = 0xFFFFFFFFu;
+constexpr int THREADS = 256;
+
+__device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }   // -126 <= e <= 127
+
+// bits of |x|: ordered like the magnitudes, infinities and NaN above all numbers
+__device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
+// x 2^(133 - b) in two exact steps (2^133 is no fp32 number)
+__device__ __forceinline__ int code_of(float x, float s1, float s2) {
+    return max(-127, min(127, __float2int_rn(x * s1 * s2)));
+}
+__device__ __forceinline__ void scales_of(uint32_t b, float &s1, float &s2) {
+    const int up = 133 - (int)b, h = up >> 1;
+    s1 = pow2(h);
+    s2 = pow2(up - h);
+}
+// 2^(b - 133), subnormal below b = 7; NaN for b = 255
+__device__ __forceinline__ float step_of(uint32_t b) {
+    if (b == 255u) return __int_as_float(0x7FC00000);
+    return __uint_as_float(b >= 7u ? (b - 6u) << 23 : 1u << (b + 16u));
+}
+
+__device__ __forceinline__ void load8(const float *p, float (&v)[8]) {
+    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void load8(const __nv_bfloat16 *p, float (&v)[8]) {
+    const uint4 a = *reinterpret_cast<const uint4 *>(p);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void store8(float *p, const float (&v)[8]) {
+    reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void store8(__nv_bfloat16 *p, const float (&v)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {   // every value is a bf16 number: the upper halves are exact
+        w[i] = (__float_as_uint(v[2 * i]) >> 16) | (__float_as_uint(v[2 * i + 1]) & 0xFFFF0000u);
+    }
+    *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void store1(float *p, float v) { *p = v; }
+__device__ __forceinline__ void store1(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
+
+// n a multiple of 32: rows end at block ends, so blocks are numbered through.
+template <typename TX>
+__global__ void __launch_bounds__(THREADS) pack_vec_kernel(int64_t groups, const TX *X, int8_t *codes, uint8_t *exps) {
+    // groups of eight values; 4 groups per block, so the lanes of a block are all in or all out
+    const int64_t g = (int64_t)blockIdx.x * THREADS + threadIdx.x;
+    if (g - (threadIdx.x & 31) >= groups) return;   // whole warps leave
+    const bool in = g < groups;
+    float v[8];
+    uint32_t m = 0;
+    if (in) {
+        load8(X + g * 8, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, mag(v[i]));
+    }
+    m = max(m, __shfl_xor_sync(FULL, m, 1));
+    m = max(m, __shfl_xor_sync(FULL, m, 2));
+    if (!in) return;
+    const uint32_t b = m >> 23;
+    float s1, s2;
+    scales_of(b, s1, s2);
+    uint32_t w[2] = {0, 0};
+    if (b < 255u) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i >> 2] |= (uint32_t)(code_of(v[i], s1, s2) & 255) << (8 * (i & 3));
+    }
+    *reinterpret_cast<uint2 *>(codes + g * 8) = make_uint2(w[0], w[1]);
+    if ((threadIdx.x & 3) == 0) exps[g >> 2] = (uint8_t)b;
+}
+
+template <typename TX>
+__global__ void __launch_bounds__(THREADS) unpack_vec_kernel(int64_t groups, const int8_t *codes, const uint8_t *exps,
+                                                             TX *X) {
+    const int64_t g = (int64_t)blockIdx.x * THREADS + threadIdx.x;
+    if (g >= groups) return;
+    const uint2 w = *reinterpret_cast<const uint2 *>(codes + g * 8);
+    const float s = step_of(exps[g >> 2]);
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3))) * s;
+    store8(X + g * 8, v);
+}
+
+// Any width and alignment: warp b % nb of row b / nb.
+template <typename TX>
+__global__ void __launch_bounds__(THREADS) pack_row_kernel(int64_t T, int64_t n, int64_t nb, const TX *X,
+                                                           int8_t *codes, uint8_t *exps) {
+    const int lane = threadIdx.x & 31;
+    const int64_t w = ((int64_t)blockIdx.x * THREADS + threadIdx.x) >> 5;
+    if (w >= T * nb) return;
+    const int64_t t = w / nb, c = (w % nb) * 32 + lane;
+    const float x = c < n ? load_as_float(X, t * n + c) : 0.f;
+    const uint32_t b = __reduce_max_sync(FULL, mag(x)) >> 23;
+    float s1, s2;
+    scales_of(b, s1, s2);
+    if (c < n) codes[t * n + c] = b < 255u ? (int8_t)code_of(x, s1, s2) : 0;
+    if (lane == 0) exps[w] = (uint8_t)b;
+}
+
+template <typename TX>
+__global__ void __launch_bounds__(THREADS) unpack_row_kernel(int64_t T, int64_t n, int64_t nb, const int8_t *codes,
+                                                             const uint8_t *exps, TX *X) {
+    const int lane = threadIdx.x & 31;
+    const int64_t w = ((int64_t)blockIdx.x * THREADS + threadIdx.x) >> 5;
+    if (w >= T * nb) return;
+    const int64_t t = w / nb, c = (w % nb) * 32 + lane;
+    if (c < n) store1(X + t * n + c, (float)codes[t * n + c] * step_of(exps[w]));
+}
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+}  // namespace
+
+template <typename TX>
+static void pack_launch(cudaStream_t s, int64_t T, int64_t n, const TX *X, int8_t *codes, uint8_t *exps) {
+    const int64_t nb = (n + 31) / 32, groups = T * n / 8;
+    Launch L("checkpoint_pack", s);
+    if (n % 32 == 0 && aligned16(X) && aligned16(codes))
+        pack_vec_kernel<TX><<<(unsigned)((groups + THREADS - 1) / THREADS), THREADS, 0, s>>>(groups, X, codes, exps);
+    else
+        pack_row_kernel<TX><<<(unsigned)((T * nb * 32 + THREADS - 1) / THREADS), THREADS, 0, s>>>(T, n, nb, X, codes,
+                                                                                                  exps);
+}
+
+template <typename TX>
+static void unpack_launch(cudaStream_t s, int64_t T, int64_t n, const int8_t *codes, const uint8_t *exps, TX *X) {
+    const int64_t nb = (n + 31) / 32, groups = T * n / 8;
+    Launch L("checkpoint_unpack", s);
+    if (n % 32 == 0 && aligned16(X) && aligned16(codes))
+        unpack_vec_kernel<TX><<<(unsigned)((groups + THREADS - 1) / THREADS), THREADS, 0, s>>>(groups, codes, exps, X);
+    else
+        unpack_row_kernel<TX><<<(unsigned)((T * nb * 32 + THREADS - 1) / THREADS), THREADS, 0, s>>>(T, n, nb, codes,
+                                                                                                    exps, X);
+}
+
+realq_status_t checkpoint_pack(cudaStream_t s, int64_t T, int64_t n, const void *X, realq_dtype_t dt, int8_t *codes,
+                               uint8_t *exps) {
+    if (dt == REALQ_BF16)
+        pack_launch(s, T, n, static_cast<const __nv_bfloat16 *>(X), codes, exps);
+    else
+        pack_launch(s, T, n, static_cast<const float *>(X), codes, exps);
+    return check_launch("checkpoint_pack");
+}
+
+realq_status_t checkpoint_unpack(cudaStream_t s, int64_t T, int64_t n, const int8_t *codes, const uint8_t *exps,
+                                 void *X, realq_dtype_t dt) {
+    if (dt == REALQ_BF16)
+        unpack_launch(s, T, n, codes, exps, static_cast<__nv_bfloat16 *>(X));
+    else
+        unpack_launch(s, T, n, codes, exps, static_cast<float *>(X));
+    return check_launch("checkpoint_unpack");
+}
+
+}  // namespace realq

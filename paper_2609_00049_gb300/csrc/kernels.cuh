@@ -139,6 +139,27 @@ realq_status_t tc_split_diff(cudaStream_t s, int64_t count, const float *x, cons
 realq_status_t act_quant(cudaStream_t s, int64_t T, int64_t n, const void *X, realq_dtype_t dt, int bits, float a_clip,
                          void *Xq, uint8_t *codes, float *scale);
 
+// ---------------------------------------------- 8-bit linear operators ---
+// Sizes and pointers have been checked by the caller (see realq.h).
+realq_status_t checkpoint_pack(cudaStream_t s, int64_t T, int64_t n, const void *X, realq_dtype_t dt, int8_t *codes,
+                               uint8_t *exps);
+realq_status_t checkpoint_unpack(cudaStream_t s, int64_t T, int64_t n, const int8_t *codes, const uint8_t *exps,
+                                 void *X, realq_dtype_t dt);
+size_t checkpoint_grad_ws_bytes(int64_t T, int64_t m, int64_t n, realq_dtype_t dy_dtype, int sms);
+realq_status_t checkpoint_grad(cudaStream_t s, int64_t T, int64_t m, int64_t n, const void *dY, realq_dtype_t dt,
+                               const int8_t *codes, const uint8_t *exps, float *dW, int accumulate, void *ws, int sms);
+size_t int8_product_ws_bytes(int64_t T, int64_t n, int64_t m, int w_bits, int sms);
+realq_status_t int8_product(cudaStream_t s, int64_t T, int64_t n, int64_t m, const uint8_t *X, const float *x_scale,
+                            const uint8_t *W, int w_bits, const float *w_scale, const uint8_t *w_zero, void *Y,
+                            realq_dtype_t y_dtype, void *ws, int sms);
+realq_status_t token_logprobs(cudaStream_t s, int64_t T, int64_t V, int64_t ld, const void *X, realq_dtype_t dt,
+                              const int64_t *targets, float *logprob, float *norm, float *entropy, int k,
+                              int64_t *top_ids, float *top_lp, int sms);
+realq_status_t token_logprobs_grad(cudaStream_t s, int64_t T, int64_t V, int64_t ld, const void *X, realq_dtype_t dt,
+                                   const int64_t *targets, const float *norm, const float *d_logprob,
+                                   const float *entropy, const float *d_entropy, int k, const int64_t *top_ids,
+                                   const float *d_top, int64_t ldd, void *D);
+
 // ------------------------------------------- saliency-weighted Hessians ---
 size_t saliency_clip_ws_bytes();
 realq_status_t saliency_clip(cudaStream_t s, int64_t T, int ng, const float *S, double pct, float *S_out,
