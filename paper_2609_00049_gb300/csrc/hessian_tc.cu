@@ -334,9 +334,16 @@ static CUresult encode_tmap_2d(CUtensorMapDataType dt, CUtensorMap *map, const v
     cuuint32_t estr[2] = {1, 1};
     return g_encode(map, dt, 2, const_cast<void *>(base), dims, strides, box, estr,
                     CU_TENSOR_MAP_INTERLEAVE_NONE,
-                    swizzle128 == 2 ? CU_TENSOR_MAP_SWIZZLE_64B
+                    swizzle128 == 3   ? CU_TENSOR_MAP_SWIZZLE_32B
+                    : swizzle128 == 2 ? CU_TENSOR_MAP_SWIZZLE_64B
                                     : (swizzle128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE),
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
+CUresult encode_tmap_2d_u8(CUtensorMap *map, const void *base, uint64_t inner, uint64_t outer,
+                           uint64_t row_stride_bytes, uint32_t box_inner, uint32_t box_outer, int swizzle) {
+    return encode_tmap_2d(CU_TENSOR_MAP_DATA_TYPE_UINT8, map, base, inner, outer, row_stride_bytes, box_inner,
+                          box_outer, swizzle);
 }
 
 CUresult encode_tmap_2d_f16(CUtensorMap *map, const void *base, uint64_t inner, uint64_t outer,

@@ -264,15 +264,24 @@ realq_status_t stream(cudaStream_t s, int64_t T, int64_t n, int64_t m, const uin
 
 }  // namespace
 
+constexpr int64_t STREAM_T = 8;   // tokens up to which the streaming kernel runs
+
 size_t int8_product_ws_bytes(int64_t T, int64_t n, int64_t m, int w_bits, int sms) {
-    (void)T; (void)n; (void)m; (void)w_bits; (void)sms;
-    return 256;
+    return T <= STREAM_T ? 256 : int8_tc_ws_bytes(T, n, m, w_bits, sms);
 }
 
 realq_status_t int8_product(cudaStream_t s, int64_t T, int64_t n, int64_t m, const uint8_t *X, const float *x_scale,
                             const uint8_t *W, int w_bits, const float *w_scale, const uint8_t *w_zero, void *Y,
                             realq_dtype_t y_dtype, void *ws, int sms) {
-    (void)ws;
+    if (T > STREAM_T) {
+        const int64_t rb = w_bits == 8 ? n : (n + 1) / 2;
+        // (whole rows at an odd address go through the streaming kernel, eight tokens at a time)
+        if (rb % 16 || (reinterpret_cast<uintptr_t>(W) & 15) == 0)
+            return int8_product_tc(s, T, n, m, X, x_scale, W, w_bits, w_scale, w_zero, Y, y_dtype, ws, sms);
+        if (T > 65535 * STREAM_T)
+            return fail(REALQ_ERR_UNSUPPORTED, "int8_product: more than %lld tokens need 16-byte aligned W_codes",
+                        (long long)(65535 * STREAM_T));
+    }
     auto run = [&](auto *y) {
         return w_bits == 8 ? stream<8>(s, T, n, m, X, x_scale, W, w_scale, w_zero, y, sms)
                            : stream<4>(s, T, n, m, X, x_scale, W, w_scale, w_zero, y, sms);

@@ -1,0 +1,454 @@
+// The 8-bit product for more than a few tokens, on the 5th-generation tensor
+// cores: Y^T tiles of 128 output channels by up to 256 tokens.
+//
+// Code minus zero point is a whole number of at most nine bits, exact in fp16,
+// and so are the products in fp32 and, below 2^24, their sums: kind::f16 gives
+// the integer product at the bf16 rate (the int8 rate of this GPU is far below
+// it).  Past 2^24 each accumulated MMA may lose about a unit in the last place.
+//
+// The weight codes are converted on their way in, so that they cross HBM and L2
+// as bytes (or nibbles): TMA puts the codes of a 64-wide K step in shared
+// memory (64- or 32-byte swizzle: a thread reads its row's 16-byte chunks
+// without bank conflicts), eight converter warps, two groups taking turns, make
+// fp16 pairs of them (the byte as the low mantissa bits of 1024, less
+// 1024 + zero) and store them to TMEM as the MMA's A operand: lane = channel,
+// 32 columns per K step.  Shared memory then carries only the tokens' plane,
+// which a pass over the token codes writes as fp16 to the workspace; B is a
+// K-major tile of it (128-byte swizzle).
+//
+// Roles (448 threads, one persistent CTA per SM): warps 0-7 convert, warps
+// 8-11 drain the accumulator (lane = channel, so a warp's stores of one token
+// are contiguous), warp 12 issues TMA, warp 13 the MMAs.  TMEM: columns 0-255
+// hold the accumulator (two of them when a tile has at most 128 tokens, so that
+// a drain overlaps the next tile), 256-511 eight A slots.  One ring of stages
+// covers the codes, the tokens and the A slots.  With fewer tiles than SMs the
+// K range is split; the parts are summed in a fixed order.
+// Every wait is bounded; a tile whose wait gave up is written as NaN and the
+// status word gets ST_TIMEOUT.
+#include "kernels.cuh"
+#include "tc.cuh"
+
+#include <algorithm>
+
+namespace realq {
+namespace {
+
+constexpr int TM = 128;                    // channels per tile
+constexpr int TNMAX = 256;                 // tokens per tile
+constexpr int KS = 64;                     // K per stage
+constexpr int MAX_STAGES = 8;
+constexpr int CONV_WARPS = 8, EPI_WARPS = 4;
+constexpr int THREADS = (CONV_WARPS + EPI_WARPS + 2) * 32;
+constexpr int RING_BYTES = 204800;
+constexpr int SMEM_BYTES = RING_BYTES + 1024 + 512;
+constexpr unsigned FULL = 0xFFFFFFFFu;
+constexpr int MAX_SPLITS = 16;
+
+__device__ __forceinline__ void store1(float *p, float v) { *p = v; }
+__device__ __forceinline__ void store1(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
+
+struct Shape {
+    int64_t T, n, m;
+    int N;            // tokens per tile, a multiple of 16
+    int stages;
+    int nti, ntj;     // tiles over channels, tokens
+    int splits, per;  // K parts, K steps per part
+    int ks;           // K steps
+};
+
+// Work item -> (channel tile, token tile, K part): within a part, groups of 8
+// channel tiles, so that the CTAs running together share codes and tokens in L2.
+__device__ __forceinline__ void item_of(const Shape &sh, int w, int &ti, int &tj, int &z) {
+    constexpr int G = 8;
+    const int tiles = sh.nti * sh.ntj;
+    z = w / tiles;
+    const int t = w - z * tiles;
+    const int g = t / (G * sh.ntj), r0 = g * G, rows = min(G, sh.nti - r0), k = t - g * G * sh.ntj;
+    ti = r0 + k % rows;
+    tj = k / rows;
+}
+
+// Four bytes -> two fp16 pairs, eight nibbles of a word -> four pairs, less the zero point
+__device__ __forceinline__ uint32_t sub2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
+template <int WB, typename TY>
+__global__ void __launch_bounds__(THREADS, 1)
+    int8_tc_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtensorMap mapX, const Shape sh,
+                   const float *x_scale, const float *w_scale, const uint8_t *w_zero, TY *Y, float *part, int *err) {
+    constexpr int WROW = WB == 8 ? KS : KS / 2;   // bytes of a row of codes per stage
+    constexpr int W_BYTES = TM * WROW;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint64_t *full = reinterpret_cast<uint64_t *>(smem + RING_BYTES);
+    uint64_t *ready = full + MAX_STAGES;         // A slot converted
+    uint64_t *empty = ready + MAX_STAGES;        // stage and slot read by the MMAs
+    uint64_t *accf = empty + MAX_STAGES;         // [2] accumulator complete
+    uint64_t *acce = accf + 2;                   // [2] accumulator drained
+    uint64_t *done = acce + 2;
+    uint32_t *tslot = reinterpret_cast<uint32_t *>(done + 1);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(tslot + 1);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int x_bytes = sh.N * KS * 2, stage_bytes = x_bytes + W_BYTES;   // both multiples of 1024
+    const int items = sh.nti * sh.ntj * sh.splits, S = sh.stages;
+    const bool two = sh.N <= 128;                // two accumulators
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S; ++s) {
+            tc::mbar_init(tc::smem_u32(&full[s]), 1);
+            tc::mbar_init(tc::smem_u32(&ready[s]), 4);
+            tc::mbar_init(tc::smem_u32(&empty[s]), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            tc::mbar_init(tc::smem_u32(&accf[b]), 1);
+            tc::mbar_init(tc::smem_u32(&acce[b]), EPI_WARPS);
+        }
+        tc::mbar_init(tc::smem_u32(done), 1);
+        *abort_flag = 0;
+        tc::fence_barrier_init();
+        tc::prefetch_tmap(&mapW);
+        tc::prefetch_tmap(&mapX);
+    }
+    if (warp == 0) tc::tmem_alloc(tc::smem_u32(tslot), 512);
+    tc::fence_before_sync();
+    __syncthreads();
+    tc::fence_after_sync();
+    const uint32_t tmem = *tslot;
+    bool good = true;
+
+    if (warp < CONV_WARPS) {
+        // ---------------- converters: codes -> fp16 in TMEM ----------------
+        const int group = warp >> 2, row = (warp & 3) * 32 + lane;
+        const uint32_t a_base = tmem + 256u + ((uint32_t)((warp & 3) * 32) << 16);
+        int it = 0;   // stage counter over all of this CTA's items
+        bool ok = true;
+        for (int w = blockIdx.x; w < items && ok; w += gridDim.x) {
+            int ti, tj, z;
+            item_of(sh, w, ti, tj, z);
+            const int64_t gi = (int64_t)ti * TM + row;
+            const int zero = w_zero && gi < sh.m ? __ldg(w_zero + gi) : (WB == 8 ? 128 : 8);
+            // 1024 + z (and 64 + z for the upper nibble's position), exact in fp16
+            const uint32_t hz = 0x6400u + (uint32_t)zero;
+            const uint32_t base =
+                WB == 8 ? hz | hz << 16 : hz | (uint32_t)__half_as_ushort(__int2half_rn(64 + zero)) << 16;
+            const int nk = min(sh.per, sh.ks - z * sh.per);
+            for (int kk = 0; kk < nk; ++kk, ++it) {
+                if ((it & 1) != group) continue;
+                const int s = it % S;
+                const bool got = tc::mbar_wait(tc::smem_u32(&full[s]), (uint32_t)(it / S) & 1u, abort_flag);
+                if (!__all_sync(FULL, got)) {
+                    *abort_flag = 1;
+                    ok = false;
+                    break;
+                }
+                const uint8_t *src = smem + s * stage_bytes + x_bytes + row * WROW;
+                uint32_t h[32];
+#pragma unroll
+                for (int c = 0; c < WROW / 16; ++c) {
+                    // the swizzle's chunk of this row: bits 4-5 ^= bits 7-8 (bit 4 ^= bit 7)
+                    const int at = WB == 8 ? c ^ ((row >> 1) & 3) : c ^ ((row >> 2) & 1);
+                    const uint4 q = *reinterpret_cast<const uint4 *>(src + at * 16);
+                    const uint32_t v[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if constexpr (WB == 8) {
+                            h[c * 8 + i * 2] = sub2(__byte_perm(v[i], 0x64646464u, 0x4140), base);
+                            h[c * 8 + i * 2 + 1] = sub2(__byte_perm(v[i], 0x64646464u, 0x4342), base);
+                        } else {
+#pragma unroll
+                            for (int b = 0; b < 4; ++b) {
+                                const uint32_t t = __byte_perm(v[i], 0u, 0x4040 | b | b << 8);
+                                h[c * 16 + i * 4 + b] = sub2((t & 0x00F0000Fu) | 0x54006400u, base);
+                            }
+                        }
+                    }
+                }
+                tc::tmem_st_32x32b_x32(a_base + (uint32_t)(s * 32), h);
+                tc::tmem_wait_st();
+                tc::fence_before_sync();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(tc::smem_u32(&ready[s]));
+            }
+        }
+    } else if (warp < CONV_WARPS + EPI_WARPS) {
+        // ---------------- drain: accumulator -> Y or a part ----------------
+        const int quarter = warp & 3;
+        int lt = 0;
+        for (int w = blockIdx.x; w < items; w += gridDim.x, ++lt) {
+            int ti, tj, z;
+            item_of(sh, w, ti, tj, z);
+            const int b = two ? lt & 1 : 0, round = two ? lt >> 1 : lt;
+            if (good) {
+                const bool got = tc::mbar_wait(tc::smem_u32(&accf[b]), (uint32_t)round & 1u, abort_flag);
+                if (!__all_sync(FULL, got)) {
+                    *abort_flag = 1;
+                    good = false;   // this tile and the CTA's later ones are written as NaN
+                }
+            }
+            tc::fence_after_sync();
+            const int64_t gi = (int64_t)ti * TM + quarter * 32 + lane;
+            const int64_t t0 = (int64_t)tj * sh.N;
+            const float sw = gi < sh.m && !part ? __ldg(w_scale + gi) : 0.f;
+            const uint32_t src = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * 128);
+            for (int c0 = 0; c0 < sh.N; c0 += 16) {
+                uint32_t v[16];
+                if (good) {
+                    tc::tmem_ld_32x32b_x16(src + (uint32_t)c0, v);
+                    tc::tmem_wait_ld();
+                }
+                if (c0 + 16 >= sh.N && good) {
+                    tc::fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive(tc::smem_u32(&acce[b]));
+                }
+                if (gi >= sh.m) continue;
+#pragma unroll
+                for (int q = 0; q < 16; ++q) {
+                    const int64_t t = t0 + c0 + q;
+                    if (t >= sh.T) break;
+                    const float a = good ? __uint_as_float(v[q]) : __int_as_float(0x7fc00000);
+                    if (part)
+                        part[((int64_t)z * sh.T + t) * sh.m + gi] = a;
+                    else
+                        store1(Y + t * sh.m + gi, a * __ldg(x_scale + t) * sw);
+                }
+            }
+        }
+    } else if (warp == CONV_WARPS + EPI_WARPS) {
+        if (lane == 0) {
+            // ---------------- TMA producer ----------------
+            int it = 0;
+            bool ok = true;
+            for (int w = blockIdx.x; w < items && ok; w += gridDim.x) {
+                int ti, tj, z;
+                item_of(sh, w, ti, tj, z);
+                const int k0 = z * sh.per, nk = min(sh.per, sh.ks - k0);
+                for (int kk = 0; kk < nk; ++kk, ++it) {
+                    const int s = it % S;
+                    if (!tc::mbar_wait(tc::smem_u32(&empty[s]), ((uint32_t)(it / S) & 1u) ^ 1u, abort_flag)) {
+                        *abort_flag = 1;
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t fb = tc::smem_u32(&full[s]), dst = tc::smem_u32(smem + s * stage_bytes);
+                    tc::mbar_arrive_expect_tx(fb, (uint32_t)stage_bytes);
+                    tc::tma_load_2d(dst, &mapX, fb, (k0 + kk) * KS, tj * sh.N);
+                    tc::tma_load_2d(dst + x_bytes, &mapW, fb, (k0 + kk) * WROW, ti * TM);
+                }
+            }
+            // on abort, let the copies already issued land before the CTA exits
+            if (*abort_flag) {
+                int never = 0;
+                for (int k = (it > S ? it - S : 0); k < it; ++k)
+                    tc::mbar_wait(tc::smem_u32(&full[k % S]), (uint32_t)(k / S) & 1u, &never, 100000000ull);
+            }
+        }
+    } else if (lane == 0) {
+        // ---------------- MMA issuer ----------------
+        const uint32_t idesc = tc::idesc_f16_f32(TM, 0) | ((uint32_t)(sh.N >> 3) << 17);
+        int it = 0, lt = 0;
+        bool ok = true;
+        for (int w = blockIdx.x; w < items && ok; w += gridDim.x, ++lt) {
+            int ti, tj, z;
+            item_of(sh, w, ti, tj, z);
+            const int nk = min(sh.per, sh.ks - z * sh.per);
+            const int b = two ? lt & 1 : 0, round = two ? lt >> 1 : lt;
+            if (!tc::mbar_wait(tc::smem_u32(&acce[b]), ((uint32_t)round & 1u) ^ 1u, abort_flag)) {
+                *abort_flag = 1;
+                break;
+            }
+            tc::fence_after_sync();
+            const uint32_t d = tmem + (uint32_t)(b * 128);
+            for (int kk = 0; kk < nk; ++kk, ++it) {
+                const int s = it % S;
+                const uint32_t parity = (uint32_t)(it / S) & 1u;
+                if (!tc::mbar_wait(tc::smem_u32(&full[s]), parity, abort_flag) ||
+                    !tc::mbar_wait(tc::smem_u32(&ready[s]), parity, abort_flag)) {
+                    *abort_flag = 1;
+                    ok = false;
+                    break;
+                }
+                tc::fence_after_sync();
+                const uint32_t bop = tc::smem_u32(smem + s * stage_bytes), a = tmem + 256u + (uint32_t)(s * 32);
+#pragma unroll
+                for (int k = 0; k < KS / 16; ++k)
+                    tc::mma_f16_ts(d, a + k * 8, tc::smem_desc(bop + k * 32, 16, 1024, tc::SW_128B), idesc,
+                                   (kk > 0 || k > 0) ? 1u : 0u);
+                tc::mma_commit(tc::smem_u32(&empty[s]));
+            }
+            if (ok) tc::mma_commit(tc::smem_u32(&accf[b]));
+        }
+        // every MMA issued has retired before TMEM is freed
+        tc::mma_commit(tc::smem_u32(done));
+        int never = 0;
+        tc::mbar_wait(tc::smem_u32(done), 0u, &never, 100000000ull);
+    }
+    __syncwarp();
+    if (!good && lane == 0) atomicOr(err, ST_TIMEOUT);
+    tc::fence_before_sync();
+    __syncthreads();
+    if (warp == 0) tc::tmem_dealloc(tmem, 512);
+}
+
+// Y from the K parts, summed in order
+template <typename TY>
+__global__ void __launch_bounds__(256) int8_reduce_kernel(int64_t T, int64_t m, int splits, const float *part,
+                                                          const float *x_scale, const float *w_scale, TY *Y) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, count = T * m;
+    if (i >= count) return;
+    float a = part[i];
+    for (int z = 1; z < splits; ++z) a += part[z * count + i];
+    store1(Y + i, a * __ldg(x_scale + i / m) * __ldg(w_scale + i % m));
+}
+
+// Token codes -> fp16 plane of row stride ld (16 codes per thread where rows
+// are whole vectors)
+__global__ void __launch_bounds__(256) int8_plane_vec_kernel(int64_t count, const uint8_t *X, uint32_t *plane) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= count) return;
+    const uint4 q = __ldg(reinterpret_cast<const uint4 *>(X) + i);
+    const uint32_t v[4] = {q.x, q.y, q.z, q.w};
+    uint32_t h[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        h[2 * j] = sub2(__byte_perm(v[j], 0x64646464u, 0x4140), 0x64806480u);
+        h[2 * j + 1] = sub2(__byte_perm(v[j], 0x64646464u, 0x4342), 0x64806480u);
+    }
+    uint4 *o = reinterpret_cast<uint4 *>(plane) + 2 * i;
+    o[0] = make_uint4(h[0], h[1], h[2], h[3]);
+    o[1] = make_uint4(h[4], h[5], h[6], h[7]);
+}
+__global__ void __launch_bounds__(256) int8_plane_kernel(int64_t T, int64_t n, const uint8_t *X, __half *plane,
+                                                         int64_t ld) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= T * n) return;
+    plane[i / n * ld + i % n] = __int2half_rn((int)X[i] - 128);
+}
+// rows of W at a 16-byte stride
+__global__ void __launch_bounds__(256) int8_pad_kernel(int64_t m, int64_t rb, const uint8_t *W, uint8_t *out,
+                                                       int64_t ld) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= m * rb) return;
+    out[i / rb * ld + i % rb] = W[i];
+}
+
+int64_t pad8(int64_t x) { return (x + 7) / 8 * 8; }
+int64_t pad16(int64_t x) { return (x + 15) / 16 * 16; }
+int64_t row_bytes(int64_t n, int w_bits) { return w_bits == 8 ? n : (n + 1) / 2; }
+
+// Tokens per tile: as few tiles as 256 allows, evenly filled.  K parts: the
+// count whose waves over the SMs take the fewest K steps, each part at least
+// eight steps, the drain counted as four.
+Shape shape_of(int64_t T, int64_t n, int64_t m, int w_bits, int sms) {
+    Shape sh{};
+    sh.T = T;
+    sh.n = n;
+    sh.m = m;
+    sh.ntj = (int)((T + TNMAX - 1) / TNMAX);
+    sh.N = (int)std::max<int64_t>(16, ((T + sh.ntj - 1) / sh.ntj + 15) / 16 * 16);
+    sh.ntj = (int)((T + sh.N - 1) / sh.N);
+    sh.nti = ceil_div(m, TM);
+    sh.stages = std::min(MAX_STAGES, RING_BYTES / (sh.N * KS * 2 + TM * (w_bits == 8 ? KS : KS / 2)));
+    sh.ks = ceil_div(n, KS);
+    const int64_t tiles = (int64_t)sh.nti * sh.ntj;
+    int best = 1;
+    int64_t cost = INT64_MAX;
+    for (int s = 1; s <= MAX_SPLITS && (s == 1 || sh.ks / s >= 8) && (s == 1 || tiles < 2 * sms); ++s) {
+        const int64_t c = (tiles * s + sms - 1) / sms * ((sh.ks + s - 1) / s + 4) + (s > 1 ? 8 : 0);
+        if (c < cost) {
+            cost = c;
+            best = s;
+        }
+    }
+    sh.per = (sh.ks + best - 1) / best;
+    sh.splits = (sh.ks + sh.per - 1) / sh.per;
+    return sh;
+}
+
+struct ProductWs {
+    int *status;
+    __half *x;
+    uint8_t *w;
+    float *part;
+    size_t bytes;
+    ProductWs(void *ws, const Shape &sh, int w_bits) {
+        Carve c(ws);
+        const int64_t rb = row_bytes(sh.n, w_bits);
+        status = c.take<int>(64);
+        x = c.take<__half>((size_t)(sh.T * pad8(sh.n)));
+        w = c.take<uint8_t>(rb % 16 ? (size_t)(sh.m * pad16(rb)) : 0);
+        part = c.take<float>(sh.splits > 1 ? (size_t)(sh.splits * sh.T * sh.m) : 0);
+        bytes = c.off;
+    }
+};
+
+template <int WB, typename TY>
+realq_status_t tc_launch(cudaStream_t s, const Shape &sh, const CUtensorMap &mapW, const CUtensorMap &mapX,
+                         const float *xs, const float *ws, const uint8_t *wz, TY *Y, const ProductWs &b, int sms) {
+    const void *k = reinterpret_cast<const void *>(int8_tc_kernel<WB, TY>);
+    REALQ_TRY(set_smem_limit(k, SMEM_BYTES));
+    const int64_t items = (int64_t)sh.nti * sh.ntj * sh.splits;
+    {
+        Launch L("int8_product_tc", s);
+        int8_tc_kernel<WB, TY><<<(unsigned)std::min<int64_t>(items, sms), THREADS, SMEM_BYTES, s>>>(
+            mapW, mapX, sh, xs, ws, wz, Y, sh.splits > 1 ? b.part : nullptr, b.status);
+    }
+    REALQ_TRY(check_launch("int8_product_tc"));
+    if (sh.splits > 1) {
+        Launch L("int8_product_reduce", s);
+        int8_reduce_kernel<TY><<<(unsigned)((sh.T * sh.m + 255) / 256), 256, 0, s>>>(sh.T, sh.m, sh.splits, b.part, xs,
+                                                                                    ws, Y);
+    }
+    return check_launch("int8_product_reduce");
+}
+
+}  // namespace
+
+size_t int8_tc_ws_bytes(int64_t T, int64_t n, int64_t m, int w_bits, int sms) {
+    return ProductWs(nullptr, shape_of(T, n, m, w_bits, sms), w_bits).bytes;
+}
+
+
+realq_status_t int8_product_tc(cudaStream_t s, int64_t T, int64_t n, int64_t m, const uint8_t *X, const float *x_scale,
+                               const uint8_t *W, int w_bits, const float *w_scale, const uint8_t *w_zero, void *Y,
+                               realq_dtype_t y_dtype, void *ws, int sms) {
+    const Shape sh = shape_of(T, n, m, w_bits, sms);
+    const ProductWs b(ws, sh, w_bits);
+    REALQ_CUDA_TRY(cudaMemsetAsync(b.status, 0, sizeof(int), s));
+    const int64_t ldx = pad8(n), rb = row_bytes(n, w_bits);
+    {
+        Launch L("int8_product_plane", s);
+        if (n % 16 == 0 && (reinterpret_cast<uintptr_t>(X) & 15) == 0)
+            int8_plane_vec_kernel<<<(unsigned)((T * n / 16 + 255) / 256), 256, 0, s>>>(
+                T * n / 16, X, reinterpret_cast<uint32_t *>(b.x));
+        else
+            int8_plane_kernel<<<(unsigned)((T * n + 255) / 256), 256, 0, s>>>(T, n, X, b.x, ldx);
+    }
+    REALQ_TRY(check_launch("int8_product_plane"));
+    const uint8_t *w = W;
+    int64_t ldw = rb;
+    if (rb % 16) {
+        ldw = pad16(rb);
+        w = b.w;
+        Launch L("int8_product_pad", s);
+        int8_pad_kernel<<<(unsigned)((m * rb + 255) / 256), 256, 0, s>>>(m, rb, W, b.w, ldw);
+        REALQ_TRY(check_launch("int8_product_pad"));
+    }
+    CUtensorMap mapW, mapX;
+    CUresult cr = encode_tmap_2d_u8(&mapW, w, (uint64_t)rb, (uint64_t)m, (uint64_t)ldw, w_bits == 8 ? KS : KS / 2, TM,
+                                    w_bits == 8 ? 2 : 3);
+    if (cr == CUDA_SUCCESS)
+        cr = encode_tmap_2d_f16(&mapX, b.x, (uint64_t)n, (uint64_t)T, (uint64_t)ldx * 2, KS, (uint32_t)sh.N, 1);
+    if (cr != CUDA_SUCCESS) return fail(REALQ_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)cr);
+    auto run = [&](auto *y) {
+        return w_bits == 8 ? tc_launch<8>(s, sh, mapW, mapX, x_scale, w_scale, w_zero, y, b, sms)
+                           : tc_launch<4>(s, sh, mapW, mapX, x_scale, w_scale, w_zero, y, b, sms);
+    };
+    return y_dtype == REALQ_BF16 ? run(static_cast<__nv_bfloat16 *>(Y)) : run(static_cast<float *>(Y));
+}
+
+}  // namespace realq

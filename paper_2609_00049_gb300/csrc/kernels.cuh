@@ -148,6 +148,10 @@ realq_status_t checkpoint_unpack(cudaStream_t s, int64_t T, int64_t n, const int
 size_t checkpoint_grad_ws_bytes(int64_t T, int64_t m, int64_t n, realq_dtype_t dy_dtype, int sms);
 realq_status_t checkpoint_grad(cudaStream_t s, int64_t T, int64_t m, int64_t n, const void *dY, realq_dtype_t dt,
                                const int8_t *codes, const uint8_t *exps, float *dW, int accumulate, void *ws, int sms);
+size_t int8_tc_ws_bytes(int64_t T, int64_t n, int64_t m, int w_bits, int sms);
+realq_status_t int8_product_tc(cudaStream_t s, int64_t T, int64_t n, int64_t m, const uint8_t *X, const float *x_scale,
+                               const uint8_t *W, int w_bits, const float *w_scale, const uint8_t *w_zero, void *Y,
+                               realq_dtype_t y_dtype, void *ws, int sms);
 size_t int8_product_ws_bytes(int64_t T, int64_t n, int64_t m, int w_bits, int sms);
 realq_status_t int8_product(cudaStream_t s, int64_t T, int64_t n, int64_t m, const uint8_t *X, const float *x_scale,
                             const uint8_t *W, int w_bits, const float *w_scale, const uint8_t *w_zero, void *Y,
