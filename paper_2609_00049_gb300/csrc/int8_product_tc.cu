@@ -56,6 +56,19 @@ struct Shape {
     int ks;           // K steps
 };
 
+// Stage index and phase parity of a ring of S stages
+struct Ring {
+    int s = 0, S;
+    uint32_t phase = 0;
+    __device__ __forceinline__ explicit Ring(int stages) : S(stages) {}
+    __device__ __forceinline__ void next() {
+        if (++s == S) {
+            s = 0;
+            phase ^= 1u;
+        }
+    }
+};
+
 // Work item -> (channel tile, token tile, K part): within a part, groups of 8
 // channel tiles, so that the CTAs running together share codes and tokens in L2.
 __device__ __forceinline__ void item_of(const Shape &sh, int w, int &ti, int &tj, int &z) {
@@ -124,8 +137,9 @@ __global__ void __launch_bounds__(THREADS, 1)
         // ---------------- converters: codes -> fp16 in TMEM ----------------
         const int group = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t a_base = tmem + 256u + ((uint32_t)((warp & 3) * 32) << 16);
-        int it = 0;   // stage counter over all of this CTA's items
+        Ring r(S);   // over all of this CTA's items
         bool ok = true;
+        int turn = 0;
         for (int w = blockIdx.x; w < items && ok; w += gridDim.x) {
             int ti, tj, z;
             item_of(sh, w, ti, tj, z);
@@ -136,10 +150,10 @@ __global__ void __launch_bounds__(THREADS, 1)
             const uint32_t base =
                 WB == 8 ? hz | hz << 16 : hz | (uint32_t)__half_as_ushort(__int2half_rn(64 + zero)) << 16;
             const int nk = min(sh.per, sh.ks - z * sh.per);
-            for (int kk = 0; kk < nk; ++kk, ++it) {
-                if ((it & 1) != group) continue;
-                const int s = it % S;
-                const bool got = tc::mbar_wait(tc::smem_u32(&full[s]), (uint32_t)(it / S) & 1u, abort_flag);
+            for (int kk = 0; kk < nk; ++kk, r.next(), turn ^= 1) {
+                if (turn != group) continue;
+                const int s = r.s;
+                const bool got = tc::mbar_wait(tc::smem_u32(&full[s]), r.phase, abort_flag);
                 if (!__all_sync(FULL, got)) {
                     *abort_flag = 1;
                     ok = false;
@@ -221,15 +235,16 @@ __global__ void __launch_bounds__(THREADS, 1)
     } else if (warp == CONV_WARPS + EPI_WARPS) {
         if (lane == 0) {
             // ---------------- TMA producer ----------------
+            Ring r(S);
             int it = 0;
             bool ok = true;
             for (int w = blockIdx.x; w < items && ok; w += gridDim.x) {
                 int ti, tj, z;
                 item_of(sh, w, ti, tj, z);
                 const int k0 = z * sh.per, nk = min(sh.per, sh.ks - k0);
-                for (int kk = 0; kk < nk; ++kk, ++it) {
-                    const int s = it % S;
-                    if (!tc::mbar_wait(tc::smem_u32(&empty[s]), ((uint32_t)(it / S) & 1u) ^ 1u, abort_flag)) {
+                for (int kk = 0; kk < nk; ++kk, ++it, r.next()) {
+                    const int s = r.s;
+                    if (!tc::mbar_wait(tc::smem_u32(&empty[s]), r.phase ^ 1u, abort_flag)) {
                         *abort_flag = 1;
                         ok = false;
                         break;
@@ -247,43 +262,45 @@ __global__ void __launch_bounds__(THREADS, 1)
                     tc::mbar_wait(tc::smem_u32(&full[k % S]), (uint32_t)(k / S) & 1u, &never, 100000000ull);
             }
         }
-    } else if (lane == 0) {
-        // ---------------- MMA issuer ----------------
+    } else {
+        // ---------------- MMA issuer (the whole warp waits, one lane issues) ----------------
         const uint32_t idesc = tc::idesc_f16_f32(TM, 0) | ((uint32_t)(sh.N >> 3) << 17);
-        int it = 0, lt = 0;
+        const uint64_t desc0 = tc::smem_desc(tc::smem_u32(smem), 16, 1024, tc::SW_128B);
+        Ring r(S);
+        int lt = 0;
         bool ok = true;
         for (int w = blockIdx.x; w < items && ok; w += gridDim.x, ++lt) {
             int ti, tj, z;
             item_of(sh, w, ti, tj, z);
             const int nk = min(sh.per, sh.ks - z * sh.per);
             const int b = two ? lt & 1 : 0, round = two ? lt >> 1 : lt;
-            if (!tc::mbar_wait(tc::smem_u32(&acce[b]), ((uint32_t)round & 1u) ^ 1u, abort_flag)) {
-                *abort_flag = 1;
-                break;
-            }
+            ok = __all_sync(FULL, tc::mbar_wait(tc::smem_u32(&acce[b]), ((uint32_t)round & 1u) ^ 1u, abort_flag));
+            if (!ok) break;
             tc::fence_after_sync();
             const uint32_t d = tmem + (uint32_t)(b * 128);
-            for (int kk = 0; kk < nk; ++kk, ++it) {
-                const int s = it % S;
-                const uint32_t parity = (uint32_t)(it / S) & 1u;
-                if (!tc::mbar_wait(tc::smem_u32(&full[s]), parity, abort_flag) ||
-                    !tc::mbar_wait(tc::smem_u32(&ready[s]), parity, abort_flag)) {
-                    *abort_flag = 1;
-                    ok = false;
-                    break;
-                }
+            for (int kk = 0; kk < nk; ++kk, r.next()) {
+                ok = tc::mbar_wait(tc::smem_u32(&ready[r.s]), r.phase, abort_flag) &&
+                     tc::mbar_wait(tc::smem_u32(&full[r.s]), r.phase, abort_flag);
+                ok = __all_sync(FULL, ok);
+                if (!ok) break;
                 tc::fence_after_sync();
-                const uint32_t bop = tc::smem_u32(smem + s * stage_bytes), a = tmem + 256u + (uint32_t)(s * 32);
+                const uint64_t desc = desc0 + (uint32_t)(r.s * stage_bytes >> 4);
+                const uint32_t a = tmem + 256u + (uint32_t)(r.s * 32);
+                if (tc::elect_one()) {
 #pragma unroll
-                for (int k = 0; k < KS / 16; ++k)
-                    tc::mma_f16_ts(d, a + k * 8, tc::smem_desc(bop + k * 32, 16, 1024, tc::SW_128B), idesc,
-                                   (kk > 0 || k > 0) ? 1u : 0u);
-                tc::mma_commit(tc::smem_u32(&empty[s]));
+                    for (int k = 0; k < KS / 16; ++k)
+                        tc::mma_f16_ts(d, a + k * 8, desc + k * 2, idesc, (kk > 0 || k > 0) ? 1u : 0u);
+                    tc::mma_commit(tc::smem_u32(&empty[r.s]));
+                }
+                __syncwarp();
             }
-            if (ok) tc::mma_commit(tc::smem_u32(&accf[b]));
+            if (ok && tc::elect_one()) tc::mma_commit(tc::smem_u32(&accf[b]));
+            __syncwarp();
         }
+        if (!ok) *abort_flag = 1;
         // every MMA issued has retired before TMEM is freed
-        tc::mma_commit(tc::smem_u32(done));
+        if (tc::elect_one()) tc::mma_commit(tc::smem_u32(done));
+        __syncwarp();
         int never = 0;
         tc::mbar_wait(tc::smem_u32(done), 0u, &never, 100000000ull);
     }
