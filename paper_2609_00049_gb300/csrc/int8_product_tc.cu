@@ -16,12 +16,15 @@
 // which a pass over the token codes writes as fp16 to the workspace; B is a
 // K-major tile of it (128-byte swizzle).
 //
-// Roles (448 threads, one persistent CTA per SM): warps 0-7 convert, warps
-// 8-11 drain the accumulator (lane = channel, so a warp's stores of one token
-// are contiguous), warp 12 issues TMA, warp 13 the MMAs.  TMEM: columns 0-255
+// Roles (608 threads, one persistent CTA per SM): warps 0-7 convert, warps
+// 8-15 drain the accumulator (lane = channel, so a warp's stores of one token
+// are contiguous; two warps take turns at a lane quarter's 32-column blocks),
+// warps 16 and 17 issue the TMA loads of tokens and codes, warp 18 the MMAs.  TMEM: columns 0-255
 // hold the accumulator (two of them when a tile has at most 128 tokens, so that
-// a drain overlaps the next tile), 256-511 eight A slots.  One ring of stages
-// covers the codes, the tokens and the A slots.  With fewer tiles than SMs the
+// a drain overlaps the next tile), 256-511 eight A slots.  The codes have a ring
+// of their own, freed by the converters, and run ahead of the tokens, whose
+// stages (and the A slots) the MMAs free: a stage of either then covers one
+// memory latency, not the conversion as well.  With fewer tiles than SMs the
 // K range is split; the parts are summed in a fixed order.
 // Every wait is bounded; a tile whose wait gave up is written as NaN and the
 // status word gets ST_TIMEOUT.
@@ -36,9 +39,10 @@ namespace {
 constexpr int TM = 128;                    // channels per tile
 constexpr int TNMAX = 256;                 // tokens per tile
 constexpr int KS = 64;                     // K per stage
-constexpr int MAX_STAGES = 8;
-constexpr int CONV_WARPS = 8, EPI_WARPS = 4;
-constexpr int THREADS = (CONV_WARPS + EPI_WARPS + 2) * 32;
+constexpr int MAX_STAGES = 8;              // of the tokens' ring and of A in TMEM
+constexpr int MAX_WSTAGES = 16;            // of the codes' ring
+constexpr int CONV_WARPS = 8, EPI_WARPS = 8;
+constexpr int THREADS = (CONV_WARPS + EPI_WARPS + 3) * 32;
 constexpr int RING_BYTES = 204800;
 constexpr int SMEM_BYTES = RING_BYTES + 1024 + 512;
 constexpr unsigned FULL = 0xFFFFFFFFu;
@@ -50,7 +54,7 @@ __device__ __forceinline__ void store1(__nv_bfloat16 *p, float v) { *p = __float
 struct Shape {
     int64_t T, n, m;
     int N;            // tokens per tile, a multiple of 16
-    int stages;
+    int stages, wstages;   // ring lengths: tokens and A slots, codes
     int nti, ntj;     // tiles over channels, tokens
     int splits, per;  // K parts, K steps per part
     int ks;           // K steps
@@ -96,25 +100,32 @@ __global__ void __launch_bounds__(THREADS, 1)
     constexpr int W_BYTES = TM * WROW;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint64_t *full = reinterpret_cast<uint64_t *>(smem + RING_BYTES);
-    uint64_t *ready = full + MAX_STAGES;         // A slot converted
-    uint64_t *empty = ready + MAX_STAGES;        // stage and slot read by the MMAs
-    uint64_t *accf = empty + MAX_STAGES;         // [2] accumulator complete
+    uint64_t *xfull = reinterpret_cast<uint64_t *>(smem + RING_BYTES);
+    uint64_t *ready = xfull + MAX_STAGES;        // A slot converted
+    uint64_t *empty = ready + MAX_STAGES;        // tokens' stage and A slot read by the MMAs
+    uint64_t *wfull = empty + MAX_STAGES;
+    uint64_t *wempty = wfull + MAX_WSTAGES;      // codes' stage converted
+    uint64_t *accf = wempty + MAX_WSTAGES;       // [2] accumulator complete
     uint64_t *acce = accf + 2;                   // [2] accumulator drained
     uint64_t *done = acce + 2;
     uint32_t *tslot = reinterpret_cast<uint32_t *>(done + 1);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tslot + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int x_bytes = sh.N * KS * 2, stage_bytes = x_bytes + W_BYTES;   // both multiples of 1024
-    const int items = sh.nti * sh.ntj * sh.splits, S = sh.stages;
+    const int x_bytes = sh.N * KS * 2;           // a multiple of 1024, as W_BYTES
+    const int items = sh.nti * sh.ntj * sh.splits, S = sh.stages, SW = sh.wstages;
+    uint8_t *wring = smem + S * x_bytes;
     const bool two = sh.N <= 128;                // two accumulators
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
-            tc::mbar_init(tc::smem_u32(&full[s]), 1);
+            tc::mbar_init(tc::smem_u32(&xfull[s]), 1);
             tc::mbar_init(tc::smem_u32(&ready[s]), 4);
             tc::mbar_init(tc::smem_u32(&empty[s]), 1);
+        }
+        for (int s = 0; s < SW; ++s) {
+            tc::mbar_init(tc::smem_u32(&wfull[s]), 1);
+            tc::mbar_init(tc::smem_u32(&wempty[s]), 4);
         }
         for (int b = 0; b < 2; ++b) {
             tc::mbar_init(tc::smem_u32(&accf[b]), 1);
@@ -137,7 +148,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         // ---------------- converters: codes -> fp16 in TMEM ----------------
         const int group = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t a_base = tmem + 256u + ((uint32_t)((warp & 3) * 32) << 16);
-        Ring r(S);   // over all of this CTA's items
+        Ring r(S), rw(SW);   // over all of this CTA's items
         bool ok = true;
         int turn = 0;
         for (int w = blockIdx.x; w < items && ok; w += gridDim.x) {
@@ -150,16 +161,17 @@ __global__ void __launch_bounds__(THREADS, 1)
             const uint32_t base =
                 WB == 8 ? hz | hz << 16 : hz | (uint32_t)__half_as_ushort(__int2half_rn(64 + zero)) << 16;
             const int nk = min(sh.per, sh.ks - z * sh.per);
-            for (int kk = 0; kk < nk; ++kk, r.next(), turn ^= 1) {
+            for (int kk = 0; kk < nk; ++kk, r.next(), rw.next(), turn ^= 1) {
                 if (turn != group) continue;
-                const int s = r.s;
-                const bool got = tc::mbar_wait(tc::smem_u32(&full[s]), r.phase, abort_flag);
+                const bool got = tc::mbar_wait(tc::smem_u32(&wfull[rw.s]), rw.phase, abort_flag) &&
+                                 tc::mbar_wait(tc::smem_u32(&empty[r.s]), r.phase ^ 1u, abort_flag);
                 if (!__all_sync(FULL, got)) {
                     *abort_flag = 1;
                     ok = false;
                     break;
                 }
-                const uint8_t *src = smem + s * stage_bytes + x_bytes + row * WROW;
+                tc::fence_after_sync();
+                const uint8_t *src = wring + rw.s * W_BYTES + row * WROW;
                 uint32_t h[32];
 #pragma unroll
                 for (int c = 0; c < WROW / 16; ++c) {
@@ -181,21 +193,34 @@ __global__ void __launch_bounds__(THREADS, 1)
                         }
                     }
                 }
-                tc::tmem_st_32x32b_x32(a_base + (uint32_t)(s * 32), h);
+                tc::tmem_st_32x32b_x32(a_base + (uint32_t)(r.s * 32), h);
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(tc::smem_u32(&wempty[rw.s]));
                 tc::tmem_wait_st();
                 tc::fence_before_sync();
                 __syncwarp();
-                if (lane == 0) tc::mbar_arrive(tc::smem_u32(&ready[s]));
+                if (lane == 0) tc::mbar_arrive(tc::smem_u32(&ready[r.s]));
             }
         }
     } else if (warp < CONV_WARPS + EPI_WARPS) {
         // ---------------- drain: accumulator -> Y or a part ----------------
-        const int quarter = warp & 3;
+        const int quarter = warp & 3, half = (warp - CONV_WARPS) >> 2;
         int lt = 0;
         for (int w = blockIdx.x; w < items; w += gridDim.x, ++lt) {
             int ti, tj, z;
             item_of(sh, w, ti, tj, z);
             const int b = two ? lt & 1 : 0, round = two ? lt >> 1 : lt;
+            const int64_t gi = (int64_t)ti * TM + quarter * 32 + lane;
+            const int64_t t0 = (int64_t)tj * sh.N;
+            const bool mine = gi < sh.m;
+            const int nt = (int)min((int64_t)sh.N, sh.T - t0);   // tokens of this tile
+            const float sw = part ? 1.f : (mine ? __ldg(w_scale + gi) : 0.f);
+            float sx[4];                                         // of this warp's four blocks, one token to a lane
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int t = (2 * j + half) * 32 + lane;
+                sx[j] = !part && t < nt ? __ldg(x_scale + t0 + t) : 1.f;
+            }
             if (good) {
                 const bool got = tc::mbar_wait(tc::smem_u32(&accf[b]), (uint32_t)round & 1u, abort_flag);
                 if (!__all_sync(FULL, got)) {
@@ -204,62 +229,76 @@ __global__ void __launch_bounds__(THREADS, 1)
                 }
             }
             tc::fence_after_sync();
-            const int64_t gi = (int64_t)ti * TM + quarter * 32 + lane;
-            const int64_t t0 = (int64_t)tj * sh.N;
-            const float sw = gi < sh.m && !part ? __ldg(w_scale + gi) : 0.f;
             const uint32_t src = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * 128);
-            for (int c0 = 0; c0 < sh.N; c0 += 16) {
-                uint32_t v[16];
-                if (good) {
-                    tc::tmem_ld_32x32b_x16(src + (uint32_t)c0, v);
-                    tc::tmem_wait_ld();
-                }
-                if (c0 + 16 >= sh.N && good) {
-                    tc::fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) tc::mbar_arrive(tc::smem_u32(&acce[b]));
-                }
-                if (gi >= sh.m) continue;
+            const int blocks = (sh.N + 31) / 32, mine_last = (blocks - 1 - half) / 2;   // blocks 2 j + half, j <= mine_last
+            if (good && blocks <= half) {
+                tc::fence_before_sync();
+                if (lane == 0) tc::mbar_arrive(tc::smem_u32(&acce[b]));
+            }
 #pragma unroll
-                for (int q = 0; q < 16; ++q) {
-                    const int64_t t = t0 + c0 + q;
-                    if (t >= sh.T) break;
-                    const float a = good ? __uint_as_float(v[q]) : __int_as_float(0x7fc00000);
-                    if (part)
-                        part[((int64_t)z * sh.T + t) * sh.m + gi] = a;
-                    else
-                        store1(Y + t * sh.m + gi, a * __ldg(x_scale + t) * sw);
+            for (int j = 0; j < 4; ++j) {
+                const int c0 = (2 * j + half) * 32;
+                if (c0 >= sh.N) continue;
+                uint32_t v[32];
+                if (good) {
+                    // (a last block of 16 columns reads 16 more, which stay unused)
+                    tc::tmem_ld_32x32b_x32(src + (uint32_t)c0, v);
+                    if (j == mine_last) {
+                        tc::fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0) tc::mbar_arrive(tc::smem_u32(&acce[b]));
+                    }
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 32; ++q) v[q] = 0x7fc00000u;
+                }
+                const int nq = nt - c0;
+                if (part) {
+                    float *p = part + ((int64_t)z * sh.T + t0 + c0) * sh.m + gi;
+#pragma unroll
+                    for (int q = 0; q < 32; ++q, p += sh.m)
+                        if (mine && q < nq) *p = __uint_as_float(v[q]);
+                } else {
+                    TY *y = Y + (t0 + c0) * sh.m + gi;
+#pragma unroll
+                    for (int q = 0; q < 32; ++q, y += sh.m) {
+                        const float r = __uint_as_float(v[q]) * __shfl_sync(FULL, sx[j], q) * sw;
+                        if (mine && q < nq) store1(y, r);
+                    }
                 }
             }
         }
-    } else if (warp == CONV_WARPS + EPI_WARPS) {
+    } else if (warp < CONV_WARPS + EPI_WARPS + 2) {
         if (lane == 0) {
-            // ---------------- TMA producer ----------------
-            Ring r(S);
+            // ---------------- TMA producers: tokens, codes ----------------
+            const bool codes = warp == CONV_WARPS + EPI_WARPS + 1;
+            uint64_t *fulls = codes ? wfull : xfull, *empties = codes ? wempty : empty;
+            uint8_t *ring = codes ? wring : smem;
+            const int bytes = codes ? W_BYTES : x_bytes;
+            const CUtensorMap *map = codes ? &mapW : &mapX;
+            Ring r(codes ? SW : S);
             int it = 0;
             bool ok = true;
             for (int w = blockIdx.x; w < items && ok; w += gridDim.x) {
                 int ti, tj, z;
                 item_of(sh, w, ti, tj, z);
                 const int k0 = z * sh.per, nk = min(sh.per, sh.ks - k0);
-                for (int kk = 0; kk < nk; ++kk, ++it, r.next()) {
-                    const int s = r.s;
-                    if (!tc::mbar_wait(tc::smem_u32(&empty[s]), r.phase ^ 1u, abort_flag)) {
-                        *abort_flag = 1;
-                        ok = false;
-                        break;
-                    }
-                    const uint32_t fb = tc::smem_u32(&full[s]), dst = tc::smem_u32(smem + s * stage_bytes);
-                    tc::mbar_arrive_expect_tx(fb, (uint32_t)stage_bytes);
-                    tc::tma_load_2d(dst, &mapX, fb, (k0 + kk) * KS, tj * sh.N);
-                    tc::tma_load_2d(dst + x_bytes, &mapW, fb, (k0 + kk) * WROW, ti * TM);
+                const int dx = codes ? WROW : KS, y = codes ? ti * TM : tj * sh.N;
+                int x = k0 * dx;
+                for (int kk = 0; kk < nk; ++kk, ++it, r.next(), x += dx) {
+                    ok = tc::mbar_wait(tc::smem_u32(&empties[r.s]), r.phase ^ 1u, abort_flag);
+                    if (!ok) break;
+                    const uint32_t fb = tc::smem_u32(&fulls[r.s]);
+                    tc::mbar_arrive_expect_tx(fb, (uint32_t)bytes);
+                    tc::tma_load_2d(tc::smem_u32(ring + r.s * bytes), map, fb, x, y);
                 }
             }
             // on abort, let the copies already issued land before the CTA exits
-            if (*abort_flag) {
+            if (!ok || *abort_flag) {
+                *abort_flag = 1;
                 int never = 0;
-                for (int k = (it > S ? it - S : 0); k < it; ++k)
-                    tc::mbar_wait(tc::smem_u32(&full[k % S]), (uint32_t)(k / S) & 1u, &never, 100000000ull);
+                for (int k = (it > r.S ? it - r.S : 0); k < it; ++k)
+                    tc::mbar_wait(tc::smem_u32(&fulls[k % r.S]), (uint32_t)(k / r.S) & 1u, &never, 100000000ull);
             }
         }
     } else {
@@ -280,11 +319,11 @@ __global__ void __launch_bounds__(THREADS, 1)
             const uint32_t d = tmem + (uint32_t)(b * 128);
             for (int kk = 0; kk < nk; ++kk, r.next()) {
                 ok = tc::mbar_wait(tc::smem_u32(&ready[r.s]), r.phase, abort_flag) &&
-                     tc::mbar_wait(tc::smem_u32(&full[r.s]), r.phase, abort_flag);
+                     tc::mbar_wait(tc::smem_u32(&xfull[r.s]), r.phase, abort_flag);
                 ok = __all_sync(FULL, ok);
                 if (!ok) break;
                 tc::fence_after_sync();
-                const uint64_t desc = desc0 + (uint32_t)(r.s * stage_bytes >> 4);
+                const uint64_t desc = desc0 + (uint32_t)(r.s * x_bytes >> 4);
                 const uint32_t a = tmem + 256u + (uint32_t)(r.s * 32);
                 if (tc::elect_one()) {
 #pragma unroll
@@ -369,7 +408,9 @@ Shape shape_of(int64_t T, int64_t n, int64_t m, int w_bits, int sms) {
     sh.N = (int)std::max<int64_t>(16, ((T + sh.ntj - 1) / sh.ntj + 15) / 16 * 16);
     sh.ntj = (int)((T + sh.N - 1) / sh.N);
     sh.nti = ceil_div(m, TM);
-    sh.stages = std::min(MAX_STAGES, RING_BYTES / (sh.N * KS * 2 + TM * (w_bits == 8 ? KS : KS / 2)));
+    const int xb = sh.N * KS * 2, wb = TM * (w_bits == 8 ? KS : KS / 2);
+    sh.stages = std::min(MAX_STAGES, RING_BYTES / (xb + wb));
+    sh.wstages = std::min(MAX_WSTAGES, (RING_BYTES - sh.stages * xb) / wb);
     sh.ks = ceil_div(n, KS);
     const int64_t tiles = (int64_t)sh.nti * sh.ntj;
     int best = 1;
