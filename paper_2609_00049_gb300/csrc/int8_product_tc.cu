@@ -24,8 +24,9 @@
 // a drain overlaps the next tile), 256-511 eight A slots.  The codes have a ring
 // of their own, freed by the converters, and run ahead of the tokens, whose
 // stages (and the A slots) the MMAs free: a stage of either then covers one
-// memory latency, not the conversion as well.  With fewer tiles than SMs the
-// K range is split; the parts are summed in a fixed order.
+// memory latency, not the conversion as well.  Tiles beyond whole
+// waves over the SMs have their K range split; a second pass adds the
+// parts in their order.
 // Every wait is bounded; a tile whose wait gave up is written as NaN and the
 // status word gets ST_TIMEOUT.
 #include "kernels.cuh"
@@ -56,8 +57,16 @@ struct Shape {
     int N;            // tokens per tile, a multiple of 16
     int stages, wstages;   // ring lengths: tokens and A slots, codes
     int nti, ntj;     // tiles over channels, tokens
-    int splits, per;  // K parts, K steps per part
+    int whole;        // tiles that keep their K range; the others are split
+    int splits, per;  // K parts of those, K steps per part
     int ks;           // K steps
+    int items;
+};
+
+struct Item {
+    int ti, tj;       // channel tile, token tile
+    int k0, nk;       // K steps
+    int slot, z;      // split tiles: number among them and part (slot < 0: whole)
 };
 
 // Stage index and phase parity of a ring of S stages
@@ -73,16 +82,30 @@ struct Ring {
     }
 };
 
-// Work item -> (channel tile, token tile, K part): within a part, groups of 8
-// channel tiles, so that the CTAs running together share codes and tokens in L2.
-__device__ __forceinline__ void item_of(const Shape &sh, int w, int &ti, int &tj, int &z) {
+// Work item w: first the whole tiles, then the parts of the others (all first
+// parts, all second parts, ...).  Tiles go in groups of 8 channel tiles, so that
+// the CTAs running together share codes and tokens in L2.
+__device__ __forceinline__ Item item_of(const Shape &sh, int w) {
     constexpr int G = 8;
-    const int tiles = sh.nti * sh.ntj;
-    z = w / tiles;
-    const int t = w - z * tiles;
+    Item it;
+    int t = w;
+    if (w < sh.whole) {
+        it.k0 = 0;
+        it.nk = sh.ks;
+        it.slot = -1;
+        it.z = 0;
+    } else {
+        const int cut = sh.nti * sh.ntj - sh.whole;
+        it.z = (w - sh.whole) / cut;
+        it.slot = w - sh.whole - it.z * cut;
+        it.k0 = it.z * sh.per;
+        it.nk = min(sh.per, sh.ks - it.k0);
+        t = sh.whole + it.slot;
+    }
     const int g = t / (G * sh.ntj), r0 = g * G, rows = min(G, sh.nti - r0), k = t - g * G * sh.ntj;
-    ti = r0 + k % rows;
-    tj = k / rows;
+    it.ti = r0 + k % rows;
+    it.tj = k / rows;
+    return it;
 }
 
 // Four bytes -> two fp16 pairs, eight nibbles of a word -> four pairs, less the zero point
@@ -113,7 +136,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int x_bytes = sh.N * KS * 2;           // a multiple of 1024, as W_BYTES
-    const int items = sh.nti * sh.ntj * sh.splits, S = sh.stages, SW = sh.wstages;
+    const int items = sh.items, S = sh.stages, SW = sh.wstages;
     uint8_t *wring = smem + S * x_bytes;
     const bool two = sh.N <= 128;                // two accumulators
 
@@ -152,16 +175,14 @@ __global__ void __launch_bounds__(THREADS, 1)
         bool ok = true;
         int turn = 0;
         for (int w = blockIdx.x; w < items && ok; w += gridDim.x) {
-            int ti, tj, z;
-            item_of(sh, w, ti, tj, z);
-            const int64_t gi = (int64_t)ti * TM + row;
+            const Item im = item_of(sh, w);
+            const int64_t gi = (int64_t)im.ti * TM + row;
             const int zero = w_zero && gi < sh.m ? __ldg(w_zero + gi) : (WB == 8 ? 128 : 8);
             // 1024 + z (and 64 + z for the upper nibble's position), exact in fp16
             const uint32_t hz = 0x6400u + (uint32_t)zero;
             const uint32_t base =
                 WB == 8 ? hz | hz << 16 : hz | (uint32_t)__half_as_ushort(__int2half_rn(64 + zero)) << 16;
-            const int nk = min(sh.per, sh.ks - z * sh.per);
-            for (int kk = 0; kk < nk; ++kk, r.next(), rw.next(), turn ^= 1) {
+            for (int kk = 0; kk < im.nk; ++kk, r.next(), rw.next(), turn ^= 1) {
                 if (turn != group) continue;
                 const bool got = tc::mbar_wait(tc::smem_u32(&wfull[rw.s]), rw.phase, abort_flag) &&
                                  tc::mbar_wait(tc::smem_u32(&empty[r.s]), r.phase ^ 1u, abort_flag);
@@ -207,20 +228,24 @@ __global__ void __launch_bounds__(THREADS, 1)
         const int quarter = warp & 3, half = (warp - CONV_WARPS) >> 2;
         int lt = 0;
         for (int w = blockIdx.x; w < items; w += gridDim.x, ++lt) {
-            int ti, tj, z;
-            item_of(sh, w, ti, tj, z);
+            const Item im = item_of(sh, w);
+            const bool cut = im.slot >= 0;
             const int b = two ? lt & 1 : 0, round = two ? lt >> 1 : lt;
-            const int64_t gi = (int64_t)ti * TM + quarter * 32 + lane;
-            const int64_t t0 = (int64_t)tj * sh.N;
+            const int64_t gi = (int64_t)im.ti * TM + quarter * 32 + lane;
+            const int64_t t0 = (int64_t)im.tj * sh.N;
             const bool mine = gi < sh.m;
             const int nt = (int)min((int64_t)sh.N, sh.T - t0);   // tokens of this tile
-            const float sw = part ? 1.f : (mine ? __ldg(w_scale + gi) : 0.f);
+            const float sw = mine ? __ldg(w_scale + gi) : 0.f;
             float sx[4];                                         // of this warp's four blocks, one token to a lane
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int t = (2 * j + half) * 32 + lane;
-                sx[j] = !part && t < nt ? __ldg(x_scale + t0 + t) : 1.f;
+                sx[j] = t < nt ? __ldg(x_scale + t0 + t) : 0.f;
             }
+            const int ncut = sh.nti * sh.ntj - sh.whole;
+            auto part_of = [&](int z) {   // this lane's channel of a part: tokens TM apart
+                return part + ((int64_t)z * ncut + im.slot) * sh.N * TM + quarter * 32 + lane;
+            };
             if (good) {
                 const bool got = tc::mbar_wait(tc::smem_u32(&accf[b]), (uint32_t)round & 1u, abort_flag);
                 if (!__all_sync(FULL, got)) {
@@ -253,11 +278,11 @@ __global__ void __launch_bounds__(THREADS, 1)
                     for (int q = 0; q < 32; ++q) v[q] = 0x7fc00000u;
                 }
                 const int nq = nt - c0;
-                if (part) {
-                    float *p = part + ((int64_t)z * sh.T + t0 + c0) * sh.m + gi;
+                if (cut) {
+                    float *p = part_of(im.z) + c0 * TM;
 #pragma unroll
-                    for (int q = 0; q < 32; ++q, p += sh.m)
-                        if (mine && q < nq) *p = __uint_as_float(v[q]);
+                    for (int q = 0; q < 32; ++q)
+                        if (q < nq) p[q * TM] = __uint_as_float(v[q]);
                 } else {
                     TY *y = Y + (t0 + c0) * sh.m + gi;
 #pragma unroll
@@ -280,12 +305,10 @@ __global__ void __launch_bounds__(THREADS, 1)
             int it = 0;
             bool ok = true;
             for (int w = blockIdx.x; w < items && ok; w += gridDim.x) {
-                int ti, tj, z;
-                item_of(sh, w, ti, tj, z);
-                const int k0 = z * sh.per, nk = min(sh.per, sh.ks - k0);
-                const int dx = codes ? WROW : KS, y = codes ? ti * TM : tj * sh.N;
-                int x = k0 * dx;
-                for (int kk = 0; kk < nk; ++kk, ++it, r.next(), x += dx) {
+                const Item im = item_of(sh, w);
+                const int dx = codes ? WROW : KS, y = codes ? im.ti * TM : im.tj * sh.N;
+                int x = im.k0 * dx;
+                for (int kk = 0; kk < im.nk; ++kk, ++it, r.next(), x += dx) {
                     ok = tc::mbar_wait(tc::smem_u32(&empties[r.s]), r.phase ^ 1u, abort_flag);
                     if (!ok) break;
                     const uint32_t fb = tc::smem_u32(&fulls[r.s]);
@@ -309,15 +332,13 @@ __global__ void __launch_bounds__(THREADS, 1)
         int lt = 0;
         bool ok = true;
         for (int w = blockIdx.x; w < items && ok; w += gridDim.x, ++lt) {
-            int ti, tj, z;
-            item_of(sh, w, ti, tj, z);
-            const int nk = min(sh.per, sh.ks - z * sh.per);
+            const Item im = item_of(sh, w);
             const int b = two ? lt & 1 : 0, round = two ? lt >> 1 : lt;
             ok = __all_sync(FULL, tc::mbar_wait(tc::smem_u32(&acce[b]), ((uint32_t)round & 1u) ^ 1u, abort_flag));
             if (!ok) break;
             tc::fence_after_sync();
             const uint32_t d = tmem + (uint32_t)(b * 128);
-            for (int kk = 0; kk < nk; ++kk, r.next()) {
+            for (int kk = 0; kk < im.nk; ++kk, r.next()) {
                 ok = tc::mbar_wait(tc::smem_u32(&ready[r.s]), r.phase, abort_flag) &&
                      tc::mbar_wait(tc::smem_u32(&xfull[r.s]), r.phase, abort_flag);
                 ok = __all_sync(FULL, ok);
@@ -350,21 +371,40 @@ __global__ void __launch_bounds__(THREADS, 1)
     if (warp == 0) tc::tmem_dealloc(tmem, 512);
 }
 
-// Y from the K parts, summed in order
+// The split tiles: parts added in their order, scaled and stored.  A block takes
+// 8 tokens of a tile, a thread four neighbouring channels.
 template <typename TY>
-__global__ void __launch_bounds__(256) int8_reduce_kernel(int64_t T, int64_t m, int splits, const float *part,
-                                                          const float *x_scale, const float *w_scale, TY *Y) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, count = T * m;
-    if (i >= count) return;
-    float a = part[i];
-    for (int z = 1; z < splits; ++z) a += part[z * count + i];
-    store1(Y + i, a * __ldg(x_scale + i / m) * __ldg(w_scale + i % m));
+__global__ void __launch_bounds__(256) int8_reduce_kernel(const Shape sh, const float *part, const float *x_scale,
+                                                          const float *w_scale, TY *Y) {
+    const int cut = sh.nti * sh.ntj - sh.whole, slot = blockIdx.x;
+    const Item im = item_of(sh, sh.whole + slot);
+    const int t = blockIdx.y * 8 + (threadIdx.x >> 5), c = (threadIdx.x & 31) * 4;
+    const int64_t tok = (int64_t)im.tj * sh.N + t, i = (int64_t)im.ti * TM + c;
+    if (t >= sh.N || tok >= sh.T || i >= sh.m) return;
+    const float4 *p = reinterpret_cast<const float4 *>(part + ((int64_t)slot * sh.N + t) * TM + c);
+    const int64_t step = (int64_t)cut * sh.N * TM / 4;
+    float4 a = __ldg(p);
+#pragma unroll 4
+    for (int z = 1; z < sh.splits; ++z) {
+        const float4 b = __ldg(p + z * step);
+        a.x += b.x;
+        a.y += b.y;
+        a.z += b.z;
+        a.w += b.w;
+    }
+    const float sx = __ldg(x_scale + tok), v[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (i + k < sh.m) store1(Y + tok * sh.m + i + k, v[k] * sx * __ldg(w_scale + i + k));
 }
 
 // Token codes -> fp16 plane of row stride ld (16 codes per thread where rows
 // are whole vectors)
-__global__ void __launch_bounds__(256) int8_plane_vec_kernel(int64_t count, const uint8_t *X, uint32_t *plane) {
+// (both also clear the status word)
+__global__ void __launch_bounds__(256) int8_plane_vec_kernel(int64_t count, const uint8_t *X, uint32_t *plane,
+                                                             int *status) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i == 0) *status = 0;
     if (i >= count) return;
     const uint4 q = __ldg(reinterpret_cast<const uint4 *>(X) + i);
     const uint32_t v[4] = {q.x, q.y, q.z, q.w};
@@ -379,8 +419,9 @@ __global__ void __launch_bounds__(256) int8_plane_vec_kernel(int64_t count, cons
     o[1] = make_uint4(h[4], h[5], h[6], h[7]);
 }
 __global__ void __launch_bounds__(256) int8_plane_kernel(int64_t T, int64_t n, const uint8_t *X, __half *plane,
-                                                         int64_t ld) {
+                                                         int64_t ld, int *status) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i == 0) *status = 0;
     if (i >= T * n) return;
     plane[i / n * ld + i % n] = __int2half_rn((int)X[i] - 128);
 }
@@ -396,9 +437,11 @@ int64_t pad8(int64_t x) { return (x + 7) / 8 * 8; }
 int64_t pad16(int64_t x) { return (x + 15) / 16 * 16; }
 int64_t row_bytes(int64_t n, int w_bits) { return w_bits == 8 ? n : (n + 1) / 2; }
 
-// Tokens per tile: as few tiles as 256 allows, evenly filled.  K parts: the
-// count whose waves over the SMs take the fewest K steps, each part at least
-// eight steps, the drain counted as four.
+// Tokens per tile: as few tiles as 256 allows, evenly filled.  Tiles that fill
+// whole waves over the SMs keep their K range; the rest is cut into the count of
+// parts that is estimated the fastest, in cycles: a K step takes 2 N (the MMAs)
+// but at least 360 (its codes from HBM), a tile's start and drain 1500, the
+// pass over the parts 5000 and the parts' bytes 3400 to a cycle, twice.
 Shape shape_of(int64_t T, int64_t n, int64_t m, int w_bits, int sms) {
     Shape sh{};
     sh.T = T;
@@ -412,11 +455,13 @@ Shape shape_of(int64_t T, int64_t n, int64_t m, int w_bits, int sms) {
     sh.stages = std::min(MAX_STAGES, RING_BYTES / (xb + wb));
     sh.wstages = std::min(MAX_WSTAGES, (RING_BYTES - sh.stages * xb) / wb);
     sh.ks = ceil_div(n, KS);
-    const int64_t tiles = (int64_t)sh.nti * sh.ntj;
+    const int64_t tiles = (int64_t)sh.nti * sh.ntj, rest = tiles % sms;
     int best = 1;
     int64_t cost = INT64_MAX;
-    for (int s = 1; s <= MAX_SPLITS && (s == 1 || sh.ks / s >= 8) && (s == 1 || tiles < 2 * sms); ++s) {
-        const int64_t c = (tiles * s + sms - 1) / sms * ((sh.ks + s - 1) / s + 4) + (s > 1 ? 8 : 0);
+    for (int s = 1; s <= MAX_SPLITS && (s == 1 || sh.ks / s >= 4) && rest > 0; ++s) {
+        const int64_t step = std::max(2 * sh.N, 360);
+        const int64_t c = (rest * s + sms - 1) / sms * ((sh.ks + s - 1) / s * step + 1500) +
+                          (s > 1 ? 5000 + 2 * rest * s * sh.N * TM * 4 / 3400 : 0);
         if (c < cost) {
             cost = c;
             best = s;
@@ -424,6 +469,8 @@ Shape shape_of(int64_t T, int64_t n, int64_t m, int w_bits, int sms) {
     }
     sh.per = (sh.ks + best - 1) / best;
     sh.splits = (sh.ks + sh.per - 1) / sh.per;
+    sh.whole = (int)(sh.splits > 1 ? tiles - rest : tiles);
+    sh.items = (int)(sh.whole + (tiles - sh.whole) * sh.splits);
     return sh;
 }
 
@@ -436,10 +483,11 @@ struct ProductWs {
     ProductWs(void *ws, const Shape &sh, int w_bits) {
         Carve c(ws);
         const int64_t rb = row_bytes(sh.n, w_bits);
+        const int64_t cut = sh.splits > 1 ? (int64_t)sh.nti * sh.ntj - sh.whole : 0;
         status = c.take<int>(64);
         x = c.take<__half>((size_t)(sh.T * pad8(sh.n)));
         w = c.take<uint8_t>(rb % 16 ? (size_t)(sh.m * pad16(rb)) : 0);
-        part = c.take<float>(sh.splits > 1 ? (size_t)(sh.splits * sh.T * sh.m) : 0);
+        part = c.take<float>((size_t)(cut * sh.splits * sh.N * TM));
         bytes = c.off;
     }
 };
@@ -449,17 +497,16 @@ realq_status_t tc_launch(cudaStream_t s, const Shape &sh, const CUtensorMap &map
                          const float *xs, const float *ws, const uint8_t *wz, TY *Y, const ProductWs &b, int sms) {
     const void *k = reinterpret_cast<const void *>(int8_tc_kernel<WB, TY>);
     REALQ_TRY(set_smem_limit(k, SMEM_BYTES));
-    const int64_t items = (int64_t)sh.nti * sh.ntj * sh.splits;
     {
         Launch L("int8_product_tc", s);
-        int8_tc_kernel<WB, TY><<<(unsigned)std::min<int64_t>(items, sms), THREADS, SMEM_BYTES, s>>>(
-            mapW, mapX, sh, xs, ws, wz, Y, sh.splits > 1 ? b.part : nullptr, b.status);
+        int8_tc_kernel<WB, TY><<<(unsigned)std::min(sh.items, sms), THREADS, SMEM_BYTES, s>>>(
+            mapW, mapX, sh, xs, ws, wz, Y, b.part, b.status);
     }
     REALQ_TRY(check_launch("int8_product_tc"));
     if (sh.splits > 1) {
         Launch L("int8_product_reduce", s);
-        int8_reduce_kernel<TY><<<(unsigned)((sh.T * sh.m + 255) / 256), 256, 0, s>>>(sh.T, sh.m, sh.splits, b.part, xs,
-                                                                                    ws, Y);
+        int8_reduce_kernel<TY><<<dim3((unsigned)(sh.nti * sh.ntj - sh.whole), (unsigned)((sh.N + 7) / 8)), 256, 0, s>>>(
+            sh, b.part, xs, ws, Y);
     }
     return check_launch("int8_product_reduce");
 }
@@ -476,15 +523,14 @@ realq_status_t int8_product_tc(cudaStream_t s, int64_t T, int64_t n, int64_t m, 
                                realq_dtype_t y_dtype, void *ws, int sms) {
     const Shape sh = shape_of(T, n, m, w_bits, sms);
     const ProductWs b(ws, sh, w_bits);
-    REALQ_CUDA_TRY(cudaMemsetAsync(b.status, 0, sizeof(int), s));
     const int64_t ldx = pad8(n), rb = row_bytes(n, w_bits);
     {
         Launch L("int8_product_plane", s);
         if (n % 16 == 0 && (reinterpret_cast<uintptr_t>(X) & 15) == 0)
             int8_plane_vec_kernel<<<(unsigned)((T * n / 16 + 255) / 256), 256, 0, s>>>(
-                T * n / 16, X, reinterpret_cast<uint32_t *>(b.x));
+                T * n / 16, X, reinterpret_cast<uint32_t *>(b.x), b.status);
         else
-            int8_plane_kernel<<<(unsigned)((T * n + 255) / 256), 256, 0, s>>>(T, n, X, b.x, ldx);
+            int8_plane_kernel<<<(unsigned)((T * n + 255) / 256), 256, 0, s>>>(T, n, X, b.x, ldx, b.status);
     }
     REALQ_TRY(check_launch("int8_product_plane"));
     const uint8_t *w = W;
