@@ -134,43 +134,46 @@ __global__ void __launch_bounds__(THREADS, 1)
             }
         }
     } else if (warp == DRAIN_WARPS + 1) {
-        if (lane == 0) {
-            // ---------------- MMA issuer ----------------
-            for (int c = 0; c < nch && !*abort_flag; ++c) {
-                const int b = c & 1;
-                if (c >= 2 && !tc::mbar_wait(tc::smem_u32(&acce[b]), (uint32_t)((c >> 1) - 1) & 1u, abort_flag)) {
-                    *abort_flag = 1;
-                    break;
-                }
+        // ---------------- MMA issuer (the whole warp waits, one lane issues) ----------------
+        const uint64_t desc0 = tc::smem_desc(tc::smem_u32(smem), BOX_BYTES, 1024, tc::SW_128B);
+        int s = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int c = 0; c < nch && ok; ++c) {
+            const int b = c & 1;
+            if (c >= 2) {
+                ok = __all_sync(FULL, tc::mbar_wait(tc::smem_u32(&acce[b]), (uint32_t)((c >> 1) - 1) & 1u, abort_flag));
+                if (!ok) break;
+            }
+            tc::fence_after_sync();
+            const uint32_t d = tmem + (uint32_t)(b * TN);
+            const int cnt = min(CHUNK_STAGES, nk - c * CHUNK_STAGES);
+            for (int i = 0; i < cnt; ++i) {
+                ok = __all_sync(FULL, tc::mbar_wait(tc::smem_u32(&full[s]), phase, abort_flag));
+                if (!ok) break;
                 tc::fence_after_sync();
-                const uint32_t d = tmem + (uint32_t)(b * TN);
-                const int it_end = min(nk, (c + 1) * CHUNK_STAGES);
-                for (int it = c * CHUNK_STAGES; it < it_end; ++it) {
-                    const int s = it % STAGES;
-                    const uint32_t r = (uint32_t)(it / STAGES);
-                    if (!tc::mbar_wait(tc::smem_u32(&full[s]), r & 1u, abort_flag)) {
-                        *abort_flag = 1;
-                        break;
-                    }
-                    tc::fence_after_sync();
-                    const uint32_t a = tc::smem_u32(smem + s * STAGE_BYTES);
-                    const uint32_t bop = a + A_BYTES;
-                    const bool first = it == c * CHUNK_STAGES;
+                const uint64_t da = desc0 + (uint32_t)(s * STAGE_BYTES >> 4), db = da + (A_BYTES >> 4);
+                if (tc::elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < KSTAGE / 16; ++k) {
-                        const uint64_t da = tc::smem_desc(a + k * 2048, BOX_BYTES, 1024, tc::SW_128B);
-                        const uint64_t db = tc::smem_desc(bop + k * 2048, BOX_BYTES, 1024, tc::SW_128B);
-                        tc::mma_bf16_ss(d, da, db, IDESC, (first && k == 0) ? 0u : 1u);
-                    }
+                    for (int k = 0; k < KSTAGE / 16; ++k)
+                        tc::mma_bf16_ss(d, da + k * (2048 >> 4), db + k * (2048 >> 4), IDESC, (i > 0 || k > 0) ? 1u : 0u);
                     tc::mma_commit(tc::smem_u32(&empty[s]));
                 }
-                tc::mma_commit(tc::smem_u32(&accf[b]));
+                __syncwarp();
+                if (++s == STAGES) {
+                    s = 0;
+                    phase ^= 1u;
+                }
             }
-            // every MMA issued has retired before TMEM is freed
-            tc::mma_commit(tc::smem_u32(done));
-            int never = 0;
-            tc::mbar_wait(tc::smem_u32(done), 0u, &never, 100000000ull);
+            if (ok && tc::elect_one()) tc::mma_commit(tc::smem_u32(&accf[b]));
+            __syncwarp();
         }
+        if (!ok) *abort_flag = 1;
+        // every MMA issued has retired before TMEM is freed
+        if (tc::elect_one()) tc::mma_commit(tc::smem_u32(done));
+        __syncwarp();
+        int never = 0;
+        tc::mbar_wait(tc::smem_u32(done), 0u, &never, 100000000ull);
     } else {
         // ------- drain warps: TMEM chunk -> fp32 registers (lane quarter, column half) -------
         const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
@@ -230,17 +233,36 @@ __global__ void __launch_bounds__(256) weight_grad_reduce(int64_t count, int spl
 }
 
 // X̂ as a bf16 plane of row stride ldx (columns from n on are not written and
-// lie outside the tensor map).
+// lie outside the tensor map).  A thread unpacks 16 values (half a block) where
+// rows are whole blocks, else a warp a block.
+__device__ __forceinline__ float step_of(uint32_t b) {
+    if (b == 255u) return __int_as_float(0x7FC00000);
+    return __uint_as_float(b >= 7u ? (b - 6u) << 23 : 1u << (b + 16u));
+}
+__global__ void __launch_bounds__(256) unpack_plane_vec_kernel(int64_t count, const uint4 *codes, const uint8_t *exps,
+                                                               uint4 *X) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= count) return;
+    const uint4 q = __ldg(codes + i);
+    const float s = step_of(__ldg(exps + (i >> 1)));
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    uint32_t h[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {   // (bf16 numbers: the upper halves are exact)
+        const float lo = (float)(int8_t)(w[k >> 1] >> (16 * (k & 1))) * s;
+        const float hi = (float)(int8_t)(w[k >> 1] >> (16 * (k & 1) + 8)) * s;
+        h[k] = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
+    }
+    X[2 * i] = make_uint4(h[0], h[1], h[2], h[3]);
+    X[2 * i + 1] = make_uint4(h[4], h[5], h[6], h[7]);
+}
 __global__ void __launch_bounds__(256) unpack_plane_kernel(int64_t T, int64_t n, int64_t nb, const int8_t *codes,
                                                            const uint8_t *exps, __nv_bfloat16 *X, int64_t ldx) {
     const int lane = threadIdx.x & 31;
     const int64_t w = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 5;
     if (w >= T * nb) return;
     const int64_t t = w / nb, c = (w % nb) * 32 + lane;
-    const uint32_t b = exps[w];
-    const float step = b == 255u ? __int_as_float(0x7FC00000)
-                                 : __uint_as_float(b >= 7u ? (b - 6u) << 23 : 1u << (b + 16u));
-    if (c < n) X[t * ldx + c] = __float2bfloat16_rn((float)codes[t * n + c] * step);
+    if (c < n) X[t * ldx + c] = __float2bfloat16_rn((float)codes[t * n + c] * step_of(exps[w]));
 }
 
 // dY's planes: bf16 copied to an aligned row stride, fp32 as three bf16 planes
@@ -307,7 +329,11 @@ realq_status_t checkpoint_grad(cudaStream_t s, int64_t T, int64_t m, int64_t n, 
     const int64_t nb = (n + 31) / 32, ldx = pad8(n);
     {
         Launch L("checkpoint_grad_unpack", s);
-        unpack_plane_kernel<<<(unsigned)((T * nb * 32 + 255) / 256), 256, 0, s>>>(T, n, nb, codes, exps, w.x, ldx);
+        if (n % 32 == 0 && (reinterpret_cast<uintptr_t>(codes) & 15) == 0)
+            unpack_plane_vec_kernel<<<(unsigned)((T * n / 16 + 255) / 256), 256, 0, s>>>(
+                T * n / 16, reinterpret_cast<const uint4 *>(codes), exps, reinterpret_cast<uint4 *>(w.x));
+        else
+            unpack_plane_kernel<<<(unsigned)((T * nb * 32 + 255) / 256), 256, 0, s>>>(T, n, nb, codes, exps, w.x, ldx);
     }
     REALQ_TRY(check_launch("checkpoint_grad_unpack"));
     const bool direct = dt == REALQ_BF16 && m % 8 == 0;

@@ -6,237 +6,317 @@
 // and the result is rounded once to Y's type.
 //
 // Streaming kernel (few tokens): bound by reading the weight codes once from
-// HBM.  A warp owns R rows of W and up to eight tokens; each lane multiplies
-// 16 bytes of codes at a time with dp4a, unsigned weight codes times signed
-// token codes, exact in 32-bit integers; the zero point enters once per row:
-// sum_j (w - z) x = sum_j w x - z sum_j x.  Integer sums do not depend on their
-// order, so the warps of a row are joined through shared memory in any.
+// HBM.  A warp takes RT x 16 channels and all tokens (NT x 8) over a share of K
+// with mma.sync m16n8k16 in fp16 (dp4a needs no conversion, but runs at 16 lanes
+// a cycle on an SM here: from four tokens on it took longer than the codes' way
+// from HBM).  The order of K inside the product is free as long as both operands
+// share it, so a lane reads 16 bytes of codes of a channel at a time and uses
+// them where they are:
+//   - an unsigned code c in the low mantissa bits of an fp16 is the subnormal
+//     c 2^-24, so weight codes become A with one byte permute per pair, nibbles
+//     with one mask per pair (upper nibbles read as c 2^-20);
+//   - the tokens' codes become fp16 whole numbers x (those that meet upper
+//     nibbles x / 16), exactly;
+//   - the zero point enters once: sum (c - z) x = sum c x - z sum x, where an A
+//     of ones gives sum x on the way.
+// Products and sums are whole multiples of 2^-24 and exact while below 2^24 of
+// them; the sums are moved to 32-bit integers before they can get there
+// (FLUSH), so the result is the exact integer sum whatever the codes.  The
+// eight warps of a CTA, and up to eight CTAs of a cluster where channels alone
+// do not fill the SMs evenly, add their shares of K as integers.
+#include <cooperative_groups.h>
+
+#include <algorithm>
+
 #include "kernels.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace realq {
 namespace {
 
-constexpr unsigned FULL = 0xFFFFFFFFu;
-constexpr int SW = 8;   // warps of a streaming CTA
+constexpr int SW = 8;             // warps of a CTA
+constexpr int MAX_CLUSTER = 8;
 
-__device__ __forceinline__ int dp4a_us(uint32_t a, uint32_t b, int c) {   // unsigned a, signed b
-    int d;
-    asm("dp4a.u32.s32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-    return d;
-}
 __device__ __forceinline__ void store1(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store1(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 
-// Four code bytes at any address inside [lo, hi): two aligned words where they
-// lie inside, else single bytes.
-__device__ __forceinline__ uint32_t load_word(const uint8_t *p, const uint8_t *lo, const uint8_t *hi) {
+__device__ __forceinline__ uint32_t sub2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// 16 bytes at any address, those from `hi` on zero: aligned words where they
+// lie inside [lo, hi), else single bytes
+__device__ __forceinline__ uint4 load16(const uint8_t *p, const uint8_t *lo, const uint8_t *hi) {
     const uint32_t mis = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 3);
     const uint8_t *a = p - mis;
-    if (mis == 0 && p + 4 <= hi) return __ldg(reinterpret_cast<const uint32_t *>(p));
-    if (a >= lo && a + 8 <= hi) {
-        const uint32_t w0 = __ldg(reinterpret_cast<const uint32_t *>(a));
-        const uint32_t w1 = __ldg(reinterpret_cast<const uint32_t *>(a) + 1);
-        return __funnelshift_r(w0, w1, 8 * mis);
-    }
-    uint32_t w = 0;
+    uint32_t v[4] = {0, 0, 0, 0};
+    if (a >= lo && a + 20 <= hi) {
+        uint32_t w[5];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (p + i < hi) w |= (uint32_t)__ldg(p + i) << (8 * i);
-    return w;
-}
-
-// One word of weight codes times a token's codes.  8 bits: x[0] holds the four
-// token codes; 4 bits: x[0] those of the even, x[1] those of the odd columns.
-template <int WB>
-__device__ __forceinline__ int mac(uint32_t w, const uint32_t (&x)[WB == 8 ? 1 : 2], int acc) {
-    if constexpr (WB == 8) {
-        return dp4a_us(w, x[0], acc);
+        for (int i = 0; i < 5; ++i) w[i] = __ldg(reinterpret_cast<const uint32_t *>(a) + i);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __funnelshift_r(w[i], w[i + 1], 8 * mis);
     } else {
-        return dp4a_us((w >> 4) & 0x0F0F0F0Fu, x[1], dp4a_us(w & 0x0F0F0F0Fu, x[0], acc));
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (p + i < hi) v[i >> 2] |= (uint32_t)__ldg(p + i) << (8 * (i & 3));
     }
+    return make_uint4(v[0], v[1], v[2], v[3]);
 }
-template <int WB>
-__device__ __forceinline__ int sum_codes(const uint32_t (&x)[WB == 8 ? 1 : 2], int acc) {
-    acc = dp4a_us(0x01010101u, x[0], acc);
-    if constexpr (WB == 4) acc = dp4a_us(0x01010101u, x[1], acc);
-    return acc;
-}
-// token codes as signed bytes in the order mac() takes them
-template <int WB>
-__device__ __forceinline__ void token_codes(const uint32_t *raw, uint32_t (&x)[WB == 8 ? 1 : 2]) {
-    if constexpr (WB == 8) {
-        x[0] = raw[0] ^ 0x80808080u;
-    } else {
-        x[0] = __byte_perm(raw[0], raw[1], 0x6420) ^ 0x80808080u;
-        x[1] = __byte_perm(raw[0], raw[1], 0x7531) ^ 0x80808080u;
-    }
-}
-
-// ALIGNED: rows of whole 16-byte vectors (n a multiple of 16, or of 32 for 4
-// bits, and 16-byte aligned buffers).  Otherwise rows are walked in aligned
-// 4-byte words, their first and last bytes singly; a warp's rows lie four
-// apart, so they share their offset from the word boundary and with it the
-// (unaligned) token words.
-template <bool ALIGNED, int WB, int TT, int R, typename TY>
-__global__ void __launch_bounds__(SW * 32)
-    int8_stream_kernel(int64_t T, int64_t n, int64_t m, int kw, const uint8_t *X, const float *x_scale,
-                       const uint8_t *W, const float *w_scale, const uint8_t *w_zero, TY *Y) {
-    constexpr int XW = WB == 8 ? 1 : 2;
-    __shared__ int part[SW][R * TT + TT];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int group = warp / kw, kpart = warp % kw, groups = SW / kw;
-    const int64_t t0 = (int64_t)blockIdx.y * TT;
-    const int64_t rb = WB == 8 ? n : (n + 1) / 2;   // bytes of a row of W
-    // row of (group, j)
-    const int64_t rbase = (int64_t)blockIdx.x * groups * R;
-    auto row_of = [&](int j) -> int64_t {
-        if (ALIGNED || R == 1) return rbase + group * R + j;
-        return rbase + (group & 3) + 4 * (j + (int64_t)R * (group >> 2));   // groups is a multiple of 4 here
-    };
-    int acc[R][TT], xs[TT];
-#pragma unroll
-    for (int t = 0; t < TT; ++t) {
-        xs[t] = 0;
-#pragma unroll
-        for (int j = 0; j < R; ++j) acc[j][t] = 0;
-    }
-    const uint8_t *wrow[R];
-#pragma unroll
-    for (int j = 0; j < R; ++j)   // rows past m repeat the warp's first (same offset from the word boundary), unwritten
-        wrow[j] = W + (row_of(j) < m ? row_of(j) : (row_of(0) < m ? row_of(0) : 0)) * rb;
-    const uint8_t *xrow[TT];
-#pragma unroll
-    for (int t = 0; t < TT; ++t) xrow[t] = X + (t0 + t < T ? t0 + t : T - 1) * n;
-
+// Weight codes are read once: they pass L1 by, which keeps the tokens.
+template <bool ALIGNED>
+__device__ __forceinline__ uint4 load_weight(const uint8_t *p, const uint8_t *lo, const uint8_t *hi) {
     if constexpr (ALIGNED) {
-        const int nv = (int)(rb / 16);
-#pragma unroll 2
-        for (int v = kpart * 32 + lane; v < nv; v += kw * 32) {
-            uint32_t w[R][4];
-#pragma unroll
-            for (int j = 0; j < R; ++j) {
-                const uint4 q = __ldg(reinterpret_cast<const uint4 *>(wrow[j]) + v);
-                w[j][0] = q.x; w[j][1] = q.y; w[j][2] = q.z; w[j][3] = q.w;
-            }
-#pragma unroll
-            for (int t = 0; t < TT; ++t) {
-                uint32_t raw[4 * XW];
-#pragma unroll
-                for (int h = 0; h < XW; ++h) {
-                    const uint4 q = __ldg(reinterpret_cast<const uint4 *>(xrow[t]) + v * XW + h);
-                    raw[4 * h] = q.x; raw[4 * h + 1] = q.y; raw[4 * h + 2] = q.z; raw[4 * h + 3] = q.w;
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t x[XW];
-                    token_codes<WB>(raw + i * XW, x);
-                    xs[t] = sum_codes<WB>(x, xs[t]);
-#pragma unroll
-                    for (int j = 0; j < R; ++j) acc[j][t] = mac<WB>(w[j][i], x, acc[j][t]);
-                }
-            }
-        }
+        uint4 v;
+        asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                     : "l"(p));
+        return v;
+    }
+    return load16(p, lo, hi);
+}
+template <bool ALIGNED>
+__device__ __forceinline__ uint4 load_token(const uint8_t *p, const uint8_t *lo, const uint8_t *hi) {
+    if constexpr (ALIGNED) return __ldg(reinterpret_cast<const uint4 *>(p));
+    return load16(p, lo, hi);
+}
+
+__device__ __forceinline__ uint32_t word_of(const uint4 &v, int i) {
+    return i == 0 ? v.x : (i == 1 ? v.y : (i == 2 ? v.z : v.w));
+}
+
+// Lane's 16 bytes of weight codes as A pairs: word i gives pairs 2 i, 2 i + 1
+// (bytes 0 1, 2 3) or 4 i .. 4 i + 3 (nibbles 0 4, 1 5, 2 6, 3 7).
+template <int WB>
+__device__ __forceinline__ uint32_t weight_pair(uint32_t w, int j) {
+    if constexpr (WB == 8) {
+        return j == 0 ? __byte_perm(w, 0u, 0x4140) : __byte_perm(w, 0u, 0x4342);
     } else {
-        const uint8_t *xlo = X, *xhi = X + T * n;
-        const int mis = (int)(reinterpret_cast<uintptr_t>(wrow[0]) & 3);
-        const int64_t head = mis ? (4 - mis < rb ? 4 - mis : rb) : 0;
-        const int64_t nw = (rb - head) / 4, tail = rb - head - 4 * nw;
-        for (int64_t v = kpart * 32 + lane; v < nw; v += kw * 32) {
-            uint32_t w[R];
+        const uint32_t v = j < 2 ? w : w >> 8;
+        return j & 1 ? v & 0x00F000F0u : v & 0x000F000Fu;
+    }
+}
+// The tokens' pairs in the same order, for one word of weight codes.
+template <int WB>
+__device__ __forceinline__ void token_pairs(const uint4 *k, int i, uint32_t *x) {
+    if constexpr (WB == 8) {
+        const uint32_t w = word_of(k[0], i);
+        x[0] = sub2(__byte_perm(w, 0x64646464u, 0x4140), 0x64806480u);   // 1024 + c less 1152
+        x[1] = sub2(__byte_perm(w, 0x64646464u, 0x4342), 0x64806480u);
+    } else {
+        const uint32_t w0 = word_of(k[i >> 1], (i & 1) * 2), w1 = word_of(k[i >> 1], (i & 1) * 2 + 1);
+        const uint32_t a = __byte_perm(w0, w1, 0x5140), b = __byte_perm(w0, w1, 0x7362);   // columns 0 4 1 5, 2 6 3 7
+        x[0] = sub2(__byte_perm(a, 0x64646464u, 0x4140), 0x64806480u);
+        x[1] = sub2(__byte_perm(a, 0x54545454u, 0x4342), 0x54805480u);   // 64 + c / 16 less 72
+        x[2] = sub2(__byte_perm(b, 0x64646464u, 0x4140), 0x64806480u);
+        x[3] = sub2(__byte_perm(b, 0x54545454u, 0x4342), 0x54805480u);
+    }
+}
+
+// ALIGNED: rows of whole 16-byte pieces of codes (n a multiple of 16, or of 32
+// for 4 bits) at 16-byte aligned addresses.
+template <bool ALIGNED, int WB, int NT, int RT, typename TY>
+__global__ void __launch_bounds__(SW * 32, NT * RT == 1 ? 3 : 2)
+    int8_stream_kernel(int64_t T, int64_t n, int64_t m, const uint8_t *X, const float *x_scale, const uint8_t *W,
+                       const float *w_scale, const uint8_t *w_zero, TY *Y) {
+    constexpr int XP = WB == 8 ? 1 : 2;           // 16-byte pieces of token codes to one of weight codes
+    constexpr int WP = WB == 8 ? 2 : 4;           // pairs of a word
+    constexpr int ROWS = RT * 16, TOK = NT * 8, OUT = ROWS * TOK;
+    constexpr int UNROLL = NT * RT == 1 ? 4 : (NT * RT == 2 ? 2 : 1);
+    // steps between flushes: 8 bits, 64 codes of at most 255 x 128 each; 4 bits, 128 codes of 15 x 128
+    constexpr int FLUSH = WB == 8 ? 8 : 64;
+    static_assert(FLUSH % UNROLL == 0, "flushes fall between rounds of loads");
+    __shared__ int red[SW * OUT];
+    __shared__ int xred[SW * TOK];
+    cg::cluster_group cluster = cg::this_cluster();
+    const int CL = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+    const int64_t i0 = (int64_t)(blockIdx.x / CL) * ROWS;
+    const int64_t rb = WB == 8 ? n : (n + 1) / 2;   // bytes of a row of W
+    const int pieces = (int)((rb + 15) / 16);
+
+    const uint8_t *wrow[RT][2], *xrow[NT];
 #pragma unroll
-            for (int j = 0; j < R; ++j) w[j] = __ldg(reinterpret_cast<const uint32_t *>(wrow[j] + head) + v);
-            const int64_t c = (head + 4 * v) * XW;   // first column
-            const bool last = WB == 4 && c + 8 > n;   // the byte of an odd width's last column holds one code
+    for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int t = 0; t < TT; ++t) {
-                uint32_t raw[XW], x[XW];
+        for (int h = 0; h < 2; ++h)   // (rows past m repeat the last, unwritten)
+            wrow[r][h] = W + min(i0 + r * 16 + h * 8 + g, m - 1) * rb;
 #pragma unroll
-                for (int h = 0; h < XW; ++h) raw[h] = load_word(xrow[t] + c + 4 * h, xlo, xhi);
-                token_codes<WB>(raw, x);
-                if (last) x[XW - 1] &= 0x00FFFFFFu;
-                xs[t] = sum_codes<WB>(x, xs[t]);
+    for (int t = 0; t < NT; ++t) xrow[t] = X + min((int64_t)(t * 8 + g), T - 1) * n;
+    const uint8_t *whi = W + m * rb, *xhi = X + T * n;
+
+    float acc[RT][NT][4] = {}, xacc[NT][4] = {};
+    int sum[RT][NT][4] = {};
+    auto flush = [&] {
 #pragma unroll
-                for (int j = 0; j < R; ++j) acc[j][t] = mac<WB>(w[j], x, acc[j][t]);
-            }
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sum[r][t][e] += __float2int_rn(acc[r][t][e] * 16777216.f);
+                    acc[r][t][e] = 0.f;
+                }
+    };
+
+    // four neighbouring pieces (64 bytes of each row) to a step; the cluster's warps take steps in turn
+    const int steps = (pieces + 3) / 4;
+    int since = 0;
+    for (int s0 = rank * SW + warp; s0 < steps; s0 += CL * SW * UNROLL) {
+        uint4 wq[UNROLL][RT][2];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int v = (s0 + u * CL * SW) * 4 + q;
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    wq[u][r][h] = make_uint4(0, 0, 0, 0);
+                    if (v < pieces) wq[u][r][h] = load_weight<ALIGNED>(wrow[r][h] + (int64_t)v * 16, W, whi);
+                }
         }
-        // head and tail bytes, one to a lane of the first K part
-        if (kpart == 0 && lane < head + tail) {
-            const int64_t b = lane < head ? lane : rb - tail + (lane - head);
 #pragma unroll
-            for (int t = 0; t < TT; ++t)
+        for (int u = 0; u < UNROLL; ++u) {
+            const int v = (s0 + u * CL * SW) * 4 + q;
+            if ((s0 + u * CL * SW) >= steps) break;   // (the same for the whole warp)
+            uint4 k[NT][XP];
 #pragma unroll
-                for (int h = 0; h < XW; ++h) {
-                    const int64_t c = b * XW + h;
-                    if (c < n) {
-                        const int xv = (int)__ldg(xrow[t] + c) - 128;
-                        xs[t] += xv;
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int j = 0; j < R; ++j) {
-                            const int wv = __ldg(wrow[j] + b);
-                            acc[j][t] += (WB == 8 ? wv : (h ? wv >> 4 : wv & 15)) * xv;
+                for (int p = 0; p < XP; ++p) {
+                    const int64_t c = ((int64_t)v * XP + p) * 16;   // first column
+                    k[t][p] = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
+                    if (v < pieces && c < n) {
+                        k[t][p] = load_token<ALIGNED>(xrow[t] + c, X, xhi);
+                        if (!ALIGNED && c + 16 > n) {   // columns from n on take no part
+                            uint32_t *w = &k[t][p].x;
+                            for (int b = (int)(n - c); b < 16; ++b)
+                                w[b >> 2] = (w[b >> 2] & ~(0xFFu << 8 * (b & 3))) | 0x80u << 8 * (b & 3);
                         }
                     }
                 }
-        }
-    }
 #pragma unroll
-    for (int t = 0; t < TT; ++t) {
-        xs[t] = __reduce_add_sync(FULL, xs[t]);
+            for (int i = 0; i < 4; ++i) {             // words of the 16 bytes
+                uint32_t x[NT][WP];
 #pragma unroll
-        for (int j = 0; j < R; ++j) acc[j][t] = __reduce_add_sync(FULL, acc[j][t]);
-    }
-    if (kw > 1) {
-        if (lane == 0) {
+                for (int t = 0; t < NT; ++t) token_pairs<WB>(k[t], i, x[t]);
 #pragma unroll
-            for (int t = 0; t < TT; ++t) {
-                part[warp][R * TT + t] = xs[t];
+                for (int j = 0; j < WP; j += 2) {     // a product takes two pairs
 #pragma unroll
-                for (int j = 0; j < R; ++j) part[warp][j * TT + t] = acc[j][t];
-            }
-        }
-        __syncthreads();
-        if (kpart != 0) return;
+                    for (int r = 0; r < RT; ++r) {
+                        uint32_t a[4];
 #pragma unroll
-        for (int t = 0; t < TT; ++t) {
-            for (int p = 1; p < kw; ++p) xs[t] += part[warp + p][R * TT + t];
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t w = word_of(wq[u][r][h], i);
+                            a[h] = weight_pair<WB>(w, j);
+                            a[2 + h] = weight_pair<WB>(w, j + 1);
+                        }
 #pragma unroll
-            for (int j = 0; j < R; ++j)
-                for (int p = 1; p < kw; ++p) acc[j][t] += part[warp + p][j * TT + t];
-        }
-    }
-    // lane j TT + t writes (row j, token t)
-    static_assert(R * TT <= 32, "one result to a lane");
+                        for (int t = 0; t < NT; ++t) mma16816(acc[r][t], a, x[t][j], x[t][j + 1]);
+                    }
+                    // ones (16 where the pair holds x / 16)
+                    const uint32_t one[4] = {0x3C003C00u, 0x3C003C00u, WB == 8 ? 0x3C003C00u : 0x4C004C00u,
+                                             WB == 8 ? 0x3C003C00u : 0x4C004C00u};
 #pragma unroll
-    for (int j = 0; j < R; ++j)
-#pragma unroll
-        for (int t = 0; t < TT; ++t)
-            if (lane == j * TT + t) {
-                const int64_t i = row_of(j), tok = t0 + t;
-                if (i < m && tok < T) {
-                    const int z = w_zero ? w_zero[i] : (WB == 8 ? 128 : 8);
-                    // (mod 2^32: the true sum fits, its two parts need not)
-                    const int v = (int)((uint32_t)acc[j][t] - (uint32_t)z * (uint32_t)xs[t]);
-                    store1(Y + tok * m + i, (float)v * x_scale[tok] * w_scale[i]);
+                    for (int t = 0; t < NT; ++t) mma16816(xacc[t], one, x[t][j], x[t][j + 1]);
                 }
             }
+        }
+        since += UNROLL;
+        if (since == FLUSH) {
+            flush();
+            since = 0;
+        }
+    }
+    flush();
+
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                red[warp * OUT + (t * 8 + 2 * q + (e & 1)) * ROWS + r * 16 + (e >> 1) * 8 + g] = sum[r][t][e];
+    if (g == 0) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) xred[warp * TOK + t * 8 + 2 * q + e] = __float2int_rn(xacc[t][e]);
+    }
+    __syncthreads();
+    // the warps' shares, then the cluster's; integers, so any order is the same
+    for (int k = threadIdx.x; k < OUT + TOK; k += SW * 32) {
+        int *p = k < OUT ? red + k : xred + k - OUT;
+        const int step = k < OUT ? OUT : TOK;
+        int a = p[0];
+#pragma unroll
+        for (int w = 1; w < SW; ++w) a += p[w * step];
+        p[0] = a;
+    }
+    if (CL > 1) {
+        cluster.sync();
+        if (rank == 0) {
+            for (int k = threadIdx.x; k < OUT + TOK; k += SW * 32) {
+                int *p = k < OUT ? red + k : xred + k - OUT;
+                int a = p[0];
+                for (int c = 1; c < CL; ++c) a += *cluster.map_shared_rank(p, c);
+                p[0] = a;
+            }
+        }
+        cluster.sync();   // the other CTAs' sums have been read
+        if (rank != 0) return;
+    } else {
+        __syncthreads();
+    }
+    for (int k = threadIdx.x; k < OUT; k += SW * 32) {
+        const int64_t i = i0 + k % ROWS, t = k / ROWS;
+        if (i < m && t < T) {
+            const int z = w_zero ? w_zero[i] : (WB == 8 ? 128 : 8);
+            // (mod 2^32: the true sum fits, its two parts need not)
+            const int v = (int)((uint32_t)red[k] - (uint32_t)z * (uint32_t)xred[k / ROWS]);
+            store1(Y + t * m + i, (float)v * __ldg(x_scale + t) * __ldg(w_scale + i));
+        }
+    }
 }
 
-template <bool ALIGNED, int WB, int TT, int R, typename TY>
+template <bool ALIGNED, int WB, int NT, int RT, typename TY>
 realq_status_t stream_launch(cudaStream_t s, int64_t T, int64_t n, int64_t m, const uint8_t *X, const float *xs,
                              const uint8_t *W, const float *ws, const uint8_t *wz, TY *Y, int sms) {
-    // Warps per group of R rows: as many as it takes to put 16 warps on each
-    // SM, but no more than leave each its own 512-byte step of K.
-    const int64_t rb = WB == 8 ? n : (n + 1) / 2;
-    int kw = 1;
-    const int kmax = ALIGNED || R == 1 ? SW : 2;   // (the unaligned rows need four groups per CTA)
-    const int64_t ygroups = (T + TT - 1) / TT;
-    while (kw < kmax && (m + R - 1) / R * kw * ygroups < (int64_t)sms * 16 && rb > 512 * kw) kw *= 2;
-    const int64_t rows = (int64_t)(SW / kw) * R;
+    // CTAs over K: the count whose waves take the fewest steps of a warp, its
+    // start and end counted as four, each warp keeping at least two.
+    const int64_t rb = WB == 8 ? n : (n + 1) / 2, ctas = (m + RT * 16 - 1) / (RT * 16), steps = (rb + 63) / 64;
+    const int64_t slots = (int64_t)sms * (NT * RT == 1 ? 3 : 2);
+    int cl = 1;
+    int64_t best = INT64_MAX;
+    for (int c = 1; c <= MAX_CLUSTER && (c == 1 || steps >= 2 * SW * c); c *= 2) {
+        const int64_t cost = (ctas * c + slots - 1) / slots * ((steps + SW * c - 1) / (SW * c) + 4);
+        if (cost < best) {
+            best = cost;
+            cl = c;
+        }
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(ctas * cl));
+    cfg.blockDim = dim3(SW * 32);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)cl;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
     {
         Launch L("int8_product_stream", s);
-        int8_stream_kernel<ALIGNED, WB, TT, R, TY>
-            <<<dim3((unsigned)((m + rows - 1) / rows), (unsigned)ygroups), SW * 32, 0, s>>>(T, n, m, kw, X, xs, W, ws,
-                                                                                          wz, Y);
+        REALQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, int8_stream_kernel<ALIGNED, WB, NT, RT, TY>, T, n, m, X, xs, W, ws, wz, Y));
     }
     return check_launch("int8_product_stream");
 }
@@ -244,13 +324,13 @@ realq_status_t stream_launch(cudaStream_t s, int64_t T, int64_t n, int64_t m, co
 template <bool ALIGNED, int WB, typename TY>
 realq_status_t stream_tokens(cudaStream_t s, int64_t T, int64_t n, int64_t m, const uint8_t *X, const float *xs,
                              const uint8_t *W, const float *ws, const uint8_t *wz, TY *Y, int sms) {
-    if (T == 1) {
-        if (m < (int64_t)sms * 64) return stream_launch<ALIGNED, WB, 1, 1, TY>(s, T, n, m, X, xs, W, ws, wz, Y, sms);
-        return stream_launch<ALIGNED, WB, 1, 4, TY>(s, T, n, m, X, xs, W, ws, wz, Y, sms);
-    }
-    if (T == 2) return stream_launch<ALIGNED, WB, 2, 4, TY>(s, T, n, m, X, xs, W, ws, wz, Y, sms);
-    if (T <= 4) return stream_launch<ALIGNED, WB, 4, 4, TY>(s, T, n, m, X, xs, W, ws, wz, Y, sms);
-    return stream_launch<ALIGNED, WB, 8, 4, TY>(s, T, n, m, X, xs, W, ws, wz, Y, sms);
+    // 32 channels to a warp halve the work on the tokens' codes, where there are enough of them
+    const bool wide = m >= (int64_t)sms * 32;
+    if (T <= 8)
+        return wide ? stream_launch<ALIGNED, WB, 1, 2, TY>(s, T, n, m, X, xs, W, ws, wz, Y, sms)
+                    : stream_launch<ALIGNED, WB, 1, 1, TY>(s, T, n, m, X, xs, W, ws, wz, Y, sms);
+    return wide ? stream_launch<ALIGNED, WB, 2, 2, TY>(s, T, n, m, X, xs, W, ws, wz, Y, sms)
+                : stream_launch<ALIGNED, WB, 2, 1, TY>(s, T, n, m, X, xs, W, ws, wz, Y, sms);
 }
 
 template <int WB, typename TY>
@@ -262,9 +342,12 @@ realq_status_t stream(cudaStream_t s, int64_t T, int64_t n, int64_t m, const uin
                    : stream_tokens<false, WB, TY>(s, T, n, m, X, xs, W, ws, wz, Y, sms);
 }
 
-}  // namespace
+// Tokens up to which the streaming kernel runs.  8192 -> 28672: 16 tokens take
+// 57 us here and 56 in the tensor-core product with 8-bit weights, 42 and 60
+// with 4-bit ones; at 1024 -> 2048 3.0 and 9.4.
+constexpr int64_t STREAM_T = 16;
 
-constexpr int64_t STREAM_T = 8;   // tokens up to which the streaming kernel runs
+}  // namespace
 
 size_t int8_product_ws_bytes(int64_t T, int64_t n, int64_t m, int w_bits, int sms) {
     return T <= STREAM_T ? 256 : int8_tc_ws_bytes(T, n, m, w_bits, sms);
@@ -273,18 +356,18 @@ size_t int8_product_ws_bytes(int64_t T, int64_t n, int64_t m, int w_bits, int sm
 realq_status_t int8_product(cudaStream_t s, int64_t T, int64_t n, int64_t m, const uint8_t *X, const float *x_scale,
                             const uint8_t *W, int w_bits, const float *w_scale, const uint8_t *w_zero, void *Y,
                             realq_dtype_t y_dtype, void *ws, int sms) {
-    if (T > STREAM_T) {
-        const int64_t rb = w_bits == 8 ? n : (n + 1) / 2;
-        // (whole rows at an odd address go through the streaming kernel, eight tokens at a time)
-        if (rb % 16 || (reinterpret_cast<uintptr_t>(W) & 15) == 0)
-            return int8_product_tc(s, T, n, m, X, x_scale, W, w_bits, w_scale, w_zero, Y, y_dtype, ws, sms);
-        if (T > 65535 * STREAM_T)
-            return fail(REALQ_ERR_UNSUPPORTED, "int8_product: more than %lld tokens need 16-byte aligned W_codes",
-                        (long long)(65535 * STREAM_T));
-    }
-    auto run = [&](auto *y) {
-        return w_bits == 8 ? stream<8>(s, T, n, m, X, x_scale, W, w_scale, w_zero, y, sms)
-                           : stream<4>(s, T, n, m, X, x_scale, W, w_scale, w_zero, y, sms);
+    // (whole 16-byte rows at an odd address cannot be a tensor map's, and are
+    // streamed for 16 tokens at a time)
+    const bool odd = (w_bits == 8 ? n : (n + 1) / 2) % 16 == 0 && (reinterpret_cast<uintptr_t>(W) & 15) != 0;
+    if (T > STREAM_T && !odd)
+        return int8_product_tc(s, T, n, m, X, x_scale, W, w_bits, w_scale, w_zero, Y, y_dtype, ws, sms);
+    auto run = [&](auto *y) -> realq_status_t {
+        for (int64_t t = 0; t < T; t += STREAM_T) {
+            const int64_t k = std::min(STREAM_T, T - t);
+            REALQ_TRY(w_bits == 8 ? stream<8>(s, k, n, m, X + t * n, x_scale + t, W, w_scale, w_zero, y + t * m, sms)
+                                  : stream<4>(s, k, n, m, X + t * n, x_scale + t, W, w_scale, w_zero, y + t * m, sms));
+        }
+        return REALQ_OK;
     };
     return y_dtype == REALQ_BF16 ? run(static_cast<__nv_bfloat16 *>(Y)) : run(static_cast<float *>(Y));
 }
