@@ -12,12 +12,20 @@
 // drain warps add each into fp32 registers (IEEE additions) while the other
 // fills.
 //
-// One CTA owns a 128 x 256 tile of dW (rows of dY's width, columns of X̂'s) and
-// a range of tokens.  Both operands are token-major, i.e. MN-major for the
-// MMA: a TMA box of 64 tokens x 64 channels (128-byte rows, 128-byte swizzle)
-// is one canonical atom stack, two boxes make A and four make B.  Tokens are
-// split over CTAs when the tiles alone do not fill the SMs; the parts are
-// summed in a fixed order.
+// Two CTAs of a cluster work as a pair (cta_group::2) on a tile of dW of 256
+// columns (X̂'s channels, the MMA's rows, 128 to each CTA) by 256 rows (dY's
+// channels, the MMA's columns): each CTA loads its 128 channels of either
+// operand, and the MMA takes B from both, so an operand byte in shared memory
+// serves twice the products of a single CTA's tile (a 128 x 256 tile per CTA
+// waited on L2: 806 cycles for 512 of MMA).  X̂'s channels lie on the TMEM lanes,
+// so that a warp's stores of one row of dW are contiguous.  Both operands are
+// token-major, i.e. MN-major for the MMA: a TMA box of 64 tokens x 64 channels
+// (128-byte rows, 128-byte swizzle) is one canonical atom stack.  Persistent
+// pairs walk the tiles; the accumulation lies in the drain warps' registers, so
+// storing a tile overlaps the next one's MMAs.  Tokens are split over pairs
+// when the tiles alone do not fill the SMs; the parts are summed in a fixed
+// order.  Every wait is bounded; a tile whose wait gave up is written as NaN
+// and the status word gets ST_TIMEOUT.
 #include "kernels.cuh"
 #include "tc.cuh"
 
@@ -26,55 +34,62 @@
 namespace realq {
 namespace {
 
-constexpr int TM = 128;
-constexpr int TN = 256;
+constexpr int TC = 128;                          // channels of either operand per CTA
+constexpr int TT = 2 * TC;                       // tile side
 constexpr int KSTAGE = 64;                       // tokens per pipeline stage
-constexpr int STAGES = 4;
-constexpr int CHUNK_STAGES = 16;                 // stages per TMEM accumulator pass
+constexpr int STAGES = 6;
+constexpr int CHUNK_STAGES = 8;                  // stages per TMEM accumulator pass
 constexpr int DRAIN_WARPS = 8;
 constexpr int THREADS = (DRAIN_WARPS + 2) * 32;
 constexpr int BOX_BYTES = 64 * KSTAGE * 2;
-constexpr int A_BYTES = TM * KSTAGE * 2;
-constexpr int B_BYTES = TN * KSTAGE * 2;
-constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
+constexpr int OP_BYTES = TC * KSTAGE * 2;        // an operand's stage in one CTA: two boxes
+constexpr int STAGE_BYTES = 2 * OP_BYTES;
 constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 1024 + 256;
-constexpr uint32_t IDESC = tc::idesc_bf16_f32(TM, TN, 1, 1);
+constexpr uint32_t IDESC = tc::idesc_bf16_f32(TT, TT, 1, 1);
 constexpr unsigned FULL = 0xFFFFFFFFu;
 constexpr int MAX_SPLITS = 8;
 
-// Tile t of the nti x ntj grid, in groups of 8 row tiles: the CTAs resident
-// together cover a compact block of dW and share operands through L2.
-__device__ __forceinline__ void tile_of(int t, int nti, int ntj, int &ti, int &tj) {
+struct Work {
+    int64_t m, n, T, tper;     // tokens per part, a multiple of KSTAGE
+    int64_t plane_rows;        // dY's planes lie this many rows apart
+    int planes, nti, ntj;      // tiles over X̂'s channels, dY's channels
+    int items;                 // tiles x parts
+};
+struct Item {
+    int i0, j0, z, nk;         // first channels, part, stages
+    int64_t t0;
+};
+// Parts outermost; within one, groups of 8 tile rows, so that the pairs running
+// together share operands in L2.
+__device__ __forceinline__ Item item_of(const Work &w, int k) {
     constexpr int G = 8;
-    const int g = t / (G * ntj), r0 = g * G, rows = min(G, nti - r0), k = t - g * G * ntj;
-    ti = r0 + k % rows;
-    tj = k / rows;
+    const int tiles = w.nti * w.ntj;
+    Item it;
+    it.z = k / tiles;
+    const int t = k - it.z * tiles, g = t / (G * w.ntj), r0 = g * G, rows = min(G, w.nti - r0), u = t - g * G * w.ntj;
+    it.i0 = (r0 + u % rows) * TT;
+    it.j0 = (u / rows) * TT;
+    it.t0 = it.z * w.tper;
+    it.nk = (int)((min(w.T - it.t0, w.tper) + KSTAGE - 1) / KSTAGE) * w.planes;
+    return it;
 }
 
-// planes: token rows [p T_pad, p T_pad + T) of A hold dY's plane p
-__global__ void __launch_bounds__(THREADS, 1)
-    weight_grad_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, int planes,
-                       int64_t plane_rows, int64_t m, int64_t n, int64_t T, int64_t tper, float *dW, int accumulate,
-                       float *part, int *err) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
+    weight_grad_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapY, const Work wk,
+                       float *dW, int accumulate, float *part, int *err) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint64_t *full = reinterpret_cast<uint64_t *>(smem + STAGES * STAGE_BYTES);
+    uint64_t *full = reinterpret_cast<uint64_t *>(smem + STAGES * STAGE_BYTES);   // the leader's: both CTAs' loads
     uint64_t *empty = full + STAGES;
     uint64_t *accf = empty + STAGES;             // [2] accumulator b holds a finished chunk
-    uint64_t *acce = accf + 2;                   // [2] accumulator b has been drained
+    uint64_t *acce = accf + 2;                   // [2] the leader's: accumulator b drained by both CTAs
     uint64_t *done = acce + 2;                   // every MMA issued has retired
     uint32_t *tslot = reinterpret_cast<uint32_t *>(done + 1);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tslot + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int ti, tj;
-    tile_of((int)blockIdx.x, (int)((m + TM - 1) / TM), (int)((n + TN - 1) / TN), ti, tj);
-    const int i0 = ti * TM, j0 = tj * TN;
-    const int64_t t_begin = (int64_t)blockIdx.y * tper;
-    const int64_t t_end = min(T, t_begin + tper);
-    const int nkp = t_end > t_begin ? (int)((t_end - t_begin + KSTAGE - 1) / KSTAGE) : 0;   // stages per plane
-    const int nk = nkp * planes;
-    const int nch = (nk + CHUNK_STAGES - 1) / CHUNK_STAGES;
+    const uint32_t rank = tc::cluster_rank();
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
@@ -83,144 +98,162 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         for (int b = 0; b < 2; ++b) {
             tc::mbar_init(tc::smem_u32(&accf[b]), 1);
-            tc::mbar_init(tc::smem_u32(&acce[b]), DRAIN_WARPS);
+            tc::mbar_init(tc::smem_u32(&acce[b]), 2 * DRAIN_WARPS);
         }
         tc::mbar_init(tc::smem_u32(done), 1);
         *abort_flag = 0;
         tc::fence_barrier_init();
-        tc::prefetch_tmap(&mapA);
-        tc::prefetch_tmap(&mapB);
+        tc::prefetch_tmap(&mapX);
+        tc::prefetch_tmap(&mapY);
     }
-    if (warp == 0) tc::tmem_alloc(tc::smem_u32(tslot), 2 * TN);
+    if (warp == 0) tc::tmem_alloc_pair(tc::smem_u32(tslot), 2 * TT);
     tc::fence_before_sync();
     __syncthreads();
+    tc::cluster_sync();
     tc::fence_after_sync();
     const uint32_t tmem = *tslot;
-
-    float acc[128];
-#pragma unroll
-    for (int c = 0; c < 128; ++c) acc[c] = 0.f;
     bool good = true;
 
     if (warp == DRAIN_WARPS) {
         if (lane == 0) {
-            // ---------------- TMA producer ----------------
-            // the planes of a token range follow one another stage by stage
-            int it = 0;
-            for (; it < nk; ++it) {
-                const int s = it % STAGES;
-                const uint32_t r = (uint32_t)(it / STAGES);
-                if (!tc::mbar_wait(tc::smem_u32(&empty[s]), (r & 1u) ^ 1u, abort_flag)) {
-                    *abort_flag = 1;
-                    break;
+            // ---------------- TMA producer: this CTA's channels ----------------
+            int s = 0, it = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int k = pair; k < wk.items && ok; k += pairs) {
+                const Item im = item_of(wk, k);
+                const int xi = im.i0 + (int)rank * TC, xj = im.j0 + (int)rank * TC;
+                int y = (int)im.t0, p = 0;
+                for (int i = 0; i < im.nk; ++i, ++it) {
+                    ok = tc::mbar_wait(tc::smem_u32(&empty[s]), phase ^ 1u, abort_flag);
+                    if (!ok) break;
+                    const uint32_t fb = tc::map_rank(tc::smem_u32(&full[s]), 0);
+                    if (rank == 0) tc::mbar_arrive_expect_tx(tc::smem_u32(&full[s]), 2 * STAGE_BYTES);
+                    const uint32_t a = tc::smem_u32(smem + s * STAGE_BYTES);
+                    const int yp = (int)(p * wk.plane_rows) + y;
+                    tc::tma_load_2d_pair(a, &mapX, fb, xi, y);
+                    tc::tma_load_2d_pair(a + BOX_BYTES, &mapX, fb, xi + 64, y);
+                    tc::tma_load_2d_pair(a + OP_BYTES, &mapY, fb, xj, yp);
+                    tc::tma_load_2d_pair(a + OP_BYTES + BOX_BYTES, &mapY, fb, xj + 64, yp);
+                    if (++p == wk.planes) {   // the planes of 64 tokens follow one another
+                        p = 0;
+                        y += KSTAGE;
+                    }
+                    if (++s == STAGES) {
+                        s = 0;
+                        phase ^= 1u;
+                    }
                 }
-                const uint32_t fb = tc::smem_u32(&full[s]);
-                tc::mbar_arrive_expect_tx(fb, STAGE_BYTES);
-                const int p = it % planes;
-                const int y = (int)(t_begin + (int64_t)(it / planes) * KSTAGE);
-                const int ya = (int)(p * plane_rows) + y;
-                const uint32_t a = tc::smem_u32(smem + s * STAGE_BYTES);
-                tc::tma_load_2d(a, &mapA, fb, i0, ya);
-                tc::tma_load_2d(a + BOX_BYTES, &mapA, fb, i0 + 64, ya);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) tc::tma_load_2d(a + A_BYTES + q * BOX_BYTES, &mapB, fb, j0 + 64 * q, y);
             }
-            // on abort, let the copies already issued land before the CTA exits
-            if (*abort_flag) {
+            if (!ok) *abort_flag = 1;
+            // On abort, the copies already issued land before the pair's shared memory goes: the leader waits for
+            // both CTAs' (its barriers count them), the other for the leader's exit below.
+            if (*abort_flag && rank == 0) {
                 int never = 0;
                 for (int k = (it > STAGES ? it - STAGES : 0); k < it; ++k)
-                    tc::mbar_wait(tc::smem_u32(&full[k % STAGES]), (uint32_t)(k / STAGES) & 1u, &never,
-                                  100000000ull);
+                    tc::mbar_wait(tc::smem_u32(&full[k % STAGES]), (uint32_t)(k / STAGES) & 1u, &never, 100000000ull);
             }
         }
     } else if (warp == DRAIN_WARPS + 1) {
-        // ---------------- MMA issuer (the whole warp waits, one lane issues) ----------------
-        const uint64_t desc0 = tc::smem_desc(tc::smem_u32(smem), BOX_BYTES, 1024, tc::SW_128B);
-        int s = 0;
-        uint32_t phase = 0;
-        bool ok = true;
-        for (int c = 0; c < nch && ok; ++c) {
-            const int b = c & 1;
-            if (c >= 2) {
-                ok = __all_sync(FULL, tc::mbar_wait(tc::smem_u32(&acce[b]), (uint32_t)((c >> 1) - 1) & 1u, abort_flag));
-                if (!ok) break;
-            }
-            tc::fence_after_sync();
-            const uint32_t d = tmem + (uint32_t)(b * TN);
-            const int cnt = min(CHUNK_STAGES, nk - c * CHUNK_STAGES);
-            for (int i = 0; i < cnt; ++i) {
-                ok = __all_sync(FULL, tc::mbar_wait(tc::smem_u32(&full[s]), phase, abort_flag));
-                if (!ok) break;
-                tc::fence_after_sync();
-                const uint64_t da = desc0 + (uint32_t)(s * STAGE_BYTES >> 4), db = da + (A_BYTES >> 4);
-                if (tc::elect_one()) {
+        if (rank == 0) {
+            // ---------------- MMA issuer (the whole warp waits, one lane issues) ----------------
+            const uint64_t desc0 = tc::smem_desc(tc::smem_u32(smem), BOX_BYTES, 1024, tc::SW_128B);
+            int s = 0, c = 0;   // stage; accumulator pass over all items
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int k = pair; k < wk.items && ok; k += pairs) {
+                const Item im = item_of(wk, k);
+                for (int i0 = 0; i0 < im.nk && ok; i0 += CHUNK_STAGES, ++c) {
+                    const int b = c & 1;
+                    ok = __all_sync(FULL, tc::mbar_wait(tc::smem_u32(&acce[b]), ((uint32_t)(c >> 1) & 1u) ^ 1u, abort_flag));
+                    if (!ok) break;
+                    tc::fence_after_sync();
+                    const uint32_t d = tmem + (uint32_t)(b * TT);
+                    const int cnt = min(CHUNK_STAGES, im.nk - i0);
+                    for (int i = 0; i < cnt; ++i) {
+                        ok = __all_sync(FULL, tc::mbar_wait(tc::smem_u32(&full[s]), phase, abort_flag));
+                        if (!ok) break;
+                        tc::fence_after_sync();
+                        const uint64_t da = desc0 + (uint32_t)(s * STAGE_BYTES >> 4), db = da + (OP_BYTES >> 4);
+                        if (tc::elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < KSTAGE / 16; ++k)
-                        tc::mma_bf16_ss(d, da + k * (2048 >> 4), db + k * (2048 >> 4), IDESC, (i > 0 || k > 0) ? 1u : 0u);
-                    tc::mma_commit(tc::smem_u32(&empty[s]));
-                }
-                __syncwarp();
-                if (++s == STAGES) {
-                    s = 0;
-                    phase ^= 1u;
+                            for (int q = 0; q < KSTAGE / 16; ++q)
+                                tc::mma_f16_ss_pair(d, da + q * (2048 >> 4), db + q * (2048 >> 4), IDESC,
+                                                    (i > 0 || q > 0) ? 1u : 0u);
+                            tc::mma_commit_pair(tc::smem_u32(&empty[s]));
+                        }
+                        __syncwarp();
+                        if (++s == STAGES) {
+                            s = 0;
+                            phase ^= 1u;
+                        }
+                    }
+                    if (ok && tc::elect_one()) tc::mma_commit_pair(tc::smem_u32(&accf[b]));
+                    __syncwarp();
                 }
             }
-            if (ok && tc::elect_one()) tc::mma_commit(tc::smem_u32(&accf[b]));
+            if (!ok) *abort_flag = 1;
+            // every MMA issued has retired before either CTA frees its TMEM
+            if (tc::elect_one()) tc::mma_commit_pair(tc::smem_u32(done));
             __syncwarp();
+            int never = 0;
+            tc::mbar_wait(tc::smem_u32(done), 0u, &never, 100000000ull);
         }
-        if (!ok) *abort_flag = 1;
-        // every MMA issued has retired before TMEM is freed
-        if (tc::elect_one()) tc::mma_commit(tc::smem_u32(done));
-        __syncwarp();
-        int never = 0;
-        tc::mbar_wait(tc::smem_u32(done), 0u, &never, 100000000ull);
     } else {
-        // ------- drain warps: TMEM chunk -> fp32 registers (lane quarter, column half) -------
-        const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t col_base = (uint32_t)((warp >> 2) * 128);
-        for (int c = 0; c < nch; ++c) {
-            const int b = c & 1;
-            const bool ok = tc::mbar_wait(tc::smem_u32(&accf[b]), (uint32_t)(c >> 1) & 1u, abort_flag);
-            if (!__all_sync(FULL, ok)) {
-                good = false;
-                *abort_flag = 1;
-                break;
-            }
-            tc::fence_after_sync();
+        // ------- drain warps: TMEM passes -> fp32 registers (lane quarter, column half) -> dW -------
+        const uint32_t src = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)((warp >> 2) * 128);
+        int c = 0;
+        for (int k = pair; k < wk.items; k += pairs) {
+            const Item im = item_of(wk, k);
+            float acc[128];
 #pragma unroll
-            for (int c0 = 0; c0 < 128; c0 += 32) {
-                uint32_t v[32];
-                tc::tmem_ld_32x32b_x32(tmem + lane_base + (uint32_t)(b * TN) + col_base + (uint32_t)c0, v);
+            for (int q = 0; q < 128; ++q) acc[q] = 0.f;
+            for (int i0 = 0; i0 < im.nk && good; i0 += CHUNK_STAGES, ++c) {
+                const int b = c & 1;
+                if (!__all_sync(FULL, tc::mbar_wait(tc::smem_u32(&accf[b]), (uint32_t)(c >> 1) & 1u, abort_flag))) {
+                    *abort_flag = 1;
+                    good = false;   // this tile and the pair's later ones are written as NaN
+                    break;
+                }
+                tc::fence_after_sync();
 #pragma unroll
-                for (int q = 0; q < 32; ++q) acc[c0 + q] += __uint_as_float(v[q]);
+                for (int c0 = 0; c0 < 128; c0 += 16) {
+                    uint32_t v[16];
+                    tc::tmem_ld_32x32b_x16(src + (uint32_t)(b * TT + c0), v);
+                    tc::tmem_wait_ld();
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) acc[c0 + q] += __uint_as_float(v[q]);
+                }
+                tc::fence_before_sync();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive_cluster(tc::map_rank(tc::smem_u32(&acce[b]), 0));
             }
-            tc::fence_before_sync();
-            __syncwarp();
-            if (lane == 0) tc::mbar_arrive(tc::smem_u32(&acce[b]));
+            const int64_t col = im.i0 + (int)rank * TC + (warp & 3) * 32 + lane;
+            const int64_t row = im.j0 + (warp >> 2) * 128;
+            if (col < wk.n) {
+                float *o = (part ? part + im.z * wk.m * wk.n : dW) + row * wk.n + col;
+                const bool add = !part && accumulate;
+                const int rows = (int)min((int64_t)128, wk.m - row);
+#pragma unroll
+                for (int q = 0; q < 128; ++q, o += wk.n)
+                    if (q < rows) {
+                        const float v = good ? acc[q] : __int_as_float(0x7fc00000);
+                        *o = add ? *o + v : v;
+                    }
+            }
         }
     }
     __syncwarp();
-    const bool all_good = __syncthreads_and(good && !*abort_flag) != 0;
-
-    if (warp < DRAIN_WARPS) {
-        const int64_t gi = i0 + (warp & 3) * 32 + lane;
-        const int64_t gj0 = j0 + (warp >> 2) * 128;
-        if (gi < m) {
-            float *out = part ? part + (int64_t)blockIdx.y * m * n : dW;
-            const bool add = !part && accumulate;
-#pragma unroll
-            for (int q = 0; q < 128; ++q)
-                if (gj0 + q < n) {
-                    const float v = all_good ? acc[q] : __int_as_float(0x7fc00000);
-                    float *o = out + gi * n + gj0 + q;
-                    *o = add ? *o + v : v;
-                }
-        }
-    }
-    if (!all_good && threadIdx.x == 0) atomicOr(err, ST_TIMEOUT);
+    if (!good && lane == 0) atomicOr(err, ST_TIMEOUT);
     tc::fence_before_sync();
     __syncthreads();
-    if (warp == 0) tc::tmem_dealloc(tmem, 2 * TN);
+    if (rank == 1 && warp == 0) {   // the leader's last arrival here, after all its others
+        int never = 0;
+        tc::mbar_wait(tc::smem_u32(done), 0u, &never);
+    }
+    __syncwarp();
+    tc::cluster_sync();   // neither CTA's shared memory, barriers or TMEM are in use by the other any more
+    if (warp == 0) tc::tmem_dealloc_pair(tmem, 2 * TT);
 }
 
 __global__ void __launch_bounds__(256) weight_grad_reduce(int64_t count, int splits, const float *part, float *dW,
@@ -291,12 +324,12 @@ __global__ void __launch_bounds__(256) split_plane_kernel(int64_t T, int64_t m, 
 
 int64_t pad8(int64_t x) { return (x + 7) / 8 * 8; }
 
-// Token ranges: with fewer tiles than SMs, as many as fill them without
-// leaving a range under four stages.
+// Token ranges: with fewer tiles than pairs of SMs, as many as fill them without
+// leaving a range under eight stages.
 int grad_splits(int64_t T, int64_t m, int64_t n, int sms) {
-    const int64_t tiles = (int64_t)ceil_div(m, TM) * ceil_div(n, TN);
-    int64_t s = sms / tiles;
-    s = std::min<int64_t>(s, T / (4 * KSTAGE));
+    const int64_t tiles = (int64_t)ceil_div(m, TT) * ceil_div(n, TT);
+    int64_t s = sms / 2 / tiles;
+    s = std::min<int64_t>(s, T / (8 * KSTAGE));
     return (int)std::max<int64_t>(1, std::min<int64_t>(s, MAX_SPLITS));
 }
 
@@ -348,21 +381,30 @@ realq_status_t checkpoint_grad(cudaStream_t s, int64_t T, int64_t m, int64_t n, 
             split_plane_kernel<<<g, 256, 0, s>>>(T, m, static_cast<const float *>(dY), w.dy, ldy);
         REALQ_TRY(check_launch("checkpoint_grad_planes"));
     }
-    CUtensorMap mapA, mapB;
-    CUresult cr = encode_tmap_2d_bf16(&mapA, direct ? dY : (const void *)w.dy, (uint64_t)m, (uint64_t)(planes * T),
+    CUtensorMap mapY, mapX;
+    CUresult cr = encode_tmap_2d_bf16(&mapY, direct ? dY : (const void *)w.dy, (uint64_t)m, (uint64_t)(planes * T),
                                       (uint64_t)ldy * 2, 64, KSTAGE, 1);
     if (cr == CUDA_SUCCESS)
-        cr = encode_tmap_2d_bf16(&mapB, w.x, (uint64_t)n, (uint64_t)T, (uint64_t)ldx * 2, 64, KSTAGE, 1);
+        cr = encode_tmap_2d_bf16(&mapX, w.x, (uint64_t)n, (uint64_t)T, (uint64_t)ldx * 2, 64, KSTAGE, 1);
     if (cr != CUDA_SUCCESS) return fail(REALQ_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)cr);
     int64_t tper = (T + splits - 1) / splits;
     tper = (tper + KSTAGE - 1) / KSTAGE * KSTAGE;
     splits = (int)((T + tper - 1) / tper);
     REALQ_TRY(set_smem_limit(reinterpret_cast<const void *>(weight_grad_kernel), SMEM_BYTES));
-    const int64_t tiles = (int64_t)ceil_div(m, TM) * ceil_div(n, TN);
+    Work wk{};
+    wk.m = m;
+    wk.n = n;
+    wk.T = T;
+    wk.tper = tper;
+    wk.plane_rows = T;
+    wk.planes = planes;
+    wk.nti = ceil_div(n, TT);
+    wk.ntj = ceil_div(m, TT);
+    wk.items = wk.nti * wk.ntj * splits;
     {
         Launch L("checkpoint_weight_grad", s);
-        weight_grad_kernel<<<dim3((unsigned)tiles, (unsigned)splits), THREADS, SMEM_BYTES, s>>>(
-            mapA, mapB, planes, T, m, n, T, tper, dW, accumulate, splits > 1 ? w.part : nullptr, w.status);
+        weight_grad_kernel<<<(unsigned)(2 * std::min(wk.items, sms / 2)), THREADS, SMEM_BYTES, s>>>(
+            mapX, mapY, wk, dW, accumulate, splits > 1 ? w.part : nullptr, w.status);
     }
     REALQ_TRY(check_launch("checkpoint_weight_grad"));
     if (splits > 1) {
