@@ -24,15 +24,19 @@ namespace {
 
 constexpr unsigned FULL = 0xFFFFFFFFu;
 constexpr int THREADS = 256;
+constexpr int UN = 2;   // groups of eight values per thread
 
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }   // -126 <= e <= 127
 
 // bits of |x|: ordered like the magnitudes, infinities and NaN above all numbers
 __device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
 
-// x 2^(133 - b) in two exact steps (2^133 is no fp32 number)
-__device__ __forceinline__ int code_of(float x, float s1, float s2) {
-    return max(-127, min(127, __float2int_rn(x * s1 * s2)));
+// The code in the low byte.  x 2^(133 - b) in two exact steps (2^133 is no fp32
+// number); adding 1.5 2^23 rounds it to the nearest even whole number, which
+// then stands in the low mantissa bits.
+__device__ __forceinline__ uint32_t code_of(float x, float s1, float s2) {
+    const float y = fminf(fmaxf(x * s1 * s2, -127.f), 127.f);
+    return __float_as_uint(__fadd_rn(y, 12582912.f));
 }
 __device__ __forceinline__ void scales_of(uint32_t b, float &s1, float &s2) {
     const int up = 133 - (int)b, h = up >> 1;
@@ -74,46 +78,68 @@ __device__ __forceinline__ void store8(__nv_bfloat16 *p, const float (&v)[8]) {
 __device__ __forceinline__ void store1(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store1(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 
-// n a multiple of 32: rows end at block ends, so blocks are numbered through.
+// n a multiple of 32: rows end at block ends, so blocks are numbered through
+// and a thread takes UN groups of eight values, a CTA's width apart, with all
+// their loads in flight.
 template <typename TX>
 __global__ void __launch_bounds__(THREADS) pack_vec_kernel(int64_t groups, const TX *X, int8_t *codes, uint8_t *exps) {
-    // groups of eight values; 4 groups per block, so the lanes of a block are all in or all out
-    const int64_t g = (int64_t)blockIdx.x * THREADS + threadIdx.x;
-    if (g - (threadIdx.x & 31) >= groups) return;   // whole warps leave
-    const bool in = g < groups;
-    float v[8];
-    uint32_t m = 0;
-    if (in) {
-        load8(X + g * 8, v);
+    const int64_t g0 = (int64_t)blockIdx.x * (THREADS * UN) + threadIdx.x;
+    float v[UN][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m = max(m, mag(v[i]));
-    }
-    m = max(m, __shfl_xor_sync(FULL, m, 1));
-    m = max(m, __shfl_xor_sync(FULL, m, 2));
-    if (!in) return;
-    const uint32_t b = m >> 23;
-    float s1, s2;
-    scales_of(b, s1, s2);
-    uint32_t w[2] = {0, 0};
-    if (b < 255u) {
+    for (int k = 0; k < UN; ++k)
+        if (g0 + k * THREADS < groups) load8(X + (g0 + k * THREADS) * 8, v[k]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i >> 2] |= (uint32_t)(code_of(v[i], s1, s2) & 255) << (8 * (i & 3));
+    for (int k = 0; k < UN; ++k) {
+        const int64_t g = g0 + k * THREADS;
+        const bool in = g < groups;   // (4 groups a block: its lanes are all in or all out)
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, in ? mag(v[k][i]) : 0u);
+        m = max(m, __shfl_xor_sync(FULL, m, 1));
+        m = max(m, __shfl_xor_sync(FULL, m, 2));
+        if (!in) continue;
+        const uint32_t b = m >> 23;
+        float s1, s2;
+        scales_of(b, s1, s2);
+        uint32_t w[2] = {0, 0};
+        if (b < 255u) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                uint32_t q[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) q[j] = code_of(v[k][4 * i + j], s1, s2);
+                w[i] = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+            }
+        }
+        *reinterpret_cast<uint2 *>(codes + g * 8) = make_uint2(w[0], w[1]);
+        if ((threadIdx.x & 3) == 0) exps[g >> 2] = (uint8_t)b;
     }
-    *reinterpret_cast<uint2 *>(codes + g * 8) = make_uint2(w[0], w[1]);
-    if ((threadIdx.x & 3) == 0) exps[g >> 2] = (uint8_t)b;
 }
 
 template <typename TX>
 __global__ void __launch_bounds__(THREADS) unpack_vec_kernel(int64_t groups, const int8_t *codes, const uint8_t *exps,
                                                              TX *X) {
-    const int64_t g = (int64_t)blockIdx.x * THREADS + threadIdx.x;
-    if (g >= groups) return;
-    const uint2 w = *reinterpret_cast<const uint2 *>(codes + g * 8);
-    const float s = step_of(exps[g >> 2]);
-    float v[8];
+    const int64_t g0 = (int64_t)blockIdx.x * (THREADS * UN) + threadIdx.x;
+    uint2 w[UN];
+    uint32_t b[UN];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3))) * s;
-    store8(X + g * 8, v);
+    for (int k = 0; k < UN; ++k) {
+        const int64_t g = g0 + k * THREADS;
+        if (g < groups) {
+            w[k] = __ldg(reinterpret_cast<const uint2 *>(codes) + g);
+            b[k] = __ldg(exps + (g >> 2));
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < UN; ++k) {
+        const int64_t g = g0 + k * THREADS;
+        if (g >= groups) continue;
+        const float s = step_of(b[k]);
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)((i < 4 ? w[k].x : w[k].y) >> (8 * (i & 3))) * s;
+        store8(X + g * 8, v);
+    }
 }
 
 // Any width and alignment: warp b % nb of row b / nb.
@@ -128,7 +154,7 @@ __global__ void __launch_bounds__(THREADS) pack_row_kernel(int64_t T, int64_t n,
     const uint32_t b = __reduce_max_sync(FULL, mag(x)) >> 23;
     float s1, s2;
     scales_of(b, s1, s2);
-    if (c < n) codes[t * n + c] = b < 255u ? (int8_t)code_of(x, s1, s2) : 0;
+    if (c < n) codes[t * n + c] = b < 255u ? (int8_t)(code_of(x, s1, s2) & 255u) : 0;
     if (lane == 0) exps[w] = (uint8_t)b;
 }
 
@@ -151,7 +177,7 @@ static void pack_launch(cudaStream_t s, int64_t T, int64_t n, const TX *X, int8_
     const int64_t nb = (n + 31) / 32, groups = T * n / 8;
     Launch L("checkpoint_pack", s);
     if (n % 32 == 0 && aligned16(X) && aligned16(codes))
-        pack_vec_kernel<TX><<<(unsigned)((groups + THREADS - 1) / THREADS), THREADS, 0, s>>>(groups, X, codes, exps);
+        pack_vec_kernel<TX><<<(unsigned)((groups + THREADS * UN - 1) / (THREADS * UN)), THREADS, 0, s>>>(groups, X, codes, exps);
     else
         pack_row_kernel<TX><<<(unsigned)((T * nb * 32 + THREADS - 1) / THREADS), THREADS, 0, s>>>(T, n, nb, X, codes,
                                                                                                   exps);
@@ -162,7 +188,7 @@ static void unpack_launch(cudaStream_t s, int64_t T, int64_t n, const int8_t *co
     const int64_t nb = (n + 31) / 32, groups = T * n / 8;
     Launch L("checkpoint_unpack", s);
     if (n % 32 == 0 && aligned16(X) && aligned16(codes))
-        unpack_vec_kernel<TX><<<(unsigned)((groups + THREADS - 1) / THREADS), THREADS, 0, s>>>(groups, codes, exps, X);
+        unpack_vec_kernel<TX><<<(unsigned)((groups + THREADS * UN - 1) / (THREADS * UN)), THREADS, 0, s>>>(groups, codes, exps, X);
     else
         unpack_row_kernel<TX><<<(unsigned)((T * nb * 32 + THREADS - 1) / THREADS), THREADS, 0, s>>>(T, n, nb, codes,
                                                                                                     exps, X);

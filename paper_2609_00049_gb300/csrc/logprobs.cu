@@ -7,7 +7,7 @@
 // so one pass with running (m, s, u) gives all three.  The row is read once
 // from HBM, which bounds the kernel.  A CTA owns a row; when there are too few
 // rows to fill the SMs, a cluster of up to eight CTAs shares one and joins its
-// parts through distributed shared memory in rank order.
+// parts through distributed shared memory in a fixed order.
 //
 // The k likeliest in the same pass: each thread notes the maximum of every
 // 64-byte run it reads (runs merged so that it has at most 16 notes).  The two
@@ -68,7 +68,14 @@ template <> struct Vec<float> {
     static __device__ __forceinline__ uint4 join(const float (&v)[4]) {
         return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
     }
-    static __device__ __forceinline__ float round1(float v) { return v; }
+    static __device__ __forceinline__ float top(const uint4 (&r)[U]) {
+        float m = neg_inf();
+#pragma unroll
+        for (int q = 0; q < U; ++q)
+            m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(r[q].x), __uint_as_float(r[q].y)),
+                               fmaxf(__uint_as_float(r[q].z), __uint_as_float(r[q].w))));
+        return m;
+    }
 };
 template <> struct Vec<__nv_bfloat16> {
     static constexpr int E = 8;
@@ -91,6 +98,15 @@ template <> struct Vec<__nv_bfloat16> {
             w[i] = *reinterpret_cast<const uint32_t *>(&h);
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    static __device__ __forceinline__ float top(const uint4 (&r)[U]) {   // pairwise in bf16, exact
+        __nv_bfloat162 m = __halves2bfloat162(__ushort_as_bfloat16(0xFF80), __ushort_as_bfloat16(0xFF80));
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
+            const __nv_bfloat162 *h = reinterpret_cast<const __nv_bfloat162 *>(&r[q]);
+            m = __hmax2(m, __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
+        }
+        return fmaxf(__low2float(m), __high2float(m));
     }
 };
 __device__ __forceinline__ void store1(float *p, float v) { *p = v; }
@@ -125,34 +141,90 @@ __device__ __forceinline__ void raise(Stat &a, float m) {   // a's sums relative
     a.s *= c;
     a.m = m;
 }
-__device__ __forceinline__ Stat join(Stat a, Stat b) {
-    const float m = fmaxf(a.m, b.m);
+// two fp32 numbers in one register pair
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t r, float &a, float &b) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r));
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+// two logits into pairs of partial sums (nbase = minus the maximum, twice)
+__device__ __forceinline__ void add_pair(uint64_t &s, uint64_t &u, float x0, float x1, uint64_t nbase) {
+    const uint64_t t = mul2(add2(pack2(x0, x1), nbase), pack2(LOG2E, LOG2E));
+    float t0, t1;
+    unpack2(t, t0, t1);
+    const uint64_t e = pack2(ex2(t0), ex2(t1));
+    s = add2(s, e);
+    // (e is 0 below -200: -inf and the type's lowest value stay out of the product)
+    u = fma2(e, pack2(fmaxf(t0, -200.f), fmaxf(t1, -200.f)), u);
+}
+
+// The warp's largest value (no NaN among them): one reduction of integers in the order of the floats.
+__device__ __forceinline__ float warp_max(float v) {
+    const int b = __float_as_int(v), m = __reduce_max_sync(FULL, b ^ ((b >> 31) & 0x7FFFFFFF));
+    return __int_as_float(m ^ ((m >> 31) & 0x7FFFFFFF));
+}
+// the warp's joined sums, on each lane
+__device__ __forceinline__ Stat join_warp(Stat a) {
+    const float m = warp_max(a.m);
     if (a.m < m) raise(a, m);
-    if (b.m < m) raise(b, m);
-    return Stat{m, a.s + b.s, a.u + b.u};
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        a.s += __shfl_xor_sync(FULL, a.s, o);
+        a.u += __shfl_xor_sync(FULL, a.u, o);
+    }
+    a.m = m;
+    return a;
 }
-__device__ __forceinline__ void add(Stat &a, float x, float base) {
-    const float t = (x - base) * LOG2E, e = ex2(t);
-    a.s += e;
-    a.u += e * fmaxf(t, -200.f);   // e is 0 there; -inf and the type's lowest value stay out of the product
+
+// A candidate as one number: larger values first, equal ones by the lower index.
+__device__ __forceinline__ uint64_t key_of(float v, int i) {
+    const uint32_t b = __float_as_uint(v + 0.f);   // (-0 counts as 0)
+    return (uint64_t)(b & 0x80000000u ? ~b : b | 0x80000000u) << 32 | (uint32_t)(INT32_MAX - i);
 }
+__device__ __forceinline__ float key_value(uint64_t k) {
+    const uint32_t b = (uint32_t)(k >> 32);
+    return __uint_as_float(b & 0x80000000u ? b & 0x7FFFFFFFu : ~b);
+}
+__device__ __forceinline__ int key_index(uint64_t k) { return INT32_MAX - (int)(uint32_t)k; }
 
 __device__ __forceinline__ bool before(float va, int ia, float vb, int ib) { return va > vb || (va == vb && ia < ib); }
 
 struct FwdSmem {
     float note[NOTES][NT];
-    float cv[CAP];
-    int ci[CAP];
-    float topv[KMAX];
-    int topi[KMAX];
+    uint64_t cand[CAP];
+    uint64_t top[KMAX];       // keys, 0 where there is none
     float wmax[32];
     Stat part[16];
     Stat total;
-    float rv[16];
-    int ri[16];
+    uint64_t best[16];
     float tau;
     int count;
 };
+// the place of key among n others (none equal)
+__device__ __forceinline__ int place_of(const uint64_t *keys, int n, uint64_t key) {
+    int above = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) above += keys[j] > key;
+    return above;
+}
 
 template <typename TX>
 __global__ void __launch_bounds__(NT, 2)
@@ -176,35 +248,49 @@ __global__ void __launch_bounds__(NT, 2)
     if (rank == CL - 1 && tid >= NT - row.tail) scol = V - (NT - tid);
     const float sx = scol >= 0 ? load_as_float(row.p, scol) : neg_inf();
 
-    Stat st{neg_inf(), 0.f, 0.f};
-    float tmax = sx, note = neg_inf();
-    if (scol >= 0) {
-        st.m = sx;
-        add(st, sx, sx == neg_inf() ? 0.f : sx);
-        if (!(sx == sx)) st.m = neg_inf();   // a NaN is kept in s alone
+    int64_t y = -1;   // the target, fetched early
+    float xy = 0.f;
+    if (logprob && rank == 0 && tid == 0) {
+        y = targets[r];
+        if (y >= 0 && y < V) xy = load_as_float(row.p, y);
     }
-    if (!(tmax == tmax)) tmax = neg_inf();
-    for (int it = 0; it < iters; ++it) {
-        uint4 raw[U];
+
+    Stat st{neg_inf(), 0.f, 0.f};
+    float note = neg_inf();
+    if (scol >= 0) {   // e^0 = 1; a NaN or +inf is kept in s as a NaN, with or without its maximum
+        st.m = sx == sx ? sx : neg_inf();
+        st.s = sx == neg_inf() ? 0.f : 1.f + (sx - sx);
+    }
+    uint4 raw[U];
+    auto load = [&](int it) {
         const int b = v0 + it * (NT * U) + tid;
 #pragma unroll
         for (int q = 0; q < U; ++q) raw[q] = b + q * NT < v1 ? row.vec(b + q * NT) : Vec<TX>::fill();
-        float x[U][E];
-        float cm = neg_inf();
+    };
+    if (iters > 0) load(0);
+    for (int it = 0; it < iters; ++it) {
+        uint4 cur[U];
+#pragma unroll
+        for (int q = 0; q < U; ++q) cur[q] = raw[q];
+        if (it + 1 < iters) load(it + 1);   // in flight during this one's arithmetic
+        const float cm = Vec<TX>::top(cur);
+        if (cm > st.m) raise(st, cm);
+        const float nb = st.m == neg_inf() ? 0.f : -st.m;
+        const uint64_t nbase = pack2(nb, nb);
+        uint64_t s2 = pack2(st.s, 0.f), u2 = pack2(st.u, 0.f);
 #pragma unroll
         for (int q = 0; q < U; ++q) {
-            Vec<TX>::split(raw[q], x[q]);
+            float x[E];
+            Vec<TX>::split(cur[q], x);
 #pragma unroll
-            for (int e = 0; e < E; ++e) cm = fmaxf(cm, x[q][e]);
+            for (int e = 0; e < E; e += 2) add_pair(s2, u2, x[e], x[e + 1], nbase);
         }
-        if (cm > st.m) raise(st, cm);
-        const float base = st.m == neg_inf() ? 0.f : st.m;
-#pragma unroll
-        for (int q = 0; q < U; ++q)
-#pragma unroll
-            for (int e = 0; e < E; ++e) add(st, x[q][e], base);
+        float a, b;
+        unpack2(s2, a, b);
+        st.s = a + b;
+        unpack2(u2, a, b);
+        st.u = a + b;
         note = fmaxf(note, cm);
-        tmax = fmaxf(tmax, cm);
         if (k > 0 && (it + 1 == iters || ((it + 1) >> shift) != (it >> shift))) {
             sm.note[it >> shift][tid] = note;
             note = neg_inf();
@@ -212,49 +298,29 @@ __global__ void __launch_bounds__(NT, 2)
     }
 
     // ---- join the threads' sums ----
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        Stat b;
-        b.m = __shfl_xor_sync(FULL, st.m, o);
-        b.s = __shfl_xor_sync(FULL, st.s, o);
-        b.u = __shfl_xor_sync(FULL, st.u, o);
-        st = join(st, b);
-    }
-    if (lane == 0) sm.part[warp] = st;
-    if (k > 0) {
-        float w1 = tmax;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) w1 = fmaxf(w1, __shfl_xor_sync(FULL, w1, o));
-        const int holder = __ffs(__ballot_sync(FULL, tmax == w1)) - 1;
-        float w2 = lane == holder ? neg_inf() : tmax;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) w2 = fmaxf(w2, __shfl_xor_sync(FULL, w2, o));
+    const Stat joined = join_warp(st);
+    if (lane == 0) sm.part[warp] = joined;
+    if (k > 0) {   // (st.m is the thread's maximum)
+        const float w1 = joined.m;
+        const int holder = __ffs(__ballot_sync(FULL, st.m == w1)) - 1;
+        const float w2 = warp_max(lane == holder ? neg_inf() : st.m);
         if (lane == 0) {
             sm.wmax[2 * warp] = w1;
             sm.wmax[2 * warp + 1] = w2;
         }
-        if (tid < KMAX) {
-            sm.topv[tid] = neg_inf();
-            sm.topi[tid] = -1;
-        }
+        if (tid < KMAX) sm.top[tid] = 0;
         if (tid == 0) sm.count = 0;
     }
     __syncthreads();
     if (warp == 0) {
-        if (lane == 0) {
-            Stat t = sm.part[0];
-            for (int w = 1; w < NT / 32; ++w) t = join(t, sm.part[w]);
-            sm.total = t;
-        }
-        if (k > 0) {
-            const float v = sm.wmax[lane];
-            int above = 0;
-            for (int j = 0; j < 32; ++j) {
-                const float o = __shfl_sync(FULL, v, j);
-                above += before(o, j, v, lane);
-            }
-            if (above == k - 1) sm.tau = v;
-        }
+        const Stat t = join_warp(lane < NT / 32 ? sm.part[lane] : Stat{neg_inf(), 0.f, 0.f});
+        if (lane == 0) sm.total = t;
+    } else if (warp == 1 && k > 0) {
+        const float v = sm.wmax[lane];
+        int above = 0;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) above += before(sm.wmax[j], j, v, lane);
+        if (above == k - 1) sm.tau = v;
     }
     __syncthreads();
 
@@ -264,10 +330,7 @@ __global__ void __launch_bounds__(NT, 2)
         auto offer = [&](float x, int col) {
             if (x >= tau && x > neg_inf()) {
                 const int at = atomicAdd(&sm.count, 1);
-                if (at < CAP) {
-                    sm.cv[at] = x;
-                    sm.ci[at] = col;
-                }
+                if (at < CAP) sm.cand[at] = key_of(x, col);
             }
         };
         if (scol >= 0) offer(sx, scol);
@@ -275,41 +338,39 @@ __global__ void __launch_bounds__(NT, 2)
         for (int n = 0; n < nn; ++n) {
             const float top = sm.note[n][tid];
             if (!(top >= tau && top > neg_inf())) continue;
-            for (int it = n << shift; it < min(iters, (n + 1) << shift); ++it)
+            for (int it = n << shift; it < min(iters, (n + 1) << shift); ++it) {
+                if (iters > 1) load(it);   // (a single run is still in registers)
+#pragma unroll
                 for (int q = 0; q < U; ++q) {
                     const int v = v0 + it * (NT * U) + q * NT + tid;
-                    if (v >= v1) continue;
                     float x[E];
-                    Vec<TX>::split(row.vec(v), x);
+                    Vec<TX>::split(raw[q], x);
+                    float mx = x[0];
 #pragma unroll
-                    for (int e = 0; e < E; ++e) offer(x[e], row.head + v * E + e);
+                    for (int e = 1; e < E; ++e) mx = fmaxf(mx, x[e]);
+                    if (mx >= tau) {   // (what lies past the end reads as -inf)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) offer(x[e], row.head + v * E + e);
+                    }
                 }
+            }
         }
         __syncthreads();
         const int C = sm.count;
         if (C <= CAP) {
             for (int i = tid; i < C; i += NT) {
-                const float v = sm.cv[i];
-                const int c = sm.ci[i];
-                int above = 0;
-                for (int j = 0; j < C; ++j) above += before(sm.cv[j], sm.ci[j], v, c);
-                if (above < k) {
-                    sm.topv[above] = v;
-                    sm.topi[above] = c;
-                }
+                const uint64_t key = sm.cand[i];
+                const int at = place_of(sm.cand, C, key);
+                if (at < k) sm.top[at] = key;
             }
         } else {
             // too many equal values: the k first of the row's order, one at a time
-            float pv = __int_as_float(0x7F800000);
-            int pi = -1;
+            uint64_t last = ~0ull;
             for (int j = 0; j < k; ++j) {
-                float bv = neg_inf();
-                int bi = INT32_MAX;
+                uint64_t best = 0;
                 auto see = [&](float x, int col) {
-                    if (x > neg_inf() && before(pv, pi, x, col) && before(x, col, bv, bi)) {
-                        bv = x;
-                        bi = col;
-                    }
+                    const uint64_t key = key_of(x, col);
+                    if (x > neg_inf() && key < last && key > best) best = key;
                 };
                 if (scol >= 0) see(sx, scol);
                 for (int v = v0 + tid; v < v1; v += NT) {
@@ -319,34 +380,15 @@ __global__ void __launch_bounds__(NT, 2)
                     for (int e = 0; e < E; ++e) see(x[e], row.head + v * E + e);
                 }
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) {
-                    const float ov = __shfl_xor_sync(FULL, bv, o);
-                    const int oi = __shfl_xor_sync(FULL, bi, o);
-                    if (before(ov, oi, bv, bi)) {
-                        bv = ov;
-                        bi = oi;
-                    }
-                }
-                if (lane == 0) {
-                    sm.rv[warp] = bv;
-                    sm.ri[warp] = bi;
-                }
+                for (int o = 16; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(FULL, best, o));
+                if (lane == 0) sm.best[warp] = best;
                 __syncthreads();
-                bv = sm.rv[0];
-                bi = sm.ri[0];
-                for (int w = 1; w < NT / 32; ++w)
-                    if (before(sm.rv[w], sm.ri[w], bv, bi)) {
-                        bv = sm.rv[w];
-                        bi = sm.ri[w];
-                    }
+#pragma unroll
+                for (int w = 0; w < NT / 32; ++w) best = max(best, sm.best[w]);
                 __syncthreads();
-                if (bv == neg_inf()) break;   // (the same on every thread)
-                if (tid == 0) {
-                    sm.topv[j] = bv;
-                    sm.topi[j] = bi;
-                }
-                pv = bv;
-                pi = bi;
+                if (best == 0) break;   // (the same on every thread)
+                if (tid == 0) sm.top[j] = best;
+                last = best;
             }
         }
         __syncthreads();
@@ -356,32 +398,20 @@ __global__ void __launch_bounds__(NT, 2)
     if (CL > 1) {
         cluster.sync();
         if (rank == 0) {
-            if (tid == 0) {
-                Stat t = sm.total;
-                for (int c = 1; c < CL; ++c) t = join(t, *cluster.map_shared_rank(&sm.total, c));
-                sm.total = t;
+            Stat t{neg_inf(), 0.f, 0.f};
+            if (warp == NT / 32 - 1) {
+                if (lane < CL) t = *cluster.map_shared_rank(&sm.total, lane);
+                t = join_warp(t);
             }
-            const bool mine = tid < CL * k;
-            if (mine) {
-                const FwdSmem *o = cluster.map_shared_rank(&sm, tid / k);
-                sm.cv[tid] = o->topv[tid % k];
-                sm.ci[tid] = o->topi[tid % k];
-            }
+            const int c = tid < CL * k ? tid / k : -1;
+            const uint64_t key = c >= 0 ? cluster.map_shared_rank(&sm, c)->top[tid - c * k] : 0;
+            if (c >= 0) sm.cand[tid] = key;
             __syncthreads();
-            if (k > 0 && tid < k) {
-                sm.topv[tid] = neg_inf();
-                sm.topi[tid] = -1;
-            }
+            if (tid == NT - 1) sm.total = t;
+            if (tid < k) sm.top[tid] = 0;
+            const int at = key ? place_of(sm.cand, CL * k, key) : k;
             __syncthreads();
-            if (mine && sm.ci[tid] >= 0) {
-                int above = 0;
-                for (int j = 0; j < CL * k; ++j)
-                    above += sm.ci[j] >= 0 && before(sm.cv[j], sm.ci[j], sm.cv[tid], sm.ci[tid]);
-                if (above < k) {
-                    sm.topv[above] = sm.cv[tid];
-                    sm.topi[above] = sm.ci[tid];
-                }
-            }
+            if (at < k) sm.top[at] = key;
             __syncthreads();
         }
         cluster.sync();   // the other CTAs' shared memory has been read
@@ -402,19 +432,18 @@ __global__ void __launch_bounds__(NT, 2)
             entropy[r] = bad ? nan_f() : (H < 0.f ? 0.f : H);
         }
         if (logprob) {
-            const int64_t y = targets[r];
             float lp = 0.f;
             if (y >= V)
                 lp = nan_f();
             else if (y >= 0)
-                lp = empty ? neg_inf() : (load_as_float(row.p, y) - m) - ls;
+                lp = empty ? neg_inf() : (xy - m) - ls;
             logprob[r] = lp;
         }
     }
     if (tid < k) {
-        const int id = bad ? -1 : sm.topi[tid];
-        top_ids[r * k + tid] = id;
-        if (top_lp) top_lp[r * k + tid] = bad ? nan_f() : (id >= 0 ? (sm.topv[tid] - m) - ls : neg_inf());
+        const uint64_t key = bad ? 0 : sm.top[tid];
+        top_ids[r * k + tid] = key ? key_index(key) : -1;
+        if (top_lp) top_lp[r * k + tid] = bad ? nan_f() : (key ? (key_value(key) - m) - ls : neg_inf());
     }
 }
 
