@@ -10,8 +10,8 @@
 // parts through distributed shared memory in a fixed order.
 //
 // The k likeliest in the same pass: each thread notes the maximum of every
-// 64-byte run it reads (runs merged so that it has at most 16 notes).  The two
-// largest thread maxima of each of the 16 warps are 32 different elements of
+// 64-byte run it reads (runs merged so that it has at most 32 notes).  The four
+// largest thread maxima of each of the 8 warps are 32 different elements of
 // the row, so the k-th largest of them is a lower bound tau of the k-th
 // largest element.  Only runs whose note reaches tau are read again (from L2),
 // their elements >= tau collected and ranked by (value, lower index).  Where
@@ -38,9 +38,10 @@ namespace {
 constexpr unsigned FULL = 0xFFFFFFFFu;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
-constexpr int NT = 512;       // threads of a forward CTA (16 warps: 32 maxima for tau)
+constexpr int NT = 256;       // threads of a forward CTA
+constexpr int PER_WARP = 1024 / NT;   // thread maxima that each warp gives for tau (32 in all)
 constexpr int U = 4;          // 16-byte loads in flight per thread
-constexpr int NOTES = 16;     // run maxima kept per thread
+constexpr int NOTES = 32;     // run maxima kept per thread
 constexpr int CAP = 1024;     // collected candidates
 constexpr int KMAX = 32;
 constexpr int MAX_CLUSTER = 8;
@@ -212,9 +213,9 @@ struct FwdSmem {
     uint64_t cand[CAP];
     uint64_t top[KMAX];       // keys, 0 where there is none
     float wmax[32];
-    Stat part[16];
+    Stat part[NT / 32];
     Stat total;
-    uint64_t best[16];
+    uint64_t best[NT / 32];
     float tau;
     int count;
 };
@@ -227,7 +228,7 @@ __device__ __forceinline__ int place_of(const uint64_t *keys, int n, uint64_t ke
 }
 
 template <typename TX>
-__global__ void __launch_bounds__(NT, 2)
+__global__ void __launch_bounds__(NT, 1024 / NT)
     logprobs_kernel(int V, int64_t ld, const TX *X, const int64_t *targets, float *logprob, float *norm,
                     float *entropy, int k, int64_t *top_ids, float *top_lp) {
     constexpr int E = Vec<TX>::E;
@@ -301,12 +302,12 @@ __global__ void __launch_bounds__(NT, 2)
     const Stat joined = join_warp(st);
     if (lane == 0) sm.part[warp] = joined;
     if (k > 0) {   // (st.m is the thread's maximum)
-        const float w1 = joined.m;
-        const int holder = __ffs(__ballot_sync(FULL, st.m == w1)) - 1;
-        const float w2 = warp_max(lane == holder ? neg_inf() : st.m);
-        if (lane == 0) {
-            sm.wmax[2 * warp] = w1;
-            sm.wmax[2 * warp + 1] = w2;
+        float v = st.m, top = joined.m;
+#pragma unroll
+        for (int p = 0; p < PER_WARP; ++p) {
+            if (p > 0) top = warp_max(v);
+            if (lane == 0) sm.wmax[PER_WARP * warp + p] = top;
+            if (lane == __ffs(__ballot_sync(FULL, v == top)) - 1) v = neg_inf();
         }
         if (tid < KMAX) sm.top[tid] = 0;
         if (tid == 0) sm.count = 0;
@@ -562,10 +563,10 @@ template <typename TX>
 realq_status_t fwd_launch(cudaStream_t s, int64_t T, int64_t V, int64_t ld, const void *X, const int64_t *targets,
                           float *logprob, float *norm, float *entropy, int k, int64_t *top_ids, float *top_lp,
                           int sms) {
-    // Two CTAs fit an SM.  A row gets as many CTAs (a power of two up to 8) as
+    // Four CTAs fit an SM.  A row gets as many CTAs (a power of two up to 8) as
     // leave no second wave; each should still have a full pass of vectors.
     int cl = 1;
-    while (cl < MAX_CLUSTER && T * cl * 2 <= 2 * (int64_t)sms && V / (2 * cl) >= (int64_t)NT * Vec<TX>::E) cl *= 2;
+    while (cl < MAX_CLUSTER && T * cl * 2 <= 1024 / NT * (int64_t)sms && V / (2 * cl) >= (int64_t)NT * Vec<TX>::E) cl *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(T * cl));
     cfg.blockDim = dim3(NT);

@@ -246,7 +246,7 @@ def test_logprobs_match_the_definition(T, V, dtype, masked):
         check_forward(forward(x, y, k), forward_exact(x, y, k), V, k)
 
 
-def test_logprobs_of_a_vocabulary_past_16_notes():
+def test_logprobs_of_a_vocabulary_past_the_notes():
     """Rows so long that a thread's run maxima are merged."""
     x, y = logits_case(2, 1_500_003, torch.float32, "")
     x[0, 7], x[0, 1_500_002], x[1, 750_000] = 40.0, 40.0, 41.0
