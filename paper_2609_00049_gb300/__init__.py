@@ -89,6 +89,7 @@ def bgd_cfg(lr, steps_per_block=1, optimizer=REALQ_OPT_ADAM, beta1=0.9, beta2=0.
     return BgdCfg(steps_per_block, optimizer, lr, beta1, beta2, eps, b_global_start, B_total)
 
 
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 _lib = None
 _vp, _i64, _sz, _int, _f32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_size_t, ctypes.c_int, ctypes.c_float
 _f64 = ctypes.c_double
@@ -218,7 +219,7 @@ def _ptr(t: Optional[torch.Tensor]):
         raise ValueError("expected a CUDA tensor")
     if not t.is_contiguous():
         raise ValueError("expected a contiguous tensor")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()   # (an int: the declared argument types convert it)
 
 
 def _dtype(t: torch.Tensor) -> int:
@@ -229,15 +230,15 @@ def _dtype(t: torch.Tensor) -> int:
     raise ValueError(f"unsupported dtype {t.dtype}")
 
 
-def _stream(stream) -> ctypes.c_void_p:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+def _stream(stream) -> int:
+    # the current stream's handle without the Stream object around it, which takes longer to make than a small kernel
+    return _raw_stream(_current_device()) if stream is None else stream.cuda_stream
 
 
 def _need(t, dtype, shape, name):
     if t is None:
         return
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
 
 
@@ -394,7 +395,7 @@ def _rows(t: torch.Tensor, name: str):
         raise ValueError(f"{name}: expected a matrix with contiguous, non-overlapping rows")
     if not t.is_cuda:
         raise ValueError("expected a CUDA tensor")
-    return ctypes.c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
 
 
 def realq_int8_product_workspace_size(T: int, n: int, m: int, w_bits: int = 8) -> int:
@@ -768,7 +769,7 @@ def _block_weights(w: dict, dims: Optional[BlockDims] = None) -> BlockWeights:
             raise ValueError(f"block weight {k}: expected shape {shapes[k]}, got {tuple(t.shape)}")
     out = BlockWeights()
     for k in _BLOCK_KEYS:
-        setattr(out, k, _ptr(w[k]).value)
+        setattr(out, k, _ptr(w[k]))
     return out
 
 
