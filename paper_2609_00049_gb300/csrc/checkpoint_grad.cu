@@ -87,6 +87,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     uint32_t *tslot = reinterpret_cast<uint32_t *>(done + 1);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tslot + 1);
 
+    dependents_may_start();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = tc::cluster_rank();
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
@@ -117,6 +118,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     if (warp == DRAIN_WARPS) {
         if (lane == 0) {
             // ---------------- TMA producer: this CTA's channels ----------------
+            wait_for_previous();   // the planes
             int s = 0, it = 0;
             uint32_t phase = 0;
             bool ok = true;
@@ -256,70 +258,128 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     if (warp == 0) tc::tmem_dealloc_pair(tmem, 2 * TT);
 }
 
+// parts added in their order, four neighbours to a thread
 __global__ void __launch_bounds__(256) weight_grad_reduce(int64_t count, int splits, const float *part, float *dW,
                                                           int accumulate) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    wait_for_previous();
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
     if (i >= count) return;
-    float v = part[i];
-    for (int z = 1; z < splits; ++z) v += part[z * count + i];
-    dW[i] = accumulate ? dW[i] + v : v;
+    const int left = (int)min((int64_t)4, count - i);
+    if (left == 4 && count % 4 == 0 && (reinterpret_cast<uintptr_t>(dW) & 15) == 0) {
+        float4 v = __ldg(reinterpret_cast<const float4 *>(part + i));
+#pragma unroll 4
+        for (int z = 1; z < splits; ++z) {
+            const float4 p = __ldg(reinterpret_cast<const float4 *>(part + z * count + i));
+            v.x += p.x;
+            v.y += p.y;
+            v.z += p.z;
+            v.w += p.w;
+        }
+        float4 *o = reinterpret_cast<float4 *>(dW + i);
+        if (accumulate) {
+            const float4 d = *o;
+            v = make_float4(d.x + v.x, d.y + v.y, d.z + v.z, d.w + v.w);
+        }
+        *o = v;
+        return;
+    }
+    for (int k = 0; k < left; ++k) {
+        float v = part[i + k];
+        for (int z = 1; z < splits; ++z) v += part[z * count + i + k];
+        dW[i + k] = accumulate ? dW[i + k] + v : v;
+    }
 }
 
-// X̂ as a bf16 plane of row stride ldx (columns from n on are not written and
-// lie outside the tensor map).  A thread unpacks 16 values (half a block) where
-// rows are whole blocks, else a warp a block.
+// 2^(b - 133), subnormal below b = 7; NaN for b = 255
 __device__ __forceinline__ float step_of(uint32_t b) {
     if (b == 255u) return __int_as_float(0x7FC00000);
     return __uint_as_float(b >= 7u ? (b - 6u) << 23 : 1u << (b + 16u));
 }
-__global__ void __launch_bounds__(256) unpack_plane_vec_kernel(int64_t count, const uint4 *codes, const uint8_t *exps,
-                                                               uint4 *X) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= count) return;
-    const uint4 q = __ldg(codes + i);
-    const float s = step_of(__ldg(exps + (i >> 1)));
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-    uint32_t h[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {   // (bf16 numbers: the upper halves are exact)
-        const float lo = (float)(int8_t)(w[k >> 1] >> (16 * (k & 1))) * s;
-        const float hi = (float)(int8_t)(w[k >> 1] >> (16 * (k & 1) + 8)) * s;
-        h[k] = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
-    }
-    X[2 * i] = make_uint4(h[0], h[1], h[2], h[3]);
-    X[2 * i + 1] = make_uint4(h[4], h[5], h[6], h[7]);
-}
-__global__ void __launch_bounds__(256) unpack_plane_kernel(int64_t T, int64_t n, int64_t nb, const int8_t *codes,
-                                                           const uint8_t *exps, __nv_bfloat16 *X, int64_t ldx) {
-    const int lane = threadIdx.x & 31;
-    const int64_t w = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 5;
-    if (w >= T * nb) return;
-    const int64_t t = w / nb, c = (w % nb) * 32 + lane;
-    if (c < n) X[t * ldx + c] = __float2bfloat16_rn((float)codes[t * n + c] * step_of(exps[w]));
+// two fp32 numbers that are bf16 numbers, as a bf16 pair
+__device__ __forceinline__ uint32_t upper2(float lo, float hi) {
+    return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
 }
 
-// dY's planes: bf16 copied to an aligned row stride, fp32 as three bf16 planes
-__global__ void __launch_bounds__(256) copy_plane_kernel(int64_t T, int64_t m, const __nv_bfloat16 *dY,
-                                                         __nv_bfloat16 *out, int64_t ld) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= T * m) return;
-    out[i / m * ld + i % m] = dY[i];
-}
-__global__ void __launch_bounds__(256) split_plane_kernel(int64_t T, int64_t m, const float *dY, __nv_bfloat16 *out,
-                                                          int64_t ld) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= T * m) return;
-    const float v = dY[i];
+// fp32 v = hi + mid + lo, each of eight significant bits, by truncation (an
+// infinity or NaN stays in hi; a NaN whose payload lies in the lower half must
+// not become an infinity)
+__device__ __forceinline__ void split3(float v, float &hi, float &mid, float &lo) {
     const bool num = (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u;
-    const uint32_t hi = __float_as_uint(v) & 0xFFFF0000u;
-    const float r1 = num ? v - __uint_as_float(hi) : 0.f;   // infinities and NaN stay in the first plane
-    const uint32_t mid = __float_as_uint(r1) & 0xFFFF0000u;
-    const uint32_t lo = __float_as_uint(r1 - __uint_as_float(mid)) & 0xFFFF0000u;
-    const int64_t at = i / m * ld + i % m, plane = T * ld;
-    // (a NaN whose payload lies in the lower half must not become an infinity)
-    out[at] = num ? __ushort_as_bfloat16((unsigned short)(hi >> 16)) : __float2bfloat16_rn(v);
-    out[at + plane] = __ushort_as_bfloat16((unsigned short)(mid >> 16));
-    out[at + 2 * plane] = __ushort_as_bfloat16((unsigned short)(lo >> 16));
+    hi = num ? __uint_as_float(__float_as_uint(v) & 0xFFFF0000u) : __bfloat162float(__float2bfloat16_rn(v));
+    const float r = num ? v - hi : 0.f;
+    mid = __uint_as_float(__float_as_uint(r) & 0xFFFF0000u);
+    lo = r - mid;
+}
+
+// The operands' planes, in one launch: the first xblocks blocks unpack X̂ to
+// bf16 (row stride ldx), the others bring dY to its planes (bf16 copied to an
+// aligned row stride, fp32 split in three).  XV: rows of X̂ are whole blocks of
+// 32 (16 values a thread; otherwise a warp a block); YV: fp32 rows of whole
+// 16-byte pieces.  Columns past the widths are not written and lie outside the
+// tensor maps.
+struct Planes {
+    int64_t T, n, m, ldx, ldy;
+    unsigned xblocks;
+    const int8_t *codes;
+    const uint8_t *exps;
+    __nv_bfloat16 *x;
+    const void *dY;
+    int dy_f32;
+    __nv_bfloat16 *dy;
+    int *status;
+};
+template <bool XV, bool YV>
+__global__ void __launch_bounds__(256) grad_planes_kernel(const Planes p) {
+    dependents_may_start();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = 0;
+    if (blockIdx.x < p.xblocks) {
+        const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+        if (XV) {
+            if (i >= p.T * p.n / 16) return;
+            const uint4 q = __ldg(reinterpret_cast<const uint4 *>(p.codes) + i);
+            const float s = step_of(__ldg(p.exps + (i >> 1)));
+            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+            uint32_t h[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                h[k] = upper2((float)(int8_t)(w[k >> 1] >> (16 * (k & 1))) * s,
+                              (float)(int8_t)(w[k >> 1] >> (16 * (k & 1) + 8)) * s);
+            uint4 *o = reinterpret_cast<uint4 *>(p.x) + 2 * i;
+            o[0] = make_uint4(h[0], h[1], h[2], h[3]);
+            o[1] = make_uint4(h[4], h[5], h[6], h[7]);
+        } else {
+            const int64_t nb = (p.n + 31) / 32, w = i >> 5;
+            if (w >= p.T * nb) return;
+            const int64_t t = w / nb, c = (w % nb) * 32 + (threadIdx.x & 31);
+            if (c < p.n) p.x[t * p.ldx + c] = __float2bfloat16_rn((float)p.codes[t * p.n + c] * step_of(p.exps[w]));
+        }
+        return;
+    }
+    const int64_t i = (int64_t)(blockIdx.x - p.xblocks) * 256 + threadIdx.x, plane = p.T * p.ldy;
+    if (YV) {   // (m a multiple of 8, so ldy = m)
+        if (i >= p.T * p.m / 4) return;
+        const float4 v = __ldg(reinterpret_cast<const float4 *>(p.dY) + i);
+        const float a[4] = {v.x, v.y, v.z, v.w};
+        float h[3][4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) split3(a[k], h[0][k], h[1][k], h[2][k]);
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            *reinterpret_cast<uint2 *>(p.dy + k * plane + 4 * i) =
+                make_uint2(upper2(h[k][0], h[k][1]), upper2(h[k][2], h[k][3]));
+    } else {
+        if (i >= p.T * p.m) return;
+        const int64_t at = i / p.m * p.ldy + i % p.m;
+        if (p.dy_f32) {
+            float h[3];
+            split3(static_cast<const float *>(p.dY)[i], h[0], h[1], h[2]);
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+                p.dy[at + k * plane] = __ushort_as_bfloat16((unsigned short)(__float_as_uint(h[k]) >> 16));
+        } else {
+            p.dy[at] = static_cast<const __nv_bfloat16 *>(p.dY)[i];
+        }
+    }
 }
 
 int64_t pad8(int64_t x) { return (x + 7) / 8 * 8; }
@@ -358,29 +418,25 @@ realq_status_t checkpoint_grad(cudaStream_t s, int64_t T, int64_t m, int64_t n, 
                                const int8_t *codes, const uint8_t *exps, float *dW, int accumulate, void *ws, int sms) {
     int splits = grad_splits(T, m, n, sms);
     const GradWs w(ws, T, m, n, dt, splits);
-    REALQ_CUDA_TRY(cudaMemsetAsync(w.status, 0, sizeof(int), s));
-    const int64_t nb = (n + 31) / 32, ldx = pad8(n);
-    {
-        Launch L("checkpoint_grad_unpack", s);
-        if (n % 32 == 0 && (reinterpret_cast<uintptr_t>(codes) & 15) == 0)
-            unpack_plane_vec_kernel<<<(unsigned)((T * n / 16 + 255) / 256), 256, 0, s>>>(
-                T * n / 16, reinterpret_cast<const uint4 *>(codes), exps, reinterpret_cast<uint4 *>(w.x));
-        else
-            unpack_plane_kernel<<<(unsigned)((T * nb * 32 + 255) / 256), 256, 0, s>>>(T, n, nb, codes, exps, w.x, ldx);
-    }
-    REALQ_TRY(check_launch("checkpoint_grad_unpack"));
-    const bool direct = dt == REALQ_BF16 && m % 8 == 0;
+    const bool direct = dt == REALQ_BF16 && m % 8 == 0;   // dY read where it lies
     const int planes = dt == REALQ_F32 ? 3 : 1;
-    const int64_t ldy = pad8(m);
-    if (!direct) {
+    const int64_t nb = (n + 31) / 32, ldx = pad8(n), ldy = pad8(m);
+    const bool xv = n % 32 == 0 && (reinterpret_cast<uintptr_t>(codes) & 15) == 0, yv = dt == REALQ_F32 && m % 8 == 0;
+    Planes p{T, n, m, ldx, ldy, (unsigned)(((xv ? T * n / 16 : T * nb * 32) + 255) / 256), codes, exps, w.x, dY,
+             dt == REALQ_F32, w.dy, w.status};
+    const unsigned blocks = p.xblocks + (direct ? 0u : (unsigned)(((yv ? T * m / 4 : T * m) + 255) / 256));
+    {
         Launch L("checkpoint_grad_planes", s);
-        const unsigned g = (unsigned)((T * m + 255) / 256);
-        if (dt == REALQ_BF16)
-            copy_plane_kernel<<<g, 256, 0, s>>>(T, m, static_cast<const __nv_bfloat16 *>(dY), w.dy, ldy);
+        if (xv && yv)
+            grad_planes_kernel<true, true><<<blocks, 256, 0, s>>>(p);
+        else if (xv)
+            grad_planes_kernel<true, false><<<blocks, 256, 0, s>>>(p);
+        else if (yv)
+            grad_planes_kernel<false, true><<<blocks, 256, 0, s>>>(p);
         else
-            split_plane_kernel<<<g, 256, 0, s>>>(T, m, static_cast<const float *>(dY), w.dy, ldy);
-        REALQ_TRY(check_launch("checkpoint_grad_planes"));
+            grad_planes_kernel<false, false><<<blocks, 256, 0, s>>>(p);
     }
+    REALQ_TRY(check_launch("checkpoint_grad_planes"));
     CUtensorMap mapY, mapX;
     CUresult cr = encode_tmap_2d_bf16(&mapY, direct ? dY : (const void *)w.dy, (uint64_t)m, (uint64_t)(planes * T),
                                       (uint64_t)ldy * 2, 64, KSTAGE, 1);
@@ -403,13 +459,15 @@ realq_status_t checkpoint_grad(cudaStream_t s, int64_t T, int64_t m, int64_t n, 
     wk.items = wk.nti * wk.ntj * splits;
     {
         Launch L("checkpoint_weight_grad", s);
-        weight_grad_kernel<<<(unsigned)(2 * std::min(wk.items, sms / 2)), THREADS, SMEM_BYTES, s>>>(
-            mapX, mapY, wk, dW, accumulate, splits > 1 ? w.part : nullptr, w.status);
+        REALQ_CUDA_TRY(launch_overlapped(weight_grad_kernel, dim3((unsigned)(2 * std::min(wk.items, sms / 2))),
+                                         dim3(THREADS), SMEM_BYTES, s, mapX, mapY, wk, dW, accumulate,
+                                         splits > 1 ? w.part : nullptr, w.status));
     }
     REALQ_TRY(check_launch("checkpoint_weight_grad"));
     if (splits > 1) {
         Launch L("checkpoint_grad_reduce", s);
-        weight_grad_reduce<<<(unsigned)((m * n + 255) / 256), 256, 0, s>>>(m * n, splits, w.part, dW, accumulate);
+        REALQ_CUDA_TRY(launch_overlapped(weight_grad_reduce, dim3((unsigned)((m * n + 1023) / 1024)), dim3(256), 0, s,
+                                         m * n, splits, (const float *)w.part, dW, accumulate));
         REALQ_TRY(check_launch("checkpoint_grad_reduce"));
     }
     return REALQ_OK;

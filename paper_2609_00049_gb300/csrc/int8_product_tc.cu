@@ -134,6 +134,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     uint32_t *tslot = reinterpret_cast<uint32_t *>(done + 1);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tslot + 1);
 
+    dependents_may_start();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int x_bytes = sh.N * KS * 2;           // a multiple of 1024, as W_BYTES
     const int items = sh.items, S = sh.stages, SW = sh.wstages;
@@ -297,6 +298,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (lane == 0) {
             // ---------------- TMA producers: tokens, codes ----------------
             const bool codes = warp == CONV_WARPS + EPI_WARPS + 1;
+            if (!codes) wait_for_previous();   // the tokens' plane (the codes are there)
             uint64_t *fulls = codes ? wfull : xfull, *empties = codes ? wempty : empty;
             uint8_t *ring = codes ? wring : smem;
             const int bytes = codes ? W_BYTES : x_bytes;
@@ -376,6 +378,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 template <typename TY>
 __global__ void __launch_bounds__(256) int8_reduce_kernel(const Shape sh, const float *part, const float *x_scale,
                                                           const float *w_scale, TY *Y) {
+    wait_for_previous();
     const int cut = sh.nti * sh.ntj - sh.whole, slot = blockIdx.x;
     const Item im = item_of(sh, sh.whole + slot);
     const int t = blockIdx.y * 8 + (threadIdx.x >> 5), c = (threadIdx.x & 31) * 4;
@@ -403,6 +406,7 @@ __global__ void __launch_bounds__(256) int8_reduce_kernel(const Shape sh, const 
 // (both also clear the status word)
 __global__ void __launch_bounds__(256) int8_plane_vec_kernel(int64_t count, const uint8_t *X, uint32_t *plane,
                                                              int *status) {
+    dependents_may_start();
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i == 0) *status = 0;
     if (i >= count) return;
@@ -420,6 +424,7 @@ __global__ void __launch_bounds__(256) int8_plane_vec_kernel(int64_t count, cons
 }
 __global__ void __launch_bounds__(256) int8_plane_kernel(int64_t T, int64_t n, const uint8_t *X, __half *plane,
                                                          int64_t ld, int *status) {
+    dependents_may_start();
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i == 0) *status = 0;
     if (i >= T * n) return;
@@ -499,14 +504,15 @@ realq_status_t tc_launch(cudaStream_t s, const Shape &sh, const CUtensorMap &map
     REALQ_TRY(set_smem_limit(k, SMEM_BYTES));
     {
         Launch L("int8_product_tc", s);
-        int8_tc_kernel<WB, TY><<<(unsigned)std::min(sh.items, sms), THREADS, SMEM_BYTES, s>>>(
-            mapW, mapX, sh, xs, ws, wz, Y, b.part, b.status);
+        REALQ_CUDA_TRY(launch_overlapped(int8_tc_kernel<WB, TY>, dim3((unsigned)std::min(sh.items, sms)), dim3(THREADS),
+                                         SMEM_BYTES, s, mapW, mapX, sh, xs, ws, wz, Y, b.part, b.status));
     }
     REALQ_TRY(check_launch("int8_product_tc"));
     if (sh.splits > 1) {
         Launch L("int8_product_reduce", s);
-        int8_reduce_kernel<TY><<<dim3((unsigned)(sh.nti * sh.ntj - sh.whole), (unsigned)((sh.N + 7) / 8)), 256, 0, s>>>(
-            sh, b.part, xs, ws, Y);
+        REALQ_CUDA_TRY(launch_overlapped(int8_reduce_kernel<TY>,
+                                         dim3((unsigned)(sh.nti * sh.ntj - sh.whole), (unsigned)((sh.N + 7) / 8)),
+                                         dim3(256), 0, s, sh, (const float *)b.part, xs, ws, Y));
     }
     return check_launch("int8_product_reduce");
 }
@@ -524,15 +530,6 @@ realq_status_t int8_product_tc(cudaStream_t s, int64_t T, int64_t n, int64_t m, 
     const Shape sh = shape_of(T, n, m, w_bits, sms);
     const ProductWs b(ws, sh, w_bits);
     const int64_t ldx = pad8(n), rb = row_bytes(n, w_bits);
-    {
-        Launch L("int8_product_plane", s);
-        if (n % 16 == 0 && (reinterpret_cast<uintptr_t>(X) & 15) == 0)
-            int8_plane_vec_kernel<<<(unsigned)((T * n / 16 + 255) / 256), 256, 0, s>>>(
-                T * n / 16, X, reinterpret_cast<uint32_t *>(b.x), b.status);
-        else
-            int8_plane_kernel<<<(unsigned)((T * n + 255) / 256), 256, 0, s>>>(T, n, X, b.x, ldx, b.status);
-    }
-    REALQ_TRY(check_launch("int8_product_plane"));
     const uint8_t *w = W;
     int64_t ldw = rb;
     if (rb % 16) {
@@ -542,6 +539,15 @@ realq_status_t int8_product_tc(cudaStream_t s, int64_t T, int64_t n, int64_t m, 
         int8_pad_kernel<<<(unsigned)((m * rb + 255) / 256), 256, 0, s>>>(m, rb, W, b.w, ldw);
         REALQ_TRY(check_launch("int8_product_pad"));
     }
+    {
+        Launch L("int8_product_plane", s);
+        if (n % 16 == 0 && (reinterpret_cast<uintptr_t>(X) & 15) == 0)
+            int8_plane_vec_kernel<<<(unsigned)((T * n / 16 + 255) / 256), 256, 0, s>>>(
+                T * n / 16, X, reinterpret_cast<uint32_t *>(b.x), b.status);
+        else
+            int8_plane_kernel<<<(unsigned)((T * n + 255) / 256), 256, 0, s>>>(T, n, X, b.x, ldx, b.status);
+    }
+    REALQ_TRY(check_launch("int8_product_plane"));
     CUtensorMap mapW, mapX;
     CUresult cr = encode_tmap_2d_u8(&mapW, w, (uint64_t)rb, (uint64_t)m, (uint64_t)ldw, w_bits == 8 ? KS : KS / 2, TM,
                                     w_bits == 8 ? 2 : 3);
