@@ -17,6 +17,7 @@
 // neighbouring lanes share a block, so its maximum takes two shuffles;
 // widths that are not a multiple of 32 and unaligned rows take a warp per
 // block, one value to a lane.
+#include "bytes.cuh"
 #include "kernels.cuh"
 
 namespace realq {
@@ -142,30 +143,52 @@ __global__ void __launch_bounds__(THREADS) unpack_vec_kernel(int64_t groups, con
     }
 }
 
-// Any width and alignment: warp b % nb of row b / nb.
+// Any width and alignment: a warp takes UB neighbouring blocks of a row, one
+// value of each to a lane (nw warps to a row).
+constexpr int UB = 4;
 template <typename TX>
-__global__ void __launch_bounds__(THREADS) pack_row_kernel(int64_t T, int64_t n, int64_t nb, const TX *X,
+__global__ void __launch_bounds__(THREADS) pack_row_kernel(int64_t T, int64_t n, int64_t nw, const TX *X,
                                                            int8_t *codes, uint8_t *exps) {
     const int lane = threadIdx.x & 31;
     const int64_t w = ((int64_t)blockIdx.x * THREADS + threadIdx.x) >> 5;
-    if (w >= T * nb) return;
-    const int64_t t = w / nb, c = (w % nb) * 32 + lane;
-    const float x = c < n ? load_as_float(X, t * n + c) : 0.f;
-    const uint32_t b = __reduce_max_sync(FULL, mag(x)) >> 23;
-    float s1, s2;
-    scales_of(b, s1, s2);
-    if (c < n) codes[t * n + c] = b < 255u ? (int8_t)(code_of(x, s1, s2) & 255u) : 0;
-    if (lane == 0) exps[w] = (uint8_t)b;
+    if (w >= T * nw) return;
+    int64_t c0;
+    const int64_t t = divide(w, nw, c0);
+    c0 = c0 * (32 * UB) + lane;
+    float x[UB];
+#pragma unroll
+    for (int k = 0; k < UB; ++k) x[k] = c0 + 32 * k < n ? load_as_float(X, t * n + c0 + 32 * k) : 0.f;
+#pragma unroll
+    for (int k = 0; k < UB; ++k) {
+        const uint32_t b = __reduce_max_sync(FULL, mag(x[k])) >> 23;
+        float s1, s2;
+        scales_of(b, s1, s2);
+        const int64_t c = c0 + 32 * k;
+        if (c < n) codes[t * n + c] = b < 255u ? (int8_t)(code_of(x[k], s1, s2) & 255u) : 0;
+        if (lane == 0 && c < n) exps[t * ((n + 31) / 32) + c / 32] = (uint8_t)b;
+    }
 }
 
 template <typename TX>
-__global__ void __launch_bounds__(THREADS) unpack_row_kernel(int64_t T, int64_t n, int64_t nb, const int8_t *codes,
+__global__ void __launch_bounds__(THREADS) unpack_row_kernel(int64_t T, int64_t n, int64_t nw, const int8_t *codes,
                                                              const uint8_t *exps, TX *X) {
     const int lane = threadIdx.x & 31;
     const int64_t w = ((int64_t)blockIdx.x * THREADS + threadIdx.x) >> 5;
-    if (w >= T * nb) return;
-    const int64_t t = w / nb, c = (w % nb) * 32 + lane;
-    if (c < n) store1(X + t * n + c, (float)codes[t * n + c] * step_of(exps[w]));
+    if (w >= T * nw) return;
+    int64_t c0;
+    const int64_t t = divide(w, nw, c0);
+    c0 = c0 * (32 * UB) + lane;
+    int8_t q[UB];
+    uint32_t b[UB];
+#pragma unroll
+    for (int k = 0; k < UB; ++k) {
+        const int64_t c = c0 + 32 * k;
+        q[k] = c < n ? __ldg(codes + t * n + c) : 0;
+        b[k] = c < n ? __ldg(exps + t * ((n + 31) / 32) + c / 32) : 0;
+    }
+#pragma unroll
+    for (int k = 0; k < UB; ++k)
+        if (c0 + 32 * k < n) store1(X + t * n + c0 + 32 * k, (float)q[k] * step_of(b[k]));
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -174,23 +197,23 @@ bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 
 
 template <typename TX>
 static void pack_launch(cudaStream_t s, int64_t T, int64_t n, const TX *X, int8_t *codes, uint8_t *exps) {
-    const int64_t nb = (n + 31) / 32, groups = T * n / 8;
+    const int64_t nw = (n + 32 * UB - 1) / (32 * UB), groups = T * n / 8;
     Launch L("checkpoint_pack", s);
     if (n % 32 == 0 && aligned16(X) && aligned16(codes))
         pack_vec_kernel<TX><<<(unsigned)((groups + THREADS * UN - 1) / (THREADS * UN)), THREADS, 0, s>>>(groups, X, codes, exps);
     else
-        pack_row_kernel<TX><<<(unsigned)((T * nb * 32 + THREADS - 1) / THREADS), THREADS, 0, s>>>(T, n, nb, X, codes,
+        pack_row_kernel<TX><<<(unsigned)((T * nw * 32 + THREADS - 1) / THREADS), THREADS, 0, s>>>(T, n, nw, X, codes,
                                                                                                   exps);
 }
 
 template <typename TX>
 static void unpack_launch(cudaStream_t s, int64_t T, int64_t n, const int8_t *codes, const uint8_t *exps, TX *X) {
-    const int64_t nb = (n + 31) / 32, groups = T * n / 8;
+    const int64_t nw = (n + 32 * UB - 1) / (32 * UB), groups = T * n / 8;
     Launch L("checkpoint_unpack", s);
     if (n % 32 == 0 && aligned16(X) && aligned16(codes))
         unpack_vec_kernel<TX><<<(unsigned)((groups + THREADS * UN - 1) / (THREADS * UN)), THREADS, 0, s>>>(groups, codes, exps, X);
     else
-        unpack_row_kernel<TX><<<(unsigned)((T * nb * 32 + THREADS - 1) / THREADS), THREADS, 0, s>>>(T, n, nb, codes,
+        unpack_row_kernel<TX><<<(unsigned)((T * nw * 32 + THREADS - 1) / THREADS), THREADS, 0, s>>>(T, n, nw, codes,
                                                                                                     exps, X);
 }
 

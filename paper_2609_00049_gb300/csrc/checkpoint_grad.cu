@@ -26,6 +26,7 @@
 // when the tiles alone do not fill the SMs; the parts are summed in a fixed
 // order.  Every wait is bounded; a tile whose wait gave up is written as NaN
 // and the status word gets ST_TIMEOUT.
+#include "bytes.cuh"
 #include "kernels.cuh"
 #include "tc.cuh"
 
@@ -312,11 +313,11 @@ __device__ __forceinline__ void split3(float v, float &hi, float &mid, float &lo
 }
 
 // The operands' planes, in one launch: the first xblocks blocks unpack X̂ to
-// bf16 (row stride ldx), the others bring dY to its planes (bf16 copied to an
-// aligned row stride, fp32 split in three).  XV: rows of X̂ are whole blocks of
-// 32 (16 values a thread; otherwise a warp a block); YV: fp32 rows of whole
-// 16-byte pieces.  Columns past the widths are not written and lie outside the
-// tensor maps.
+// bf16 (row stride ldx), 16 values a thread; the others bring dY to its planes
+// (row stride ldy): bf16 copied, 16 bytes a thread, or fp32 split in three, four
+// values a thread.  FLAT: rows follow one another at whole pieces (n a multiple
+// of 32, m of 8), so pieces are numbered through.  Columns past the widths lie
+// outside the tensor maps.
 struct Planes {
     int64_t T, n, m, ldx, ldy;
     unsigned xblocks;
@@ -328,57 +329,76 @@ struct Planes {
     __nv_bfloat16 *dy;
     int *status;
 };
-template <bool XV, bool YV>
+template <bool FLATX, bool FLATY>
 __global__ void __launch_bounds__(256) grad_planes_kernel(const Planes p) {
     dependents_may_start();
     if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = 0;
     if (blockIdx.x < p.xblocks) {
-        const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-        if (XV) {
-            if (i >= p.T * p.n / 16) return;
-            const uint4 q = __ldg(reinterpret_cast<const uint4 *>(p.codes) + i);
-            const float s = step_of(__ldg(p.exps + (i >> 1)));
-            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-            uint32_t h[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                h[k] = upper2((float)(int8_t)(w[k >> 1] >> (16 * (k & 1))) * s,
-                              (float)(int8_t)(w[k >> 1] >> (16 * (k & 1) + 8)) * s);
-            uint4 *o = reinterpret_cast<uint4 *>(p.x) + 2 * i;
-            o[0] = make_uint4(h[0], h[1], h[2], h[3]);
-            o[1] = make_uint4(h[4], h[5], h[6], h[7]);
+        const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, pieces = (p.n + 15) / 16;
+        if (i >= p.T * pieces) return;
+        uint4 q;
+        uint32_t b;
+        uint4 *o;
+        bool both = true;
+        if (FLATX) {
+            q = __ldg(reinterpret_cast<const uint4 *>(p.codes) + i);
+            b = __ldg(p.exps + (i >> 1));
+            o = reinterpret_cast<uint4 *>(p.x) + 2 * i;
         } else {
-            const int64_t nb = (p.n + 31) / 32, w = i >> 5;
-            if (w >= p.T * nb) return;
-            const int64_t t = w / nb, c = (w % nb) * 32 + (threadIdx.x & 31);
-            if (c < p.n) p.x[t * p.ldx + c] = __float2bfloat16_rn((float)p.codes[t * p.n + c] * step_of(p.exps[w]));
+            int64_t c;
+            const int64_t t = divide(i, pieces, c);
+            const uint8_t *lo = reinterpret_cast<const uint8_t *>(p.codes);
+            q = load16(lo + t * p.n + c * 16, lo, lo + p.T * p.n);
+            b = __ldg(p.exps + t * ((p.n + 31) / 32) + (c >> 1));
+            o = reinterpret_cast<uint4 *>(p.x + t * p.ldx + c * 16);
+            both = c * 16 + 8 < p.ldx;
         }
+        const float s = step_of(b);
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+        uint32_t h[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            h[k] = upper2((float)(int8_t)(w[k >> 1] >> (16 * (k & 1))) * s,
+                          (float)(int8_t)(w[k >> 1] >> (16 * (k & 1) + 8)) * s);
+        o[0] = make_uint4(h[0], h[1], h[2], h[3]);
+        if (both) o[1] = make_uint4(h[4], h[5], h[6], h[7]);
         return;
     }
     const int64_t i = (int64_t)(blockIdx.x - p.xblocks) * 256 + threadIdx.x, plane = p.T * p.ldy;
-    if (YV) {   // (m a multiple of 8, so ldy = m)
-        if (i >= p.T * p.m / 4) return;
-        const float4 v = __ldg(reinterpret_cast<const float4 *>(p.dY) + i);
-        const float a[4] = {v.x, v.y, v.z, v.w};
+    if (p.dy_f32) {
+        const int64_t pieces = (p.m + 3) / 4;
+        if (i >= p.T * pieces) return;
+        float a[4];
+        int64_t at;
+        if (FLATY) {
+            const float4 v = __ldg(reinterpret_cast<const float4 *>(p.dY) + i);
+            a[0] = v.x;
+            a[1] = v.y;
+            a[2] = v.z;
+            a[3] = v.w;
+            at = 4 * i;
+        } else {
+            int64_t c;
+            const int64_t t = divide(i, pieces, c);
+            const float *src = static_cast<const float *>(p.dY) + t * p.m + c * 4;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) a[k] = c * 4 + k < p.m ? __ldg(src + k) : 0.f;
+            at = t * p.ldy + c * 4;
+        }
         float h[3][4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) split3(a[k], h[0][k], h[1][k], h[2][k]);
 #pragma unroll
         for (int k = 0; k < 3; ++k)
-            *reinterpret_cast<uint2 *>(p.dy + k * plane + 4 * i) =
+            *reinterpret_cast<uint2 *>(p.dy + k * plane + at) =
                 make_uint2(upper2(h[k][0], h[k][1]), upper2(h[k][2], h[k][3]));
     } else {
-        if (i >= p.T * p.m) return;
-        const int64_t at = i / p.m * p.ldy + i % p.m;
-        if (p.dy_f32) {
-            float h[3];
-            split3(static_cast<const float *>(p.dY)[i], h[0], h[1], h[2]);
-#pragma unroll
-            for (int k = 0; k < 3; ++k)
-                p.dy[at + k * plane] = __ushort_as_bfloat16((unsigned short)(__float_as_uint(h[k]) >> 16));
-        } else {
-            p.dy[at] = static_cast<const __nv_bfloat16 *>(p.dY)[i];
-        }
+        const int64_t pieces = p.ldy / 8;
+        if (i >= p.T * pieces) return;
+        int64_t c;
+        const int64_t t = divide(i, pieces, c);
+        const uint8_t *lo = static_cast<const uint8_t *>(p.dY);
+        reinterpret_cast<uint4 *>(p.dy)[i] = load16(lo + (t * p.m + c * 8) * 2, lo, lo + p.T * p.m * 2);
     }
 }
 
@@ -420,11 +440,12 @@ realq_status_t checkpoint_grad(cudaStream_t s, int64_t T, int64_t m, int64_t n, 
     const GradWs w(ws, T, m, n, dt, splits);
     const bool direct = dt == REALQ_BF16 && m % 8 == 0;   // dY read where it lies
     const int planes = dt == REALQ_F32 ? 3 : 1;
-    const int64_t nb = (n + 31) / 32, ldx = pad8(n), ldy = pad8(m);
+    const int64_t ldx = pad8(n), ldy = pad8(m);
     const bool xv = n % 32 == 0 && (reinterpret_cast<uintptr_t>(codes) & 15) == 0, yv = dt == REALQ_F32 && m % 8 == 0;
-    Planes p{T, n, m, ldx, ldy, (unsigned)(((xv ? T * n / 16 : T * nb * 32) + 255) / 256), codes, exps, w.x, dY,
+    Planes p{T, n, m, ldx, ldy, (unsigned)((T * ((n + 15) / 16) + 255) / 256), codes, exps, w.x, dY,
              dt == REALQ_F32, w.dy, w.status};
-    const unsigned blocks = p.xblocks + (direct ? 0u : (unsigned)(((yv ? T * m / 4 : T * m) + 255) / 256));
+    const int64_t ypieces = T * (dt == REALQ_F32 ? (m + 3) / 4 : ldy / 8);
+    const unsigned blocks = p.xblocks + (direct ? 0u : (unsigned)((ypieces + 255) / 256));
     {
         Launch L("checkpoint_grad_planes", s);
         if (xv && yv)

@@ -28,6 +28,7 @@
 
 #include <algorithm>
 
+#include "bytes.cuh"
 #include "kernels.cuh"
 
 namespace cg = cooperative_groups;
@@ -53,41 +54,43 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// 16 bytes at any address, those from `hi` on zero: aligned words where they
-// lie inside [lo, hi), else single bytes
-__device__ __forceinline__ uint4 load16(const uint8_t *p, const uint8_t *lo, const uint8_t *hi) {
-    const uint32_t mis = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 3);
-    const uint8_t *a = p - mis;
+// Weight codes are read once: they pass L1 by, which keeps the tokens.
+__device__ __forceinline__ uint4 load_weight(const uint8_t *p) {
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "l"(p));
+    return v;
+}
+// An aligned piece, of which some bytes may lie outside the codes (and read 0).
+__device__ __forceinline__ uint4 load_piece(const uint8_t *p, const uint8_t *lo, const uint8_t *hi) {
+    if (p >= lo && p + 16 <= hi) return load_weight(p);
     uint32_t v[4] = {0, 0, 0, 0};
-    if (a >= lo && a + 20 <= hi) {
-        uint32_t w[5];
 #pragma unroll
-        for (int i = 0; i < 5; ++i) w[i] = __ldg(reinterpret_cast<const uint32_t *>(a) + i);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = __funnelshift_r(w[i], w[i + 1], 8 * mis);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (p + i < hi) v[i >> 2] |= (uint32_t)__ldg(p + i) << (8 * (i & 3));
-    }
+    for (int i = 0; i < 16; ++i)
+        if (p + i >= lo && p + i < hi) v[i >> 2] |= (uint32_t)__ldg(p + i) << (8 * (i & 3));
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
-// Weight codes are read once: they pass L1 by, which keeps the tokens.
-template <bool ALIGNED>
-__device__ __forceinline__ uint4 load_weight(const uint8_t *p, const uint8_t *lo, const uint8_t *hi) {
-    if constexpr (ALIGNED) {
-        uint4 v;
-        asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-                     : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                     : "l"(p));
-        return v;
-    }
-    return load16(p, lo, hi);
+__device__ __forceinline__ uint4 shfl4(const uint4 &v, int src) {
+    return make_uint4(__shfl_sync(0xFFFFFFFFu, v.x, src), __shfl_sync(0xFFFFFFFFu, v.y, src),
+                      __shfl_sync(0xFFFFFFFFu, v.z, src), __shfl_sync(0xFFFFFFFFu, v.w, src));
 }
-template <bool ALIGNED>
-__device__ __forceinline__ uint4 load_token(const uint8_t *p, const uint8_t *lo, const uint8_t *hi) {
-    if constexpr (ALIGNED) return __ldg(reinterpret_cast<const uint4 *>(p));
-    return load16(p, lo, hi);
+// 16 bytes from byte `mis` of the 32 in a, b on
+__device__ __forceinline__ uint4 realign(const uint4 &a, const uint4 &b, uint32_t mis) {
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    uint32_t u[6], t[5];
+#pragma unroll
+    for (int i = 0; i < 6; ++i) u[i] = mis & 8 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) t[i] = mis & 4 ? u[i + 1] : u[i];
+    const uint32_t s = 8 * (mis & 3);
+    return make_uint4(__funnelshift_r(t[0], t[1], s), __funnelshift_r(t[1], t[2], s), __funnelshift_r(t[2], t[3], s),
+                      __funnelshift_r(t[3], t[4], s));
+}
+// the first `count` bytes of w, the others the code of zero
+__device__ __forceinline__ uint32_t first_bytes(uint32_t w, int count) {
+    const uint32_t keep = count >= 4 ? ~0u : (count <= 0 ? 0u : (1u << 8 * count) - 1u);
+    return (w & keep) | (0x80808080u & ~keep);
 }
 
 __device__ __forceinline__ uint32_t word_of(const uint4 &v, int i) {
@@ -122,19 +125,91 @@ __device__ __forceinline__ void token_pairs(const uint4 *k, int i, uint32_t *x) 
     }
 }
 
+// 16 bytes global -> shared without a register, or zeros
+template <bool KEEP>
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there) {
+    const int bytes = there ? 16 : 0;
+    if constexpr (KEEP)
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+    else
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+// A warp's sums over its share of K.
+template <int WB, int NT, int RT> struct Sums {
+    static constexpr int XP = WB == 8 ? 1 : 2;    // 16-byte pieces of token codes to one of weight codes
+    static constexpr int WP = WB == 8 ? 2 : 4;    // pairs of a word
+    // steps between flushes: 8 bits, 64 codes of at most 255 x 128 each; 4 bits, 128 codes of 15 x 128
+    static constexpr int FLUSH = WB == 8 ? 8 : 64;
+    float acc[RT][NT][4] = {}, xacc[NT][4] = {};
+    int sum[RT][NT][4] = {};
+    int since = 0;
+
+    __device__ __forceinline__ void flush() {
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sum[r][t][e] += __float2int_rn(acc[r][t][e] * 16777216.f);
+                    acc[r][t][e] = 0.f;
+                }
+        since = 0;
+    }
+    // one step: this lane's 16 bytes of 2 RT channels, and the codes of NT tokens that meet them
+    __device__ __forceinline__ void step(const uint4 (&wq)[RT][2], const uint4 (&k)[NT][XP]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {             // words of the 16 bytes
+            uint32_t x[NT][WP];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) token_pairs<WB>(k[t], i, x[t]);
+#pragma unroll
+            for (int j = 0; j < WP; j += 2) {     // a product takes two pairs
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    uint32_t a[4];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t w = word_of(wq[r][h], i);
+                        a[h] = weight_pair<WB>(w, j);
+                        a[2 + h] = weight_pair<WB>(w, j + 1);
+                    }
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) mma16816(acc[r][t], a, x[t][j], x[t][j + 1]);
+                }
+                // ones (16 where the pair holds x / 16)
+                const uint32_t one[4] = {0x3C003C00u, 0x3C003C00u, WB == 8 ? 0x3C003C00u : 0x4C004C00u,
+                                         WB == 8 ? 0x3C003C00u : 0x4C004C00u};
+#pragma unroll
+                for (int t = 0; t < NT; ++t) mma16816(xacc[t], one, x[t][j], x[t][j + 1]);
+            }
+        }
+        if (++since == FLUSH) flush();
+    }
+};
+
 // ALIGNED: rows of whole 16-byte pieces of codes (n a multiple of 16, or of 32
-// for 4 bits) at 16-byte aligned addresses.
+// for 4 bits) at 16-byte aligned addresses.  Each lane then copies the pieces it
+// will use into a ring of its own in shared memory, several steps ahead, so that
+// the loads in flight cost no registers (held in registers they left 16 warps on
+// an SM and 64 KB in flight at best: 29 us for 8 tokens x 8192 x 28672 with 4-bit
+// weights).  Other rows are loaded to registers, realigned between lanes.
+template <int WB, int NT, int RT> struct Ring {
+    static constexpr int XP = WB == 8 ? 1 : 2;
+    static constexpr int SLOT = (2 * RT + NT * XP) * 512;                // bytes of a warp's step
+    static constexpr int STAGES = 72 * 1024 / (SW * SLOT) < 6 ? 72 * 1024 / (SW * SLOT) : 6;
+    static constexpr int BYTES = SW * SLOT * STAGES;
+};
+
 template <bool ALIGNED, int WB, int NT, int RT, typename TY>
-__global__ void __launch_bounds__(SW * 32, NT * RT == 1 ? 3 : 2)
+__global__ void __launch_bounds__(SW * 32, ALIGNED ? 3 : 2)
     int8_stream_kernel(int64_t T, int64_t n, int64_t m, const uint8_t *X, const float *x_scale, const uint8_t *W,
                        const float *w_scale, const uint8_t *w_zero, TY *Y) {
-    constexpr int XP = WB == 8 ? 1 : 2;           // 16-byte pieces of token codes to one of weight codes
-    constexpr int WP = WB == 8 ? 2 : 4;           // pairs of a word
-    constexpr int ROWS = RT * 16, TOK = NT * 8, OUT = ROWS * TOK;
-    constexpr int UNROLL = NT * RT == 1 ? 4 : (NT * RT == 2 ? 2 : 1);
-    // steps between flushes: 8 bits, 64 codes of at most 255 x 128 each; 4 bits, 128 codes of 15 x 128
-    constexpr int FLUSH = WB == 8 ? 8 : 64;
-    static_assert(FLUSH % UNROLL == 0, "flushes fall between rounds of loads");
+    using S = Sums<WB, NT, RT>;
+    using R = Ring<WB, NT, RT>;
+    constexpr int XP = S::XP, ROWS = RT * 16, TOK = NT * 8, OUT = ROWS * TOK;
+    extern __shared__ __align__(16) uint8_t ring[];
     __shared__ int red[SW * OUT];
     __shared__ int xred[SW * TOK];
     cg::cluster_group cluster = cg::this_cluster();
@@ -152,92 +227,100 @@ __global__ void __launch_bounds__(SW * 32, NT * RT == 1 ? 3 : 2)
             wrow[r][h] = W + min(i0 + r * 16 + h * 8 + g, m - 1) * rb;
 #pragma unroll
     for (int t = 0; t < NT; ++t) xrow[t] = X + min((int64_t)(t * 8 + g), T - 1) * n;
-    const uint8_t *whi = W + m * rb, *xhi = X + T * n;
+    const uint4 zeros = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);   // codes of x = 0
 
-    float acc[RT][NT][4] = {}, xacc[NT][4] = {};
-    int sum[RT][NT][4] = {};
-    auto flush = [&] {
+    // Four neighbouring pieces (64 bytes of each row) to a step.
+    const int steps = (pieces + 3) / 4;
+    S sums;
+    if constexpr (ALIGNED) {
+        // the cluster's warps take steps in turn
+        const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(ring)) + warp * R::SLOT + lane * 16;
+        auto fetch = [&](int k, int slot) {
+            const int64_t v = ((int64_t)k * CL * SW + rank * SW + warp) * 4 + q;
+            const bool there = v < pieces;
+            const int64_t at = there ? v * 16 : 0;
+            const uint32_t dst = mine + slot * (SW * R::SLOT);
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) copy16<false>(dst + (2 * r + h) * 512, wrow[r][h] + at, there);
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    sum[r][t][e] += __float2int_rn(acc[r][t][e] * 16777216.f);
-                    acc[r][t][e] = 0.f;
-                }
-    };
-
-    // four neighbouring pieces (64 bytes of each row) to a step; the cluster's warps take steps in turn
-    const int steps = (pieces + 3) / 4;
-    int since = 0;
-    for (int s0 = rank * SW + warp; s0 < steps; s0 += CL * SW * UNROLL) {
-        uint4 wq[UNROLL][RT][2];
+                for (int p = 0; p < XP; ++p)
+                    copy16<true>(dst + (2 * RT + t * XP + p) * 512, xrow[t] + at * XP + p * 16, there);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            const int v = (s0 + u * CL * SW) * 4 + q;
+        for (int k = 0; k < R::STAGES - 1; ++k) fetch(k, k);
+        int slot = 0;
+        for (int k = 0; k * CL * SW + rank * SW + warp < steps; ++k) {
+            fetch(k + R::STAGES - 1, slot == 0 ? R::STAGES - 1 : slot - 1);
+            asm volatile("cp.async.wait_group %0;" ::"n"(R::STAGES - 1) : "memory");
+            const uint4 *src = reinterpret_cast<const uint4 *>(ring + (slot * SW + warp) * R::SLOT) + lane;
+            uint4 wq[RT][2], kq[NT][XP];
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) wq[r][h] = src[(2 * r + h) * 32];
+            const bool there = (k * CL * SW + rank * SW + warp) * 4 + q < pieces;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int p = 0; p < XP; ++p) kq[t][p] = there ? src[(2 * RT + t * XP + p) * 32] : zeros;
+            sums.step(wq, kq);
+            if (++slot == R::STAGES) slot = 0;
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    } else {
+        // Pairs of neighbouring steps in turn: a lane loads aligned pieces and has the following one
+        // from the next lane (the pair's last lane loads it itself).
+        const uint8_t *whi = W + m * rb, *xhi = X + T * n;
+        for (int s0 = 2 * (rank * SW + warp); s0 < steps; s0 += 2 * CL * SW) {
+            uint4 wq[2][RT][2], next[RT][2];
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    wq[u][r][h] = make_uint4(0, 0, 0, 0);
-                    if (v < pieces) wq[u][r][h] = load_weight<ALIGNED>(wrow[r][h] + (int64_t)v * 16, W, whi);
+                    const uint8_t *p = wrow[r][h] - (reinterpret_cast<uintptr_t>(wrow[r][h]) & 15) + ((int64_t)s0 * 4 + q) * 16;
+                    wq[0][r][h] = load_piece(p, W, whi);
+                    wq[1][r][h] = load_piece(p + 64, W, whi);
+                    if (q == 3) next[r][h] = load_piece(p + 80, W, whi);
                 }
-        }
+            const int src = (lane & ~3) | ((q + 1) & 3);
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            const int v = (s0 + u * CL * SW) * 4 + q;
-            if ((s0 + u * CL * SW) >= steps) break;   // (the same for the whole warp)
-            uint4 k[NT][XP];
+            for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t mis = (uint32_t)(reinterpret_cast<uintptr_t>(wrow[r][h]) & 15);
+                    const uint4 n0 = shfl4(q == 0 ? wq[1][r][h] : wq[0][r][h], src), n1 = shfl4(wq[1][r][h], src);
+                    wq[0][r][h] = realign(wq[0][r][h], n0, mis);
+                    wq[1][r][h] = realign(wq[1][r][h], q == 3 ? next[r][h] : n1, mis);
+                }
 #pragma unroll
-                for (int p = 0; p < XP; ++p) {
-                    const int64_t c = ((int64_t)v * XP + p) * 16;   // first column
-                    k[t][p] = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
-                    if (v < pieces && c < n) {
-                        k[t][p] = load_token<ALIGNED>(xrow[t] + c, X, xhi);
-                        if (!ALIGNED && c + 16 > n) {   // columns from n on take no part
-                            uint32_t *w = &k[t][p].x;
-                            for (int b = (int)(n - c); b < 16; ++b)
-                                w[b >> 2] = (w[b >> 2] & ~(0xFFu << 8 * (b & 3))) | 0x80u << 8 * (b & 3);
+            for (int u = 0; u < 2; ++u) {
+                if (s0 + u >= steps) break;   // (the same for the whole warp)
+                uint4 kq[NT][XP];
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int p = 0; p < XP; ++p) {
+                        const int64_t c = (((int64_t)s0 + u) * 4 + q) * (16 * XP) + p * 16;   // first column
+                        kq[t][p] = zeros;
+                        if (c < n) {
+                            kq[t][p] = load16(xrow[t] + c, X, xhi);
+                            if (c + 16 > n) {   // columns from n on take no part
+                                const int left = (int)(n - c);
+                                kq[t][p] = make_uint4(first_bytes(kq[t][p].x, left), first_bytes(kq[t][p].y, left - 4),
+                                                      first_bytes(kq[t][p].z, left - 8), first_bytes(kq[t][p].w, left - 12));
+                            }
                         }
                     }
-                }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {             // words of the 16 bytes
-                uint32_t x[NT][WP];
-#pragma unroll
-                for (int t = 0; t < NT; ++t) token_pairs<WB>(k[t], i, x[t]);
-#pragma unroll
-                for (int j = 0; j < WP; j += 2) {     // a product takes two pairs
-#pragma unroll
-                    for (int r = 0; r < RT; ++r) {
-                        uint32_t a[4];
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const uint32_t w = word_of(wq[u][r][h], i);
-                            a[h] = weight_pair<WB>(w, j);
-                            a[2 + h] = weight_pair<WB>(w, j + 1);
-                        }
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) mma16816(acc[r][t], a, x[t][j], x[t][j + 1]);
-                    }
-                    // ones (16 where the pair holds x / 16)
-                    const uint32_t one[4] = {0x3C003C00u, 0x3C003C00u, WB == 8 ? 0x3C003C00u : 0x4C004C00u,
-                                             WB == 8 ? 0x3C003C00u : 0x4C004C00u};
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) mma16816(xacc[t], one, x[t][j], x[t][j + 1]);
-                }
+                sums.step(wq[u], kq);
             }
         }
-        since += UNROLL;
-        if (since == FLUSH) {
-            flush();
-            since = 0;
-        }
     }
-    flush();
+    sums.flush();
 
 #pragma unroll
     for (int r = 0; r < RT; ++r)
@@ -245,12 +328,12 @@ __global__ void __launch_bounds__(SW * 32, NT * RT == 1 ? 3 : 2)
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                red[warp * OUT + (t * 8 + 2 * q + (e & 1)) * ROWS + r * 16 + (e >> 1) * 8 + g] = sum[r][t][e];
+                red[warp * OUT + (t * 8 + 2 * q + (e & 1)) * ROWS + r * 16 + (e >> 1) * 8 + g] = sums.sum[r][t][e];
     if (g == 0) {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) xred[warp * TOK + t * 8 + 2 * q + e] = __float2int_rn(xacc[t][e]);
+            for (int e = 0; e < 2; ++e) xred[warp * TOK + t * 8 + 2 * q + e] = __float2int_rn(sums.xacc[t][e]);
     }
     __syncthreads();
     // the warps' shares, then the cluster's; integers, so any order is the same
@@ -294,7 +377,7 @@ realq_status_t stream_launch(cudaStream_t s, int64_t T, int64_t n, int64_t m, co
     // CTAs over K: the count whose waves take the fewest steps of a warp, its
     // start and end counted as four, each warp keeping at least two.
     const int64_t rb = WB == 8 ? n : (n + 1) / 2, ctas = (m + RT * 16 - 1) / (RT * 16), steps = (rb + 63) / 64;
-    const int64_t slots = (int64_t)sms * (NT * RT == 1 ? 3 : 2);
+    const int64_t slots = (int64_t)sms * (ALIGNED ? 3 : 2);
     int cl = 1;
     int64_t best = INT64_MAX;
     for (int c = 1; c <= MAX_CLUSTER && (c == 1 || steps >= 2 * SW * c); c *= 2) {
@@ -307,7 +390,11 @@ realq_status_t stream_launch(cudaStream_t s, int64_t T, int64_t n, int64_t m, co
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(ctas * cl));
     cfg.blockDim = dim3(SW * 32);
+    cfg.dynamicSmemBytes = ALIGNED ? Ring<WB, NT, RT>::BYTES : 0;
     cfg.stream = s;
+    if (ALIGNED)
+        REALQ_TRY(set_smem_limit(reinterpret_cast<const void *>(int8_stream_kernel<ALIGNED, WB, NT, RT, TY>),
+                                 Ring<WB, NT, RT>::BYTES));
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)cl;

@@ -29,6 +29,7 @@
 // parts in their order.
 // Every wait is bounded; a tile whose wait gave up is written as NaN and the
 // status word gets ST_TIMEOUT.
+#include "bytes.cuh"
 #include "kernels.cuh"
 #include "tc.cuh"
 
@@ -404,13 +405,7 @@ __global__ void __launch_bounds__(256) int8_reduce_kernel(const Shape sh, const 
 // Token codes -> fp16 plane of row stride ld (16 codes per thread where rows
 // are whole vectors)
 // (both also clear the status word)
-__global__ void __launch_bounds__(256) int8_plane_vec_kernel(int64_t count, const uint8_t *X, uint32_t *plane,
-                                                             int *status) {
-    dependents_may_start();
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i == 0) *status = 0;
-    if (i >= count) return;
-    const uint4 q = __ldg(reinterpret_cast<const uint4 *>(X) + i);
+__device__ __forceinline__ void store_codes(uint4 *o, const uint4 &q, bool both) {
     const uint32_t v[4] = {q.x, q.y, q.z, q.w};
     uint32_t h[8];
 #pragma unroll
@@ -418,24 +413,37 @@ __global__ void __launch_bounds__(256) int8_plane_vec_kernel(int64_t count, cons
         h[2 * j] = sub2(__byte_perm(v[j], 0x64646464u, 0x4140), 0x64806480u);
         h[2 * j + 1] = sub2(__byte_perm(v[j], 0x64646464u, 0x4342), 0x64806480u);
     }
-    uint4 *o = reinterpret_cast<uint4 *>(plane) + 2 * i;
     o[0] = make_uint4(h[0], h[1], h[2], h[3]);
-    o[1] = make_uint4(h[4], h[5], h[6], h[7]);
+    if (both) o[1] = make_uint4(h[4], h[5], h[6], h[7]);
 }
-__global__ void __launch_bounds__(256) int8_plane_kernel(int64_t T, int64_t n, const uint8_t *X, __half *plane,
-                                                         int64_t ld, int *status) {
+__global__ void __launch_bounds__(256) int8_plane_vec_kernel(int64_t count, const uint8_t *X, uint32_t *plane,
+                                                             int *status) {
     dependents_may_start();
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i == 0) *status = 0;
-    if (i >= T * n) return;
-    plane[i / n * ld + i % n] = __int2half_rn((int)X[i] - 128);
+    if (i < count)
+        store_codes(reinterpret_cast<uint4 *>(plane) + 2 * i, __ldg(reinterpret_cast<const uint4 *>(X) + i), true);
 }
-// rows of W at a 16-byte stride
+// any width and address; 16 codes a thread, ld a multiple of 8
+__global__ void __launch_bounds__(256) int8_plane_kernel(int64_t T, int64_t n, const uint8_t *X, __half *plane,
+                                                         int64_t ld, int *status) {
+    dependents_may_start();
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, pieces = (n + 15) / 16;
+    if (i == 0) *status = 0;
+    if (i >= T * pieces) return;
+    int64_t c;
+    const int64_t t = divide(i, pieces, c);
+    store_codes(reinterpret_cast<uint4 *>(plane + t * ld + c * 16), load16(X + t * n + c * 16, X, X + T * n),
+                c * 16 + 8 < ld);
+}
+// rows of W at a stride of whole 16-byte pieces (what pads them lies outside the tensor map)
 __global__ void __launch_bounds__(256) int8_pad_kernel(int64_t m, int64_t rb, const uint8_t *W, uint8_t *out,
                                                        int64_t ld) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= m * rb) return;
-    out[i / rb * ld + i % rb] = W[i];
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, pieces = ld / 16;
+    if (i >= m * pieces) return;
+    int64_t c;
+    const int64_t r = divide(i, pieces, c);
+    reinterpret_cast<uint4 *>(out)[i] = load16(W + r * rb + c * 16, W, W + m * rb);
 }
 
 int64_t pad8(int64_t x) { return (x + 7) / 8 * 8; }
@@ -536,7 +544,7 @@ realq_status_t int8_product_tc(cudaStream_t s, int64_t T, int64_t n, int64_t m, 
         ldw = pad16(rb);
         w = b.w;
         Launch L("int8_product_pad", s);
-        int8_pad_kernel<<<(unsigned)((m * rb + 255) / 256), 256, 0, s>>>(m, rb, W, b.w, ldw);
+        int8_pad_kernel<<<(unsigned)((m * (ldw / 16) + 255) / 256), 256, 0, s>>>(m, rb, W, b.w, ldw);
         REALQ_TRY(check_launch("int8_product_pad"));
     }
     {
@@ -545,7 +553,7 @@ realq_status_t int8_product_tc(cudaStream_t s, int64_t T, int64_t n, int64_t m, 
             int8_plane_vec_kernel<<<(unsigned)((T * n / 16 + 255) / 256), 256, 0, s>>>(
                 T * n / 16, X, reinterpret_cast<uint32_t *>(b.x), b.status);
         else
-            int8_plane_kernel<<<(unsigned)((T * n + 255) / 256), 256, 0, s>>>(T, n, X, b.x, ldx, b.status);
+            int8_plane_kernel<<<(unsigned)((T * ((n + 15) / 16) + 255) / 256), 256, 0, s>>>(T, n, X, b.x, ldx, b.status);
     }
     REALQ_TRY(check_launch("int8_product_plane"));
     CUtensorMap mapW, mapX;
