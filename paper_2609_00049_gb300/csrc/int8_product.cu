@@ -132,7 +132,7 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there
     if constexpr (KEEP)
         asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
     else
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+        asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
 // A warp's sums over its share of K.
@@ -198,12 +198,12 @@ template <int WB, int NT, int RT> struct Sums {
 template <int WB, int NT, int RT> struct Ring {
     static constexpr int XP = WB == 8 ? 1 : 2;
     static constexpr int SLOT = (2 * RT + NT * XP) * 512;                // bytes of a warp's step
-    static constexpr int STAGES = 72 * 1024 / (SW * SLOT) < 6 ? 72 * 1024 / (SW * SLOT) : 6;
+    static constexpr int STAGES = 104 * 1024 / (SW * SLOT) < 8 ? 104 * 1024 / (SW * SLOT) : 8;
     static constexpr int BYTES = SW * SLOT * STAGES;
 };
 
 template <bool ALIGNED, int WB, int NT, int RT, typename TY>
-__global__ void __launch_bounds__(SW * 32, ALIGNED ? 3 : 2)
+__global__ void __launch_bounds__(SW * 32, 2)
     int8_stream_kernel(int64_t T, int64_t n, int64_t m, const uint8_t *X, const float *x_scale, const uint8_t *W,
                        const float *w_scale, const uint8_t *w_zero, TY *Y) {
     using S = Sums<WB, NT, RT>;
@@ -377,7 +377,7 @@ realq_status_t stream_launch(cudaStream_t s, int64_t T, int64_t n, int64_t m, co
     // CTAs over K: the count whose waves take the fewest steps of a warp, its
     // start and end counted as four, each warp keeping at least two.
     const int64_t rb = WB == 8 ? n : (n + 1) / 2, ctas = (m + RT * 16 - 1) / (RT * 16), steps = (rb + 63) / 64;
-    const int64_t slots = (int64_t)sms * (ALIGNED ? 3 : 2);
+    const int64_t slots = (int64_t)sms * 2;
     int cl = 1;
     int64_t best = INT64_MAX;
     for (int c = 1; c <= MAX_CLUSTER && (c == 1 || steps >= 2 * SW * c); c *= 2) {

@@ -7,12 +7,13 @@
 // it).  Past 2^24 each accumulated MMA may lose about a unit in the last place.
 //
 // The weight codes are converted on their way in, so that they cross HBM and L2
-// as bytes (or nibbles): TMA puts the codes of a 64-wide K step in shared
-// memory (64- or 32-byte swizzle: a thread reads its row's 16-byte chunks
+// as bytes (or nibbles): TMA puts the codes of a K step (64, or 128 where a
+// tile has at most 128 tokens and the waits between roles would cost more than
+// the MMAs) in shared memory (swizzled by row length: a thread reads its row's 16-byte chunks
 // without bank conflicts), eight converter warps, two groups taking turns, make
 // fp16 pairs of them (the byte as the low mantissa bits of 1024, less
 // 1024 + zero) and store them to TMEM as the MMA's A operand: lane = channel,
-// 32 columns per K step.  Shared memory then carries only the tokens' plane,
+// a column to two of K.  Shared memory then carries only the tokens' plane,
 // which a pass over the token codes writes as fp16 to the workspace; B is a
 // K-major tile of it (128-byte swizzle).
 //
@@ -21,7 +22,8 @@
 // are contiguous; two warps take turns at a lane quarter's 32-column blocks),
 // warps 16 and 17 issue the TMA loads of tokens and codes, warp 18 the MMAs.  TMEM: columns 0-255
 // hold the accumulator (two of them when a tile has at most 128 tokens, so that
-// a drain overlaps the next tile), 256-511 eight A slots.  The codes have a ring
+// a drain overlaps the next tile), 256-511 eight A slots of 64
+// K (four of 128).  The codes have a ring
 // of their own, freed by the converters, and run ahead of the tokens, whose
 // stages (and the A slots) the MMAs free: a stage of either then covers one
 // memory latency, not the conversion as well.  Tiles beyond whole
@@ -40,7 +42,6 @@ namespace {
 
 constexpr int TM = 128;                    // channels per tile
 constexpr int TNMAX = 256;                 // tokens per tile
-constexpr int KS = 64;                     // K per stage
 constexpr int MAX_STAGES = 8;              // of the tokens' ring and of A in TMEM
 constexpr int MAX_WSTAGES = 16;            // of the codes' ring
 constexpr int CONV_WARPS = 8, EPI_WARPS = 8;
@@ -56,6 +57,7 @@ __device__ __forceinline__ void store1(__nv_bfloat16 *p, float v) { *p = __float
 struct Shape {
     int64_t T, n, m;
     int N;            // tokens per tile, a multiple of 16
+    int kstep;        // K per stage
     int stages, wstages;   // ring lengths: tokens and A slots, codes
     int nti, ntj;     // tiles over channels, tokens
     int whole;        // tiles that keep their K range; the others are split
@@ -116,7 +118,7 @@ __device__ __forceinline__ uint32_t sub2(uint32_t a, uint32_t b) {
     return d;
 }
 
-template <int WB, typename TY>
+template <int WB, int KS, typename TY>
 __global__ void __launch_bounds__(THREADS, 1)
     int8_tc_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtensorMap mapX, const Shape sh,
                    const float *x_scale, const float *w_scale, const uint8_t *w_zero, TY *Y, float *part, int *err) {
@@ -137,7 +139,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 
     dependents_may_start();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int x_bytes = sh.N * KS * 2;           // a multiple of 1024, as W_BYTES
+    const int x_bytes = sh.N * KS * 2;           // a multiple of 1024, as W_BYTES; KS / 64 boxes
     const int items = sh.items, S = sh.stages, SW = sh.wstages;
     uint8_t *wring = smem + S * x_bytes;
     const bool two = sh.N <= 128;                // two accumulators
@@ -195,28 +197,34 @@ __global__ void __launch_bounds__(THREADS, 1)
                 }
                 tc::fence_after_sync();
                 const uint8_t *src = wring + rw.s * W_BYTES + row * WROW;
-                uint32_t h[32];
+                constexpr int CH = WB == 8 ? 4 : 2;   // 16-byte chunks to 64 of K
 #pragma unroll
-                for (int c = 0; c < WROW / 16; ++c) {
-                    // the swizzle's chunk of this row: bits 4-5 ^= bits 7-8 (bit 4 ^= bit 7)
-                    const int at = WB == 8 ? c ^ ((row >> 1) & 3) : c ^ ((row >> 2) & 1);
-                    const uint4 q = *reinterpret_cast<const uint4 *>(src + at * 16);
-                    const uint32_t v[4] = {q.x, q.y, q.z, q.w};
+                for (int o = 0; o < KS / 64; ++o) {
+                    uint32_t h[32];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if constexpr (WB == 8) {
-                            h[c * 8 + i * 2] = sub2(__byte_perm(v[i], 0x64646464u, 0x4140), base);
-                            h[c * 8 + i * 2 + 1] = sub2(__byte_perm(v[i], 0x64646464u, 0x4342), base);
-                        } else {
+                    for (int c = 0; c < CH; ++c) {
+                        // the swizzle's place of the row's chunk: 128-byte rows, bits 4-6 ^= 7-9; 64, bits 4-5 ^= 7-8;
+                        // 32, bit 4 ^= 7
+                        const int cc = o * CH + c;
+                        const int at = WROW == 128 ? cc ^ (row & 7) : (WROW == 64 ? cc ^ ((row >> 1) & 3) : cc ^ ((row >> 2) & 1));
+                        const uint4 q = *reinterpret_cast<const uint4 *>(src + at * 16);
+                        const uint32_t v[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-                            for (int b = 0; b < 4; ++b) {
-                                const uint32_t t = __byte_perm(v[i], 0u, 0x4040 | b | b << 8);
-                                h[c * 16 + i * 4 + b] = sub2((t & 0x00F0000Fu) | 0x54006400u, base);
+                        for (int i = 0; i < 4; ++i) {
+                            if constexpr (WB == 8) {
+                                h[c * 8 + i * 2] = sub2(__byte_perm(v[i], 0x64646464u, 0x4140), base);
+                                h[c * 8 + i * 2 + 1] = sub2(__byte_perm(v[i], 0x64646464u, 0x4342), base);
+                            } else {
+#pragma unroll
+                                for (int b = 0; b < 4; ++b) {
+                                    const uint32_t t = __byte_perm(v[i], 0u, 0x4040 | b | b << 8);
+                                    h[c * 16 + i * 4 + b] = sub2((t & 0x00F0000Fu) | 0x54006400u, base);
+                                }
                             }
                         }
                     }
+                    tc::tmem_st_32x32b_x32(a_base + (uint32_t)(r.s * (KS / 2) + o * 32), h);
                 }
-                tc::tmem_st_32x32b_x32(a_base + (uint32_t)(r.s * 32), h);
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(tc::smem_u32(&wempty[rw.s]));
                 tc::tmem_wait_st();
@@ -316,7 +324,9 @@ __global__ void __launch_bounds__(THREADS, 1)
                     if (!ok) break;
                     const uint32_t fb = tc::smem_u32(&fulls[r.s]);
                     tc::mbar_arrive_expect_tx(fb, (uint32_t)bytes);
-                    tc::tma_load_2d(tc::smem_u32(ring + r.s * bytes), map, fb, x, y);
+                    const uint32_t dst = tc::smem_u32(ring + r.s * bytes);
+                    tc::tma_load_2d(dst, map, fb, x, y);
+                    if (KS == 128 && !codes) tc::tma_load_2d(dst + (x_bytes >> 1), map, fb, x + 64, y);
                 }
             }
             // on abort, let the copies already issued land before the CTA exits
@@ -348,11 +358,12 @@ __global__ void __launch_bounds__(THREADS, 1)
                 if (!ok) break;
                 tc::fence_after_sync();
                 const uint64_t desc = desc0 + (uint32_t)(r.s * x_bytes >> 4);
-                const uint32_t a = tmem + 256u + (uint32_t)(r.s * 32);
+                const uint32_t a = tmem + 256u + (uint32_t)(r.s * (KS / 2));
                 if (tc::elect_one()) {
 #pragma unroll
                     for (int k = 0; k < KS / 16; ++k)
-                        tc::mma_f16_ts(d, a + k * 8, desc + k * 2, idesc, (kk > 0 || k > 0) ? 1u : 0u);
+                        tc::mma_f16_ts(d, a + k * 8, desc + (k & 3) * 2 + (k >> 2) * (uint32_t)(x_bytes >> 5), idesc,
+                                       (kk > 0 || k > 0) ? 1u : 0u);
                     tc::mma_commit(tc::smem_u32(&empty[r.s]));
                 }
                 __syncwarp();
@@ -464,15 +475,16 @@ Shape shape_of(int64_t T, int64_t n, int64_t m, int w_bits, int sms) {
     sh.N = (int)std::max<int64_t>(16, ((T + sh.ntj - 1) / sh.ntj + 15) / 16 * 16);
     sh.ntj = (int)((T + sh.N - 1) / sh.N);
     sh.nti = ceil_div(m, TM);
-    const int xb = sh.N * KS * 2, wb = TM * (w_bits == 8 ? KS : KS / 2);
-    sh.stages = std::min(MAX_STAGES, RING_BYTES / (xb + wb));
+    sh.kstep = sh.N <= 128 ? 128 : 64;
+    const int KS = sh.kstep, xb = sh.N * KS * 2, wb = TM * (w_bits == 8 ? KS : KS / 2);
+    sh.stages = std::min(MAX_STAGES * 64 / KS, RING_BYTES / (xb + wb));
     sh.wstages = std::min(MAX_WSTAGES, (RING_BYTES - sh.stages * xb) / wb);
     sh.ks = ceil_div(n, KS);
     const int64_t tiles = (int64_t)sh.nti * sh.ntj, rest = tiles % sms;
     int best = 1;
     int64_t cost = INT64_MAX;
     for (int s = 1; s <= MAX_SPLITS && (s == 1 || sh.ks / s >= 4) && rest > 0; ++s) {
-        const int64_t step = std::max(2 * sh.N, 360);
+        const int64_t step = std::max(2 * sh.N, 360) * KS / 64;
         const int64_t c = (rest * s + sms - 1) / sms * ((sh.ks + s - 1) / s * step + 1500) +
                           (s > 1 ? 5000 + 2 * rest * s * sh.N * TM * 4 / 3400 : 0);
         if (c < cost) {
@@ -505,14 +517,14 @@ struct ProductWs {
     }
 };
 
-template <int WB, typename TY>
+template <int WB, int KS, typename TY>
 realq_status_t tc_launch(cudaStream_t s, const Shape &sh, const CUtensorMap &mapW, const CUtensorMap &mapX,
                          const float *xs, const float *ws, const uint8_t *wz, TY *Y, const ProductWs &b, int sms) {
-    const void *k = reinterpret_cast<const void *>(int8_tc_kernel<WB, TY>);
+    const void *k = reinterpret_cast<const void *>(int8_tc_kernel<WB, KS, TY>);
     REALQ_TRY(set_smem_limit(k, SMEM_BYTES));
     {
         Launch L("int8_product_tc", s);
-        REALQ_CUDA_TRY(launch_overlapped(int8_tc_kernel<WB, TY>, dim3((unsigned)std::min(sh.items, sms)), dim3(THREADS),
+        REALQ_CUDA_TRY(launch_overlapped(int8_tc_kernel<WB, KS, TY>, dim3((unsigned)std::min(sh.items, sms)), dim3(THREADS),
                                          SMEM_BYTES, s, mapW, mapX, sh, xs, ws, wz, Y, b.part, b.status));
     }
     REALQ_TRY(check_launch("int8_product_tc"));
@@ -556,15 +568,19 @@ realq_status_t int8_product_tc(cudaStream_t s, int64_t T, int64_t n, int64_t m, 
             int8_plane_kernel<<<(unsigned)((T * ((n + 15) / 16) + 255) / 256), 256, 0, s>>>(T, n, X, b.x, ldx, b.status);
     }
     REALQ_TRY(check_launch("int8_product_plane"));
+    const int wrow = w_bits == 8 ? sh.kstep : sh.kstep / 2;
     CUtensorMap mapW, mapX;
-    CUresult cr = encode_tmap_2d_u8(&mapW, w, (uint64_t)rb, (uint64_t)m, (uint64_t)ldw, w_bits == 8 ? KS : KS / 2, TM,
-                                    w_bits == 8 ? 2 : 3);
+    CUresult cr = encode_tmap_2d_u8(&mapW, w, (uint64_t)rb, (uint64_t)m, (uint64_t)ldw, (uint32_t)wrow, TM,
+                                    wrow == 128 ? 1 : (wrow == 64 ? 2 : 3));
     if (cr == CUDA_SUCCESS)
-        cr = encode_tmap_2d_f16(&mapX, b.x, (uint64_t)n, (uint64_t)T, (uint64_t)ldx * 2, KS, (uint32_t)sh.N, 1);
+        cr = encode_tmap_2d_f16(&mapX, b.x, (uint64_t)n, (uint64_t)T, (uint64_t)ldx * 2, 64, (uint32_t)sh.N, 1);
     if (cr != CUDA_SUCCESS) return fail(REALQ_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)cr);
     auto run = [&](auto *y) {
-        return w_bits == 8 ? tc_launch<8>(s, sh, mapW, mapX, x_scale, w_scale, w_zero, y, b, sms)
-                           : tc_launch<4>(s, sh, mapW, mapX, x_scale, w_scale, w_zero, y, b, sms);
+        if (sh.kstep == 128)
+            return w_bits == 8 ? tc_launch<8, 128>(s, sh, mapW, mapX, x_scale, w_scale, w_zero, y, b, sms)
+                               : tc_launch<4, 128>(s, sh, mapW, mapX, x_scale, w_scale, w_zero, y, b, sms);
+        return w_bits == 8 ? tc_launch<8, 64>(s, sh, mapW, mapX, x_scale, w_scale, w_zero, y, b, sms)
+                           : tc_launch<4, 64>(s, sh, mapW, mapX, x_scale, w_scale, w_zero, y, b, sms);
     };
     return y_dtype == REALQ_BF16 ? run(static_cast<__nv_bfloat16 *>(Y)) : run(static_cast<float *>(Y));
 }
