@@ -405,11 +405,11 @@ __global__ void __launch_bounds__(256) grad_planes_kernel(const Planes p) {
 int64_t pad8(int64_t x) { return (x + 7) / 8 * 8; }
 
 // Token ranges: with fewer tiles than pairs of SMs, as many as fill them without
-// leaving a range under eight stages.
-int grad_splits(int64_t T, int64_t m, int64_t n, int sms) {
+// leaving a range under eight stages (dY's planes counted).
+int grad_splits(int64_t T, int64_t m, int64_t n, int planes, int sms) {
     const int64_t tiles = (int64_t)ceil_div(m, TT) * ceil_div(n, TT);
     int64_t s = sms / 2 / tiles;
-    s = std::min<int64_t>(s, T / (8 * KSTAGE));
+    s = std::min<int64_t>(s, T * planes / (8 * KSTAGE));
     return (int)std::max<int64_t>(1, std::min<int64_t>(s, MAX_SPLITS));
 }
 
@@ -431,12 +431,12 @@ struct GradWs {
 }  // namespace
 
 size_t checkpoint_grad_ws_bytes(int64_t T, int64_t m, int64_t n, realq_dtype_t dt, int sms) {
-    return GradWs(nullptr, T, m, n, dt, grad_splits(T, m, n, sms)).bytes;
+    return GradWs(nullptr, T, m, n, dt, grad_splits(T, m, n, dt == REALQ_F32 ? 3 : 1, sms)).bytes;
 }
 
 realq_status_t checkpoint_grad(cudaStream_t s, int64_t T, int64_t m, int64_t n, const void *dY, realq_dtype_t dt,
                                const int8_t *codes, const uint8_t *exps, float *dW, int accumulate, void *ws, int sms) {
-    int splits = grad_splits(T, m, n, sms);
+    int splits = grad_splits(T, m, n, dt == REALQ_F32 ? 3 : 1, sms);
     const GradWs w(ws, T, m, n, dt, splits);
     const bool direct = dt == REALQ_BF16 && m % 8 == 0;   // dY read where it lies
     const int planes = dt == REALQ_F32 ? 3 : 1;

@@ -215,180 +215,206 @@ __global__ void __launch_bounds__(SW * 32, 2)
     cg::cluster_group cluster = cg::this_cluster();
     const int CL = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    const int64_t i0 = (int64_t)(blockIdx.x / CL) * ROWS;
     const int64_t rb = WB == 8 ? n : (n + 1) / 2;   // bytes of a row of W
     const int pieces = (int)((rb + 15) / 16);
+    const int steps = (pieces + 3) / 4;             // four neighbouring pieces (64 bytes of each row) to a step
+    const int64_t tiles = (m + ROWS - 1) / ROWS;
+    const int64_t clusters = gridDim.x / CL;
 
-    const uint8_t *wrow[RT][2], *xrow[NT];
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int h = 0; h < 2; ++h)   // (rows past m repeat the last, unwritten)
-            wrow[r][h] = W + min(i0 + r * 16 + h * 8 + g, m - 1) * rb;
+    const uint8_t *xrow[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) xrow[t] = X + min((int64_t)(t * 8 + g), T - 1) * n;
+    auto rows_of = [&](int64_t tile, const uint8_t *(&wrow)[RT][2]) {   // (rows past m repeat the last, unwritten)
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) wrow[r][h] = W + min(tile * ROWS + r * 16 + h * 8 + g, m - 1) * rb;
+    };
     const uint4 zeros = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);   // codes of x = 0
 
-    // Four neighbouring pieces (64 bytes of each row) to a step.
-    const int steps = (pieces + 3) / 4;
-    S sums;
-    if constexpr (ALIGNED) {
-        // the cluster's warps take steps in turn
-        const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(ring)) + warp * R::SLOT + lane * 16;
-        auto fetch = [&](int k, int slot) {
-            const int64_t v = ((int64_t)k * CL * SW + rank * SW + warp) * 4 + q;
+    // ALIGNED: the warps of the cluster take a tile's steps in turn, `turns` each (some beyond the end, which read as
+    // zeros); the copies run ahead across tiles.
+    const int turns = (steps + CL * SW - 1) / (CL * SW);
+    int64_t ftile = blockIdx.x / CL;
+    int fturn = 0, fslot = 0, slot = 0;
+    const uint8_t *frow[RT][2];
+    const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(ring)) + warp * R::SLOT + lane * 16;
+    auto fetch = [&] {
+        if (ftile < tiles) {
+            const int64_t v = ((int64_t)(fturn * CL + rank) * SW + warp) * 4 + q;
             const bool there = v < pieces;
             const int64_t at = there ? v * 16 : 0;
-            const uint32_t dst = mine + slot * (SW * R::SLOT);
+            const uint32_t dst = mine + fslot * (SW * R::SLOT);
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) copy16<false>(dst + (2 * r + h) * 512, wrow[r][h] + at, there);
+                for (int h = 0; h < 2; ++h) copy16<false>(dst + (2 * r + h) * 512, frow[r][h] + at, there);
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int p = 0; p < XP; ++p)
                     copy16<true>(dst + (2 * RT + t * XP + p) * 512, xrow[t] + at * XP + p * 16, there);
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        };
-#pragma unroll
-        for (int k = 0; k < R::STAGES - 1; ++k) fetch(k, k);
-        int slot = 0;
-        for (int k = 0; k * CL * SW + rank * SW + warp < steps; ++k) {
-            fetch(k + R::STAGES - 1, slot == 0 ? R::STAGES - 1 : slot - 1);
-            asm volatile("cp.async.wait_group %0;" ::"n"(R::STAGES - 1) : "memory");
-            const uint4 *src = reinterpret_cast<const uint4 *>(ring + (slot * SW + warp) * R::SLOT) + lane;
-            uint4 wq[RT][2], kq[NT][XP];
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) wq[r][h] = src[(2 * r + h) * 32];
-            const bool there = (k * CL * SW + rank * SW + warp) * 4 + q < pieces;
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int p = 0; p < XP; ++p) kq[t][p] = there ? src[(2 * RT + t * XP + p) * 32] : zeros;
-            sums.step(wq, kq);
-            if (++slot == R::STAGES) slot = 0;
+            if (++fturn == turns) {
+                fturn = 0;
+                ftile += clusters;
+                rows_of(ftile, frow);
+            }
         }
-        asm volatile("cp.async.wait_all;" ::: "memory");
-    } else {
-        // Pairs of neighbouring steps in turn: a lane loads aligned pieces and has the following one
-        // from the next lane (the pair's last lane loads it itself).
-        const uint8_t *whi = W + m * rb, *xhi = X + T * n;
-        for (int s0 = 2 * (rank * SW + warp); s0 < steps; s0 += 2 * CL * SW) {
-            uint4 wq[2][RT][2], next[RT][2];
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (++fslot == R::STAGES) fslot = 0;
+    };
+    if constexpr (ALIGNED) {
+        rows_of(ftile, frow);
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
+        for (int k = 0; k < R::STAGES - 1; ++k) fetch();
+    }
+
+    for (int64_t tile = blockIdx.x / CL; tile < tiles; tile += clusters) {
+        S sums;
+        if constexpr (ALIGNED) {
+            for (int k = 0; k < turns; ++k) {
+                fetch();
+                asm volatile("cp.async.wait_group %0;" ::"n"(R::STAGES - 1) : "memory");
+                const uint4 *src = reinterpret_cast<const uint4 *>(ring + (slot * SW + warp) * R::SLOT) + lane;
+                uint4 wq[RT][2], kq[NT][XP];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint8_t *p = wrow[r][h] - (reinterpret_cast<uintptr_t>(wrow[r][h]) & 15) + ((int64_t)s0 * 4 + q) * 16;
-                    wq[0][r][h] = load_piece(p, W, whi);
-                    wq[1][r][h] = load_piece(p + 64, W, whi);
-                    if (q == 3) next[r][h] = load_piece(p + 80, W, whi);
-                }
-            const int src = (lane & ~3) | ((q + 1) & 3);
+                for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t mis = (uint32_t)(reinterpret_cast<uintptr_t>(wrow[r][h]) & 15);
-                    const uint4 n0 = shfl4(q == 0 ? wq[1][r][h] : wq[0][r][h], src), n1 = shfl4(wq[1][r][h], src);
-                    wq[0][r][h] = realign(wq[0][r][h], n0, mis);
-                    wq[1][r][h] = realign(wq[1][r][h], q == 3 ? next[r][h] : n1, mis);
-                }
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                if (s0 + u >= steps) break;   // (the same for the whole warp)
-                uint4 kq[NT][XP];
+                    for (int h = 0; h < 2; ++h) wq[r][h] = src[(2 * r + h) * 32];
+                const bool there = ((k * CL + rank) * SW + warp) * 4 + q < pieces;
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int p = 0; p < XP; ++p) {
-                        const int64_t c = (((int64_t)s0 + u) * 4 + q) * (16 * XP) + p * 16;   // first column
-                        kq[t][p] = zeros;
-                        if (c < n) {
-                            kq[t][p] = load16(xrow[t] + c, X, xhi);
-                            if (c + 16 > n) {   // columns from n on take no part
-                                const int left = (int)(n - c);
-                                kq[t][p] = make_uint4(first_bytes(kq[t][p].x, left), first_bytes(kq[t][p].y, left - 4),
-                                                      first_bytes(kq[t][p].z, left - 8), first_bytes(kq[t][p].w, left - 12));
+                    for (int p = 0; p < XP; ++p) kq[t][p] = there ? src[(2 * RT + t * XP + p) * 32] : zeros;
+                sums.step(wq, kq);
+                if (++slot == R::STAGES) slot = 0;
+            }
+        } else {
+            // Pairs of neighbouring steps in turn: a lane loads aligned pieces and has the following one
+            // from the next lane (the pair's last lane loads it itself).
+            const uint8_t *whi = W + m * rb, *xhi = X + T * n, *wrow[RT][2];
+            rows_of(tile, wrow);
+            for (int s0 = 2 * (rank * SW + warp); s0 < steps; s0 += 2 * CL * SW) {
+                uint4 wq[2][RT][2], next[RT][2];
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint8_t *p =
+                            wrow[r][h] - (reinterpret_cast<uintptr_t>(wrow[r][h]) & 15) + ((int64_t)s0 * 4 + q) * 16;
+                        wq[0][r][h] = load_piece(p, W, whi);
+                        wq[1][r][h] = load_piece(p + 64, W, whi);
+                        if (q == 3) next[r][h] = load_piece(p + 80, W, whi);
+                    }
+                const int src = (lane & ~3) | ((q + 1) & 3);
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t mis = (uint32_t)(reinterpret_cast<uintptr_t>(wrow[r][h]) & 15);
+                        const uint4 n0 = shfl4(q == 0 ? wq[1][r][h] : wq[0][r][h], src), n1 = shfl4(wq[1][r][h], src);
+                        wq[0][r][h] = realign(wq[0][r][h], n0, mis);
+                        wq[1][r][h] = realign(wq[1][r][h], q == 3 ? next[r][h] : n1, mis);
+                    }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    if (s0 + u >= steps) break;   // (the same for the whole warp)
+                    uint4 kq[NT][XP];
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int p = 0; p < XP; ++p) {
+                            const int64_t c = (((int64_t)s0 + u) * 4 + q) * (16 * XP) + p * 16;   // first column
+                            kq[t][p] = zeros;
+                            if (c < n) {
+                                kq[t][p] = load16(xrow[t] + c, X, xhi);
+                                if (c + 16 > n) {   // columns from n on take no part
+                                    const int left = (int)(n - c);
+                                    kq[t][p] =
+                                        make_uint4(first_bytes(kq[t][p].x, left), first_bytes(kq[t][p].y, left - 4),
+                                                   first_bytes(kq[t][p].z, left - 8), first_bytes(kq[t][p].w, left - 12));
+                                }
                             }
                         }
-                    }
-                sums.step(wq[u], kq);
+                    sums.step(wq[u], kq);
+                }
             }
         }
-    }
-    sums.flush();
+        sums.flush();
 
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
+        for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                red[warp * OUT + (t * 8 + 2 * q + (e & 1)) * ROWS + r * 16 + (e >> 1) * 8 + g] = sums.sum[r][t][e];
-    if (g == 0) {
+                for (int e = 0; e < 4; ++e)
+                    red[warp * OUT + (t * 8 + 2 * q + (e & 1)) * ROWS + r * 16 + (e >> 1) * 8 + g] = sums.sum[r][t][e];
+        if (g == 0) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) xred[warp * TOK + t * 8 + 2 * q + e] = __float2int_rn(sums.xacc[t][e]);
-    }
-    __syncthreads();
-    // the warps' shares, then the cluster's; integers, so any order is the same
-    for (int k = threadIdx.x; k < OUT + TOK; k += SW * 32) {
-        int *p = k < OUT ? red + k : xred + k - OUT;
-        const int step = k < OUT ? OUT : TOK;
-        int a = p[0];
+                for (int e = 0; e < 2; ++e) xred[warp * TOK + t * 8 + 2 * q + e] = __float2int_rn(sums.xacc[t][e]);
+        }
+        __syncthreads();
+        // the warps' shares, then the cluster's; integers, so any order is the same
+        for (int k = threadIdx.x; k < OUT + TOK; k += SW * 32) {
+            int *p = k < OUT ? red + k : xred + k - OUT;
+            const int step = k < OUT ? OUT : TOK;
+            int a = p[0];
 #pragma unroll
-        for (int w = 1; w < SW; ++w) a += p[w * step];
-        p[0] = a;
-    }
-    if (CL > 1) {
-        cluster.sync();
+            for (int w = 1; w < SW; ++w) a += p[w * step];
+            p[0] = a;
+        }
+        if (CL > 1) {
+            cluster.sync();
+            if (rank == 0) {
+                for (int k = threadIdx.x; k < OUT + TOK; k += SW * 32) {
+                    int *p = k < OUT ? red + k : xred + k - OUT;
+                    int a = p[0];
+                    for (int c = 1; c < CL; ++c) a += *cluster.map_shared_rank(p, c);
+                    p[0] = a;
+                }
+            }
+            cluster.sync();   // the other CTAs' sums have been read
+        } else {
+            __syncthreads();
+        }
         if (rank == 0) {
-            for (int k = threadIdx.x; k < OUT + TOK; k += SW * 32) {
-                int *p = k < OUT ? red + k : xred + k - OUT;
-                int a = p[0];
-                for (int c = 1; c < CL; ++c) a += *cluster.map_shared_rank(p, c);
-                p[0] = a;
+            for (int k = threadIdx.x; k < OUT; k += SW * 32) {
+                const int64_t i = tile * ROWS + k % ROWS, t = k / ROWS;
+                if (i < m && t < T) {
+                    const int z = w_zero ? w_zero[i] : (WB == 8 ? 128 : 8);
+                    // (mod 2^32: the true sum fits, its two parts need not)
+                    const int v = (int)((uint32_t)red[k] - (uint32_t)z * (uint32_t)xred[k / ROWS]);
+                    store1(Y + t * m + i, (float)v * __ldg(x_scale + t) * __ldg(w_scale + i));
+                }
             }
         }
-        cluster.sync();   // the other CTAs' sums have been read
-        if (rank != 0) return;
-    } else {
-        __syncthreads();
+        __syncthreads();   // the sums have been read
     }
-    for (int k = threadIdx.x; k < OUT; k += SW * 32) {
-        const int64_t i = i0 + k % ROWS, t = k / ROWS;
-        if (i < m && t < T) {
-            const int z = w_zero ? w_zero[i] : (WB == 8 ? 128 : 8);
-            // (mod 2^32: the true sum fits, its two parts need not)
-            const int v = (int)((uint32_t)red[k] - (uint32_t)z * (uint32_t)xred[k / ROWS]);
-            store1(Y + t * m + i, (float)v * __ldg(x_scale + t) * __ldg(w_scale + i));
-        }
-    }
+    if constexpr (ALIGNED) asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 template <bool ALIGNED, int WB, int NT, int RT, typename TY>
 realq_status_t stream_launch(cudaStream_t s, int64_t T, int64_t n, int64_t m, const uint8_t *X, const float *xs,
                              const uint8_t *W, const float *ws, const uint8_t *wz, TY *Y, int sms) {
-    // CTAs over K: the count whose waves take the fewest steps of a warp, its
-    // start and end counted as four, each warp keeping at least two.
-    const int64_t rb = WB == 8 ? n : (n + 1) / 2, ctas = (m + RT * 16 - 1) / (RT * 16), steps = (rb + 63) / 64;
+    // Clusters walk the tiles of RT x 16 channels; CTAs over K: the count whose
+    // turns take the fewest steps of a warp, a tile's end counted as two, each
+    // warp keeping at least two steps.
+    const int64_t rb = WB == 8 ? n : (n + 1) / 2, tiles = (m + RT * 16 - 1) / (RT * 16), steps = (rb + 63) / 64;
     const int64_t slots = (int64_t)sms * 2;
     int cl = 1;
     int64_t best = INT64_MAX;
     for (int c = 1; c <= MAX_CLUSTER && (c == 1 || steps >= 2 * SW * c); c *= 2) {
-        const int64_t cost = (ctas * c + slots - 1) / slots * ((steps + SW * c - 1) / (SW * c) + 4);
+        const int64_t held = slots / c;   // clusters at once
+        const int64_t cost = (tiles + held - 1) / held * ((steps + SW * c - 1) / (SW * c) + 2);
         if (cost < best) {
             best = cost;
             cl = c;
         }
     }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(ctas * cl));
+    cfg.gridDim = dim3((unsigned)(std::min(tiles, slots / cl) * cl));
     cfg.blockDim = dim3(SW * 32);
     cfg.dynamicSmemBytes = ALIGNED ? Ring<WB, NT, RT>::BYTES : 0;
     cfg.stream = s;

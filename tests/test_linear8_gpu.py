@@ -548,3 +548,45 @@ def test_weight_grad_of_no_tokens():
     assert (dW == 1).all()
     rq.realq_checkpoint_weight_grad(*none, dW)
     assert (dW == 0).all()
+
+
+# ------------------------------------------------------ together: the head ---
+@pytest.mark.parametrize("T,d,vocab,dtype", [(1, 128, 1000, torch.bfloat16), (5, 96, 777, torch.float32),
+                                             (130, 256, 4096, torch.bfloat16), (300, 1024, 5001, torch.float32)])
+def test_head_scores_and_trains(T, d, vocab, dtype):
+    from paper_2609_00049_gb300.head import Head8
+    g = gen(T)
+    W = 0.05 * torch.randn(vocab, d, generator=g, device="cuda")
+    h = torch.randn(T, d, generator=g, device="cuda")
+    y = torch.randint(0, vocab, (T,), generator=g, device="cuda")
+    if T > 2:
+        y[2] = -1
+    head = Head8(W, logits_dtype=dtype)
+    step = head.forward(h, y, k=min(5, vocab))
+    # the codes' own values give the logits exactly, up to the scales' roundings and the logits' type
+    x8, w8 = torch.empty_like(h), torch.empty_like(W)
+    xc, xs = torch.empty(T, d, dtype=torch.uint8, device="cuda"), torch.empty(T, device="cuda")
+    rq.realq_quantize_activations(h, 8, 1.0, X_q=x8, codes=xc, scale=xs)
+    rq.realq_quantize_activations(W, 8, 1.0, X_q=w8)
+    logits = x8.double() @ w8.double().T
+    tol = (x8.double().abs() @ w8.double().abs().T) * 2 * U + logits.abs() * (4 * U + (BF if dtype == torch.bfloat16 else 0.0))
+    assert ((step.logits.double() - logits).abs() <= tol).all()
+    # scores and gradient are those of the logits as they were stored
+    stored = step.logits.clone()
+    ref = forward_exact(stored, y, 5)
+    check_forward(dict(logprob=step.logprob, norm=step.norm, entropy=step.entropy, top_ids=step.top_ids,
+                       top_logprob=step.top_logprob), ref, vocab, 5)
+    scored = y >= 0
+    assert abs(step.perplexity() / math.exp(-ref["logprob"][scored].mean().item()) - 1) <= sum_bound(vocab) + 40 * U
+    w = torch.where(scored, -1.0 / scored.sum(), 0.0).float()
+    dW = head.weight_grad(step, w)
+    X = torch.empty(T, d, device="cuda")
+    rq.realq_checkpoint_unpack(step.codes, step.exps, X)
+    dl, size = grad_exact(stored, y, w, torch.zeros(T, device="cuda"), None, None)
+    err = size * (sum_bound(vocab) * (4 + 2 * math.log(vocab)) + 16 * U + 400 * U) + (dl.abs() * BF if dtype == torch.bfloat16 else 0.0) * (1 + BF) + 1e-37
+    bound = err.T @ X.double().abs() + weight_grad_bound(T, (dl.abs() + err).float(), X)
+    assert ((dW.double() - dl.T @ X.double()).abs() <= bound * 1.01).all()
+    # (checkpoints of h, not of its 8-bit row codes: half a step of 1/64 of a block's largest value)
+    assert ((X - h).abs() <= h.abs().amax(dim=1, keepdim=True) / 64).all()
+    with pytest.raises(ValueError):
+        head.weight_grad(step, w)
