@@ -212,6 +212,11 @@ __global__ void __launch_bounds__(SW * 32, 2)
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ int red[SW * OUT];
     __shared__ int xred[SW * TOK];
+    const int64_t tok0 = (int64_t)blockIdx.y * TOK;   // this CTA's group of tokens
+    T -= tok0;
+    X += tok0 * n;
+    x_scale += tok0;
+    Y += tok0 * m;
     cg::cluster_group cluster = cg::this_cluster();
     const int CL = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
@@ -402,7 +407,7 @@ realq_status_t stream_launch(cudaStream_t s, int64_t T, int64_t n, int64_t m, co
     // turns take the fewest steps of a warp, a tile's end counted as two, each
     // warp keeping at least two steps.
     const int64_t rb = WB == 8 ? n : (n + 1) / 2, tiles = (m + RT * 16 - 1) / (RT * 16), steps = (rb + 63) / 64;
-    const int64_t slots = (int64_t)sms * 2;
+    const int64_t groups = (T + NT * 8 - 1) / (NT * 8), slots = std::max<int64_t>(2 * sms / groups, MAX_CLUSTER);
     int cl = 1;
     int64_t best = INT64_MAX;
     for (int c = 1; c <= MAX_CLUSTER && (c == 1 || steps >= 2 * SW * c); c *= 2) {
@@ -414,7 +419,7 @@ realq_status_t stream_launch(cudaStream_t s, int64_t T, int64_t n, int64_t m, co
         }
     }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(std::min(tiles, slots / cl) * cl));
+    cfg.gridDim = dim3((unsigned)(std::min(tiles, slots / cl) * cl), (unsigned)groups);
     cfg.blockDim = dim3(SW * 32);
     cfg.dynamicSmemBytes = ALIGNED ? Ring<WB, NT, RT>::BYTES : 0;
     cfg.stream = s;
@@ -455,15 +460,21 @@ realq_status_t stream(cudaStream_t s, int64_t T, int64_t n, int64_t m, const uin
                    : stream_tokens<false, WB, TY>(s, T, n, m, X, xs, W, ws, wz, Y, sms);
 }
 
-// Tokens up to which the streaming kernel runs.  8192 -> 28672: 16 tokens take
-// 57 us here and 56 in the tensor-core product with 8-bit weights, 42 and 60
-// with 4-bit ones; at 1024 -> 2048 3.0 and 9.4.
-constexpr int64_t STREAM_T = 16;
+// Whether the streaming kernel runs: for up to 16 tokens (8192 -> 28672: 16
+// tokens take 44 us here, 47 in the tensor-core product with 8-bit weights, 40
+// and 47 with 4-bit ones), and for up to 64 where reading the codes once for
+// every 16 of them is less than the other product's planes, launches and ramps
+// (1024 -> 2048: 64 tokens 5.4 and 7.8 us, 128 tokens 9.2 and 8.8).
+constexpr int64_t GROUP = 16, MOST_GROUPED = 64, STREAM_BYTES = 24 << 20;
+bool streams(int64_t T, int64_t n, int64_t m, int w_bits) {
+    const int64_t bytes = m * (w_bits == 8 ? n : (n + 1) / 2);
+    return T <= GROUP || (T <= MOST_GROUPED && (T + GROUP - 1) / GROUP * bytes <= STREAM_BYTES);
+}
 
 }  // namespace
 
 size_t int8_product_ws_bytes(int64_t T, int64_t n, int64_t m, int w_bits, int sms) {
-    return T <= STREAM_T ? 256 : int8_tc_ws_bytes(T, n, m, w_bits, sms);
+    return streams(T, n, m, w_bits) ? 256 : int8_tc_ws_bytes(T, n, m, w_bits, sms);
 }
 
 realq_status_t int8_product(cudaStream_t s, int64_t T, int64_t n, int64_t m, const uint8_t *X, const float *x_scale,
@@ -472,11 +483,12 @@ realq_status_t int8_product(cudaStream_t s, int64_t T, int64_t n, int64_t m, con
     // (whole 16-byte rows at an odd address cannot be a tensor map's, and are
     // streamed for 16 tokens at a time)
     const bool odd = (w_bits == 8 ? n : (n + 1) / 2) % 16 == 0 && (reinterpret_cast<uintptr_t>(W) & 15) != 0;
-    if (T > STREAM_T && !odd)
+    if (!odd && !streams(T, n, m, w_bits))
         return int8_product_tc(s, T, n, m, X, x_scale, W, w_bits, w_scale, w_zero, Y, y_dtype, ws, sms);
     auto run = [&](auto *y) -> realq_status_t {
-        for (int64_t t = 0; t < T; t += STREAM_T) {
-            const int64_t k = std::min(STREAM_T, T - t);
+        constexpr int64_t MOST = GROUP * 65535;   // a grid's
+        for (int64_t t = 0; t < T; t += MOST) {
+            const int64_t k = std::min(MOST, T - t);
             REALQ_TRY(w_bits == 8 ? stream<8>(s, k, n, m, X + t * n, x_scale + t, W, w_scale, w_zero, y + t * m, sms)
                                   : stream<4>(s, k, n, m, X + t * n, x_scale + t, W, w_scale, w_zero, y + t * m, sms));
         }
