@@ -114,6 +114,17 @@ def test_product_of_unaligned_codes(T, bx, bw, w_bits):
     assert ((Y - ref).abs() <= product_bound(N, ref, 352, torch.float32)).all()
 
 
+@pytest.mark.parametrize("T,n,m", [(17, 4096, 6400), (40, 4096, 4200), (64, 5120, 5000), (2100, 320, 2500), (3, 256, 20000),
+                                   (12, 320, 20003), (5, 33, 11000)])
+@pytest.mark.parametrize("w_bits", [8, 4])
+def test_product_of_many_tiles(T, n, m, w_bits):
+    """Token tiles of every width, more tiles than SMs, and more rows than the streaming CTAs hold at once."""
+    c = product_case(T, n, m, w_bits, True, seed=m)
+    N, ref = product_exact(*c, w_bits)
+    Y = run_product(*c, w_bits, torch.float32).double()
+    assert ((Y - ref).abs() <= product_bound(N, ref, n, torch.float32)).all()
+
+
 def test_product_of_the_sweeps_codes():
     """The sweep's 4-bit codes, scales and zero points (one group per row) run as
     they are and give the dequantized weights' product."""
@@ -514,6 +525,14 @@ def test_weight_grad_matches_the_definition(T, m, n, dtype):
     both = weight_grad(dy, codes, exps, base.clone(), accumulate=True)
     assert ((both.double() - (ref + base.double())).abs() <= weight_grad_bound(T, dy, X) + 2 * U * (ref.abs() + base.double().abs())).all()
     assert torch.equal(got, weight_grad(dy, codes, exps))   # bitwise repeatable
+
+
+@pytest.mark.parametrize("T,m,n", [(300, 2600, 2200), (700, 64, 20000), (129, 20001, 70)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_weight_grad_of_many_tiles(T, m, n, dtype):
+    dy, codes, exps, X = weight_grad_case(T, m, n, dtype, seed=T)
+    ref = dy.double().T @ X.double()
+    assert ((weight_grad(dy, codes, exps).double() - ref).abs() <= weight_grad_bound(T, dy, X)).all()
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
