@@ -481,6 +481,25 @@ def test_checkpoint_of_the_ends_of_the_range():
     assert (y[:, 32:] == 1.5).all() and exps[4:7, 0].tolist() == [255] * 3
 
 
+def test_checkpoint_of_tiny_and_huge_bf16():
+    """Blocks whose scale is no bf16 number, and subnormal values beside the smallest that is."""
+    g = gen(0)
+    x = torch.randn(64, 256, generator=g, device="cuda")
+    e = torch.arange(64, device="cuda")
+    x[:32] *= torch.exp2(-133.0 + 0.5 * e[:32, None])     # 2^-133 .. 2^-117
+    x[32:] *= torch.exp2(94.0 + e[32:, None].clamp(max=62) - 32)
+    x = x.clamp(-3e38, 3e38).to(torch.bfloat16)
+    codes = torch.empty(64, 256, dtype=torch.int8, device="cuda")
+    exps = torch.empty(64, 8, dtype=torch.uint8, device="cuda")
+    rq.realq_checkpoint_pack(x, codes, exps)
+    q, byte, val = pack_exact(x)
+    assert torch.equal(codes, q) and torch.equal(exps, byte)
+    for out_dtype in (torch.float32, torch.bfloat16):
+        y = torch.empty(64, 256, dtype=out_dtype, device="cuda")
+        rq.realq_checkpoint_unpack(codes, exps, y)
+        assert torch.equal(y.double(), val)
+
+
 # ------------------------------------------------------- weight gradients ---
 def weight_grad_case(T, m, n, dtype, seed=0):
     g = gen(seed)
