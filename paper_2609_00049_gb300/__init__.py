@@ -386,15 +386,30 @@ def realq_quantize_activations(X: torch.Tensor, bits: int = 4, a_clip: float = 0
 
 
 # ------------------------------------------------- 8-bit linear operators ---
+# (Small calls of these take less time on the GPU than in here, so an argument's
+# checks and its address are one call.)
 TOP_MAX = 32
+
+
+def _arg(t: Optional[torch.Tensor], dtype, shape, name: str):
+    """_need and _ptr together."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if not (t.is_cuda and t.is_contiguous()):
+        raise ValueError(f"{name}: expected a contiguous CUDA tensor")
+    return t.data_ptr()
 
 
 def _rows(t: torch.Tensor, name: str):
     """Address and row stride of a matrix whose rows may lie apart."""
+    if not t.is_cuda:
+        raise ValueError(f"{name}: expected a CUDA tensor")
+    if t.is_contiguous() and t.dim() == 2:
+        return t.data_ptr(), t.shape[1]
     if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
         raise ValueError(f"{name}: expected a matrix with contiguous, non-overlapping rows")
-    if not t.is_cuda:
-        raise ValueError("expected a CUDA tensor")
     return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
 
 
@@ -410,15 +425,12 @@ def realq_int8_product(X_codes: torch.Tensor, x_scale: torch.Tensor, W_codes: to
     channel codes.  w_zero None: 2^(w_bits - 1)."""
     T, n = X_codes.shape
     m = W_codes.shape[0]
-    _need(X_codes, torch.uint8, (T, n), "X_codes")
-    _need(W_codes, torch.uint8, (m, n if w_bits == 8 else (n + 1) // 2), "W_codes")
-    _need(x_scale, torch.float32, (T,), "x_scale")
-    _need(w_scale, torch.float32, (m,), "w_scale")
-    _need(w_zero, torch.uint8, (m,), "w_zero")
-    _need(Y, Y.dtype, (T, m), "Y")
     wp, wb = _ws(ws)
-    _check(lib().realq_int8_product(_stream(stream), T, n, m, _ptr(X_codes), _ptr(x_scale), _ptr(W_codes), w_bits,
-                                    _ptr(w_scale), _ptr(w_zero), _ptr(Y), _dtype(Y), wp, wb))
+    x, xs = _arg(X_codes, torch.uint8, (T, n), "X_codes"), _arg(x_scale, torch.float32, (T,), "x_scale")
+    w = _arg(W_codes, torch.uint8, (m, n if w_bits == 8 else (n + 1) // 2), "W_codes")
+    wsc, wz = _arg(w_scale, torch.float32, (m,), "w_scale"), _arg(w_zero, torch.uint8, (m,), "w_zero")
+    _check(lib().realq_int8_product(_stream(stream), T, n, m, x, xs, w, w_bits, wsc, wz, _arg(Y, Y.dtype, (T, m), "Y"),
+                                    _dtype(Y), wp, wb))
     return Y
 
 
@@ -434,14 +446,11 @@ def realq_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor],
     k = 0 if top_ids is None else top_ids.shape[1]
     if top_logprob is not None and top_ids is None:
         raise ValueError("top_logprob needs top_ids")
-    _need(targets, torch.int64, (T,), "targets")
-    _need(logprob, torch.float32, (T,), "logprob")
-    _need(norm, torch.float32, (T, 2), "norm")
-    _need(entropy, torch.float32, (T,), "entropy")
-    _need(top_ids, torch.int64, (T, k), "top_ids")
-    _need(top_logprob, torch.float32, (T, k), "top_logprob")
-    _check(lib().realq_token_logprobs(_stream(stream), T, V, ld, p, _dtype(logits), _ptr(targets), _ptr(logprob),
-                                      _ptr(norm), _ptr(entropy), k, _ptr(top_ids), _ptr(top_logprob)))
+    _check(lib().realq_token_logprobs(
+        _stream(stream), T, V, ld, p, _dtype(logits), _arg(targets, torch.int64, (T,), "targets"),
+        _arg(logprob, torch.float32, (T,), "logprob"), _arg(norm, torch.float32, (T, 2), "norm"),
+        _arg(entropy, torch.float32, (T,), "entropy"), k, _arg(top_ids, torch.int64, (T, k), "top_ids"),
+        _arg(top_logprob, torch.float32, (T, k), "top_logprob")))
 
 
 def realq_token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Tensor], norm: torch.Tensor,
@@ -457,17 +466,12 @@ def realq_token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Tens
         raise ValueError("d_logits must match logits")
     pd, ldd = _rows(d_logits, "d_logits")
     k = 0 if d_top is None else d_top.shape[1]
-    _need(targets, torch.int64, (T,), "targets")
-    _need(norm, torch.float32, (T, 2), "norm")
-    _need(d_logprob, torch.float32, (T,), "d_logprob")
-    _need(entropy, torch.float32, (T,), "entropy")
-    _need(d_entropy, torch.float32, (T,), "d_entropy")
-    _need(d_top, torch.float32, (T, k), "d_top")
-    if k:
-        _need(top_ids, torch.int64, (T, k), "top_ids")
-    _check(lib().realq_token_logprobs_grad(_stream(stream), T, V, ld, p, _dtype(logits), _ptr(targets), _ptr(norm),
-                                           _ptr(d_logprob), _ptr(entropy), _ptr(d_entropy), k,
-                                           _ptr(top_ids) if k else None, _ptr(d_top) if k else None, ldd, pd))
+    _check(lib().realq_token_logprobs_grad(
+        _stream(stream), T, V, ld, p, _dtype(logits), _arg(targets, torch.int64, (T,), "targets"),
+        _arg(norm, torch.float32, (T, 2), "norm"), _arg(d_logprob, torch.float32, (T,), "d_logprob"),
+        _arg(entropy, torch.float32, (T,), "entropy"), _arg(d_entropy, torch.float32, (T,), "d_entropy"), k,
+        _arg(top_ids, torch.int64, (T, k), "top_ids") if k else None,
+        _arg(d_top, torch.float32, (T, k), "d_top") if k else None, ldd, pd))
     return d_logits
 
 
@@ -475,17 +479,16 @@ def realq_checkpoint_pack(X: torch.Tensor, codes: torch.Tensor, exps: torch.Tens
     """Keep X (T x n) as 8-bit codes with a power-of-two scale byte per 32 values
     of a token: codes int8 T x n, exps uint8 T x ceil(n/32)."""
     T, n = X.shape
-    _need(codes, torch.int8, (T, n), "codes")
-    _need(exps, torch.uint8, (T, (n + 31) // 32), "exps")
-    _check(lib().realq_checkpoint_pack(_stream(stream), T, n, _ptr(X), _dtype(X), _ptr(codes), _ptr(exps)))
+    c, e = _arg(codes, torch.int8, (T, n), "codes"), _arg(exps, torch.uint8, (T, (n + 31) // 32), "exps")
+    _check(lib().realq_checkpoint_pack(_stream(stream), T, n, _ptr(X), _dtype(X), c, e))
 
 
 def realq_checkpoint_unpack(codes: torch.Tensor, exps: torch.Tensor, X: torch.Tensor, stream=None) -> torch.Tensor:
+    """The values of a checkpoint, written to X (T x n, bf16 or fp32)."""
     T, n = codes.shape
-    _need(codes, torch.int8, (T, n), "codes")
-    _need(exps, torch.uint8, (T, (n + 31) // 32), "exps")
-    _need(X, X.dtype, (T, n), "X")
-    _check(lib().realq_checkpoint_unpack(_stream(stream), T, n, _ptr(codes), _ptr(exps), _ptr(X), _dtype(X)))
+    _check(lib().realq_checkpoint_unpack(_stream(stream), T, n, _arg(codes, torch.int8, (T, n), "codes"),
+                                         _arg(exps, torch.uint8, (T, (n + 31) // 32), "exps"),
+                                         _arg(X, X.dtype, (T, n), "X"), _dtype(X)))
     return X
 
 
@@ -500,12 +503,11 @@ def realq_checkpoint_weight_grad(dY: torch.Tensor, codes: torch.Tensor, exps: to
     """dW (fp32) = dY^T X (added to dW with accumulate), X read from its 8-bit checkpoint."""
     T, m = dY.shape
     n = codes.shape[1]
-    _need(codes, torch.int8, (T, n), "codes")
-    _need(exps, torch.uint8, (T, (n + 31) // 32), "exps")
-    _need(dW, torch.float32, (m, n), "dW")
     wp, wb = _ws(ws)
-    _check(lib().realq_checkpoint_weight_grad(_stream(stream), T, m, n, _ptr(dY), _dtype(dY), _ptr(codes), _ptr(exps),
-                                              _ptr(dW), int(bool(accumulate)), wp, wb))
+    _check(lib().realq_checkpoint_weight_grad(
+        _stream(stream), T, m, n, _ptr(dY), _dtype(dY), _arg(codes, torch.int8, (T, n), "codes"),
+        _arg(exps, torch.uint8, (T, (n + 31) // 32), "exps"), _arg(dW, torch.float32, (m, n), "dW"),
+        int(bool(accumulate)), wp, wb))
     return dW
 
 

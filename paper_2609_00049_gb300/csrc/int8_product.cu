@@ -432,7 +432,7 @@ realq_status_t stream_launch(cudaStream_t s, int64_t T, int64_t n, int64_t m, co
     attr[0].val.clusterDim.x = (unsigned)cl;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cl > 1 ? 1 : 0;
     {
         Launch L("int8_product_stream", s);
         REALQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, int8_stream_kernel<ALIGNED, WB, NT, RT, TY>, T, n, m, X, xs, W, ws, wz, Y, status));

@@ -576,7 +576,7 @@ realq_status_t fwd_launch(cudaStream_t s, int64_t T, int64_t V, int64_t ld, cons
     attr[0].val.clusterDim.x = (unsigned)cl;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cl > 1 ? 1 : 0;
     {
         Launch L("token_logprobs", s);
         REALQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, logprobs_kernel<TX>, (int)V, ld, static_cast<const TX *>(X), targets,
