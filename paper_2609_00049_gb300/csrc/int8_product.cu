@@ -24,6 +24,11 @@
 // (FLUSH), so the result is the exact integer sum whatever the codes.  The
 // eight warps of a CTA, and up to eight CTAs of a cluster where channels alone
 // do not fill the SMs evenly, add their shares of K as integers.
+//
+// Measured, 8 tokens x 8192 x 28672: 37.7 us with 8-bit weights (235 MB at 6.2
+// TB/s, 0.92 of the copy rate); 26 us with 4-bit ones (4.5 TB/s: half the bytes
+// but the same conversions and products; the issue slots are 54 % and the ALU
+// pipe 56 % busy, the tensor pipe 39 %).  1 token x 1024 x 2048: 2.5 us, a launch.
 #include <cooperative_groups.h>
 
 #include <algorithm>

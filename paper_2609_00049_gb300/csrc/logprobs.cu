@@ -26,6 +26,13 @@
 // their columns.
 //
 // All sums are fp32 per thread (a few hundred terms), joined pairwise.
+//
+// Measured, 4096 rows x 128256 in bf16: 183 us with 5 alternatives (5.7 TB/s),
+// 165 without (6.4 TB/s); the rows' ends, where the candidates are ranked, are
+// the difference.  Taking the arithmetic's clamp or its packing away does not
+// change it, more CTAs per SM (five or six, 40 to 48 registers) make it slower
+// (208 to 217 us).  The gradient: 313 us (6.7 TB/s).  One row: 10 us, of which
+// reading it takes 2.
 #include <cooperative_groups.h>
 
 #include "kernels.cuh"
