@@ -272,7 +272,7 @@ realq_status_t realq_quantize_activations(realq_stream_t stream, int64_t T, int6
  *            realq_workspace_status reads (REALQ_ERR_TIMEOUT: Y holds NaN
  *            where a bounded wait gave up).
  * Any alignment of the codes.  n at most REALQ_INT8_PRODUCT_MAX_N, T and m
- * below 2^30.  T = 0 is a no-op.  Asynchronous. */
+ * below 2^30, T m at most 2^40.  T = 0 is a no-op.  Asynchronous. */
 #define REALQ_INT8_PRODUCT_MAX_N 131071
 size_t realq_int8_product_workspace_size(int64_t T, int64_t n, int64_t m, int w_bits);
 realq_status_t realq_int8_product(realq_stream_t stream, int64_t T, int64_t n, int64_t m, const uint8_t *X_codes,

@@ -370,8 +370,9 @@ realq_status_t realq_int8_product(realq_stream_t stream, int64_t T, int64_t n, i
     if (!X_codes || !x_scale || !W_codes || !w_scale || !Y) return fail(REALQ_ERR_INVALID_ARG, "int8_product: NULL argument");
     if (reinterpret_cast<uintptr_t>(Y) % (y_dtype == REALQ_BF16 ? 2 : 4))
         return fail(REALQ_ERR_INVALID_ARG, "int8_product: Y is not aligned to its type");
-    if (n > REALQ_INT8_PRODUCT_MAX_N || m >= (1ll << 30) || T >= (1ll << 30))
-        return fail(REALQ_ERR_UNSUPPORTED, "int8_product: n at most %d, m and T below 2^30", REALQ_INT8_PRODUCT_MAX_N);
+    if (n > REALQ_INT8_PRODUCT_MAX_N || m >= (1ll << 30) || T >= (1ll << 30) || T * m > (1ll << 40))
+        return fail(REALQ_ERR_UNSUPPORTED, "int8_product: n at most %d, m and T below 2^30, T m at most 2^40",
+                    REALQ_INT8_PRODUCT_MAX_N);
     REALQ_TRY(check_ws(ws, ws_bytes, int8_product_ws_bytes(T, n, m, w_bits, num_sms()), "int8_product"));
     return int8_product(S(stream), T, n, m, X_codes, x_scale, W_codes, w_bits, w_scale, w_zero, Y, y_dtype, ws, num_sms());
 }
@@ -455,8 +456,8 @@ realq_status_t realq_checkpoint_weight_grad(realq_stream_t stream, int64_t T, in
     }
     if (reinterpret_cast<uintptr_t>(dY) % 16)
         return fail(REALQ_ERR_INVALID_ARG, "checkpoint_weight_grad: dY must be 16-byte aligned");
-    if (m >= (1ll << 30) || n >= (1ll << 30) || T >= (1ll << 29))
-        return fail(REALQ_ERR_UNSUPPORTED, "checkpoint_weight_grad: m, n below 2^30 and T below 2^29");
+    if (m >= (1ll << 30) || n >= (1ll << 30) || T >= (1ll << 29) || m * n > (1ll << 40))
+        return fail(REALQ_ERR_UNSUPPORTED, "checkpoint_weight_grad: m, n below 2^30, T below 2^29, m n at most 2^40");
     REALQ_TRY(check_ws(ws, ws_bytes, checkpoint_grad_ws_bytes(T, m, n, dy_dtype, num_sms()), "checkpoint_weight_grad"));
     return checkpoint_grad(S(stream), T, m, n, dY, dy_dtype, codes, exps, dW, accumulate, ws, num_sms());
 }

@@ -395,8 +395,11 @@ __global__ void __launch_bounds__(SW * 32, 2)
                 const int64_t i = tile * ROWS + k % ROWS, t = k / ROWS;
                 if (i < m && t < T) {
                     const int z = w_zero ? w_zero[i] : (WB == 8 ? 128 : 8);
-                    // (mod 2^32: the true sum fits, its two parts need not)
-                    const int v = (int)((uint32_t)red[k] - (uint32_t)z * (uint32_t)xred[k / ROWS]);
+                    // The sum about the middle code fits 32 bits (its two parts need not: mod 2^32); the zero
+                    // point's distance from it may take the rest past them.
+                    constexpr int MID = WB == 8 ? 128 : 8;
+                    const int xsum = xred[k / ROWS], about = (int)((uint32_t)red[k] - (uint32_t)MID * (uint32_t)xsum);
+                    const int64_t v = about + (int64_t)(MID - z) * xsum;
                     store1(Y + t * m + i, (float)v * __ldg(x_scale + t) * __ldg(w_scale + i));
                 }
             }

@@ -103,6 +103,40 @@ def test_product_of_the_largest_codes(T, n):
     assert ((Y - ref).abs() <= product_bound(N, ref, n, torch.float32)).all()
 
 
+@pytest.mark.parametrize("T", [1, 8, 16, 40, 100, 200])
+@pytest.mark.parametrize("w_bits", [8, 4])
+@pytest.mark.parametrize("n", [64, 480, 512])
+def test_product_is_exact_below_2_24(T, w_bits, n):
+    """Large codes of one sign with single units among them: the sum is a whole
+    number below 2^24 (512 x 255 x 127) and, with scales of one, the result."""
+    g = gen(n)
+    m = 200
+    xc = torch.randint(228, 256, (T, n), generator=g, device="cuda")
+    xc[torch.rand(T, n, generator=g, device="cuda") < 0.1] = 129      # x = 1
+    hi = 255 if w_bits == 8 else 15
+    w = torch.randint(hi - hi // 8, hi + 1, (m, n), generator=g, device="cuda")
+    w[torch.rand(m, n, generator=g, device="cuda") < 0.1] = 1
+    wc = w.to(torch.uint8) if w_bits == 8 else (w[:, 0::2] | (w[:, 1::2] << 4)).to(torch.uint8).contiguous()
+    one = torch.ones
+    Y = run_product(xc.to(torch.uint8), one(T, device="cuda"), wc, one(m, device="cuda"),
+                    torch.zeros(m, dtype=torch.uint8, device="cuda"), w_bits, torch.float32)
+    assert torch.equal(Y.double(), (xc.double() - 128) @ w.double().T)
+
+
+@pytest.mark.parametrize("T", [1, 16, 20, 70])
+@pytest.mark.parametrize("x,w,z", [(0, 255, 0), (255, 255, 0), (0, 0, 255), (255, 0, 255), (0, 255, 128)])
+def test_product_past_32_bits(T, x, w, z):
+    """The longest sums of one sign: 131071 x 255 x 128 is more than 2^31."""
+    n, m = 131071, 40
+    xc = torch.full((T, n), x, dtype=torch.uint8, device="cuda")
+    wc = torch.full((m, n), w, dtype=torch.uint8, device="cuda")
+    c = (xc, torch.ones(T, device="cuda"), wc, torch.ones(m, device="cuda"),
+         torch.full((m,), z, dtype=torch.uint8, device="cuda"))
+    N, ref = product_exact(*c, 8)
+    Y = run_product(*c, 8, torch.float32).double()
+    assert ((Y - ref).abs() <= product_bound(N, ref, n, torch.float32)).all()
+
+
 @pytest.mark.parametrize("T", [1, 3, 8, 20, 150])
 @pytest.mark.parametrize("bx,bw", [(0, 1), (1, 0), (2, 3), (8, 8), (5, 7)])
 @pytest.mark.parametrize("w_bits", [8, 4])
@@ -166,6 +200,52 @@ def test_operators_on_another_stream():
     s.synchronize()
     assert ((Y.double() - ref).abs() <= ref.abs() * 4 * U + 1e-30).all()
     assert torch.isfinite(lp).all()
+
+
+def test_operators_in_a_captured_graph():
+    """A head step's operators recorded once and replayed on new inputs."""
+    T, d, vocab = 96, 512, 3000
+    W = 0.05 * torch.randn(vocab, d, generator=gen(1), device="cuda")
+    wc, ws = torch.empty(vocab, d, dtype=torch.uint8, device="cuda"), torch.empty(vocab, device="cuda")
+    rq.realq_quantize_activations(W, 8, 1.0, codes=wc, scale=ws)
+    xc, xs = torch.empty(T, d, dtype=torch.uint8, device="cuda"), torch.empty(T, device="cuda")
+    h, y = torch.empty(T, d, device="cuda"), torch.randint(0, vocab, (T,), generator=gen(2), device="cuda")
+    hq = torch.empty_like(h)
+    logits, lp, norm = torch.empty(T, vocab, device="cuda"), torch.empty(T, device="cuda"), torch.empty(T, 2, device="cuda")
+    codes, exps = torch.empty(T, d, dtype=torch.int8, device="cuda"), torch.empty(T, d // 32, dtype=torch.uint8, device="cuda")
+    g, dW = torch.full((T,), -1.0 / T, device="cuda"), torch.empty(vocab, d, device="cuda")
+    b1 = rq.workspace(rq.realq_int8_product_workspace_size(T, d, vocab))
+    b2 = rq.workspace(rq.realq_checkpoint_weight_grad_workspace_size(T, vocab, d, torch.float32))
+
+    def step(s):
+        rq.realq_quantize_activations(h, 8, 1.0, X_q=hq, codes=xc, scale=xs, stream=s)
+        rq.realq_int8_product(xc, xs, wc, ws, logits, ws=b1, stream=s)
+        rq.realq_token_logprobs(logits, y, lp, norm, stream=s)
+        rq.realq_checkpoint_pack(h, codes, exps, stream=s)
+        rq.realq_token_logprobs_grad(logits, y, norm, logits, d_logprob=g, stream=s)
+        rq.realq_checkpoint_weight_grad(logits, codes, exps, dW, ws=b2, stream=s)
+
+    s = torch.cuda.Stream()
+    h.normal_(generator=gen(3))
+    s.wait_stream(torch.cuda.current_stream())
+    step(s)
+    s.synchronize()
+    rq.realq_graph_begin(s)
+    step(s)
+    graph = rq.realq_graph_end(s)
+    for seed in (4, 5):
+        h.normal_(generator=gen(seed))
+        s.wait_stream(torch.cuda.current_stream())
+        step(s)
+        s.synchronize()
+        want = [v.clone() for v in (lp, norm, logits, dW)]
+        for v in (lp, norm, logits, dW):
+            v.fill_(math.nan)
+        s.wait_stream(torch.cuda.current_stream())
+        graph.launch(s)
+        s.synchronize()
+        for v, w in zip((lp, norm, logits, dW), want):
+            assert torch.equal(v, w)
 
 
 # ------------------------------------------------------ log probabilities ---
