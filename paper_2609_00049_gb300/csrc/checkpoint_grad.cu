@@ -22,8 +22,8 @@
 // token-major, i.e. MN-major for the MMA: a TMA box of 64 tokens x 64 channels
 // (128-byte rows, 128-byte swizzle) is one canonical atom stack.  Persistent
 // pairs walk the tiles; the accumulation lies in the drain warps' registers, so
-// storing a tile overlaps the next one's MMAs.  Tokens are split over pairs
-// when the tiles alone do not fill the SMs; the parts are summed in a fixed
+// storing a tile overlaps the next one's MMAs.  Tiles beyond whole rounds over
+// the pairs have their tokens split; a second pass adds the parts in their
 // order.  Every wait is bounded; a tile whose wait gave up is written as NaN
 // and the status word gets ST_TIMEOUT.
 //
@@ -54,30 +54,45 @@ constexpr int STAGE_BYTES = 2 * OP_BYTES;
 constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 1024 + 256;
 constexpr uint32_t IDESC = tc::idesc_bf16_f32(TT, TT, 1, 1);
 constexpr unsigned FULL = 0xFFFFFFFFu;
-constexpr int MAX_SPLITS = 8;
+constexpr int MAX_SPLITS = 16;
 
 struct Work {
-    int64_t m, n, T, tper;     // tokens per part, a multiple of KSTAGE
+    int64_t m, n, T;
     int64_t plane_rows;        // dY's planes lie this many rows apart
     int planes, nti, ntj;      // tiles over X̂'s channels, dY's channels
-    int items;                 // tiles x parts
+    int whole;                 // tiles that keep their token range; the others are split
+    int splits;                // token parts of those
+    int64_t tper;              // tokens per part, a multiple of KSTAGE
+    int items;
 };
 struct Item {
-    int i0, j0, z, nk;         // first channels, part, stages
+    int i0, j0, nk;            // first channels, stages
+    int slot, z;               // split tiles: number among them and part (slot < 0: whole)
     int64_t t0;
 };
-// Parts outermost; within one, groups of 8 tile rows, so that the pairs running
-// together share operands in L2.
-__device__ __forceinline__ Item item_of(const Work &w, int k) {
+// Item k: first the whole tiles, then the parts of the others (all first parts,
+// all second parts, ...).  Tiles go in groups of 8 tile rows, so that the pairs
+// running together share operands in L2.
+__host__ __device__ __forceinline__ Item item_of(const Work &w, int k) {
     constexpr int G = 8;
-    const int tiles = w.nti * w.ntj;
     Item it;
-    it.z = k / tiles;
-    const int t = k - it.z * tiles, g = t / (G * w.ntj), r0 = g * G, rows = min(G, w.nti - r0), u = t - g * G * w.ntj;
+    it.slot = -1;
+    it.z = 0;
+    it.t0 = 0;
+    int64_t tokens = w.T;
+    int t = k;
+    if (k >= w.whole) {
+        const int cut = w.nti * w.ntj - w.whole;
+        it.z = (k - w.whole) / cut;
+        it.slot = k - w.whole - it.z * cut;
+        it.t0 = it.z * w.tper;
+        tokens = w.T - it.t0 < w.tper ? w.T - it.t0 : w.tper;
+        t = w.whole + it.slot;
+    }
+    const int g = t / (G * w.ntj), r0 = g * G, left = w.nti - r0, rows = G < left ? G : left, u = t - g * G * w.ntj;
     it.i0 = (r0 + u % rows) * TT;
     it.j0 = (u / rows) * TT;
-    it.t0 = it.z * w.tper;
-    it.nk = (int)((min(w.T - it.t0, w.tper) + KSTAGE - 1) / KSTAGE) * w.planes;
+    it.nk = (int)((tokens + KSTAGE - 1) / KSTAGE) * w.planes;
     return it;
 }
 
@@ -237,17 +252,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive_cluster(tc::map_rank(tc::smem_u32(&acce[b]), 0));
             }
-            const int64_t col = im.i0 + (int)rank * TC + (warp & 3) * 32 + lane;
-            const int64_t row = im.j0 + (warp >> 2) * 128;
-            if (col < wk.n) {
-                float *o = (part ? part + im.z * wk.m * wk.n : dW) + row * wk.n + col;
-                const bool add = !part && accumulate;
+            const int tc0 = (int)rank * TC + (warp & 3) * 32 + lane, tr0 = (warp >> 2) * 128;   // in the tile
+            if (im.slot >= 0) {   // a part: the whole tile, 256 x 256
+                float *o = part + (((int64_t)im.z * (wk.nti * wk.ntj - wk.whole) + im.slot) * TT + tr0) * TT + tc0;
+#pragma unroll
+                for (int q = 0; q < 128; ++q) o[q * TT] = good ? acc[q] : __int_as_float(0x7fc00000);
+            } else if (im.i0 + tc0 < wk.n) {
+                const int64_t row = im.j0 + tr0;
+                float *o = dW + row * wk.n + im.i0 + tc0;
                 const int rows = (int)min((int64_t)128, wk.m - row);
 #pragma unroll
                 for (int q = 0; q < 128; ++q, o += wk.n)
                     if (q < rows) {
                         const float v = good ? acc[q] : __int_as_float(0x7fc00000);
-                        *o = add ? *o + v : v;
+                        *o = accumulate ? *o + v : v;
                     }
             }
         }
@@ -265,36 +283,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     if (warp == 0) tc::tmem_dealloc_pair(tmem, 2 * TT);
 }
 
-// parts added in their order, four neighbours to a thread
-__global__ void __launch_bounds__(256) weight_grad_reduce(int64_t count, int splits, const float *part, float *dW,
-                                                          int accumulate) {
+// The split tiles: parts added in their order.  A block takes four rows of a
+// tile, a thread four neighbouring columns.
+__global__ void __launch_bounds__(256) weight_grad_reduce(const Work wk, const float *part, float *dW, int accumulate) {
     wait_for_previous();
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (i >= count) return;
-    const int left = (int)min((int64_t)4, count - i);
-    if (left == 4 && count % 4 == 0 && (reinterpret_cast<uintptr_t>(dW) & 15) == 0) {
-        float4 v = __ldg(reinterpret_cast<const float4 *>(part + i));
+    const int slot = blockIdx.x, cut = wk.nti * wk.ntj - wk.whole;
+    const Item im = item_of(wk, wk.whole + slot);
+    const int r = blockIdx.y * 4 + (threadIdx.x >> 6), c = (threadIdx.x & 63) * 4;
+    const int64_t row = im.j0 + r, col = im.i0 + c;
+    if (row >= wk.m || col >= wk.n) return;
+    const float4 *p = reinterpret_cast<const float4 *>(part + ((int64_t)slot * TT + r) * TT + c);
+    const int64_t step = (int64_t)cut * TT * TT / 4;
+    float4 v = __ldg(p);
 #pragma unroll 4
-        for (int z = 1; z < splits; ++z) {
-            const float4 p = __ldg(reinterpret_cast<const float4 *>(part + z * count + i));
-            v.x += p.x;
-            v.y += p.y;
-            v.z += p.z;
-            v.w += p.w;
-        }
-        float4 *o = reinterpret_cast<float4 *>(dW + i);
-        if (accumulate) {
-            const float4 d = *o;
-            v = make_float4(d.x + v.x, d.y + v.y, d.z + v.z, d.w + v.w);
-        }
-        *o = v;
-        return;
+    for (int z = 1; z < wk.splits; ++z) {
+        const float4 b = __ldg(p + z * step);
+        v.x += b.x;
+        v.y += b.y;
+        v.z += b.z;
+        v.w += b.w;
     }
-    for (int k = 0; k < left; ++k) {
-        float v = part[i + k];
-        for (int z = 1; z < splits; ++z) v += part[z * count + i + k];
-        dW[i + k] = accumulate ? dW[i + k] + v : v;
-    }
+    const float a[4] = {v.x, v.y, v.z, v.w};
+    float *o = dW + row * wk.n + col;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (col + k < wk.n) o[k] = accumulate ? o[k] + a[k] : a[k];
 }
 
 // 2^(b - 133), subnormal below b = 7; NaN for b = 255
@@ -410,13 +423,36 @@ __global__ void __launch_bounds__(256) grad_planes_kernel(const Planes p) {
 
 int64_t pad8(int64_t x) { return (x + 7) / 8 * 8; }
 
-// Token ranges: with fewer tiles than pairs of SMs, as many as fill them without
-// leaving a range under eight stages (dY's planes counted).
-int grad_splits(int64_t T, int64_t m, int64_t n, int planes, int sms) {
-    const int64_t tiles = (int64_t)ceil_div(m, TT) * ceil_div(n, TT);
-    int64_t s = sms / 2 / tiles;
-    s = std::min<int64_t>(s, T * planes / (8 * KSTAGE));
-    return (int)std::max<int64_t>(1, std::min<int64_t>(s, MAX_SPLITS));
+// Tiles that fill whole rounds over the pairs of SMs keep their token range; the
+// rest is cut into the count of parts that is estimated the fastest, in cycles: a
+// stage takes 512 (the MMAs), a tile's start and end 3000, the pass over the
+// parts 5000 and the parts' bytes 3400 to a cycle, twice; a part keeps at least
+// four stages.
+Work work_of(int64_t T, int64_t m, int64_t n, int planes, int sms) {
+    Work w{};
+    w.m = m;
+    w.n = n;
+    w.T = T;
+    w.plane_rows = T;
+    w.planes = planes;
+    w.nti = ceil_div(n, TT);
+    w.ntj = ceil_div(m, TT);
+    const int64_t pairs = sms / 2, tiles = (int64_t)w.nti * w.ntj, rest = tiles % pairs, ks = (T + KSTAGE - 1) / KSTAGE;
+    int best = 1;
+    int64_t cost = INT64_MAX;
+    for (int s = 1; s <= MAX_SPLITS && (s == 1 || ks * planes / s >= 4) && s <= ks && rest > 0; ++s) {
+        const int64_t c = (rest * s + pairs - 1) / pairs * ((ks + s - 1) / s * planes * 512 + 3000) +
+                          (s > 1 ? 5000 + 2 * rest * s * TT * TT * 4 / 3400 : 0);
+        if (c < cost) {
+            cost = c;
+            best = s;
+        }
+    }
+    w.tper = (ks + best - 1) / best * KSTAGE;
+    w.splits = (int)((T + w.tper - 1) / w.tper);
+    w.whole = (int)(w.splits > 1 ? tiles - rest : tiles);
+    w.items = (int)(w.whole + (tiles - w.whole) * w.splits);
+    return w;
 }
 
 struct GradWs {
@@ -424,12 +460,12 @@ struct GradWs {
     __nv_bfloat16 *x, *dy;
     float *part;
     size_t bytes;
-    GradWs(void *ws, int64_t T, int64_t m, int64_t n, realq_dtype_t dt, int splits) {
+    GradWs(void *ws, const Work &w, realq_dtype_t dt) {
         Carve c(ws);
         status = c.take<int>(64);
-        x = c.take<__nv_bfloat16>((size_t)(T * pad8(n)));
-        dy = c.take<__nv_bfloat16>((size_t)(T * pad8(m)) * (dt == REALQ_F32 ? 3 : (m % 8 ? 1 : 0)));
-        part = c.take<float>(splits > 1 ? (size_t)splits * m * n : 0);
+        x = c.take<__nv_bfloat16>((size_t)(w.T * pad8(w.n)));
+        dy = c.take<__nv_bfloat16>((size_t)(w.T * pad8(w.m)) * (dt == REALQ_F32 ? 3 : (w.m % 8 ? 1 : 0)));
+        part = c.take<float>((size_t)(w.items - w.whole) * TT * TT);
         bytes = c.off;
     }
 };
@@ -437,15 +473,15 @@ struct GradWs {
 }  // namespace
 
 size_t checkpoint_grad_ws_bytes(int64_t T, int64_t m, int64_t n, realq_dtype_t dt, int sms) {
-    return GradWs(nullptr, T, m, n, dt, grad_splits(T, m, n, dt == REALQ_F32 ? 3 : 1, sms)).bytes;
+    return GradWs(nullptr, work_of(T, m, n, dt == REALQ_F32 ? 3 : 1, sms), dt).bytes;
 }
 
 realq_status_t checkpoint_grad(cudaStream_t s, int64_t T, int64_t m, int64_t n, const void *dY, realq_dtype_t dt,
                                const int8_t *codes, const uint8_t *exps, float *dW, int accumulate, void *ws, int sms) {
-    int splits = grad_splits(T, m, n, dt == REALQ_F32 ? 3 : 1, sms);
-    const GradWs w(ws, T, m, n, dt, splits);
-    const bool direct = dt == REALQ_BF16 && m % 8 == 0;   // dY read where it lies
     const int planes = dt == REALQ_F32 ? 3 : 1;
+    const Work wk = work_of(T, m, n, planes, sms);
+    const GradWs w(ws, wk, dt);
+    const bool direct = dt == REALQ_BF16 && m % 8 == 0;   // dY read where it lies
     const int64_t ldx = pad8(n), ldy = pad8(m);
     const bool xv = n % 32 == 0 && (reinterpret_cast<uintptr_t>(codes) & 15) == 0, yv = dt == REALQ_F32 && m % 8 == 0;
     Planes p{T, n, m, ldx, ldy, (unsigned)((T * ((n + 15) / 16) + 255) / 256), codes, exps, w.x, dY,
@@ -470,31 +506,18 @@ realq_status_t checkpoint_grad(cudaStream_t s, int64_t T, int64_t m, int64_t n, 
     if (cr == CUDA_SUCCESS)
         cr = encode_tmap_2d_bf16(&mapX, w.x, (uint64_t)n, (uint64_t)T, (uint64_t)ldx * 2, 64, KSTAGE, 1);
     if (cr != CUDA_SUCCESS) return fail(REALQ_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)cr);
-    int64_t tper = (T + splits - 1) / splits;
-    tper = (tper + KSTAGE - 1) / KSTAGE * KSTAGE;
-    splits = (int)((T + tper - 1) / tper);
     REALQ_TRY(set_smem_limit(reinterpret_cast<const void *>(weight_grad_kernel), SMEM_BYTES));
-    Work wk{};
-    wk.m = m;
-    wk.n = n;
-    wk.T = T;
-    wk.tper = tper;
-    wk.plane_rows = T;
-    wk.planes = planes;
-    wk.nti = ceil_div(n, TT);
-    wk.ntj = ceil_div(m, TT);
-    wk.items = wk.nti * wk.ntj * splits;
     {
         Launch L("checkpoint_weight_grad", s);
         REALQ_CUDA_TRY(launch_overlapped(weight_grad_kernel, dim3((unsigned)(2 * std::min(wk.items, sms / 2))),
-                                         dim3(THREADS), SMEM_BYTES, s, mapX, mapY, wk, dW, accumulate,
-                                         splits > 1 ? w.part : nullptr, w.status));
+                                         dim3(THREADS), SMEM_BYTES, s, mapX, mapY, wk, dW, accumulate, w.part,
+                                         w.status));
     }
     REALQ_TRY(check_launch("checkpoint_weight_grad"));
-    if (splits > 1) {
+    if (wk.splits > 1) {
         Launch L("checkpoint_grad_reduce", s);
-        REALQ_CUDA_TRY(launch_overlapped(weight_grad_reduce, dim3((unsigned)((m * n + 1023) / 1024)), dim3(256), 0, s,
-                                         m * n, splits, (const float *)w.part, dW, accumulate));
+        REALQ_CUDA_TRY(launch_overlapped(weight_grad_reduce, dim3((unsigned)(wk.nti * wk.ntj - wk.whole), TT / 4),
+                                         dim3(256), 0, s, wk, (const float *)w.part, dW, accumulate));
         REALQ_TRY(check_launch("checkpoint_grad_reduce"));
     }
     return REALQ_OK;
