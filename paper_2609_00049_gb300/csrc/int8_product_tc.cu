@@ -466,42 +466,54 @@ int64_t pad8(int64_t x) { return (x + 7) / 8 * 8; }
 int64_t pad16(int64_t x) { return (x + 15) / 16 * 16; }
 int64_t row_bytes(int64_t n, int w_bits) { return w_bits == 8 ? n : (n + 1) / 2; }
 
-// Tokens per tile: as few tiles as 256 allows, evenly filled.  Tiles that fill
-// whole waves over the SMs keep their K range; the rest is cut into the count of
-// parts that is estimated the fastest, in cycles: a K step takes 2 N (the MMAs)
-// but at least 360 (its codes from HBM), a tile's start and drain 1500, the
-// pass over the parts 5000 and the parts' bytes 3400 to a cycle, twice.
+// The shape estimated the fastest, in cycles.  Token tiles: from as few as 256
+// tokens allow to four times that (smaller tiles use tensor cores less well, but
+// fill more SMs), evenly filled.  Tiles that fill whole waves over the SMs keep
+// their K range; the rest is cut into parts of at least four steps.  For 64 of K
+// a tile of more than 128 tokens takes 560 cycles (2 N of MMA and the rest of a
+// round), a smaller one 440 (its conversions and waits); a tile's start and
+// drain 2500, the pass over the parts 5000 and the parts' bytes 3400 to a cycle,
+// twice.
 Shape shape_of(int64_t T, int64_t n, int64_t m, int w_bits, int sms) {
-    Shape sh{};
-    sh.T = T;
-    sh.n = n;
-    sh.m = m;
-    sh.ntj = (int)((T + TNMAX - 1) / TNMAX);
-    sh.N = (int)std::max<int64_t>(16, ((T + sh.ntj - 1) / sh.ntj + 15) / 16 * 16);
-    sh.ntj = (int)((T + sh.N - 1) / sh.N);
-    sh.nti = ceil_div(m, TM);
-    sh.kstep = sh.N <= 128 ? 128 : 64;
-    const int KS = sh.kstep, xb = sh.N * KS * 2, wb = TM * (w_bits == 8 ? KS : KS / 2);
-    sh.stages = std::min(MAX_STAGES * 64 / KS, RING_BYTES / (xb + wb));
-    sh.wstages = std::min(MAX_WSTAGES, (RING_BYTES - sh.stages * xb) / wb);
-    sh.ks = ceil_div(n, KS);
-    const int64_t tiles = (int64_t)sh.nti * sh.ntj, rest = tiles % sms;
-    int best = 1;
-    int64_t cost = INT64_MAX;
-    for (int s = 1; s <= MAX_SPLITS && (s == 1 || sh.ks / s >= 4) && rest > 0; ++s) {
-        const int64_t step = std::max(2 * sh.N, 360) * KS / 64;
-        const int64_t c = (rest * s + sms - 1) / sms * ((sh.ks + s - 1) / s * step + 1500) +
-                          (s > 1 ? 5000 + 2 * rest * s * sh.N * TM * 4 / 3400 : 0);
-        if (c < cost) {
-            cost = c;
-            best = s;
+    Shape best{};
+    int64_t best_cost = INT64_MAX;
+    const int64_t fewest = (T + TNMAX - 1) / TNMAX, stride = std::max<int64_t>(1, fewest / 2);
+    for (int64_t ntj = fewest; ntj <= 4 * fewest; ntj += stride) {
+        Shape sh{};
+        sh.T = T;
+        sh.n = n;
+        sh.m = m;
+        sh.N = (int)std::max<int64_t>(16, ((T + ntj - 1) / ntj + 15) / 16 * 16);
+        sh.ntj = (int)((T + sh.N - 1) / sh.N);
+        sh.nti = ceil_div(m, TM);
+        sh.kstep = sh.N <= 128 ? 128 : 64;
+        const int KS = sh.kstep, xb = sh.N * KS * 2, wb = TM * (w_bits == 8 ? KS : KS / 2);
+        sh.stages = std::min(MAX_STAGES * 64 / KS, RING_BYTES / (xb + wb));
+        sh.wstages = std::min(MAX_WSTAGES, (RING_BYTES - sh.stages * xb) / wb);
+        sh.ks = ceil_div(n, KS);
+        const int64_t tiles = (int64_t)sh.nti * sh.ntj, rest = tiles % sms, step = sh.N <= 128 ? 880 : 560;
+        int parts = 1;
+        int64_t cost = rest > 0 ? INT64_MAX : 0;
+        for (int s = 1; s <= MAX_SPLITS && (s == 1 || sh.ks * KS / 64 / s >= 4) && s <= sh.ks && rest > 0 && (s == 1 || rest * s <= 2 * sms); ++s) {
+            const int64_t c = (rest * s + sms - 1) / sms * ((sh.ks + s - 1) / s * step + 2500) +
+                              (s > 1 ? 5000 + 2 * rest * s * sh.N * TM * 4 / 3400 : 0);
+            if (c < cost) {
+                cost = c;
+                parts = s;
+            }
         }
+        cost += tiles / sms * (sh.ks * step + 2500);
+        sh.per = (sh.ks + parts - 1) / parts;
+        sh.splits = (sh.ks + sh.per - 1) / sh.per;
+        sh.whole = (int)(sh.splits > 1 ? tiles - rest : tiles);
+        sh.items = (int)(sh.whole + (tiles - sh.whole) * sh.splits);
+        if (cost < best_cost) {
+            best_cost = cost;
+            best = sh;
+        }
+        if (tiles >= 4 * sms) break;   // (finer tiles would change little)
     }
-    sh.per = (sh.ks + best - 1) / best;
-    sh.splits = (sh.ks + sh.per - 1) / sh.per;
-    sh.whole = (int)(sh.splits > 1 ? tiles - rest : tiles);
-    sh.items = (int)(sh.whole + (tiles - sh.whole) * sh.splits);
-    return sh;
+    return best;
 }
 
 struct ProductWs {
