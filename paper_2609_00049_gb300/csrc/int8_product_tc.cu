@@ -20,10 +20,10 @@
 // Roles (608 threads, one persistent CTA per SM): warps 0-7 convert, warps
 // 8-15 drain the accumulator (lane = channel, so a warp's stores of one token
 // are contiguous; two warps take turns at a lane quarter's 32-column blocks),
-// warps 16 and 17 issue the TMA loads of tokens and codes, warp 18 the MMAs.  TMEM: columns 0-255
-// hold the accumulator (two of them when a tile has at most 128 tokens, so that
-// a drain overlaps the next tile), 256-511 eight A slots of 64
-// K (four of 128).  The codes have a ring
+// warps 16 and 17 issue the TMA loads of tokens and codes, warp 18 the MMAs.  TMEM: an
+// accumulator of up to 256 columns and eight A slots of 64 K, or two of up to
+// 192 (a drain then overlaps the next tile) and four, or two of up to 128 and
+// four of 128 K.  The codes have a ring
 // of their own, freed by the converters, and run ahead of the tokens, whose
 // stages (and the A slots) the MMAs free: a stage of either then covers one
 // memory latency, not the conversion as well.  Tiles beyond whole
@@ -63,6 +63,7 @@ struct Shape {
     int64_t T, n, m;
     int N;            // tokens per tile, a multiple of 16
     int kstep;        // K per stage
+    int acc, a0;      // TMEM: columns between the two accumulators (0: there is one), first column of the A slots
     int stages, wstages;   // ring lengths: tokens and A slots, codes
     int nti, ntj;     // tiles over channels, tokens
     int whole;        // tiles that keep their K range; the others are split
@@ -147,7 +148,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int x_bytes = sh.N * KS * 2;           // a multiple of 1024, as W_BYTES; KS / 64 boxes
     const int items = sh.items, S = sh.stages, SW = sh.wstages;
     uint8_t *wring = smem + S * x_bytes;
-    const bool two = sh.N <= 128;                // two accumulators
+    const bool two = sh.acc > 0;                 // two accumulators
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
@@ -179,7 +180,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     if (warp < CONV_WARPS) {
         // ---------------- converters: codes -> fp16 in TMEM ----------------
         const int group = warp >> 2, row = (warp & 3) * 32 + lane;
-        const uint32_t a_base = tmem + 256u + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t a_base = tmem + (uint32_t)sh.a0 + ((uint32_t)((warp & 3) * 32) << 16);
         Ring r(S), rw(SW);   // over all of this CTA's items
         bool ok = true;
         int turn = 0;
@@ -269,7 +270,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 }
             }
             tc::fence_after_sync();
-            const uint32_t src = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * 128);
+            const uint32_t src = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(b * sh.acc);
             const int blocks = (sh.N + 31) / 32, mine_last = (blocks - 1 - half) / 2;   // blocks 2 j + half, j <= mine_last
             if (good && blocks <= half) {
                 tc::fence_before_sync();
@@ -355,7 +356,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             ok = __all_sync(FULL, tc::mbar_wait(tc::smem_u32(&acce[b]), ((uint32_t)round & 1u) ^ 1u, abort_flag));
             if (!ok) break;
             tc::fence_after_sync();
-            const uint32_t d = tmem + (uint32_t)(b * 128);
+            const uint32_t d = tmem + (uint32_t)(b * sh.acc);
             for (int kk = 0; kk < im.nk; ++kk, r.next()) {
                 ok = tc::mbar_wait(tc::smem_u32(&ready[r.s]), r.phase, abort_flag) &&
                      tc::mbar_wait(tc::smem_u32(&xfull[r.s]), r.phase, abort_flag);
@@ -363,7 +364,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 if (!ok) break;
                 tc::fence_after_sync();
                 const uint64_t desc = desc0 + (uint32_t)(r.s * x_bytes >> 4);
-                const uint32_t a = tmem + 256u + (uint32_t)(r.s * (KS / 2));
+                const uint32_t a = tmem + (uint32_t)(sh.a0 + r.s * (KS / 2));
                 if (tc::elect_one()) {
 #pragma unroll
                     for (int k = 0; k < KS / 16; ++k)
@@ -466,53 +467,63 @@ int64_t pad8(int64_t x) { return (x + 7) / 8 * 8; }
 int64_t pad16(int64_t x) { return (x + 15) / 16 * 16; }
 int64_t row_bytes(int64_t n, int w_bits) { return w_bits == 8 ? n : (n + 1) / 2; }
 
-// The shape estimated the fastest, in cycles.  Token tiles: from as few as 256
-// tokens allow to four times that (smaller tiles use tensor cores less well, but
-// fill more SMs), evenly filled.  Tiles that fill whole waves over the SMs keep
-// their K range; the rest is cut into parts of at least four steps.  For 64 of K
-// a tile of more than 128 tokens takes 560 cycles (2 N of MMA and the rest of a
-// round), a smaller one 440 (its conversions and waits); a tile's start and
-// drain 2500, the pass over the parts 5000 and the parts' bytes 3400 to a cycle,
-// twice.
-Shape shape_of(int64_t T, int64_t n, int64_t m, int w_bits, int sms) {
-    Shape best{};
-    int64_t best_cost = INT64_MAX;
-    const int64_t fewest = (T + TNMAX - 1) / TNMAX, stride = std::max<int64_t>(1, fewest / 2);
-    for (int64_t ntj = fewest; ntj <= 4 * fewest; ntj += stride) {
-        Shape sh{};
-        sh.T = T;
-        sh.n = n;
-        sh.m = m;
-        sh.N = (int)std::max<int64_t>(16, ((T + ntj - 1) / ntj + 15) / 16 * 16);
-        sh.ntj = (int)((T + sh.N - 1) / sh.N);
-        sh.nti = ceil_div(m, TM);
-        sh.kstep = sh.N <= 128 ? 128 : 64;
-        const int KS = sh.kstep, xb = sh.N * KS * 2, wb = TM * (w_bits == 8 ? KS : KS / 2);
-        sh.stages = std::min(MAX_STAGES * 64 / KS, RING_BYTES / (xb + wb));
-        sh.wstages = std::min(MAX_WSTAGES, (RING_BYTES - sh.stages * xb) / wb);
-        sh.ks = ceil_div(n, KS);
-        const int64_t tiles = (int64_t)sh.nti * sh.ntj, rest = tiles % sms, step = sh.N <= 128 ? 880 : 560;
-        int parts = 1;
-        int64_t cost = rest > 0 ? INT64_MAX : 0;
-        for (int s = 1; s <= MAX_SPLITS && (s == 1 || sh.ks * KS / 64 / s >= 4) && s <= sh.ks && rest > 0 && (s == 1 || rest * s <= 2 * sms); ++s) {
-            const int64_t c = (rest * s + sms - 1) / sms * ((sh.ks + s - 1) / s * step + 2500) +
-                              (s > 1 ? 5000 + 2 * rest * s * sh.N * TM * 4 / 3400 : 0);
-            if (c < cost) {
-                cost = c;
-                parts = s;
-            }
+// One choice of token tiles: ntj of them, evenly filled, and its estimate in
+// cycles.  Tiles that fill whole waves over the SMs keep their K range; the rest
+// is cut into parts of at least four steps.  For 64 of K a tile of up to 128
+// tokens takes 440 cycles (its conversions and waits), a larger one 2 N and 60,
+// at least 520; its start and drain take 3500, or 800 where a second accumulator
+// lets them overlap the next tile; the pass over the parts 5000 and the parts'
+// bytes 3400 to a cycle, twice.
+int64_t shape_for(Shape &sh, int64_t T, int64_t n, int64_t m, int64_t ntj, int w_bits, int sms) {
+    sh.T = T;
+    sh.n = n;
+    sh.m = m;
+    sh.N = (int)std::max<int64_t>(16, ((T + ntj - 1) / ntj + 15) / 16 * 16);
+    sh.ntj = (int)((T + sh.N - 1) / sh.N);
+    sh.nti = ceil_div(m, TM);
+    sh.kstep = sh.N <= 128 ? 128 : 64;
+    sh.acc = sh.N <= 128 ? 128 : (sh.N <= 192 ? 192 : 0);
+    sh.a0 = sh.acc == 192 ? 384 : 256;
+    const int KS = sh.kstep, xb = sh.N * KS * 2, wb = TM * (w_bits == 8 ? KS : KS / 2);
+    sh.stages = std::min((512 - sh.a0) / (KS / 2), RING_BYTES / (xb + wb));
+    sh.wstages = std::min(MAX_WSTAGES, (RING_BYTES - sh.stages * xb) / wb);
+    sh.ks = ceil_div(n, KS);
+    const int64_t tiles = (int64_t)sh.nti * sh.ntj, rest = tiles % sms;
+    const int64_t step = sh.N <= 128 ? 880 : std::max(520, 2 * sh.N + 60), ends = sh.acc ? 800 : 3500;
+    int parts = 1;
+    int64_t cost = rest > 0 ? INT64_MAX : 0;
+    for (int s = 1; s <= MAX_SPLITS && (s == 1 || sh.ks * KS / 64 / s >= 4) && s <= sh.ks && rest > 0 &&
+                    (s == 1 || rest * s <= 2 * sms); ++s) {
+        const int64_t c = (rest * s + sms - 1) / sms * ((sh.ks + s - 1) / s * step + ends) +
+                          (s > 1 ? 5000 + 2 * rest * s * sh.N * TM * 4 / 3400 : 0);
+        if (c < cost) {
+            cost = c;
+            parts = s;
         }
-        cost += tiles / sms * (sh.ks * step + 2500);
-        sh.per = (sh.ks + parts - 1) / parts;
-        sh.splits = (sh.ks + sh.per - 1) / sh.per;
-        sh.whole = (int)(sh.splits > 1 ? tiles - rest : tiles);
-        sh.items = (int)(sh.whole + (tiles - sh.whole) * sh.splits);
+    }
+    sh.per = (sh.ks + parts - 1) / parts;
+    sh.splits = (sh.ks + sh.per - 1) / sh.per;
+    sh.whole = (int)(sh.splits > 1 ? tiles - rest : tiles);
+    sh.items = (int)(sh.whole + (tiles - sh.whole) * sh.splits);
+    return cost + tiles / sms * (sh.ks * step + ends);
+}
+
+// The fastest of: tiles of up to 256 tokens, of up to 192 (two accumulators), and
+// smaller ones where that leaves SMs idle.
+Shape shape_of(int64_t T, int64_t n, int64_t m, int w_bits, int sms) {
+    const int64_t fewest = (T + TNMAX - 1) / TNMAX, stride = std::max<int64_t>(1, fewest / 2);
+    Shape best{}, sh{};
+    int64_t best_cost = shape_for(best, T, n, m, fewest, w_bits, sms);
+    auto offer = [&](int64_t ntj) {
+        const int64_t cost = shape_for(sh, T, n, m, ntj, w_bits, sms);
         if (cost < best_cost) {
             best_cost = cost;
             best = sh;
         }
-        if (tiles >= 4 * sms) break;   // (finer tiles would change little)
-    }
+    };
+    offer((T + 191) / 192);
+    if ((int64_t)best.nti * fewest < 4 * sms)
+        for (int64_t ntj = fewest + stride; ntj <= 4 * fewest; ntj += stride) offer(ntj);
     return best;
 }
 
