@@ -59,39 +59,6 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Weight codes are read once: they pass L1 by, which keeps the tokens.
-__device__ __forceinline__ uint4 load_weight(const uint8_t *p) {
-    uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                 : "l"(p));
-    return v;
-}
-// An aligned piece, of which some bytes may lie outside the codes (and read 0).
-__device__ __forceinline__ uint4 load_piece(const uint8_t *p, const uint8_t *lo, const uint8_t *hi) {
-    if (p >= lo && p + 16 <= hi) return load_weight(p);
-    uint32_t v[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-        if (p + i >= lo && p + i < hi) v[i >> 2] |= (uint32_t)__ldg(p + i) << (8 * (i & 3));
-    return make_uint4(v[0], v[1], v[2], v[3]);
-}
-__device__ __forceinline__ uint4 shfl4(const uint4 &v, int src) {
-    return make_uint4(__shfl_sync(0xFFFFFFFFu, v.x, src), __shfl_sync(0xFFFFFFFFu, v.y, src),
-                      __shfl_sync(0xFFFFFFFFu, v.z, src), __shfl_sync(0xFFFFFFFFu, v.w, src));
-}
-// 16 bytes from byte `mis` of the 32 in a, b on
-__device__ __forceinline__ uint4 realign(const uint4 &a, const uint4 &b, uint32_t mis) {
-    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    uint32_t u[6], t[5];
-#pragma unroll
-    for (int i = 0; i < 6; ++i) u[i] = mis & 8 ? w[i + 2] : w[i];
-#pragma unroll
-    for (int i = 0; i < 5; ++i) t[i] = mis & 4 ? u[i + 1] : u[i];
-    const uint32_t s = 8 * (mis & 3);
-    return make_uint4(__funnelshift_r(t[0], t[1], s), __funnelshift_r(t[1], t[2], s), __funnelshift_r(t[2], t[3], s),
-                      __funnelshift_r(t[3], t[4], s));
-}
 // the first `count` bytes of w, the others the code of zero
 __device__ __forceinline__ uint32_t first_bytes(uint32_t w, int count) {
     const uint32_t keep = count >= 4 ? ~0u : (count <= 0 ? 0u : (1u << 8 * count) - 1u);
