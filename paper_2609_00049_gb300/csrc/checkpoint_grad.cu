@@ -27,9 +27,9 @@
 // order.  Every wait is bounded; a tile whose wait gave up is written as NaN
 // and the status word gets ST_TIMEOUT.
 //
-// Measured, 8192 tokens x 8192 x 8192 with bf16 dY: 608 us (1.81 PFLOP/s; the
-// tensor pipe 80 % active at 4096 x 4864 x 8192) and 36 us for X̂'s plane, which
-// HBM bounds; one CTA per tile took 1.09 ms.  With few tokens the stores of dW
+// Measured, 8192 tokens x 8192 x 8192 with bf16 dY: 594 us (1.85 PFLOP/s; the
+// tensor pipe 80 % active at 4096 x 4864 x 8192), 36 us for X̂'s plane, which
+// HBM bounds, and 8 for the parts; one CTA per tile took 1.09 ms.  With few tokens the stores of dW
 // bound it (21 x 7936 x 28416: 170 us for 902 MB; 280 us where an odd n puts
 // rows off the 32-byte sectors).
 #include "bytes.cuh"

@@ -418,8 +418,10 @@ realq_status_t stream_launch(cudaStream_t s, int64_t T, int64_t n, int64_t m, co
 template <bool ALIGNED, int WB, typename TY>
 realq_status_t stream_tokens(cudaStream_t s, int64_t T, int64_t n, int64_t m, const uint8_t *X, const float *xs,
                              const uint8_t *W, const float *ws, const uint8_t *wz, TY *Y, int *status, int sms) {
-    // 32 channels to a warp halve the work on the tokens' codes, where there are enough of them
-    const bool wide = m >= (int64_t)sms * 32;
+    // 32 channels to a warp halve the work on the tokens' codes, where there are enough of them; unaligned tokens are
+    // more work, so there a quarter of that is enough where rows are long (1 x 15767 x 3927: 26 us against 33)
+    const int64_t rb = WB == 8 ? n : (n + 1) / 2;
+    const bool wide = m >= (int64_t)sms * 32 || (!ALIGNED && m >= (int64_t)sms * 8 && rb >= 4096);
     if (T <= 8)
         return wide ? stream_launch<ALIGNED, WB, 1, 2, TY>(s, T, n, m, X, xs, W, ws, wz, Y, status, sms)
                     : stream_launch<ALIGNED, WB, 1, 1, TY>(s, T, n, m, X, xs, W, ws, wz, Y, status, sms);
