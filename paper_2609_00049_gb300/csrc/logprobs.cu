@@ -45,8 +45,6 @@ namespace {
 constexpr unsigned FULL = 0xFFFFFFFFu;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
-constexpr int NT = 256;       // threads of a forward CTA
-constexpr int PER_WARP = 1024 / NT;   // thread maxima that each warp gives for tau (32 in all)
 constexpr int U = 4;          // 16-byte loads in flight per thread
 constexpr int NOTES = 32;     // run maxima kept per thread
 constexpr int CAP = 1024;     // collected candidates
@@ -215,7 +213,7 @@ __device__ __forceinline__ int key_index(uint64_t k) { return INT32_MAX - (int)(
 
 __device__ __forceinline__ bool before(float va, int ia, float vb, int ib) { return va > vb || (va == vb && ia < ib); }
 
-struct FwdSmem {
+template <int NT> struct FwdSmem {   // NT: threads of a forward CTA
     float note[NOTES][NT];
     uint64_t cand[CAP];
     uint64_t top[KMAX];       // keys, 0 where there is none
@@ -234,12 +232,13 @@ __device__ __forceinline__ int place_of(const uint64_t *keys, int n, uint64_t ke
     return above;
 }
 
-template <typename TX>
+template <typename TX, int NT>
 __global__ void __launch_bounds__(NT, 1024 / NT)
     logprobs_kernel(int V, int64_t ld, const TX *X, const int64_t *targets, float *logprob, float *norm,
                     float *entropy, int k, int64_t *top_ids, float *top_lp) {
     constexpr int E = Vec<TX>::E;
-    __shared__ FwdSmem sm;
+    constexpr int PER_WARP = 1024 / NT;   // thread maxima that each warp gives for tau (32 in all)
+    __shared__ FwdSmem<NT> sm;
     cg::cluster_group cluster = cg::this_cluster();
     const int CL = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int64_t r = blockIdx.x / CL;
@@ -566,11 +565,17 @@ __global__ void __launch_bounds__(BT)
     }
 }
 
-template <typename TX>
-realq_status_t fwd_launch(cudaStream_t s, int64_t T, int64_t V, int64_t ld, const void *X, const int64_t *targets,
+// More rows than CTAs of 256 threads fit, and short ones: CTAs of 128, so that
+// twice as many rows are under way (3469 x 4236 in fp32: 18 against 24 us; 4000 x
+// 32000 in bf16: 65 against 70; longer rows are slower so: 2250 x 16774 in fp32
+// 39 against 35).
+constexpr int64_t SMALL_ROW = 65536;   // bytes
+
+template <typename TX, int NT>
+realq_status_t fwd_launch_nt(cudaStream_t s, int64_t T, int64_t V, int64_t ld, const void *X, const int64_t *targets,
                           float *logprob, float *norm, float *entropy, int k, int64_t *top_ids, float *top_lp,
                           int sms) {
-    // Four CTAs fit an SM.  A row gets as many CTAs (a power of two up to 8) as
+    // 1024 threads fit an SM.  A row gets as many CTAs (a power of two up to 8) as
     // leave no second wave; each should still have a full pass of vectors.
     int cl = 1;
     while (cl < MAX_CLUSTER && T * cl * 2 <= 1024 / NT * (int64_t)sms && V / (2 * cl) >= (int64_t)NT * Vec<TX>::E) cl *= 2;
@@ -586,10 +591,19 @@ realq_status_t fwd_launch(cudaStream_t s, int64_t T, int64_t V, int64_t ld, cons
     cfg.numAttrs = cl > 1 ? 1 : 0;
     {
         Launch L("token_logprobs", s);
-        REALQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, logprobs_kernel<TX>, (int)V, ld, static_cast<const TX *>(X), targets,
+        REALQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, logprobs_kernel<TX, NT>, (int)V, ld, static_cast<const TX *>(X), targets,
                                           logprob, norm, entropy, k, top_ids, top_lp));
     }
     return check_launch("token_logprobs");
+}
+
+template <typename TX>
+realq_status_t fwd_launch(cudaStream_t s, int64_t T, int64_t V, int64_t ld, const void *X, const int64_t *targets,
+                          float *logprob, float *norm, float *entropy, int k, int64_t *top_ids, float *top_lp,
+                          int sms) {
+    if (T > 4 * sms && V * (int64_t)sizeof(TX) <= SMALL_ROW)
+        return fwd_launch_nt<TX, 128>(s, T, V, ld, X, targets, logprob, norm, entropy, k, top_ids, top_lp, sms);
+    return fwd_launch_nt<TX, 256>(s, T, V, ld, X, targets, logprob, norm, entropy, k, top_ids, top_lp, sms);
 }
 
 template <typename TX>

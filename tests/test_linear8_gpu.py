@@ -337,6 +337,15 @@ def test_logprobs_match_the_definition(T, V, dtype, masked):
         check_forward(forward(x, y, k), forward_exact(x, y, k), V, k)
 
 
+@pytest.mark.parametrize("T,V", [(700, 8), (700, 1001), (1300, 4099), (900, 16384), (650, 32768)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("masked", ["", "few", "ties"])
+def test_logprobs_of_many_short_rows(T, V, dtype, masked):
+    x, y = logits_case(T, V, dtype, masked, seed=V)
+    for k in (0, 7, 32):
+        check_forward(forward(x, y, k), forward_exact(x, y, k), V, k)
+
+
 def test_logprobs_of_a_vocabulary_past_the_notes():
     """Rows so long that a thread's run maxima are merged."""
     x, y = logits_case(2, 1_500_003, torch.float32, "")
