@@ -48,6 +48,7 @@ constexpr float LN2 = 0.6931471805599453f;
 constexpr int U = 4;          // 16-byte loads in flight per thread
 constexpr int NOTES = 32;     // run maxima kept per thread
 constexpr int CAP = 1024;     // collected candidates
+constexpr int RUNS = 256;     // runs that are read again
 constexpr int KMAX = 32;
 constexpr int MAX_CLUSTER = 8;
 
@@ -217,6 +218,10 @@ template <int NT> struct FwdSmem {   // NT: threads of a forward CTA
     float note[NOTES][NT];
     uint64_t cand[CAP];
     uint64_t top[KMAX];       // keys, 0 where there is none
+    uint64_t cluster_top[MAX_CLUSTER * KMAX];   // on the cluster's first CTA: every CTA's
+    Stat cluster_total[MAX_CLUSTER];
+    uint32_t run[RUNS];       // runs that reach tau: note << 16 | thread
+    int runs;
     float wmax[32];
     Stat part[NT / 32];
     Stat total;
@@ -316,7 +321,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
             if (lane == __ffs(__ballot_sync(FULL, v == top)) - 1) v = neg_inf();
         }
         if (tid < KMAX) sm.top[tid] = 0;
-        if (tid == 0) sm.count = 0;
+        if (tid == 0) sm.count = sm.runs = 0;
     }
     __syncthreads();
     if (warp == 0) {
@@ -342,22 +347,52 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
         };
         if (scol >= 0) offer(sx, scol);
         const int nn = iters > 0 ? ((iters - 1) >> shift) + 1 : 0;
-        for (int n = 0; n < nn; ++n) {
-            const float top = sm.note[n][tid];
-            if (!(top >= tau && top > neg_inf())) continue;
-            for (int it = n << shift; it < min(iters, (n + 1) << shift); ++it) {
-                if (iters > 1) load(it);   // (a single run is still in registers)
+        if (iters == 1) {   // the only run is still in registers
+            if (sm.note[0][tid] >= tau) {
 #pragma unroll
                 for (int q = 0; q < U; ++q) {
-                    const int v = v0 + it * (NT * U) + q * NT + tid;
                     float x[E];
                     Vec<TX>::split(raw[q], x);
-                    float mx = x[0];
 #pragma unroll
-                    for (int e = 1; e < E; ++e) mx = fmaxf(mx, x[e]);
-                    if (mx >= tau) {   // (what lies past the end reads as -inf)
+                    for (int e = 0; e < E; ++e) offer(x[e], row.head + (v0 + q * NT + tid) * E + e);   // (past the end: -inf)
+                }
+            }
+        } else {
+            for (int n = 0; n < nn; ++n) {
+                const float top = sm.note[n][tid];
+                if (top >= tau && top > neg_inf()) {
+                    const int at = atomicAdd(&sm.runs, 1);
+                    if (at < RUNS) sm.run[at] = (uint32_t)(n << 16 | tid);
+                }
+            }
+            __syncthreads();
+            // a run's 64 bytes by a warp, one value to a lane, several runs in flight
+            constexpr int PER = 4, VALUES = U * E;
+            const int R = sm.runs;
+            if (R > RUNS) {
+                if (tid == 0) sm.count = CAP + 1;
+            } else {
+                for (int i0 = warp; i0 < R; i0 += PER * (NT / 32)) {
+                    for (int half = 0; half < 1 << shift; ++half) {
+                        float x[PER];
+                        int col[PER];
 #pragma unroll
-                        for (int e = 0; e < E; ++e) offer(x[e], row.head + v * E + e);
+                        for (int p = 0; p < PER; ++p) {
+                            const int i = i0 + p * (NT / 32);
+                            x[p] = neg_inf();
+                            col[p] = 0;
+                            if (i < R && lane < VALUES) {
+                                const uint32_t run = sm.run[i];
+                                const int it = ((int)(run >> 16) << shift) + half;
+                                const int v = v0 + it * (NT * U) + lane / E * NT + (int)(run & 0xFFFFu);
+                                if (it < iters && v < v1) {
+                                    col[p] = row.head + v * E + lane % E;
+                                    x[p] = load_as_float(row.p, col[p]);
+                                }
+                            }
+                        }
+#pragma unroll
+                        for (int p = 0; p < PER; ++p) offer(x[p], col[p]);
                     }
                 }
             }
@@ -401,28 +436,25 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
         __syncthreads();
     }
 
-    // ---- join the cluster's parts on its first CTA ----
+    // ---- join the cluster's parts on its first CTA, into which every CTA writes its own ----
     if (CL > 1) {
+        FwdSmem<NT> *first = cluster.map_shared_rank(&sm, 0);
+        if (tid == 0) first->cluster_total[rank] = sm.total;
+        if (tid < k) first->cluster_top[rank * k + tid] = sm.top[tid];
         cluster.sync();
-        if (rank == 0) {
-            Stat t{neg_inf(), 0.f, 0.f};
-            if (warp == NT / 32 - 1) {
-                if (lane < CL) t = *cluster.map_shared_rank(&sm.total, lane);
-                t = join_warp(t);
-            }
-            const int c = tid < CL * k ? tid / k : -1;
-            const uint64_t key = c >= 0 ? cluster.map_shared_rank(&sm, c)->top[tid - c * k] : 0;
-            if (c >= 0) sm.cand[tid] = key;
-            __syncthreads();
-            if (tid == NT - 1) sm.total = t;
-            if (tid < k) sm.top[tid] = 0;
-            const int at = key ? place_of(sm.cand, CL * k, key) : k;
-            __syncthreads();
-            if (at < k) sm.top[at] = key;
-            __syncthreads();
-        }
-        cluster.sync();   // the other CTAs' shared memory has been read
         if (rank != 0) return;
+        if (warp == NT / 32 - 1) {
+            const Stat t = join_warp(lane < CL ? sm.cluster_total[lane] : Stat{neg_inf(), 0.f, 0.f});
+            if (lane == 0) sm.total = t;
+        }
+        if (tid < k) sm.top[tid] = 0;
+        __syncthreads();
+        for (int i = tid; i < CL * k; i += NT) {
+            const uint64_t key = sm.cluster_top[i];
+            const int at = key ? place_of(sm.cluster_top, CL * k, key) : k;
+            if (at < k) sm.top[at] = key;
+        }
+        __syncthreads();
     }
 
     const Stat t = sm.total;
