@@ -449,10 +449,19 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
         }
         if (tid < k) sm.top[tid] = 0;
         __syncthreads();
-        for (int i = tid; i < CL * k; i += NT) {
-            const uint64_t key = sm.cluster_top[i];
-            const int at = key ? place_of(sm.cluster_top, CL * k, key) : k;
-            if (at < k) sm.top[at] = key;
+        // a key's place: eight lanes count the larger keys, each in one CTA's list, which is in order
+        for (int u0 = 0; u0 < CL * k * MAX_CLUSTER; u0 += NT) {
+            const int i = (u0 + tid) / MAX_CLUSTER, list = tid % MAX_CLUSTER;
+            const uint64_t key = i < CL * k ? sm.cluster_top[i] : 0;
+            int above = 0;
+            if (key && list < CL) {
+                for (int step = KMAX / 2; step > 0; step >>= 1)   // (above < k always leaves a key to look at)
+                    if (above + step <= k && sm.cluster_top[list * k + above + step - 1] > key) above += step;
+                if (above < k && sm.cluster_top[list * k + above] > key) ++above;
+            }
+#pragma unroll
+            for (int o = 1; o < MAX_CLUSTER; o <<= 1) above += __shfl_xor_sync(FULL, above, o);
+            if (key && list == 0 && above < k) sm.top[above] = key;
         }
         __syncthreads();
     }
