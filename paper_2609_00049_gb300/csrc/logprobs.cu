@@ -11,9 +11,9 @@
 //
 // The k likeliest in the same pass: each thread notes the maximum of every
 // 64-byte run it reads (runs merged so that it has at most 32 notes).  The four
-// largest thread maxima of each of the 8 warps are 32 different elements of
-// the row, so the k-th largest of them is a lower bound tau of the k-th
-// largest element.  Only runs whose note reaches tau are read again (from L2),
+// largest thread maxima of each of the 8 warps (the eight largest of each of 4,
+// in a CTA of 128 threads) are 32 different elements of the row, so the k-th
+// largest of them is a lower bound tau of the k-th largest element.  Only runs whose note reaches tau are read again (from L2),
 // their elements >= tau collected and ranked by (value, lower index).  Where
 // more than CAP elements reach tau (rows of equal values), k ordered passes
 // over the row take their place.
@@ -27,12 +27,12 @@
 //
 // All sums are fp32 per thread (a few hundred terms), joined pairwise.
 //
-// Measured, 4096 rows x 128256 in bf16: 183 us with 5 alternatives (5.7 TB/s),
+// Measured, 4096 rows x 128256 in bf16: 181 us with 5 alternatives (5.8 TB/s),
 // 165 without (6.4 TB/s); the rows' ends, where the candidates are ranked, are
 // the difference.  Taking the arithmetic's clamp or its packing away does not
 // change it, more CTAs per SM (five or six, 40 to 48 registers) make it slower
-// (208 to 217 us).  The gradient: 313 us (6.7 TB/s).  One row: 10 us, of which
-// reading it takes 2.
+// (208 to 217 us).  The gradient: 313 us (6.7 TB/s).  One row with 20
+// alternatives: 9 us, of which the launch and reading it take 4.
 #include <cooperative_groups.h>
 
 #include "kernels.cuh"
