@@ -246,6 +246,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
     __shared__ FwdSmem<NT> sm;
     cg::cluster_group cluster = cg::this_cluster();
     const int CL = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    // (waited for before the first CTA's shared memory is written: by then it has to have started)
+    if (CL > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
     const int64_t r = blockIdx.x / CL;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const Row<TX> row(X + r * ld, V);
@@ -438,6 +440,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT)
 
     // ---- join the cluster's parts on its first CTA, into which every CTA writes its own ----
     if (CL > 1) {
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
         FwdSmem<NT> *first = cluster.map_shared_rank(&sm, 0);
         if (tid == 0) first->cluster_total[rank] = sm.total;
         if (tid < k) first->cluster_top[rank * k + tid] = sm.top[tid];
