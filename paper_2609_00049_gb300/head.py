@@ -21,6 +21,7 @@ arithmetic happens here beyond the mean of the scored log probabilities.
 """
 from __future__ import annotations
 
+import contextlib
 from dataclasses import dataclass
 from typing import Optional
 
@@ -43,16 +44,32 @@ class HeadStep:
     targets: torch.Tensor
     codes: torch.Tensor                   # the hidden states' checkpoint
     exps: torch.Tensor
+    done: Optional[torch.cuda.Event] = None   # the pass has run
 
     def perplexity(self) -> float:
         """exp of minus the mean log probability of the scored tokens (synchronizes)."""
+        if self.done is not None:
+            torch.cuda.current_stream(self.logprob.device).wait_event(self.done)
         scored = self.targets >= 0
         return float(torch.exp(-self.logprob[scored].double().mean()))
 
 
+def _used_on(stream, *tensors: Optional[torch.Tensor]) -> None:
+    """Keep the tensors' memory from being handed on before `stream` is done with it."""
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+
+
 class Head8:
-    """An LM head of 8-bit channel codes with one scale per output token.  Its
-    workspaces are reused from call to call, so use one stream at a time."""
+    """An LM head of 8-bit channel codes with one scale per output token.
+
+    Any stream: a pass on a stream other than the current one (`stream`) starts
+    after what the current stream holds and takes its memory from its own
+    stream; its results are there once that stream has run, and the current
+    stream has to wait for it before it reads them, as with any operator.  The
+    head's workspaces are reused from call to call, so its passes run one after
+    the other, whatever their streams."""
 
     def __init__(self, W: torch.Tensor, logits_dtype=torch.bfloat16):
         self.vocab, self.d = W.shape
@@ -61,30 +78,51 @@ class Head8:
         self.scale = torch.empty(self.vocab, dtype=torch.float32, device=W.device)
         realq_quantize_activations(W, 8, 1.0, codes=self.codes, scale=self.scale)   # a row's symmetric 8-bit grid
         self._ws = {}
+        self._last = torch.cuda.current_stream(W.device).record_event()   # the head's codes, then its latest pass
 
-    def _workspace(self, key: str, nbytes: int, device) -> Optional[torch.Tensor]:
+    def _workspace(self, key: str, nbytes: int, stream, device) -> Optional[torch.Tensor]:
         have = self._ws.get(key)
         if have is None or have.numel() < nbytes:
             self._ws[key] = have = workspace(nbytes, device)
+        _used_on(stream, have)
         return have
+
+    @contextlib.contextmanager
+    def _pass(self, stream):
+        """A pass on `stream` (None: the current one), which becomes the current
+        one: allocations belong to it.  It starts after the caller's work and the
+        head's latest pass.  Yields it and the caller's stream."""
+        caller = torch.cuda.current_stream(self.codes.device)
+        s = caller if stream is None else stream
+        if s != caller:
+            s.wait_stream(caller)
+        s.wait_event(self._last)
+        with torch.cuda.stream(s):
+            _used_on(s, self.codes, self.scale)
+            try:
+                yield s, caller
+            finally:   # (a refused call may follow launched ones)
+                self._last = s.record_event()
 
     def forward(self, h: torch.Tensor, targets: torch.Tensor, k: int = 0, stream=None) -> HeadStep:
         """Score the next tokens (negative targets are not scored) with the k
         likeliest alternatives of each position."""
         T, dev = h.shape[0], h.device
         new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=dev)  # noqa: E731
-        xc, xs = new(T, self.d, dtype=torch.uint8), new(T)
-        realq_quantize_activations(h, 8, 1.0, codes=xc, scale=xs, stream=stream)
-        logits = new(T, self.vocab, dtype=self.logits_dtype)
-        ws = self._workspace("product", realq_int8_product_workspace_size(T, self.d, self.vocab), dev)
-        realq_int8_product(xc, xs, self.codes, self.scale, logits, ws=ws, stream=stream)
-        step = HeadStep(new(T), new(T), new(T, k, dtype=torch.int64) if k else None, new(T, k) if k else None, logits,
-                        new(T, 2), targets, new(T, self.d, dtype=torch.int8),
-                        new(T, (self.d + 31) // 32, dtype=torch.uint8))
-        realq_token_logprobs(logits, targets, step.logprob, step.norm, step.entropy, step.top_ids, step.top_logprob,
-                             stream=stream)
-        realq_checkpoint_pack(h, step.codes, step.exps, stream=stream)
-        return step
+        with self._pass(stream) as (s, caller):
+            _used_on(s, h, targets)
+            xc, xs = new(T, self.d, dtype=torch.uint8), new(T)
+            realq_quantize_activations(h, 8, 1.0, codes=xc, scale=xs, stream=s)
+            logits = new(T, self.vocab, dtype=self.logits_dtype)
+            ws = self._workspace("product", realq_int8_product_workspace_size(T, self.d, self.vocab), s, dev)
+            realq_int8_product(xc, xs, self.codes, self.scale, logits, ws=ws, stream=s)
+            out = dict(logprob=new(T), norm=new(T, 2), entropy=new(T),
+                       top_ids=new(T, k, dtype=torch.int64) if k else None, top_logprob=new(T, k) if k else None)
+            realq_token_logprobs(logits, targets, **out, stream=s)
+            codes, exps = new(T, self.d, dtype=torch.int8), new(T, (self.d + 31) // 32, dtype=torch.uint8)
+            realq_checkpoint_pack(h, codes, exps, stream=s)
+            _used_on(caller, logits, codes, exps, *out.values())
+        return HeadStep(**out, logits=logits, targets=targets, codes=codes, exps=exps, done=self._last)
 
     def weight_grad(self, step: HeadStep, d_logprob: torch.Tensor, d_entropy: Optional[torch.Tensor] = None,
                     dW: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
@@ -95,13 +133,16 @@ class Head8:
             raise ValueError("this step's logits have been used by a backward pass")
         T, dev = step.codes.shape[0], step.codes.device
         d_logits, step.logits = step.logits, None
-        realq_token_logprobs_grad(d_logits, step.targets, step.norm, d_logits, d_logprob=d_logprob,
-                                  entropy=step.entropy if d_entropy is not None else None, d_entropy=d_entropy,
-                                  stream=stream)
-        accumulate = dW is not None
-        if dW is None:
-            dW = torch.empty((self.vocab, self.d), dtype=torch.float32, device=dev)
-        ws = self._workspace("grad", realq_checkpoint_weight_grad_workspace_size(T, self.vocab, self.d, d_logits.dtype),
-                             dev)
-        return realq_checkpoint_weight_grad(d_logits, step.codes, step.exps, dW, accumulate=accumulate, ws=ws,
-                                            stream=stream)
+        with self._pass(stream) as (s, caller):
+            _used_on(s, d_logits, step.targets, step.norm, step.entropy, step.codes, step.exps, d_logprob, d_entropy, dW)
+            realq_token_logprobs_grad(d_logits, step.targets, step.norm, d_logits, d_logprob=d_logprob,
+                                      entropy=step.entropy if d_entropy is not None else None, d_entropy=d_entropy,
+                                      stream=s)
+            accumulate = dW is not None
+            if dW is None:
+                dW = torch.empty((self.vocab, self.d), dtype=torch.float32, device=dev)
+                _used_on(caller, dW)
+            ws = self._workspace("grad", realq_checkpoint_weight_grad_workspace_size(T, self.vocab, self.d,
+                                                                                     d_logits.dtype), s, dev)
+            return realq_checkpoint_weight_grad(d_logits, step.codes, step.exps, dW, accumulate=accumulate, ws=ws,
+                                                stream=s)
