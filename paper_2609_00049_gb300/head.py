@@ -132,6 +132,12 @@ class Head8:
         if step.logits is None:
             raise ValueError("this step's logits have been used by a backward pass")
         T, dev = step.codes.shape[0], step.codes.device
+        for name, t, shape in (("d_logprob", d_logprob, (T,)), ("d_entropy", d_entropy, (T,)),
+                               ("dW", dW, (self.vocab, self.d))):   # before the logits are used up
+            if t is not None and (t.dtype != torch.float32 or t.shape != shape or t.device != dev
+                                  or not t.is_contiguous()):
+                raise ValueError(f"{name}: expected a contiguous float32 tensor of shape {shape} on {dev}, got "
+                                 f"{t.dtype} {tuple(t.shape)} on {t.device}")
         d_logits, step.logits = step.logits, None
         with self._pass(stream) as (s, caller):
             _used_on(s, d_logits, step.targets, step.norm, step.entropy, step.codes, step.exps, d_logprob, d_entropy, dW)

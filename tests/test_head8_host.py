@@ -144,3 +144,21 @@ def test_perplexity_waits_for_the_pass(world):
     at = len(log)
     step.perplexity()
     assert ("wait_event", "main", "side") in log[at:]
+
+
+def test_a_refused_backward_pass_keeps_the_logits():
+    """A backward pass whose arguments are refused has not used the step's
+    logits: it can be called again with the right ones."""
+    head = head_module.Head8.__new__(head_module.Head8)   # (no GPU: the fields that the checks read)
+    head.vocab, head.d = 12, 8
+    head.codes, head.scale = torch.zeros(12, 8, dtype=torch.uint8), torch.zeros(12)
+    logits, f = torch.zeros(4, 12), torch.zeros(4)
+    step = head_module.HeadStep(f, f, None, None, logits, torch.zeros(4, 2), torch.zeros(4, dtype=torch.int64),
+                                torch.zeros(4, 8, dtype=torch.int8), torch.zeros(4, 1, dtype=torch.uint8))
+    for bad in (dict(d_logprob=torch.zeros(5)), dict(d_logprob=torch.zeros(4, dtype=torch.float64)),
+                dict(d_logprob=f, d_entropy=torch.zeros(3)), dict(d_logprob=f, dW=torch.zeros(12, 9)),
+                dict(d_logprob=f, dW=torch.zeros(12, 8, dtype=torch.bfloat16)),
+                dict(d_logprob=f, dW=torch.zeros(8, 12).t())):
+        with pytest.raises(ValueError):
+            head.weight_grad(step, **bad)
+        assert step.logits is logits
