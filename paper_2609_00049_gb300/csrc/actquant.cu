@@ -12,7 +12,9 @@
 // formed in fp32 and stored in the input's format.  Every operation that
 // decides an integer is an explicitly rounded fp32 operation (no contraction),
 // so the codes are reproducible bit for bit.  A row of zeros gets the range
-// [-1, 1].
+// [-1, 1].  A row holding an infinity or a NaN has no grid: its scale and its
+// x_q are NaN and its codes the zero point, so that whatever is formed from the
+// codes and the scale shows it.
 #include "kernels.cuh"
 
 namespace realq {
@@ -32,14 +34,17 @@ __global__ void __launch_bounds__(256) act_quant_kernel(int64_t T, int64_t n, co
     const int64_t t = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
     if (t >= T) return;
     const TX *x = X + t * n;
-    float amax = 0.f;
-    for (int64_t c = lane; c < n; c += 32) amax = fmaxf(amax, fabsf(to_f(x[c])));
+    // the bits of |x| are ordered like the magnitudes, infinities and NaN above all numbers (fmaxf would drop a NaN)
+    uint32_t top = 0;
+    for (int64_t c = lane; c < n; c += 32) top = max(top, __float_as_uint(to_f(x[c])) & 0x7FFFFFFFu);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(FULL, amax, o));
+    for (int o = 16; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(FULL, top, o));
+    const bool finite = top < 0x7F800000u;
+    const float amax = __uint_as_float(top);
     const int maxq = (1 << bits) - 1, zero = 1 << (bits - 1);
     float xmax = __fmul_rn(a_clip, amax);
     if (xmax == 0.f) xmax = 1.f;
-    const float scale = __fdiv_rn(__fadd_rn(xmax, xmax), (float)maxq);
+    const float scale = finite ? __fdiv_rn(__fadd_rn(xmax, xmax), (float)maxq) : __uint_as_float(0x7FC00000u);
     if (lane == 0 && scale_out) scale_out[t] = scale;
     TX *xq = Xq + t * n;
     const bool packed = bits <= 4;
@@ -50,7 +55,7 @@ __global__ void __launch_bounds__(256) act_quant_kernel(int64_t T, int64_t n, co
         if (c < n) {
             float r = rintf(__fdiv_rn(to_f(x[c]), scale));
             r = fminf(fmaxf(r, (float)(-zero - 1)), (float)(maxq - zero + 1));
-            q = min(max((int)r + zero, 0), maxq);
+            q = finite ? min(max((int)r + zero, 0), maxq) : zero;
             store(xq + c, __fmul_rn(scale, (float)(q - zero)));
         }
         if (codes) {

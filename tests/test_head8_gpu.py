@@ -62,3 +62,55 @@ def test_a_pass_on_a_side_stream_gives_the_same_bits(T):
             assert ppl == want[i][1]
             for a, b in zip(kept + [dW], want[i][0] + [want[i][2]]):
                 assert torch.equal(a, b)
+
+
+BAD = [math.nan, math.inf, -math.inf]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("n", [1, 31, 64, 515])
+def test_quantized_activations_show_what_is_not_finite(dtype, bits, n):
+    """A token with an infinity or a NaN: NaN scale and values; the others are as without it."""
+    x = torch.randn(9, n, generator=gen(n), device="cuda").to(dtype)
+
+    def run(v):
+        codes = torch.empty(9, (n + 1) // 2 if bits <= 4 else n, dtype=torch.uint8, device="cuda")
+        scale = torch.empty(9, device="cuda")
+        return rq.realq_quantize_activations(v, bits, 0.9, codes=codes, scale=scale), codes, scale
+
+    want = run(x)
+    bad = x.clone()
+    for i, v in enumerate(BAD):
+        bad[2 * i + 1, (n // 2 + i) % n] = v
+    got = run(bad)
+    rows = torch.arange(9, device="cuda")
+    hit = (rows % 2 == 1) & (rows < 6)
+    assert torch.isnan(got[0][hit]).all() and torch.isnan(got[2][hit]).all()
+    packed = 128 if bits == 8 else 0x88
+    assert (got[1][hit][:, : n // 2] == packed).all()
+    for a, b in zip(got, want):
+        assert torch.equal(a[~hit], b[~hit])
+
+
+@pytest.mark.parametrize("T", [5, 40])     # both sides of the product's dispatch
+@pytest.mark.parametrize("logits", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("value", BAD)
+def test_a_hidden_state_that_is_not_finite_shows(T, logits, value):
+    """Its log probability and entropy are NaN, the other tokens' are untouched,
+    and the weight gradient of the same step is NaN where it takes part."""
+    d, vocab = 1024, 30011
+    h, y, w = inputs(T, d, vocab)
+    head = Head8(0.05 * torch.randn(vocab, d, generator=gen(2), device="cuda"), logits_dtype=logits)
+    want = head.forward(h, y, k=4)
+    h = h.clone()
+    h[3, 700] = value
+    step = head.forward(h, y, k=4)
+    rows = torch.arange(T, device="cuda") != 3
+    assert torch.isnan(step.logits[3]).all() and torch.isnan(step.logprob[3]) and torch.isnan(step.entropy[3])
+    assert (step.top_ids[3] == -1).all()
+    assert math.isnan(step.perplexity())
+    for a, b in ((step.logprob, want.logprob), (step.entropy, want.entropy), (step.top_ids, want.top_ids)):
+        assert torch.equal(a[rows], b[rows])
+    dW = head.weight_grad(step, w)
+    assert torch.isnan(dW).all()
