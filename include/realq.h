@@ -270,8 +270,10 @@ realq_status_t realq_quantize_activations(realq_stream_t stream, int64_t T, int6
  *   Y        T x m, y_dtype.
  *   ws       realq_int8_product_workspace_size(T, n, m, w_bits) bytes,
  *            256-byte aligned; the first word is the status that
- *            realq_workspace_status reads (REALQ_ERR_TIMEOUT: Y holds NaN
- *            where a bounded wait gave up).
+ *            realq_workspace_status reads and clears (REALQ_ERR_TIMEOUT: a
+ *            call since the last reading left NaN in Y where a bounded wait
+ *            gave up).  Zero that word before a workspace's first use; calls
+ *            only add to it.
  * Any alignment of the codes.  n at most REALQ_INT8_PRODUCT_MAX_N, T and m
  * below 2^30, T m at most 2^40.  T = 0 is a no-op.  Asynchronous. */
 #define REALQ_INT8_PRODUCT_MAX_N 131071
@@ -330,9 +332,10 @@ realq_status_t realq_token_logprobs_grad(realq_stream_t stream, int64_t T, int64
  * accumulate != 0.  dY: T x m, dy_dtype, 16-byte aligned.  Products are exact,
  * sums fp32; a fixed order of summation (bitwise repeatable).  ws:
  * realq_checkpoint_weight_grad_workspace_size(T, m, n, dy_dtype) bytes,
- * 256-byte aligned; its first word is the status that realq_workspace_status
- * reads (REALQ_ERR_TIMEOUT: NaN where a bounded wait gave up).  T = 0 leaves
- * or clears dW.  Asynchronous. */
+ * 256-byte aligned; its first word is a status as that of realq_int8_product's
+ * workspace (zeroed before the first use, added to by calls, read and cleared
+ * by realq_workspace_status; REALQ_ERR_TIMEOUT: NaN in dW where a bounded wait
+ * gave up).  T = 0 leaves or clears dW.  Asynchronous. */
 realq_status_t realq_checkpoint_pack(realq_stream_t stream, int64_t T, int64_t n, const void *X, realq_dtype_t x_dtype,
                                      int8_t *codes, uint8_t *exps);
 realq_status_t realq_checkpoint_unpack(realq_stream_t stream, int64_t T, int64_t n, const int8_t *codes,
@@ -529,7 +532,7 @@ realq_status_t realq_surrogate_loss(realq_stream_t stream, int64_t m, int64_t n,
 size_t realq_surrogate_workspace_size(int64_t m, int64_t n);
 
 /* Synchronizes `stream`, returns the device status word recorded at the start
- * of a Hessian, quantize or block-ops workspace (REALQ_OK, REALQ_ERR_TIMEOUT,
+ * of a Hessian, quantize, block-ops, product or weight-gradient workspace (REALQ_OK, REALQ_ERR_TIMEOUT,
  * REALQ_ERR_NONFINITE) and clears it. */
 realq_status_t realq_workspace_status(realq_stream_t stream, void *ws, size_t ws_bytes);
 

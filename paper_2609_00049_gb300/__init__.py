@@ -1025,7 +1025,8 @@ def realq_quantize_layer_window(dims: BlockDims, this_block: dict, next_block: O
 
 
 def realq_workspace_status(ws: torch.Tensor, stream=None) -> int:
-    """Synchronizes; raises RealqError if the sweep recorded a non-finite weight."""
+    """Synchronizes; raises RealqError if the workspace's kernels recorded a
+    non-finite weight or a bounded wait that gave up, and clears the record."""
     wp, wb = _ws(ws)
     _check(lib().realq_workspace_status(_stream(stream), wp, wb))
     return REALQ_OK

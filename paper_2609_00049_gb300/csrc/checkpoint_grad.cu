@@ -346,12 +346,10 @@ struct Planes {
     const void *dY;
     int dy_f32;
     __nv_bfloat16 *dy;
-    int *status;
 };
 template <bool FLATX, bool FLATY>
 __global__ void __launch_bounds__(256) grad_planes_kernel(const Planes p) {
     dependents_may_start();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = 0;
     if (blockIdx.x < p.xblocks) {
         const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, pieces = (p.n + 15) / 16;
         if (i >= p.T * pieces) return;
@@ -485,7 +483,7 @@ realq_status_t checkpoint_grad(cudaStream_t s, int64_t T, int64_t m, int64_t n, 
     const int64_t ldx = pad8(n), ldy = pad8(m);
     const bool xv = n % 32 == 0 && (reinterpret_cast<uintptr_t>(codes) & 15) == 0, yv = dt == REALQ_F32 && m % 8 == 0;
     Planes p{T, n, m, ldx, ldy, (unsigned)((T * ((n + 15) / 16) + 255) / 256), codes, exps, w.x, dY,
-             dt == REALQ_F32, w.dy, w.status};
+             dt == REALQ_F32, w.dy};
     const int64_t ypieces = T * (dt == REALQ_F32 ? (m + 3) / 4 : ldy / 8);
     const unsigned blocks = p.xblocks + (direct ? 0u : (unsigned)((ypieces + 255) / 256));
     {

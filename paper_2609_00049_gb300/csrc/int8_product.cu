@@ -177,8 +177,7 @@ template <int WB, int NT, int RT> struct Ring {
 template <bool ALIGNED, int WB, int NT, int RT, typename TY>
 __global__ void __launch_bounds__(SW * 32, 2)
     int8_stream_kernel(int64_t T, int64_t n, int64_t m, const uint8_t *X, const float *x_scale, const uint8_t *W,
-                       const float *w_scale, const uint8_t *w_zero, TY *Y, int *status) {
-    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *status = 0;   // (no wait here can give up)
+                       const float *w_scale, const uint8_t *w_zero, TY *Y) {
     using S = Sums<WB, NT, RT>;
     using R = Ring<WB, NT, RT>;
     constexpr int XP = S::XP, ROWS = RT * 16, TOK = NT * 8, OUT = ROWS * TOK;
@@ -378,7 +377,7 @@ __global__ void __launch_bounds__(SW * 32, 2)
 
 template <bool ALIGNED, int WB, int NT, int RT, typename TY>
 realq_status_t stream_launch(cudaStream_t s, int64_t T, int64_t n, int64_t m, const uint8_t *X, const float *xs,
-                             const uint8_t *W, const float *ws, const uint8_t *wz, TY *Y, int *status, int sms) {
+                             const uint8_t *W, const float *ws, const uint8_t *wz, TY *Y, int sms) {
     // Clusters walk the tiles of RT x 16 channels; CTAs over K: the count whose
     // turns take the fewest steps of a warp, a tile's end counted as two, each
     // warp keeping at least two steps.
@@ -410,32 +409,32 @@ realq_status_t stream_launch(cudaStream_t s, int64_t T, int64_t n, int64_t m, co
     cfg.numAttrs = cl > 1 ? 1 : 0;
     {
         Launch L("int8_product_stream", s);
-        REALQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, int8_stream_kernel<ALIGNED, WB, NT, RT, TY>, T, n, m, X, xs, W, ws, wz, Y, status));
+        REALQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, int8_stream_kernel<ALIGNED, WB, NT, RT, TY>, T, n, m, X, xs, W, ws, wz, Y));
     }
     return check_launch("int8_product_stream");
 }
 
 template <bool ALIGNED, int WB, typename TY>
 realq_status_t stream_tokens(cudaStream_t s, int64_t T, int64_t n, int64_t m, const uint8_t *X, const float *xs,
-                             const uint8_t *W, const float *ws, const uint8_t *wz, TY *Y, int *status, int sms) {
+                             const uint8_t *W, const float *ws, const uint8_t *wz, TY *Y, int sms) {
     // 32 channels to a warp halve the work on the tokens' codes, where there are enough of them; unaligned tokens are
     // more work, so there a quarter of that is enough where rows are long (1 x 15767 x 3927: 26 us against 33)
     const int64_t rb = WB == 8 ? n : (n + 1) / 2;
     const bool wide = m >= (int64_t)sms * 32 || (!ALIGNED && m >= (int64_t)sms * 8 && rb >= 4096);
     if (T <= 8)
-        return wide ? stream_launch<ALIGNED, WB, 1, 2, TY>(s, T, n, m, X, xs, W, ws, wz, Y, status, sms)
-                    : stream_launch<ALIGNED, WB, 1, 1, TY>(s, T, n, m, X, xs, W, ws, wz, Y, status, sms);
-    return wide ? stream_launch<ALIGNED, WB, 2, 2, TY>(s, T, n, m, X, xs, W, ws, wz, Y, status, sms)
-                : stream_launch<ALIGNED, WB, 2, 1, TY>(s, T, n, m, X, xs, W, ws, wz, Y, status, sms);
+        return wide ? stream_launch<ALIGNED, WB, 1, 2, TY>(s, T, n, m, X, xs, W, ws, wz, Y, sms)
+                    : stream_launch<ALIGNED, WB, 1, 1, TY>(s, T, n, m, X, xs, W, ws, wz, Y, sms);
+    return wide ? stream_launch<ALIGNED, WB, 2, 2, TY>(s, T, n, m, X, xs, W, ws, wz, Y, sms)
+                : stream_launch<ALIGNED, WB, 2, 1, TY>(s, T, n, m, X, xs, W, ws, wz, Y, sms);
 }
 
 template <int WB, typename TY>
 realq_status_t stream(cudaStream_t s, int64_t T, int64_t n, int64_t m, const uint8_t *X, const float *xs,
-                      const uint8_t *W, const float *ws, const uint8_t *wz, TY *Y, int *status, int sms) {
+                      const uint8_t *W, const float *ws, const uint8_t *wz, TY *Y, int sms) {
     const bool aligned = n % (WB == 8 ? 16 : 32) == 0 &&
                          ((reinterpret_cast<uintptr_t>(X) | reinterpret_cast<uintptr_t>(W)) & 15) == 0;
-    return aligned ? stream_tokens<true, WB, TY>(s, T, n, m, X, xs, W, ws, wz, Y, status, sms)
-                   : stream_tokens<false, WB, TY>(s, T, n, m, X, xs, W, ws, wz, Y, status, sms);
+    return aligned ? stream_tokens<true, WB, TY>(s, T, n, m, X, xs, W, ws, wz, Y, sms)
+                   : stream_tokens<false, WB, TY>(s, T, n, m, X, xs, W, ws, wz, Y, sms);
 }
 
 // Whether the streaming kernel runs: for up to 16 tokens (8192 -> 28672: 16
@@ -467,8 +466,8 @@ realq_status_t int8_product(cudaStream_t s, int64_t T, int64_t n, int64_t m, con
         constexpr int64_t MOST = GROUP * 65535;   // a grid's
         for (int64_t t = 0; t < T; t += MOST) {
             const int64_t k = std::min(MOST, T - t);
-            REALQ_TRY(w_bits == 8 ? stream<8>(s, k, n, m, X + t * n, x_scale + t, W, w_scale, w_zero, y + t * m, static_cast<int *>(ws), sms)
-                                  : stream<4>(s, k, n, m, X + t * n, x_scale + t, W, w_scale, w_zero, y + t * m, static_cast<int *>(ws), sms));
+            REALQ_TRY(w_bits == 8 ? stream<8>(s, k, n, m, X + t * n, x_scale + t, W, w_scale, w_zero, y + t * m, sms)
+                                  : stream<4>(s, k, n, m, X + t * n, x_scale + t, W, w_scale, w_zero, y + t * m, sms));
         }
         return REALQ_OK;
     };

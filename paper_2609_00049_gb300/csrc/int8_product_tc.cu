@@ -421,7 +421,6 @@ __global__ void __launch_bounds__(256) int8_reduce_kernel(const Shape sh, const 
 
 // Token codes -> fp16 plane of row stride ld (16 codes per thread where rows
 // are whole vectors)
-// (both also clear the status word)
 __device__ __forceinline__ void store_codes(uint4 *o, const uint4 &q, bool both) {
     const uint32_t v[4] = {q.x, q.y, q.z, q.w};
     uint32_t h[8];
@@ -433,20 +432,17 @@ __device__ __forceinline__ void store_codes(uint4 *o, const uint4 &q, bool both)
     o[0] = make_uint4(h[0], h[1], h[2], h[3]);
     if (both) o[1] = make_uint4(h[4], h[5], h[6], h[7]);
 }
-__global__ void __launch_bounds__(256) int8_plane_vec_kernel(int64_t count, const uint8_t *X, uint32_t *plane,
-                                                             int *status) {
+__global__ void __launch_bounds__(256) int8_plane_vec_kernel(int64_t count, const uint8_t *X, uint32_t *plane) {
     dependents_may_start();
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i == 0) *status = 0;
     if (i < count)
         store_codes(reinterpret_cast<uint4 *>(plane) + 2 * i, __ldg(reinterpret_cast<const uint4 *>(X) + i), true);
 }
 // any width and address; 16 codes a thread, ld a multiple of 8
 __global__ void __launch_bounds__(256) int8_plane_kernel(int64_t T, int64_t n, const uint8_t *X, __half *plane,
-                                                         int64_t ld, int *status) {
+                                                         int64_t ld) {
     dependents_may_start();
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, pieces = (n + 15) / 16;
-    if (i == 0) *status = 0;
     if (i >= T * pieces) return;
     int64_t c;
     const int64_t t = divide(i, pieces, c);
@@ -591,9 +587,9 @@ realq_status_t int8_product_tc(cudaStream_t s, int64_t T, int64_t n, int64_t m, 
         Launch L("int8_product_plane", s);
         if (n % 16 == 0 && (reinterpret_cast<uintptr_t>(X) & 15) == 0)
             int8_plane_vec_kernel<<<(unsigned)((T * n / 16 + 255) / 256), 256, 0, s>>>(
-                T * n / 16, X, reinterpret_cast<uint32_t *>(b.x), b.status);
+                T * n / 16, X, reinterpret_cast<uint32_t *>(b.x));
         else
-            int8_plane_kernel<<<(unsigned)((T * ((n + 15) / 16) + 255) / 256), 256, 0, s>>>(T, n, X, b.x, ldx, b.status);
+            int8_plane_kernel<<<(unsigned)((T * ((n + 15) / 16) + 255) / 256), 256, 0, s>>>(T, n, X, b.x, ldx);
     }
     REALQ_TRY(check_launch("int8_product_plane"));
     const int wrow = w_bits == 8 ? sh.kstep : sh.kstep / 2;

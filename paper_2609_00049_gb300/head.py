@@ -29,7 +29,7 @@ import torch
 
 from . import (realq_checkpoint_pack, realq_checkpoint_weight_grad, realq_checkpoint_weight_grad_workspace_size,
                realq_int8_product, realq_int8_product_workspace_size, realq_quantize_activations,
-               realq_token_logprobs, realq_token_logprobs_grad, workspace)
+               realq_token_logprobs, realq_token_logprobs_grad, realq_workspace_status, workspace)
 
 
 @dataclass
@@ -45,11 +45,15 @@ class HeadStep:
     codes: torch.Tensor                   # the hidden states' checkpoint
     exps: torch.Tensor
     done: Optional[torch.cuda.Event] = None   # the pass has run
+    head: Optional["Head8"] = None
 
     def perplexity(self) -> float:
-        """exp of minus the mean log probability of the scored tokens (synchronizes)."""
+        """exp of minus the mean log probability of the scored tokens (synchronizes).
+        Raises RealqError if a pass of the head since its last check gave up."""
         if self.done is not None:
             torch.cuda.current_stream(self.logprob.device).wait_event(self.done)
+        if self.head is not None:
+            self.head.check()
         scored = self.targets >= 0
         return float(torch.exp(-self.logprob[scored].double().mean()))
 
@@ -83,7 +87,10 @@ class Head8:
     def _workspace(self, key: str, nbytes: int, stream, device) -> Optional[torch.Tensor]:
         have = self._ws.get(key)
         if have is None or have.numel() < nbytes:
-            self._ws[key] = have = workspace(nbytes, device)
+            new = workspace(nbytes, device)
+            if have is not None:
+                new[:4].copy_(have[:4])   # the status word
+            self._ws[key] = have = new
         _used_on(stream, have)
         return have
 
@@ -104,6 +111,15 @@ class Head8:
             finally:   # (a refused call may follow launched ones)
                 self._last = s.record_event()
 
+    def check(self) -> None:
+        """Raises RealqError if a bounded wait gave up in a pass since the last
+        check, whose results then hold NaN (synchronizes)."""
+        with self._pass(None) as (s, _):
+            for ws in self._ws.values():
+                if ws is not None:
+                    _used_on(s, ws)
+                    realq_workspace_status(ws, stream=s)
+
     def forward(self, h: torch.Tensor, targets: torch.Tensor, k: int = 0, stream=None) -> HeadStep:
         """Score the next tokens (negative targets are not scored) with the k
         likeliest alternatives of each position."""
@@ -122,7 +138,7 @@ class Head8:
             codes, exps = new(T, self.d, dtype=torch.int8), new(T, (self.d + 31) // 32, dtype=torch.uint8)
             realq_checkpoint_pack(h, codes, exps, stream=s)
             _used_on(caller, logits, codes, exps, *out.values())
-        return HeadStep(**out, logits=logits, targets=targets, codes=codes, exps=exps, done=self._last)
+        return HeadStep(**out, logits=logits, targets=targets, codes=codes, exps=exps, done=self._last, head=self)
 
     def weight_grad(self, step: HeadStep, d_logprob: torch.Tensor, d_entropy: Optional[torch.Tensor] = None,
                     dW: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:

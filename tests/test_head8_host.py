@@ -77,6 +77,7 @@ def world(monkeypatch):
     monkeypatch.setattr(head_module, "realq_token_logprobs", operator("logprobs"))
     monkeypatch.setattr(head_module, "realq_token_logprobs_grad", operator("logprobs_grad"))
     monkeypatch.setattr(head_module, "realq_checkpoint_pack", operator("pack"))
+    monkeypatch.setattr(head_module, "realq_workspace_status", operator("status"), raising=False)
     monkeypatch.setattr(head_module, "realq_checkpoint_weight_grad", operator("weight_grad", result=3))
     monkeypatch.setattr(head_module, "realq_int8_product_workspace_size", lambda T, n, m: 256 * T)
     monkeypatch.setattr(head_module, "realq_checkpoint_weight_grad_workspace_size", lambda T, m, n, dt: 256 * T)
