@@ -294,10 +294,10 @@ __global__ void __launch_bounds__(256) weight_grad_reduce(const Work wk, const f
     if (row >= wk.m || col >= wk.n) return;
     const float4 *p = reinterpret_cast<const float4 *>(part + ((int64_t)slot * TT + r) * TT + c);
     const int64_t step = (int64_t)cut * TT * TT / 4;
-    float4 v = __ldg(p);
+    float4 v = load_after_wait(p);
 #pragma unroll 4
     for (int z = 1; z < wk.splits; ++z) {
-        const float4 b = __ldg(p + z * step);
+        const float4 b = load_after_wait(p + z * step);
         v.x += b.x;
         v.y += b.y;
         v.z += b.z;

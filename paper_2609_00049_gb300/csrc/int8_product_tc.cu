@@ -404,10 +404,10 @@ __global__ void __launch_bounds__(256) int8_reduce_kernel(const Shape sh, const 
     if (t >= sh.N || tok >= sh.T || i >= sh.m) return;
     const float4 *p = reinterpret_cast<const float4 *>(part + ((int64_t)slot * sh.N + t) * TM + c);
     const int64_t step = (int64_t)cut * sh.N * TM / 4;
-    float4 a = __ldg(p);
+    float4 a = load_after_wait(p);
 #pragma unroll 4
     for (int z = 1; z < sh.splits; ++z) {
-        const float4 b = __ldg(p + z * step);
+        const float4 b = load_after_wait(p + z * step);
         a.x += b.x;
         a.y += b.y;
         a.z += b.z;
