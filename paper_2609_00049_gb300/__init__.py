@@ -89,7 +89,6 @@ def bgd_cfg(lr, steps_per_block=1, optimizer=REALQ_OPT_ADAM, beta1=0.9, beta2=0.
     return BgdCfg(steps_per_block, optimizer, lr, beta1, beta2, eps, b_global_start, B_total)
 
 
-_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 _lib = None
 _vp, _i64, _sz, _int, _f32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_size_t, ctypes.c_int, ctypes.c_float
 _f64 = ctypes.c_double
@@ -231,8 +230,11 @@ def _dtype(t: torch.Tensor) -> int:
 
 
 def _stream(stream) -> int:
-    # the current stream's handle without the Stream object around it, which takes longer to make than a small kernel
-    return _raw_stream(_current_device()) if stream is None else stream.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    # the current stream's handle without the Stream object around it, which takes longer to make than a small
+    # kernel (looked up here, not at import: a torch without CUDA lacks both)
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _need(t, dtype, shape, name):

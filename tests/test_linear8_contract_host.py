@@ -38,3 +38,15 @@ def test_kernels_read_what_the_kernel_before_writes_with_ordinary_loads(source):
         for arg in re.findall(r"__ldg\(([^;]*?)\)", body):
             assert not names & set(re.findall(r"\w+", arg)), (name, arg)
     assert found == 1
+
+
+def test_the_package_imports_with_a_torch_without_cuda():
+    """Workspace sizes and refusals need the library, not torch's CUDA bindings."""
+    code = ("import torch\n"
+            "for name in ('_cuda_getCurrentRawStream', '_cuda_getDevice'):\n"
+            "    if hasattr(torch._C, name): delattr(torch._C, name)\n"
+            "import paper_2609_00049_gb300 as rq\n"
+            "from paper_2609_00049_gb300 import block, build, head, layer\n"
+            "build.build()\n"
+            "assert rq.realq_int8_product_workspace_size(8, 8, 8) > 0\n")
+    subprocess.run([sys.executable, "-c", code], cwd=ROOT, check=True)
