@@ -34,6 +34,7 @@
 #include <algorithm>
 
 #include "bytes.cuh"
+#include "code_sums.cuh"
 #include "kernels.cuh"
 
 namespace cg = cooperative_groups;
@@ -114,7 +115,7 @@ template <int WB, int NT, int RT> struct Sums {
     // steps between flushes: 8 bits, 64 codes of at most 255 x 128 each; 4 bits, 128 codes of 15 x 128
     static constexpr int FLUSH = WB == 8 ? 8 : 64;
     float acc[RT][NT][4] = {}, xacc[NT][4] = {};
-    int sum[RT][NT][4] = {};
+    uint32_t sum[RT][NT][4] = {};   // modulo 2^32
     int since = 0;
 
     __device__ __forceinline__ void flush() {
@@ -124,7 +125,7 @@ template <int WB, int NT, int RT> struct Sums {
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    sum[r][t][e] += __float2int_rn(acc[r][t][e] * 16777216.f);
+                    sum[r][t][e] = add_share(sum[r][t][e], __float2int_rn(acc[r][t][e] * 16777216.f));
                     acc[r][t][e] = 0.f;
                 }
         since = 0;
@@ -182,8 +183,8 @@ __global__ void __launch_bounds__(SW * 32, 2)
     using R = Ring<WB, NT, RT>;
     constexpr int XP = S::XP, ROWS = RT * 16, TOK = NT * 8, OUT = ROWS * TOK;
     extern __shared__ __align__(16) uint8_t ring[];
-    __shared__ int red[SW * OUT];
-    __shared__ int xred[SW * TOK];
+    __shared__ uint32_t red[SW * OUT];
+    __shared__ uint32_t xred[SW * TOK];
     const int64_t tok0 = (int64_t)blockIdx.y * TOK;   // this CTA's group of tokens
     T -= tok0;
     X += tok0 * n;
@@ -330,14 +331,15 @@ __global__ void __launch_bounds__(SW * 32, 2)
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) xred[warp * TOK + t * 8 + 2 * q + e] = __float2int_rn(sums.xacc[t][e]);
+                for (int e = 0; e < 2; ++e)
+                    xred[warp * TOK + t * 8 + 2 * q + e] = (uint32_t)__float2int_rn(sums.xacc[t][e]);
         }
         __syncthreads();
-        // the warps' shares, then the cluster's; integers, so any order is the same
+        // the warps' shares, then the cluster's; modulo 2^32, so any order is the same
         for (int k = threadIdx.x; k < OUT + TOK; k += SW * 32) {
-            int *p = k < OUT ? red + k : xred + k - OUT;
+            uint32_t *p = k < OUT ? red + k : xred + k - OUT;
             const int step = k < OUT ? OUT : TOK;
-            int a = p[0];
+            uint32_t a = p[0];
 #pragma unroll
             for (int w = 1; w < SW; ++w) a += p[w * step];
             p[0] = a;
@@ -346,8 +348,8 @@ __global__ void __launch_bounds__(SW * 32, 2)
             cluster.sync();
             if (rank == 0) {
                 for (int k = threadIdx.x; k < OUT + TOK; k += SW * 32) {
-                    int *p = k < OUT ? red + k : xred + k - OUT;
-                    int a = p[0];
+                    uint32_t *p = k < OUT ? red + k : xred + k - OUT;
+                    uint32_t a = p[0];
                     for (int c = 1; c < CL; ++c) a += *cluster.map_shared_rank(p, c);
                     p[0] = a;
                 }
@@ -361,11 +363,7 @@ __global__ void __launch_bounds__(SW * 32, 2)
                 const int64_t i = tile * ROWS + k % ROWS, t = k / ROWS;
                 if (i < m && t < T) {
                     const int z = w_zero ? w_zero[i] : (WB == 8 ? 128 : 8);
-                    // The sum about the middle code fits 32 bits (its two parts need not: mod 2^32); the zero
-                    // point's distance from it may take the rest past them.
-                    constexpr int MID = WB == 8 ? 128 : 8;
-                    const int xsum = xred[k / ROWS], about = (int)((uint32_t)red[k] - (uint32_t)MID * (uint32_t)xsum);
-                    const int64_t v = about + (int64_t)(MID - z) * xsum;
+                    const int64_t v = centred_sum(red[k], (int32_t)xred[k / ROWS], WB == 8 ? 128 : 8, z);
                     store1(Y + t * m + i, (float)v * __ldg(x_scale + t) * __ldg(w_scale + i));
                 }
             }

@@ -13,7 +13,7 @@ CSRC = os.path.join(ROOT, "paper_2609_00049_gb300", "csrc")
 
 def kernels(path):
     """(name, parameters, body) of each kernel of a source file."""
-    text = re.sub(r"//[^\n]*", "", open(path).read())
+    text = re.sub(r"//[^\n]*|__launch_bounds__\([^)]*\)", "", open(path).read())
     for m in re.finditer(r"__global__\s+void[^{;]*?(\w+)\(([^{;]*?)\)\s*\{", text):
         depth, at = 1, m.end()
         while depth:
@@ -50,3 +50,34 @@ def test_the_package_imports_with_a_torch_without_cuda():
             "build.build()\n"
             "assert rq.realq_int8_product_workspace_size(8, 8, 8) > 0\n")
     subprocess.run([sys.executable, "-c", code], cwd=ROOT, check=True)
+
+
+# (raw sum, sum of x, middle code, zero point) of n equal columns x, c
+LONGEST = [(131071, x, c, z, 128) for x in (-128, 127) for c in (0, 255) for z in (0, 128, 255)] + \
+          [(131071, x, c, z, 8) for x in (-128, 127) for c in (0, 15) for z in (0, 15, 255)]
+
+
+def test_integer_sums_stay_within_defined_arithmetic(tmp_path):
+    """The whole-number arithmetic of the longest sums, evaluated by the compiler,
+    which refuses a signed overflow in a constant; the plain signed form of the
+    same sums is refused."""
+    lines = ['#include "code_sums.cuh"', "using namespace realq;",
+             "constexpr uint32_t raw(int n, int x, int c) { uint32_t a = 0;"
+             " for (int j = 0; j < 8; ++j) a = add_share(a, (n / 8) * x * c);"
+             " return add_share(a, (n % 8) * x * c); }"]
+    for n, x, c, z, mid in LONGEST:
+        lines.append(f"static_assert(centred_sum(raw({n}, {x}, {c}), {n * x}, {mid}, {z}) == {n * x * (c - z)}ll);")
+    # shares as the warps have them add up past 32 bits
+    signed = ("constexpr int32_t plain(int n, int x, int c) { int32_t a = 0;"
+              " for (int j = 0; j < 8; ++j) a += (n / 8) * x * c; return a; }\n"
+              "static_assert(plain(131071, -128, 255) != 1);")
+
+    def compiles(text):
+        f = tmp_path / "sums.cpp"
+        f.write_text(text + "\n")
+        return subprocess.run(["g++", "-std=c++17", "-fsyntax-only", f"-I{CSRC}", str(f)], capture_output=True).returncode == 0
+
+    assert not compiles("\n".join(lines + [signed]))
+    assert compiles("\n".join(lines))
+    kernel = dict((n, b) for n, _, b in kernels(os.path.join(CSRC, "int8_product.cu")))["int8_stream_kernel"]
+    assert not re.search(r"\bint\s+(\*?\s*)?(red|xred)\b", kernel) and "centred_sum(" in kernel
