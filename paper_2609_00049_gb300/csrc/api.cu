@@ -114,6 +114,11 @@ realq_status_t check_ws(void *ws, size_t have, size_t need, const char *who) {
 
 bool valid_dtype(realq_dtype_t d) { return d == REALQ_F32 || d == REALQ_BF16; }
 
+// Whether every address is one that an element of `size` bytes can have (NULL is)
+template <class... P> bool aligned_to(uintptr_t size, const P *...p) {
+    return ((reinterpret_cast<uintptr_t>(p) | ...) & (size - 1)) == 0;
+}
+
 realq_status_t check_qcfg(const realq_quant_cfg_t *q, int64_t n) {
     if (!q) return fail(REALQ_ERR_INVALID_ARG, "qcfg is NULL");
     if (q->bits < 2 || q->bits > 4) return fail(REALQ_ERR_INVALID_ARG, "bits must be in [2, 4] (got %d)", q->bits);
@@ -370,6 +375,7 @@ realq_status_t realq_int8_product(realq_stream_t stream, int64_t T, int64_t n, i
     if (!X_codes || !x_scale || !W_codes || !w_scale || !Y) return fail(REALQ_ERR_INVALID_ARG, "int8_product: NULL argument");
     if (reinterpret_cast<uintptr_t>(Y) % (y_dtype == REALQ_BF16 ? 2 : 4))
         return fail(REALQ_ERR_INVALID_ARG, "int8_product: Y is not aligned to its type");
+    if (!aligned_to(4, x_scale, w_scale)) return fail(REALQ_ERR_INVALID_ARG, "int8_product: scales not aligned to their type");
     if (n > REALQ_INT8_PRODUCT_MAX_N || m >= (1ll << 30) || T >= (1ll << 30) || T * m > (1ll << 40))
         return fail(REALQ_ERR_UNSUPPORTED, "int8_product: n at most %d, m and T below 2^30, T m at most 2^40",
                     REALQ_INT8_PRODUCT_MAX_N);
@@ -388,6 +394,8 @@ realq_status_t realq_token_logprobs(realq_stream_t stream, int64_t T, int64_t V,
         return fail(REALQ_ERR_INVALID_ARG, "token_logprobs: NULL logits, targets or top_ids");
     if (reinterpret_cast<uintptr_t>(logits) % (dtype == REALQ_BF16 ? 2 : 4))
         return fail(REALQ_ERR_INVALID_ARG, "token_logprobs: logits not aligned to their type");
+    if (!aligned_to(4, logprob, norm, entropy, top_logprob) || !aligned_to(8, targets, top_ids))
+        return fail(REALQ_ERR_INVALID_ARG, "token_logprobs: targets or an output not aligned to its type");
     if (V > INT32_MAX - 65536 || T > INT32_MAX / 8) return fail(REALQ_ERR_UNSUPPORTED, "token_logprobs: too many rows or columns");
     return token_logprobs(S(stream), T, V, ld, logits, dtype, targets, logprob, norm, entropy, k, top_ids, top_logprob,
                           num_sms());
@@ -409,6 +417,8 @@ realq_status_t realq_token_logprobs_grad(realq_stream_t stream, int64_t T, int64
     const uintptr_t es = dtype == REALQ_BF16 ? 2 : 4;
     if (reinterpret_cast<uintptr_t>(logits) % es || reinterpret_cast<uintptr_t>(d_logits) % es)
         return fail(REALQ_ERR_INVALID_ARG, "token_logprobs_grad: logits not aligned to their type");
+    if (!aligned_to(4, norm, d_logprob, entropy, d_entropy, d_top) || !aligned_to(8, targets, top_ids))
+        return fail(REALQ_ERR_INVALID_ARG, "token_logprobs_grad: an argument is not aligned to its type");
     if (d_logits == logits && ld_d != ld)
         return fail(REALQ_ERR_INVALID_ARG, "token_logprobs_grad: in place, ld_d must be ld");
     if (V > INT32_MAX - 65536 || T > INT32_MAX / ((V + 4095) / 4096))
@@ -450,6 +460,7 @@ realq_status_t realq_checkpoint_weight_grad(realq_stream_t stream, int64_t T, in
     if (m <= 0) return fail(REALQ_ERR_INVALID_ARG, "checkpoint_weight_grad: m > 0 required");
     REALQ_TRY(check_checkpoint("checkpoint_weight_grad", T, n, dY, dy_dtype, codes, exps));
     if (!dW) return fail(REALQ_ERR_INVALID_ARG, "checkpoint_weight_grad: NULL dW");
+    if (!aligned_to(4, dW)) return fail(REALQ_ERR_INVALID_ARG, "checkpoint_weight_grad: dW not aligned to its type");
     if (T == 0) {   // an empty sum
         if (!accumulate) REALQ_CUDA_TRY(cudaMemsetAsync(dW, 0, (size_t)m * n * sizeof(float), S(stream)));
         return REALQ_OK;

@@ -81,3 +81,34 @@ def test_integer_sums_stay_within_defined_arithmetic(tmp_path):
     assert compiles("\n".join(lines))
     kernel = dict((n, b) for n, _, b in kernels(os.path.join(CSRC, "int8_product.cu")))["int8_stream_kernel"]
     assert not re.search(r"\bint\s+(\*?\s*)?(red|xred)\b", kernel) and "centred_sum(" in kernel
+
+
+INVALID = 1
+
+
+def test_side_arrays_off_their_types_alignment_are_refused():
+    """Scales, log probabilities, targets and the other arrays beside the large
+    ones: an address that their element type cannot have comes back as a status."""
+    import ctypes
+    from paper_2609_00049_gb300 import build as b
+    b.build()
+    import paper_2609_00049_gb300 as rq
+    L = rq.lib()
+    ok, odd, odd8 = ctypes.c_void_p(0x10000), ctypes.c_void_p(0x10002), ctypes.c_void_p(0x10004)   # never dereferenced
+
+    def product(xs=ok, ws=ok):
+        return L.realq_int8_product(None, 4, 64, 32, ok, xs, ok, 8, ws, None, ok, 1, ok, 1 << 40)
+    for bad in (dict(xs=odd), dict(ws=odd)):
+        assert product(**bad) == INVALID, bad
+
+    def logprobs(y=ok, lp=ok, norm=ok, H=ok, ids=ok, top=ok):
+        return L.realq_token_logprobs(None, 4, 100, 100, ok, 1, y, lp, norm, H, 2, ids, top)
+    for bad in (dict(y=odd8), dict(ids=odd8), dict(lp=odd), dict(norm=odd), dict(H=odd), dict(top=odd)):
+        assert logprobs(**bad) == INVALID, bad
+
+    def grad(y=ok, norm=ok, g=ok, H=ok, gH=ok, ids=ok, gt=ok):
+        return L.realq_token_logprobs_grad(None, 4, 100, 100, ok, 1, y, norm, g, H, gH, 2, ids, gt, 100, ctypes.c_void_p(0x20000))
+    for bad in (dict(y=odd8), dict(ids=odd8), dict(norm=odd), dict(g=odd), dict(H=odd), dict(gH=odd), dict(gt=odd)):
+        assert grad(**bad) == INVALID, bad
+
+    assert L.realq_checkpoint_weight_grad(None, 4, 8, 64, ok, 1, ok, ok, odd, 0, ok, 1 << 40) == INVALID
