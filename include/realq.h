@@ -242,8 +242,8 @@ realq_status_t realq_quantize_layer_tokens(realq_stream_t stream, int64_t m, int
  *           even column in the low nibble), T x n bytes for bits 5..8.
  *   scale   NULL, or T floats.
  * A token holding an infinity or a NaN gets scale NaN, X_q NaN throughout and
- * codes 2^(bits-1).  bits in [2, 8], 0 < a_clip <= 1.  Asynchronous; allocates
- * nothing. */
+ * codes 2^(bits-1).  bits in [2, 8], 0 < a_clip <= 1.  T = 0 is a no-op.
+ * Asynchronous; allocates nothing. */
 realq_status_t realq_quantize_activations(realq_stream_t stream, int64_t T, int64_t n, const void *X,
                                           realq_dtype_t x_dtype, int bits, float a_clip, void *X_q, uint8_t *codes,
                                           float *scale);

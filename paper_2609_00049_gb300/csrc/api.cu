@@ -351,7 +351,8 @@ realq_status_t realq_hessian_prepare_noalloc(realq_stream_t stream, int64_t n, i
 realq_status_t realq_quantize_activations(realq_stream_t stream, int64_t T, int64_t n, const void *X,
                                           realq_dtype_t x_dtype, int bits, float a_clip, void *X_q, uint8_t *codes,
                                           float *scale) {
-    if (T < 0 || n <= 0 || !X || !X_q) return fail(REALQ_ERR_INVALID_ARG, "quantize_activations: bad argument");
+    if (T < 0 || n <= 0 || (T > 0 && (!X || !X_q)))
+        return fail(REALQ_ERR_INVALID_ARG, "quantize_activations: bad argument");
     if (x_dtype != REALQ_BF16 && x_dtype != REALQ_F32)
         return fail(REALQ_ERR_INVALID_ARG, "quantize_activations: x_dtype must be REALQ_BF16 or REALQ_F32");
     if (bits < 2 || bits > 8) return fail(REALQ_ERR_INVALID_ARG, "quantize_activations: bits must be in [2, 8]");

@@ -114,3 +114,13 @@ def test_a_hidden_state_that_is_not_finite_shows(T, logits, value):
         assert torch.equal(a[rows], b[rows])
     dW = head.weight_grad(step, w)
     assert torch.isnan(dW).all()
+
+
+def test_a_pass_of_no_tokens():
+    head = Head8(torch.randn(300, 64, generator=gen(0), device="cuda"))
+    h, y, w = torch.empty(0, 64, device="cuda"), torch.empty(0, dtype=torch.int64, device="cuda"), torch.empty(0, device="cuda")
+    step = head.forward(h, y, k=2)
+    assert step.logprob.shape == (0,) and step.top_ids.shape == (0, 2) and math.isnan(step.perplexity())
+    dW = torch.ones(300, 64, device="cuda")
+    assert (head.weight_grad(step, w, dW=dW) == 1).all()
+    assert (head.weight_grad(head.forward(h, y), w) == 0).all()

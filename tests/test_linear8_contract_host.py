@@ -112,3 +112,16 @@ def test_side_arrays_off_their_types_alignment_are_refused():
         assert grad(**bad) == INVALID, bad
 
     assert L.realq_checkpoint_weight_grad(None, 4, 8, 64, ok, 1, ok, ok, odd, 0, ok, 1 << 40) == INVALID
+
+
+def test_quantizing_no_tokens_is_no_work():
+    """An empty matrix has no address: T = 0 is a no-op, not a refusal."""
+    import ctypes
+    from paper_2609_00049_gb300 import build as b
+    b.build()
+    import paper_2609_00049_gb300 as rq
+    L, ok = rq.lib(), ctypes.c_void_p(0x10000)
+    assert L.realq_quantize_activations(None, 0, 64, None, 1, 8, 1.0, None, None, None) == 0
+    assert L.realq_quantize_activations(None, 4, 64, None, 1, 8, 1.0, ok, None, None) == INVALID
+    assert L.realq_quantize_activations(None, 4, 64, ok, 1, 8, 1.0, None, None, None) == INVALID
+    assert L.realq_quantize_activations(None, 0, 64, None, 1, 9, 1.0, None, None, None) == INVALID
