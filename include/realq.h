@@ -257,9 +257,15 @@ realq_status_t realq_quantize_activations(realq_stream_t stream, int64_t T, int6
 
 /* realq_int8_product: Y = X̂ Ŵᵀ from the codes of both,
  *   Y[t][i] = x_scale[t] w_scale[i] sum_j (X_codes[t][j] - 128) (w_ij - z_i),
- * the sum a whole number (exact below 2^24 in magnitude; above, accumulated
- * in fp32), times x_scale[t], times w_scale[i] in fp32, rounded once to
- * y_dtype.
+ * the sum a whole number, times x_scale[t], times w_scale[i] in fp32, rounded
+ * once to y_dtype.  Up to 16 tokens (up to 64 where W is small) the sum is
+ * formed exactly, whatever the codes, and rounded once to fp32.  For more
+ * tokens it is accumulated in fp32 on the tensor cores: exact as long as every
+ * sum over consecutive columns, the running ones included, stays below 2^24 in
+ * magnitude (sums of random codes spread as 5461 sqrt(n)); past that each 16
+ * columns may lose 2^-23 of the largest such sum, also where the final sum is
+ * small again.  A token's result may then differ in its last bits with the
+ * number of tokens it is computed with.
  *   X_codes  T x n bytes and x_scale (T floats): the codes and scales of
  *            realq_quantize_activations with bits = 8 (zero point 128).
  *   W_codes  w_bits = 8: m x n bytes (those of realq_quantize_activations on

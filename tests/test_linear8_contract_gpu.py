@@ -87,3 +87,82 @@ def test_a_head_reports_a_pass_that_gave_up():
     with pytest.raises(rq.RealqError):
         head.check()
     head.check()
+
+
+# ------------------------------------------------------------------- sums ---
+def exact_sums(xc, w, z):
+    return (xc.double() - 128) @ (w.double() - z).T
+
+
+def largest_running_sum(xc, w, z, step=16):
+    """The largest magnitude of a sum over consecutive columns, taken 16 columns
+    at a time (their products' magnitudes added for what lies inside a step)."""
+    x, v = xc.double() - 128, w.double() - z
+    lo = hi = total = torch.zeros(x.shape[0], v.shape[0], dtype=torch.float64, device="cuda")
+    inside = torch.zeros_like(lo)
+    for j in range(0, x.shape[1], step):
+        a, b = x[:, j:j + step], v[:, j:j + step]
+        total = total + a @ b.T
+        inside = torch.maximum(inside, a.abs() @ b.abs().T)
+        lo, hi = torch.minimum(lo, total), torch.maximum(hi, total)
+    return hi - lo + 2 * inside
+
+
+def check_sums(T, xc, w, wc, z, w_bits):
+    """With scales of one.  Up to 16 tokens the integer sum is exact and rounded
+    once; above, each 16 columns may lose 2 U of the largest running sum once
+    that passes 2^24 (and the parts of a split sum, at most 16, as much again)."""
+    n, m = xc.shape[1], w.shape[0]
+    Y = torch.empty(T, m, device="cuda")
+    ws = rq.workspace(rq.realq_int8_product_workspace_size(T, n, m, w_bits))
+    zero = torch.full((m,), z, dtype=torch.uint8, device="cuda")
+    rq.realq_int8_product(xc, torch.ones(T, device="cuda"), wc, torch.ones(m, device="cuda"), Y, w_bits=w_bits,
+                          w_zero=zero, ws=ws)
+    rq.realq_workspace_status(ws)
+    N = exact_sums(xc, w, z)
+    if T <= 16:
+        assert torch.equal(Y, N.float())
+    else:
+        run = largest_running_sum(xc, w, z)
+        lost = torch.where(run < 2.0 ** 24, torch.zeros_like(run), 2 * U * (n / 16 + 16) * run)
+        assert ((Y.double() - N).abs() <= lost + U * N.abs()).all()
+
+
+def packed(w):
+    if w.shape[1] % 2:
+        w = torch.cat([w, torch.zeros_like(w[:, :1])], dim=1)
+    return (w[:, 0::2] | (w[:, 1::2] << 4)).contiguous()
+
+
+@pytest.mark.parametrize("T", [1, 16, 17, 40, 200, 300])
+@pytest.mark.parametrize("n", [4096, 8192, 20001])
+def test_sums_that_cancel_past_2_24(T, n):
+    """The first half of the columns adds up to far more than 2^24, the second
+    half takes it away again but for a few units."""
+    m = 70
+    xc = torch.full((T, n), 255, dtype=torch.uint8, device="cuda")
+    xc[:, n // 2:] = 1
+    w = torch.full((m, n), 255, dtype=torch.uint8, device="cuda")
+    w[:, : m] -= torch.eye(m, dtype=torch.uint8, device="cuda") * 7
+    check_sums(T, xc, w, w, 0, 8)
+
+
+@pytest.mark.parametrize("T", [1, 8, 16, 20, 150])
+@pytest.mark.parametrize("n", [131071, 131040])
+@pytest.mark.parametrize("x,c,z", [(255, 15, 0), (0, 15, 0), (0, 0, 15), (255, 0, 15)])
+def test_longest_sums_of_4_bit_codes(T, n, x, c, z):
+    m = 40
+    xc = torch.full((T, n), x, dtype=torch.uint8, device="cuda")
+    w = torch.full((m, n), c, dtype=torch.uint8, device="cuda")
+    check_sums(T, xc, w, packed(w), z, 4)
+
+
+@pytest.mark.parametrize("T", [1, 9, 40, 300])
+@pytest.mark.parametrize("n", [96, 1003])
+@pytest.mark.parametrize("z", [16, 100, 255])
+def test_4_bit_zero_points_beyond_the_codes(T, n, z):
+    """A zero point is a byte, whatever the width of the codes."""
+    m = 130
+    xc = torch.randint(0, 256, (T, n), generator=gen(n), device="cuda").to(torch.uint8)
+    w = torch.randint(0, 16, (m, n), generator=gen(z), device="cuda").to(torch.uint8)
+    check_sums(T, xc, w, packed(w), z, 4)
