@@ -27,6 +27,13 @@ __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float
 __device__ __forceinline__ void store(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 
+// the larger one, NaN if either is (fmaxf drops a NaN)
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+    return m;
+}
+
 template <typename TX>
 __global__ void __launch_bounds__(256) act_quant_kernel(int64_t T, int64_t n, const TX *X, TX *Xq, uint8_t *codes,
                                                         float *scale_out, int bits, float a_clip) {
@@ -34,18 +41,18 @@ __global__ void __launch_bounds__(256) act_quant_kernel(int64_t T, int64_t n, co
     const int64_t t = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
     if (t >= T) return;
     const TX *x = X + t * n;
-    // the bits of |x| are ordered like the magnitudes, infinities and NaN above all numbers (fmaxf would drop a NaN)
-    uint32_t top = 0;
-    for (int64_t c = lane; c < n; c += 32) top = max(top, __float_as_uint(to_f(x[c])) & 0x7FFFFFFFu);
+    float amax = 0.f;
+    for (int64_t c = lane; c < n; c += 32) amax = max_nan(amax, fabsf(to_f(x[c])));
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(FULL, top, o));
-    const bool finite = top < 0x7F800000u;
-    const float amax = __uint_as_float(top);
+    for (int o = 16; o > 0; o >>= 1) amax = max_nan(amax, __shfl_xor_sync(FULL, amax, o));
+    const bool finite = amax < __uint_as_float(0x7F800000u);
     const int maxq = (1 << bits) - 1, zero = 1 << (bits - 1);
     float xmax = __fmul_rn(a_clip, amax);
     if (xmax == 0.f) xmax = 1.f;
     const float scale = finite ? __fdiv_rn(__fadd_rn(xmax, xmax), (float)maxq) : __uint_as_float(0x7FC00000u);
     if (lane == 0 && scale_out) scale_out[t] = scale;
+    // the clamp's ends, one beyond the codes; both zero in a row without a grid
+    const float lo = finite ? (float)(-zero - 1) : 0.f, hi = finite ? (float)(maxq - zero + 1) : 0.f;
     TX *xq = Xq + t * n;
     const bool packed = bits <= 4;
     const int64_t ldc = packed ? (n + 1) / 2 : n;
@@ -54,8 +61,8 @@ __global__ void __launch_bounds__(256) act_quant_kernel(int64_t T, int64_t n, co
         int q = 0;
         if (c < n) {
             float r = rintf(__fdiv_rn(to_f(x[c]), scale));
-            r = fminf(fmaxf(r, (float)(-zero - 1)), (float)(maxq - zero + 1));
-            q = finite ? min(max((int)r + zero, 0), maxq) : zero;
+            r = fminf(fmaxf(r, lo), hi);
+            q = min(max((int)r + zero, 0), maxq);
             store(xq + c, __fmul_rn(scale, (float)(q - zero)));
         }
         if (codes) {
