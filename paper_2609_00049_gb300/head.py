@@ -29,7 +29,7 @@ import torch
 
 from . import (realq_checkpoint_pack, realq_checkpoint_weight_grad, realq_checkpoint_weight_grad_workspace_size,
                realq_int8_product, realq_int8_product_workspace_size, realq_quantize_activations,
-               realq_token_logprobs, realq_token_logprobs_grad, realq_workspace_status, workspace)
+               realq_token_logprobs, realq_token_logprobs_grad, realq_workspace_status, workspace, _stream)
 
 
 @dataclass
@@ -44,18 +44,23 @@ class HeadStep:
     targets: torch.Tensor
     codes: torch.Tensor                   # the hidden states' checkpoint
     exps: torch.Tensor
-    done: Optional[torch.cuda.Event] = None   # the pass has run
+    stream: Optional[torch.cuda.Stream] = None   # the pass's
     head: Optional["Head8"] = None
 
     def perplexity(self) -> float:
         """exp of minus the mean log probability of the scored tokens (synchronizes).
         Raises RealqError if a pass of the head since its last check gave up."""
-        if self.done is not None:
-            torch.cuda.current_stream(self.logprob.device).wait_event(self.done)
+        if self.stream is not None:
+            current = torch.cuda.current_stream(self.logprob.device)
+            if current != self.stream:
+                current.wait_stream(self.stream)
         if self.head is not None:
             self.head.check()
         scored = self.targets >= 0
         return float(torch.exp(-self.logprob[scored].double().mean()))
+
+
+_HERE = contextlib.nullcontext()
 
 
 def _used_on(stream, *tensors: Optional[torch.Tensor]) -> None:
@@ -82,63 +87,67 @@ class Head8:
         self.scale = torch.empty(self.vocab, dtype=torch.float32, device=W.device)
         realq_quantize_activations(W, 8, 1.0, codes=self.codes, scale=self.scale)   # a row's symmetric 8-bit grid
         self._ws = {}
-        self._last = torch.cuda.current_stream(W.device).record_event()   # the head's codes, then its latest pass
+        self._stream = torch.cuda.current_stream(W.device)   # the latest pass's
+        self._handle = self._stream.cuda_stream
 
-    def _workspace(self, key: str, nbytes: int, stream, device) -> Optional[torch.Tensor]:
+    def _workspace(self, key: str, nbytes: int, device) -> Optional[torch.Tensor]:
         have = self._ws.get(key)
         if have is None or have.numel() < nbytes:
             new = workspace(nbytes, device)
             if have is not None:
                 new[:4].copy_(have[:4])   # the status word
             self._ws[key] = have = new
-        _used_on(stream, have)
         return have
 
-    @contextlib.contextmanager
-    def _pass(self, stream):
-        """A pass on `stream` (None: the current one), which becomes the current
-        one: allocations belong to it.  It starts after the caller's work and the
-        head's latest pass.  Yields it and the caller's stream."""
+    def _begin(self, stream):
+        """A pass on `stream` (None: the current one) begins: after the caller's
+        work and the head's latest pass.  The stream for the pass's operators, and
+        the caller's where that is another (the pass is then run with its own
+        current, so that allocations belong to it)."""
+        handle = _stream(stream)
+        if handle == self._handle and (stream is None or handle == _stream(None)):
+            return stream, None   # (nothing to order; making stream objects would take as long as a small kernel)
         caller = torch.cuda.current_stream(self.codes.device)
         s = caller if stream is None else stream
-        if s != caller:
-            s.wait_stream(caller)
-        s.wait_event(self._last)
-        with torch.cuda.stream(s):
-            _used_on(s, self.codes, self.scale)
-            try:
-                yield s, caller
-            finally:   # (a refused call may follow launched ones)
-                self._last = s.record_event()
+        if handle != self._handle:
+            s.wait_stream(self._stream)
+            _used_on(s, self.codes, self.scale, *self._ws.values())
+            self._stream, self._handle = s, handle
+        if s == caller:
+            return s, None
+        s.wait_stream(caller)
+        return s, caller
 
     def check(self) -> None:
         """Raises RealqError if a bounded wait gave up in a pass since the last
         check, whose results then hold NaN (synchronizes)."""
-        with self._pass(None) as (s, _):
-            for ws in self._ws.values():
-                if ws is not None:
-                    _used_on(s, ws)
-                    realq_workspace_status(ws, stream=s)
+        s, _ = self._begin(None)
+        for ws in self._ws.values():
+            if ws is not None:
+                realq_workspace_status(ws, stream=s)
 
     def forward(self, h: torch.Tensor, targets: torch.Tensor, k: int = 0, stream=None) -> HeadStep:
         """Score the next tokens (negative targets are not scored) with the k
         likeliest alternatives of each position."""
         T, dev = h.shape[0], h.device
         new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=dev)  # noqa: E731
-        with self._pass(stream) as (s, caller):
-            _used_on(s, h, targets)
+        s, caller = self._begin(stream)
+        with _HERE if caller is None else torch.cuda.stream(s):
+            if caller is not None:
+                _used_on(s, h, targets)
             xc, xs = new(T, self.d, dtype=torch.uint8), new(T)
             realq_quantize_activations(h, 8, 1.0, codes=xc, scale=xs, stream=s)
             logits = new(T, self.vocab, dtype=self.logits_dtype)
-            ws = self._workspace("product", realq_int8_product_workspace_size(T, self.d, self.vocab), s, dev)
+            ws = self._workspace("product", realq_int8_product_workspace_size(T, self.d, self.vocab), dev)
             realq_int8_product(xc, xs, self.codes, self.scale, logits, ws=ws, stream=s)
             out = dict(logprob=new(T), norm=new(T, 2), entropy=new(T),
                        top_ids=new(T, k, dtype=torch.int64) if k else None, top_logprob=new(T, k) if k else None)
             realq_token_logprobs(logits, targets, **out, stream=s)
             codes, exps = new(T, self.d, dtype=torch.int8), new(T, (self.d + 31) // 32, dtype=torch.uint8)
             realq_checkpoint_pack(h, codes, exps, stream=s)
-            _used_on(caller, logits, codes, exps, *out.values())
-        return HeadStep(**out, logits=logits, targets=targets, codes=codes, exps=exps, done=self._last, head=self)
+            if caller is not None:
+                _used_on(caller, logits, codes, exps, *out.values())
+        return HeadStep(**out, logits=logits, targets=targets, codes=codes, exps=exps, stream=self._stream, head=self)
 
     def weight_grad(self, step: HeadStep, d_logprob: torch.Tensor, d_entropy: Optional[torch.Tensor] = None,
                     dW: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
@@ -155,16 +164,21 @@ class Head8:
                 raise ValueError(f"{name}: expected a contiguous float32 tensor of shape {shape} on {dev}, got "
                                  f"{t.dtype} {tuple(t.shape)} on {t.device}")
         d_logits, step.logits = step.logits, None
-        with self._pass(stream) as (s, caller):
-            _used_on(s, d_logits, step.targets, step.norm, step.entropy, step.codes, step.exps, d_logprob, d_entropy, dW)
+        s, caller = self._begin(stream)
+        with _HERE if caller is None else torch.cuda.stream(s):
+            if caller is not None:
+                _used_on(s, step.targets, d_logprob, d_entropy, dW)
+            if self._stream is not step.stream:
+                _used_on(self._stream, d_logits, step.targets, step.norm, step.entropy, step.codes, step.exps)
             realq_token_logprobs_grad(d_logits, step.targets, step.norm, d_logits, d_logprob=d_logprob,
                                       entropy=step.entropy if d_entropy is not None else None, d_entropy=d_entropy,
                                       stream=s)
             accumulate = dW is not None
             if dW is None:
                 dW = torch.empty((self.vocab, self.d), dtype=torch.float32, device=dev)
-                _used_on(caller, dW)
+                if caller is not None:
+                    _used_on(caller, dW)
             ws = self._workspace("grad", realq_checkpoint_weight_grad_workspace_size(T, self.vocab, self.d,
-                                                                                     d_logits.dtype), s, dev)
+                                                                                     d_logits.dtype), dev)
             return realq_checkpoint_weight_grad(d_logits, step.codes, step.exps, dW, accumulate=accumulate, ws=ws,
                                                 stream=s)

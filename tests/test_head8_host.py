@@ -18,7 +18,7 @@ class FakeEvent:
 
 class FakeStream:
     def __init__(self, name, log):
-        self.name, self.log = name, log
+        self.name, self.log, self.cuda_stream = name, log, hash(name)
 
     def wait_stream(self, other):
         self.log.append(("wait_stream", self.name, other.name))
@@ -50,6 +50,7 @@ def world(monkeypatch):
     monkeypatch.setattr(torch.cuda, "stream", on)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: current[-1])
     monkeypatch.setattr(torch.cuda, "Event", FakeEvent)
+    monkeypatch.setattr(head_module, "_stream", lambda s: (s or current[-1]).cuda_stream, raising=False)
     monkeypatch.setattr(torch.Tensor, "record_stream",
                         lambda t, s: log.append(("record", id(t), s.name)), raising=False)
     keep = []   # tensors stay alive, so that an id names one of them
@@ -84,6 +85,16 @@ def world(monkeypatch):
     return main, side, log
 
 
+def kept(log, t, stream):
+    """The allocator does not hand t's memory on while `stream` may use it: it
+    belongs to that stream or its use there has been recorded."""
+    return ("alloc", id(t), stream) in log or ("record", id(t), stream) in log
+
+
+def waits(log, stream, other):
+    return ("wait_stream", stream, other) in log or ("wait_event", stream, other) in log
+
+
 def results(step):
     return [step.logprob, step.entropy, step.top_ids, step.top_logprob, step.logits, step.norm, step.codes, step.exps]
 
@@ -100,23 +111,23 @@ def test_a_head_on_another_stream_is_ordered_and_keeps_its_memory(world):
     step = head.forward(h, y, k=2, stream=side)
     done = len(log)
     first = next(i for i in range(built, done) if log[i][0] in ("op", "alloc"))
-    assert ("wait_stream", "side", "main") in log[built:first]
+    assert waits(log[built:first], "side", "main")
     assert {e[2] for e in log[built:done] if e[0] == "op"} == {"side"}
     assert {e[2] for e in log[built:done] if e[0] == "alloc"} == {"side"}
-    for t in (h, y, head.codes, head.scale):
-        assert ("record", id(t), "side") in log[built:done]
+    for t in (h, y, head.codes, head.scale, head._ws["product"]):
+        assert kept(log[built:done], t, "side")
     for t in results(step):
-        assert ("record", id(t), "main") in log[built:done]
+        assert kept(log[built:done], t, "main")
 
     logits = step.logits
     dW = head.weight_grad(step, g, stream=side)
     assert {e[2] for e in log[done:] if e[0] == "op"} == {"side"}
     assert {e[2] for e in log[done:] if e[0] == "alloc"} == {"side"}
     first = next(i for i in range(done, len(log)) if log[i][0] in ("op", "alloc"))
-    assert ("wait_stream", "side", "main") in log[done:first]
-    for t in (g, y, logits, step.norm, step.codes, step.exps):
-        assert ("record", id(t), "side") in log[done:]
-    assert ("record", id(dW), "main") in log[done:]
+    assert waits(log[done:first], "side", "main")
+    for t in (g, y, logits, step.norm, step.codes, step.exps, head._ws["grad"]):
+        assert kept(log, t, "side")
+    assert kept(log[done:], dW, "main")
 
 
 def test_a_head_used_on_two_streams_orders_its_workspaces(world):
@@ -126,16 +137,19 @@ def test_a_head_used_on_two_streams_orders_its_workspaces(world):
     head = head_module.Head8(torch.zeros(12, 8))
     head.forward(torch.zeros(2, 8), torch.zeros(2, dtype=torch.int64), stream=side)
     old, at = head._ws["product"], len(log)
-    assert ("record", id(old), "side") in log
+    assert kept(log, old, "side")
     step = head.forward(torch.zeros(9, 8), torch.zeros(9, dtype=torch.int64))   # larger: the workspace is replaced
     first = next(i for i in range(at, len(log)) if log[i][0] == "op")
-    assert ("wait_event", "main", "side") in log[at:first]
-    assert head._ws["product"] is not old
+    assert waits(log[at:first], "main", "side")
+    assert head._ws["product"] is not old and kept(log, old, "main")
     assert {e[2] for e in log[at:] if e[0] == "op"} == {"main"}
     at = len(log)
+    logits = step.logits
     head.weight_grad(step, torch.zeros(9), stream=side)
     first = next(i for i in range(at, len(log)) if log[i][0] == "op")
-    assert ("wait_event", "side", "main") in log[at:first]
+    assert waits(log[at:first], "side", "main")
+    for t in (logits, step.norm, step.codes, step.exps):   # (the forward pass was on main)
+        assert kept(log, t, "side")
 
 
 def test_perplexity_waits_for_the_pass(world):
@@ -144,7 +158,7 @@ def test_perplexity_waits_for_the_pass(world):
     step = head.forward(torch.zeros(4, 8), torch.zeros(4, dtype=torch.int64), stream=side)
     at = len(log)
     step.perplexity()
-    assert ("wait_event", "main", "side") in log[at:]
+    assert waits(log[at:], "main", "side")
 
 
 def test_a_refused_backward_pass_keeps_the_logits():
@@ -152,7 +166,7 @@ def test_a_refused_backward_pass_keeps_the_logits():
     logits: it can be called again with the right ones."""
     head = head_module.Head8.__new__(head_module.Head8)   # (no GPU: the fields that the checks read)
     head.vocab, head.d = 12, 8
-    head.codes, head.scale = torch.zeros(12, 8, dtype=torch.uint8), torch.zeros(12)
+    head.codes, head.scale, head._handle = torch.zeros(12, 8, dtype=torch.uint8), torch.zeros(12), 0
     logits, f = torch.zeros(4, 12), torch.zeros(4)
     step = head_module.HeadStep(f, f, None, None, logits, torch.zeros(4, 2), torch.zeros(4, dtype=torch.int64),
                                 torch.zeros(4, 8, dtype=torch.int8), torch.zeros(4, 1, dtype=torch.uint8))
@@ -163,3 +177,11 @@ def test_a_refused_backward_pass_keeps_the_logits():
         with pytest.raises(ValueError):
             head.weight_grad(step, **bad)
         assert step.logits is logits
+
+
+def test_passes_on_the_callers_own_stream_add_no_waits(world):
+    main, side, log = world
+    head = head_module.Head8(torch.zeros(12, 8))
+    step = head.forward(torch.zeros(4, 8), torch.zeros(4, dtype=torch.int64), k=2)
+    head.weight_grad(step, torch.zeros(4), stream=main)
+    assert {e[0] for e in log} == {"alloc", "op"}
