@@ -280,7 +280,9 @@ realq_status_t realq_quantize_activations(realq_stream_t stream, int64_t T, int6
  *            call since the last reading left NaN in Y where a bounded wait
  *            gave up).  Zero that word before a workspace's first use; calls
  *            only add to it.
- * Any alignment of the codes.  n at most REALQ_INT8_PRODUCT_MAX_N, T and m
+ * Any alignment of the codes (W in rows of whole 16-byte pieces at an address
+ * that is no multiple of 16 is read once for every 16 tokens: align it where
+ * there are many).  n at most REALQ_INT8_PRODUCT_MAX_N, T and m
  * below 2^30, T m at most 2^40.  T = 0 is a no-op.  Asynchronous. */
 #define REALQ_INT8_PRODUCT_MAX_N 131071
 size_t realq_int8_product_workspace_size(int64_t T, int64_t n, int64_t m, int w_bits);

@@ -27,11 +27,13 @@
 // order.  Every wait is bounded; a tile whose wait gave up is written as NaN
 // and the status word gets ST_TIMEOUT.
 //
-// Measured, 8192 tokens x 8192 x 8192 with bf16 dY: 594 us (1.85 PFLOP/s; the
-// tensor pipe 80 % active at 4096 x 4864 x 8192), 36 us for X̂'s plane, which
-// HBM bounds, and 8 for the parts; one CTA per tile took 1.09 ms.  With few tokens the stores of dW
-// bound it (21 x 7936 x 28416: 170 us for 902 MB; 280 us where an odd n puts
-// rows off the 32-byte sectors).
+// Measured, 8192 tokens x 8192 x 8192 with bf16 dY: 596 us alone (1.85 PFLOP/s;
+// the tensor pipe 80 % active at 4096 x 4864 x 8192), 38 us for X̂'s plane, which
+// HBM bounds, and 10 for the parts; a call 632 to 720 us among others, as the
+// power cap has it.  One CTA per tile took 1.09 ms.  With few tokens the stores
+// of dW bound it (21 x 7936 x 28416: 170 us for 902 MB; 217 with bf16 and 329
+// with fp32 dY for 21 x 7834 x 28327, where an odd n puts rows off the 32-byte
+// sectors).  fp32 dY: 1999 x 1024 x 4096 45 us, 4000 x 5000 x 800 122.
 #include "bytes.cuh"
 #include "kernels.cuh"
 #include "tc.cuh"

@@ -25,10 +25,14 @@
 // eight warps of a CTA, and up to eight CTAs of a cluster where channels alone
 // do not fill the SMs evenly, add their shares of K as integers.
 //
-// Measured, 8 tokens x 8192 x 28672: 37.7 us with 8-bit weights (235 MB at 6.2
-// TB/s, 0.92 of the copy rate); 26 us with 4-bit ones (4.5 TB/s: half the bytes
-// but the same conversions and products; the issue slots are 54 % and the ALU
-// pipe 56 % busy, the tensor pipe 39 %).  1 token x 1024 x 2048: 2.5 us, a launch.
+// Measured, 8 tokens x 8192 x 28672, among calls (in a captured graph): 41.7 us
+// (38.1) with 8-bit weights, 235 MB at 5.6 TB/s (6.2, 0.91 of the copy rate);
+// 28.7 us (25.6) with 4-bit ones, 118 MB at 4.1 TB/s (4.6).  With 4 bits no unit
+// is full (issue slots 54 %, ALU pipe 56 %, tensor pipe 39 %, DRAM 0.61 to 0.68
+// of the copy rate): half the bytes take the same conversions and products, of
+// which about a third are the tokens' own, repeated for every channel tile.
+// 1 token x 1024 x 2048: 2.4 us in a graph, a launch.  Unaligned rows, 1 token x
+// 8191 x 28672: 75 us with 8-bit weights, 55 with 4-bit ones (floors 35 and 17).
 #include <cooperative_groups.h>
 
 #include <algorithm>

@@ -37,9 +37,10 @@
 // Every wait is bounded; a tile whose wait gave up is written as NaN and the
 // status word gets ST_TIMEOUT.
 //
-// Measured, 8192 tokens x 8192 x 8192: 540 us alone (2.04 PFLOP/s; the tensor
-// pipe 82 % active at 2048 x 4096 x 9728), 36 us for the tokens' plane and 9 for
-// the parts.  Issued by one lane under a branch, with one ring for codes and
+// Measured, 8192 tokens x 8192 x 8192: 568 us alone (1.94 PFLOP/s; the tensor
+// pipe 82 % active at 2048 x 4096 x 9728), 36 us for the tokens' plane and 10 for
+// the parts; a call 588 to 655 us among others, as the power cap has it, 575 to
+// 602 with 4-bit weights.  Issued by one lane under a branch, with one ring for codes and
 // tokens and the scales fetched while draining, it was 1.04 ms.
 #include "bytes.cuh"
 #include "kernels.cuh"

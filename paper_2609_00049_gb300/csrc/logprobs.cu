@@ -28,10 +28,10 @@
 // All sums are fp32 per thread (a few hundred terms), joined pairwise.
 //
 // Measured, 4096 rows x 128256 in bf16: 181 us with 5 alternatives (5.8 TB/s),
-// 165 without (6.4 TB/s); the rows' ends, where the candidates are ranked, are
+// 168 without (6.3 TB/s); the rows' ends, where the candidates are ranked, are
 // the difference.  Taking the arithmetic's clamp or its packing away does not
 // change it, more CTAs per SM (five or six, 40 to 48 registers) make it slower
-// (208 to 217 us).  The gradient: 313 us (6.7 TB/s).  One row with 20
+// (208 to 217 us).  The gradient: 315 us (6.7 TB/s).  One row with 20
 // alternatives: 9 us, of which the launch and reading it take 4.
 #include <cooperative_groups.h>
 
@@ -610,9 +610,10 @@ __global__ void __launch_bounds__(BT)
 }
 
 // More rows than CTAs of 256 threads fit, and short ones: CTAs of 128, so that
-// twice as many rows are under way (3469 x 4236 in fp32: 18 against 24 us; 4000 x
-// 32000 in bf16: 65 against 70; longer rows are slower so: 2250 x 16774 in fp32
-// 39 against 35).
+// more rows are under way (seven to an SM, by their 28 KB of shared memory and
+// the 1 KB that each CTA takes; registers would let eight).  With 5 alternatives,
+// 128 threads against 256: 3469 x 4236 in fp32 30.7 and 35.1 us, 4000 x 32000 in
+// bf16 61.7 and 65.6; longer rows are slower so: 2250 x 16774 in fp32 48 and 41.
 constexpr int64_t SMALL_ROW = 65536;   // bytes
 
 template <typename TX, int NT>

@@ -1,6 +1,7 @@
 // sm_103a building blocks in inline PTX: mbarriers with bounded waits, 2-D TMA
-// tile loads, TMEM allocation, tcgen05.mma (kind::f16, one CTA) and
-// tcgen05.ld, plus the shared-memory / instruction descriptors they take.
+// tile loads, TMEM allocation, tcgen05.mma (kind::f16, one CTA or a pair of
+// them), tcgen05.ld and st, plus the shared-memory / instruction descriptors
+// they take.
 #pragma once
 
 #include <cuda.h>

@@ -16,7 +16,9 @@ backward pass turns the logits into their gradient in place
 (realq_checkpoint_weight_grad).  The paper evaluates perplexities (Sec. 5) and
 takes its Fisher from the gradient of the token log probabilities at the head
 (App. "Pre-computation of the aggregated Fisher and last-transformer-block
-handling"); it has no 8-bit head.  Buffers are allocated with torch; no
+handling"); it has no 8-bit head.  The logits are kept in bf16
+(logits_dtype), whose rounding a perplexity of more than three digits shows;
+torch.float32 avoids it.  Buffers are allocated with torch; no
 arithmetic happens here beyond the mean of the scored log probabilities.
 """
 from __future__ import annotations
