@@ -75,7 +75,7 @@ def draw(rng):
         S, L = _spread(rng, 1, 128), _spread(rng, 1, 131072)
         new = min(L, rng.choice([1, 1, 1, rng.randint(2, 9), _spread(rng, 10, 8192)]))
         budget = 8192 ** 2 * 32 * 128 // (_SZ[dt] // 2 * S * kv * G * D)  # pairs of a query and a key in each sequence
-        new = min(new, max(1, math.isqrt(budget)))
+        new = min(new, max(1, math.isqrt(budget)), max(1, 2 ** 29 // (S * kv * G * D * _SZ[dt])))
         L = max(1, min(L, 500000 * 8 * 128 // (S * kv * D), budget // new))
         new = min(L, new)
         return {"kind": kind, "S": S, "L": L, "new": new, "H": kv * G, "kv": kv, "D": D, "page": page, "block": block,
