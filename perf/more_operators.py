@@ -231,7 +231,7 @@ def _buffers(s):
         s["out"] = {"out": torch.empty_like(s["q"]), "lse": torch.empty(s["q"].shape[:2], device="cuda")}
         s["ws"] = rq.workspace(rq.realq_kv_attention_workspace_size(s["handle"], c["S"], s["q"].shape[0], c["H"]))
     else:
-        s["ws"] = rq.workspace(rq.realq_pages_workspace_size(c["pages"], c["S"]))
+        s["ws"] = rq.workspace(rq.realq_pages_workspace_size(c["pages"], *s["tables"].shape))
         s["pages"] = rq.kv_pages(s["used"], s["tables"], s["lengths"])
         if kind == "fork":
             s["positions"] = torch.empty(s["rows"].numel(), dtype=torch.int64, device="cuda")
