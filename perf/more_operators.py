@@ -290,7 +290,7 @@ def _append(codes, scale, x, rows, positions, tables, page, block):
     old = by_block(scale)
     fresh = torch.zeros_like(old).scatter_reduce_(0, at, (slot % block == 0).float()[:, None].expand_as(at).contiguous(), "amax")
     have = torch.where(fresh > 0, torch.zeros_like(old), old)
-    top = torch.zeros_like(old).scatter_reduce_(0, at, x.abs().amax(dim=2), "amax") / 127.0
+    top = (torch.zeros_like(old).scatter_reduce_(0, at, x.abs().amax(dim=2), "amax").double() / 127.0).float()  # (in 32 bits torch multiplies by 1 / 127)
     touched = torch.zeros_like(old).scatter_(0, at, 1.0) > 0
     now = torch.where(touched, torch.maximum(have, top), old)
     ratio = torch.where(touched & (now > have) & (have > 0), have / now, torch.ones_like(old))
