@@ -64,7 +64,8 @@ typedef enum {
     REALQ_ERR_NONFINITE = 4,   /* NaN/Inf met in the weights during the sweep */
     REALQ_ERR_TIMEOUT = 5,     /* a bounded device-side wait gave up */
     REALQ_ERR_CUDA = 6,        /* a CUDA runtime call or launch failed */
-    REALQ_ERR_UNSUPPORTED = 7  /* valid but not implemented combination */
+    REALQ_ERR_UNSUPPORTED = 7, /* valid but not implemented combination */
+    REALQ_ERR_NO_PAGES = 8     /* a page pool had too few free pages, or a table row too few entries */
 } realq_status_t;
 
 typedef enum { REALQ_F32 = 0, REALQ_BF16 = 1 } realq_dtype_t;
@@ -352,6 +353,191 @@ size_t realq_checkpoint_weight_grad_workspace_size(int64_t T, int64_t m, int64_t
 realq_status_t realq_checkpoint_weight_grad(realq_stream_t stream, int64_t T, int64_t m, int64_t n, const void *dY,
                                             realq_dtype_t dy_dtype, const int8_t *codes, const uint8_t *exps, float *dW,
                                             int accumulate, void *ws, size_t ws_bytes);
+
+/* ---- An 8-bit key/value cache ----
+ * What a quantized model needs to generate: rotary positions, keys and values
+ * kept as 8-bit codes in pages, attention of the newest tokens over them, and
+ * the pages' bookkeeping.  The paper has no counterpart for these; the decoder
+ * block they serve is that of realq_block_forward (grouped-query attention:
+ * query head i reads key/value head i / (n_heads / n_kv)).
+ *
+ * realq_kv_cache_t: the cache of n_layers layers in n_pages pages of page_size
+ * tokens (16, 32, 64, 128 or 256) each.
+ *   k_codes, v_codes  n_layers x n_pages x n_kv x page_size x head_dim bytes,
+ *                     16-byte aligned; head_dim a multiple of 16, at most 256.
+ *   k_scale, v_scale  n_layers x n_pages x n_kv x (page_size / scale_block)
+ *                     floats: one for each scale_block (a power of two, at
+ *                     most page_size) consecutive tokens of a page and head.
+ * A value is scale (code - 128).  A sequence's token at position p lies in
+ * page tables[row][p / page_size] at place p % page_size; page numbers are the
+ * same in every layer.
+ *
+ * realq_kv_pages_t: who holds which pages.
+ *   used     n_pages ints: how many table entries name the page; 0 is free.
+ *   tables   n_rows x max_pages ints: the pages of each row's sequence in
+ *            order, -1 behind them.  All -1 and used all 0 at the start.
+ *   lengths  n_rows ints: tokens of each row's sequence (0: none).
+ *
+ * The operators below read lists (starts, positions, tables, rows) on the
+ * device and check what they read: a sequence whose entries of `starts` are not
+ * in order or lie outside [0, T], a position below zero or beyond the table's
+ * row and a page outside the pool take no part, and nothing outside the buffers
+ * is touched. */
+typedef struct {
+    int64_t n_layers, n_pages, n_kv, page_size, head_dim, scale_block;
+    uint8_t *k_codes, *v_codes;
+    float *k_scale, *v_scale;
+} realq_kv_cache_t;
+typedef struct {
+    int64_t n_pages, n_rows, max_pages;
+    int32_t *used, *tables, *lengths;
+} realq_kv_pages_t;
+
+/* realq_rotary: rotary positions of T tokens' queries and keys in one launch,
+ *   (a, b) -> amplitude (a cos t - b sin t, b cos t + a sin t),
+ *   t = positions[token] inv_freq[i],
+ * for the rot_dim / 2 pairs of a head's first rot_dim values: (x[i],
+ * x[i + rot_dim / 2]), or (x[2 i], x[2 i + 1]) with interleaved != 0.  The
+ * values behind rot_dim are copied.  transpose != 0 turns by -t, which is the
+ * gradient: d x from d out, with the same amplitude.
+ *   positions  T int64, any sign.    inv_freq  rot_dim / 2 finite doubles:
+ *              radians per position (realq_rotary_frequencies).  The angle is
+ *              reduced exactly: a position's error does not grow with it.
+ *   q, k       T x n_q (n_k) x head_dim of dtype, token t's head h at
+ *              t ld + h hs elements; k NULL with n_k = 0.  q_out, k_out
+ *              likewise; an output may be its input (with the same strides),
+ *              else the two do not overlap.
+ * rot_dim even, in [2, head_dim]; head_dim at most 1024; T at most 2^30.  fp32 arithmetic, one
+ * rounding.  T = 0 is a no-op.  Asynchronous; no workspace.
+ *
+ * realq_rotary_frequencies (host arithmetic in double): inv_freq[i] =
+ * base^(-2 i / rot_dim) into rot_dim / 2 doubles (host), scaled for contexts
+ * beyond the original_context tokens a model was trained on:
+ *   REALQ_ROPE_PLAIN   not at all;
+ *   REALQ_ROPE_LINEAR  all divided by factor;
+ *   REALQ_ROPE_BASE    the base raised to base factor^(rot_dim / (rot_dim - 2)),
+ *                      which divides the slowest by factor, the fastest by 1;
+ *   REALQ_ROPE_RAMP    by turns r = original_context f / (2 pi) in the original
+ *                      context: kept where r >= high, divided by factor where
+ *                      r <= low, f (w + (1 - w) / factor) with
+ *                      w = (r - low) / (high - low) between (LLaMA-3.1: factor
+ *                      8, low 1, high 4, 8192 tokens, base 500000). */
+enum { REALQ_ROPE_PLAIN = 0, REALQ_ROPE_LINEAR = 1, REALQ_ROPE_BASE = 2, REALQ_ROPE_RAMP = 3 };
+realq_status_t realq_rotary_frequencies(int64_t rot_dim, double base, int scaling, double factor,
+                                        double original_context, double low, double high, double *inv_freq);
+realq_status_t realq_rotary(realq_stream_t stream, int64_t T, int64_t head_dim, int64_t rot_dim,
+                            const int64_t *positions, const double *inv_freq, int interleaved, float amplitude,
+                            int transpose, realq_dtype_t dtype, int64_t n_q, const void *q, int64_t q_ld, int64_t q_hs,
+                            void *q_out, int64_t qo_ld, int64_t qo_hs, int64_t n_k, const void *k, int64_t k_ld,
+                            int64_t k_hs, void *k_out, int64_t ko_ld, int64_t ko_hs);
+
+/* realq_kv_append: new tokens' keys and values into one layer of the cache.
+ * Sequence s (row s of the tables) has the tokens starts[s] .. starts[s + 1] - 1
+ * of k and v (T x n_kv x head_dim of dtype, head h of token t at t ld + h hs
+ * elements); they go to consecutive positions from positions[starts[s]] on
+ * (nothing is written where that is negative).  For each block of tokens and
+ * head that gets some: with a the largest magnitude of its new values and s0
+ * its scale before (0 where its first token is among the new ones),
+ *   scale = max(s0, a / 127),
+ *   a kept code c becomes rint((c - 128) (s0 / scale)) + 128,
+ *   a new value   x becomes clamp(rint(x / scale), -127, 127) + 128,
+ * with IEEE fp32 operations, ties to even; scale 0 gives codes 128.  A block
+ * that meets an infinity or a NaN gets scale NaN and reads as NaN until its
+ * first token is written again.  Tokens of the block behind the new ones (a
+ * sequence put back to fewer tokens) no longer count.  n_seqs rows; tables has
+ * max_pages entries a row; one page is to be written by one sequence only
+ * (realq_pages_reserve sees to it).  T = 0 is a no-op.  Asynchronous.
+ *
+ * realq_kv_read: the values of tokens starts[s] .. starts[s + 1] - 1 (at
+ * positions[token], in any order) of each sequence into k_out and v_out
+ * (T x n_kv x head_dim, dtype, each may be NULL): the way out of the cache.
+ * A token without a page reads as NaN; tokens outside every sequence are left
+ * as they were. */
+realq_status_t realq_kv_append(realq_stream_t stream, const realq_kv_cache_t *cache, int64_t layer, int64_t n_seqs,
+                               int64_t T, const void *k, int64_t k_ld, int64_t k_hs, const void *v, int64_t v_ld,
+                               int64_t v_hs, realq_dtype_t dtype, const int32_t *starts, const int64_t *positions,
+                               const int32_t *tables, int64_t max_pages);
+realq_status_t realq_kv_read(realq_stream_t stream, const realq_kv_cache_t *cache, int64_t layer, int64_t n_seqs,
+                             int64_t T, const int32_t *starts, const int64_t *positions, const int32_t *tables,
+                             int64_t max_pages, void *k_out, void *v_out, realq_dtype_t dtype);
+
+/* realq_kv_attention: attention of each sequence's newest tokens over its
+ * cached ones.  Sequence s has the query tokens starts[s] .. starts[s + 1] - 1
+ * (m of them) and lengths[s] cached tokens, the queries' own among them: query
+ * i has position p = lengths[s] - m + i.  With k_j, v_j the cached values,
+ *   out[t][h] = sum_j softmax_j(scale q[t][h] . k_j) v_j,
+ * over j <= p when causal != 0 (all j < lengths[s] otherwise), and, with
+ * window > 0 (causal only), over the last `window` of them, j > p - window.
+ *   q    T x n_heads x head_dim of dtype (head h of token t at t q_ld + h q_hs
+ *        elements); n_heads a multiple of n_kv.
+ *   out  T x n_heads x head_dim, dtype.  lse  T x n_heads floats, or NULL:
+ *        the natural log of the softmax's sum.
+ *   max_new   at least every sequence's number of query tokens, for the choice
+ *        of kernels alone (T is always right; results hold whatever it is).
+ *   ws   realq_kv_attention_workspace_size(cache, n_seqs, T, n_heads) bytes,
+ *        256-byte aligned, zeroed before its first use; calls leave it ready
+ *        for the next, whatever its sizes.  Its first word is a status as that
+ *        of realq_int8_product's workspace.  Calls that may run at the same time need a
+ *        workspace each.
+ * A query that sees no token gets zeros and lse -inf.  Tokens that a query does
+ * not see have no influence, whatever the cache holds there.  Rows of q outside
+ * every sequence are left as they were in out and lse.  Scores, sums and
+ * outputs are held in fp32; with bf16 inputs the weights of the values are
+ * rounded to fp16 (2^-12 of each), with fp32 inputs queries and weights are
+ * taken as two fp16 parts each.  The order of summation is fixed by the
+ * lengths and sizes (bitwise repeatable).  T = 0 is a no-op.  Asynchronous. */
+size_t realq_kv_attention_workspace_size(const realq_kv_cache_t *cache, int64_t n_seqs, int64_t T, int64_t n_heads);
+realq_status_t realq_kv_attention(realq_stream_t stream, const realq_kv_cache_t *cache, int64_t layer, int64_t n_seqs,
+                                  int64_t T, int64_t n_heads, const void *q, int64_t q_ld, int64_t q_hs,
+                                  realq_dtype_t dtype, const int32_t *starts, const int32_t *lengths,
+                                  const int32_t *tables, int64_t max_pages, float scale, int causal, int64_t window,
+                                  int64_t max_new, void *out, float *lse, void *ws, size_t ws_bytes);
+
+/* Pages.  Every call is one or two launches on `stream`; nothing is read back.
+ * ws: realq_pages_workspace_size(n_pages, n_rows, max_pages) bytes, 256-byte
+ * aligned, zeroed before its first use; its first word is a status that
+ * realq_workspace_status reads and clears.
+ *
+ * realq_pages_reserve: room for starts[s + 1] - starts[s] more tokens in each
+ * row s (starts: n_rows + 1 ints): lengths grow, table entries are filled with
+ * the lowest-numbered free pages in the order of the rows, and positions (an
+ * int64 for each new token, starts[n_rows] of them, at most T) receives the new
+ * tokens' positions.  Where a row's last page is partly filled and held by
+ * others too, the row first gets a copy of it, in every layer of cache (the
+ * last row of the call may keep the page where all its holders are in the
+ * call): what realq_kv_append writes afterwards is the row's own.  All or
+ * nothing: with too few free pages, entries or positions, or starts out of
+ * order, nothing changes, all T positions become -1 (so that appending does
+ * nothing) and the status becomes REALQ_ERR_NO_PAGES.
+ * realq_pages_fork: row dst[i] takes over the sequence of row src[i], sharing
+ * its pages, for i < n, all at once: sources are the rows as they were before
+ * the call (a beam search's reordering).  What dst[i] held is released.  Of
+ * several entries with the same dst the last counts; entries with a row outside
+ * the table do not.
+ * realq_pages_release: the listed rows give up their pages and become empty
+ * (a row may be listed twice).
+ * realq_pages_compact: moves the used pages' contents, in every layer of cache,
+ * to the front of the pool: with u pages in use, those numbered u or above go
+ * to the free ones below u, both in ascending order.  moved_to[p] (n_pages
+ * ints) is page p's new number, -1 for a free one; used_out and tables_out are
+ * used and tables after it (they may be used and tables).  Pages that were
+ * moved keep their contents until they are written again.
+ * realq_pages_copy: page src[i]'s contents to page dst[i], i < n, in every
+ * layer of cache.  No page is to be both a source and a destination; of several
+ * copies to one page either remains, piece by piece.  No workspace. */
+size_t realq_pages_workspace_size(int64_t n_pages, int64_t n_rows, int64_t max_pages);
+realq_status_t realq_pages_reserve(realq_stream_t stream, const realq_kv_pages_t *pages, const int32_t *starts,
+                                   int64_t T, int64_t *positions, const realq_kv_cache_t *cache, void *ws,
+                                   size_t ws_bytes);
+realq_status_t realq_pages_fork(realq_stream_t stream, const realq_kv_pages_t *pages, int64_t n, const int32_t *src,
+                                const int32_t *dst, void *ws, size_t ws_bytes);
+realq_status_t realq_pages_release(realq_stream_t stream, const realq_kv_pages_t *pages, int64_t n,
+                                   const int32_t *rows);
+realq_status_t realq_pages_compact(realq_stream_t stream, const realq_kv_pages_t *pages, const realq_kv_cache_t *cache,
+                                   int32_t *used_out, int32_t *tables_out, int32_t *moved_to, void *ws,
+                                   size_t ws_bytes);
+realq_status_t realq_pages_copy(realq_stream_t stream, const realq_kv_cache_t *cache, int64_t n, const int32_t *src,
+                                const int32_t *dst);
 
 /* Saliency-weighted Hessians of the coarse stage (Sec. 3.3 Eq.
  * saliency_hessian, used by Alg. 1 for every row group g; N_g = 4 in the

@@ -23,7 +23,10 @@ __all__ = [
     "realq_hessian_prepare_deferred", "realq_prepare_status", "Graph", "realq_graph_begin", "realq_graph_end", "realq_scale_moment", "realq_quantize_layer",
     "realq_quantize_activations", "realq_int8_product_workspace_size", "realq_int8_product", "realq_token_logprobs",
     "realq_token_logprobs_grad", "realq_checkpoint_pack", "realq_checkpoint_unpack",
-    "realq_checkpoint_weight_grad_workspace_size", "realq_checkpoint_weight_grad", "realq_saliency_clip", "realq_hessian_weighted_workspace_size",
+    "realq_checkpoint_weight_grad_workspace_size", "realq_checkpoint_weight_grad", "KvCache", "kv_cache", "KvPages",
+    "kv_pages", "realq_rotary_frequencies", "realq_rotary", "realq_kv_append", "realq_kv_read",
+    "realq_kv_attention_workspace_size", "realq_kv_attention", "realq_pages_workspace_size", "realq_pages_reserve",
+    "realq_pages_fork", "realq_pages_release", "realq_pages_compact", "realq_pages_copy", "realq_saliency_clip", "realq_hessian_weighted_workspace_size",
     "realq_hessian_accumulate_weighted", "realq_hessian_prepare_scaled", "realq_quantize_layer_grouped",
     "realq_quantize_grouped_workspace_size", "realq_quantize_layer_minibatch",
     "realq_quantize_minibatch_workspace_size", "realq_quantize_tokens_workspace_size", "realq_quantize_layer_tokens",
@@ -42,6 +45,7 @@ library_path = os.path.join(_HERE, "_lib", "librealq.so")
 
 REALQ_OK, REALQ_ERR_INVALID_ARG, REALQ_ERR_WORKSPACE, REALQ_ERR_NOT_SPD = 0, 1, 2, 3
 REALQ_ERR_NONFINITE, REALQ_ERR_TIMEOUT, REALQ_ERR_CUDA, REALQ_ERR_UNSUPPORTED = 4, 5, 6, 7
+REALQ_ERR_NO_PAGES = 8
 REALQ_F32, REALQ_BF16 = 0, 1
 REALQ_OPT_ADAM, REALQ_OPT_SGD = 0, 1
 
@@ -74,6 +78,18 @@ class BlockDims(ctypes.Structure):
 
 class BlockWeights(ctypes.Structure):
     _fields_ = [(k, ctypes.c_void_p) for k in ("g1", "Wq", "Wk", "Wv", "Wo", "g2", "Wg", "Wu", "Wd")]
+
+
+class KvCache(ctypes.Structure):
+    """realq_kv_cache_t (kv_cache makes it); `tensors` holds its buffers."""
+    _fields_ = [(k, ctypes.c_int64) for k in ("n_layers", "n_pages", "n_kv", "page_size", "head_dim", "scale_block")] + [
+        (k, ctypes.c_void_p) for k in ("k_codes", "v_codes", "k_scale", "v_scale")]
+
+
+class KvPages(ctypes.Structure):
+    """realq_kv_pages_t (kv_pages makes it); `tensors` holds its buffers."""
+    _fields_ = [(k, ctypes.c_int64) for k in ("n_pages", "n_rows", "max_pages")] + [
+        (k, ctypes.c_void_p) for k in ("used", "tables", "lengths")]
 
 
 class KernelStat(ctypes.Structure):
@@ -117,6 +133,21 @@ _SIGS = {
     "realq_checkpoint_unpack": ([_vp, _i64, _i64, _vp, _vp, _vp, _int], _int),
     "realq_checkpoint_weight_grad_workspace_size": ([_i64, _i64, _i64, _int], _sz),
     "realq_checkpoint_weight_grad": ([_vp, _i64, _i64, _i64, _vp, _int, _vp, _vp, _vp, _int, _vp, _sz], _int),
+    "realq_rotary_frequencies": ([_i64, _f64, _int, _f64, _f64, _f64, _f64, _vp], _int),
+    "realq_rotary": ([_vp, _i64, _i64, _i64, _vp, _vp, _int, _f32, _int, _int] + [_i64, _vp, _i64, _i64, _vp, _i64,
+                                                                               _i64] * 2, _int),
+    "realq_kv_append": ([_vp, _vp, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _int, _vp, _vp, _vp, _i64],
+                        _int),
+    "realq_kv_read": ([_vp, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _i64, _vp, _vp, _int], _int),
+    "realq_kv_attention_workspace_size": ([_vp, _i64, _i64, _i64], _sz),
+    "realq_kv_attention": ([_vp, _vp, _i64, _i64, _i64, _i64, _vp, _i64, _i64, _int, _vp, _vp, _vp, _i64, _f32, _int,
+                            _i64, _i64, _vp, _vp, _vp, _sz], _int),
+    "realq_pages_workspace_size": ([_i64, _i64, _i64], _sz),
+    "realq_pages_reserve": ([_vp, _vp, _vp, _i64, _vp, _vp, _vp, _sz], _int),
+    "realq_pages_fork": ([_vp, _vp, _i64, _vp, _vp, _vp, _sz], _int),
+    "realq_pages_release": ([_vp, _vp, _i64, _vp], _int),
+    "realq_pages_compact": ([_vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz], _int),
+    "realq_pages_copy": ([_vp, _vp, _i64, _vp, _vp], _int),
     "realq_saliency_clip": ([_vp, _i64, _int, _vp, _f64, _vp, _vp], _int),
     "realq_hessian_weighted_workspace_size": ([_i64, _i64], _sz),
     "realq_hessian_accumulate_weighted": ([_vp, _i64, _i64, _vp, _int, _vp, _vp, _vp, _vp, _sz], _int),
@@ -511,6 +542,212 @@ def realq_checkpoint_weight_grad(dY: torch.Tensor, codes: torch.Tensor, exps: to
         _arg(exps, torch.uint8, (T, (n + 31) // 32), "exps"), _arg(dW, torch.float32, (m, n), "dW"),
         int(bool(accumulate)), wp, wb))
     return dW
+
+
+# ------------------------------------------------ 8-bit key/value cache ---
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3}
+
+
+def _ints(t: Optional[torch.Tensor], shape, name: str, device: int, dtype=torch.int32):
+    """Address of a list on the device of the call."""
+    p = _arg(t, dtype, shape, name)
+    if t is not None and t.get_device() != device:
+        raise ValueError(f"{name}: on another device than the cache or the heads")
+    return p
+
+
+def _heads(t: torch.Tensor, name: str, device: int, shape=None):
+    """Address, token stride and head stride of tokens x heads x values, of which
+    the tokens and heads may lie apart."""
+    if t.dim() != 3 or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name}: expected {'tokens x heads x head_dim' if shape is None else tuple(shape)}, got {tuple(t.shape)}")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: expected a CUDA tensor on the device of the other arguments")
+    T, H, D = t.shape
+    if D > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name}: a head's values have to lie together")
+    hs = t.stride(1) if H > 1 else D
+    return t.data_ptr(), (t.stride(0) if T > 1 else H * hs), hs
+
+
+def _on(device: int) -> int:
+    """`device`, which has to be the current one: the library launches there."""
+    if device < 0:
+        raise ValueError("expected CUDA tensors")
+    if device != torch._C._cuda_getDevice():
+        raise ValueError(f"tensors on cuda:{device}, which is not the current device")
+    return device
+
+
+def kv_cache(k_codes: torch.Tensor, v_codes: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor) -> KvCache:
+    """The 8-bit key/value cache in these buffers: codes uint8 n_layers x n_pages x
+    n_kv x page_size x head_dim, scales fp32 n_layers x n_pages x n_kv x
+    (page_size / scale_block).  They stay the caller's and are kept alive."""
+    if k_codes.dim() != 5 or k_scale.dim() != 4 or k_scale.shape[3] == 0 or k_codes.shape[3] % k_scale.shape[3]:
+        raise ValueError("k_codes: layers x pages x kv heads x page_size x head_dim, k_scale: layers x pages x kv heads "
+                         f"x page_size / scale_block expected, got {tuple(k_codes.shape)}, {tuple(k_scale.shape)}")
+    la, n, kv, page, D = k_codes.shape
+    scales = (la, n, kv, k_scale.shape[3])
+    c = KvCache(la, n, kv, page, D, page // k_scale.shape[3], _arg(k_codes, torch.uint8, (la, n, kv, page, D), "k_codes"),
+                _arg(v_codes, torch.uint8, (la, n, kv, page, D), "v_codes"), _arg(k_scale, torch.float32, scales, "k_scale"),
+                _arg(v_scale, torch.float32, scales, "v_scale"))
+    c.device = k_codes.get_device()
+    if any(t.get_device() != c.device for t in (v_codes, k_scale, v_scale)):
+        raise ValueError("the cache's buffers are on different devices")
+    c.tensors = (k_codes, v_codes, k_scale, v_scale)
+    return c
+
+
+def kv_pages(used: torch.Tensor, tables: torch.Tensor, lengths: torch.Tensor) -> KvPages:
+    """The pool's bookkeeping in these int32 buffers: used (n_pages; zeros at the
+    start), tables (n_rows x max_pages; -1), lengths (n_rows; zeros)."""
+    if used.dim() != 1 or tables.dim() != 2:
+        raise ValueError("used: pages, tables: rows x max_pages expected")
+    p = KvPages(used.shape[0], *tables.shape, _arg(used, torch.int32, used.shape, "used"),
+                _arg(tables, torch.int32, tables.shape, "tables"),
+                _arg(lengths, torch.int32, (tables.shape[0],), "lengths"))
+    p.device = used.get_device()
+    if tables.get_device() != p.device or lengths.get_device() != p.device:
+        raise ValueError("the pool's lists are on different devices")
+    p.tensors = (used, tables, lengths)
+    return p
+
+
+def realq_rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
+                             original_context: float = 8192.0, low: float = 1.0, high: float = 4.0) -> torch.Tensor:
+    """Radians per position of rot_dim / 2 pairs (host, float64); scaling "plain",
+    "linear", "base" or "ramp" for contexts beyond the original one."""
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling: one of {', '.join(ROPE_SCALINGS)} expected")
+    f = torch.empty(max(0, rot_dim // 2), dtype=torch.float64)
+    _check(lib().realq_rotary_frequencies(rot_dim, base, ROPE_SCALINGS[scaling], factor, original_context, low, high,
+                                          f.data_ptr()))
+    return f
+
+
+def realq_rotary(q: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, q_out: torch.Tensor,
+                 k: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, interleaved: bool = False,
+                 amplitude: float = 1.0, transpose: bool = False, stream=None) -> None:
+    """Rotary positions of q (tokens x heads x head_dim) and k in one launch, over
+    the first 2 x len(inv_freq) values of each head; outputs may be the inputs.
+    With transpose the gradient: from d q_out, d k_out to d q, d k."""
+    dev = _on(q.get_device())
+    T, H, D = q.shape if q.dim() == 3 else (0, 0, 0)
+    dt = _dtype(q)
+    a = (*_heads(q, "q", dev), *_heads(q_out, "q_out", dev, q.shape))
+    n_k, b = 0, (None, 0, 0, None, 0, 0)
+    if k is not None:
+        if k_out is None or k.dim() != 3 or k.shape[0] != T or k.shape[2] != D:
+            raise ValueError(f"k, k_out: {T} tokens x kv heads x {D} expected")
+        n_k, b = k.shape[1], (*_heads(k, "k", dev), *_heads(k_out, "k_out", dev, k.shape))
+    if any(t is not None and t.dtype != q.dtype for t in (q_out, k, k_out)):
+        raise ValueError("q, k and their outputs have one dtype")
+    _check(lib().realq_rotary(_stream(stream), T, D, 2 * inv_freq.shape[0], _ints(positions, (T,), "positions", dev, torch.int64),
+                              _ints(inv_freq, inv_freq.shape[:1], "inv_freq", dev, torch.float64), interleaved,
+                              amplitude, transpose, dt, H, *a, n_k, *b))
+
+
+def realq_kv_append(cache: KvCache, layer: int, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor,
+                    positions: torch.Tensor, tables: torch.Tensor, stream=None) -> None:
+    """New tokens' keys and values (tokens x n_kv x head_dim) into a layer of the
+    cache: row s of tables has the tokens starts[s] .. starts[s + 1] - 1 (int32),
+    at consecutive positions (int64, one per token)."""
+    dev = _on(cache.device)
+    T, (S, M) = k.shape[0], tables.shape
+    shape = (T, cache.n_kv, cache.head_dim)
+    if v.dtype != k.dtype:
+        raise ValueError("k and v have one dtype")
+    _check(lib().realq_kv_append(_stream(stream), ctypes.byref(cache), layer, S, T, *_heads(k, "k", dev, shape),
+                                 *_heads(v, "v", dev, shape), _dtype(k), _ints(starts, (S + 1,), "starts", dev),
+                                 _ints(positions, (T,), "positions", dev, torch.int64),
+                                 _ints(tables, (S, M), "tables", dev), M))
+
+
+def realq_kv_read(cache: KvCache, layer: int, starts: torch.Tensor, positions: torch.Tensor, tables: torch.Tensor,
+                  k_out: Optional[torch.Tensor], v_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The cached values of tokens at the given positions of each sequence (as
+    realq_kv_append's), into k_out and v_out (tokens x n_kv x head_dim, bf16 or fp32)."""
+    dev = _on(cache.device)
+    T, (S, M) = positions.shape[0], tables.shape
+    shape, some = (T, cache.n_kv, cache.head_dim), k_out if k_out is not None else v_out
+    if some is None or (v_out is not None and v_out.dtype != some.dtype):
+        raise ValueError("k_out or v_out expected, of one dtype")
+    ko, vo = _ints(k_out, shape, "k_out", dev, some.dtype), _ints(v_out, shape, "v_out", dev, some.dtype)
+    _check(lib().realq_kv_read(_stream(stream), ctypes.byref(cache), layer, S, T, _ints(starts, (S + 1,), "starts", dev),
+                               _ints(positions, (T,), "positions", dev, torch.int64),
+                               _ints(tables, (S, M), "tables", dev), M, ko, vo, _dtype(some)))
+
+
+def realq_kv_attention_workspace_size(cache: KvCache, n_seqs: int, T: int, n_heads: int) -> int:
+    return int(lib().realq_kv_attention_workspace_size(ctypes.byref(cache), n_seqs, T, n_heads))
+
+
+def realq_kv_attention(q: torch.Tensor, cache: KvCache, layer: int, starts: torch.Tensor, lengths: torch.Tensor,
+                       tables: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor] = None,
+                       scale: Optional[float] = None, causal: bool = True, window: int = 0,
+                       max_new: Optional[int] = None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention of each sequence's newest tokens (q: tokens x heads x head_dim, row
+    s of tables has starts[s] .. starts[s + 1] - 1) over its lengths[s] cached ones.
+    scale None: 1 / sqrt(head_dim).  max_new: the most new tokens of a sequence,
+    where the caller knows it (1 when decoding); it chooses among kernels."""
+    dev = _on(cache.device)
+    (T, H, D), (S, M) = q.shape, tables.shape
+    wp, wb = _ws(ws)
+    if D != cache.head_dim:
+        raise ValueError(f"q: heads of {cache.head_dim} values expected")
+    _check(lib().realq_kv_attention(
+        _stream(stream), ctypes.byref(cache), layer, S, T, H, *_heads(q, "q", dev), _dtype(q),
+        _ints(starts, (S + 1,), "starts", dev), _ints(lengths, (S,), "lengths", dev), _ints(tables, (S, M), "tables", dev),
+        M, D ** -0.5 if scale is None else scale, causal, window, max(T, 1) if max_new is None else max_new,
+        _ints(out, (T, H, D), "out", dev, q.dtype), _ints(lse, (T, H), "lse", dev, torch.float32), wp, wb))
+    return out
+
+
+def realq_pages_workspace_size(n_pages: int, n_rows: int, max_pages: int) -> int:
+    return int(lib().realq_pages_workspace_size(n_pages, n_rows, max_pages))
+
+
+def realq_pages_reserve(pages: KvPages, starts: torch.Tensor, positions: torch.Tensor, cache: KvCache,
+                        ws: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Room for starts[s + 1] - starts[s] more tokens in each row; positions (int64)
+    receives theirs, or -1 throughout where the pool has too few free pages (then
+    realq_workspace_status(ws) raises REALQ_ERR_NO_PAGES and nothing has changed)."""
+    dev, (wp, wb) = _on(pages.device), _ws(ws)
+    T = positions.shape[0]
+    _check(lib().realq_pages_reserve(_stream(stream), ctypes.byref(pages), _ints(starts, (pages.n_rows + 1,), "starts", dev), T,
+                                     _ints(positions, (T,), "positions", dev, torch.int64), ctypes.byref(cache), wp, wb))
+
+
+def realq_pages_fork(pages: KvPages, src: torch.Tensor, dst: torch.Tensor, ws: Optional[torch.Tensor] = None,
+                     stream=None) -> None:
+    """Rows dst[i] take over the sequences of rows src[i] (int32), all at once, sharing their pages."""
+    dev, (wp, wb), n = _on(pages.device), _ws(ws), src.shape[0]
+    _check(lib().realq_pages_fork(_stream(stream), ctypes.byref(pages), n, _ints(src, (n,), "src", dev),
+                                  _ints(dst, (n,), "dst", dev), wp, wb))
+
+
+def realq_pages_release(pages: KvPages, rows: torch.Tensor, stream=None) -> None:
+    """The listed rows (int32) give up their pages."""
+    dev, n = _on(pages.device), rows.shape[0]
+    _check(lib().realq_pages_release(_stream(stream), ctypes.byref(pages), n, _ints(rows, (n,), "rows", dev)))
+
+
+def realq_pages_compact(pages: KvPages, cache: KvCache, used_out: torch.Tensor, tables_out: torch.Tensor,
+                        moved_to: torch.Tensor, ws: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The used pages move to the front of the pool: used_out and tables_out
+    (which may be the pool's own) follow, moved_to has each page's new number."""
+    dev, (wp, wb) = _on(pages.device), _ws(ws)
+    n = pages.n_pages
+    _check(lib().realq_pages_compact(
+        _stream(stream), ctypes.byref(pages), ctypes.byref(cache), _ints(used_out, (n,), "used_out", dev),
+        _ints(tables_out, (pages.n_rows, pages.max_pages), "tables_out", dev), _ints(moved_to, (n,), "moved_to", dev), wp, wb))
+
+
+def realq_pages_copy(cache: KvCache, src: torch.Tensor, dst: torch.Tensor, stream=None) -> None:
+    """Page src[i]'s contents to page dst[i] (int32) in every layer."""
+    dev, n = _on(cache.device), src.shape[0]
+    _check(lib().realq_pages_copy(_stream(stream), ctypes.byref(cache), n, _ints(src, (n,), "src", dev),
+                                  _ints(dst, (n,), "dst", dev)))
 
 
 def realq_saliency_clip(S: torch.Tensor, pct: float = 0.99, S_out: Optional[torch.Tensor] = None,

@@ -173,6 +173,7 @@ const char *realq_status_string(realq_status_t s) {
         case REALQ_ERR_TIMEOUT: return "bounded device wait timed out";
         case REALQ_ERR_CUDA: return "CUDA error";
         case REALQ_ERR_UNSUPPORTED: return "unsupported configuration";
+        case REALQ_ERR_NO_PAGES: return "too few free pages or table entries";
     }
     return "unknown status";
 }
@@ -980,7 +981,259 @@ realq_status_t realq_workspace_status(realq_stream_t stream, void *ws, size_t ws
     REALQ_CUDA_TRY(cudaMemsetAsync(ws, 0, sizeof(int), S(stream)));
     if (st & ST_TIMEOUT) return fail(REALQ_ERR_TIMEOUT, "a bounded device-side wait gave up");
     if (st & ST_NONFINITE) return fail(REALQ_ERR_NONFINITE, "non-finite weight met during the sweep");
+    if (st & ST_NO_PAGES) return fail(REALQ_ERR_NO_PAGES, "pages_reserve: too few free pages, table entries or positions, or starts out of order");
     return REALQ_OK;
+}
+
+// --------------------------------------------------- 8-bit key/value cache ---
+static bool power_of_two(int64_t v) { return v > 0 && (v & (v - 1)) == 0; }
+static int log2_of(int64_t v) {
+    int n = 0;
+    while ((1ll << n) < v) ++n;
+    return n;
+}
+// The cache's sizes and buffers; *v the view of `layer`.
+static realq_status_t check_cache(const char *who, const realq_kv_cache_t *c, int64_t layer, KvView *v) {
+    if (!c) return fail(REALQ_ERR_INVALID_ARG, "%s: NULL cache", who);
+    if (c->n_layers <= 0 || c->n_pages <= 0 || c->n_kv <= 0) return fail(REALQ_ERR_INVALID_ARG, "%s: empty cache", who);
+    if (layer < 0 || layer >= c->n_layers) return fail(REALQ_ERR_INVALID_ARG, "%s: layer %lld of %lld", who, (long long)layer, (long long)c->n_layers);
+    if (!power_of_two(c->page_size) || c->page_size < 16 || c->page_size > 256)
+        return fail(REALQ_ERR_INVALID_ARG, "%s: page_size must be 16, 32, 64, 128 or 256 (got %lld)", who, (long long)c->page_size);
+    if (!power_of_two(c->scale_block) || c->scale_block > c->page_size)
+        return fail(REALQ_ERR_INVALID_ARG, "%s: scale_block must be a power of two up to page_size (got %lld)", who, (long long)c->scale_block);
+    if (c->head_dim <= 0 || c->head_dim % 16 || c->head_dim > 256)
+        return fail(REALQ_ERR_INVALID_ARG, "%s: head_dim must be a multiple of 16 up to 256 (got %lld)", who, (long long)c->head_dim);
+    if (c->n_kv > 4096 || c->n_pages >= (1ll << 30) || c->n_layers >= (1ll << 20))
+        return fail(REALQ_ERR_UNSUPPORTED, "%s: n_kv at most 4096, n_pages below 2^30, n_layers below 2^20", who);
+    if (!c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale) return fail(REALQ_ERR_INVALID_ARG, "%s: NULL cache buffer", who);
+    if (!aligned_to(16, c->k_codes, c->v_codes) || !aligned_to(4, c->k_scale, c->v_scale))
+        return fail(REALQ_ERR_INVALID_ARG, "%s: codes must be 16-byte aligned, scales 4-byte", who);
+    v->n_pages = (int)c->n_pages, v->n_kv = (int)c->n_kv, v->head_dim = (int)c->head_dim;
+    v->log_page = log2_of(c->page_size), v->log_block = log2_of(c->scale_block);
+    const int64_t codes = layer * c->n_pages * c->n_kv * c->page_size * c->head_dim;
+    const int64_t scales = layer * c->n_pages * c->n_kv * (c->page_size / c->scale_block);
+    v->k_codes = c->k_codes + codes, v->v_codes = c->v_codes + codes;
+    v->k_scale = c->k_scale + scales, v->v_scale = c->v_scale + scales;
+    return REALQ_OK;
+}
+static realq_status_t check_lists(const char *who, int64_t n_seqs, int64_t T, const int32_t *starts, const int32_t *tables,
+                                  int64_t max_pages) {
+    if (n_seqs < 0 || T < 0 || max_pages < 0) return fail(REALQ_ERR_INVALID_ARG, "%s: n_seqs, T, max_pages >= 0 required", who);
+    if (n_seqs > (1ll << 24) || T > (1ll << 30) || max_pages > (1ll << 24))
+        return fail(REALQ_ERR_UNSUPPORTED, "%s: n_seqs and max_pages at most 2^24, T at most 2^30", who);
+    if (n_seqs > 0 && T > 0 && (!starts || (max_pages > 0 && !tables))) return fail(REALQ_ERR_INVALID_ARG, "%s: NULL starts or tables", who);
+    if (!aligned_to(4, starts, tables)) return fail(REALQ_ERR_INVALID_ARG, "%s: starts or tables not aligned to their type", who);
+    return REALQ_OK;
+}
+// rows of T tokens x `heads` heads x `dim` values that lie at t ld + h hs
+static realq_status_t check_heads(const char *who, const char *name, int64_t T, int64_t heads, int64_t dim, const void *p, int64_t ld,
+                                  int64_t hs, realq_dtype_t dt) {
+    if (heads == 0 || T == 0) return REALQ_OK;
+    if (!p) return fail(REALQ_ERR_INVALID_ARG, "%s: NULL %s", who, name);
+    if (reinterpret_cast<uintptr_t>(p) % (dt == REALQ_BF16 ? 2 : 4)) return fail(REALQ_ERR_INVALID_ARG, "%s: %s not aligned to its type", who, name);
+    if ((heads > 1 && hs < dim) || (T > 1 && ld < (heads - 1) * hs + dim) || ld < 0 || hs < 0)
+        return fail(REALQ_ERR_INVALID_ARG, "%s: %s's heads or tokens overlap", who, name);
+    if (hs > (1ll << 40) || ld > (1ll << 40)) return fail(REALQ_ERR_UNSUPPORTED, "%s: %s's strides pass 2^40", who, name);
+    return REALQ_OK;
+}
+
+realq_status_t realq_rotary_frequencies(int64_t rot_dim, double base, int scaling, double factor, double original_context,
+                                        double low, double high, double *inv_freq) {
+    if (rot_dim < 2 || rot_dim % 2 || rot_dim > 1024) return fail(REALQ_ERR_INVALID_ARG, "rotary_frequencies: rot_dim must be even, in [2, 1024]");
+    if (!inv_freq) return fail(REALQ_ERR_INVALID_ARG, "rotary_frequencies: NULL inv_freq");
+    if (!(base > 0.0) || !std::isfinite(base)) return fail(REALQ_ERR_INVALID_ARG, "rotary_frequencies: base must be finite and > 0");
+    if (scaling < REALQ_ROPE_PLAIN || scaling > REALQ_ROPE_RAMP) return fail(REALQ_ERR_INVALID_ARG, "rotary_frequencies: bad scaling");
+    if (scaling != REALQ_ROPE_PLAIN && (!(factor > 0.0) || !std::isfinite(factor)))
+        return fail(REALQ_ERR_INVALID_ARG, "rotary_frequencies: factor must be finite and > 0");
+    if (scaling == REALQ_ROPE_RAMP && (!(original_context > 0.0) || !std::isfinite(original_context) || !(low < high) || !std::isfinite(low) || !std::isfinite(high)))
+        return fail(REALQ_ERR_INVALID_ARG, "rotary_frequencies: original_context > 0 and low < high required");
+    rotary_frequencies(rot_dim, base, scaling, factor, original_context, low, high, inv_freq);
+    return REALQ_OK;
+}
+
+realq_status_t realq_rotary(realq_stream_t stream, int64_t T, int64_t head_dim, int64_t rot_dim, const int64_t *positions,
+                            const double *inv_freq, int interleaved, float amplitude, int transpose, realq_dtype_t dtype,
+                            int64_t n_q, const void *q, int64_t q_ld, int64_t q_hs, void *q_out, int64_t qo_ld, int64_t qo_hs,
+                            int64_t n_k, const void *k, int64_t k_ld, int64_t k_hs, void *k_out, int64_t ko_ld, int64_t ko_hs) {
+    const char *who = "rotary";
+    if (T < 0 || n_q < 0 || n_k < 0 || n_q + n_k <= 0) return fail(REALQ_ERR_INVALID_ARG, "rotary: T >= 0 and some heads required");
+    if (head_dim < 2 || head_dim > 1024 || rot_dim < 2 || rot_dim % 2 || rot_dim > head_dim)
+        return fail(REALQ_ERR_INVALID_ARG, "rotary: rot_dim must be even, in [2, head_dim], head_dim at most 1024");
+    if (!valid_dtype(dtype)) return fail(REALQ_ERR_INVALID_ARG, "rotary: bad dtype");
+    if (!std::isfinite(amplitude)) return fail(REALQ_ERR_INVALID_ARG, "rotary: amplitude must be finite");
+    if (n_q > 65536 || n_k > 65536 || T > (1ll << 30)) return fail(REALQ_ERR_UNSUPPORTED, "rotary: at most 65536 heads each and 2^30 tokens");
+    REALQ_TRY(check_heads(who, "q", T, n_q, head_dim, q, q_ld, q_hs, dtype));
+    REALQ_TRY(check_heads(who, "q_out", T, n_q, head_dim, q_out, qo_ld, qo_hs, dtype));
+    REALQ_TRY(check_heads(who, "k", T, n_k, head_dim, k, k_ld, k_hs, dtype));
+    REALQ_TRY(check_heads(who, "k_out", T, n_k, head_dim, k_out, ko_ld, ko_hs, dtype));
+    if (T == 0) return REALQ_OK;
+    if (!positions || !inv_freq) return fail(REALQ_ERR_INVALID_ARG, "rotary: NULL positions or inv_freq");
+    if (!aligned_to(8, positions, inv_freq)) return fail(REALQ_ERR_INVALID_ARG, "rotary: positions or inv_freq not aligned to their type");
+    if ((n_q > 0 && q == q_out && ((T > 1 && q_ld != qo_ld) || (n_q > 1 && q_hs != qo_hs))) ||
+        (n_k > 0 && k == k_out && ((T > 1 && k_ld != ko_ld) || (n_k > 1 && k_hs != ko_hs))))
+        return fail(REALQ_ERR_INVALID_ARG, "rotary: in place, an output has its input's strides");
+    RotaryArgs a = {};
+    a.T = T, a.head_dim = (int)head_dim, a.rot_dim = (int)rot_dim, a.interleaved = interleaved != 0, a.transpose = transpose != 0;
+    a.n_q = (int)n_q, a.n_k = (int)n_k, a.amplitude = amplitude, a.positions = positions, a.inv_freq = inv_freq;
+    a.copy_rest = rot_dim < head_dim && ((n_q > 0 && q != q_out) || (n_k > 0 && k != k_out));
+    a.q = q, a.q_ld = q_ld, a.q_hs = q_hs, a.q_out = q_out, a.qo_ld = qo_ld, a.qo_hs = qo_hs;
+    a.k = k, a.k_ld = k_ld, a.k_hs = k_hs, a.k_out = k_out, a.ko_ld = ko_ld, a.ko_hs = ko_hs;
+    return rotary(S(stream), a, dtype, num_sms());
+}
+
+realq_status_t realq_kv_append(realq_stream_t stream, const realq_kv_cache_t *cache, int64_t layer, int64_t n_seqs, int64_t T,
+                               const void *k, int64_t k_ld, int64_t k_hs, const void *v, int64_t v_ld, int64_t v_hs,
+                               realq_dtype_t dtype, const int32_t *starts, const int64_t *positions, const int32_t *tables,
+                               int64_t max_pages) {
+    const char *who = "kv_append";
+    KvAppendArgs a = {};
+    REALQ_TRY(check_cache(who, cache, layer, &a.c));
+    REALQ_TRY(check_lists(who, n_seqs, T, starts, tables, max_pages));
+    if (!valid_dtype(dtype)) return fail(REALQ_ERR_INVALID_ARG, "kv_append: bad dtype");
+    REALQ_TRY(check_heads(who, "k", T, cache->n_kv, cache->head_dim, k, k_ld, k_hs, dtype));
+    REALQ_TRY(check_heads(who, "v", T, cache->n_kv, cache->head_dim, v, v_ld, v_hs, dtype));
+    if (T == 0 || n_seqs == 0 || max_pages == 0) return REALQ_OK;
+    if (!positions || !aligned_to(8, positions)) return fail(REALQ_ERR_INVALID_ARG, "kv_append: positions NULL or not aligned to their type");
+    if (((T >> a.c.log_block) + 2 * n_seqs) * 2 * a.c.n_kv / 4 >= INT32_MAX) return fail(REALQ_ERR_UNSUPPORTED, "kv_append: too many blocks");
+    a.n_seqs = (int)n_seqs, a.T = T, a.k = k, a.k_ld = k_ld, a.k_hs = k_hs, a.v = v, a.v_ld = v_ld, a.v_hs = v_hs;
+    a.starts = starts, a.positions = positions, a.tables = tables, a.max_pages = max_pages;
+    return kv_append(S(stream), a, dtype);
+}
+
+realq_status_t realq_kv_read(realq_stream_t stream, const realq_kv_cache_t *cache, int64_t layer, int64_t n_seqs, int64_t T,
+                             const int32_t *starts, const int64_t *positions, const int32_t *tables, int64_t max_pages,
+                             void *k_out, void *v_out, realq_dtype_t dtype) {
+    const char *who = "kv_read";
+    KvReadArgs a = {};
+    REALQ_TRY(check_cache(who, cache, layer, &a.c));
+    REALQ_TRY(check_lists(who, n_seqs, T, starts, tables, max_pages));
+    if (!valid_dtype(dtype)) return fail(REALQ_ERR_INVALID_ARG, "kv_read: bad dtype");
+    if (!aligned_to(dtype == REALQ_BF16 ? 2 : 4, (const char *)k_out, (const char *)v_out))
+        return fail(REALQ_ERR_INVALID_ARG, "kv_read: an output is not aligned to its type");
+    if (T == 0 || n_seqs == 0 || (!k_out && !v_out)) return REALQ_OK;
+    if (!positions || !aligned_to(8, positions)) return fail(REALQ_ERR_INVALID_ARG, "kv_read: positions NULL or not aligned to their type");
+    if (T * a.c.n_kv * (a.c.head_dim / 16) / 128 >= INT32_MAX) return fail(REALQ_ERR_UNSUPPORTED, "kv_read: too many values");
+    a.n_seqs = (int)n_seqs, a.T = T, a.max_pages = max_pages, a.starts = starts, a.positions = positions, a.tables = tables;
+    a.k_out = k_out, a.v_out = v_out;
+    return kv_read(S(stream), a, dtype);
+}
+
+size_t realq_kv_attention_workspace_size(const realq_kv_cache_t *cache, int64_t n_seqs, int64_t T, int64_t n_heads) {
+    KvView v;
+    if (n_seqs <= 0 || T <= 0 || n_heads <= 0 || check_cache("kv_attention_workspace_size", cache, 0, &v) != REALQ_OK || n_heads % v.n_kv) return 0;
+    return kv_decode_ws_bytes(v.head_dim, num_sms());
+}
+
+realq_status_t realq_kv_attention(realq_stream_t stream, const realq_kv_cache_t *cache, int64_t layer, int64_t n_seqs, int64_t T,
+                                  int64_t n_heads, const void *q, int64_t q_ld, int64_t q_hs, realq_dtype_t dtype,
+                                  const int32_t *starts, const int32_t *lengths, const int32_t *tables, int64_t max_pages,
+                                  float scale, int causal, int64_t window, int64_t max_new, void *out, float *lse, void *ws,
+                                  size_t ws_bytes) {
+    const char *who = "kv_attention";
+    KvAttnArgs a = {};
+    REALQ_TRY(check_cache(who, cache, layer, &a.c));
+    REALQ_TRY(check_lists(who, n_seqs, T, starts, tables, max_pages));
+    if (!valid_dtype(dtype)) return fail(REALQ_ERR_INVALID_ARG, "kv_attention: bad dtype");
+    if (n_heads <= 0 || n_heads % a.c.n_kv) return fail(REALQ_ERR_INVALID_ARG, "kv_attention: n_heads must be a multiple of n_kv");
+    if (n_heads / a.c.n_kv > 1024) return fail(REALQ_ERR_UNSUPPORTED, "kv_attention: at most 1024 heads to a key/value head");
+    if (!std::isfinite(scale)) return fail(REALQ_ERR_INVALID_ARG, "kv_attention: scale must be finite");
+    if (window < 0 || (window > 0 && !causal)) return fail(REALQ_ERR_INVALID_ARG, "kv_attention: window >= 0, and only with causal != 0");
+    if (max_new < 1 && T > 0) return fail(REALQ_ERR_INVALID_ARG, "kv_attention: max_new >= 1 required");
+    REALQ_TRY(check_heads(who, "q", T, n_heads, a.c.head_dim, q, q_ld, q_hs, dtype));
+    if (T == 0 || n_seqs == 0) return REALQ_OK;
+    if (!lengths || !out) return fail(REALQ_ERR_INVALID_ARG, "kv_attention: NULL lengths or out");
+    if (!aligned_to(4, lengths, lse) || !aligned_to(dtype == REALQ_BF16 ? 2 : 4, (const char *)out))
+        return fail(REALQ_ERR_INVALID_ARG, "kv_attention: lengths or an output not aligned to its type");
+    if (T * (n_heads / a.c.n_kv) >= INT32_MAX / 2) return fail(REALQ_ERR_UNSUPPORTED, "kv_attention: T n_heads / n_kv must be below 2^30");
+    REALQ_TRY(check_ws(ws, ws_bytes, kv_decode_ws_bytes(a.c.head_dim, num_sms()), who));
+    a.n_seqs = (int)n_seqs, a.n_heads = (int)n_heads, a.group = (int)(n_heads / a.c.n_kv), a.causal = causal != 0;
+    a.T = T, a.q = q, a.q_ld = q_ld, a.q_hs = q_hs, a.max_pages = max_pages, a.window = window;
+    a.starts = starts, a.lengths = lengths, a.tables = tables, a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+    a.out = out, a.lse = lse;
+    a.min_new = 1, a.max_new = INT32_MAX;
+    return kv_decode(S(stream), a, dtype, std::min(max_new, T) * a.group, ws, num_sms());
+}
+
+static realq_status_t check_pages(const char *who, const realq_kv_pages_t *p, KvPagesView *v) {
+    if (!p) return fail(REALQ_ERR_INVALID_ARG, "%s: NULL pages", who);
+    if (p->n_pages <= 0 || p->n_rows <= 0 || p->max_pages <= 0) return fail(REALQ_ERR_INVALID_ARG, "%s: n_pages, n_rows, max_pages > 0 required", who);
+    if (p->n_pages >= (1ll << 30) || p->n_rows > (1ll << 24) || p->max_pages > (1ll << 24))
+        return fail(REALQ_ERR_UNSUPPORTED, "%s: n_pages below 2^30, n_rows and max_pages at most 2^24", who);
+    if (!p->used || !p->tables || !p->lengths) return fail(REALQ_ERR_INVALID_ARG, "%s: NULL used, tables or lengths", who);
+    if (!aligned_to(4, p->used, p->tables, p->lengths)) return fail(REALQ_ERR_INVALID_ARG, "%s: a list is not aligned to its type", who);
+    v->n_pages = p->n_pages, v->n_rows = p->n_rows, v->max_pages = p->max_pages;
+    v->used = p->used, v->tables = p->tables, v->lengths = p->lengths;
+    return REALQ_OK;
+}
+static realq_status_t check_pool(const char *who, const realq_kv_cache_t *cache, const KvPagesView &v, KvView *c) {
+    REALQ_TRY(check_cache(who, cache, 0, c));
+    if (cache->n_pages != v.n_pages) return fail(REALQ_ERR_INVALID_ARG, "%s: the cache has %lld pages, the pool %lld", who, (long long)cache->n_pages, (long long)v.n_pages);
+    return REALQ_OK;
+}
+
+size_t realq_pages_workspace_size(int64_t n_pages, int64_t n_rows, int64_t max_pages) {
+    return n_pages > 0 && n_pages < (1ll << 30) && n_rows > 0 && n_rows <= (1ll << 24) && max_pages > 0 && max_pages <= (1ll << 24)
+               ? pages_ws_bytes(n_pages, n_rows, max_pages) : 0;
+}
+
+realq_status_t realq_pages_reserve(realq_stream_t stream, const realq_kv_pages_t *pages, const int32_t *starts, int64_t T,
+                                   int64_t *positions, const realq_kv_cache_t *cache, void *ws, size_t ws_bytes) {
+    KvPagesView v;
+    KvView c;
+    REALQ_TRY(check_pages("pages_reserve", pages, &v));
+    REALQ_TRY(check_pool("pages_reserve", cache, v, &c));
+    if (T < 0) return fail(REALQ_ERR_INVALID_ARG, "pages_reserve: T >= 0 required");
+    if (T > (1ll << 30)) return fail(REALQ_ERR_UNSUPPORTED, "pages_reserve: T at most 2^30");
+    if (!starts || (T > 0 && !positions)) return fail(REALQ_ERR_INVALID_ARG, "pages_reserve: NULL starts or positions");
+    if (!aligned_to(4, starts) || !aligned_to(8, positions)) return fail(REALQ_ERR_INVALID_ARG, "pages_reserve: starts or positions not aligned to their type");
+    REALQ_TRY(check_ws(ws, ws_bytes, pages_ws_bytes(v.n_pages, v.n_rows, v.max_pages), "pages_reserve"));
+    return pages_reserve(S(stream), v, starts, T, positions, c, cache->n_layers, ws, num_sms());
+}
+
+realq_status_t realq_pages_fork(realq_stream_t stream, const realq_kv_pages_t *pages, int64_t n, const int32_t *src,
+                                const int32_t *dst, void *ws, size_t ws_bytes) {
+    KvPagesView v;
+    REALQ_TRY(check_pages("pages_fork", pages, &v));
+    if (n < 0) return fail(REALQ_ERR_INVALID_ARG, "pages_fork: n >= 0 required");
+    if (n > (1ll << 24)) return fail(REALQ_ERR_UNSUPPORTED, "pages_fork: n at most 2^24");
+    if (n == 0) return REALQ_OK;
+    if (!src || !dst || !aligned_to(4, src, dst)) return fail(REALQ_ERR_INVALID_ARG, "pages_fork: src or dst NULL or not aligned to its type");
+    REALQ_TRY(check_ws(ws, ws_bytes, pages_ws_bytes(v.n_pages, v.n_rows, v.max_pages), "pages_fork"));
+    return pages_fork(S(stream), v, n, src, dst, ws);
+}
+
+realq_status_t realq_pages_release(realq_stream_t stream, const realq_kv_pages_t *pages, int64_t n, const int32_t *rows) {
+    KvPagesView v;
+    REALQ_TRY(check_pages("pages_release", pages, &v));
+    if (n < 0) return fail(REALQ_ERR_INVALID_ARG, "pages_release: n >= 0 required");
+    if (n > (1ll << 24)) return fail(REALQ_ERR_UNSUPPORTED, "pages_release: n at most 2^24");
+    if (n == 0) return REALQ_OK;
+    if (!rows || !aligned_to(4, rows)) return fail(REALQ_ERR_INVALID_ARG, "pages_release: rows NULL or not aligned to its type");
+    return pages_release(S(stream), v, n, rows);
+}
+
+realq_status_t realq_pages_compact(realq_stream_t stream, const realq_kv_pages_t *pages, const realq_kv_cache_t *cache,
+                                   int32_t *used_out, int32_t *tables_out, int32_t *moved_to, void *ws, size_t ws_bytes) {
+    KvPagesView v;
+    KvView c;
+    REALQ_TRY(check_pages("pages_compact", pages, &v));
+    REALQ_TRY(check_pool("pages_compact", cache, v, &c));
+    if (!used_out || !tables_out || !moved_to || !aligned_to(4, used_out, tables_out, moved_to))
+        return fail(REALQ_ERR_INVALID_ARG, "pages_compact: an output is NULL or not aligned to its type");
+    if (moved_to == v.used || moved_to == v.tables || moved_to == used_out || moved_to == tables_out)
+        return fail(REALQ_ERR_INVALID_ARG, "pages_compact: moved_to must be a buffer of its own");
+    REALQ_TRY(check_ws(ws, ws_bytes, pages_ws_bytes(v.n_pages, v.n_rows, v.max_pages), "pages_compact"));
+    return pages_compact(S(stream), v, c, cache->n_layers, used_out, tables_out, moved_to, ws, num_sms());
+}
+
+realq_status_t realq_pages_copy(realq_stream_t stream, const realq_kv_cache_t *cache, int64_t n, const int32_t *src, const int32_t *dst) {
+    KvView c;
+    REALQ_TRY(check_cache("pages_copy", cache, 0, &c));
+    if (n < 0) return fail(REALQ_ERR_INVALID_ARG, "pages_copy: n >= 0 required");
+    if (n > (1ll << 30)) return fail(REALQ_ERR_UNSUPPORTED, "pages_copy: n at most 2^30");
+    if (n == 0) return REALQ_OK;
+    if (!src || !dst || !aligned_to(4, src, dst)) return fail(REALQ_ERR_INVALID_ARG, "pages_copy: src or dst NULL or not aligned to its type");
+    return pages_copy(S(stream), c, cache->n_layers, n, src, dst, num_sms());
 }
 
 }  // extern "C"

@@ -39,6 +39,7 @@ enum : int {
     ST_NONFINITE = 1,
     ST_NOT_SPD = 2,
     ST_TIMEOUT = 4,
+    ST_NO_PAGES = 8,
 };
 
 // A kernel launched so that it may start while the kernel before it in the

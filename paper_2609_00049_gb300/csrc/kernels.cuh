@@ -164,6 +164,79 @@ realq_status_t token_logprobs_grad(cudaStream_t s, int64_t T, int64_t V, int64_t
                                    const float *entropy, const float *d_entropy, int k, const int64_t *top_ids,
                                    const float *d_top, int64_t ldd, void *D);
 
+// ------------------------------------------------ 8-bit key/value cache ---
+// Sizes, strides and pointers have been checked by the caller (see realq.h);
+// what lies on the device (starts, positions, tables, lengths) has not.
+struct RotaryArgs {
+    int64_t T;
+    int head_dim, rot_dim, interleaved, transpose, n_q, n_k, copy_rest;
+    float amplitude;
+    const int64_t *positions;
+    const double *inv_freq;
+    const void *q, *k;
+    void *q_out, *k_out;
+    int64_t q_ld, q_hs, qo_ld, qo_hs, k_ld, k_hs, ko_ld, ko_hs;
+};
+realq_status_t rotary(cudaStream_t s, const RotaryArgs &a, realq_dtype_t dt, int sms);
+void rotary_frequencies(int64_t R, double base, int scaling, double factor, double context, double low, double high,
+                        double *out);
+
+struct KvView {            // a layer's part of the cache (the first one's, for the page copies)
+    int n_pages, n_kv, head_dim, log_page, log_block;
+    uint8_t *k_codes, *v_codes;
+    float *k_scale, *v_scale;
+};
+struct KvAppendArgs {
+    KvView c;
+    int n_seqs;
+    int64_t T, k_ld, k_hs, v_ld, v_hs, max_pages;
+    const void *k, *v;
+    const int *starts, *tables;
+    const int64_t *positions;
+};
+struct KvReadArgs {
+    KvView c;
+    int n_seqs, wide;
+    int64_t T, max_pages;
+    const int *starts, *tables;
+    const int64_t *positions;
+    void *k_out, *v_out;
+};
+realq_status_t kv_append(cudaStream_t s, const KvAppendArgs &a, realq_dtype_t dt);
+realq_status_t kv_read(cudaStream_t s, const KvReadArgs &a, realq_dtype_t dt);
+
+constexpr int KV_MAX_CTAS_PER_SM = 4;
+struct KvAttnArgs {
+    KvView c;
+    int n_seqs, n_heads, group, causal;   // group: query heads of a key/value head
+    int64_t T, q_ld, q_hs, max_pages, window;
+    const void *q;
+    const int *starts, *lengths, *tables;
+    float scale_log2;                     // scale log2(e)
+    void *out;
+    float *lse;
+    int min_new, max_new;                 // the kernel takes sequences of min_new .. max_new new tokens
+    int *counters;
+    float *part;
+    __device__ __forceinline__ bool takes(int m) const { return m >= min_new && m <= max_new; }
+};
+size_t kv_decode_ws_bytes(int head_dim, int sms);
+realq_status_t kv_decode(cudaStream_t s, const KvAttnArgs &a, realq_dtype_t dt, int64_t rows, void *ws, int sms);
+
+struct KvPagesView {
+    int64_t n_pages, n_rows, max_pages;
+    int *used, *tables, *lengths;
+};
+size_t pages_ws_bytes(int64_t n_pages, int64_t n_rows, int64_t max_pages);
+realq_status_t pages_reserve(cudaStream_t s, const KvPagesView &v, const int *starts, int64_t T, int64_t *positions,
+                             const KvView &c, int64_t n_layers, void *ws, int sms);
+realq_status_t pages_fork(cudaStream_t s, const KvPagesView &v, int64_t n, const int *src, const int *dst, void *ws);
+realq_status_t pages_release(cudaStream_t s, const KvPagesView &v, int64_t n, const int *rows);
+realq_status_t pages_compact(cudaStream_t s, const KvPagesView &v, const KvView &c, int64_t n_layers, int *used_out,
+                             int *tables_out, int *moved_to, void *ws, int sms);
+realq_status_t pages_copy(cudaStream_t s, const KvView &c, int64_t n_layers, int64_t n, const int *src, const int *dst,
+                          int sms);
+
 // ------------------------------------------- saliency-weighted Hessians ---
 size_t saliency_clip_ws_bytes();
 realq_status_t saliency_clip(cudaStream_t s, int64_t T, int ng, const float *S, double pct, float *S_out,

@@ -1,0 +1,648 @@
+// Attention of a few query rows over the 8-bit cache: single tokens, drafts.
+//
+// The rows that share a key/value head (its G query heads times the sequence's
+// new tokens) are taken together, 8, 16 or 32 at a time (NT tiles of 8), against
+// tiles of 64 cached tokens, 16 to a warp.  Bound by reading the codes once from
+// HBM, so everything else has to fit under that:
+//
+// - Products by mma.sync m16n8k16 in fp16, transposed: S^T = K Q^T takes the
+//   warp's 16 tokens as rows and 8 query rows as columns, so that a single query
+//   head wastes seven columns of a cheap instruction, not fifteen rows of an
+//   expensive one.  O^T = V^T P^T then takes 16 channels as rows.
+// - Codes become fp16 exactly: a byte permute puts code c behind 0x64 (1024 + c),
+//   one subtraction takes 1152 off.  The order of the channels inside a product
+//   is free, so a lane uses the 16 consecutive bytes that it reads; V's bytes of
+//   two tokens are interleaved by one more permute for two pairs.
+// - Query rows are scaled by a power of two so that their largest value lies in
+//   [2^14, 2^15): a bf16 row is exact in fp16 down to 2^-29 of its largest value, an fp32 row
+//   is taken as the sum of two fp16 parts (22 bits).
+// - The block scales of K multiply the scores in fp32, those of V the weights
+//   before these become fp16: p = 2^(s - M) vscale with M = 14 less than the
+//   running maximum of s + log2 vscale, so that the largest weight is about 2^14
+//   and what fp16 cannot hold is 2^-38 of it.  With bf16 inputs p is rounded to
+//   fp16 (2^-12 relative, a sixteenth of the output's own rounding); with fp32 ones it
+//   is two fp16 parts.  The softmax's sum adds 2^(s - M) in fp32.
+// - A warp keeps its own maximum, sum and output; the four are joined at the end
+//   of a CTA's share, and shares of one row tile by the CTA that ends last.
+//
+// Work is split evenly whatever the lengths: all (sequence, head, row tile)
+// units' 64-token tiles in a row are cut into one share per resident CTA.  A
+// unit that lies in one share is finished there; otherwise its CTAs leave
+// (maximum, sum, output) in the workspace and the last to arrive adds them in
+// the order of the shares, so results repeat bit by bit.  The arrival counter
+// wraps to zero by itself.
+#include <algorithm>
+
+#include "kernels.cuh"
+
+namespace realq {
+namespace {
+
+constexpr int WARPS = 4, THREADS = 32 * WARPS, GROUP = 16, TILE = GROUP * WARPS;
+constexpr int SEQS = 512;                 // sequences whose tile counts are held at a time
+constexpr float NEG = -INFINITY;
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float log2_fast(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t hsub2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+    uint32_t d;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+// what pack_half left of (lo, hi)
+__device__ __forceinline__ uint32_t pack_rest(float lo, float hi, uint32_t h) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+    return pack_half(lo - f.x, hi - f.y);
+}
+// bytes 0 1 / 2 3 of w as two fp16 whole numbers c - 128
+__device__ __forceinline__ uint32_t codes01(uint32_t w) { return hsub2(__byte_perm(w, 0x64646464u, 0x4140), 0x64806480u); }
+__device__ __forceinline__ uint32_t codes23(uint32_t w) { return hsub2(__byte_perm(w, 0x64646464u, 0x4342), 0x64806480u); }
+__device__ __forceinline__ uint32_t transposed8x8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void *src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Sizes of the kernel for heads of up to DP channels and NT tiles of 8 rows.
+template <int DP, int NT, bool F32> struct Shape {
+    static constexpr int CH = DP / 16;                        // 16-byte pieces of a token's codes
+    static constexpr int STEPS = DP / 16;                     // of the products over channels
+    static constexpr int MT = DP / 16;                        // tiles of 16 channels of the output
+    static constexpr int ROWS = 8 * NT;
+    static constexpr int PARTS = F32 ? 2 : 1;                 // fp16 parts of a query
+    static constexpr int SCALES = 2 * GROUP * 4;              // bytes
+    static constexpr int STAGE = 2 * GROUP * DP + SCALES;     // a warp's 16 tokens
+    static constexpr int STAGES = DP == 64 ? 6 : (DP == 128 ? 4 : 3);
+    static constexpr int RING = STAGE * STAGES;               // per warp; its output at the end of a share
+    static constexpr int QFRAG = STEPS * NT * PARTS * 32 * 8;
+    static constexpr bool QREG = NT * STEPS * PARTS <= 16;    // held in registers
+    static constexpr int SMEM = WARPS * RING + QFRAG;
+    static_assert(ROWS * DP * 4 <= RING, "a warp's output fits its ring");
+    // where a token's piece c lies in its row: spread so that neither the lanes of K (two tokens, four pieces) nor
+    // those of V (four tokens, two pieces) meet in a bank
+    __device__ static __forceinline__ int swizzle(int token, int c) {
+        if constexpr (CH >= 8) return c ^ (((token >> 1) & 3) << 1) ^ ((token & 1) << 2);
+        return c ^ ((token >> 1) & 3);
+    }
+};
+
+struct Unit {        // one sequence, key/value head and row tile
+    int seq, head, tile;
+    int q0, m;       // the sequence's first query token and their number
+    int len;         // cached tokens
+    int r0, rows;    // rows of the tile: r0 .. r0 + rows - 1 of m x G
+    int lo, hi;      // cached tokens that any row sees: [lo, hi)
+};
+
+// Tiles of one row tile of a sequence (at least one: rows that see nothing are written too).
+__device__ __forceinline__ void span(const KvAttnArgs &a, int m, int len, int r0, int r1, int *lo, int *hi) {
+    const int p0 = len - m + r0 / a.group, p1 = len - m + (r1 - 1) / a.group;
+    *hi = a.causal ? max(0, min(len, p1 + 1)) : len;
+    *lo = a.window > 0 ? (int)min((int64_t)*hi, max((int64_t)0, (int64_t)p0 - a.window + 1)) : 0;
+}
+__device__ __forceinline__ int tiles_of(int lo, int hi) { return hi > lo ? (hi - 1) / TILE - lo / TILE + 1 : 1; }
+
+struct Seq {
+    int q0, m, len;
+    __device__ Seq(const KvAttnArgs &a, int s) {
+        const int64_t b = a.starts[s], e = a.starts[s + 1];
+        const bool ok = b >= 0 && e > b && e <= a.T;
+        q0 = ok ? (int)b : 0, m = ok ? (int)(e - b) : 0;
+        len = (int)min((int64_t)max(a.lengths[s], 0), a.max_pages << a.c.log_page);
+        if (m > 0 && !a.takes(m)) m = 0;   // another kernel's
+    }
+};
+template <int ROWS> __device__ int64_t seq_tiles(const KvAttnArgs &a, int s) {   // of one head
+    const Seq q(a, s);
+    int64_t n = 0;
+    for (int r = 0; r < q.m * a.group; r += ROWS) {
+        int lo, hi;
+        span(a, q.m, q.len, r, min(r + ROWS, q.m * a.group), &lo, &hi);
+        n += tiles_of(lo, hi);
+    }
+    return n;
+}
+
+// The tile counts of SEQS sequences from `first` on, as a running sum (of one head).
+struct Window {
+    int first;
+    int64_t base;               // tiles of all heads before them
+    int64_t sum[SEQS + 1];
+    int64_t warp_sum[WARPS];
+};
+template <int ROWS> __device__ void fill_window(const KvAttnArgs &a, Window &w, int first, int64_t base) {
+    constexpr int PER = SEQS / THREADS;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int64_t mine[PER], total = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int s = first + threadIdx.x * PER + i;
+        mine[i] = s < a.n_seqs ? seq_tiles<ROWS>(a, s) : 0;
+        total += mine[i];
+    }
+    int64_t x = total;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const int64_t y = __shfl_up_sync(0xFFFFFFFFu, x, d);
+        if (lane >= d) x += y;
+    }
+    __syncthreads();
+    if (lane == 31) w.warp_sum[warp] = x;
+    __syncthreads();
+    int64_t at = x - total;
+    for (int i = 0; i < warp; ++i) at += w.warp_sum[i];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        w.sum[threadIdx.x * PER + i] = at;
+        at += mine[i];
+    }
+    if (threadIdx.x == THREADS - 1) w.sum[SEQS] = at;
+    if (threadIdx.x == 0) w.first = first, w.base = base;
+    __syncthreads();
+}
+
+template <int DP, int NT, bool F32, class T>
+__global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
+    using Sh = Shape<DP, NT, F32>;
+    constexpr int ROWS = Sh::ROWS;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ Window win;
+    __shared__ float row_scale[ROWS];
+    __shared__ int row_lo[ROWS], row_hi[ROWS];
+    __shared__ float join_m[WARPS][ROWS], join_l[WARPS][ROWS];
+    __shared__ int last_one;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    uint8_t *ring = smem + warp * Sh::RING;
+    uint2 *qfrag = reinterpret_cast<uint2 *>(smem + WARPS * Sh::RING);
+    const int D = a.c.head_dim, pieces = D / 16;
+    float *const part = a.part;
+    constexpr int PART = ROWS * (DP + 2);
+
+    // all tiles, and this CTA's share
+    int64_t all = 0;
+    for (int first = 0; first < a.n_seqs; first += SEQS) {
+        fill_window<ROWS>(a, win, first, all);
+        all += win.sum[SEQS] * a.c.n_kv;
+    }
+    const int64_t ctas = min((int64_t)gridDim.x, all);
+    if (blockIdx.x >= ctas) return;
+    const auto begin = [&](int64_t c) { return c * all / ctas; };
+    const auto owner = [&](int64_t x) {   // of tile x
+        int64_t c = (x * ctas + ctas - 1) / all;
+        while (c > 0 && begin(c) > x) --c;
+        while (c + 1 < ctas && begin(c + 1) <= x) ++c;
+        return (int)c;
+    };
+    int64_t at = begin(blockIdx.x);
+    const int64_t end = begin(blockIdx.x + 1);
+    if (a.n_seqs > SEQS) {
+        fill_window<ROWS>(a, win, 0, 0);
+    }
+    while (at < end) {
+        // ---- the unit that holds tile `at` ----
+        // (lengths that another stream changes meanwhile give wrong results; the loops end all the same)
+        while (at >= win.base + win.sum[SEQS] * a.c.n_kv && win.first + SEQS < a.n_seqs)
+            fill_window<ROWS>(a, win, win.first + SEQS, win.base + win.sum[SEQS] * a.c.n_kv);
+        Unit u;
+        int64_t unit0;   // the unit's first tile
+        int tiles;
+        {
+            int lo = 0, hi = SEQS - 1;   // the last sequence that begins at or before the tile
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (win.base + win.sum[mid] * a.c.n_kv <= at)
+                    lo = mid;
+                else
+                    hi = mid - 1;
+            }
+            u.seq = win.first + lo;
+            const int64_t per_head = max((int64_t)1, win.sum[lo + 1] - win.sum[lo]);
+            int64_t off = at - (win.base + win.sum[lo] * a.c.n_kv);
+            u.head = (int)min(off / per_head, (int64_t)a.c.n_kv - 1);
+            unit0 = at - off + u.head * per_head;
+            off -= u.head * per_head;
+            const Seq q(a, u.seq);
+            u.q0 = q.q0, u.m = q.m, u.len = q.len;
+            const int rows_all = q.m * a.group;
+            for (u.r0 = 0, u.tile = 0;; u.r0 += ROWS, ++u.tile) {
+                u.rows = min(ROWS, rows_all - u.r0);
+                span(a, q.m, q.len, u.r0, u.r0 + u.rows, &u.lo, &u.hi);
+                tiles = tiles_of(u.lo, u.hi);
+                if (off < tiles || u.r0 + ROWS >= rows_all) break;
+                off -= tiles, unit0 += tiles;
+            }
+        }
+        const int from = (int)min(at - unit0, (int64_t)tiles - 1);
+        const int count = (int)min(end - at, (int64_t)(tiles - from));
+        const int tile0 = u.lo / TILE + from;
+        at += count;
+
+        // ---- queries: a warp takes a tile of 8 rows ----
+        for (int nt = warp; nt < NT; nt += WARPS) {
+            const int r = u.r0 + 8 * nt + g;
+            const bool row_in = 8 * nt + g < u.rows;
+            const int qi = row_in ? r / a.group : 0;
+            const T *q = (const T *)a.q + (int64_t)(u.q0 + qi) * a.q_ld + (int64_t)(u.head * a.group + (row_in ? r % a.group : 0)) * a.q_hs;
+            float v[DP / 4];
+            float top = 0.f;
+#pragma unroll
+            for (int j = 0; j < DP / 64; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int d = 16 * (t + 4 * j) + e;
+                    const float x = row_in && d < D ? load_as_float(q, d) : 0.f;
+                    v[16 * j + e] = x;
+                    top = fmaxf(top, fabsf(x));
+                }
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+            // 2^k with top 2^k in [2^14, 2^15), by two factors: one alone may pass the range of fp32
+            int k = 0;
+            if (top > 0.f && top < INFINITY) k = 14 - ilogbf(top);
+            const float up0 = scalbnf(1.f, k / 2), up1 = scalbnf(1.f, k - k / 2);
+#pragma unroll
+            for (int j = 0; j < DP / 64; ++j)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    float x[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = v[16 * j + 4 * w + e] * up0 * up1;
+                    const uint2 h = make_uint2(pack_half(x[0], x[1]), pack_half(x[2], x[3]));
+                    const int step = 4 * j + w;
+                    qfrag[((step * NT + nt) * Sh::PARTS) * 32 + lane] = h;
+                    if constexpr (F32)
+                        qfrag[((step * NT + nt) * 2 + 1) * 32 + lane] = make_uint2(pack_rest(x[0], x[1], h.x), pack_rest(x[2], x[3], h.y));
+                }
+            if (t == 0) {
+                const int p = u.len - u.m + qi;
+                row_scale[8 * nt + g] = a.scale_log2 * scalbnf(1.f, -(k / 2)) * scalbnf(1.f, -(k - k / 2));
+                row_hi[8 * nt + g] = !row_in ? 0 : (a.causal ? min(u.len, p + 1) : u.len);
+                row_lo[8 * nt + g] = a.window > 0 ? (int)max((int64_t)0, (int64_t)p - a.window + 1) : 0;
+            }
+        }
+        __syncthreads();
+        uint2 qreg[Sh::QREG ? Sh::STEPS * NT * Sh::PARTS : 1];
+        if constexpr (Sh::QREG) {
+#pragma unroll
+            for (int i = 0; i < Sh::STEPS * NT * Sh::PARTS; ++i) qreg[i] = qfrag[i * 32 + lane];
+        }
+        float rs[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) rs[nt][0] = row_scale[8 * nt + 2 * t], rs[nt][1] = row_scale[8 * nt + 2 * t + 1];
+        // tokens that every row sees
+        const int p_first = u.len - u.m + u.r0 / a.group, p_last = u.len - u.m + (u.r0 + u.rows - 1) / a.group;
+        const int clear_hi = a.causal ? min(u.len, p_first + 1) : u.len;
+        const int64_t clear_lo = a.window > 0 ? (int64_t)p_last - a.window + 1 : 0;
+
+        // ---- this warp's 16 tokens of every tile ----
+        const int *table = a.tables + (int64_t)u.seq * a.max_pages;
+        const auto page_of = [&](int i) {   // of the warp's group i, -1 where there is none
+            const int k0 = (tile0 + i) * TILE + warp * GROUP;
+            if (i >= count || k0 >= u.hi || k0 + GROUP <= u.lo) return -1;
+            const int pg = table[k0 >> a.c.log_page];
+            return pg >= 0 && pg < a.c.n_pages ? pg : -1;
+        };
+        int pages = page_of(lane), pages_next = -1;   // of 32 groups, and of the next 32
+        const auto page_at = [&](int i) { return __shfl_sync(0xFFFFFFFFu, pages, i & 31); };
+        const auto load = [&](int i, int pg) {
+            if (pg >= 0) {
+                const int k0 = (tile0 + i) * TILE + warp * GROUP, place = k0 & ((1 << a.c.log_page) - 1);
+                const int64_t tile = (int64_t)pg * a.c.n_kv + u.head;
+                const int64_t src = ((tile << a.c.log_page) + place) * D;
+                const uint32_t to = smem_addr(ring + (i % Sh::STAGES) * Sh::STAGE);
+                for (int j = lane; j < GROUP * Sh::CH; j += 32) {
+                    const int token = j / Sh::CH, c = j % Sh::CH;
+                    if (c < pieces) {
+                        const uint32_t off = token * DP + Sh::swizzle(token, c) * 16;
+                        copy16(to + off, a.c.k_codes + src + token * D + 16 * c);
+                        copy16(to + GROUP * DP + off, a.c.v_codes + src + token * D + 16 * c);
+                    }
+                }
+                const int64_t sc = (tile << (a.c.log_page - a.c.log_block)) + ((place + (lane & 15)) >> a.c.log_block);
+                copy4(to + 2 * GROUP * DP + 4 * lane, (lane < 16 ? a.c.k_scale : a.c.v_scale) + sc);
+            }
+            copies_end();
+        };
+        uint32_t have = 0;   // bit i % 32: group i has a page
+        int loaded = 0;
+        const auto load_next = [&]() {
+            if (loaded < count) {
+                if ((loaded & 31) == 0) {
+                    if (loaded > 0) pages = pages_next;
+                    pages_next = page_of(loaded + 32 + lane);
+                }
+                const int pg = page_at(loaded);
+                have = (have & ~(1u << (loaded & 31))) | ((pg >= 0 ? 1u : 0u) << (loaded & 31));
+                load(loaded, pg);
+            } else {
+                copies_end();
+            }
+            ++loaded;
+        };
+#pragma unroll 1
+        for (int i = 0; i < Sh::STAGES - 1; ++i) load_next();
+
+        float o[Sh::MT][NT][4];
+#pragma unroll
+        for (int i = 0; i < Sh::MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) o[i][j][0] = o[i][j][1] = o[i][j][2] = o[i][j][3] = 0.f;
+        float mx[NT][2], sum[NT][2];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) mx[j][0] = mx[j][1] = NEG, sum[j][0] = sum[j][1] = 0.f;
+
+#pragma unroll 1
+        for (int i = 0; i < count; ++i) {
+            copies_wait<Sh::STAGES - 2>();
+            __syncwarp();
+            load_next();   // into the stage that was read last
+            if (!((have >> (i & 31)) & 1)) continue;
+            const uint8_t *st = ring + (i % Sh::STAGES) * Sh::STAGE;
+            const float *scales = reinterpret_cast<const float *>(st + 2 * GROUP * DP);
+            const int k0 = (tile0 + i) * TILE + warp * GROUP;
+            // scores
+            float s[NT][4];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
+#pragma unroll
+            for (int j = 0; j < DP / 64; ++j) {
+                const uint4 ka = *reinterpret_cast<const uint4 *>(st + g * DP + Sh::swizzle(g, t + 4 * j) * 16);
+                const uint4 kb = *reinterpret_cast<const uint4 *>(st + (g + 8) * DP + Sh::swizzle(g + 8, t + 4 * j) * 16);
+                const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const uint32_t A[4] = {codes01(wa[w]), codes01(wb[w]), codes23(wa[w]), codes23(wb[w])};
+                    const int step = 4 * j + w;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int pt = 0; pt < Sh::PARTS; ++pt) {
+                            const int f = (step * NT + nt) * Sh::PARTS + pt;
+                            const uint2 b = Sh::QREG ? qreg[Sh::QREG ? f : 0] : qfrag[f * 32 + lane];
+                            mma16816(s[nt], A, b.x, b.y);
+                        }
+                }
+            }
+            float ksc[2] = {scales[g], scales[g + 8]}, vsc[2] = {scales[16 + g], scales[16 + g + 8]};
+            const float lv0 = fmaxf(log2_fast(vsc[0]), -60.f), lv1 = fmaxf(log2_fast(vsc[1]), -60.f);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                s[nt][0] *= ksc[0] * rs[nt][0], s[nt][1] *= ksc[0] * rs[nt][1];
+                s[nt][2] *= ksc[1] * rs[nt][0], s[nt][3] *= ksc[1] * rs[nt][1];
+            }
+            const bool masked = k0 + GROUP > clear_hi || k0 < clear_lo;
+            if (masked) {
+                const int ka = k0 + g, kb = k0 + g + 8;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int hi = row_hi[8 * nt + 2 * t + e], lo = row_lo[8 * nt + 2 * t + e];
+                        if (ka >= hi || ka < lo) s[nt][e] = NEG;
+                        if (kb >= hi || kb < lo) s[nt][2 + e] = NEG;
+                    }
+            }
+            // the running maximum of s + log2 vscale over the warp's tokens, by query row
+            float shrink[NT][2];
+            bool grew = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float m = fmaxf(s[nt][e] + lv0, s[nt][2 + e] + lv1);
+                    m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 4));
+                    m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 8));
+                    m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
+                    m = fmaxf(m, mx[nt][e]);
+                    shrink[nt][e] = m == NEG ? 1.f : exp2_fast(mx[nt][e] - m);
+                    grew = grew || m > mx[nt][e];
+                    mx[nt][e] = m;
+                }
+            if (__any_sync(0xFFFFFFFFu, grew)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    sum[nt][0] *= shrink[nt][0], sum[nt][1] *= shrink[nt][1];
+#pragma unroll
+                    for (int d = 0; d < Sh::MT; ++d) {
+                        o[d][nt][0] *= shrink[nt][0], o[d][nt][1] *= shrink[nt][1];
+                        o[d][nt][2] *= shrink[nt][0], o[d][nt][3] *= shrink[nt][1];
+                    }
+                }
+            }
+            uint32_t pb[NT][Sh::PARTS][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float p[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float m = mx[nt][e & 1];
+                    const float x = exp2_fast(s[nt][e] - (m == NEG ? 0.f : m - 14.f));
+                    sum[nt][e & 1] += x;
+                    p[e] = x * vsc[e >> 1];
+                    if (masked && s[nt][e] == NEG) p[e] = 0.f;   // whatever the scale of a token that is not seen
+                }
+                const uint32_t h0 = pack_half(p[0], p[1]), h1 = pack_half(p[2], p[3]);
+                pb[nt][0][0] = transposed8x8(h0), pb[nt][0][1] = transposed8x8(h1);
+                if constexpr (F32) {
+                    pb[nt][1][0] = transposed8x8(pack_rest(p[0], p[1], h0));
+                    pb[nt][1][1] = transposed8x8(pack_rest(p[2], p[3], h1));
+                }
+            }
+            // output: a lane has tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9 of channels g DP / 8 ..
+            const uint8_t *vt = st + GROUP * DP;
+            const auto times_v = [&](int mt, uint32_t w0, uint32_t w1, uint32_t w8, uint32_t w9) {   // 4 channels: tiles mt, mt + 1
+                const uint32_t a01 = __byte_perm(w0, w1, 0x5140), a23 = __byte_perm(w0, w1, 0x7362);
+                const uint32_t b01 = __byte_perm(w8, w9, 0x5140), b23 = __byte_perm(w8, w9, 0x7362);
+                const uint32_t A0[4] = {codes01(a01), codes23(a01), codes01(b01), codes23(b01)};
+                const uint32_t A1[4] = {codes01(a23), codes23(a23), codes01(b23), codes23(b23)};
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int pt = 0; pt < Sh::PARTS; ++pt) {
+                        mma16816(o[mt][nt], A0, pb[nt][pt][0], pb[nt][pt][1]);
+                        mma16816(o[mt + 1][nt], A1, pb[nt][pt][0], pb[nt][pt][1]);
+                    }
+            };
+            const int tok[4] = {2 * t, 2 * t + 1, 2 * t + 8, 2 * t + 9};
+            if constexpr (DP == 64) {
+                uint2 w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    w[e] = *reinterpret_cast<const uint2 *>(vt + tok[e] * DP + Sh::swizzle(tok[e], g >> 1) * 16 + (g & 1) * 8);
+                times_v(0, w[0].x, w[1].x, w[2].x, w[3].x);
+                times_v(2, w[0].y, w[1].y, w[2].y, w[3].y);
+            } else {
+#pragma unroll
+                for (int j = 0; j < DP / 128; ++j) {
+                    uint4 w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        w[e] = *reinterpret_cast<const uint4 *>(vt + tok[e] * DP + Sh::swizzle(tok[e], g + 8 * j) * 16);
+                    times_v(8 * j + 0, w[0].x, w[1].x, w[2].x, w[3].x);
+                    times_v(8 * j + 2, w[0].y, w[1].y, w[2].y, w[3].y);
+                    times_v(8 * j + 4, w[0].z, w[1].z, w[2].z, w[3].z);
+                    times_v(8 * j + 6, w[0].w, w[1].w, w[2].w, w[3].w);
+                }
+            }
+        }
+        copies_wait<0>();
+        __syncwarp();
+
+        // ---- the four warps' shares: each leaves its output in its ring ----
+        float *mine = reinterpret_cast<float *>(ring);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float l = sum[nt][e];
+                l += __shfl_xor_sync(0xFFFFFFFFu, l, 4);
+                l += __shfl_xor_sync(0xFFFFFFFFu, l, 8);
+                l += __shfl_xor_sync(0xFFFFFFFFu, l, 16);
+                const int r = 8 * nt + 2 * t + e;
+                if (g == 0) join_m[warp][r] = mx[nt][e], join_l[warp][r] = l;
+#pragma unroll
+                for (int d = 0; d < Sh::MT; ++d) {   // tile d holds channels 2 d, 2 d + 1 of the lane's (of 16 j + .. with DP 256)
+                    const int ch = DP == 64 ? 8 * g + 2 * d : 16 * (g + 8 * (d / 8)) + 2 * (d % 8);
+                    *reinterpret_cast<float2 *>(mine + r * DP + ch) = make_float2(o[d][nt][e], o[d][nt][2 + e]);
+                }
+            }
+        __syncthreads();
+        const bool whole = count == tiles;
+        const int first_cta = owner(unit0), last_cta = owner(unit0 + tiles - 1);
+        float *slot = part + ((int64_t)2 * blockIdx.x + (from == 0 ? 1 : 0)) * PART;
+        const auto finish = [&](int r, int d, float acc, float m, float l) {   // one value of row r
+            const int rr = u.r0 + r, qi = rr / a.group;
+            const int64_t row = (int64_t)(u.q0 + qi) * a.n_heads + u.head * a.group + rr % a.group;
+            const float y = l == 0.f ? 0.f : acc / l;   // (a sum of nothing: the row sees no token)
+            if constexpr (F32)
+                ((float *)a.out)[row * D + d] = y;
+            else
+                ((__nv_bfloat16 *)a.out)[row * D + d] = __float2bfloat16_rn(y);
+            if (d == 0 && a.lse != nullptr) a.lse[row] = l == 0.f ? NEG : (m - 14.f + log2f(l)) * 0.6931471805599453f;
+        };
+        for (int i = threadIdx.x; i < u.rows * DP; i += THREADS) {
+            const int r = i / DP, d = i % DP;
+            float m = NEG, l = 0.f, acc = 0.f;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) m = fmaxf(m, join_m[w][r]);
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) {
+                const float mw = join_m[w][r], f = mw == NEG ? 0.f : exp2_fast(mw - m);
+                if (mw == NEG && join_l[w][r] == 0.f) continue;
+                l += join_l[w][r] * f;
+                acc += reinterpret_cast<const float *>(smem + w * Sh::RING)[i] * f;
+            }
+            if (whole) {
+                if (d < D) finish(r, d, acc, m, l);
+            } else {
+                slot[r * DP + d] = acc;
+                if (d == 0) slot[ROWS * DP + r] = m, slot[ROWS * DP + ROWS + r] = l;
+            }
+        }
+        if (!whole) {
+            __threadfence();
+            __syncthreads();
+            if (threadIdx.x == 0)
+                last_one = atomicInc(reinterpret_cast<unsigned *>(a.counters) + first_cta, (unsigned)(last_cta - first_cta)) ==
+                           (unsigned)(last_cta - first_cta);
+            __syncthreads();
+            if (last_one) {
+                __threadfence();
+                for (int i = threadIdx.x; i < u.rows * DP; i += THREADS) {
+                    const int r = i / DP, d = i % DP;
+                    if (d >= D) continue;
+                    float m = NEG, l = 0.f, acc = 0.f;
+                    const auto slot_of = [&](int c) { return part + ((int64_t)2 * c + (c == first_cta ? 1 : 0)) * PART; };
+                    for (int c = first_cta; c <= last_cta; ++c) m = fmaxf(m, __ldcg(slot_of(c) + ROWS * DP + r));
+                    for (int c = first_cta; c <= last_cta; ++c) {
+                        const float *p = slot_of(c);
+                        const float mc = __ldcg(p + ROWS * DP + r), lc = __ldcg(p + ROWS * DP + ROWS + r);
+                        if (mc == NEG && lc == 0.f) continue;
+                        const float f = mc == NEG ? 0.f : exp2_fast(mc - m);
+                        l += lc * f;
+                        acc += __ldcg(p + i) * f;
+                    }
+                    finish(r, d, acc, m, l);
+                }
+            }
+        }
+        __syncthreads();   // the rings and the rows' numbers are free again
+    }
+}
+
+template <int DP, int NT, bool F32, class T> realq_status_t launch(cudaStream_t s, const KvAttnArgs &a, int sms) {
+    using Sh = Shape<DP, NT, F32>;
+    const auto kernel = decode_kernel<DP, NT, F32, T>;
+    REALQ_TRY(set_smem_limit((const void *)kernel, Sh::SMEM));
+    int per_sm = 0;
+    REALQ_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, THREADS, Sh::SMEM));
+    per_sm = std::max(1, std::min(per_sm, KV_MAX_CTAS_PER_SM));
+    Launch l("kv_attention", s);
+    kernel<<<(unsigned)(per_sm * sms), THREADS, Sh::SMEM, s>>>(a);
+    return check_launch("kv_attention");
+}
+template <int DP, bool F32, class T> realq_status_t by_rows(cudaStream_t s, const KvAttnArgs &a, int64_t rows, int sms) {
+    if (rows <= 8) return launch<DP, 1, F32, T>(s, a, sms);
+    if constexpr (DP == 256) {
+        return launch<DP, 2, F32, T>(s, a, sms);
+    } else {
+        if (rows <= 16) return launch<DP, 2, F32, T>(s, a, sms);
+        return launch<DP, 4, F32, T>(s, a, sms);
+    }
+}
+template <class T> realq_status_t by_size(cudaStream_t s, const KvAttnArgs &a, int64_t rows, int sms) {
+    constexpr bool F32 = sizeof(T) == 4;
+    if (a.c.head_dim <= 64) return by_rows<64, F32, T>(s, a, rows, sms);
+    if (a.c.head_dim <= 128) return by_rows<128, F32, T>(s, a, rows, sms);
+    return by_rows<256, F32, T>(s, a, rows, sms);
+}
+
+}  // namespace
+
+// Partial results: two a CTA of at most 32 rows of DP + 2 numbers each (16 rows of 256 + 2 are fewer).
+size_t kv_decode_ws_bytes(int head_dim, int sms) {
+    Carve c(nullptr);
+    c.take<int>(64);
+    c.take<int>(KV_MAX_CTAS_PER_SM * sms);
+    c.take<float>((size_t)2 * KV_MAX_CTAS_PER_SM * sms * 32 * (128 + 2));
+    (void)head_dim;
+    return c.off;
+}
+
+realq_status_t kv_decode(cudaStream_t s, const KvAttnArgs &args, realq_dtype_t dt, int64_t rows, void *ws, int sms) {
+    KvAttnArgs a = args;
+    Carve c(ws);
+    c.take<int>(64);
+    a.counters = c.take<int>(KV_MAX_CTAS_PER_SM * sms);
+    a.part = c.take<float>(0);
+    return dt == REALQ_BF16 ? by_size<__nv_bfloat16>(s, a, rows, sms) : by_size<float>(s, a, rows, sms);
+}
+
+}  // namespace realq
