@@ -1118,10 +1118,12 @@ realq_status_t realq_kv_read(realq_stream_t stream, const realq_kv_cache_t *cach
     return kv_read(S(stream), a, dtype);
 }
 
+static size_t kv_attention_ws_bytes() { return kAlign + kv_decode_ws_bytes(num_sms()) + kv_prompt_ws_bytes(num_sms()); }
+
 size_t realq_kv_attention_workspace_size(const realq_kv_cache_t *cache, int64_t n_seqs, int64_t T, int64_t n_heads) {
     KvView v;
     if (n_seqs <= 0 || T <= 0 || n_heads <= 0 || check_cache("kv_attention_workspace_size", cache, 0, &v) != REALQ_OK || n_heads % v.n_kv) return 0;
-    return kv_decode_ws_bytes(v.head_dim, num_sms());
+    return kv_attention_ws_bytes();
 }
 
 realq_status_t realq_kv_attention(realq_stream_t stream, const realq_kv_cache_t *cache, int64_t layer, int64_t n_seqs, int64_t T,
@@ -1145,13 +1147,23 @@ realq_status_t realq_kv_attention(realq_stream_t stream, const realq_kv_cache_t 
     if (!aligned_to(4, lengths, lse) || !aligned_to(dtype == REALQ_BF16 ? 2 : 4, (const char *)out))
         return fail(REALQ_ERR_INVALID_ARG, "kv_attention: lengths or an output not aligned to its type");
     if (T * (n_heads / a.c.n_kv) >= INT32_MAX / 2) return fail(REALQ_ERR_UNSUPPORTED, "kv_attention: T n_heads / n_kv must be below 2^30");
-    REALQ_TRY(check_ws(ws, ws_bytes, kv_decode_ws_bytes(a.c.head_dim, num_sms()), who));
+    REALQ_TRY(check_ws(ws, ws_bytes, kv_attention_ws_bytes(), who));
     a.n_seqs = (int)n_seqs, a.n_heads = (int)n_heads, a.group = (int)(n_heads / a.c.n_kv), a.causal = causal != 0;
     a.T = T, a.q = q, a.q_ld = q_ld, a.q_hs = q_hs, a.max_pages = max_pages, a.window = window;
     a.starts = starts, a.lengths = lengths, a.tables = tables, a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.out = out, a.lse = lse;
+    // Few rows and many have a kernel each, which take their sequences out of the call's; where the caller has none
+    // of many rows, one launch takes all (and serves longer ones too, 32 rows at a time).
+    char *decode_ws = static_cast<char *>(ws) + kAlign, *prompt_ws = decode_ws + kv_decode_ws_bytes(num_sms());
+    const int64_t rows = std::min(max_new, T) * a.group;
+    const int few = KV_FEW_ROWS / a.group;   // new tokens
     a.min_new = 1, a.max_new = INT32_MAX;
-    return kv_decode(S(stream), a, dtype, std::min(max_new, T) * a.group, ws, num_sms());
+    if (rows <= KV_FEW_ROWS) return kv_decode(S(stream), a, dtype, rows, decode_ws, num_sms());
+    a.min_new = few + 1;
+    REALQ_TRY(kv_prompt(S(stream), a, dtype, static_cast<int *>(ws), prompt_ws, num_sms()));
+    if (few == 0) return REALQ_OK;
+    a.min_new = 1, a.max_new = few;
+    return kv_decode(S(stream), a, dtype, KV_FEW_ROWS, decode_ws, num_sms());
 }
 
 static realq_status_t check_pages(const char *who, const realq_kv_pages_t *p, KvPagesView *v) {

@@ -220,8 +220,12 @@ struct KvAttnArgs {
     float *part;
     __device__ __forceinline__ bool takes(int m) const { return m >= min_new && m <= max_new; }
 };
-size_t kv_decode_ws_bytes(int head_dim, int sms);
+// few query rows (the new tokens' heads that share a key/value head), and many; disjoint workspaces
+constexpr int KV_FEW_ROWS = 32;
+size_t kv_decode_ws_bytes(int sms);
 realq_status_t kv_decode(cudaStream_t s, const KvAttnArgs &a, realq_dtype_t dt, int64_t rows, void *ws, int sms);
+size_t kv_prompt_ws_bytes(int sms);
+realq_status_t kv_prompt(cudaStream_t s, const KvAttnArgs &a, realq_dtype_t dt, int *err, void *ws, int sms);
 
 struct KvPagesView {
     int64_t n_pages, n_rows, max_pages;

@@ -33,43 +33,14 @@
 // wraps to zero by itself.
 #include <algorithm>
 
-#include "kernels.cuh"
+#include "kv_schedule.cuh"
 
 namespace realq {
 namespace {
 
 constexpr int WARPS = 4, THREADS = 32 * WARPS, GROUP = 16, TILE = GROUP * WARPS;
-constexpr int SEQS = 512;                 // sequences whose tile counts are held at a time
 constexpr float NEG = -INFINITY;
 
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float log2_fast(float x) {
-    float y;
-    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t hsub2(uint32_t a, uint32_t b) {
-    uint32_t d;
-    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
-    uint32_t d;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-    return d;
-}
-// what pack_half left of (lo, hi)
-__device__ __forceinline__ uint32_t pack_rest(float lo, float hi, uint32_t h) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
-    return pack_half(lo - f.x, hi - f.y);
-}
-// bytes 0 1 / 2 3 of w as two fp16 whole numbers c - 128
-__device__ __forceinline__ uint32_t codes01(uint32_t w) { return hsub2(__byte_perm(w, 0x64646464u, 0x4140), 0x64806480u); }
-__device__ __forceinline__ uint32_t codes23(uint32_t w) { return hsub2(__byte_perm(w, 0x64646464u, 0x4342), 0x64806480u); }
 __device__ __forceinline__ uint32_t transposed8x8(uint32_t x) {
     uint32_t y;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
@@ -113,81 +84,6 @@ template <int DP, int NT, bool F32> struct Shape {
     }
 };
 
-struct Unit {        // one sequence, key/value head and row tile
-    int seq, head, tile;
-    int q0, m;       // the sequence's first query token and their number
-    int len;         // cached tokens
-    int r0, rows;    // rows of the tile: r0 .. r0 + rows - 1 of m x G
-    int lo, hi;      // cached tokens that any row sees: [lo, hi)
-};
-
-// Tiles of one row tile of a sequence (at least one: rows that see nothing are written too).
-__device__ __forceinline__ void span(const KvAttnArgs &a, int m, int len, int r0, int r1, int *lo, int *hi) {
-    const int p0 = len - m + r0 / a.group, p1 = len - m + (r1 - 1) / a.group;
-    *hi = a.causal ? max(0, min(len, p1 + 1)) : len;
-    *lo = a.window > 0 ? (int)min((int64_t)*hi, max((int64_t)0, (int64_t)p0 - a.window + 1)) : 0;
-}
-__device__ __forceinline__ int tiles_of(int lo, int hi) { return hi > lo ? (hi - 1) / TILE - lo / TILE + 1 : 1; }
-
-struct Seq {
-    int q0, m, len;
-    __device__ Seq(const KvAttnArgs &a, int s) {
-        const int64_t b = a.starts[s], e = a.starts[s + 1];
-        const bool ok = b >= 0 && e > b && e <= a.T;
-        q0 = ok ? (int)b : 0, m = ok ? (int)(e - b) : 0;
-        len = (int)min((int64_t)max(a.lengths[s], 0), a.max_pages << a.c.log_page);
-        if (m > 0 && !a.takes(m)) m = 0;   // another kernel's
-    }
-};
-template <int ROWS> __device__ int64_t seq_tiles(const KvAttnArgs &a, int s) {   // of one head
-    const Seq q(a, s);
-    int64_t n = 0;
-    for (int r = 0; r < q.m * a.group; r += ROWS) {
-        int lo, hi;
-        span(a, q.m, q.len, r, min(r + ROWS, q.m * a.group), &lo, &hi);
-        n += tiles_of(lo, hi);
-    }
-    return n;
-}
-
-// The tile counts of SEQS sequences from `first` on, as a running sum (of one head).
-struct Window {
-    int first;
-    int64_t base;               // tiles of all heads before them
-    int64_t sum[SEQS + 1];
-    int64_t warp_sum[WARPS];
-};
-template <int ROWS> __device__ void fill_window(const KvAttnArgs &a, Window &w, int first, int64_t base) {
-    constexpr int PER = SEQS / THREADS;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int64_t mine[PER], total = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int s = first + threadIdx.x * PER + i;
-        mine[i] = s < a.n_seqs ? seq_tiles<ROWS>(a, s) : 0;
-        total += mine[i];
-    }
-    int64_t x = total;
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-        const int64_t y = __shfl_up_sync(0xFFFFFFFFu, x, d);
-        if (lane >= d) x += y;
-    }
-    __syncthreads();
-    if (lane == 31) w.warp_sum[warp] = x;
-    __syncthreads();
-    int64_t at = x - total;
-    for (int i = 0; i < warp; ++i) at += w.warp_sum[i];
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        w.sum[threadIdx.x * PER + i] = at;
-        at += mine[i];
-    }
-    if (threadIdx.x == THREADS - 1) w.sum[SEQS] = at;
-    if (threadIdx.x == 0) w.first = first, w.base = base;
-    __syncthreads();
-}
-
 template <int DP, int NT, bool F32, class T>
 __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
     using Sh = Shape<DP, NT, F32>;
@@ -208,57 +104,22 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
     // all tiles, and this CTA's share
     int64_t all = 0;
     for (int first = 0; first < a.n_seqs; first += SEQS) {
-        fill_window<ROWS>(a, win, first, all);
+        fill_window<ROWS, TILE, false>(a, win, first, all);
         all += win.sum[SEQS] * a.c.n_kv;
     }
-    const int64_t ctas = min((int64_t)gridDim.x, all);
-    if (blockIdx.x >= ctas) return;
-    const auto begin = [&](int64_t c) { return c * all / ctas; };
-    const auto owner = [&](int64_t x) {   // of tile x
-        int64_t c = (x * ctas + ctas - 1) / all;
-        while (c > 0 && begin(c) > x) --c;
-        while (c + 1 < ctas && begin(c + 1) <= x) ++c;
-        return (int)c;
-    };
-    int64_t at = begin(blockIdx.x);
-    const int64_t end = begin(blockIdx.x + 1);
-    if (a.n_seqs > SEQS) {
-        fill_window<ROWS>(a, win, 0, 0);
+    const Shares shares{all, min((int64_t)gridDim.x, all)};
+    if (blockIdx.x >= shares.ctas) {
+        wait_for_previous();
+        return;
     }
+    int64_t at = shares.begin(blockIdx.x);
+    const int64_t end = shares.begin(blockIdx.x + 1);
+    if (a.n_seqs > SEQS) fill_window<ROWS, TILE, false>(a, win, 0, 0);
     while (at < end) {
-        // ---- the unit that holds tile `at` ----
-        // (lengths that another stream changes meanwhile give wrong results; the loops end all the same)
-        while (at >= win.base + win.sum[SEQS] * a.c.n_kv && win.first + SEQS < a.n_seqs)
-            fill_window<ROWS>(a, win, win.first + SEQS, win.base + win.sum[SEQS] * a.c.n_kv);
         Unit u;
         int64_t unit0;   // the unit's first tile
         int tiles;
-        {
-            int lo = 0, hi = SEQS - 1;   // the last sequence that begins at or before the tile
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) >> 1;
-                if (win.base + win.sum[mid] * a.c.n_kv <= at)
-                    lo = mid;
-                else
-                    hi = mid - 1;
-            }
-            u.seq = win.first + lo;
-            const int64_t per_head = max((int64_t)1, win.sum[lo + 1] - win.sum[lo]);
-            int64_t off = at - (win.base + win.sum[lo] * a.c.n_kv);
-            u.head = (int)min(off / per_head, (int64_t)a.c.n_kv - 1);
-            unit0 = at - off + u.head * per_head;
-            off -= u.head * per_head;
-            const Seq q(a, u.seq);
-            u.q0 = q.q0, u.m = q.m, u.len = q.len;
-            const int rows_all = q.m * a.group;
-            for (u.r0 = 0, u.tile = 0;; u.r0 += ROWS, ++u.tile) {
-                u.rows = min(ROWS, rows_all - u.r0);
-                span(a, q.m, q.len, u.r0, u.r0 + u.rows, &u.lo, &u.hi);
-                tiles = tiles_of(u.lo, u.hi);
-                if (off < tiles || u.r0 + ROWS >= rows_all) break;
-                off -= tiles, unit0 += tiles;
-            }
-        }
+        locate<ROWS, TILE, false>(a, win, at, u, unit0, tiles);
         const int from = (int)min(at - unit0, (int64_t)tiles - 1);
         const int count = (int)min(end - at, (int64_t)(tiles - from));
         const int tile0 = u.lo / TILE + from;
@@ -411,7 +272,7 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
                 }
             }
             float ksc[2] = {scales[g], scales[g + 8]}, vsc[2] = {scales[16 + g], scales[16 + g + 8]};
-            const float lv0 = fmaxf(log2_fast(vsc[0]), -60.f), lv1 = fmaxf(log2_fast(vsc[1]), -60.f);
+            const float lv0 = fmaxf(log2_fast(vsc[0]), -100.f), lv1 = fmaxf(log2_fast(vsc[1]), -100.f);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 s[nt][0] *= ksc[0] * rs[nt][0], s[nt][1] *= ksc[0] * rs[nt][1];
@@ -535,7 +396,7 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
             }
         __syncthreads();
         const bool whole = count == tiles;
-        const int first_cta = owner(unit0), last_cta = owner(unit0 + tiles - 1);
+        const int first_cta = shares.owner(unit0), last_cta = shares.owner(unit0 + tiles - 1);
         float *slot = part + ((int64_t)2 * blockIdx.x + (from == 0 ? 1 : 0)) * PART;
         const auto finish = [&](int r, int d, float acc, float m, float l) {   // one value of row r
             const int rr = u.r0 + r, qi = rr / a.group;
@@ -595,6 +456,7 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
         }
         __syncthreads();   // the rings and the rows' numbers are free again
     }
+    wait_for_previous();   // (the prompts' kernel, beside which this one may run: what comes after waits for both)
 }
 
 template <int DP, int NT, bool F32, class T> realq_status_t launch(cudaStream_t s, const KvAttnArgs &a, int sms) {
@@ -605,7 +467,7 @@ template <int DP, int NT, bool F32, class T> realq_status_t launch(cudaStream_t 
     REALQ_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, THREADS, Sh::SMEM));
     per_sm = std::max(1, std::min(per_sm, KV_MAX_CTAS_PER_SM));
     Launch l("kv_attention", s);
-    kernel<<<(unsigned)(per_sm * sms), THREADS, Sh::SMEM, s>>>(a);
+    REALQ_CUDA_TRY(launch_overlapped(kernel, dim3((unsigned)(per_sm * sms)), dim3(THREADS), Sh::SMEM, s, a));
     return check_launch("kv_attention");
 }
 template <int DP, bool F32, class T> realq_status_t by_rows(cudaStream_t s, const KvAttnArgs &a, int64_t rows, int sms) {
@@ -627,19 +489,16 @@ template <class T> realq_status_t by_size(cudaStream_t s, const KvAttnArgs &a, i
 }  // namespace
 
 // Partial results: two a CTA of at most 32 rows of DP + 2 numbers each (16 rows of 256 + 2 are fewer).
-size_t kv_decode_ws_bytes(int head_dim, int sms) {
+size_t kv_decode_ws_bytes(int sms) {
     Carve c(nullptr);
-    c.take<int>(64);
     c.take<int>(KV_MAX_CTAS_PER_SM * sms);
     c.take<float>((size_t)2 * KV_MAX_CTAS_PER_SM * sms * 32 * (128 + 2));
-    (void)head_dim;
     return c.off;
 }
 
 realq_status_t kv_decode(cudaStream_t s, const KvAttnArgs &args, realq_dtype_t dt, int64_t rows, void *ws, int sms) {
     KvAttnArgs a = args;
     Carve c(ws);
-    c.take<int>(64);
     a.counters = c.take<int>(KV_MAX_CTAS_PER_SM * sms);
     a.part = c.take<float>(0);
     return dt == REALQ_BF16 ? by_size<__nv_bfloat16>(s, a, rows, sms) : by_size<float>(s, a, rows, sms);

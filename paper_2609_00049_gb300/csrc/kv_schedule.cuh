@@ -1,0 +1,215 @@
+// How the attention kernels cut their work: one unit is a sequence, a key/value
+// head and a tile of ROWS query rows (the head's query heads times the new
+// tokens, token by token); its cached tokens are taken in tiles of TILE.  All
+// units' tiles in a row are cut into one share per CTA.
+#pragma once
+
+#include "kernels.cuh"
+
+namespace realq {
+namespace {
+
+constexpr int SEQS = 512;                 // sequences whose tile counts are held at a time
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float log2_fast(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t hsub2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+    uint32_t d;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+// what pack_half left of (lo, hi)
+__device__ __forceinline__ uint32_t pack_rest(float lo, float hi, uint32_t h) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+    return pack_half(lo - f.x, hi - f.y);
+}
+// bytes 0 1 / 2 3 of w as two fp16 whole numbers c - 128
+__device__ __forceinline__ uint32_t codes01(uint32_t w) { return hsub2(__byte_perm(w, 0x64646464u, 0x4140), 0x64806480u); }
+__device__ __forceinline__ uint32_t codes23(uint32_t w) { return hsub2(__byte_perm(w, 0x64646464u, 0x4342), 0x64806480u); }
+
+struct Unit {        // one sequence, key/value head and row tile
+    int seq, head;
+    int q0, m;       // the sequence's first query token and their number
+    int len;         // cached tokens
+    int r0, rows;    // rows of the tile: r0 .. r0 + rows - 1 of m x G
+    int lo, hi;      // cached tokens that any row sees: [lo, hi)
+};
+
+// The cached tokens [lo, hi) that rows r0 .. r1 - 1 of a sequence see; their tiles (at least one: rows that see nothing
+// are written too).
+__device__ __forceinline__ void span(const KvAttnArgs &a, int m, int len, int r0, int r1, int *lo, int *hi) {
+    const int p0 = len - m + r0 / a.group, p1 = len - m + (r1 - 1) / a.group;
+    *hi = a.causal ? max(0, min(len, p1 + 1)) : len;
+    *lo = a.window > 0 ? (int)min((int64_t)*hi, max((int64_t)0, (int64_t)p0 - a.window + 1)) : 0;
+}
+template <int TILE> __device__ __forceinline__ int tiles_of(int lo, int hi) {
+    return hi > lo ? (hi - 1) / TILE - lo / TILE + 1 : 1;
+}
+
+struct Seq {
+    int q0, m, len;
+    __device__ Seq(const KvAttnArgs &a, int s) {
+        const int64_t b = a.starts[s], e = a.starts[s + 1];
+        const bool ok = b >= 0 && e > b && e <= a.T;
+        q0 = ok ? (int)b : 0, m = ok ? (int)(e - b) : 0;
+        len = (int)min((int64_t)max(a.lengths[s], 0), a.max_pages << a.c.log_page);
+        if (m > 0 && !a.takes(m)) m = 0;   // another kernel's
+    }
+};
+template <int ROWS, int TILE> __device__ __forceinline__ int row_tiles(const KvAttnArgs &a, const Seq &q, int r0) {
+    int lo, hi;
+    span(a, q.m, q.len, r0, min(r0 + ROWS, q.m * a.group), &lo, &hi);
+    return tiles_of<TILE>(lo, hi);
+}
+template <int ROWS, int TILE> __device__ int64_t seq_tiles(const KvAttnArgs &a, int s) {   // of one head
+    const Seq q(a, s);
+    int64_t n = 0;
+    for (int r = 0; r < q.m * a.group; r += ROWS) n += row_tiles<ROWS, TILE>(a, q, r);
+    return n;
+}
+
+// The tile counts of SEQS sequences from `first` on, as a running sum (of one head).
+struct Window {
+    int first;
+    int64_t base;               // tiles of all heads before them
+    int64_t sum[SEQS + 1];
+    int64_t warp_sum[16];
+};
+// All threads of the CTA call it; the first 128 add up.  A sequence's row tiles are gone
+// over by one thread, or, for prompts of many (LONG), by a warp.
+template <int ROWS, int TILE, bool LONG> __device__ void fill_window(const KvAttnArgs &a, Window &w, int first, int64_t base) {
+    constexpr int COUNT = 128, PER = SEQS / COUNT;
+    const bool counts = threadIdx.x < COUNT;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int64_t mine[PER], total = 0;
+    if constexpr (LONG) {
+        __syncthreads();
+        for (int i = warp; i < SEQS; i += blockDim.x / 32) {
+            int n = 0;
+            if (first + i < a.n_seqs) {
+                const Seq q(a, first + i);
+                for (int r = lane * ROWS; r < q.m * a.group; r += 32 * ROWS) n += row_tiles<ROWS, TILE>(a, q, r);
+                n = __reduce_add_sync(0xFFFFFFFFu, n);
+            }
+            if (lane == 0) w.sum[i] = n;
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int k = threadIdx.x * PER + i;
+        if constexpr (LONG)
+            mine[i] = counts ? w.sum[k] : 0;
+        else
+            mine[i] = counts && first + k < a.n_seqs ? seq_tiles<ROWS, TILE>(a, first + k) : 0;
+        total += mine[i];
+    }
+    int64_t x = total;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const int64_t y = __shfl_up_sync(0xFFFFFFFFu, x, d);
+        if (lane >= d) x += y;
+    }
+    __syncthreads();
+    if (lane == 31) w.warp_sum[warp] = x;
+    __syncthreads();
+    if (counts) {
+        int64_t at = x - total;
+        for (int i = 0; i < warp; ++i) at += w.warp_sum[i];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            w.sum[threadIdx.x * PER + i] = at;
+            at += mine[i];
+        }
+        if (threadIdx.x == COUNT - 1) w.sum[SEQS] = at;
+    }
+    if (threadIdx.x == 0) w.first = first, w.base = base;
+    __syncthreads();
+}
+
+// The unit that holds tile `at` (at least the window's base), where it begins and how many tiles it has.  Called by
+// whole warps.
+template <int ROWS, int TILE, bool LONG>
+__device__ __forceinline__ void locate(const KvAttnArgs &a, Window &win, int64_t at, Unit &u, int64_t &unit0, int &tiles) {
+    // (lengths that another stream changes meanwhile give wrong results; the loops end all the same)
+    while (at >= win.base + win.sum[SEQS] * a.c.n_kv && win.first + SEQS < a.n_seqs)
+        fill_window<ROWS, TILE, LONG>(a, win, win.first + SEQS, win.base + win.sum[SEQS] * a.c.n_kv);
+    int lo = 0, hi = SEQS - 1;   // the last sequence that begins at or before the tile
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (win.base + win.sum[mid] * a.c.n_kv <= at)
+            lo = mid;
+        else
+            hi = mid - 1;
+    }
+    u.seq = win.first + lo;
+    const int64_t per_head = max((int64_t)1, win.sum[lo + 1] - win.sum[lo]);
+    int64_t off = at - (win.base + win.sum[lo] * a.c.n_kv);
+    u.head = (int)min(off / per_head, (int64_t)a.c.n_kv - 1);
+    unit0 = at - off + u.head * per_head;
+    off -= u.head * per_head;
+    const Seq q(a, u.seq);
+    u.q0 = q.q0, u.m = q.m, u.len = q.len, u.r0 = 0;
+    const int rows_all = q.m * a.group, lane = threadIdx.x & 31;
+    if (LONG && rows_all > ROWS) {
+        for (;; u.r0 += 32 * ROWS) {   // 32 row tiles at a time
+            const int r = u.r0 + lane * ROWS;
+            const int n = r < rows_all ? row_tiles<ROWS, TILE>(a, q, r) : 0;
+            int x = n;
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const int y = __shfl_up_sync(0xFFFFFFFFu, x, d);
+                if (lane >= d) x += y;
+            }
+            const int sum = __shfl_sync(0xFFFFFFFFu, x, 31);
+            if (off >= sum && u.r0 + 32 * ROWS < rows_all) {
+                off -= sum, unit0 += sum;
+                continue;
+            }
+            const uint32_t over = __ballot_sync(0xFFFFFFFFu, x > off);
+            const int j = over ? __ffs(over) - 1 : (rows_all - 1 - u.r0) / ROWS;
+            const int before = __shfl_sync(0xFFFFFFFFu, x - n, j);
+            u.r0 += j * ROWS, unit0 += before;
+            break;
+        }
+        u.rows = min(ROWS, rows_all - u.r0);
+        span(a, q.m, q.len, u.r0, u.r0 + u.rows, &u.lo, &u.hi);
+        tiles = tiles_of<TILE>(u.lo, u.hi);
+        return;
+    }
+    for (;; u.r0 += ROWS) {
+        u.rows = min(ROWS, rows_all - u.r0);
+        span(a, q.m, q.len, u.r0, u.r0 + u.rows, &u.lo, &u.hi);
+        tiles = tiles_of<TILE>(u.lo, u.hi);
+        if (off < tiles || u.r0 + ROWS >= rows_all) break;
+        off -= tiles, unit0 += tiles;
+    }
+}
+
+// Even shares of `all` tiles among `ctas` CTAs.
+struct Shares {
+    int64_t all, ctas;
+    __device__ __forceinline__ int64_t begin(int64_t c) const { return c * all / ctas; }
+    __device__ __forceinline__ int owner(int64_t x) const {   // of tile x
+        int64_t c = (x * ctas + ctas - 1) / all;
+        while (c > 0 && begin(c) > x) --c;
+        while (c + 1 < ctas && begin(c + 1) <= x) ++c;
+        return (int)c;
+    }
+};
+
+}  // namespace
+}  // namespace realq
