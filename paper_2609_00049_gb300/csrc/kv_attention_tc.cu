@@ -6,10 +6,10 @@
 // the new tokens) as two tiles of 128, and goes over their cached tokens in tiles
 // of 128.  Per tile of tokens the tensor cores take 4 x 512 cycles for the two row
 // tiles' two products (at 128 channels), which bounds the kernel; beside them fit
-//   - four producer warps: codes from the pages to fp16 in shared memory (exact:
-//     a byte permute to 1024 + c, one subtraction of 1152), a tile ahead in
-//     registers, K as the K-major and V as the MN-major B operand of the same layout: boxes of 64
-//     channels, a token's 128-byte row swizzled;
+//   - a loader warp: page numbers, bulk copies of the codes into shared memory, the scales;
+//   - four converter warps: codes to fp16 (exact: a byte permute to 1024 + c, one
+//     subtraction of 1152), K as the K-major and V as the MN-major B operand of the
+//     same layout: boxes of 64 channels, a token's 128-byte row swizzled;
 //   - two softmax warpgroups, one to a row tile, a thread to a row: while one works
 //     on its scores the tensor cores work for the other;
 //   - one warp that issues the products.
@@ -30,6 +30,7 @@
 // them in order.  Work is cut as for few rows (kv_schedule.cuh), partial results
 // joined by the warpgroup that ends last.
 #include <algorithm>
+#include <type_traits>
 
 #include "kv_schedule.cuh"
 #include "tc.cuh"
@@ -38,7 +39,11 @@ namespace realq {
 namespace {
 
 constexpr uint32_t FULL = 0xFFFFFFFFu;
-constexpr int SOFT_WARPS = 8, PROD_WARPS = 4, THREADS = 32 * (SOFT_WARPS + PROD_WARPS + 1);
+constexpr int SOFT_WARPS = 8, CONV_WARPS = 4, THREADS = 512;
+constexpr int MMA_WARP = SOFT_WARPS + CONV_WARPS, LOAD_WARP = MMA_WARP + 1;   // (two more are idle)
+constexpr int RAW_SLOTS = 3;             // half tiles of codes on their way
+// registers of a thread by role: 128 x (2 x 168 + 88 + 88) = 512 x 128, what the block starts with
+constexpr int SOFT_REGS = 168, CONV_REGS = 88, REST_REGS = 88;
 constexpr int SLOTS = 4;                 // of block scales
 constexpr float NEG = -INFINITY, LIFT = 6.f, SLACK = 8.f;
 
@@ -52,17 +57,20 @@ template <int DP, bool F32> struct Shape {
     static constexpr int Q_BYTES = 128 * DP * 2;                                // one row tile, one part
     static constexpr int KV_BYTES = KT * DP * 2;
     static constexpr int SLOT_BYTES = 4 * KT * 4;
-    static constexpr int RING = NM * PARTS * Q_BYTES, SCALES = RING + 2 * STAGES * KV_BYTES, BARS = SCALES + SLOTS * SLOT_BYTES;
+    static constexpr int HALF = KT / 2, RAW_BYTES = HALF * DP;                  // codes come by half tiles
+    static constexpr int RING = NM * PARTS * Q_BYTES, RAW = RING + 2 * STAGES * KV_BYTES, SCALES = RAW + RAW_SLOTS * RAW_BYTES,
+                         BARS = SCALES + SLOTS * SLOT_BYTES;
     static constexpr int SMEM = BARS + 256 + 1024;
-    static constexpr int NI = (KT / 8) * BOXES / PROD_WARPS;                    // 16-byte pieces of a tile to a producer
     static constexpr int PART = 128 * (DP + 2);                                 // numbers of a row tile's partial result
     // TMEM columns
     static constexpr int S(int i) { return i * KT; }
     static constexpr int O(int i) { return NM * KT + i * DP; }
     static constexpr int LO(int i) { return NM * (KT + DP) + i * (KT / 2); }
-    static_assert(SMEM <= 232448 && NM * (KT + DP + (F32 ? KT / 2 : 0)) <= 512, "shared and tensor memory");
+    static_assert(SMEM + 512 <= 232448 && (int)sizeof(Window) <= RAW_SLOTS * RAW_BYTES && NM * (KT + DP + (F32 ? KT / 2 : 0)) <= 512, "shared and tensor memory");
 };
 
+template <int N> __device__ __forceinline__ void more_regs() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void fewer_regs() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void group_sync(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
 __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t *r) {
@@ -71,6 +79,55 @@ __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t *r) {
         "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
         "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
+}
+
+// two fp32 values in one register pair
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 halves(uint64_t x) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ void tmem_ld_x32(uint32_t taddr, uint32_t (&r)[32]) {   // complete after tmem_wait_ld
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr));
+}
+
+// `bytes` consecutive bytes global -> shared, counted on `bar` (all three multiples of 16)
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
+
+// tc::mbar_wait by the SM's clock.  Gives up after about two seconds.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *abort) {
+    if (tc::mbar_try_wait(bar, parity)) return true;
+    const int64_t t0 = clock64();
+    for (uint32_t it = 1;; ++it) {
+        if (tc::mbar_try_wait(bar, parity)) return true;
+        if ((it & 63u) == 0 && (*abort || clock64() - t0 > 4000000000ll)) return false;
+    }
 }
 
 struct Ring {   // stage and phase of something that goes round
@@ -82,22 +139,22 @@ struct Ring {   // stage and phase of something that goes round
     }
 };
 
-// The units of a CTA's share, one after the other; every role walks them for itself.
+// The units of a CTA's share, one after the other.  Each role has its own in shared memory (registers are
+// short), which one of its threads moves on.
 template <int ROWS, int KT> struct Walk {
-    const KvAttnArgs &a;
     Unit u;
     int tiles, from, count;    // of the unit, the share's first and how many
     int64_t unit0, at, end;
-    __device__ Walk(const KvAttnArgs &args, const Unit &u0, int64_t first, int tiles0, int64_t at0, int64_t end0)
-        : a(args), u(u0), tiles(tiles0), unit0(first), at(at0), end(end0) {
-        set();
-    }
     __device__ __forceinline__ void set() {
         from = (int)min(at - unit0, (int64_t)tiles - 1);
         count = (int)min(end - at, (int64_t)(tiles - from));
     }
+    __device__ void start(const Unit &u0, int64_t first, int tiles0, int64_t at0, int64_t end0) {
+        u = u0, tiles = tiles0, unit0 = first, at = at0, end = end0;
+        set();
+    }
     __device__ __forceinline__ bool more() const { return at < end; }
-    __device__ void next() {
+    __device__ __forceinline__ void next(const KvAttnArgs &a) {
         at += count;
         if (at >= end) return;
         unit0 += tiles;
@@ -125,32 +182,40 @@ template <int ROWS, int KT> struct Walk {
 };
 
 template <int DP, bool F32, class T>
-__global__ void __launch_bounds__(THREADS, 1) prompt_kernel(KvAttnArgs a, int *err) {
+__global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constant__ KvAttnArgs a, int *err) {
     using Sh = Shape<DP, F32>;
     constexpr int NM = Sh::NM, KT = Sh::KT, ROWS = Sh::ROWS;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    __shared__ Window win;
+    Window &win = *reinterpret_cast<Window *>(smem + Sh::RAW);   // (before the first codes come)
     __shared__ int last_one[2];
+    __shared__ Shares shares;
+    __shared__ Walk<ROWS, KT> walks[5];
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + Sh::BARS);
     uint64_t *k_full = bars, *k_empty = bars + 2, *v_full = bars + 4, *v_empty = bars + 6;
     uint64_t *q_full = bars + 8, *s_full = bars + 10, *p_full = bars + 12, *o_full = bars + 14, *done = bars + 16;
-    uint32_t *tslot = reinterpret_cast<uint32_t *>(bars + 17);
+    uint64_t *raw_full = bars + 17, *raw_empty = raw_full + RAW_SLOTS;
+    uint32_t *tslot = reinterpret_cast<uint32_t *>(raw_empty + RAW_SLOTS);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tslot + 1);
+    uint32_t *raw_there = tslot + 2;   // of each slot's groups of 16 tokens, those that have a page
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int D = a.c.head_dim;
 
     dependents_may_start();
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
-            tc::mbar_init(tc::smem_u32(k_full + i), 32 * PROD_WARPS);
-            tc::mbar_init(tc::smem_u32(v_full + i), 32 * PROD_WARPS);
+            tc::mbar_init(tc::smem_u32(k_full + i), CONV_WARPS + 1);   // and the scales
+            tc::mbar_init(tc::smem_u32(v_full + i), CONV_WARPS);
             tc::mbar_init(tc::smem_u32(k_empty + i), 1);
             tc::mbar_init(tc::smem_u32(v_empty + i), 1);
-            tc::mbar_init(tc::smem_u32(q_full + i), 128);
+            tc::mbar_init(tc::smem_u32(q_full + i), 4);
             tc::mbar_init(tc::smem_u32(s_full + i), 1);
-            tc::mbar_init(tc::smem_u32(p_full + i), 128);
+            tc::mbar_init(tc::smem_u32(p_full + i), 4);
             tc::mbar_init(tc::smem_u32(o_full + i), 1);
+        }
+        for (int i = 0; i < RAW_SLOTS; ++i) {
+            tc::mbar_init(tc::smem_u32(raw_full + i), 1);
+            tc::mbar_init(tc::smem_u32(raw_empty + i), CONV_WARPS);
         }
         tc::mbar_init(tc::smem_u32(done), 1);
         *abort_flag = 0;
@@ -162,15 +227,21 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(KvAttnArgs a, int *e
         fill_window<ROWS, KT, true>(a, win, first, all);
         all += win.sum[SEQS] * a.c.n_kv;
     }
-    const Shares shares{all, min((int64_t)gridDim.x, all)};
-    if (blockIdx.x >= shares.ctas) return;
+    const Shares sh{all, min((int64_t)gridDim.x, all)};
+    if (blockIdx.x >= sh.ctas) return;
     if (a.n_seqs > SEQS) fill_window<ROWS, KT, true>(a, win, 0, 0);
-    const int64_t at0 = shares.begin(blockIdx.x), end0 = shares.begin(blockIdx.x + 1);
-    Unit u0;
-    int64_t first0;
-    int tiles0;
-    locate<ROWS, KT, true>(a, win, at0, u0, first0, tiles0);
-    Walk<ROWS, KT> w(a, u0, first0, tiles0, at0, end0);
+    {
+        const int64_t at0 = sh.begin(blockIdx.x);
+        Unit u0;
+        int64_t first0;
+        int tiles0;
+        locate<ROWS, KT, true>(a, win, at0, u0, first0, tiles0);
+        fence_async_smem();   // (the codes' copies come over win)
+        __syncthreads();
+        if (threadIdx.x < 5) walks[threadIdx.x].start(u0, first0, tiles0, at0, sh.begin(blockIdx.x + 1));
+        if (threadIdx.x == 0) shares = sh;
+    }
+    Walk<ROWS, KT> &w = walks[warp == LOAD_WARP ? 4 : warp >> 2];
 
     if (warp == 0) tc::tmem_alloc(tc::smem_u32(tslot), 512);
     tc::fence_before_sync();
@@ -181,6 +252,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(KvAttnArgs a, int *e
 
     if (warp < SOFT_WARPS) {
         // ---------------- softmax: thread = row of row tile i ----------------
+        more_regs<SOFT_REGS>();
         const int i = warp >> 2, row = threadIdx.x & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_at = tmem + lanes + Sh::S(i), o_at = tmem + lanes + Sh::O(i), lo_at = tmem + lanes + Sh::LO(i);
@@ -188,106 +260,129 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(KvAttnArgs a, int *e
         uint8_t *qs = smem + i * Sh::PARTS * Sh::Q_BYTES;
         uint32_t s_phase = 0, o_phase = 0;
         int slot = 0;
-        // the row's query into shared memory; returns what its scores are multiplied by
+        // The row tile's queries into shared memory; returns what this thread's row's scores are multiplied by.  LANES
+        // lanes take a row, 8 values each, a warp its own 32 rows.
+        constexpr int LANES = DP / 8, AT_ONCE = 32 / LANES, BATCH = 4;
+        const bool wide = ((reinterpret_cast<uintptr_t>(a.q) | (uintptr_t)(a.q_ld * sizeof(T)) | (uintptr_t)(a.q_hs * sizeof(T))) & 15) == 0;
         const auto load_q = [&](const Unit &u) {
-            const int r = u.r0 + 128 * i + row;
-            const bool in = 128 * i + row < u.rows;
-            const int qi = in ? r / a.group : 0;
-            const T *q = (const T *)a.q + (int64_t)(u.q0 + qi) * a.q_ld + (int64_t)(u.head * a.group + (in ? r % a.group : 0)) * a.q_hs;
-            const bool wide = ((reinterpret_cast<uintptr_t>(a.q) | (uintptr_t)(a.q_ld * sizeof(T)) | (uintptr_t)(a.q_hs * sizeof(T))) & 15) == 0;
-            float top = 0.f;
-            const auto values = [&](int d, float (&x)[8]) {   // q[d .. d + 7]
-                if (!in) {
+            const int d = lane % LANES * 8, sub = lane / LANES;
+            float mine = 0.f;
+            int rw = (warp & 3) * 32 + sub;                             // row of the tile: token qi, head g of the group
+            int qi = (u.r0 + 128 * i + rw) / a.group, g = u.r0 + 128 * i + rw - qi * a.group;
+#pragma unroll 1
+            for (int j0 = 0; j0 < LANES; j0 += BATCH) {
+                uint4 raw[BATCH][F32 ? 2 : 1];
+                const int rw0 = rw;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = 0.f;
-                } else if (wide) {
-                    if constexpr (F32) {
-                        const float4 v0 = *reinterpret_cast<const float4 *>(q + d), v1 = *reinterpret_cast<const float4 *>(q + d + 4);
-                        x[0] = v0.x, x[1] = v0.y, x[2] = v0.z, x[3] = v0.w, x[4] = v1.x, x[5] = v1.y, x[6] = v1.z, x[7] = v1.w;
-                    } else {
-                        const uint4 v = *reinterpret_cast<const uint4 *>(q + d);
-                        const uint32_t h[4] = {v.x, v.y, v.z, v.w};
+                for (int j = 0; j < BATCH; ++j) {
+                    const T *q = (const T *)a.q + (int64_t)(u.q0 + qi) * a.q_ld + (int64_t)(u.head * a.group + g) * a.q_hs + d;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            x[2 * e] = __uint_as_float(h[e] << 16), x[2 * e + 1] = __uint_as_float(h[e] & 0xFFFF0000u);
+                    for (int e = 0; e < (F32 ? 2 : 1); ++e) raw[j][e] = make_uint4(0, 0, 0, 0);
+                    if (128 * i + rw < u.rows && d < D) {
+                        if (wide) {
+#pragma unroll
+                            for (int e = 0; e < (F32 ? 2 : 1); ++e) raw[j][e] = reinterpret_cast<const uint4 *>(q)[e];
+                        } else if constexpr (F32) {
+                            const uint32_t *w = reinterpret_cast<const uint32_t *>(q);
+                            raw[j][0] = make_uint4(w[0], w[1], w[2], w[3]), raw[j][1] = make_uint4(w[4], w[5], w[6], w[7]);
+                        } else {
+                            const uint16_t *w = reinterpret_cast<const uint16_t *>(q);
+                            raw[j][0] = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+                        }
                     }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = load_as_float(q, d + e);
+                    rw += AT_ONCE;
+                    for (g += AT_ONCE; g >= a.group; g -= a.group) ++qi;
                 }
-            };
-#pragma unroll 2
-            for (int d = 0; d < D; d += 8) {
-                float x[8];
-                values(d, x);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
-            }
-            int k = 0;
-            if (top > 0.f && top < INFINITY) k = 14 - ilogbf(top);
-            const float sign = a.scale_log2 < 0.f ? -1.f : 1.f;   // the scores' factor is to be positive
-            const float up0 = sign * scalbnf(1.f, k / 2), up1 = scalbnf(1.f, k - k / 2);
-#pragma unroll 2
-            for (int d = 0; d < D; d += 8) {
-                float x[8];
-                values(d, x);
-                uint32_t h[4];
-                const uint32_t to = (uint32_t)(d >> 6) * 16384u + row * 128 + ((((d >> 3) & 7) ^ (row & 7)) << 4);
+                for (int j = 0; j < BATCH; ++j) {
+                    float x[8];
+                    if constexpr (F32) {
+                        const uint32_t w[8] = {raw[j][0].x, raw[j][0].y, raw[j][0].z, raw[j][0].w, raw[j][1].x, raw[j][1].y, raw[j][1].z, raw[j][1].w};
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = x[e] * up0 * up1;
+                        for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(w[e]);
+                    } else {
+                        const uint32_t w[4] = {raw[j][0].x, raw[j][0].y, raw[j][0].z, raw[j][0].w};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) h[e] = pack_half(x[2 * e], x[2 * e + 1]);
-                *reinterpret_cast<uint4 *>(qs + to) = make_uint4(h[0], h[1], h[2], h[3]);
-                if constexpr (F32) {
+                        for (int e = 0; e < 4; ++e) x[2 * e] = __uint_as_float(w[e] << 16), x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+                    }
+                    float top = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) h[e] = pack_rest(x[2 * e], x[2 * e + 1], h[e]);
-                    *reinterpret_cast<uint4 *>(qs + Sh::Q_BYTES + to) = make_uint4(h[0], h[1], h[2], h[3]);
+                    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
+#pragma unroll
+                    for (int o = 1; o < LANES; o *= 2) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
+                    // times 2^k: the largest lies in [2^14, 2^15) after that (a row below 2^-112 a little lower)
+                    const int e = (int)(__float_as_uint(top) >> 23), k = e == 0 || e == 255 ? 0 : min(126, 141 - e);
+                    float up = __uint_as_float((uint32_t)(127 + k) << 23);
+                    const float back = fabsf(a.scale_log2) * __uint_as_float((uint32_t)(127 - k) << 23);
+                    if (a.scale_log2 < 0.f) up = -up;   // (the scores' factor is to be positive)
+                    const float theirs = __shfl_sync(FULL, back, (lane - (j0 + j) * AT_ONCE) * LANES & 31);
+                    if (lane / AT_ONCE == j0 + j) mine = theirs;
+                    if (d < D) {
+                        uint32_t h[4];
+                        const int r = rw0 + j * AT_ONCE;
+                        uint8_t *to = qs + (d >> 6) * 16384 + r * 128 + ((((d >> 3) & 7) ^ (r & 7)) << 4);
+#pragma unroll
+                        for (int n = 0; n < 8; ++n) x[n] *= up;
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) h[n] = pack_half(x[2 * n], x[2 * n + 1]);
+                        *reinterpret_cast<uint4 *>(to) = make_uint4(h[0], h[1], h[2], h[3]);
+                        if constexpr (F32) {
+#pragma unroll
+                            for (int n = 0; n < 4; ++n) h[n] = pack_rest(x[2 * n], x[2 * n + 1], h[n]);
+                            *reinterpret_cast<uint4 *>(to + Sh::Q_BYTES) = make_uint4(h[0], h[1], h[2], h[3]);
+                        }
+                    }
                 }
             }
             fence_async_smem();
-            tc::mbar_arrive(tc::smem_u32(q_full + i));
-            return fabsf(a.scale_log2) * scalbnf(1.f, -(k / 2)) * scalbnf(1.f, -(k - k / 2));
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(tc::smem_u32(q_full + i));
+            return mine;
         };
         float rs = 0.f;
         bool loaded = false;
+        const auto advance = [&]() {
+            group_sync(1 + i);
+            if (row == 0) w.next(a);
+            group_sync(1 + i);
+        };
         while (w.more() && ok) {
-            const Unit u = w.u;
-            const int from = w.from, count = w.count, tiles = w.tiles;
-            const int64_t unit0 = w.unit0;
-            if (128 * i >= u.rows) {   // the row tile is empty: its tiles of tokens pass by
+            const int count = w.count;
+            if (128 * i >= w.u.rows) {   // the row tile is empty: its tiles of tokens pass by
                 slot = (slot + count) & (SLOTS - 1);
-                w.next();
+                advance();
                 continue;
             }
-            if (!loaded) rs = load_q(u);
+            if (!loaded) rs = load_q(w.u);
             const float factor = rs;
-            const int r = u.r0 + 128 * i + row, qi = r / a.group, p = u.len - u.m + qi;
-            const bool in = 128 * i + row < u.rows;
-            const int row_hi = !in ? 0 : (a.causal ? min(u.len, p + 1) : u.len);
-            const int row_lo = a.window > 0 ? (int)max((int64_t)0, (int64_t)p - a.window + 1) : 0;
+            const bool in = 128 * i + row < w.u.rows;
+            int row_hi = 0, row_lo = 0;
+            int64_t out_row;
+            {
+                const int r = w.u.r0 + 128 * i + row, qi = r / a.group, p = w.u.len - w.u.m + qi;
+                if (in) row_hi = a.causal ? min(w.u.len, p + 1) : w.u.len;
+                if (a.window > 0) row_lo = (int)max((int64_t)0, (int64_t)p - a.window + 1);
+                out_row = (int64_t)(w.u.q0 + qi) * a.n_heads + w.u.head * a.group + (r - qi * a.group);
+            }
             const int all_hi = __reduce_min_sync(FULL, in ? row_hi : INT32_MAX), all_lo = __reduce_max_sync(FULL, in ? row_lo : 0);
+            int k0 = (w.u.lo / KT + w.from) * KT;
             float m = NEG, l = 0.f, bad = 0.f;   // bad: NaN once a value that the row sees is
-            for (int t = 0; t < count && ok; ++t, slot = (slot + 1) & (SLOTS - 1)) {
-                ok = __all_sync(FULL, tc::mbar_wait(tc::smem_u32(s_full + i), s_phase, abort_flag));
+            for (int t = 0; t < count && ok; ++t, k0 += KT, slot = (slot + 1) & (SLOTS - 1)) {
+                ok = __all_sync(FULL, bar_wait(tc::smem_u32(s_full + i), s_phase, abort_flag));
                 s_phase ^= 1u;
                 if (!ok) break;
                 tc::fence_after_sync();
-                const int k0 = (u.lo / KT + from + t) * KT;
                 const bool masked = k0 + KT > all_hi || k0 < all_lo;
                 const float *sc = reinterpret_cast<const float *>(smem + Sh::SCALES + slot * Sh::SLOT_BYTES);
                 const auto seen = [&](int j) { return k0 + j < row_hi && k0 + j >= row_lo; };
                 // the largest S ks r + lv
                 float top = NEG;
+                const auto largest = [&](auto masks, auto fines, int c, uint32_t(&v)[32]) {
+                    if constexpr (masks) {
 #pragma unroll
-                for (int c = 0; c < KT; c += 32) {
-                    uint32_t v[32];
-                    tc::tmem_ld_32x32b_x32(s_at + c, v);
-                    if (masked) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (!seen(c + j)) v[j] = 0xFF800000u;
+                        for (int j = 0; j < 32; ++j) v[j] = seen(c + j) ? v[j] : 0xFF800000u;
                     }
-                    if (!fine) {
+                    if constexpr (!fines) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             const float4 b = reinterpret_cast<const float4 *>(sc)[c / 16 + h];
@@ -306,7 +401,39 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(KvAttnArgs a, int *e
                             top = fmaxf(top, fmaf(__uint_as_float(v[j + 3]), ks.w * factor, lv.w));
                         }
                     }
-                }
+                };
+                using yes = std::true_type;
+                using no = std::false_type;
+                // Short loops: the roles' code together has to stay in the instruction cache.  Two reads of 32 columns are
+                // under way in turn.
+                const auto over_scores = [&](auto f) {
+                    uint32_t v0[32], v1[32];
+                    tmem_ld_x32(s_at, v0);
+#pragma unroll 1
+                    for (int c = 0; c < KT; c += 64) {
+                        tc::tmem_wait_ld();
+                        tmem_ld_x32(s_at + c + 32, v1);
+                        f(c, v0);
+                        tc::tmem_wait_ld();
+                        if (c + 64 < KT) tmem_ld_x32(s_at + c + 64, v0);
+                        f(c + 32, v1);
+                    }
+                };
+                const auto over_few = [&](auto f) {   // (the rarer kinds of tiles)
+                    uint32_t v[32];
+#pragma unroll 1
+                    for (int c = 0; c < KT; c += 32) {
+                        tmem_ld_x32(s_at + c, v);
+                        tc::tmem_wait_ld();
+                        f(c, v);
+                    }
+                };
+                if (fine)
+                    over_few([&](int c, uint32_t(&v)[32]) { largest(yes{}, yes{}, c, v); });
+                else if (masked)
+                    over_few([&](int c, uint32_t(&v)[32]) { largest(yes{}, no{}, c, v); });
+                else
+                    over_scores([&](int c, uint32_t(&v)[32]) { largest(no{}, no{}, c, v); });
                 const bool grew = top > (m == NEG ? NEG : m + SLACK);
                 if (__any_sync(FULL, grew)) {
                     const float now = fmaxf(m, top), f = now == NEG ? 1.f : exp2_fast(m - now);
@@ -324,74 +451,87 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(KvAttnArgs a, int *e
                     }
                 }
                 const float base = LIFT - (m == NEG ? 0.f : m);
+                // (32 columns of P go over 16 that have been read)
+                const auto weights = [&](auto masks, auto fines, int c, uint32_t(&v)[32]) {
+                    {
+                        uint32_t hi[16];
+                        [[maybe_unused]] uint32_t lo[F32 ? 16 : 1];
+                        if constexpr (!fines) {
 #pragma unroll
-                for (int c = 0; c < KT; c += 32) {
-                    uint32_t v[32], hi[16], lo[F32 ? 16 : 1];
-                    tc::tmem_ld_32x32b_x32(s_at + c, v);
-                    if (!fine) {
+                            for (int h = 0; h < 2; ++h) {
+                                const float4 b = reinterpret_cast<const float4 *>(sc)[c / 16 + h];
+                                const float c1 = b.x * factor, c0 = b.y + base;
+                                const uint64_t c11 = pair(c1, c1), c00 = pair(c0, c0);
+                                uint64_t part2 = 0;
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const float4 b = reinterpret_cast<const float4 *>(sc)[c / 16 + h];
-                            const float c1 = b.x * factor, c0 = b.y + base;
-                            float part = 0.f;
-#pragma unroll
-                            for (int j = 16 * h; j < 16 * h + 16; j += 2) {
-                                float x0 = fmaf(__uint_as_float(v[j]), c1, c0), x1 = fmaf(__uint_as_float(v[j + 1]), c1, c0);
-                                if (masked) {
-                                    if (!seen(c + j)) x0 = NEG;
-                                    if (!seen(c + j + 1)) x1 = NEG;
+                                for (int j = 16 * h; j < 16 * h + 16; j += 2) {
+                                    float2 x = halves(fma2(pair(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), c11, c00));
+                                    if constexpr (masks) {
+                                        x.x = seen(c + j) ? x.x : NEG;
+                                        x.y = seen(c + j + 1) ? x.y : NEG;
+                                    }
+                                    x.x = exp2_fast(x.x), x.y = exp2_fast(x.y);
+                                    part2 = add2(part2, pair(x.x, x.y));
+                                    hi[j / 2] = pack_half(x.x, x.y);
+                                    if constexpr (F32) lo[j / 2] = pack_rest(x.x, x.y, hi[j / 2]);
                                 }
-                                x0 = exp2_fast(x0), x1 = exp2_fast(x1);
-                                part += x0 + x1;
-                                hi[j / 2] = pack_half(x0, x1);
-                                if constexpr (F32) lo[j / 2] = pack_rest(x0, x1, hi[j / 2]);
+                                const float2 ph = halves(part2);
+                                const float part = ph.x + ph.y;
+                                if (!masks || part != 0.f)   // (unseen tokens' scales may be anything)
+                                    l = fmaf(part, b.z, l), bad = fmaf(part, b.w, bad);
                             }
-                            if (!(masked && part == 0.f))   // (unseen tokens' scales may be anything)
-                                l = fmaf(part, b.z, l), bad = fmaf(part, b.w, bad);
-                        }
-                    } else {
+                        } else {
 #pragma unroll
-                        for (int j = 0; j < 32; j += 4) {
-                            const float4 ks = *reinterpret_cast<const float4 *>(sc + c + j), lv = *reinterpret_cast<const float4 *>(sc + KT + c + j);
-                            const float4 iv = *reinterpret_cast<const float4 *>(sc + 2 * KT + c + j);
-                            float x[4] = {fmaf(__uint_as_float(v[j]), ks.x * factor, lv.x + base), fmaf(__uint_as_float(v[j + 1]), ks.y * factor, lv.y + base),
-                                          fmaf(__uint_as_float(v[j + 2]), ks.z * factor, lv.z + base), fmaf(__uint_as_float(v[j + 3]), ks.w * factor, lv.w + base)};
-                            const float4 nv = *reinterpret_cast<const float4 *>(sc + 3 * KT + c + j);
-                            const float inv[4] = {iv.x, iv.y, iv.z, iv.w}, nan[4] = {nv.x, nv.y, nv.z, nv.w};
+                            for (int j = 0; j < 32; j += 4) {
+                                const float4 ks = *reinterpret_cast<const float4 *>(sc + c + j), lv = *reinterpret_cast<const float4 *>(sc + KT + c + j);
+                                const float4 iv = *reinterpret_cast<const float4 *>(sc + 2 * KT + c + j), nv = *reinterpret_cast<const float4 *>(sc + 3 * KT + c + j);
+                                float x[4] = {fmaf(__uint_as_float(v[j]), ks.x * factor, lv.x + base), fmaf(__uint_as_float(v[j + 1]), ks.y * factor, lv.y + base),
+                                              fmaf(__uint_as_float(v[j + 2]), ks.z * factor, lv.z + base), fmaf(__uint_as_float(v[j + 3]), ks.w * factor, lv.w + base)};
+                                const float inv[4] = {iv.x, iv.y, iv.z, iv.w}, nan[4] = {nv.x, nv.y, nv.z, nv.w};
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                if (masked && !seen(c + j + e)) x[e] = NEG;
-                                x[e] = exp2_fast(x[e]);
-                                if (!(masked && x[e] == 0.f)) l = fmaf(x[e], inv[e], l), bad = fmaf(x[e], nan[e], bad);
+                                for (int e = 0; e < 4; ++e) {
+                                    x[e] = exp2_fast(seen(c + j + e) ? x[e] : NEG);
+                                    const bool some = x[e] != 0.f;
+                                    l = fmaf(x[e], some ? inv[e] : 0.f, l), bad = fmaf(x[e], some ? nan[e] : 0.f, bad);
+                                }
+                                hi[j / 2] = pack_half(x[0], x[1]), hi[j / 2 + 1] = pack_half(x[2], x[3]);
+                                if constexpr (F32) lo[j / 2] = pack_rest(x[0], x[1], hi[j / 2]), lo[j / 2 + 1] = pack_rest(x[2], x[3], hi[j / 2 + 1]);
                             }
-                            hi[j / 2] = pack_half(x[0], x[1]), hi[j / 2 + 1] = pack_half(x[2], x[3]);
-                            if constexpr (F32) lo[j / 2] = pack_rest(x[0], x[1], hi[j / 2]), lo[j / 2 + 1] = pack_rest(x[2], x[3], hi[j / 2 + 1]);
                         }
+                        tmem_st_x16(s_at + c / 2, hi);
+                        if constexpr (F32) tmem_st_x16(lo_at + c / 2, lo);
                     }
-                    tmem_st_x16(s_at + c / 2, hi);
-                    if constexpr (F32) tmem_st_x16(lo_at + c / 2, lo);
-                }
+                };
+                if (fine)
+                    over_few([&](int c, uint32_t(&v)[32]) { weights(yes{}, yes{}, c, v); });
+                else if (masked)
+                    over_few([&](int c, uint32_t(&v)[32]) { weights(yes{}, no{}, c, v); });
+                else
+                    over_scores([&](int c, uint32_t(&v)[32]) { weights(no{}, no{}, c, v); });
                 tc::tmem_wait_st();
                 tc::fence_before_sync();
-                tc::mbar_arrive(tc::smem_u32(p_full + i));
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(tc::smem_u32(p_full + i));
             }
             if (!ok) break;
+            const bool whole = count == w.tiles, begins = w.from == 0;
+            int first_cta = 0, last_cta = 0;
+            if (!whole) first_cta = shares.owner(w.unit0), last_cta = shares.owner(w.unit0 + w.tiles - 1);
             // the next unit's queries while the last products run (this one's have been read: its last scores are there)
-            w.next();
+            advance();
             loaded = w.more() && 128 * i < w.u.rows;
             if (loaded) rs = load_q(w.u);
-            ok = __all_sync(FULL, tc::mbar_wait(tc::smem_u32(o_full + i), o_phase, abort_flag));
+            ok = __all_sync(FULL, bar_wait(tc::smem_u32(o_full + i), o_phase, abort_flag));
             o_phase ^= 1u;
             if (!ok) break;
             tc::fence_after_sync();
 
-            const int64_t out_row = (int64_t)(u.q0 + qi) * a.n_heads + u.head * a.group + r % a.group;
             const bool aligned = (reinterpret_cast<uintptr_t>(a.out) & 15) == 0;
-            const auto put = [&](int d, const float (&y)[4]) {   // out[d .. d + 3]
+            const auto put = [&](int d, const float (&y)[8]) {   // out[d .. d + 7]
                 T *o = (T *)a.out + out_row * D + d;
                 if (!aligned) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
+                    for (int e = 0; e < 8; ++e) {
                         if constexpr (F32)
                             o[e] = y[e];
                         else
@@ -399,36 +539,40 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(KvAttnArgs a, int *e
                     }
                 } else if constexpr (F32) {
                     *reinterpret_cast<float4 *>(o) = make_float4(y[0], y[1], y[2], y[3]);
+                    *reinterpret_cast<float4 *>(o + 4) = make_float4(y[4], y[5], y[6], y[7]);
                 } else {
-                    const __nv_bfloat162 h0 = __floats2bfloat162_rn(y[0], y[1]), h1 = __floats2bfloat162_rn(y[2], y[3]);
-                    *reinterpret_cast<uint2 *>(o) = make_uint2(*reinterpret_cast<const uint32_t *>(&h0), *reinterpret_cast<const uint32_t *>(&h1));
+                    uint32_t h[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const __nv_bfloat162 b = __floats2bfloat162_rn(y[2 * e], y[2 * e + 1]);
+                        h[e] = *reinterpret_cast<const uint32_t *>(&b);
+                    }
+                    *reinterpret_cast<uint4 *>(o) = make_uint4(h[0], h[1], h[2], h[3]);
                 }
             };
             const auto put_lse = [&](float mm, float ll) {
                 if (a.lse != nullptr) a.lse[out_row] = ll == 0.f ? NEG : (mm - LIFT + log2f(ll)) * 0.6931471805599453f;
             };
-            const bool whole = count == tiles;
-            const int first_cta = whole ? 0 : shares.owner(unit0), last_cta = whole ? 0 : shares.owner(unit0 + tiles - 1);
             const auto slot_of = [&](int c, bool begins) { return a.part + ((int64_t)(2 * c + (begins ? 1 : 0)) * NM + i) * Sh::PART; };
-            float *mine = slot_of(blockIdx.x, from == 0);
-            const float inv = l == 0.f ? 0.f : 1.f / l;   // (a row that sees nothing: zeros)
+            float *mine = slot_of(blockIdx.x, begins);
+            const float inv = 1.f / l;
 #pragma unroll 1
             for (int c = 0; c < D; c += 16) {
                 uint32_t v[16];
                 tc::tmem_ld_32x32b_x16(o_at + c, v);
                 tc::tmem_wait_ld();
 #pragma unroll
-                for (int j = 0; j < 16; j += 4) {
-                    float y[4];
+                for (int j = 0; j < 16; j += 8) {
+                    float y[8];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) y[e] = __uint_as_float(v[j + e]) + bad;
+                    for (int e = 0; e < 8; ++e) y[e] = __uint_as_float(v[j + e]) + bad;
                     if (whole) {
-                        if (l == 0.f) y[0] = y[1] = y[2] = y[3] = 0.f;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) y[e] *= inv;
+                        for (int e = 0; e < 8; ++e) y[e] = l == 0.f ? 0.f : y[e] * inv;   // (a row that sees nothing: zeros)
                         if (in) put(c + j, y);
                     } else {
-                        reinterpret_cast<float4 *>(mine)[(c + j) / 4 * 128 + row] = make_float4(y[0], y[1], y[2], y[3]);
+                        float4 *to = reinterpret_cast<float4 *>(mine) + (c + j) / 4 * 128 + row;
+                        to[0] = make_float4(y[0], y[1], y[2], y[3]), to[128] = make_float4(y[4], y[5], y[6], y[7]);
                     }
                 }
             }
@@ -455,114 +599,151 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(KvAttnArgs a, int *e
                 ll += mc == NEG ? lc * 0.f : lc * exp2_fast(mc - mm);   // (a NaN stays one)
             }
             const float all_inv = ll == 0.f ? 0.f : 1.f / ll;
-            for (int d = 0; d < D; d += 4) {
-                float y[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int d = 0; d < D; d += 8) {
+                float y[8] = {};
                 for (int c = first_cta; c <= last_cta; ++c) {
                     const float *s = slot_of(c, c == first_cta);
                     const float mc = __ldcg(s + 128 * DP + row), lc = __ldcg(s + 128 * DP + 128 + row);
                     if (lc == 0.f) continue;
                     const float f = mc == NEG ? 0.f : exp2_fast(mc - mm);
-                    const float4 v = __ldcg(reinterpret_cast<const float4 *>(s) + d / 4 * 128 + row);
-                    y[0] += v.x * f, y[1] += v.y * f, y[2] += v.z * f, y[3] += v.w * f;
+                    const float4 *p4 = reinterpret_cast<const float4 *>(s) + d / 4 * 128 + row;
+                    const float4 v0 = __ldcg(p4), v1 = __ldcg(p4 + 128);
+                    y[0] += v0.x * f, y[1] += v0.y * f, y[2] += v0.z * f, y[3] += v0.w * f;
+                    y[4] += v1.x * f, y[5] += v1.y * f, y[6] += v1.z * f, y[7] += v1.w * f;
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] *= all_inv;
+                for (int e = 0; e < 8; ++e) y[e] *= all_inv;
                 if (in) put(d, y);
             }
             if (in) put_lse(mm, ll);
         }
         if (!ok) *abort_flag = 1;
-    } else if (warp < SOFT_WARPS + PROD_WARPS) {
-        // ---------------- producers: codes -> fp16 ----------------
-        const int pw = warp - SOFT_WARPS, ptid = threadIdx.x - 32 * SOFT_WARPS;
-        const int pieces = D / 16, token = lane & 7, piece0 = lane >> 3;
-        const bool fine = a.c.log_block < 4;
-        const int my_token = fine ? ptid : 16 * ptid;   // whose scales this thread brings
-        Ring ring(Sh::STAGES);
-        int slot = 0;
+    } else if (warp < SOFT_WARPS + CONV_WARPS) {
+        // ---------------- converters: codes -> fp16, half a tile of K or V at a time ----------------
+        fewer_regs<CONV_REGS>();
+        // Eight lanes take four pieces of 16 channels of two neighbouring tokens, in different boxes where there are
+        // several: neither the reading nor the writing (rows of odd and even tokens swizzled apart) meets in a bank.
+        const int cw = warp - SOFT_WARPS, ptid = threadIdx.x - 32 * SOFT_WARPS, piece = lane & 3, sel = (lane >> 2) & 1;
+        const int token0 = 8 * cw + 2 * (lane >> 3) + sel, pieces = D / 16;
+        Ring ring(Sh::STAGES), raw(RAW_SLOTS);
         while (w.more() && ok) {
-            const Unit &u = w.u;
-            const int tile0 = u.lo / KT + w.from;
-            const int *table = a.tables + (int64_t)u.seq * a.max_pages;
-            const auto page_of = [&](int tile) {   // of the tile's 8 tokens `lane`
-                const int k0 = tile * KT + 8 * lane;
-                if (lane >= KT / 8 || k0 >= u.hi || k0 + 8 <= u.lo) return -1;
-                const int pg = table[k0 >> a.c.log_page];
-                return pg >= 0 && pg < a.c.n_pages ? pg : -1;
-            };
-            const auto load = [&](const uint8_t *codes, int tile, int pages, uint4 (&x)[Sh::NI]) {
-#pragma unroll
-                for (int j = 0; j < Sh::NI; ++j) {
-                    const int item = pw + PROD_WARPS * j, grp = item / Sh::BOXES, piece = item % Sh::BOXES * 4 + piece0;
-                    const int pg = __shfl_sync(FULL, pages, grp);
-                    const int place = (tile * KT + 8 * grp) & ((1 << a.c.log_page) - 1);
-                    x[j] = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
-                    if (pg >= 0 && piece < pieces)
-                        x[j] = __ldg(reinterpret_cast<const uint4 *>(
-                            codes + ((((int64_t)pg * a.c.n_kv + u.head) << a.c.log_page) + place + token) * D + 16 * piece));
-                }
-            };
-            const auto store = [&](uint8_t *to, const uint4 (&x)[Sh::NI]) {
-#pragma unroll
-                for (int j = 0; j < Sh::NI; ++j) {
-                    const int item = pw + PROD_WARPS * j, grp = item / Sh::BOXES, box = item % Sh::BOXES;
-                    if (box * 4 + piece0 >= pieces) continue;
-                    uint8_t *line = to + box * (KT * 128) + (8 * grp + token) * 128;
-                    *reinterpret_cast<uint4 *>(line + (((2 * piece0) ^ token) << 4)) =
-                        make_uint4(codes01(x[j].x), codes23(x[j].x), codes01(x[j].y), codes23(x[j].y));
-                    *reinterpret_cast<uint4 *>(line + (((2 * piece0 + 1) ^ token) << 4)) =
-                        make_uint4(codes01(x[j].z), codes23(x[j].z), codes01(x[j].w), codes23(x[j].w));
-                }
-            };
-            float ks = 0.f, vs = 0.f;
-            bool there = false;
-            const auto load_scales = [&](int tile, int pages) {
-                const int pg = __shfl_sync(FULL, pages, (my_token >> 3) & 31);
-                there = my_token < KT && pg >= 0;
-                if (there) {
-                    const int place = (tile * KT + my_token) & ((1 << a.c.log_page) - 1);
-                    const int64_t at = (((int64_t)pg * a.c.n_kv + u.head) << (a.c.log_page - a.c.log_block)) + (place >> a.c.log_block);
-                    ks = __ldg(a.c.k_scale + at), vs = __ldg(a.c.v_scale + at);
-                }
-            };
-            uint4 kx[Sh::NI], vx[Sh::NI];
-            int pages = page_of(tile0);
-            load(a.c.k_codes, tile0, pages, kx);
-            load_scales(tile0, pages);
-            for (int t = 0; t < w.count; ++t, ring.next(), slot = (slot + 1) & (SLOTS - 1)) {
-                const int next_pages = t + 1 < w.count ? page_of(tile0 + t + 1) : -1;
-                load(a.c.v_codes, tile0 + t, pages, vx);
-                ok = __all_sync(FULL, tc::mbar_wait(tc::smem_u32(k_empty + ring.s), ring.phase ^ 1u, abort_flag));
+            const int count = w.count;
+#pragma unroll 1
+            for (int h = 0; h < 4 * count; ++h) {   // K's two halves, V's two halves
+                const bool is_v = h & 2;
+                if (!(h & 1)) ok = __all_sync(FULL, bar_wait(tc::smem_u32((is_v ? v_empty : k_empty) + ring.s), ring.phase ^ 1u, abort_flag));
+                if (ok) ok = __all_sync(FULL, bar_wait(tc::smem_u32(raw_full + raw.s), raw.phase, abort_flag));
                 if (!ok) break;
-                tc::fence_after_sync();
-                store(smem + Sh::RING + ring.s * Sh::KV_BYTES, kx);
-                if (my_token < KT) {   // (the slot's last readers are behind the products that emptied this stage)
-                    float *sc = reinterpret_cast<float *>(smem + Sh::SCALES + slot * Sh::SLOT_BYTES);
-                    // a scale below 2^-100 counts as that; tokens without a page weigh nothing
-                    const bool nan = there && vs != vs;   // (its part in the sum stays: the scores are not concerned)
-                    const float lv = !there ? NEG : (nan ? 0.f : fmaxf(log2_fast(vs), -100.f)), iv = !there ? 0.f : exp2_fast(-lv);
-                    const float k = there ? ks : 0.f, nv = nan ? vs : 0.f;
-                    if (fine)
-                        sc[my_token] = k, sc[KT + my_token] = lv, sc[2 * KT + my_token] = iv, sc[3 * KT + my_token] = nv;
-                    else
-                        reinterpret_cast<float4 *>(sc)[ptid] = make_float4(k, lv, iv, nv);
+                const uint8_t *from = smem + Sh::RAW + raw.s * Sh::RAW_BYTES;
+                uint8_t *to = smem + Sh::RING + ((is_v ? Sh::STAGES : 0) + ring.s) * Sh::KV_BYTES + (h & 1) * Sh::HALF * 128;
+                const uint32_t there = raw_there[raw.s];
+#pragma unroll 1
+                for (int token = token0; token < Sh::HALF; token += 8 * CONV_WARPS)
+#pragma unroll
+                    for (int b = 0; b < Sh::BOXES; ++b) {
+                        const int box = Sh::BOXES > 1 ? b ^ sel : 0, pc = 4 * box + piece;
+                        if (pc < pieces) {
+                            uint4 x = *reinterpret_cast<const uint4 *>(from + token * D + 16 * pc);
+                            if (!((there >> (token >> 4)) & 1u)) x = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
+                            uint8_t *line = to + box * (KT * 128) + token * 128;
+                            *reinterpret_cast<uint4 *>(line + (((2 * piece) ^ (token & 7)) << 4)) =
+                                make_uint4(codes01(x.x), codes23(x.x), codes01(x.y), codes23(x.y));
+                            *reinterpret_cast<uint4 *>(line + (((2 * piece + 1) ^ (token & 7)) << 4)) =
+                                make_uint4(codes01(x.z), codes23(x.z), codes01(x.w), codes23(x.w));
+                        }
+                    }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    tc::mbar_arrive(tc::smem_u32(raw_empty + raw.s));
+                    if (h & 1) tc::mbar_arrive(tc::smem_u32((is_v ? v_full : k_full) + ring.s));
                 }
-                fence_async_smem();
-                tc::mbar_arrive(tc::smem_u32(k_full + ring.s));
-                load(a.c.k_codes, tile0 + t + 1, next_pages, kx);
-                load_scales(tile0 + t + 1, next_pages);
-                ok = __all_sync(FULL, tc::mbar_wait(tc::smem_u32(v_empty + ring.s), ring.phase ^ 1u, abort_flag));
-                if (!ok) break;
-                tc::fence_after_sync();
-                store(smem + Sh::RING + (Sh::STAGES + ring.s) * Sh::KV_BYTES, vx);
-                fence_async_smem();
-                tc::mbar_arrive(tc::smem_u32(v_full + ring.s));
-                pages = next_pages;
+                raw.next();
+                if ((h & 3) == 3) ring.next();
             }
-            if (ok) w.next();
+            group_sync(3);
+            if (ptid == 0 && ok) w.next(a);
+            group_sync(3);
         }
         if (!ok) *abort_flag = 1;
     } else {
+        fewer_regs<REST_REGS>();
+        if (warp == LOAD_WARP) {
+        // ---------------- loader: pages, codes by bulk copies of 16 tokens, scales ----------------
+        const bool fine = a.c.log_block < 4;
+        constexpr int GROUPS = Sh::HALF / 16;
+        Ring kring(Sh::STAGES), raw(RAW_SLOTS);
+        uint32_t fills = 0;
+        int slot = 0;
+        while (w.more() && ok) {
+            const int count = w.count, lo = w.u.lo, hi = w.u.hi, head = w.u.head;
+            const int *table = a.tables + (int64_t)w.u.seq * a.max_pages;
+            const int base = (lo / KT + w.from) * KT;
+            const auto page_of = [&](int t) {   // of the tile's 16 tokens `lane`
+                const int k0 = base + t * KT + 16 * lane;
+                return t < count && lane < 2 * GROUPS && k0 < hi && k0 + 16 > lo ? __ldg(table + (k0 >> a.c.log_page)) : -1;
+            };
+            int page = page_of(0), next_page = page_of(1);
+#pragma unroll 1
+            for (int t = 0; t < count && ok; ++t, kring.next(), slot = (slot + 1) & (SLOTS - 1)) {
+                const bool good = page >= 0 && page < a.c.n_pages;
+                const uint32_t there = __ballot_sync(FULL, good);
+                const int k0 = base + t * KT + 16 * lane, place = k0 & ((1 << a.c.log_page) - 1);
+                const int64_t tile = (int64_t)page * a.c.n_kv + head;
+                const int64_t at = ((tile << a.c.log_page) + place) * D;
+#pragma unroll 1
+                for (int h = 0; h < 4 && ok; ++h, raw.next()) {
+                    ok = __all_sync(FULL, bar_wait(tc::smem_u32(raw_empty + raw.s), raw.phase ^ 1u, abort_flag));
+                    if (!ok) break;
+                    const uint32_t mine = there >> ((h & 1) * GROUPS) & ((1u << GROUPS) - 1), full = tc::smem_u32(raw_full + raw.s);
+                    if (lane == 0) {
+                        raw_there[raw.s] = mine;
+                        tc::mbar_arrive_expect_tx(full, __popc(mine) * 16 * D);
+                    }
+                    ++fills;
+                    __syncwarp();
+                    if (good && lane / GROUPS == (h & 1))
+                        bulk_load(tc::smem_u32(smem + Sh::RAW + raw.s * Sh::RAW_BYTES + (lane % GROUPS) * 16 * D), (h & 2 ? a.c.v_codes : a.c.k_codes) + at,
+                                  16 * D, full);
+                    if (h == 0) {   // the tile's scales (the slot's last readers are behind what emptied the stages)
+                        float *sc = reinterpret_cast<float *>(smem + Sh::SCALES + slot * Sh::SLOT_BYTES);
+#pragma unroll 1
+                        for (int n = lane; n < (fine ? KT : KT / 16); n += 32) {
+                            const int token = fine ? n : 16 * n;
+                            const int pg = __shfl_sync(fine ? FULL : (1u << (KT / 16)) - 1, page, token >> 4);
+                            float ks = 0.f, lv = NEG, iv = 0.f, nv = 0.f;   // tokens without a page weigh nothing
+                            if (pg >= 0 && pg < a.c.n_pages) {
+                                const int pl = (base + t * KT + token) & ((1 << a.c.log_page) - 1);
+                                const int64_t s = (((int64_t)pg * a.c.n_kv + head) << (a.c.log_page - a.c.log_block)) + (pl >> a.c.log_block);
+                                ks = __ldg(a.c.k_scale + s);
+                                const float vs = __ldg(a.c.v_scale + s);
+                                const bool nan = vs != vs;   // (its part in the sum stays: the scores are not concerned)
+                                nv = nan ? vs : 0.f;
+                                lv = nan ? 0.f : fmaxf(log2_fast(vs), -100.f), iv = exp2_fast(-lv);   // (a scale below 2^-100 counts as that)
+                            }
+                            if (fine)
+                                sc[n] = ks, sc[KT + n] = lv, sc[2 * KT + n] = iv, sc[3 * KT + n] = nv;
+                            else
+                                reinterpret_cast<float4 *>(sc)[n] = make_float4(ks, lv, iv, nv);
+                        }
+                        __syncwarp();
+                        if (lane == 0) tc::mbar_arrive(tc::smem_u32(k_full + kring.s));
+                    }
+                }
+                page = next_page;
+                next_page = page_of(t + 2);
+            }
+            __syncwarp();
+            if (ok && lane == 0) w.next(a);
+            __syncwarp();
+        }
+        if (!ok) {   // copies under way land before the CTA ends
+            *abort_flag = 1;
+            int never = 0;
+            for (uint32_t k = fills > RAW_SLOTS ? fills - RAW_SLOTS : 0; k < fills; ++k)
+                tc::mbar_wait(tc::smem_u32(raw_full + k % RAW_SLOTS), k / RAW_SLOTS & 1u, &never, 100000000ull);
+        }
+        } else if (warp == MMA_WARP) {
         // ---------------- products (the whole warp waits, one lane issues) ----------------
         const uint32_t idesc_s = tc::idesc_f16_f32(128, KT), idesc_o = tc::idesc_f16_f32(128, 0) | ((uint32_t)(D >> 3) << 17) | (1u << 16);
         const uint32_t base = tc::smem_u32(smem);
@@ -570,65 +751,74 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(KvAttnArgs a, int *e
         const uint64_t k_desc = tc::smem_desc(base + Sh::RING, 16, 1024, tc::SW_128B);
         const uint64_t v_desc = tc::smem_desc(base + Sh::RING + Sh::STAGES * Sh::KV_BYTES, KT * 128, 1024, tc::SW_128B);
         const int steps = D / 16;
-        uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+        uint32_t phases = 0;   // bit i: of q_full, bit 2 + i: of p_full
         Ring kr(Sh::STAGES), vr(Sh::STAGES);
         const auto wait = [&](uint64_t *bar, uint32_t phase) {
-            if (ok) ok = __all_sync(FULL, tc::mbar_wait(tc::smem_u32(bar), phase, abort_flag));
+            if (ok) ok = __all_sync(FULL, bar_wait(tc::smem_u32(bar), phase, abort_flag));
             if (ok) tc::fence_after_sync();
         };
         const auto scores = [&](int i) {   // S_i = Q_i K^T of the K stage
             if (tc::elect_one()) {
+#pragma unroll 1
                 for (int p = 0; p < Sh::PARTS; ++p) {
                     const uint64_t qd = q_desc + (uint32_t)((i * Sh::PARTS + p) * Sh::Q_BYTES >> 4);
                     const uint64_t kd = k_desc + (uint32_t)(kr.s * Sh::KV_BYTES >> 4);
-#pragma unroll 4
-                    for (int k = 0; k < steps; ++k)
-                        tc::mma_f16_ss(tmem + Sh::S(i), qd + (k & 3) * 2 + (k >> 2) * 1024, kd + (k & 3) * 2 + (k >> 2) * (KT * 8), idesc_s,
-                                       (p > 0 || k > 0) ? 1u : 0u);
+#pragma unroll
+                    for (int k = 0; k < DP / 16; ++k)
+                        if (k < steps)
+                            tc::mma_f16_ss(tmem + i * KT, qd + (k & 3) * 2 + (k >> 2) * 1024, kd + (k & 3) * 2 + (k >> 2) * (KT * 8), idesc_s,
+                                           (p > 0 || k > 0) ? 1u : 0u);
                 }
                 tc::mma_commit(tc::smem_u32(s_full + i));
             }
             __syncwarp();
         };
+        const auto outputs = [&](int i, bool first, bool last) {   // O_i += P_i V of the V stage
+            if (tc::elect_one()) {
+#pragma unroll 1
+                for (int p = 0; p < Sh::PARTS; ++p) {
+                    const uint64_t vd = v_desc + (uint32_t)(vr.s * Sh::KV_BYTES >> 4);
+                    const uint32_t pa = tmem + (p == 0 ? Sh::S(i) : Sh::LO(i));
+#pragma unroll
+                    for (int k = 0; k < KT / 16; ++k)
+                        tc::mma_f16_ts(tmem + Sh::O(i), pa + k * 8, vd + k * 128, idesc_o, (k > 0 || p > 0 || !first) ? 1u : 0u);
+                }
+                if (last) tc::mma_commit(tc::smem_u32(o_full + i));
+            }
+            __syncwarp();
+        };
         while (w.more() && ok) {
             const int nm = w.u.rows > 128 ? 2 : 1, count = w.count;
-            for (int i = 0; i < nm; ++i) {
-                wait(q_full + i, q_phase[i]);
-                q_phase[i] ^= 1u;
-                if (i == 0) wait(k_full + kr.s, kr.phase);
-                if (ok) scores(i);
-            }
-            for (int t = 0; t < count && ok; ++t) {
-                if (tc::elect_one()) tc::mma_commit(tc::smem_u32(k_empty + kr.s));   // (the scores of this tile are issued)
-                __syncwarp();
-                kr.next();
-                wait(v_full + vr.s, vr.phase);
+            // step t: the outputs of tile t (none at -1), the scores of tile t + 1
+#pragma unroll 1
+            for (int t = -1; t < count && ok; ++t) {
+                if (t >= 0) wait(v_full + vr.s, vr.phase);
+#pragma unroll 1
                 for (int i = 0; i < nm && ok; ++i) {
-                    wait(p_full + i, p_phase[i]);
-                    p_phase[i] ^= 1u;
-                    if (!ok) break;
-                    if (tc::elect_one()) {
-                        const uint64_t vd = v_desc + (uint32_t)(vr.s * Sh::KV_BYTES >> 4);
-#pragma unroll
-                        for (int p = 0; p < Sh::PARTS; ++p) {
-                            const uint32_t pa = tmem + (p == 0 ? Sh::S(i) : Sh::LO(i));
-#pragma unroll
-                            for (int k = 0; k < KT / 16; ++k)
-                                tc::mma_f16_ts(tmem + Sh::O(i), pa + k * 8, vd + k * 128, idesc_o, (t > 0 || p > 0 || k > 0) ? 1u : 0u);
-                        }
-                        if (t + 1 == count) tc::mma_commit(tc::smem_u32(o_full + i));
+                    if (t < 0) {
+                        wait(q_full + i, phases >> i & 1u);
+                        phases ^= 1u << i;
+                    } else {
+                        wait(p_full + i, phases >> (2 + i) & 1u);
+                        phases ^= 4u << i;
+                        if (ok) outputs(i, t == 0, t + 1 == count);
                     }
-                    __syncwarp();
                     if (t + 1 < count) {
                         if (i == 0) wait(k_full + kr.s, kr.phase);
                         if (ok) scores(i);
                     }
                 }
-                if (ok && tc::elect_one()) tc::mma_commit(tc::smem_u32(v_empty + vr.s));
+                if (ok && tc::elect_one()) {
+                    if (t >= 0) tc::mma_commit(tc::smem_u32(v_empty + vr.s));
+                    if (t + 1 < count) tc::mma_commit(tc::smem_u32(k_empty + kr.s));
+                }
                 __syncwarp();
-                vr.next();
+                if (t >= 0) vr.next();
+                if (t + 1 < count) kr.next();
             }
-            if (ok) w.next();
+            __syncwarp();
+            if (ok && lane == 0) w.next(a);
+            __syncwarp();
         }
         if (!ok) *abort_flag = 1;
         // every product issued has retired before TMEM is freed
@@ -636,6 +826,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(KvAttnArgs a, int *e
         __syncwarp();
         int never = 0;
         tc::mbar_wait(tc::smem_u32(done), 0u, &never, 100000000ull);
+        }
     }
     __syncwarp();
     if (!ok && lane == 0) atomicOr(err, (int)ST_TIMEOUT);
