@@ -7,7 +7,7 @@
 // of 128.  Per tile of tokens the tensor cores take 4 x 512 cycles for the two row
 // tiles' two products (at 128 channels), which bounds the kernel; beside them fit
 //   - a loader warp: page numbers, bulk copies of the codes into shared memory, the scales;
-//   - four converter warps: codes to fp16 (exact: a byte permute to 1024 + c, one
+//   - eight converter warps, four for K and four for V: codes to fp16 (exact: a byte permute to 1024 + c, one
 //     subtraction of 1152), K as the K-major and V as the MN-major B operand of the
 //     same layout: boxes of 64 channels, a token's 128-byte row swizzled;
 //   - two softmax warpgroups, one to a row tile, a thread to a row: while one works
@@ -39,11 +39,11 @@ namespace realq {
 namespace {
 
 constexpr uint32_t FULL = 0xFFFFFFFFu;
-constexpr int SOFT_WARPS = 8, CONV_WARPS = 4, THREADS = 512;
-constexpr int MMA_WARP = SOFT_WARPS + CONV_WARPS, LOAD_WARP = MMA_WARP + 1;   // (two more are idle)
+constexpr int SOFT_WARPS = 8, CONV_WARPS = 4;   // (converters: four for K and four for V)
+constexpr int MMA_WARP = SOFT_WARPS + 2 * CONV_WARPS, LOAD_WARP = MMA_WARP + 1, THREADS = 32 * (MMA_WARP + 4);   // (two are idle)
 constexpr int RAW_SLOTS = 3;             // half tiles of codes on their way
-// registers of a thread by role: 128 x (2 x 168 + 88 + 88) = 512 x 128, what the block starts with
-constexpr int SOFT_REGS = 168, CONV_REGS = 88, REST_REGS = 88;
+// registers of a thread by role: 128 x (2 x 136 + 2 x 64 + 80) = 640 x 96, what the block starts with
+constexpr int SOFT_REGS = 136, CONV_REGS = 64, REST_REGS = 80;
 constexpr int SLOTS = 4;                 // of block scales
 constexpr float NEG = -INFINITY, LIFT = 6.f, SLACK = 8.f;
 
@@ -120,12 +120,24 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
                  : "memory");
 }
 
-// tc::mbar_wait by the SM's clock.  Gives up after about two seconds.
+// tc::mbar_wait by the SM's clock, the thread asleep meanwhile (a warp that polls takes issue slots from the others).
+// Gives up after about two seconds.
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(1000000u)   // ns, at most
+        : "memory");
+    return ok != 0;
+}
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *abort) {
-    if (tc::mbar_try_wait(bar, parity)) return true;
+    if (try_wait(bar, parity)) return true;
     const int64_t t0 = clock64();
     for (uint32_t it = 1;; ++it) {
-        if (tc::mbar_try_wait(bar, parity)) return true;
+        if (try_wait(bar, parity)) return true;
         if ((it & 63u) == 0 && (*abort || clock64() - t0 > 4000000000ll)) return false;
     }
 }
@@ -190,7 +202,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
     Window &win = *reinterpret_cast<Window *>(smem + Sh::RAW);   // (before the first codes come)
     __shared__ int last_one[2];
     __shared__ Shares shares;
-    __shared__ Walk<ROWS, KT> walks[5];
+    __shared__ Walk<ROWS, KT> walks[6];
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + Sh::BARS);
     uint64_t *k_full = bars, *k_empty = bars + 2, *v_full = bars + 4, *v_empty = bars + 6;
     uint64_t *q_full = bars + 8, *s_full = bars + 10, *p_full = bars + 12, *o_full = bars + 14, *done = bars + 16;
@@ -238,10 +250,10 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
         locate<ROWS, KT, true>(a, win, at0, u0, first0, tiles0);
         fence_async_smem();   // (the codes' copies come over win)
         __syncthreads();
-        if (threadIdx.x < 5) walks[threadIdx.x].start(u0, first0, tiles0, at0, sh.begin(blockIdx.x + 1));
+        if (threadIdx.x < 6) walks[threadIdx.x].start(u0, first0, tiles0, at0, sh.begin(blockIdx.x + 1));
         if (threadIdx.x == 0) shares = sh;
     }
-    Walk<ROWS, KT> &w = walks[warp == LOAD_WARP ? 4 : warp >> 2];
+    Walk<ROWS, KT> &w = walks[warp == LOAD_WARP ? 5 : warp >> 2];
 
     if (warp == 0) tc::tmem_alloc(tc::smem_u32(tslot), 512);
     tc::fence_before_sync();
@@ -618,52 +630,54 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
             if (in) put_lse(mm, ll);
         }
         if (!ok) *abort_flag = 1;
-    } else if (warp < SOFT_WARPS + CONV_WARPS) {
-        // ---------------- converters: codes -> fp16, half a tile of K or V at a time ----------------
+    } else if (warp < MMA_WARP) {
+        // ---------------- converters of K or of V: codes -> fp16, half a tile at a time ----------------
         fewer_regs<CONV_REGS>();
         // Eight lanes take four pieces of 16 channels of two neighbouring tokens, in different boxes where there are
         // several: neither the reading nor the writing (rows of odd and even tokens swizzled apart) meets in a bank.
-        const int cw = warp - SOFT_WARPS, ptid = threadIdx.x - 32 * SOFT_WARPS, piece = lane & 3, sel = (lane >> 2) & 1;
+        const bool is_v = warp >= SOFT_WARPS + CONV_WARPS;
+        const int cw = warp & (CONV_WARPS - 1), piece = lane & 3, sel = (lane >> 2) & 1;
         const int token0 = 8 * cw + 2 * (lane >> 3) + sel, pieces = D / 16;
+        const int to0 = token0 * 128 + (((2 * piece) ^ (token0 & 7)) << 4), to1 = token0 * 128 + (((2 * piece + 1) ^ (token0 & 7)) << 4);
+        uint8_t *const stages = smem + Sh::RING + (is_v ? Sh::STAGES * Sh::KV_BYTES : 0);
+        uint64_t *const empty = is_v ? v_empty : k_empty, *const filled = is_v ? v_full : k_full;
         Ring ring(Sh::STAGES), raw(RAW_SLOTS);
+        if (is_v) raw.next(), raw.next();      // halves come in the order K, K, V, V
         while (w.more() && ok) {
             const int count = w.count;
 #pragma unroll 1
-            for (int h = 0; h < 4 * count; ++h) {   // K's two halves, V's two halves
-                const bool is_v = h & 2;
-                if (!(h & 1)) ok = __all_sync(FULL, bar_wait(tc::smem_u32((is_v ? v_empty : k_empty) + ring.s), ring.phase ^ 1u, abort_flag));
+            for (int h = 0; h < 2 * count; ++h) {
+                if (!(h & 1)) ok = __all_sync(FULL, bar_wait(tc::smem_u32(empty + ring.s), ring.phase ^ 1u, abort_flag));
                 if (ok) ok = __all_sync(FULL, bar_wait(tc::smem_u32(raw_full + raw.s), raw.phase, abort_flag));
                 if (!ok) break;
-                const uint8_t *from = smem + Sh::RAW + raw.s * Sh::RAW_BYTES;
-                uint8_t *to = smem + Sh::RING + ((is_v ? Sh::STAGES : 0) + ring.s) * Sh::KV_BYTES + (h & 1) * Sh::HALF * 128;
+                const uint8_t *from = smem + Sh::RAW + raw.s * Sh::RAW_BYTES + token0 * D + 16 * piece;
+                uint8_t *to = stages + ring.s * Sh::KV_BYTES + (h & 1) * Sh::HALF * 128;
                 const uint32_t there = raw_there[raw.s];
-#pragma unroll 1
-                for (int token = token0; token < Sh::HALF; token += 8 * CONV_WARPS)
+#pragma unroll
+                for (int i = 0; i < Sh::HALF / (8 * CONV_WARPS); ++i)
 #pragma unroll
                     for (int b = 0; b < Sh::BOXES; ++b) {
-                        const int box = Sh::BOXES > 1 ? b ^ sel : 0, pc = 4 * box + piece;
-                        if (pc < pieces) {
-                            uint4 x = *reinterpret_cast<const uint4 *>(from + token * D + 16 * pc);
-                            if (!((there >> (token >> 4)) & 1u)) x = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
-                            uint8_t *line = to + box * (KT * 128) + token * 128;
-                            *reinterpret_cast<uint4 *>(line + (((2 * piece) ^ (token & 7)) << 4)) =
-                                make_uint4(codes01(x.x), codes23(x.x), codes01(x.y), codes23(x.y));
-                            *reinterpret_cast<uint4 *>(line + (((2 * piece + 1) ^ (token & 7)) << 4)) =
-                                make_uint4(codes01(x.z), codes23(x.z), codes01(x.w), codes23(x.w));
+                        const int box = Sh::BOXES > 1 ? b ^ sel : 0, skip = i * 8 * CONV_WARPS;
+                        if (4 * box + piece < pieces) {
+                            uint4 x = *reinterpret_cast<const uint4 *>(from + skip * D + 64 * box);
+                            if (!((there >> ((token0 + skip) >> 4)) & 1u)) x = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
+                            uint8_t *line = to + box * (KT * 128) + skip * 128;
+                            *reinterpret_cast<uint4 *>(line + to0) = make_uint4(codes01(x.x), codes23(x.x), codes01(x.y), codes23(x.y));
+                            *reinterpret_cast<uint4 *>(line + to1) = make_uint4(codes01(x.z), codes23(x.z), codes01(x.w), codes23(x.w));
                         }
                     }
-                fence_async_smem();
+                if (h & 1) fence_async_smem();
                 __syncwarp();
                 if (lane == 0) {
                     tc::mbar_arrive(tc::smem_u32(raw_empty + raw.s));
-                    if (h & 1) tc::mbar_arrive(tc::smem_u32((is_v ? v_full : k_full) + ring.s));
+                    if (h & 1) tc::mbar_arrive(tc::smem_u32(filled + ring.s));
                 }
                 raw.next();
-                if ((h & 3) == 3) ring.next();
+                if (h & 1) ring.next(), raw.next(), raw.next();
             }
-            group_sync(3);
-            if (ptid == 0 && ok) w.next(a);
-            group_sync(3);
+            group_sync(3 + is_v);
+            if ((threadIdx.x & 127) == 0 && ok) w.next(a);
+            group_sync(3 + is_v);
         }
         if (!ok) *abort_flag = 1;
     } else {
