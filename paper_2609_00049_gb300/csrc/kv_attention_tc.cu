@@ -10,8 +10,8 @@
 //   - eight converter warps, four for K and four for V: codes to fp16 (exact: a byte permute to 1024 + c, one
 //     subtraction of 1152), K as the K-major and V as the MN-major B operand of the
 //     same layout: boxes of 64 channels, a token's 128-byte row swizzled;
-//   - two softmax warpgroups, one to a row tile, a thread to a row: while one works
-//     on its scores the tensor cores work for the other;
+//   - sixteen softmax warps, eight to a row tile, a thread to half of a row: while those of
+//     one row tile work on its scores the tensor cores work for the other;
 //   - one warp that issues the products.
 // Per value of S a softmax thread spends a maximum, a multiply-add, an exponential, an addition and
 // half a conversion: the block scales enter by the 16 tokens that share them.  With ks, vs a
@@ -28,7 +28,7 @@
 // P lies over S in TMEM (its low part, with fp32, has columns of its own), so the next
 // product into S is issued behind the product that reads P; the tensor cores run
 // them in order.  Work is cut as for few rows (kv_schedule.cuh), partial results
-// joined by the warpgroup that ends last.
+// joined by the warps that end last.
 #include <algorithm>
 #include <type_traits>
 
@@ -39,11 +39,9 @@ namespace realq {
 namespace {
 
 constexpr uint32_t FULL = 0xFFFFFFFFu;
-constexpr int SOFT_WARPS = 8, CONV_WARPS = 4;   // (converters: four for K and four for V)
+constexpr int SOFT_WARPS = 16, CONV_WARPS = 4;   // (softmax: eight to a row tile; converters: four for K and four for V)
 constexpr int MMA_WARP = SOFT_WARPS + 2 * CONV_WARPS, LOAD_WARP = MMA_WARP + 1, THREADS = 32 * (MMA_WARP + 4);   // (two are idle)
 constexpr int RAW_SLOTS = 3;             // half tiles of codes on their way
-// registers of a thread by role: 128 x (2 x 136 + 2 x 64 + 80) = 640 x 96, what the block starts with
-constexpr int SOFT_REGS = 136, CONV_REGS = 64, REST_REGS = 80;
 constexpr int SLOTS = 4;                 // of block scales
 constexpr float NEG = -INFINITY, LIFT = 6.f, SLACK = 8.f;
 
@@ -56,7 +54,7 @@ template <int DP, bool F32> struct Shape {
     static constexpr int BOXES = DP / 64;
     static constexpr int Q_BYTES = 128 * DP * 2;                                // one row tile, one part
     static constexpr int KV_BYTES = KT * DP * 2;
-    static constexpr int SLOT_BYTES = 4 * KT * 4;
+    static constexpr int SLOT_BYTES = 3 * KT * 4;
     static constexpr int HALF = KT / 2, RAW_BYTES = HALF * DP;                  // codes come by half tiles
     static constexpr int RING = NM * PARTS * Q_BYTES, RAW = RING + 2 * STAGES * KV_BYTES, SCALES = RAW + RAW_SLOTS * RAW_BYTES,
                          BARS = SCALES + SLOTS * SLOT_BYTES;
@@ -66,13 +64,12 @@ template <int DP, bool F32> struct Shape {
     static constexpr int S(int i) { return i * KT; }
     static constexpr int O(int i) { return NM * KT + i * DP; }
     static constexpr int LO(int i) { return NM * (KT + DP) + i * (KT / 2); }
-    static_assert(SMEM + 512 <= 232448 && (int)sizeof(Window) <= RAW_SLOTS * RAW_BYTES && NM * (KT + DP + (F32 ? KT / 2 : 0)) <= 512, "shared and tensor memory");
+    static_assert(SMEM + 512 + 1024 * NM <= 232448 && (int)sizeof(Window) <= RAW_SLOTS * RAW_BYTES && NM * (KT + DP + (F32 ? KT / 2 : 0)) <= 512, "shared and tensor memory");
 };
 
-template <int N> __device__ __forceinline__ void more_regs() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N> __device__ __forceinline__ void fewer_regs() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void group_sync(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
+// barriers 1 to 8: the two warps that share 32 rows; 9, 10: a row tile's eight; 11, 12: K's and V's converters
+template <int N> __device__ __forceinline__ void group_sync(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(N) : "memory"); }
 __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t *r) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
@@ -81,6 +78,11 @@ __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t *r) {
         : "memory");
 }
 
+__device__ __forceinline__ void tmem_st_x8(uint32_t taddr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+                 "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
 // two fp32 values in one register pair
 __device__ __forceinline__ uint64_t pair(float a, float b) {
     uint64_t r;
@@ -102,18 +104,6 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-__device__ __forceinline__ void tmem_ld_x32(uint32_t taddr, uint32_t (&r)[32]) {   // complete after tmem_wait_ld
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr));
-}
-
 // `bytes` consecutive bytes global -> shared, counted on `bar` (all three multiples of 16)
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
@@ -202,7 +192,8 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
     Window &win = *reinterpret_cast<Window *>(smem + Sh::RAW);   // (before the first codes come)
     __shared__ int last_one[2];
     __shared__ Shares shares;
-    __shared__ Walk<ROWS, KT> walks[6];
+    __shared__ Walk<ROWS, KT> walks[6];   // row tiles, K's and V's converters, products, loader
+    __shared__ float swap[2][NM][128];   // between the threads of a row
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + Sh::BARS);
     uint64_t *k_full = bars, *k_empty = bars + 2, *v_full = bars + 4, *v_empty = bars + 6;
     uint64_t *q_full = bars + 8, *s_full = bars + 10, *p_full = bars + 12, *o_full = bars + 14, *done = bars + 16;
@@ -220,9 +211,9 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
             tc::mbar_init(tc::smem_u32(v_full + i), CONV_WARPS);
             tc::mbar_init(tc::smem_u32(k_empty + i), 1);
             tc::mbar_init(tc::smem_u32(v_empty + i), 1);
-            tc::mbar_init(tc::smem_u32(q_full + i), 4);
+            tc::mbar_init(tc::smem_u32(q_full + i), 8);
             tc::mbar_init(tc::smem_u32(s_full + i), 1);
-            tc::mbar_init(tc::smem_u32(p_full + i), 4);
+            tc::mbar_init(tc::smem_u32(p_full + i), 8);
             tc::mbar_init(tc::smem_u32(o_full + i), 1);
         }
         for (int i = 0; i < RAW_SLOTS; ++i) {
@@ -253,7 +244,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
         if (threadIdx.x < 6) walks[threadIdx.x].start(u0, first0, tiles0, at0, sh.begin(blockIdx.x + 1));
         if (threadIdx.x == 0) shares = sh;
     }
-    Walk<ROWS, KT> &w = walks[warp == LOAD_WARP ? 5 : warp >> 2];
+    Walk<ROWS, KT> &w = walks[warp == LOAD_WARP ? 5 : (warp < SOFT_WARPS ? warp >> 3 : (warp - SOFT_WARPS) / 4 + 2)];
 
     if (warp == 0) tc::tmem_alloc(tc::smem_u32(tslot), 512);
     tc::fence_before_sync();
@@ -263,26 +254,25 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
     bool ok = true;
 
     if (warp < SOFT_WARPS) {
-        // ---------------- softmax: thread = row of row tile i ----------------
-        more_regs<SOFT_REGS>();
-        const int i = warp >> 2, row = threadIdx.x & 127;
+        // ---------------- softmax: a thread has half of a row of row tile i ----------------
+        const int i = warp >> 3, half = (warp >> 2) & 1, row = threadIdx.x & 127, pair_id = 1 + (warp & 3) + 4 * i;
+        constexpr int COLS = KT / 2;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t s_at = tmem + lanes + Sh::S(i), o_at = tmem + lanes + Sh::O(i), lo_at = tmem + lanes + Sh::LO(i);
+        const uint32_t s_at = tmem + lanes + Sh::S(i) + half * COLS, o_at = tmem + lanes + Sh::O(i), lo_at = tmem + lanes + Sh::LO(i) + half * (COLS / 2);
         const bool fine = a.c.log_block < 4;
         uint8_t *qs = smem + i * Sh::PARTS * Sh::Q_BYTES;
         uint32_t s_phase = 0, o_phase = 0;
         int slot = 0;
         // The row tile's queries into shared memory; returns what this thread's row's scores are multiplied by.  LANES
-        // lanes take a row, 8 values each, a warp its own 32 rows.
+        // lanes take a row, 8 values each, a warp 16 of the rows; the rows' factors go by shared memory.
         constexpr int LANES = DP / 8, AT_ONCE = 32 / LANES, BATCH = 4;
         const bool wide = ((reinterpret_cast<uintptr_t>(a.q) | (uintptr_t)(a.q_ld * sizeof(T)) | (uintptr_t)(a.q_hs * sizeof(T))) & 15) == 0;
         const auto load_q = [&](const Unit &u) {
             const int d = lane % LANES * 8, sub = lane / LANES;
-            float mine = 0.f;
-            int rw = (warp & 3) * 32 + sub;                             // row of the tile: token qi, head g of the group
+            int rw = (warp & 3) * 32 + half * 16 + sub;                 // row of the tile: token qi, head g of the group
             int qi = (u.r0 + 128 * i + rw) / a.group, g = u.r0 + 128 * i + rw - qi * a.group;
 #pragma unroll 1
-            for (int j0 = 0; j0 < LANES; j0 += BATCH) {
+            for (int j0 = 0; j0 < LANES / 2; j0 += BATCH) {
                 uint4 raw[BATCH][F32 ? 2 : 1];
                 const int rw0 = rw;
 #pragma unroll
@@ -327,8 +317,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                     float up = __uint_as_float((uint32_t)(127 + k) << 23);
                     const float back = fabsf(a.scale_log2) * __uint_as_float((uint32_t)(127 - k) << 23);
                     if (a.scale_log2 < 0.f) up = -up;   // (the scores' factor is to be positive)
-                    const float theirs = __shfl_sync(FULL, back, (lane - (j0 + j) * AT_ONCE) * LANES & 31);
-                    if (lane / AT_ONCE == j0 + j) mine = theirs;
+                    if (lane % LANES == 0) swap[0][i][rw0 + j * AT_ONCE] = back;
                     if (d < D) {
                         uint32_t h[4];
                         const int r = rw0 + j * AT_ONCE;
@@ -349,14 +338,17 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
             fence_async_smem();
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(tc::smem_u32(q_full + i));
+            group_sync<64>(pair_id);
+            const float mine = swap[0][i][row];
+            group_sync<64>(pair_id);
             return mine;
         };
         float rs = 0.f;
         bool loaded = false;
         const auto advance = [&]() {
-            group_sync(1 + i);
-            if (row == 0) w.next(a);
-            group_sync(1 + i);
+            group_sync<256>(9 + i);
+            if ((threadIdx.x & 255) == 0) w.next(a);
+            group_sync<256>(9 + i);
         };
         while (w.more() && ok) {
             const int count = w.count;
@@ -377,35 +369,33 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                 out_row = (int64_t)(w.u.q0 + qi) * a.n_heads + w.u.head * a.group + (r - qi * a.group);
             }
             const int all_hi = __reduce_min_sync(FULL, in ? row_hi : INT32_MAX), all_lo = __reduce_max_sync(FULL, in ? row_lo : 0);
-            int k0 = (w.u.lo / KT + w.from) * KT;
+            int k0 = (w.u.lo / KT + w.from) * KT + half * COLS;   // this thread's first token of a tile
             float m = NEG, l = 0.f, bad = 0.f;   // bad: NaN once a value that the row sees is
             for (int t = 0; t < count && ok; ++t, k0 += KT, slot = (slot + 1) & (SLOTS - 1)) {
                 ok = __all_sync(FULL, bar_wait(tc::smem_u32(s_full + i), s_phase, abort_flag));
                 s_phase ^= 1u;
                 if (!ok) break;
                 tc::fence_after_sync();
-                const bool masked = k0 + KT > all_hi || k0 < all_lo;
-                const float *sc = reinterpret_cast<const float *>(smem + Sh::SCALES + slot * Sh::SLOT_BYTES);
+                const bool masked = k0 + COLS > all_hi || k0 < all_lo;
+                const float *sc = reinterpret_cast<const float *>(smem + Sh::SCALES + slot * Sh::SLOT_BYTES) + half * (fine ? COLS : COLS / 4);
                 const auto seen = [&](int j) { return k0 + j < row_hi && k0 + j >= row_lo; };
                 // the largest S ks r + lv
                 float top = NEG;
-                const auto largest = [&](auto masks, auto fines, int c, uint32_t(&v)[32]) {
+                const auto largest = [&](auto masks, auto fines, int c, uint32_t(&v)[16]) {
                     if constexpr (masks) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = seen(c + j) ? v[j] : 0xFF800000u;
+                        for (int j = 0; j < 16; ++j) v[j] = seen(c + j) ? v[j] : 0xFF800000u;
                     }
                     if constexpr (!fines) {
+                        const float4 b = reinterpret_cast<const float4 *>(sc)[c / 16];
+                        float x[4];
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const float4 b = reinterpret_cast<const float4 *>(sc)[c / 16 + h];
-                            float x = __uint_as_float(v[16 * h]);
-#pragma unroll
-                            for (int j = 1; j < 16; ++j) x = fmaxf(x, __uint_as_float(v[16 * h + j]));
-                            top = fmaxf(top, fmaf(x, b.x * factor, b.y));
-                        }
+                        for (int j = 0; j < 4; ++j)
+                            x[j] = fmaxf(fmaxf(__uint_as_float(v[j]), __uint_as_float(v[4 + j])), fmaxf(__uint_as_float(v[8 + j]), __uint_as_float(v[12 + j])));
+                        top = fmaxf(top, fmaf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), b.x * factor, b.y));
                     } else {
 #pragma unroll
-                        for (int j = 0; j < 32; j += 4) {
+                        for (int j = 0; j < 16; j += 4) {
                             const float4 ks = *reinterpret_cast<const float4 *>(sc + c + j), lv = *reinterpret_cast<const float4 *>(sc + KT + c + j);
                             top = fmaxf(top, fmaf(__uint_as_float(v[j]), ks.x * factor, lv.x));
                             top = fmaxf(top, fmaf(__uint_as_float(v[j + 1]), ks.y * factor, lv.y));
@@ -416,43 +406,46 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                 };
                 using yes = std::true_type;
                 using no = std::false_type;
-                // Short loops: the roles' code together has to stay in the instruction cache.  Two reads of 32 columns are
+                // Short loops: what the roles' warps run has to stay in the instruction caches.  Two reads of 16 columns are
                 // under way in turn.
                 const auto over_scores = [&](auto f) {
-                    uint32_t v0[32], v1[32];
-                    tmem_ld_x32(s_at, v0);
+                    uint32_t v0[16], v1[16];
+                    tc::tmem_ld_32x32b_x16(s_at, v0);
 #pragma unroll 1
-                    for (int c = 0; c < KT; c += 64) {
+                    for (int c = 0; c < COLS; c += 32) {
                         tc::tmem_wait_ld();
-                        tmem_ld_x32(s_at + c + 32, v1);
+                        tc::tmem_ld_32x32b_x16(s_at + c + 16, v1);
                         f(c, v0);
                         tc::tmem_wait_ld();
-                        if (c + 64 < KT) tmem_ld_x32(s_at + c + 64, v0);
-                        f(c + 32, v1);
+                        if (c + 32 < COLS) tc::tmem_ld_32x32b_x16(s_at + c + 32, v0);
+                        f(c + 16, v1);
                     }
                 };
                 const auto over_few = [&](auto f) {   // (the rarer kinds of tiles)
-                    uint32_t v[32];
+                    uint32_t v[16];
 #pragma unroll 1
-                    for (int c = 0; c < KT; c += 32) {
-                        tmem_ld_x32(s_at + c, v);
+                    for (int c = 0; c < COLS; c += 16) {
+                        tc::tmem_ld_32x32b_x16(s_at + c, v);
                         tc::tmem_wait_ld();
                         f(c, v);
                     }
                 };
                 if (fine)
-                    over_few([&](int c, uint32_t(&v)[32]) { largest(yes{}, yes{}, c, v); });
+                    over_few([&](int c, uint32_t(&v)[16]) { largest(yes{}, yes{}, c, v); });
                 else if (masked)
-                    over_few([&](int c, uint32_t(&v)[32]) { largest(yes{}, no{}, c, v); });
+                    over_few([&](int c, uint32_t(&v)[16]) { largest(yes{}, no{}, c, v); });
                 else
-                    over_scores([&](int c, uint32_t(&v)[32]) { largest(no{}, no{}, c, v); });
+                    over_scores([&](int c, uint32_t(&v)[16]) { largest(no{}, no{}, c, v); });
+                swap[half][i][row] = top;
+                group_sync<64>(pair_id);
+                top = fmaxf(top, swap[half ^ 1][i][row]);
                 const bool grew = top > (m == NEG ? NEG : m + SLACK);
                 if (__any_sync(FULL, grew)) {
                     const float now = fmaxf(m, top), f = now == NEG ? 1.f : exp2_fast(m - now);
                     m = now, l *= f;
                     if (t > 0) {   // (the products so far are done: S came behind them)
 #pragma unroll 1
-                        for (int c = 0; c < D; c += 16) {
+                        for (int c = 16 * half; c < D; c += 32) {
                             uint32_t v[16];
                             tc::tmem_ld_32x32b_x16(o_at + c, v);
                             tc::tmem_wait_ld();
@@ -463,63 +456,59 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                     }
                 }
                 const float base = LIFT - (m == NEG ? 0.f : m);
-                // (32 columns of P go over 16 that have been read)
-                const auto weights = [&](auto masks, auto fines, int c, uint32_t(&v)[32]) {
-                    {
-                        uint32_t hi[16];
-                        [[maybe_unused]] uint32_t lo[F32 ? 16 : 1];
-                        if constexpr (!fines) {
+                // (16 columns become 8 of P, over ones that have been read)
+                const auto weights = [&](auto masks, auto fines, int c, uint32_t(&v)[16]) {
+                    uint32_t hi[8];
+                    [[maybe_unused]] uint32_t lo[F32 ? 8 : 1];
+                    if constexpr (!fines) {
+                        const float4 b = reinterpret_cast<const float4 *>(sc)[c / 16];
+                        const float c1 = b.x * factor, c0 = b.y + base;
+                        const uint64_t c11 = pair(c1, c1), c00 = pair(c0, c0);
+                        uint64_t part2 = 0;
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const float4 b = reinterpret_cast<const float4 *>(sc)[c / 16 + h];
-                                const float c1 = b.x * factor, c0 = b.y + base;
-                                const uint64_t c11 = pair(c1, c1), c00 = pair(c0, c0);
-                                uint64_t part2 = 0;
-#pragma unroll
-                                for (int j = 16 * h; j < 16 * h + 16; j += 2) {
-                                    float2 x = halves(fma2(pair(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), c11, c00));
-                                    if constexpr (masks) {
-                                        x.x = seen(c + j) ? x.x : NEG;
-                                        x.y = seen(c + j + 1) ? x.y : NEG;
-                                    }
-                                    x.x = exp2_fast(x.x), x.y = exp2_fast(x.y);
-                                    part2 = add2(part2, pair(x.x, x.y));
-                                    hi[j / 2] = pack_half(x.x, x.y);
-                                    if constexpr (F32) lo[j / 2] = pack_rest(x.x, x.y, hi[j / 2]);
-                                }
-                                const float2 ph = halves(part2);
-                                const float part = ph.x + ph.y;
-                                if (!masks || part != 0.f)   // (unseen tokens' scales may be anything)
-                                    l = fmaf(part, b.z, l), bad = fmaf(part, b.w, bad);
+                        for (int j = 0; j < 16; j += 2) {
+                            float2 x = halves(fma2(pair(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), c11, c00));
+                            if constexpr (masks) {
+                                x.x = seen(c + j) ? x.x : NEG;
+                                x.y = seen(c + j + 1) ? x.y : NEG;
                             }
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 32; j += 4) {
-                                const float4 ks = *reinterpret_cast<const float4 *>(sc + c + j), lv = *reinterpret_cast<const float4 *>(sc + KT + c + j);
-                                const float4 iv = *reinterpret_cast<const float4 *>(sc + 2 * KT + c + j), nv = *reinterpret_cast<const float4 *>(sc + 3 * KT + c + j);
-                                float x[4] = {fmaf(__uint_as_float(v[j]), ks.x * factor, lv.x + base), fmaf(__uint_as_float(v[j + 1]), ks.y * factor, lv.y + base),
-                                              fmaf(__uint_as_float(v[j + 2]), ks.z * factor, lv.z + base), fmaf(__uint_as_float(v[j + 3]), ks.w * factor, lv.w + base)};
-                                const float inv[4] = {iv.x, iv.y, iv.z, iv.w}, nan[4] = {nv.x, nv.y, nv.z, nv.w};
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    x[e] = exp2_fast(seen(c + j + e) ? x[e] : NEG);
-                                    const bool some = x[e] != 0.f;
-                                    l = fmaf(x[e], some ? inv[e] : 0.f, l), bad = fmaf(x[e], some ? nan[e] : 0.f, bad);
-                                }
-                                hi[j / 2] = pack_half(x[0], x[1]), hi[j / 2 + 1] = pack_half(x[2], x[3]);
-                                if constexpr (F32) lo[j / 2] = pack_rest(x[0], x[1], hi[j / 2]), lo[j / 2 + 1] = pack_rest(x[2], x[3], hi[j / 2 + 1]);
-                            }
+                            x.x = exp2_fast(x.x), x.y = exp2_fast(x.y);
+                            part2 = add2(part2, pair(x.x, x.y));
+                            hi[j / 2] = pack_half(x.x, x.y);
+                            if constexpr (F32) lo[j / 2] = pack_rest(x.x, x.y, hi[j / 2]);
                         }
-                        tmem_st_x16(s_at + c / 2, hi);
-                        if constexpr (F32) tmem_st_x16(lo_at + c / 2, lo);
+                        const float2 ph = halves(part2);
+                        const float part = ph.x + ph.y;
+                        if (!masks || part != 0.f)   // (unseen tokens' scales may be anything)
+                            l = fmaf(part, b.z, l), bad = fmaf(part, b.w, bad);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 16; j += 4) {
+                            const float4 ks = *reinterpret_cast<const float4 *>(sc + c + j), lv = *reinterpret_cast<const float4 *>(sc + KT + c + j);
+                            const float4 iv = *reinterpret_cast<const float4 *>(sc + 2 * KT + c + j);   // below zero: the value is NaN
+                            float x[4] = {fmaf(__uint_as_float(v[j]), ks.x * factor, lv.x + base), fmaf(__uint_as_float(v[j + 1]), ks.y * factor, lv.y + base),
+                                          fmaf(__uint_as_float(v[j + 2]), ks.z * factor, lv.z + base), fmaf(__uint_as_float(v[j + 3]), ks.w * factor, lv.w + base)};
+                            const float inv[4] = {iv.x, iv.y, iv.z, iv.w};
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                x[e] = exp2_fast(seen(c + j + e) ? x[e] : NEG);
+                                const bool some = x[e] != 0.f;
+                                l = fmaf(x[e], some ? fabsf(inv[e]) : 0.f, l);
+                                if (some && inv[e] < 0.f) bad = __uint_as_float(0x7FC00000u);
+                            }
+                            hi[j / 2] = pack_half(x[0], x[1]), hi[j / 2 + 1] = pack_half(x[2], x[3]);
+                            if constexpr (F32) lo[j / 2] = pack_rest(x[0], x[1], hi[j / 2]), lo[j / 2 + 1] = pack_rest(x[2], x[3], hi[j / 2 + 1]);
+                        }
                     }
+                    tmem_st_x8(s_at + c / 2, hi);
+                    if constexpr (F32) tmem_st_x8(lo_at + c / 2, lo);
                 };
                 if (fine)
-                    over_few([&](int c, uint32_t(&v)[32]) { weights(yes{}, yes{}, c, v); });
+                    over_few([&](int c, uint32_t(&v)[16]) { weights(yes{}, yes{}, c, v); });
                 else if (masked)
-                    over_few([&](int c, uint32_t(&v)[32]) { weights(yes{}, no{}, c, v); });
+                    over_few([&](int c, uint32_t(&v)[16]) { weights(yes{}, no{}, c, v); });
                 else
-                    over_scores([&](int c, uint32_t(&v)[32]) { weights(no{}, no{}, c, v); });
+                    over_scores([&](int c, uint32_t(&v)[16]) { weights(no{}, no{}, c, v); });
                 tc::tmem_wait_st();
                 tc::fence_before_sync();
                 __syncwarp();
@@ -567,9 +556,16 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
             };
             const auto slot_of = [&](int c, bool begins) { return a.part + ((int64_t)(2 * c + (begins ? 1 : 0)) * NM + i) * Sh::PART; };
             float *mine = slot_of(blockIdx.x, begins);
+            swap[half][i][row] = l;
+            group_sync<64>(pair_id);
+            l += swap[half ^ 1][i][row];
+            group_sync<64>(pair_id);
+            swap[half][i][row] = bad;
+            group_sync<64>(pair_id);
+            bad += swap[half ^ 1][i][row];
             const float inv = 1.f / l;
 #pragma unroll 1
-            for (int c = 0; c < D; c += 16) {
+            for (int c = 16 * half; c < D; c += 32) {
                 uint32_t v[16];
                 tc::tmem_ld_32x32b_x16(o_at + c, v);
                 tc::tmem_wait_ld();
@@ -590,17 +586,17 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
             }
             tc::fence_before_sync();
             if (whole) {
-                if (in) put_lse(m, l);
+                if (in && half == 0) put_lse(m, l);
                 continue;
             }
-            mine[128 * DP + row] = m, mine[128 * DP + 128 + row] = l;
+            if (half == 0) mine[128 * DP + row] = m, mine[128 * DP + 128 + row] = l;
             __threadfence();
-            group_sync(1 + i);
-            if (row == 0) {
+            group_sync<256>(9 + i);
+            if ((threadIdx.x & 255) == 0) {
                 const unsigned others = (unsigned)(last_cta - first_cta);
                 last_one[i] = atomicInc(reinterpret_cast<unsigned *>(a.counters) + 2 * first_cta + i, others) == others;
             }
-            group_sync(1 + i);
+            group_sync<256>(9 + i);
             if (!last_one[i]) continue;
             __threadfence();
             float mm = NEG, ll = 0.f;
@@ -611,7 +607,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                 ll += mc == NEG ? lc * 0.f : lc * exp2_fast(mc - mm);   // (a NaN stays one)
             }
             const float all_inv = ll == 0.f ? 0.f : 1.f / ll;
-            for (int d = 0; d < D; d += 8) {
+            for (int d = 8 * half; d < D; d += 16) {
                 float y[8] = {};
                 for (int c = first_cta; c <= last_cta; ++c) {
                     const float *s = slot_of(c, c == first_cta);
@@ -627,12 +623,11 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                 for (int e = 0; e < 8; ++e) y[e] *= all_inv;
                 if (in) put(d, y);
             }
-            if (in) put_lse(mm, ll);
+            if (in && half == 0) put_lse(mm, ll);
         }
         if (!ok) *abort_flag = 1;
     } else if (warp < MMA_WARP) {
         // ---------------- converters of K or of V: codes -> fp16, half a tile at a time ----------------
-        fewer_regs<CONV_REGS>();
         // Eight lanes take four pieces of 16 channels of two neighbouring tokens, in different boxes where there are
         // several: neither the reading nor the writing (rows of odd and even tokens swizzled apart) meets in a bank.
         const bool is_v = warp >= SOFT_WARPS + CONV_WARPS;
@@ -653,7 +648,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                 const uint8_t *from = smem + Sh::RAW + raw.s * Sh::RAW_BYTES + token0 * D + 16 * piece;
                 uint8_t *to = stages + ring.s * Sh::KV_BYTES + (h & 1) * Sh::HALF * 128;
                 const uint32_t there = raw_there[raw.s];
-#pragma unroll
+#pragma unroll 1
                 for (int i = 0; i < Sh::HALF / (8 * CONV_WARPS); ++i)
 #pragma unroll
                     for (int b = 0; b < Sh::BOXES; ++b) {
@@ -675,13 +670,12 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                 raw.next();
                 if (h & 1) ring.next(), raw.next(), raw.next();
             }
-            group_sync(3 + is_v);
+            group_sync<128>(11 + is_v);
             if ((threadIdx.x & 127) == 0 && ok) w.next(a);
-            group_sync(3 + is_v);
+            group_sync<128>(11 + is_v);
         }
         if (!ok) *abort_flag = 1;
     } else {
-        fewer_regs<REST_REGS>();
         if (warp == LOAD_WARP) {
         // ---------------- loader: pages, codes by bulk copies of 16 tokens, scales ----------------
         const bool fine = a.c.log_block < 4;
@@ -736,7 +730,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                                 lv = nan ? 0.f : fmaxf(log2_fast(vs), -100.f), iv = exp2_fast(-lv);   // (a scale below 2^-100 counts as that)
                             }
                             if (fine)
-                                sc[n] = ks, sc[KT + n] = lv, sc[2 * KT + n] = iv, sc[3 * KT + n] = nv;
+                                sc[n] = ks, sc[KT + n] = lv, sc[2 * KT + n] = nv != nv ? -iv : iv;
                             else
                                 reinterpret_cast<float4 *>(sc)[n] = make_float4(ks, lv, iv, nv);
                         }
@@ -758,7 +752,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                 tc::mbar_wait(tc::smem_u32(raw_full + k % RAW_SLOTS), k / RAW_SLOTS & 1u, &never, 100000000ull);
         }
         } else if (warp == MMA_WARP) {
-        // ---------------- products (the whole warp waits, one lane issues) ----------------
+        // ---------------- products ----------------
         const uint32_t idesc_s = tc::idesc_f16_f32(128, KT), idesc_o = tc::idesc_f16_f32(128, 0) | ((uint32_t)(D >> 3) << 17) | (1u << 16);
         const uint32_t base = tc::smem_u32(smem);
         const uint64_t q_desc = tc::smem_desc(base, 16, 1024, tc::SW_128B);
@@ -767,77 +761,71 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
         const int steps = D / 16;
         uint32_t phases = 0;   // bit i: of q_full, bit 2 + i: of p_full
         Ring kr(Sh::STAGES), vr(Sh::STAGES);
-        const auto wait = [&](uint64_t *bar, uint32_t phase) {
-            if (ok) ok = __all_sync(FULL, bar_wait(tc::smem_u32(bar), phase, abort_flag));
-            if (ok) tc::fence_after_sync();
-        };
-        const auto scores = [&](int i) {   // S_i = Q_i K^T of the K stage
-            if (tc::elect_one()) {
+        if (tc::elect_one()) {   // (one thread for everything: between two products there is little time)
+            const auto wait = [&](uint64_t *bar, uint32_t phase) {
+                ok = ok && bar_wait(tc::smem_u32(bar), phase, abort_flag);
+                tc::fence_after_sync();
+            };
+            while (w.more() && ok) {
+                const int nm = w.u.rows > 128 ? 2 : 1, count = w.count;
+                // step t: the outputs of tile t (none at -1), the scores of tile t + 1
 #pragma unroll 1
-                for (int p = 0; p < Sh::PARTS; ++p) {
-                    const uint64_t qd = q_desc + (uint32_t)((i * Sh::PARTS + p) * Sh::Q_BYTES >> 4);
-                    const uint64_t kd = k_desc + (uint32_t)(kr.s * Sh::KV_BYTES >> 4);
+                for (int t = -1; t < count && ok; ++t) {
+                    if (t >= 0) wait(v_full + vr.s, vr.phase);
+#pragma unroll 1
+                    for (int i = 0; i < nm && ok; ++i) {
+                        if (t < 0) {
+                            wait(q_full + i, phases >> i & 1u);
+                            phases ^= 1u << i;
+                        } else {   // O_i += P_i V
+                            wait(p_full + i, phases >> (2 + i) & 1u);
+                            phases ^= 4u << i;
+                            if (!ok) break;
+#pragma unroll 1
+                            for (int p = 0; p < Sh::PARTS; ++p) {
+                                const uint64_t vd = v_desc + (uint32_t)(vr.s * Sh::KV_BYTES >> 4);
+                                // (P's halves lie over the halves of S)
+                                const uint32_t pa = tmem + (p == 0 ? Sh::S(i) : Sh::LO(i)), up = p == 0 ? KT / 4 : 0;
 #pragma unroll
-                    for (int k = 0; k < DP / 16; ++k)
-                        if (k < steps)
-                            tc::mma_f16_ss(tmem + i * KT, qd + (k & 3) * 2 + (k >> 2) * 1024, kd + (k & 3) * 2 + (k >> 2) * (KT * 8), idesc_s,
-                                           (p > 0 || k > 0) ? 1u : 0u);
-                }
-                tc::mma_commit(tc::smem_u32(s_full + i));
-            }
-            __syncwarp();
-        };
-        const auto outputs = [&](int i, bool first, bool last) {   // O_i += P_i V of the V stage
-            if (tc::elect_one()) {
+                                for (int k = 0; k < KT / 16; ++k)
+                                    tc::mma_f16_ts(tmem + Sh::O(i), pa + k * 8 + (k >= KT / 32 ? up : 0), vd + k * 128, idesc_o, (k > 0 || p > 0 || t > 0) ? 1u : 0u);
+                            }
+                            if (t + 1 == count) tc::mma_commit(tc::smem_u32(o_full + i));
+                        }
+                        if (t + 1 < count) {   // S_i = Q_i K^T of the K stage
+                            if (i == 0) wait(k_full + kr.s, kr.phase);
+                            if (!ok) break;
 #pragma unroll 1
-                for (int p = 0; p < Sh::PARTS; ++p) {
-                    const uint64_t vd = v_desc + (uint32_t)(vr.s * Sh::KV_BYTES >> 4);
-                    const uint32_t pa = tmem + (p == 0 ? Sh::S(i) : Sh::LO(i));
+                            for (int p = 0; p < Sh::PARTS; ++p) {
+                                const uint64_t qd = q_desc + (uint32_t)((i * Sh::PARTS + p) * Sh::Q_BYTES >> 4);
+                                const uint64_t kd = k_desc + (uint32_t)(kr.s * Sh::KV_BYTES >> 4);
 #pragma unroll
-                    for (int k = 0; k < KT / 16; ++k)
-                        tc::mma_f16_ts(tmem + Sh::O(i), pa + k * 8, vd + k * 128, idesc_o, (k > 0 || p > 0 || !first) ? 1u : 0u);
-                }
-                if (last) tc::mma_commit(tc::smem_u32(o_full + i));
-            }
-            __syncwarp();
-        };
-        while (w.more() && ok) {
-            const int nm = w.u.rows > 128 ? 2 : 1, count = w.count;
-            // step t: the outputs of tile t (none at -1), the scores of tile t + 1
-#pragma unroll 1
-            for (int t = -1; t < count && ok; ++t) {
-                if (t >= 0) wait(v_full + vr.s, vr.phase);
-#pragma unroll 1
-                for (int i = 0; i < nm && ok; ++i) {
-                    if (t < 0) {
-                        wait(q_full + i, phases >> i & 1u);
-                        phases ^= 1u << i;
-                    } else {
-                        wait(p_full + i, phases >> (2 + i) & 1u);
-                        phases ^= 4u << i;
-                        if (ok) outputs(i, t == 0, t + 1 == count);
+                                for (int k = 0; k < DP / 16; ++k)
+                                    if (k < steps)
+                                        tc::mma_f16_ss(tmem + Sh::S(i), qd + (k & 3) * 2 + (k >> 2) * 1024, kd + (k & 3) * 2 + (k >> 2) * (KT * 8), idesc_s,
+                                                       (p > 0 || k > 0) ? 1u : 0u);
+                            }
+                            tc::mma_commit(tc::smem_u32(s_full + i));
+                        }
+                    }
+                    if (!ok) break;
+                    if (t >= 0) {
+                        tc::mma_commit(tc::smem_u32(v_empty + vr.s));
+                        vr.next();
                     }
                     if (t + 1 < count) {
-                        if (i == 0) wait(k_full + kr.s, kr.phase);
-                        if (ok) scores(i);
+                        tc::mma_commit(tc::smem_u32(k_empty + kr.s));
+                        kr.next();
                     }
                 }
-                if (ok && tc::elect_one()) {
-                    if (t >= 0) tc::mma_commit(tc::smem_u32(v_empty + vr.s));
-                    if (t + 1 < count) tc::mma_commit(tc::smem_u32(k_empty + kr.s));
-                }
-                __syncwarp();
-                if (t >= 0) vr.next();
-                if (t + 1 < count) kr.next();
+                if (ok) w.next(a);
             }
-            __syncwarp();
-            if (ok && lane == 0) w.next(a);
-            __syncwarp();
+            if (!ok) *abort_flag = 1;
+            tc::mma_commit(tc::smem_u32(done));
         }
-        if (!ok) *abort_flag = 1;
-        // every product issued has retired before TMEM is freed
-        if (tc::elect_one()) tc::mma_commit(tc::smem_u32(done));
         __syncwarp();
+        ok = *abort_flag == 0;
+        // every product issued has retired before TMEM is freed
         int never = 0;
         tc::mbar_wait(tc::smem_u32(done), 0u, &never, 100000000ull);
         }
