@@ -132,6 +132,18 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
     }
 }
 
+__device__ __forceinline__ void tmem_ld_x32(uint32_t taddr, uint32_t *r) {   // complete after tmem_wait_ld
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr));
+}
+
 struct Ring {   // stage and phase of something that goes round
     int s = 0, n;
     uint32_t phase = 0;
@@ -381,7 +393,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                 const auto seen = [&](int j) { return k0 + j < row_hi && k0 + j >= row_lo; };
                 // the largest S ks r + lv
                 float top = NEG;
-                const auto largest = [&](auto masks, auto fines, int c, uint32_t(&v)[16]) {
+                const auto largest = [&](auto masks, auto fines, int c, uint32_t *v) {
                     if constexpr (masks) {
 #pragma unroll
                         for (int j = 0; j < 16; ++j) v[j] = seen(c + j) ? v[j] : 0xFF800000u;
@@ -406,22 +418,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                 };
                 using yes = std::true_type;
                 using no = std::false_type;
-                // Short loops: what the roles' warps run has to stay in the instruction caches.  Two reads of 16 columns are
-                // under way in turn.
-                const auto over_scores = [&](auto f) {
-                    uint32_t v0[16], v1[16];
-                    tc::tmem_ld_32x32b_x16(s_at, v0);
-#pragma unroll 1
-                    for (int c = 0; c < COLS; c += 32) {
-                        tc::tmem_wait_ld();
-                        tc::tmem_ld_32x32b_x16(s_at + c + 16, v1);
-                        f(c, v0);
-                        tc::tmem_wait_ld();
-                        if (c + 32 < COLS) tc::tmem_ld_32x32b_x16(s_at + c + 32, v0);
-                        f(c + 16, v1);
-                    }
-                };
-                const auto over_few = [&](auto f) {   // (the rarer kinds of tiles)
+                const auto over_few = [&](auto f) {   // (the rarer kinds of tiles: short loops, for the instruction cache)
                     uint32_t v[16];
 #pragma unroll 1
                     for (int c = 0; c < COLS; c += 16) {
@@ -430,34 +427,32 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                         f(c, v);
                     }
                 };
-                if (fine)
-                    over_few([&](int c, uint32_t(&v)[16]) { largest(yes{}, yes{}, c, v); });
-                else if (masked)
-                    over_few([&](int c, uint32_t(&v)[16]) { largest(yes{}, no{}, c, v); });
-                else
-                    over_scores([&](int c, uint32_t(&v)[16]) { largest(no{}, no{}, c, v); });
-                swap[half][i][row] = top;
-                group_sync<64>(pair_id);
-                top = fmaxf(top, swap[half ^ 1][i][row]);
-                const bool grew = top > (m == NEG ? NEG : m + SLACK);
-                if (__any_sync(FULL, grew)) {
-                    const float now = fmaxf(m, top), f = now == NEG ? 1.f : exp2_fast(m - now);
-                    m = now, l *= f;
-                    if (t > 0) {   // (the products so far are done: S came behind them)
-#pragma unroll 1
-                        for (int c = 16 * half; c < D; c += 32) {
-                            uint32_t v[16];
-                            tc::tmem_ld_32x32b_x16(o_at + c, v);
-                            tc::tmem_wait_ld();
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * f);
-                            tmem_st_x16(o_at + c, v);
+                // the row's maximum from both its threads, and what that changes
+                float base = 0.f;
+                const auto agree = [&]() {
+                    swap[half][i][row] = top;
+                    group_sync<64>(pair_id);
+                    top = fmaxf(top, swap[half ^ 1][i][row]);
+                    const bool grew = top > (m == NEG ? NEG : m + SLACK);
+                    if (__any_sync(FULL, grew)) {
+                        const float now = fmaxf(m, top), f = now == NEG ? 1.f : exp2_fast(m - now);
+                        m = now, l *= f;
+                        if (t > 0) {   // (the products so far are done: S came behind them)
+    #pragma unroll 1
+                            for (int c = 16 * half; c < D; c += 32) {
+                                uint32_t v[16];
+                                tc::tmem_ld_32x32b_x16(o_at + c, v);
+                                tc::tmem_wait_ld();
+    #pragma unroll
+                                for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * f);
+                                tmem_st_x16(o_at + c, v);
+                            }
                         }
                     }
-                }
-                const float base = LIFT - (m == NEG ? 0.f : m);
+                    base = LIFT - (m == NEG ? 0.f : m);
+                };
                 // (16 columns become 8 of P, over ones that have been read)
-                const auto weights = [&](auto masks, auto fines, int c, uint32_t(&v)[16]) {
+                const auto weights = [&](auto masks, auto fines, int c, uint32_t *v) {
                     uint32_t hi[8];
                     [[maybe_unused]] uint32_t lo[F32 ? 8 : 1];
                     if constexpr (!fines) {
@@ -503,12 +498,32 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                     tmem_st_x8(s_at + c / 2, hi);
                     if constexpr (F32) tmem_st_x8(lo_at + c / 2, lo);
                 };
-                if (fine)
-                    over_few([&](int c, uint32_t(&v)[16]) { weights(yes{}, yes{}, c, v); });
-                else if (masked)
-                    over_few([&](int c, uint32_t(&v)[16]) { weights(yes{}, no{}, c, v); });
-                else
-                    over_scores([&](int c, uint32_t(&v)[16]) { weights(no{}, no{}, c, v); });
+                if (!fine && !masked) {
+                    uint32_t v[32];
+#pragma unroll 1
+                    for (int c = 0; c < COLS; c += 32) {
+                        tmem_ld_x32(s_at + c, v);
+                        tc::tmem_wait_ld();
+                        largest(no{}, no{}, c, v);
+                        largest(no{}, no{}, c + 16, v + 16);
+                    }
+                    agree();
+#pragma unroll 1
+                    for (int c = 0; c < COLS; c += 32) {
+                        tmem_ld_x32(s_at + c, v);
+                        tc::tmem_wait_ld();
+                        weights(no{}, no{}, c, v);
+                        weights(no{}, no{}, c + 16, v + 16);
+                    }
+                } else if (!fine) {
+                    over_few([&](int c, uint32_t *v) { largest(yes{}, no{}, c, v); });
+                    agree();
+                    over_few([&](int c, uint32_t *v) { weights(yes{}, no{}, c, v); });
+                } else {
+                    over_few([&](int c, uint32_t *v) { largest(yes{}, yes{}, c, v); });
+                    agree();
+                    over_few([&](int c, uint32_t *v) { weights(yes{}, yes{}, c, v); });
+                }
                 tc::tmem_wait_st();
                 tc::fence_before_sync();
                 __syncwarp();
