@@ -92,14 +92,15 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
     __shared__ Window win;
     __shared__ float row_scale[ROWS];
     __shared__ int row_lo[ROWS], row_hi[ROWS];
-    __shared__ float join_m[WARPS][ROWS], join_l[WARPS][ROWS];
+    __shared__ float join_m[WARPS][ROWS], join_l[WARPS][ROWS], row_m[ROWS], row_l[ROWS];
     __shared__ int last_one;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     uint8_t *ring = smem + warp * Sh::RING;
     uint2 *qfrag = reinterpret_cast<uint2 *>(smem + WARPS * Sh::RING);
     const int D = a.c.head_dim, pieces = D / 16;
+    const bool wide = ((reinterpret_cast<uintptr_t>(a.q) | (uintptr_t)(a.q_ld * sizeof(T)) | (uintptr_t)(a.q_hs * sizeof(T))) & 15) == 0;
     float *const part = a.part;
-    constexpr int PART = ROWS * (DP + 2);
+    constexpr int PART = ROWS * (DP + 2);   // (a multiple of 16 bytes)
 
     // all tiles, and this CTA's share
     int64_t all = 0;
@@ -124,63 +125,6 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
         const int count = (int)min(end - at, (int64_t)(tiles - from));
         const int tile0 = u.lo / TILE + from;
         at += count;
-
-        // ---- queries: a warp takes a tile of 8 rows ----
-        for (int nt = warp; nt < NT; nt += WARPS) {
-            const int r = u.r0 + 8 * nt + g;
-            const bool row_in = 8 * nt + g < u.rows;
-            const int qi = row_in ? r / a.group : 0;
-            const T *q = (const T *)a.q + (int64_t)(u.q0 + qi) * a.q_ld + (int64_t)(u.head * a.group + (row_in ? r % a.group : 0)) * a.q_hs;
-            float v[DP / 4];
-            float top = 0.f;
-#pragma unroll
-            for (int j = 0; j < DP / 64; ++j)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int d = 16 * (t + 4 * j) + e;
-                    const float x = row_in && d < D ? load_as_float(q, d) : 0.f;
-                    v[16 * j + e] = x;
-                    top = fmaxf(top, fabsf(x));
-                }
-            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-            // 2^k with top 2^k in [2^14, 2^15), by two factors: one alone may pass the range of fp32
-            int k = 0;
-            if (top > 0.f && top < INFINITY) k = 14 - ilogbf(top);
-            const float up0 = scalbnf(1.f, k / 2), up1 = scalbnf(1.f, k - k / 2);
-#pragma unroll
-            for (int j = 0; j < DP / 64; ++j)
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    float x[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = v[16 * j + 4 * w + e] * up0 * up1;
-                    const uint2 h = make_uint2(pack_half(x[0], x[1]), pack_half(x[2], x[3]));
-                    const int step = 4 * j + w;
-                    qfrag[((step * NT + nt) * Sh::PARTS) * 32 + lane] = h;
-                    if constexpr (F32)
-                        qfrag[((step * NT + nt) * 2 + 1) * 32 + lane] = make_uint2(pack_rest(x[0], x[1], h.x), pack_rest(x[2], x[3], h.y));
-                }
-            if (t == 0) {
-                const int p = u.len - u.m + qi;
-                row_scale[8 * nt + g] = a.scale_log2 * scalbnf(1.f, -(k / 2)) * scalbnf(1.f, -(k - k / 2));
-                row_hi[8 * nt + g] = !row_in ? 0 : (a.causal ? min(u.len, p + 1) : u.len);
-                row_lo[8 * nt + g] = a.window > 0 ? (int)max((int64_t)0, (int64_t)p - a.window + 1) : 0;
-            }
-        }
-        __syncthreads();
-        uint2 qreg[Sh::QREG ? Sh::STEPS * NT * Sh::PARTS : 1];
-        if constexpr (Sh::QREG) {
-#pragma unroll
-            for (int i = 0; i < Sh::STEPS * NT * Sh::PARTS; ++i) qreg[i] = qfrag[i * 32 + lane];
-        }
-        float rs[NT][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) rs[nt][0] = row_scale[8 * nt + 2 * t], rs[nt][1] = row_scale[8 * nt + 2 * t + 1];
-        // tokens that every row sees
-        const int p_first = u.len - u.m + u.r0 / a.group, p_last = u.len - u.m + (u.r0 + u.rows - 1) / a.group;
-        const int clear_hi = a.causal ? min(u.len, p_first + 1) : u.len;
-        const int64_t clear_lo = a.window > 0 ? (int64_t)p_last - a.window + 1 : 0;
 
         // ---- this warp's 16 tokens of every tile ----
         const int *table = a.tables + (int64_t)u.seq * a.max_pages;
@@ -229,6 +173,78 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
         };
 #pragma unroll 1
         for (int i = 0; i < Sh::STAGES - 1; ++i) load_next();
+
+        // ---- queries (while the first codes come): a warp takes a tile of 8 rows ----
+        for (int nt = warp; nt < NT; nt += WARPS) {
+            const int r = u.r0 + 8 * nt + g;
+            const bool row_in = 8 * nt + g < u.rows;
+            const int qi = row_in ? r / a.group : 0;
+            const T *q = (const T *)a.q + (int64_t)(u.q0 + qi) * a.q_ld + (int64_t)(u.head * a.group + (row_in ? r - qi * a.group : 0)) * a.q_hs;
+            float v[DP / 4];
+            float top = 0.f;
+#pragma unroll
+            for (int j = 0; j < DP / 64; ++j) {
+                const int d = 16 * (t + 4 * j);   // (D is a multiple of 16)
+                if (!row_in || d >= D) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) v[16 * j + e] = 0.f;
+                } else if (!wide) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) v[16 * j + e] = load_as_float(q, d + e);
+                } else if constexpr (F32) {
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        const float4 x = *reinterpret_cast<const float4 *>(q + d + e);
+                        v[16 * j + e] = x.x, v[16 * j + e + 1] = x.y, v[16 * j + e + 2] = x.z, v[16 * j + e + 3] = x.w;
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; e += 8) {
+                        const uint4 x = *reinterpret_cast<const uint4 *>(q + d + e);
+                        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            v[16 * j + e + 2 * k] = __uint_as_float(w[k] << 16), v[16 * j + e + 2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+                    }
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < DP / 4; ++e) top = fmaxf(top, fabsf(v[e]));
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+            // times 2^k: the largest lies in [2^14, 2^15) after that (a row below 2^-112 a little lower)
+            const int ex = (int)(__float_as_uint(top) >> 23), k = ex == 0 || ex == 255 ? 0 : min(126, 141 - ex);
+            const float up = __uint_as_float((uint32_t)(127 + k) << 23);
+#pragma unroll
+            for (int step = 0; step < Sh::STEPS; ++step) {
+                float x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = v[4 * step + e] * up;
+                const uint2 h = make_uint2(pack_half(x[0], x[1]), pack_half(x[2], x[3]));
+                qfrag[((step * NT + nt) * Sh::PARTS) * 32 + lane] = h;
+                if constexpr (F32)
+                    qfrag[((step * NT + nt) * 2 + 1) * 32 + lane] = make_uint2(pack_rest(x[0], x[1], h.x), pack_rest(x[2], x[3], h.y));
+            }
+            if (t == 0) {
+                const int p = u.len - u.m + qi;
+                row_scale[8 * nt + g] = a.scale_log2 * __uint_as_float((uint32_t)(127 - k) << 23);
+                row_hi[8 * nt + g] = !row_in ? 0 : (a.causal ? min(u.len, p + 1) : u.len);
+                row_lo[8 * nt + g] = a.window > 0 ? (int)max((int64_t)0, (int64_t)p - a.window + 1) : 0;
+            }
+        }
+        __syncthreads();
+        uint2 qreg[Sh::QREG ? Sh::STEPS * NT * Sh::PARTS : 1];
+        if constexpr (Sh::QREG) {
+#pragma unroll
+            for (int i = 0; i < Sh::STEPS * NT * Sh::PARTS; ++i) qreg[i] = qfrag[i * 32 + lane];
+        }
+        float rs[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) rs[nt][0] = row_scale[8 * nt + 2 * t], rs[nt][1] = row_scale[8 * nt + 2 * t + 1];
+        // tokens that every row sees
+        const int p_first = u.len - u.m + u.r0 / a.group, p_last = u.len - u.m + (u.r0 + u.rows - 1) / a.group;
+        const int clear_hi = a.causal ? min(u.len, p_first + 1) : u.len;
+        const int64_t clear_lo = a.window > 0 ? (int64_t)p_last - a.window + 1 : 0;
 
         float o[Sh::MT][NT][4];
 #pragma unroll
@@ -398,34 +414,51 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
         const bool whole = count == tiles;
         const int first_cta = shares.owner(unit0), last_cta = shares.owner(unit0 + tiles - 1);
         float *slot = part + ((int64_t)2 * blockIdx.x + (from == 0 ? 1 : 0)) * PART;
-        const auto finish = [&](int r, int d, float acc, float m, float l) {   // one value of row r
+        const auto finish = [&](int r, int d, const float4 &acc) {   // four values of row r, whose sum is row_l
             const int rr = u.r0 + r, qi = rr / a.group;
             const int64_t row = (int64_t)(u.q0 + qi) * a.n_heads + u.head * a.group + rr % a.group;
-            const float y = l == 0.f ? 0.f : acc / l;   // (a sum of nothing: the row sees no token)
-            if constexpr (F32)
-                ((float *)a.out)[row * D + d] = y;
-            else
-                ((__nv_bfloat16 *)a.out)[row * D + d] = __float2bfloat16_rn(y);
+            const float m = row_m[r], l = row_l[r];
+            const float inv = l == 0.f ? 0.f : 1.f / l;   // (a sum of nothing: the row sees no token)
+            const float y[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
+            T *o = (T *)a.out + row * D + d;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (F32)
+                    o[e] = y[e];
+                else
+                    o[e] = __float2bfloat16_rn(y[e]);
+            }
             if (d == 0 && a.lse != nullptr) a.lse[row] = l == 0.f ? NEG : (m - 14.f + log2f(l)) * 0.6931471805599453f;
         };
-        for (int i = threadIdx.x; i < u.rows * DP; i += THREADS) {
-            const int r = i / DP, d = i % DP;
-            float m = NEG, l = 0.f, acc = 0.f;
+        // (a share that saw nothing has maximum -inf, sum 0 and outputs 0; one that saw a NaN a sum of NaN)
+        if (threadIdx.x < ROWS) {
+            const int r = threadIdx.x;
+            float m = NEG, l = 0.f;
 #pragma unroll
             for (int w = 0; w < WARPS; ++w) m = fmaxf(m, join_m[w][r]);
 #pragma unroll
             for (int w = 0; w < WARPS; ++w) {
-                const float mw = join_m[w][r], f = mw == NEG ? 0.f : exp2_fast(mw - m);
-                if (mw == NEG && join_l[w][r] == 0.f) continue;
+                const float f = join_m[w][r] == NEG ? 0.f : exp2_fast(join_m[w][r] - m);
                 l += join_l[w][r] * f;
-                acc += reinterpret_cast<const float *>(smem + w * Sh::RING)[i] * f;
+                join_m[w][r] = f;
             }
-            if (whole) {
-                if (d < D) finish(r, d, acc, m, l);
-            } else {
-                slot[r * DP + d] = acc;
-                if (d == 0) slot[ROWS * DP + r] = m, slot[ROWS * DP + ROWS + r] = l;
+            row_m[r] = m, row_l[r] = l;
+            if (!whole) slot[ROWS * DP + r] = m, slot[ROWS * DP + ROWS + r] = l;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < u.rows * (DP / 4); i += THREADS) {
+            const int r = i / (DP / 4), d = i % (DP / 4) * 4;
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) {
+                const float4 v = reinterpret_cast<const float4 *>(smem + w * Sh::RING)[i];
+                const float f = join_m[w][r];
+                acc.x += v.x * f, acc.y += v.y * f, acc.z += v.z * f, acc.w += v.w * f;
             }
+            if (!whole)
+                reinterpret_cast<float4 *>(slot)[i] = acc;
+            else if (d < D)
+                finish(r, d, acc);
         }
         if (!whole) {
             __threadfence();
@@ -436,21 +469,44 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
             __syncthreads();
             if (last_one) {
                 __threadfence();
-                for (int i = threadIdx.x; i < u.rows * DP; i += THREADS) {
-                    const int r = i / DP, d = i % DP;
-                    if (d >= D) continue;
-                    float m = NEG, l = 0.f, acc = 0.f;
-                    const auto slot_of = [&](int c) { return part + ((int64_t)2 * c + (c == first_cta ? 1 : 0)) * PART; };
-                    for (int c = first_cta; c <= last_cta; ++c) m = fmaxf(m, __ldcg(slot_of(c) + ROWS * DP + r));
-                    for (int c = first_cta; c <= last_cta; ++c) {
-                        const float *p = slot_of(c);
-                        const float mc = __ldcg(p + ROWS * DP + r), lc = __ldcg(p + ROWS * DP + ROWS + r);
-                        if (mc == NEG && lc == 0.f) continue;
-                        const float f = mc == NEG ? 0.f : exp2_fast(mc - m);
-                        l += lc * f;
-                        acc += __ldcg(p + i) * f;
+                const auto slot_of = [&](int c) { return part + ((int64_t)2 * c + (c == first_cta ? 1 : 0)) * PART; };
+                // each row's maximum and sum over all shares, a warp to a row
+                for (int r = warp; r < u.rows; r += WARPS) {
+                    float m = NEG, l = 0.f;
+                    for (int c = first_cta + lane; c <= last_cta; c += 32) m = fmaxf(m, __ldcg(slot_of(c) + ROWS * DP + r));
+#pragma unroll
+                    for (int o = 16; o; o /= 2) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+                    for (int c = first_cta + lane; c <= last_cta; c += 32) {
+                        const float mc = __ldcg(slot_of(c) + ROWS * DP + r);
+                        l += __ldcg(slot_of(c) + ROWS * DP + ROWS + r) * (mc == NEG ? 0.f : exp2_fast(mc - m));
                     }
-                    finish(r, d, acc, m, l);
+#pragma unroll
+                    for (int o = 16; o; o /= 2) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
+                    if (lane == 0) row_m[r] = m, row_l[r] = l;
+                }
+                __syncthreads();
+                // the outputs in the order of the shares, eight of them under way
+                for (int i = threadIdx.x; i < u.rows * (DP / 4); i += THREADS) {
+                    const int r = i / (DP / 4), d = i % (DP / 4) * 4;
+                    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                    const float m = row_m[r];
+#pragma unroll 1
+                    for (int c0 = first_cta; c0 <= last_cta; c0 += 8) {
+                        float4 v[8];
+                        float mc[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const float *p = slot_of(min(c0 + k, last_cta));
+                            v[k] = __ldcg(reinterpret_cast<const float4 *>(p) + i);
+                            mc[k] = c0 + k <= last_cta ? __ldcg(p + ROWS * DP + r) : NEG;
+                        }
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const float f = mc[k] == NEG ? 0.f : exp2_fast(mc[k] - m);
+                            if (c0 + k <= last_cta) acc.x += v[k].x * f, acc.y += v[k].y * f, acc.z += v[k].z * f, acc.w += v[k].w * f;
+                        }
+                    }
+                    if (d < D) finish(r, d, acc);
                 }
             }
         }
@@ -467,7 +523,11 @@ template <int DP, int NT, bool F32, class T> realq_status_t launch(cudaStream_t 
     REALQ_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, THREADS, Sh::SMEM));
     per_sm = std::max(1, std::min(per_sm, KV_MAX_CTAS_PER_SM));
     Launch l("kv_attention", s);
-    REALQ_CUDA_TRY(launch_overlapped(kernel, dim3((unsigned)(per_sm * sms)), dim3(THREADS), Sh::SMEM, s, a));
+    // beside the prompts' kernel of the same call, which writes nothing that this one reads; else after what came before
+    if (a.min_new == 1 && a.max_new < INT32_MAX)
+        REALQ_CUDA_TRY(launch_overlapped(kernel, dim3((unsigned)(per_sm * sms)), dim3(THREADS), Sh::SMEM, s, a));
+    else
+        kernel<<<(unsigned)(per_sm * sms), THREADS, Sh::SMEM, s>>>(a);
     return check_launch("kv_attention");
 }
 template <int DP, bool F32, class T> realq_status_t by_rows(cudaStream_t s, const KvAttnArgs &a, int64_t rows, int sms) {

@@ -421,3 +421,27 @@ def test_attention_in_graphs_that_share_a_workspace():
             got = outs[i].clone()
             want, _ = attended(c, [i + 1] * 3, H, BF16, 0, q=qs[i], max_new=i + 1)
             assert torch.equal(got, want)
+
+
+def test_attention_right_behind_a_product():
+    """The queries come from an 8-bit product that lets the next kernel start early: attention waits for them all the same."""
+    T, n, H, D = 300, 2048, 4, 64
+    c = Cache(14, [70] * T, kv=2, D=D)
+    h = rq.kv_cache(**c.buffers())
+    xc = torch.randint(0, 256, (T, n), generator=gen(1), device="cuda").to(torch.uint8)
+    wc = torch.randint(0, 256, (H * D, n), generator=gen(2), device="cuda").to(torch.uint8)
+    xs, ws = torch.full((T,), 1e-2, device="cuda"), torch.full((H * D,), 1e-3, device="cuda")
+    pws = rq.workspace(rq.realq_int8_product_workspace_size(T, n, H * D))
+    aws = rq.workspace(rq.realq_kv_attention_workspace_size(h, T, T, H))
+    q, out = torch.zeros(T, H * D, device="cuda", dtype=BF16), torch.empty(T, H, D, device="cuda", dtype=BF16)
+    starts = starts_of([1] * T)
+    outs = []
+    for together in (False, True, True):
+        q.zero_()
+        torch.cuda.synchronize()
+        rq.realq_int8_product(xc, xs, wc, ws, q, ws=pws)
+        if not together:
+            torch.cuda.synchronize()
+        rq.realq_kv_attention(q.view(T, H, D), h, 0, starts, c.lengths, c.tables, out, max_new=1, ws=aws)
+        outs.append(out.clone())
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
