@@ -103,12 +103,17 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
     constexpr int PART = ROWS * (DP + 2);   // (a multiple of 16 bytes)
 
     // all tiles, and this CTA's share
+    const bool few = a.n_seqs <= 32;
     int64_t all = 0;
-    for (int first = 0; first < a.n_seqs; first += SEQS) {
-        fill_window<ROWS, TILE, false>(a, win, first, all);
-        all += win.sum[SEQS] * a.c.n_kv;
+    if (few) {
+        all = lanes_of<ROWS, TILE>(a).sum * a.c.n_kv;
+    } else {
+        for (int first = 0; first < a.n_seqs; first += SEQS) {
+            fill_window<ROWS, TILE, false>(a, win, first, all);
+            all += win.sum[SEQS] * a.c.n_kv;
+        }
     }
-    const Shares shares{all, min((int64_t)gridDim.x, all)};
+    const Shares shares(all, gridDim.x);
     if (blockIdx.x >= shares.ctas) {
         wait_for_previous();
         return;
@@ -120,7 +125,10 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
         Unit u;
         int64_t unit0;   // the unit's first tile
         int tiles;
-        locate<ROWS, TILE, false>(a, win, at, u, unit0, tiles);
+        if (few)
+            locate<ROWS, TILE>(a, lanes_of<ROWS, TILE>(a), at, u, unit0, tiles);   // (again: registers are short in the loop)
+        else
+            locate<ROWS, TILE, false>(a, win, at, u, unit0, tiles);
         const int from = (int)min(at - unit0, (int64_t)tiles - 1);
         const int count = (int)min(end - at, (int64_t)(tiles - from));
         const int tile0 = u.lo / TILE + from;
@@ -470,41 +478,69 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
             if (last_one) {
                 __threadfence();
                 const auto slot_of = [&](int c) { return part + ((int64_t)2 * c + (c == first_cta ? 1 : 0)) * PART; };
-                // each row's maximum and sum over all shares, a warp to a row
-                for (int r = warp; r < u.rows; r += WARPS) {
-                    float m = NEG, l = 0.f;
-                    for (int c = first_cta + lane; c <= last_cta; c += 32) m = fmaxf(m, __ldcg(slot_of(c) + ROWS * DP + r));
+                // The shares' maxima and sums, some shares at a time, into the rings; each row's maximum and sum over all of
+                // them, a warp to a row; the shares' factors.
+                constexpr int AT_ONCE = WARPS * Sh::RING / (ROWS * 8);
+                const int parts = last_cta - first_cta + 1;
+                float *const ms = reinterpret_cast<float *>(smem), *const ls = ms + AT_ONCE * ROWS;
+                for (int pass = 0; pass < 2; ++pass)   // (of more shares than fit, the maxima go first)
+                    for (int c0 = 0; c0 < parts; c0 += AT_ONCE) {
+                        const int n = min(AT_ONCE, parts - c0);
+                        if (parts <= AT_ONCE && pass == 1) break;
+                        __syncthreads();
+#pragma unroll 4
+                        for (int i = threadIdx.x; i < n * ROWS; i += THREADS) {
+                            const float *p = slot_of(first_cta + c0 + i / ROWS) + ROWS * DP + i % ROWS;
+                            ms[i] = __ldcg(p), ls[i] = __ldcg(p + ROWS);
+                        }
+                        __syncthreads();
+                        for (int r = warp; r < u.rows; r += WARPS) {
+                            float m = c0 + pass == 0 ? NEG : row_m[r], l = c0 == 0 ? 0.f : row_l[r];
+                            if (pass == 0) {
+                                for (int c = lane; c < n; c += 32) m = fmaxf(m, ms[c * ROWS + r]);
 #pragma unroll
-                    for (int o = 16; o; o /= 2) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-                    for (int c = first_cta + lane; c <= last_cta; c += 32) {
-                        const float mc = __ldcg(slot_of(c) + ROWS * DP + r);
-                        l += __ldcg(slot_of(c) + ROWS * DP + ROWS + r) * (mc == NEG ? 0.f : exp2_fast(mc - m));
+                                for (int o = 16; o; o /= 2) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+                            }
+                            if (pass == 1 || parts <= AT_ONCE) {
+                                float some = 0.f;
+                                for (int c = lane; c < n; c += 32) {
+                                    const float mc = ms[c * ROWS + r], f = mc == NEG ? 0.f : exp2_fast(mc - m);
+                                    some += ls[c * ROWS + r] * f;
+                                    ms[c * ROWS + r] = f;
+                                }
+#pragma unroll
+                                for (int o = 16; o; o /= 2) some += __shfl_xor_sync(0xFFFFFFFFu, some, o);
+                                l += some;
+                            }
+                            if (lane == 0) row_m[r] = m, row_l[r] = l;
+                        }
                     }
-#pragma unroll
-                    for (int o = 16; o; o /= 2) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
-                    if (lane == 0) row_m[r] = m, row_l[r] = l;
-                }
                 __syncthreads();
-                // the outputs in the order of the shares, eight of them under way
+                // the outputs in the order of the shares, several of them under way
+                const bool ready = parts <= AT_ONCE;
+                constexpr int DEEP = 8;   // (with more, the whole kernel takes registers that cost it a CTA to the SM)
                 for (int i = threadIdx.x; i < u.rows * (DP / 4); i += THREADS) {
                     const int r = i / (DP / 4), d = i % (DP / 4) * 4;
                     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
                     const float m = row_m[r];
 #pragma unroll 1
-                    for (int c0 = first_cta; c0 <= last_cta; c0 += 8) {
-                        float4 v[8];
-                        float mc[8];
+                    for (int c0 = 0; c0 < parts; c0 += DEEP) {
+                        float4 v[DEEP];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const float *p = slot_of(min(c0 + k, last_cta));
-                            v[k] = __ldcg(reinterpret_cast<const float4 *>(p) + i);
-                            mc[k] = c0 + k <= last_cta ? __ldcg(p + ROWS * DP + r) : NEG;
-                        }
+                        for (int k = 0; k < DEEP; ++k)
+                            if (c0 + k < parts) v[k] = __ldcg(reinterpret_cast<const float4 *>(slot_of(first_cta + c0 + k)) + i);
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const float f = mc[k] == NEG ? 0.f : exp2_fast(mc[k] - m);
-                            if (c0 + k <= last_cta) acc.x += v[k].x * f, acc.y += v[k].y * f, acc.z += v[k].z * f, acc.w += v[k].w * f;
-                        }
+                        for (int k = 0; k < DEEP; ++k)
+                            if (c0 + k < parts) {
+                                float f;
+                                if (ready) {
+                                    f = ms[(c0 + k) * ROWS + r];
+                                } else {
+                                    const float mc = __ldcg(slot_of(first_cta + c0 + k) + ROWS * DP + r);
+                                    f = mc == NEG ? 0.f : exp2_fast(mc - m);
+                                }
+                                acc.x += v[k].x * f, acc.y += v[k].y * f, acc.z += v[k].z * f, acc.w += v[k].w * f;
+                            }
                     }
                     if (d < D) finish(r, d, acc);
                 }

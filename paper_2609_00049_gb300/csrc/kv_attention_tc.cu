@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
         fill_window<ROWS, KT, true>(a, win, first, all);
         all += win.sum[SEQS] * a.c.n_kv;
     }
-    const Shares sh{all, min((int64_t)gridDim.x, all)};
+    const Shares sh(all, gridDim.x);
     if (blockIdx.x >= sh.ctas) return;
     if (a.n_seqs > SEQS) fill_window<ROWS, KT, true>(a, win, 0, 0);
     {

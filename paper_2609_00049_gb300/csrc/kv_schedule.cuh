@@ -11,6 +11,25 @@ namespace {
 
 constexpr int SEQS = 512;                 // sequences whose tile counts are held at a time
 
+// a / b for numbers that nearly always have 32 bits (a division of 64 takes longer than a read of global memory)
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+// Shares of `all` tiles among `ctas` CTAs that differ by one tile at most, the larger ones first.
+struct Shares {
+    int64_t all, ctas, each, more;
+    __device__ Shares() {}
+    __device__ __forceinline__ Shares(int64_t tiles, int64_t most) : all(tiles), ctas(min(most, tiles)) {
+        each = ctas > 0 ? quotient(all, ctas) : 0, more = all - each * ctas;
+    }
+    __device__ __forceinline__ int64_t begin(int64_t c) const { return c * each + min(c, more); }
+    __device__ __forceinline__ int owner(int64_t x) const {   // of tile x
+        const int64_t large = more * (each + 1);
+        return (int)(x < large ? quotient(x, each + 1) : more + quotient(x - large, each));
+    }
+};
+
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -140,6 +159,50 @@ template <int ROWS, int TILE, bool LONG> __device__ void fill_window(const KvAtt
     __syncthreads();
 }
 
+// Up to 32 sequences: every warp holds them all, a lane to a sequence, and needs no shared memory.
+struct Lanes {
+    int q0, m, len;
+    int64_t from, to;   // the lane's sequence's tiles of one head, in the running count
+    int64_t sum;        // of all
+};
+template <int ROWS, int TILE> __device__ __forceinline__ Lanes lanes_of(const KvAttnArgs &a) {
+    const int lane = threadIdx.x & 31;
+    Lanes r = {0, 0, 0, 0, 0, 0};
+    int64_t n = 0;
+    if (lane < a.n_seqs) {
+        const Seq q(a, lane);
+        r.q0 = q.q0, r.m = q.m, r.len = q.len;
+        for (int r0 = 0; r0 < q.m * a.group; r0 += ROWS) n += row_tiles<ROWS, TILE>(a, q, r0);
+    }
+    int64_t x = n;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const int64_t y = __shfl_up_sync(0xFFFFFFFFu, x, d);
+        if (lane >= d) x += y;
+    }
+    r.from = x - n, r.to = x, r.sum = __shfl_sync(0xFFFFFFFFu, x, 31);
+    return r;
+}
+template <int ROWS, int TILE>
+__device__ __forceinline__ void locate(const KvAttnArgs &a, const Lanes &s, int64_t at, Unit &u, int64_t &unit0, int &tiles) {
+    const uint32_t behind = __ballot_sync(0xFFFFFFFFu, s.to * a.c.n_kv > at);
+    u.seq = behind ? __ffs(behind) - 1 : 0;
+    u.q0 = __shfl_sync(0xFFFFFFFFu, s.q0, u.seq), u.m = __shfl_sync(0xFFFFFFFFu, s.m, u.seq), u.len = __shfl_sync(0xFFFFFFFFu, s.len, u.seq);
+    const int64_t from = __shfl_sync(0xFFFFFFFFu, s.from, u.seq), per_head = max((int64_t)1, __shfl_sync(0xFFFFFFFFu, s.to, u.seq) - from);
+    int64_t off = at - from * a.c.n_kv;
+    u.head = (int)min(quotient(off, per_head), (int64_t)a.c.n_kv - 1);
+    unit0 = at - off + u.head * per_head;
+    off -= u.head * per_head;
+    const int rows_all = u.m * a.group;
+    for (u.r0 = 0;; u.r0 += ROWS) {
+        u.rows = min(ROWS, rows_all - u.r0);
+        span(a, u.m, u.len, u.r0, u.r0 + u.rows, &u.lo, &u.hi);
+        tiles = tiles_of<TILE>(u.lo, u.hi);
+        if (off < tiles || u.r0 + ROWS >= rows_all) break;
+        off -= tiles, unit0 += tiles;
+    }
+}
+
 // The unit that holds tile `at` (at least the window's base), where it begins and how many tiles it has.  Called by
 // whole warps.
 template <int ROWS, int TILE, bool LONG>
@@ -158,7 +221,7 @@ __device__ __forceinline__ void locate(const KvAttnArgs &a, Window &win, int64_t
     u.seq = win.first + lo;
     const int64_t per_head = max((int64_t)1, win.sum[lo + 1] - win.sum[lo]);
     int64_t off = at - (win.base + win.sum[lo] * a.c.n_kv);
-    u.head = (int)min(off / per_head, (int64_t)a.c.n_kv - 1);
+    u.head = (int)min(quotient(off, per_head), (int64_t)a.c.n_kv - 1);
     unit0 = at - off + u.head * per_head;
     off -= u.head * per_head;
     const Seq q(a, u.seq);
@@ -198,18 +261,6 @@ __device__ __forceinline__ void locate(const KvAttnArgs &a, Window &win, int64_t
         off -= tiles, unit0 += tiles;
     }
 }
-
-// Even shares of `all` tiles among `ctas` CTAs.
-struct Shares {
-    int64_t all, ctas;
-    __device__ __forceinline__ int64_t begin(int64_t c) const { return c * all / ctas; }
-    __device__ __forceinline__ int owner(int64_t x) const {   // of tile x
-        int64_t c = (x * ctas + ctas - 1) / all;
-        while (c > 0 && begin(c) > x) --c;
-        while (c + 1 < ctas && begin(c + 1) <= x) ++c;
-        return (int)c;
-    }
-};
 
 }  // namespace
 }  // namespace realq
