@@ -353,6 +353,7 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
                     p[e] = x * vsc[e >> 1];
                     if (masked && s[nt][e] == NEG) p[e] = 0.f;   // whatever the scale of a token that is not seen
                 }
+                __syncwarp();
                 const uint32_t h0 = pack_half(p[0], p[1]), h1 = pack_half(p[2], p[3]);
                 pb[nt][0][0] = transposed8x8(h0), pb[nt][0][1] = transposed8x8(h1);
                 if constexpr (F32) {

@@ -40,8 +40,8 @@ namespace {
 
 constexpr uint32_t FULL = 0xFFFFFFFFu;
 constexpr int SOFT_WARPS = 16, CONV_WARPS = 4;   // (softmax: eight to a row tile; converters: four for K and four for V)
-constexpr int MMA_WARP = SOFT_WARPS + 2 * CONV_WARPS, LOAD_WARP = MMA_WARP + 1, THREADS = 32 * (MMA_WARP + 4);   // (two are idle)
-constexpr int RAW_SLOTS = 3;             // half tiles of codes on their way
+constexpr int MMA_WARP = SOFT_WARPS + 2 * CONV_WARPS, LOAD_WARP = MMA_WARP + 1, THREADS = 32 * (MMA_WARP + 4);   // (loaders of K and of V; one is idle)
+constexpr int UNIT = 32;                 // tokens whose codes come and are converted together
 constexpr int SLOTS = 4;                 // of block scales
 constexpr float NEG = -INFINITY, LIFT = 6.f, SLACK = 8.f;
 
@@ -55,21 +55,19 @@ template <int DP, bool F32> struct Shape {
     static constexpr int Q_BYTES = 128 * DP * 2;                                // one row tile, one part
     static constexpr int KV_BYTES = KT * DP * 2;
     static constexpr int SLOT_BYTES = 3 * KT * 4;
-    static constexpr int HALF = KT / 2, RAW_BYTES = HALF * DP;                  // codes come by half tiles
-    static constexpr int RING = NM * PARTS * Q_BYTES, RAW = RING + 2 * STAGES * KV_BYTES, SCALES = RAW + RAW_SLOTS * RAW_BYTES,
+    static constexpr int UNITS = KT / UNIT, RAW_BYTES = UNIT * DP, RAW_SLOTS = DP == 256 ? 1 : 3;   // of K's and of V's codes each
+    static constexpr int RING = NM * PARTS * Q_BYTES, RAW = RING + 2 * STAGES * KV_BYTES, SCALES = RAW + 2 * RAW_SLOTS * RAW_BYTES,
                          BARS = SCALES + SLOTS * SLOT_BYTES;
-    static constexpr int SMEM = BARS + 256 + 1024;
+    static constexpr int SMEM = BARS + 512 + 1024;
     static constexpr int PART = 128 * (DP + 2);                                 // numbers of a row tile's partial result
     // TMEM columns
     static constexpr int S(int i) { return i * KT; }
     static constexpr int O(int i) { return NM * KT + i * DP; }
     static constexpr int LO(int i) { return NM * (KT + DP) + i * (KT / 2); }
-    static_assert(SMEM + 512 + 1024 * NM <= 232448 && (int)sizeof(Window) <= RAW_SLOTS * RAW_BYTES && NM * (KT + DP + (F32 ? KT / 2 : 0)) <= 512, "shared and tensor memory");
+    static_assert(SMEM + 512 + 1024 * NM <= 232448 && (int)sizeof(Window) <= 2 * RAW_SLOTS * RAW_BYTES && NM * (KT + DP + (F32 ? KT / 2 : 0)) <= 512, "shared and tensor memory");
 };
 
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-// barriers 1 to 8: the two warps that share 32 rows; 9, 10: a row tile's eight; 11, 12: K's and V's converters
-template <int N> __device__ __forceinline__ void group_sync(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(N) : "memory"); }
 __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t *r) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
@@ -84,7 +82,7 @@ __device__ __forceinline__ void tmem_st_x8(uint32_t taddr, const uint32_t (&r)[8
                  : "memory");
 }
 // two fp32 values in one register pair
-__device__ __forceinline__ uint64_t pair(float a, float b) {
+__device__ __forceinline__ uint64_t two(float a, float b) {
     uint64_t r;
     asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
     return r;
@@ -143,6 +141,20 @@ __device__ __forceinline__ void tmem_ld_x32(uint32_t taddr, uint32_t *r) {   // 
           "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(taddr));
 }
+
+// A barrier of some warps, one arrival each, that gives up as every wait here does (a warp that gave up elsewhere does
+// not come).  Whole warps come to it, and to every tcgen05 instruction: lanes that have parted meet before.
+struct Meet {
+    uint32_t bar, phase = 0;
+    __device__ explicit Meet(uint64_t *b) : bar(tc::smem_u32(b)) {}
+    __device__ __forceinline__ bool operator()(volatile int *abort) {
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) tc::mbar_arrive(bar);
+        const bool ok = __all_sync(FULL, bar_wait(bar, phase, abort));
+        phase ^= 1u;
+        return ok;
+    }
+};
 
 struct Ring {   // stage and phase of something that goes round
     int s = 0, n;
@@ -204,13 +216,14 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
     Window &win = *reinterpret_cast<Window *>(smem + Sh::RAW);   // (before the first codes come)
     __shared__ int last_one[2];
     __shared__ Shares shares;
-    __shared__ Walk<ROWS, KT> walks[6];   // row tiles, K's and V's converters, products, loader
+    __shared__ Walk<ROWS, KT> walks[7];   // row tiles, K's and V's converters, products, loaders
     __shared__ float swap[2][NM][128];   // between the threads of a row
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + Sh::BARS);
     uint64_t *k_full = bars, *k_empty = bars + 2, *v_full = bars + 4, *v_empty = bars + 6;
     uint64_t *q_full = bars + 8, *s_full = bars + 10, *p_full = bars + 12, *o_full = bars + 14, *done = bars + 16;
-    uint64_t *raw_full = bars + 17, *raw_empty = raw_full + RAW_SLOTS;
-    uint32_t *tslot = reinterpret_cast<uint32_t *>(raw_empty + RAW_SLOTS);
+    uint64_t *raw_full = bars + 17, *raw_empty = raw_full + 2 * Sh::RAW_SLOTS;   // K's slots, V's slots
+    uint64_t *pairs = raw_empty + 2 * Sh::RAW_SLOTS, *tiles_meet = pairs + 8, *convs_meet = tiles_meet + 2;
+    uint32_t *tslot = reinterpret_cast<uint32_t *>(convs_meet + 2);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tslot + 1);
     uint32_t *raw_there = tslot + 2;   // of each slot's groups of 16 tokens, those that have a page
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -228,9 +241,14 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
             tc::mbar_init(tc::smem_u32(p_full + i), 8);
             tc::mbar_init(tc::smem_u32(o_full + i), 1);
         }
-        for (int i = 0; i < RAW_SLOTS; ++i) {
+        for (int i = 0; i < 2 * Sh::RAW_SLOTS; ++i) {
             tc::mbar_init(tc::smem_u32(raw_full + i), 1);
             tc::mbar_init(tc::smem_u32(raw_empty + i), CONV_WARPS);
+        }
+        for (int i = 0; i < 8; ++i) tc::mbar_init(tc::smem_u32(pairs + i), 2);
+        for (int i = 0; i < 2; ++i) {
+            tc::mbar_init(tc::smem_u32(tiles_meet + i), 8);
+            tc::mbar_init(tc::smem_u32(convs_meet + i), CONV_WARPS);
         }
         tc::mbar_init(tc::smem_u32(done), 1);
         *abort_flag = 0;
@@ -253,11 +271,12 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
         locate<ROWS, KT, true>(a, win, at0, u0, first0, tiles0);
         fence_async_smem();   // (the codes' copies come over win)
         __syncthreads();
-        if (threadIdx.x < 6) walks[threadIdx.x].start(u0, first0, tiles0, at0, sh.begin(blockIdx.x + 1));
+        if (threadIdx.x < 7) walks[threadIdx.x].start(u0, first0, tiles0, at0, sh.begin(blockIdx.x + 1));
         if (threadIdx.x == 0) shares = sh;
     }
-    Walk<ROWS, KT> &w = walks[warp == LOAD_WARP ? 5 : (warp < SOFT_WARPS ? warp >> 3 : (warp - SOFT_WARPS) / 4 + 2)];
+    Walk<ROWS, KT> &w = walks[warp >= LOAD_WARP ? min(warp - LOAD_WARP, 1) + 5 : (warp < SOFT_WARPS ? warp >> 3 : (warp - SOFT_WARPS) / 4 + 2)];
 
+    __syncwarp();
     if (warp == 0) tc::tmem_alloc(tc::smem_u32(tslot), 512);
     tc::fence_before_sync();
     __syncthreads();
@@ -267,7 +286,8 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
 
     if (warp < SOFT_WARPS) {
         // ---------------- softmax: a thread has half of a row of row tile i ----------------
-        const int i = warp >> 3, half = (warp >> 2) & 1, row = threadIdx.x & 127, pair_id = 1 + (warp & 3) + 4 * i;
+        const int i = warp >> 3, half = (warp >> 2) & 1, row = threadIdx.x & 127;
+        Meet pair(pairs + (warp & 3) + 4 * i), all_rows(tiles_meet + i);   // the two warps that share 32 rows; a row tile's eight
         constexpr int COLS = KT / 2;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_at = tmem + lanes + Sh::S(i) + half * COLS, o_at = tmem + lanes + Sh::O(i), lo_at = tmem + lanes + Sh::LO(i) + half * (COLS / 2);
@@ -350,17 +370,17 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
             fence_async_smem();
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(tc::smem_u32(q_full + i));
-            group_sync<64>(pair_id);
+            ok = pair(abort_flag) && ok;
             const float mine = swap[0][i][row];
-            group_sync<64>(pair_id);
+            ok = pair(abort_flag) && ok;
             return mine;
         };
         float rs = 0.f;
         bool loaded = false;
         const auto advance = [&]() {
-            group_sync<256>(9 + i);
+            ok = all_rows(abort_flag) && ok;
             if ((threadIdx.x & 255) == 0) w.next(a);
-            group_sync<256>(9 + i);
+            ok = all_rows(abort_flag) && ok;
         };
         while (w.more() && ok) {
             const int count = w.count;
@@ -431,7 +451,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                 float base = 0.f;
                 const auto agree = [&]() {
                     swap[half][i][row] = top;
-                    group_sync<64>(pair_id);
+                    ok = pair(abort_flag) && ok;
                     top = fmaxf(top, swap[half ^ 1][i][row]);
                     const bool grew = top > (m == NEG ? NEG : m + SLACK);
                     if (__any_sync(FULL, grew)) {
@@ -458,17 +478,17 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                     if constexpr (!fines) {
                         const float4 b = reinterpret_cast<const float4 *>(sc)[c / 16];
                         const float c1 = b.x * factor, c0 = b.y + base;
-                        const uint64_t c11 = pair(c1, c1), c00 = pair(c0, c0);
+                        const uint64_t c11 = two(c1, c1), c00 = two(c0, c0);
                         uint64_t part2 = 0;
 #pragma unroll
                         for (int j = 0; j < 16; j += 2) {
-                            float2 x = halves(fma2(pair(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), c11, c00));
+                            float2 x = halves(fma2(two(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), c11, c00));
                             if constexpr (masks) {
                                 x.x = seen(c + j) ? x.x : NEG;
                                 x.y = seen(c + j + 1) ? x.y : NEG;
                             }
                             x.x = exp2_fast(x.x), x.y = exp2_fast(x.y);
-                            part2 = add2(part2, pair(x.x, x.y));
+                            part2 = add2(part2, two(x.x, x.y));
                             hi[j / 2] = pack_half(x.x, x.y);
                             if constexpr (F32) lo[j / 2] = pack_rest(x.x, x.y, hi[j / 2]);
                         }
@@ -495,6 +515,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                             if constexpr (F32) lo[j / 2] = pack_rest(x[0], x[1], hi[j / 2]), lo[j / 2 + 1] = pack_rest(x[2], x[3], hi[j / 2 + 1]);
                         }
                     }
+                    if constexpr (masks) __syncwarp();
                     tmem_st_x8(s_at + c / 2, hi);
                     if constexpr (F32) tmem_st_x8(lo_at + c / 2, lo);
                 };
@@ -525,6 +546,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                     over_few([&](int c, uint32_t *v) { weights(yes{}, yes{}, c, v); });
                 }
                 tc::tmem_wait_st();
+                if (!ok) break;
                 tc::fence_before_sync();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(tc::smem_u32(p_full + i));
@@ -535,6 +557,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
             if (!whole) first_cta = shares.owner(w.unit0), last_cta = shares.owner(w.unit0 + w.tiles - 1);
             // the next unit's queries while the last products run (this one's have been read: its last scores are there)
             advance();
+            if (!ok) break;
             loaded = w.more() && 128 * i < w.u.rows;
             if (loaded) rs = load_q(w.u);
             ok = __all_sync(FULL, bar_wait(tc::smem_u32(o_full + i), o_phase, abort_flag));
@@ -572,12 +595,14 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
             const auto slot_of = [&](int c, bool begins) { return a.part + ((int64_t)(2 * c + (begins ? 1 : 0)) * NM + i) * Sh::PART; };
             float *mine = slot_of(blockIdx.x, begins);
             swap[half][i][row] = l;
-            group_sync<64>(pair_id);
+            ok = pair(abort_flag) && ok;
             l += swap[half ^ 1][i][row];
-            group_sync<64>(pair_id);
+            ok = pair(abort_flag) && ok;
             swap[half][i][row] = bad;
-            group_sync<64>(pair_id);
+            ok = pair(abort_flag) && ok;
             bad += swap[half ^ 1][i][row];
+            ok = pair(abort_flag) && ok;   // (the next scores' maximum goes there)
+            if (!ok) break;
             const float inv = 1.f / l;
 #pragma unroll 1
             for (int c = 16 * half; c < D; c += 32) {
@@ -598,6 +623,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                         to[0] = make_float4(y[0], y[1], y[2], y[3]), to[128] = make_float4(y[4], y[5], y[6], y[7]);
                     }
                 }
+                __syncwarp();
             }
             tc::fence_before_sync();
             if (whole) {
@@ -606,12 +632,14 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
             }
             if (half == 0) mine[128 * DP + row] = m, mine[128 * DP + 128 + row] = l;
             __threadfence();
-            group_sync<256>(9 + i);
+            ok = all_rows(abort_flag);
+            if (!ok) break;
             if ((threadIdx.x & 255) == 0) {
                 const unsigned others = (unsigned)(last_cta - first_cta);
                 last_one[i] = atomicInc(reinterpret_cast<unsigned *>(a.counters) + 2 * first_cta + i, others) == others;
             }
-            group_sync<256>(9 + i);
+            ok = all_rows(abort_flag);
+            if (!ok) break;
             if (!last_one[i]) continue;
             __threadfence();
             float mm = NEG, ll = 0.f;
@@ -642,7 +670,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
         }
         if (!ok) *abort_flag = 1;
     } else if (warp < MMA_WARP) {
-        // ---------------- converters of K or of V: codes -> fp16, half a tile at a time ----------------
+        // ---------------- converters of K or of V: codes -> fp16, 32 tokens at a time ----------------
         // Eight lanes take four pieces of 16 channels of two neighbouring tokens, in different boxes where there are
         // several: neither the reading nor the writing (rows of odd and even tokens swizzled apart) meets in a bank.
         const bool is_v = warp >= SOFT_WARPS + CONV_WARPS;
@@ -651,51 +679,65 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
         const int to0 = token0 * 128 + (((2 * piece) ^ (token0 & 7)) << 4), to1 = token0 * 128 + (((2 * piece + 1) ^ (token0 & 7)) << 4);
         uint8_t *const stages = smem + Sh::RING + (is_v ? Sh::STAGES * Sh::KV_BYTES : 0);
         uint64_t *const empty = is_v ? v_empty : k_empty, *const filled = is_v ? v_full : k_full;
-        Ring ring(Sh::STAGES), raw(RAW_SLOTS);
-        if (is_v) raw.next(), raw.next();      // halves come in the order K, K, V, V
+        uint64_t *const raw_in = raw_full + (is_v ? Sh::RAW_SLOTS : 0), *const raw_out = raw_empty + (is_v ? Sh::RAW_SLOTS : 0);
+        const uint8_t *const raws = smem + Sh::RAW + (is_v ? Sh::RAW_SLOTS * Sh::RAW_BYTES : 0) + token0 * D + 16 * piece;
+        uint32_t *const theres = raw_there + (is_v ? Sh::RAW_SLOTS : 0);
+        Meet meet(convs_meet + is_v);
+        Ring ring(Sh::STAGES), raw(Sh::RAW_SLOTS);
         while (w.more() && ok) {
-            const int count = w.count;
+            const int units = Sh::UNITS * w.count;
 #pragma unroll 1
-            for (int h = 0; h < 2 * count; ++h) {
-                if (!(h & 1)) ok = __all_sync(FULL, bar_wait(tc::smem_u32(empty + ring.s), ring.phase ^ 1u, abort_flag));
-                if (ok) ok = __all_sync(FULL, bar_wait(tc::smem_u32(raw_full + raw.s), raw.phase, abort_flag));
+            for (int h = 0; h < units; ++h) {
+                const int part = h % Sh::UNITS;
+                if (part == 0) ok = __all_sync(FULL, bar_wait(tc::smem_u32(empty + ring.s), ring.phase ^ 1u, abort_flag));
+                if (ok) ok = __all_sync(FULL, bar_wait(tc::smem_u32(raw_in + raw.s), raw.phase, abort_flag));
                 if (!ok) break;
-                const uint8_t *from = smem + Sh::RAW + raw.s * Sh::RAW_BYTES + token0 * D + 16 * piece;
-                uint8_t *to = stages + ring.s * Sh::KV_BYTES + (h & 1) * Sh::HALF * 128;
-                const uint32_t there = raw_there[raw.s];
-#pragma unroll 1
-                for (int i = 0; i < Sh::HALF / (8 * CONV_WARPS); ++i)
+                const uint8_t *from = raws + raw.s * Sh::RAW_BYTES;
+                uint8_t *to = stages + ring.s * Sh::KV_BYTES + part * UNIT * 128;
+                const bool there = (theres[raw.s] >> (token0 >> 4)) & 1u;
+                uint4 x[Sh::BOXES];
 #pragma unroll
-                    for (int b = 0; b < Sh::BOXES; ++b) {
-                        const int box = Sh::BOXES > 1 ? b ^ sel : 0, skip = i * 8 * CONV_WARPS;
-                        if (4 * box + piece < pieces) {
-                            uint4 x = *reinterpret_cast<const uint4 *>(from + skip * D + 64 * box);
-                            if (!((there >> ((token0 + skip) >> 4)) & 1u)) x = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
-                            uint8_t *line = to + box * (KT * 128) + skip * 128;
-                            *reinterpret_cast<uint4 *>(line + to0) = make_uint4(codes01(x.x), codes23(x.x), codes01(x.y), codes23(x.y));
-                            *reinterpret_cast<uint4 *>(line + to1) = make_uint4(codes01(x.z), codes23(x.z), codes01(x.w), codes23(x.w));
-                        }
-                    }
-                if (h & 1) fence_async_smem();
+                for (int k = 0; k < Sh::BOXES; ++k) {
+                    const int box = Sh::BOXES > 1 ? k ^ sel : 0;
+                    x[k] = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
+                    if (4 * box + piece < pieces && there) x[k] = *reinterpret_cast<const uint4 *>(from + 64 * box);
+                }
                 __syncwarp();
-                if (lane == 0) {
-                    tc::mbar_arrive(tc::smem_u32(raw_empty + raw.s));
-                    if (h & 1) tc::mbar_arrive(tc::smem_u32(filled + ring.s));
+                if (lane == 0) tc::mbar_arrive(tc::smem_u32(raw_out + raw.s));   // the next codes may come
+#pragma unroll
+                for (int k = 0; k < Sh::BOXES; ++k) {
+                    const int box = Sh::BOXES > 1 ? k ^ sel : 0;
+                    uint8_t *line = to + box * (KT * 128);
+                    if (4 * box + piece < pieces) {
+                        *reinterpret_cast<uint4 *>(line + to0) = make_uint4(codes01(x[k].x), codes23(x[k].x), codes01(x[k].y), codes23(x[k].y));
+                        *reinterpret_cast<uint4 *>(line + to1) = make_uint4(codes01(x[k].z), codes23(x[k].z), codes01(x[k].w), codes23(x[k].w));
+                    }
                 }
                 raw.next();
-                if (h & 1) ring.next(), raw.next(), raw.next();
+                if (part == Sh::UNITS - 1) {
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive(tc::smem_u32(filled + ring.s));
+                    ring.next();
+                }
             }
-            group_sync<128>(11 + is_v);
-            if ((threadIdx.x & 127) == 0 && ok) w.next(a);
-            group_sync<128>(11 + is_v);
+            if (!ok || !meet(abort_flag)) {
+                ok = false;
+                break;
+            }
+            if ((threadIdx.x & 127) == 0) w.next(a);
+            ok = meet(abort_flag);
         }
         if (!ok) *abort_flag = 1;
     } else {
-        if (warp == LOAD_WARP) {
-        // ---------------- loader: pages, codes by bulk copies of 16 tokens, scales ----------------
-        const bool fine = a.c.log_block < 4;
-        constexpr int GROUPS = Sh::HALF / 16;
-        Ring kring(Sh::STAGES), raw(RAW_SLOTS);
+        if (warp == LOAD_WARP || warp == LOAD_WARP + 1) {
+        // ---------------- loaders of K, with the scales, and of V: pages, codes by bulk copies of 16 tokens ----------------
+        const bool is_v = warp != LOAD_WARP, fine = a.c.log_block < 4;
+        uint64_t *const raw_in = raw_full + (is_v ? Sh::RAW_SLOTS : 0), *const raw_out = raw_empty + (is_v ? Sh::RAW_SLOTS : 0);
+        uint8_t *const raws = smem + Sh::RAW + (is_v ? Sh::RAW_SLOTS * Sh::RAW_BYTES : 0);
+        uint32_t *const theres = raw_there + (is_v ? Sh::RAW_SLOTS : 0);
+        const uint8_t *const codes = is_v ? a.c.v_codes : a.c.k_codes;
+        Ring kring(Sh::STAGES), raw(Sh::RAW_SLOTS);
         uint32_t fills = 0;
         int slot = 0;
         while (w.more() && ok) {
@@ -704,7 +746,18 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
             const int base = (lo / KT + w.from) * KT;
             const auto page_of = [&](int t) {   // of the tile's 16 tokens `lane`
                 const int k0 = base + t * KT + 16 * lane;
-                return t < count && lane < 2 * GROUPS && k0 < hi && k0 + 16 > lo ? __ldg(table + (k0 >> a.c.log_page)) : -1;
+                return t < count && lane < KT / 16 && k0 < hi && k0 + 16 > lo ? __ldg(table + (k0 >> a.c.log_page)) : -1;
+            };
+            float ks = 0.f, vs = 0.f;
+            bool there_s = false;
+            const auto scales_of = [&](int t, int pg16, int n) {   // of the tile's token or 16 tokens n
+                const int token = fine ? n : 16 * n, pg = __shfl_sync(FULL, pg16, (token >> 4) & 31);
+                there_s = token < KT && pg >= 0 && pg < a.c.n_pages;
+                if (there_s) {
+                    const int pl = (base + t * KT + token) & ((1 << a.c.log_page) - 1);
+                    const int64_t s = (((int64_t)pg * a.c.n_kv + head) << (a.c.log_page - a.c.log_block)) + (pl >> a.c.log_block);
+                    ks = __ldg(a.c.k_scale + s), vs = __ldg(a.c.v_scale + s);
+                }
             };
             int page = page_of(0), next_page = page_of(1);
 #pragma unroll 1
@@ -713,45 +766,47 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                 const uint32_t there = __ballot_sync(FULL, good);
                 const int k0 = base + t * KT + 16 * lane, place = k0 & ((1 << a.c.log_page) - 1);
                 const int64_t tile = (int64_t)page * a.c.n_kv + head;
-                const int64_t at = ((tile << a.c.log_page) + place) * D;
+                const uint8_t *src = codes + ((tile << a.c.log_page) + place) * D;
+                if (!is_v && !fine) scales_of(t, page, lane);   // (under way with the codes)
 #pragma unroll 1
-                for (int h = 0; h < 4 && ok; ++h, raw.next()) {
-                    ok = __all_sync(FULL, bar_wait(tc::smem_u32(raw_empty + raw.s), raw.phase ^ 1u, abort_flag));
+                for (int h = 0; h < Sh::UNITS; ++h, raw.next()) {
+                    ok = __all_sync(FULL, bar_wait(tc::smem_u32(raw_out + raw.s), raw.phase ^ 1u, abort_flag));
                     if (!ok) break;
-                    const uint32_t mine = there >> ((h & 1) * GROUPS) & ((1u << GROUPS) - 1), full = tc::smem_u32(raw_full + raw.s);
+                    const uint32_t mine = there >> (2 * h) & 3u, full = tc::smem_u32(raw_in + raw.s);
                     if (lane == 0) {
-                        raw_there[raw.s] = mine;
+                        theres[raw.s] = mine;
                         tc::mbar_arrive_expect_tx(full, __popc(mine) * 16 * D);
                     }
                     ++fills;
                     __syncwarp();
-                    if (good && lane / GROUPS == (h & 1))
-                        bulk_load(tc::smem_u32(smem + Sh::RAW + raw.s * Sh::RAW_BYTES + (lane % GROUPS) * 16 * D), (h & 2 ? a.c.v_codes : a.c.k_codes) + at,
-                                  16 * D, full);
-                    if (h == 0) {   // the tile's scales (the slot's last readers are behind what emptied the stages)
-                        float *sc = reinterpret_cast<float *>(smem + Sh::SCALES + slot * Sh::SLOT_BYTES);
+                    if (good && lane / 2 == h) bulk_load(tc::smem_u32(raws + raw.s * Sh::RAW_BYTES + (lane & 1) * 16 * D), src, 16 * D, full);
+                    __syncwarp();
+                }
+                if (!is_v && ok) {
+                    // The tile's scales, once the stage is free: then three tiles before have their weights, and with them
+                    // the slot's last readers are done, and the stage's barrier is in the phase of this tile.
+                    ok = __all_sync(FULL, bar_wait(tc::smem_u32(k_empty + kring.s), kring.phase ^ 1u, abort_flag));
+                    if (!ok) break;
+                    float *sc = reinterpret_cast<float *>(smem + Sh::SCALES + slot * Sh::SLOT_BYTES);
+                    const int entries = fine ? KT : KT / 16;
 #pragma unroll 1
-                        for (int n = lane; n < (fine ? KT : KT / 16); n += 32) {
-                            const int token = fine ? n : 16 * n;
-                            const int pg = __shfl_sync(fine ? FULL : (1u << (KT / 16)) - 1, page, token >> 4);
-                            float ks = 0.f, lv = NEG, iv = 0.f, nv = 0.f;   // tokens without a page weigh nothing
-                            if (pg >= 0 && pg < a.c.n_pages) {
-                                const int pl = (base + t * KT + token) & ((1 << a.c.log_page) - 1);
-                                const int64_t s = (((int64_t)pg * a.c.n_kv + head) << (a.c.log_page - a.c.log_block)) + (pl >> a.c.log_block);
-                                ks = __ldg(a.c.k_scale + s);
-                                const float vs = __ldg(a.c.v_scale + s);
-                                const bool nan = vs != vs;   // (its part in the sum stays: the scores are not concerned)
-                                nv = nan ? vs : 0.f;
-                                lv = nan ? 0.f : fmaxf(log2_fast(vs), -100.f), iv = exp2_fast(-lv);   // (a scale below 2^-100 counts as that)
-                            }
+                    for (int n0 = 0; n0 < entries; n0 += 32) {
+                        const int n = n0 + lane;
+                        if (n0 > 0 || fine) scales_of(t, page, n);
+                        // tokens without a page weigh nothing; a scale below 2^-100 counts as that; a NaN's part in the sum
+                        // stays (the scores are not concerned)
+                        const bool nan = there_s && vs != vs;
+                        const float k = there_s ? ks : 0.f, nv = nan ? vs : 0.f;
+                        const float lv = !there_s ? NEG : (nan ? 0.f : fmaxf(log2_fast(vs), -100.f)), iv = !there_s ? 0.f : exp2_fast(-lv);
+                        if (n < entries) {
                             if (fine)
-                                sc[n] = ks, sc[KT + n] = lv, sc[2 * KT + n] = nv != nv ? -iv : iv;
+                                sc[n] = k, sc[KT + n] = lv, sc[2 * KT + n] = nan ? -iv : iv;
                             else
-                                reinterpret_cast<float4 *>(sc)[n] = make_float4(ks, lv, iv, nv);
+                                reinterpret_cast<float4 *>(sc)[n] = make_float4(k, lv, iv, nv);
                         }
-                        __syncwarp();
-                        if (lane == 0) tc::mbar_arrive(tc::smem_u32(k_full + kring.s));
                     }
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive(tc::smem_u32(k_full + kring.s));
                 }
                 page = next_page;
                 next_page = page_of(t + 2);
@@ -763,8 +818,8 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
         if (!ok) {   // copies under way land before the CTA ends
             *abort_flag = 1;
             int never = 0;
-            for (uint32_t k = fills > RAW_SLOTS ? fills - RAW_SLOTS : 0; k < fills; ++k)
-                tc::mbar_wait(tc::smem_u32(raw_full + k % RAW_SLOTS), k / RAW_SLOTS & 1u, &never, 100000000ull);
+            for (uint32_t k = fills > Sh::RAW_SLOTS ? fills - Sh::RAW_SLOTS : 0; k < fills; ++k)
+                tc::mbar_wait(tc::smem_u32(raw_in + k % Sh::RAW_SLOTS), k / Sh::RAW_SLOTS & 1u, &never, 100000000ull);
         }
         } else if (warp == MMA_WARP) {
         // ---------------- products ----------------
