@@ -1,0 +1,122 @@
+"""Generating with an 8-bit key/value cache: sequences in pages, their new tokens'
+rotary positions, keys and values appended, attention over what is cached.
+
+    cache = Cache8(layers, n_pages, rows, max_tokens, n_kv=8, head_dim=128)
+    step = cache.begin([5, 0, 1])                       # new tokens of each row's sequence
+    for layer in range(layers):
+        out = cache.attend(step, layer, q, k, v)        # tokens x heads x head_dim; q and k are turned in place
+    cache.fork([0], [1])                                # row 1 goes on from row 0's sequence, sharing its pages
+    cache.release([0])
+    cache.compact()
+
+A step's rows are the table's: row s has `counts[s]` new tokens (0: it waits), which
+lie one row's after the other's in q, k and v.  `begin` takes the pages
+(realq_pages_reserve), `attend` runs realq_rotary, realq_kv_append and
+realq_kv_attention; the modules around it are the caller's
+(realq_int8_product on the sweep's codes, for instance).  Everything is enqueued
+on the current stream (or `stream`); nothing is read back but by `check`, which
+raises RealqError where the pool had too few pages: the step's tokens then have
+position -1, and appending them does nothing.  Buffers are allocated with torch;
+no arithmetic happens here.
+"""
+from __future__ import annotations
+
+from dataclasses import dataclass
+from typing import Optional, Sequence, Union
+
+import torch
+
+from . import (kv_cache, kv_pages, realq_kv_append, realq_kv_attention, realq_kv_attention_workspace_size,
+               realq_pages_compact, realq_pages_fork, realq_pages_release, realq_pages_reserve,
+               realq_pages_workspace_size, realq_rotary, realq_rotary_frequencies, realq_workspace_status, workspace)
+
+Rows = Union[Sequence[int], torch.Tensor]
+
+
+@dataclass
+class Step:
+    """One step's tokens: where each row's begin, their positions, the most of a row."""
+    starts: torch.Tensor      # rows + 1
+    positions: torch.Tensor   # tokens
+    most: int
+
+
+class Cache8:
+    """Keys and values of `layers` layers in `n_pages` pages of page_size tokens, 8-bit
+    codes with a scale for each scale_block tokens and head, for up to `rows`
+    sequences of max_tokens.  inv_freq: rotary frequencies (float64, by default
+    base 10000 over the whole head), amplitude and interleaved as for realq_rotary.
+    One stream at a time: its workspaces are reused from call to call."""
+
+    def __init__(self, layers: int, n_pages: int, rows: int, max_tokens: int, n_kv: int, head_dim: int, page_size: int = 64,
+                 scale_block: int = 16, inv_freq: Optional[torch.Tensor] = None, amplitude: float = 1.0, interleaved: bool = False,
+                 device="cuda"):
+        shape = (layers, n_pages, n_kv, page_size)
+        new = lambda *s, dtype: torch.zeros(s, dtype=dtype, device=device)  # noqa: E731
+        codes = [torch.full((*shape, head_dim), 128, dtype=torch.uint8, device=device) for _ in range(2)]
+        scales = [new(*shape[:3], page_size // scale_block, dtype=torch.float32) for _ in range(2)]
+        self.cache = kv_cache(codes[0], codes[1], scales[0], scales[1])
+        max_pages = -(-max_tokens // page_size)
+        self.used, self.lengths = new(n_pages, dtype=torch.int32), new(rows, dtype=torch.int32)
+        self.tables = torch.full((rows, max_pages), -1, dtype=torch.int32, device=device)
+        self.pages = kv_pages(self.used, self.tables, self.lengths)
+        self.moved_to = new(n_pages, dtype=torch.int32)
+        self.inv_freq = (realq_rotary_frequencies(head_dim) if inv_freq is None else inv_freq).to(device)
+        self.amplitude, self.interleaved = amplitude, interleaved
+        self._pages_ws = workspace(realq_pages_workspace_size(n_pages, rows, max_pages), device)
+        self._attend_ws = None
+
+    def _ints(self, rows: Rows) -> torch.Tensor:
+        if isinstance(rows, torch.Tensor):
+            return rows
+        return torch.tensor(list(rows), dtype=torch.int32).to(self.used.device)
+
+    def begin(self, counts: Sequence[int], stream=None) -> Step:
+        """Room for counts[s] new tokens in each row."""
+        if len(counts) != self.tables.shape[0] or min(counts) < 0:
+            raise ValueError(f"counts: {self.tables.shape[0]} numbers from 0 on expected")
+        at = [0]
+        for n in counts:
+            at.append(at[-1] + n)
+        step = Step(self._ints(at), torch.empty(at[-1], dtype=torch.int64, device=self.used.device), max(counts))
+        realq_pages_reserve(self.pages, step.starts, step.positions, self.cache, ws=self._pages_ws, stream=stream)
+        return step
+
+    def attend(self, step: Step, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+               out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, window: int = 0,
+               scale: Optional[float] = None, stream=None) -> torch.Tensor:
+        """The step's tokens through one layer: q and k get their positions (in place),
+        k and v go into the cache, and q attends to all of its row's tokens so far."""
+        T, H, _ = q.shape
+        if T != step.positions.shape[0]:
+            raise ValueError(f"q: {step.positions.shape[0]} tokens expected, got {T}")
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if T == 0:
+            return out
+        realq_rotary(q, step.positions, self.inv_freq, q, k=k, k_out=k, interleaved=self.interleaved, amplitude=self.amplitude,
+                     stream=stream)
+        realq_kv_append(self.cache, layer, k, v, step.starts, step.positions, self.tables, stream=stream)
+        if self._attend_ws is None:   # (its size depends on the GPU alone)
+            self._attend_ws = workspace(realq_kv_attention_workspace_size(self.cache, self.tables.shape[0], T, H), q.device)
+        return realq_kv_attention(q, self.cache, layer, step.starts, self.lengths, self.tables, out, lse=lse, scale=scale,
+                                  window=window, max_new=step.most, ws=self._attend_ws, stream=stream)
+
+    def fork(self, src: Rows, dst: Rows, stream=None) -> None:
+        """Rows dst[i] go on from rows src[i]'s sequences, all at once (a beam search's reordering)."""
+        realq_pages_fork(self.pages, self._ints(src), self._ints(dst), ws=self._pages_ws, stream=stream)
+
+    def release(self, rows: Rows, stream=None) -> None:
+        """The rows' sequences leave."""
+        realq_pages_release(self.pages, self._ints(rows), stream=stream)
+
+    def compact(self, stream=None) -> torch.Tensor:
+        """Pages in use to the front of the pool; each page's new number (-1: free)."""
+        realq_pages_compact(self.pages, self.cache, self.used, self.tables, self.moved_to, ws=self._pages_ws, stream=stream)
+        return self.moved_to
+
+    def check(self, stream=None) -> None:
+        """Raises RealqError if a step since the last check found too few pages, or a bounded wait gave up (synchronizes)."""
+        for ws in (self._pages_ws, self._attend_ws):
+            if ws is not None:
+                realq_workspace_status(ws, stream=stream)
