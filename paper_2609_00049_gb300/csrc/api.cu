@@ -1094,10 +1094,10 @@ realq_status_t realq_kv_append(realq_stream_t stream, const realq_kv_cache_t *ca
     REALQ_TRY(check_heads(who, "v", T, cache->n_kv, cache->head_dim, v, v_ld, v_hs, dtype));
     if (T == 0 || n_seqs == 0 || max_pages == 0) return REALQ_OK;
     if (!positions || !aligned_to(8, positions)) return fail(REALQ_ERR_INVALID_ARG, "kv_append: positions NULL or not aligned to their type");
-    if (((T >> a.c.log_block) + 2 * n_seqs) * 2 * a.c.n_kv / 4 >= INT32_MAX) return fail(REALQ_ERR_UNSUPPORTED, "kv_append: too many blocks");
+    if ((T >> a.c.log_block) + 2 * n_seqs >= INT32_MAX) return fail(REALQ_ERR_UNSUPPORTED, "kv_append: too many blocks");
     a.n_seqs = (int)n_seqs, a.T = T, a.k = k, a.k_ld = k_ld, a.k_hs = k_hs, a.v = v, a.v_ld = v_ld, a.v_hs = v_hs;
     a.starts = starts, a.positions = positions, a.tables = tables, a.max_pages = max_pages;
-    return kv_append(S(stream), a, dtype);
+    return kv_append(S(stream), a, dtype, num_sms());
 }
 
 realq_status_t realq_kv_read(realq_stream_t stream, const realq_kv_cache_t *cache, int64_t layer, int64_t n_seqs, int64_t T,
@@ -1112,7 +1112,7 @@ realq_status_t realq_kv_read(realq_stream_t stream, const realq_kv_cache_t *cach
         return fail(REALQ_ERR_INVALID_ARG, "kv_read: an output is not aligned to its type");
     if (T == 0 || n_seqs == 0 || (!k_out && !v_out)) return REALQ_OK;
     if (!positions || !aligned_to(8, positions)) return fail(REALQ_ERR_INVALID_ARG, "kv_read: positions NULL or not aligned to their type");
-    if (T * a.c.n_kv * (a.c.head_dim / 16) / 128 >= INT32_MAX) return fail(REALQ_ERR_UNSUPPORTED, "kv_read: too many values");
+    if (T >= INT32_MAX) return fail(REALQ_ERR_UNSUPPORTED, "kv_read: too many values");
     a.n_seqs = (int)n_seqs, a.T = T, a.max_pages = max_pages, a.starts = starts, a.positions = positions, a.tables = tables;
     a.k_out = k_out, a.v_out = v_out;
     return kv_read(S(stream), a, dtype);

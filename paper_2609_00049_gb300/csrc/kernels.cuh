@@ -202,7 +202,7 @@ struct KvReadArgs {
     const int64_t *positions;
     void *k_out, *v_out;
 };
-realq_status_t kv_append(cudaStream_t s, const KvAppendArgs &a, realq_dtype_t dt);
+realq_status_t kv_append(cudaStream_t s, const KvAppendArgs &a, realq_dtype_t dt, int sms);
 realq_status_t kv_read(cudaStream_t s, const KvReadArgs &a, realq_dtype_t dt);
 
 constexpr int KV_MAX_CTAS_PER_SM = 4;

@@ -49,11 +49,8 @@ size_t carve(void *ws, int64_t n_pages, int64_t n_rows, int64_t max_pages, PageW
 }
 
 __device__ __forceinline__ int rank() { return (int)tc::cluster_rank(); }
-// all threads of the cluster; what they wrote to global memory before is seen after
-__device__ __forceinline__ void meet() {
-    __threadfence();
-    tc::cluster_sync();
-}
+// all threads of the cluster; what they wrote to global memory before is seen after (the barrier releases and acquires)
+__device__ __forceinline__ void meet() { tc::cluster_sync(); }
 // memory that other CTAs of the cluster write during the kernel: past the L1
 __device__ __forceinline__ int peek(const int *p) { return __ldcg(p); }
 

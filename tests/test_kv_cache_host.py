@@ -91,8 +91,6 @@ def test_append_and_read_refusals(L):
         assert call(c=cache(), S=(1 << 24) + 1) == UNSUPPORTED and call(c=cache(), T=(1 << 30) + 1) == UNSUPPORTED
         assert call(c=cache(), M=(1 << 24) + 1) == UNSUPPORTED
         assert call(c=cache(), T=0, st=None, pos=None, tab=None) == 0
-    assert app(c=cache(n_kv=4096, scale_block=1), T=1 << 30, kld=1 << 20, vld=1 << 20) == UNSUPPORTED
-    assert read(c=cache(n_kv=4096), T=1 << 30) == UNSUPPORTED
 
 
 def test_attention_refusals(L):
