@@ -549,21 +549,26 @@ ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3}
 
 
 def _ints(t: Optional[torch.Tensor], shape, name: str, device: int, dtype=torch.int32):
-    """Address of a list on the device of the call."""
-    p = _arg(t, dtype, shape, name)
-    if t is not None and t.get_device() != device:
-        raise ValueError(f"{name}: on another device than the cache or the heads")
-    return p
+    """Address of a list (or another contiguous buffer) on the device of the call."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    _arg(t, dtype, shape, name)
+    raise ValueError(f"{name}: on another device than the cache or the heads")
 
 
 def _heads(t: torch.Tensor, name: str, device: int, shape=None):
     """Address, token stride and head stride of tokens x heads x values, of which
     the tokens and heads may lie apart."""
-    if t.dim() != 3 or (shape is not None and t.shape != shape):
-        raise ValueError(f"{name}: expected {'tokens x heads x head_dim' if shape is None else tuple(shape)}, got {tuple(t.shape)}")
+    s = t.shape
+    if len(s) != 3 or (shape is not None and s != shape):
+        raise ValueError(f"{name}: expected {'tokens x heads x head_dim' if shape is None else tuple(shape)}, got {tuple(s)}")
     if t.get_device() != device:
         raise ValueError(f"{name}: expected a CUDA tensor on the device of the other arguments")
-    T, H, D = t.shape
+    T, H, D = s
+    if t.is_contiguous():
+        return t.data_ptr(), H * D, D
     if D > 1 and t.stride(2) != 1:
         raise ValueError(f"{name}: a head's values have to lie together")
     hs = t.stride(1) if H > 1 else D
@@ -631,19 +636,24 @@ def realq_rotary(q: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tenso
     """Rotary positions of q (tokens x heads x head_dim) and k in one launch, over
     the first 2 x len(inv_freq) values of each head; outputs may be the inputs.
     With transpose the gradient: from d q_out, d k_out to d q, d k."""
-    dev = _on(q.get_device())
-    T, H, D = q.shape if q.dim() == 3 else (0, 0, 0)
-    dt = _dtype(q)
-    a = (*_heads(q, "q", dev), *_heads(q_out, "q_out", dev, q.shape))
-    n_k, b = 0, (None, 0, 0, None, 0, 0)
+    dev, dt, kind = _on(q.get_device()), _dtype(q), q.dtype
+    shape, n_k, b = q.shape, 0, (None, 0, 0, None, 0, 0)
+    a = (*_heads(q, "q", dev), *_heads(q_out, "q_out", dev, shape))
+    T, H, D = shape
     if k is not None:
-        if k_out is None or k.dim() != 3 or k.shape[0] != T or k.shape[2] != D:
+        ks = k.shape
+        if k_out is None or len(ks) != 3 or ks[0] != T or ks[2] != D:
             raise ValueError(f"k, k_out: {T} tokens x kv heads x {D} expected")
-        n_k, b = k.shape[1], (*_heads(k, "k", dev), *_heads(k_out, "k_out", dev, k.shape))
-    if any(t is not None and t.dtype != q.dtype for t in (q_out, k, k_out)):
+        n_k, b = ks[1], (*_heads(k, "k", dev), *_heads(k_out, "k_out", dev, ks))
+        if k.dtype is not kind or k_out.dtype is not kind:
+            raise ValueError("q, k and their outputs have one dtype")
+    if q_out.dtype is not kind:
         raise ValueError("q, k and their outputs have one dtype")
-    _check(lib().realq_rotary(_stream(stream), T, D, 2 * inv_freq.shape[0], _ints(positions, (T,), "positions", dev, torch.int64),
-                              _ints(inv_freq, inv_freq.shape[:1], "inv_freq", dev, torch.float64), interleaved,
+    pairs = inv_freq.shape
+    if len(pairs) != 1:
+        raise ValueError("inv_freq: one number for each pair expected")
+    _check(lib().realq_rotary(_stream(stream), T, D, 2 * pairs[0], _ints(positions, (T,), "positions", dev, torch.int64),
+                              _ints(inv_freq, pairs, "inv_freq", dev, torch.float64), interleaved,
                               amplitude, transpose, dt, H, *a, n_k, *b))
 
 
