@@ -21,6 +21,7 @@ no arithmetic happens here.
 """
 from __future__ import annotations
 
+import contextlib
 from dataclasses import dataclass
 from typing import Optional, Sequence, Union
 
@@ -28,9 +29,10 @@ import torch
 
 from . import (kv_cache, kv_pages, realq_kv_append, realq_kv_attention, realq_kv_attention_workspace_size,
                realq_pages_compact, realq_pages_fork, realq_pages_release, realq_pages_reserve,
-               realq_pages_workspace_size, realq_rotary, realq_rotary_frequencies, realq_workspace_status, workspace)
+               realq_pages_workspace_size, realq_rotary, realq_rotary_frequencies, realq_workspace_status, workspace, _stream)
 
 Rows = Union[Sequence[int], torch.Tensor]
+_HERE = contextlib.nullcontext()
 
 
 @dataclass
@@ -46,7 +48,16 @@ class Cache8:
     codes with a scale for each scale_block tokens and head, for up to `rows`
     sequences of max_tokens.  inv_freq: rotary frequencies (float64, by default
     base 10000 over the whole head), amplitude and interleaved as for realq_rotary.
-    One stream at a time: its workspaces are reused from call to call."""
+
+    Any stream: a call on a stream other than the current one (`stream`) starts
+    after what the current stream holds and takes its memory from its own stream,
+    and the current stream has to wait for it before it reads its results, as
+    with any operator.  The calls run one after the other, whatever their streams.
+
+    In a graph: `attend` can be captured with the buffers that it is given; `begin`
+    brings host numbers in and cannot.  To replay tokens, `begin` each one outside,
+    with as many new tokens as the captured step, and copy its starts and positions
+    there.  Replays are ordered by their streams, which is the caller's part."""
 
     def __init__(self, layers: int, n_pages: int, rows: int, max_tokens: int, n_kv: int, head_dim: int, page_size: int = 64,
                  scale_block: int = 16, inv_freq: Optional[torch.Tensor] = None, amplitude: float = 1.0, interleaved: bool = False,
@@ -64,7 +75,35 @@ class Cache8:
         self.inv_freq = (realq_rotary_frequencies(head_dim) if inv_freq is None else inv_freq).to(device)
         self.amplitude, self.interleaved = amplitude, interleaved
         self._pages_ws = workspace(realq_pages_workspace_size(n_pages, rows, max_pages), device)
-        self._attend_ws = None
+        # (its size depends on the GPU alone)
+        self._attend_ws = workspace(realq_kv_attention_workspace_size(self.cache, rows, 1, n_kv), device)
+        self._latest = torch.cuda.current_stream(self.used.device)   # the latest call's
+        self._handle = self._latest.cuda_stream
+
+    def _own(self):
+        return (*self.cache.tensors, *self.pages.tensors, self.moved_to, self.inv_freq, self._pages_ws, self._attend_ws)
+
+    def _begin(self, stream, *given: Optional[torch.Tensor]):
+        """A call on `stream` (None: the current one) begins: after the caller's work
+        and the cache's latest call.  The context that it runs in."""
+        handle = _stream(stream)
+        if handle == self._handle and (stream is None or handle == _stream(None)):
+            return _HERE   # (nothing to order; making stream objects would take as long as a small kernel)
+        if stream is None and torch.cuda.is_current_stream_capturing():
+            return _HERE
+        caller = torch.cuda.current_stream(self.used.device)
+        s = caller if stream is None else stream
+        kept = given
+        if handle != self._handle:
+            s.wait_stream(self._latest)
+            self._latest, self._handle = s, handle
+            kept += self._own()
+        if s != caller:
+            s.wait_stream(caller)
+        for t in kept:   # not to be handed on before the call is done with it
+            if isinstance(t, torch.Tensor):
+                t.record_stream(s)
+        return torch.cuda.stream(s)
 
     def _ints(self, rows: Rows) -> torch.Tensor:
         if isinstance(rows, torch.Tensor):
@@ -78,8 +117,9 @@ class Cache8:
         at = [0]
         for n in counts:
             at.append(at[-1] + n)
-        step = Step(self._ints(at), torch.empty(at[-1], dtype=torch.int64, device=self.used.device), max(counts))
-        realq_pages_reserve(self.pages, step.starts, step.positions, self.cache, ws=self._pages_ws, stream=stream)
+        with self._begin(stream):
+            step = Step(self._ints(at), torch.empty(at[-1], dtype=torch.int64, device=self.used.device), max(counts))
+            realq_pages_reserve(self.pages, step.starts, step.positions, self.cache, ws=self._pages_ws)
         return step
 
     def attend(self, step: Step, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
@@ -90,33 +130,34 @@ class Cache8:
         T, H, _ = q.shape
         if T != step.positions.shape[0]:
             raise ValueError(f"q: {step.positions.shape[0]} tokens expected, got {T}")
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        if T == 0:
-            return out
-        realq_rotary(q, step.positions, self.inv_freq, q, k=k, k_out=k, interleaved=self.interleaved, amplitude=self.amplitude,
-                     stream=stream)
-        realq_kv_append(self.cache, layer, k, v, step.starts, step.positions, self.tables, stream=stream)
-        if self._attend_ws is None:   # (its size depends on the GPU alone)
-            self._attend_ws = workspace(realq_kv_attention_workspace_size(self.cache, self.tables.shape[0], T, H), q.device)
-        return realq_kv_attention(q, self.cache, layer, step.starts, self.lengths, self.tables, out, lse=lse, scale=scale,
-                                  window=window, max_new=step.most, ws=self._attend_ws, stream=stream)
+        with self._begin(stream, q, k, v, out, lse, step.starts, step.positions):
+            if out is None:
+                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            if T == 0:
+                return out
+            realq_rotary(q, step.positions, self.inv_freq, q, k=k, k_out=k, interleaved=self.interleaved, amplitude=self.amplitude)
+            realq_kv_append(self.cache, layer, k, v, step.starts, step.positions, self.tables)
+            return realq_kv_attention(q, self.cache, layer, step.starts, self.lengths, self.tables, out, lse=lse, scale=scale,
+                                      window=window, max_new=step.most, ws=self._attend_ws)
 
     def fork(self, src: Rows, dst: Rows, stream=None) -> None:
         """Rows dst[i] go on from rows src[i]'s sequences, all at once (a beam search's reordering)."""
-        realq_pages_fork(self.pages, self._ints(src), self._ints(dst), ws=self._pages_ws, stream=stream)
+        with self._begin(stream, src, dst):
+            realq_pages_fork(self.pages, self._ints(src), self._ints(dst), ws=self._pages_ws)
 
     def release(self, rows: Rows, stream=None) -> None:
         """The rows' sequences leave."""
-        realq_pages_release(self.pages, self._ints(rows), stream=stream)
+        with self._begin(stream, rows):
+            realq_pages_release(self.pages, self._ints(rows))
 
     def compact(self, stream=None) -> torch.Tensor:
         """Pages in use to the front of the pool; each page's new number (-1: free)."""
-        realq_pages_compact(self.pages, self.cache, self.used, self.tables, self.moved_to, ws=self._pages_ws, stream=stream)
+        with self._begin(stream):
+            realq_pages_compact(self.pages, self.cache, self.used, self.tables, self.moved_to, ws=self._pages_ws)
         return self.moved_to
 
     def check(self, stream=None) -> None:
         """Raises RealqError if a step since the last check found too few pages, or a bounded wait gave up (synchronizes)."""
-        for ws in (self._pages_ws, self._attend_ws):
-            if ws is not None:
-                realq_workspace_status(ws, stream=stream)
+        with self._begin(stream):
+            for ws in (self._pages_ws, self._attend_ws):
+                realq_workspace_status(ws)

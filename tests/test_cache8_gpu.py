@@ -108,3 +108,69 @@ def test_a_refused_step_changes_nothing():
     out = through([5, 5], 9)
     cache.check()
     assert bool(torch.isfinite(out).all()) and cache.lengths.tolist() == [25, 15]
+
+
+def two_caches(**kw):
+    from paper_2609_00049_gb300.cache import Cache8
+    return [Cache8(2, 40, 3, 300, 2, 64, page_size=16, **kw) for _ in range(2)]
+
+
+def tokens(T, seed):
+    return [torch.randn(T, n, 64, generator=gen(seed + i), device="cuda").to(torch.bfloat16) for i, n in enumerate((8, 2, 2))]
+
+
+def test_calls_on_other_streams():
+    """Calls handed from stream to stream, their lists freed at once and the memory reused, give what one stream gives."""
+    here, there = two_caches()
+    streams = [torch.cuda.Stream() for _ in range(3)] + [None]
+    plan = [[70, 3, 0], ("fork", [0], [2]), [1, 1, 1], ("compact",), [1, 40, 2], ("release", [1]), [1, 0, 5], ("fork", [2], [1]), [2, 2, 2]]
+    for turn in range(3):
+        at = 0
+        for i, what in enumerate(plan):
+            if isinstance(what, tuple):
+                for c, kw in ((here, {}), (there, dict(stream=streams[(at := at + 1) % 4]))):
+                    getattr(c, what[0])(*what[1:], **kw)
+                torch.full((4096,), 7, dtype=torch.int32, device="cuda")     # (what lists' memory might become)
+                continue
+            steps = [here.begin(what), there.begin(what, stream=streams[(at := at + 1) % 4])]
+            for la in range(2):
+                x = tokens(sum(what), 100 * turn + 10 * i + la)
+                want = here.attend(steps[0], la, *[t.clone() for t in x])
+                s = streams[(at := at + 1) % 4]
+                y = [t.clone() for t in x]
+                got = there.attend(steps[1], la, *y, stream=s)
+                del y
+                torch.full((4096, 64), 7.0, device="cuda")
+                if s is not None:
+                    torch.cuda.current_stream().wait_stream(s)
+                assert torch.equal(got, want), (turn, i, la)
+        for c in (here, there):
+            c.check()
+            c.release([0, 1, 2])
+    assert there.used.sum().item() == 0
+
+
+def test_a_captured_token():
+    """`attend` captured once and replayed for the tokens after it, the first call of its cache among them."""
+    eager, captured = two_caches()
+    for c in (eager, captured):
+        c.begin([20, 7, 1])
+    step = captured.begin([1, 1, 1])
+    eager.begin([1, 1, 1])
+    buf, out = tokens(3, 0), torch.empty(3, 8, 64, device="cuda", dtype=torch.bfloat16)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        captured.attend(step, 1, *buf, out=out)
+    for t in range(5):
+        x = tokens(3, 10 + t)
+        a, b = eager.begin([1, 1, 1]), captured.begin([1, 1, 1])
+        want = eager.attend(a, 1, *[v.clone() for v in x])
+        for to, v in zip(buf, x):
+            to.copy_(v)
+        step.starts.copy_(b.starts)
+        step.positions.copy_(b.positions)
+        g.replay()
+        assert torch.equal(out, want)
+    for a, b in zip(eager.cache.tensors, captured.cache.tensors):
+        assert torch.equal(a, b)
+    captured.check()
