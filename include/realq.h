@@ -382,7 +382,9 @@ realq_status_t realq_checkpoint_weight_grad(realq_stream_t stream, int64_t T, in
  * device and check what they read: a sequence whose entries of `starts` are not
  * in order or lie outside [0, T], a position below zero or beyond the table's
  * row and a page outside the pool take no part, and nothing outside the buffers
- * is touched. */
+ * is touched.  (realq_kv_append and realq_kv_read look tokens up in `starts`:
+ * where it is not in order, sequences beside the faulty ones may be left out
+ * too.)  Lists, tables and cache must not change while a call runs. */
 typedef struct {
     int64_t n_layers, n_pages, n_kv, page_size, head_dim, scale_block;
     uint8_t *k_codes, *v_codes;
@@ -404,7 +406,8 @@ typedef struct {
  *              radians per position (realq_rotary_frequencies).  The angle is
  *              reduced exactly: a position's error does not grow with it.
  *   q, k       T x n_q (n_k) x head_dim of dtype, token t's head h at
- *              t ld + h hs elements; k NULL with n_k = 0.  q_out, k_out
+ *              t ld + h hs elements (heads within a token's row, or tokens
+ *              within a head's); k NULL with n_k = 0.  q_out, k_out
  *              likewise; an output may be its input (with the same strides),
  *              else the two do not overlap.
  * rot_dim even, in [2, head_dim]; head_dim at most 1024; T at most 2^30.  fp32 arithmetic, one
@@ -478,13 +481,17 @@ realq_status_t realq_kv_read(realq_stream_t stream, const realq_kv_cache_t *cach
  *        256-byte aligned, zeroed before its first use; calls leave it ready
  *        for the next, whatever its sizes.  Its first word is a status as that
  *        of realq_int8_product's workspace.  Calls that may run at the same time need a
- *        workspace each.
+ *        workspace each.  After REALQ_ERR_TIMEOUT the outputs are unspecified
+ *        and the workspace is to be zeroed again.
+ * n_seqs at most 2^20, n_heads at most 1024 n_kv, T n_heads / n_kv below 2^30.
+ * The block scales are those of realq_kv_append: not negative, or NaN; values'
+ * scales below 2^-100 count as that.
  * A query that sees no token gets zeros and lse -inf.  Tokens that a query does
  * not see have no influence, whatever the cache holds there.  Rows of q outside
  * every sequence are left as they were in out and lse.  Scores, sums and
  * outputs are held in fp32; with bf16 inputs the weights of the values are
- * rounded to fp16 (2^-12 of each), with fp32 inputs queries and weights are
- * taken as two fp16 parts each.  The order of summation is fixed by the
+ * rounded to fp16 (2^-11 of each, an eighth of the output's own rounding), with
+ * fp32 inputs queries and weights are taken as two fp16 parts each.  The order of summation is fixed by the
  * lengths and sizes (bitwise repeatable).  T = 0 is a no-op.  Asynchronous. */
 size_t realq_kv_attention_workspace_size(const realq_kv_cache_t *cache, int64_t n_seqs, int64_t T, int64_t n_heads);
 realq_status_t realq_kv_attention(realq_stream_t stream, const realq_kv_cache_t *cache, int64_t layer, int64_t n_seqs,
@@ -496,16 +503,19 @@ realq_status_t realq_kv_attention(realq_stream_t stream, const realq_kv_cache_t 
 /* Pages.  Every call is one or two launches on `stream`; nothing is read back.
  * ws: realq_pages_workspace_size(n_pages, n_rows, max_pages) bytes, 256-byte
  * aligned, zeroed before its first use; its first word is a status that
- * realq_workspace_status reads and clears.
+ * realq_workspace_status reads and clears.  Calls that may run at the same time
+ * need a workspace each, and a pool is one call's at a time.
  *
  * realq_pages_reserve: room for starts[s + 1] - starts[s] more tokens in each
- * row s (starts: n_rows + 1 ints): lengths grow, table entries are filled with
+ * row s (starts: n_rows + 1 ints, the first 0): lengths grow, table entries are filled with
  * the lowest-numbered free pages in the order of the rows, and positions (an
  * int64 for each new token, starts[n_rows] of them, at most T) receives the new
  * tokens' positions.  Where a row's last page is partly filled and held by
  * others too, the row first gets a copy of it, in every layer of cache (the
  * last row of the call may keep the page where all its holders are in the
- * call): what realq_kv_append writes afterwards is the row's own.  All or
+ * call): what realq_kv_append writes afterwards is the row's own.  A sequence is
+ * put back to fewer tokens by lowering its length: pages behind its end stay
+ * with the row until they are replaced here, or the row is released.  All or
  * nothing: with too few free pages, entries or positions, or starts out of
  * order, nothing changes, all T positions become -1 (so that appending does
  * nothing) and the status becomes REALQ_ERR_NO_PAGES.

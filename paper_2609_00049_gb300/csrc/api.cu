@@ -1031,9 +1031,11 @@ static realq_status_t check_heads(const char *who, const char *name, int64_t T, 
     if (heads == 0 || T == 0) return REALQ_OK;
     if (!p) return fail(REALQ_ERR_INVALID_ARG, "%s: NULL %s", who, name);
     if (reinterpret_cast<uintptr_t>(p) % (dt == REALQ_BF16 ? 2 : 4)) return fail(REALQ_ERR_INVALID_ARG, "%s: %s not aligned to its type", who, name);
-    if ((heads > 1 && hs < dim) || (T > 1 && ld < (heads - 1) * hs + dim) || ld < 0 || hs < 0)
-        return fail(REALQ_ERR_INVALID_ARG, "%s: %s's heads or tokens overlap", who, name);
     if (hs > (1ll << 40) || ld > (1ll << 40)) return fail(REALQ_ERR_UNSUPPORTED, "%s: %s's strides pass 2^40", who, name);
+    // heads within a token's row, or tokens within a head's
+    const bool apart = (heads == 1 || hs >= dim) && (T == 1 || ld >= dim) &&
+                       (heads == 1 || T == 1 || ld >= (heads - 1) * hs + dim || (hs - dim) / (T - 1) >= ld);
+    if (!apart || ld < 0 || hs < 0) return fail(REALQ_ERR_INVALID_ARG, "%s: %s's heads or tokens overlap", who, name);
     return REALQ_OK;
 }
 
@@ -1140,6 +1142,7 @@ realq_status_t realq_kv_attention(realq_stream_t stream, const realq_kv_cache_t 
     if (n_heads / a.c.n_kv > 1024) return fail(REALQ_ERR_UNSUPPORTED, "kv_attention: at most 1024 heads to a key/value head");
     if (!std::isfinite(scale)) return fail(REALQ_ERR_INVALID_ARG, "kv_attention: scale must be finite");
     if (window < 0 || (window > 0 && !causal)) return fail(REALQ_ERR_INVALID_ARG, "kv_attention: window >= 0, and only with causal != 0");
+    if (n_seqs > (1ll << 20)) return fail(REALQ_ERR_UNSUPPORTED, "kv_attention: n_seqs at most 2^20");   // (a bounded wait outlasts a walk over as many)
     if (max_new < 1 && T > 0) return fail(REALQ_ERR_INVALID_ARG, "kv_attention: max_new >= 1 required");
     REALQ_TRY(check_heads(who, "q", T, n_heads, a.c.head_dim, q, q_ld, q_hs, dtype));
     if (T == 0 || n_seqs == 0) return REALQ_OK;

@@ -117,11 +117,12 @@ template <int ROWS, int TILE, bool LONG> __device__ void fill_window(const KvAtt
     if constexpr (LONG) {
         __syncthreads();
         for (int i = warp; i < SEQS; i += blockDim.x / 32) {
-            int n = 0;
+            int64_t n = 0;   // (a prompt of millions of tokens has more tiles than 32 bits count)
             if (first + i < a.n_seqs) {
                 const Seq q(a, first + i);
                 for (int r = lane * ROWS; r < q.m * a.group; r += 32 * ROWS) n += row_tiles<ROWS, TILE>(a, q, r);
-                n = __reduce_add_sync(0xFFFFFFFFu, n);
+#pragma unroll
+                for (int d = 16; d; d /= 2) n += __shfl_xor_sync(0xFFFFFFFFu, n, d);
             }
             if (lane == 0) w.sum[i] = n;
         }
@@ -231,7 +232,7 @@ __device__ __forceinline__ void locate(const KvAttnArgs &a, Window &win, int64_t
         for (;; u.r0 += 32 * ROWS) {   // 32 row tiles at a time
             const int r = u.r0 + lane * ROWS;
             const int n = r < rows_all ? row_tiles<ROWS, TILE>(a, q, r) : 0;
-            int x = n;
+            int x = n;   // (32 times at most 2^25)
 #pragma unroll
             for (int d = 1; d < 32; d *= 2) {
                 const int y = __shfl_up_sync(0xFFFFFFFFu, x, d);

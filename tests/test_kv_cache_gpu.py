@@ -445,3 +445,71 @@ def test_attention_right_behind_a_product():
         rq.realq_kv_attention(q.view(T, H, D), h, 0, starts, c.lengths, c.tables, out, max_new=1, ws=aws)
         outs.append(out.clone())
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_tokens_within_a_heads_row(dtype):
+    """Heads first, tokens within them (a transposed view): the same bits as from tokens x heads, in every operator."""
+    news, olds, H, kv, D = [40, 1], [30, 90], 6, 2, 64
+    c = Cache(16, [o + n for o, n in zip(olds, news)], kv=kv, D=D, page=32, block=16, poison=False)
+    T, st = sum(news), starts_of(news)
+    pos = torch.cat([torch.arange(o, o + n) for o, n in zip(olds, news)]).cuda()
+    f = rq.realq_rotary_frequencies(D).cuda()
+    first = [torch.randn(n, T, D, generator=gen(n), device="cuda").to(dtype) for n in (H, kv, kv + 1)]
+    q, k, v = (x.transpose(0, 1) for x in first)
+    v = v[:, :kv]
+    h = rq.kv_cache(**c.buffers())
+    before = {n: t.clone() for n, t in c.buffers().items()}
+    ws = rq.workspace(rq.realq_kv_attention_workspace_size(h, 2, T, H))
+    got = []
+    for q1, k1, v1 in ((q, k, v), (q.contiguous(), k.contiguous(), v.contiguous())):
+        for n, t in before.items():
+            getattr(c, n).copy_(t)
+        qo, ko = torch.empty_like(q1), torch.empty_like(k1)     # (of the same strides)
+        assert qo.stride() == q1.stride()
+        rq.realq_rotary(q1, pos, f, qo, k=k1, k_out=ko)
+        rq.realq_kv_append(h, 0, ko, v1, st, pos, c.tables)
+        out, one = torch.empty(T, H, D, device="cuda", dtype=dtype), torch.empty(T, H, D, device="cuda", dtype=dtype)
+        rq.realq_kv_attention(qo, h, 0, st, c.lengths, c.tables, out, ws=ws)
+        rq.realq_kv_attention(qo, h, 0, st, c.lengths, c.tables, one, max_new=1, ws=ws)
+        got.append([qo.clone(), ko.clone(), out, one] + [t.clone() for t in c.buffers().values()])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
+def test_pages_beyond_32_bits():
+    """A pool of more than 2^32 bytes of codes of each kind: into its last pages, out of them, over them."""
+    lens, kv, D = [300, 70], 8, 256
+    c = Cache(15, lens, kv=kv, D=D, page=64, block=16, poison=False)
+    small, rows = {n: t.clone() for n, t in c.buffers().items()}, c.rows
+    n = 33000
+    at = [n - 1 - 3 * i for i in range(c.n_pages)]
+    assert min(at) * kv * 64 * D > 2 ** 32
+    for name, t in small.items():
+        big = torch.full((1, n, *t.shape[2:]), 128 if t.dtype == torch.uint8 else 0, dtype=t.dtype, device="cuda")
+        big[:, at] = t
+        setattr(c, name, big)
+    c.rows = [[at[p] if p >= 0 else p for p in r] for r in rows]
+    c.tables = i32(c.rows)
+    attended(c, [200, 1], 16, BF16, 1)
+    attended(c, [1, 1], 16, F32, 2, max_new=1)
+    h = rq.kv_cache(**c.buffers())
+    x = [torch.randn(40, kv, D, generator=gen(i), device="cuda").to(BF16) for i in (3, 4)]
+    pos = torch.arange(100, 140, device="cuda")
+    rq.realq_kv_append(h, 0, *x, starts_of([40, 0]), pos, c.tables)
+    for w, t in zip("kv", x):
+        append(small[w + "_codes"][0], small[w + "_scale"][0], t, 100, rows[0], 64, 16)
+    for name, t in small.items():
+        assert torch.equal(getattr(c, name)[:, at], t), name
+        others = torch.ones(n, dtype=torch.bool, device="cuda")
+        others[at] = False
+        assert bool((getattr(c, name)[0, -40:][others[-40:]] == (128 if t.dtype == torch.uint8 else 0)).all()), name
+    out = [torch.empty(40, kv, D, device="cuda") for _ in range(2)]
+    rq.realq_kv_read(h, 0, starts_of([40, 0]), pos, c.tables, *out)
+    for w, o in zip("kv", out):
+        want = c.values(w, 0, 0)[100:140]
+        assert bool(((o.double() - want).abs() <= U(F32) * want.abs()).all())
+    rq.realq_pages_copy(h, i32(at), i32(list(range(len(at)))))
+    rq.realq_pages_copy(h, i32(list(range(len(at)))), i32([p - 1 for p in at]))
+    for name, t in small.items():
+        assert torch.equal(getattr(c, name)[:, :len(at)], t) and torch.equal(getattr(c, name)[:, [p - 1 for p in at]], t), name

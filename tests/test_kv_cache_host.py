@@ -177,3 +177,14 @@ def test_binding_refusals(L):
     with pytest.raises(rq.RealqError):
         rq.realq_rotary_frequencies(7)
     assert rq.realq_status_string(rq.REALQ_ERR_NO_PAGES) == "too few free pages or table entries"
+
+
+def test_layouts_and_limits(L):
+    """Heads within a token's row or tokens within a head's; neither where they meet."""
+    T, H, D = 5, 8, 64
+    call = lambda ld, hs, S=3, ws=None: L.realq_kv_attention(   # noqa: E731
+        None, cache(), 0, S, T, H, FAKE, ld, hs, 1, FAKE, FAKE, FAKE, 5, 0.1, 1, 0, 5, FAKE, None, ws, 0)
+    assert call(D, T * D) == WORKSPACE and call(H * D, D) == WORKSPACE       # (past the layout, the missing workspace)
+    assert call(2 * D, 2 * T * D) == WORKSPACE and call(D, T * D - 1) == INVALID and call(D - 1, T * D) == INVALID
+    assert call(H * D - 1, D) == INVALID and call(2 * D, T * D) == INVALID and call(0, T * D) == INVALID
+    assert call(H * D, D, S=(1 << 20) + 1) == UNSUPPORTED
