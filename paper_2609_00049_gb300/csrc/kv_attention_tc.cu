@@ -81,6 +81,11 @@ __device__ __forceinline__ void tmem_st_x8(uint32_t taddr, const uint32_t (&r)[8
                  "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                  : "memory");
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
 // two fp32 values in one register pair
 __device__ __forceinline__ uint64_t two(float a, float b) {
     uint64_t r;
@@ -423,8 +428,9 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                         float x[4];
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
-                            x[j] = fmaxf(fmaxf(__uint_as_float(v[j]), __uint_as_float(v[4 + j])), fmaxf(__uint_as_float(v[8 + j]), __uint_as_float(v[12 + j])));
-                        top = fmaxf(top, fmaf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), b.x * factor, b.y));
+                            x[j] = max3(__uint_as_float(v[3 * j]), __uint_as_float(v[3 * j + 1]), __uint_as_float(v[3 * j + 2]));
+                        const float y = max3(x[0], __uint_as_float(v[12]), __uint_as_float(v[13])), z = max3(x[1], __uint_as_float(v[14]), __uint_as_float(v[15]));
+                        top = fmaxf(top, fmaf(fmaxf(max3(y, x[2], x[3]), z), b.x * factor, b.y));
                     } else {
 #pragma unroll
                         for (int j = 0; j < 16; j += 4) {
@@ -643,22 +649,26 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
             if (!last_one[i]) continue;
             __threadfence();
             float mm = NEG, ll = 0.f;
-            for (int c = first_cta; c <= last_cta; ++c) mm = fmaxf(mm, __ldcg(slot_of(c, c == first_cta) + 128 * DP + row));
-            for (int c = first_cta; c <= last_cta; ++c) {
-                const float *s = slot_of(c, c == first_cta) + 128 * DP + row;
+            const int parts = last_cta - first_cta + 1;
+#pragma unroll 4
+            for (int c = 0; c < parts; ++c) mm = fmaxf(mm, __ldcg(slot_of(first_cta + c, c == 0) + 128 * DP + row));
+#pragma unroll 4
+            for (int c = 0; c < parts; ++c) {
+                const float *s = slot_of(first_cta + c, c == 0) + 128 * DP + row;
                 const float mc = __ldcg(s), lc = __ldcg(s + 128);
                 ll += mc == NEG ? lc * 0.f : lc * exp2_fast(mc - mm);   // (a NaN stays one)
             }
             const float all_inv = ll == 0.f ? 0.f : 1.f / ll;
+#pragma unroll 1
             for (int d = 8 * half; d < D; d += 16) {
                 float y[8] = {};
-                for (int c = first_cta; c <= last_cta; ++c) {
-                    const float *s = slot_of(c, c == first_cta);
-                    const float mc = __ldcg(s + 128 * DP + row), lc = __ldcg(s + 128 * DP + 128 + row);
-                    if (lc == 0.f) continue;
-                    const float f = mc == NEG ? 0.f : exp2_fast(mc - mm);
+#pragma unroll 4
+                for (int c = 0; c < parts; ++c) {   // (where a share saw nothing its outputs are 0)
+                    const float *s = slot_of(first_cta + c, c == 0);
+                    const float mc = __ldcg(s + 128 * DP + row);
                     const float4 *p4 = reinterpret_cast<const float4 *>(s) + d / 4 * 128 + row;
                     const float4 v0 = __ldcg(p4), v1 = __ldcg(p4 + 128);
+                    const float f = mc == NEG ? 0.f : exp2_fast(mc - mm);
                     y[0] += v0.x * f, y[1] += v0.y * f, y[2] += v0.z * f, y[3] += v0.w * f;
                     y[4] += v1.x * f, y[5] += v1.y * f, y[6] += v1.z * f, y[7] += v1.w * f;
                 }
