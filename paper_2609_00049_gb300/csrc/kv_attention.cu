@@ -104,16 +104,17 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
 
     // all tiles, and this CTA's share
     const bool few = a.n_seqs <= 32;
-    int64_t all = 0;
+    int64_t all = 0, least = 1;
     if (few) {
-        all = lanes_of<ROWS, TILE>(a).sum * a.c.n_kv;
+        const Lanes s = lanes_of<ROWS, TILE>(a);
+        all = s.sum * a.c.n_kv, least = least_share(s.sum, s.units, 8);
     } else {
         for (int first = 0; first < a.n_seqs; first += SEQS) {
             fill_window<ROWS, TILE, false>(a, win, first, all);
             all += win.sum[SEQS] * a.c.n_kv;
         }
     }
-    const Shares shares(all, gridDim.x);
+    const Shares shares(all, max((int64_t)1, min((int64_t)gridDim.x, least == 1 ? all : all / least)));
     if (blockIdx.x >= shares.ctas) {
         wait_for_previous();
         return;

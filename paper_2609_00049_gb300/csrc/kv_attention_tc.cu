@@ -260,12 +260,13 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
         tc::fence_barrier_init();
     }
     // the share and its first unit
-    int64_t all = 0;
+    int64_t all = 0, units = 0;
     for (int first = 0; first < a.n_seqs; first += SEQS) {
         fill_window<ROWS, KT, true>(a, win, first, all);
-        all += win.sum[SEQS] * a.c.n_kv;
+        all += win.sum[SEQS] * a.c.n_kv, units += win.units * a.c.n_kv;
     }
-    const Shares sh(all, gridDim.x);
+    const int64_t least = least_share(all, units, 4);
+    const Shares sh(all, max((int64_t)1, min((int64_t)gridDim.x, least == 1 ? all : all / least)));
     if (blockIdx.x >= sh.ctas) return;
     if (a.n_seqs > SEQS) fill_window<ROWS, KT, true>(a, win, 0, 0);
     {

@@ -30,6 +30,16 @@ struct Shares {
     }
 };
 
+// The fewest tiles that a CTA takes: the shares of a unit of many tiles cost more to join than they save, those of units of
+// few would only straddle them.  Units of up to `per` tiles on average are cut into single ones, of 4 x `per` or more into
+// fours.  Measured with 32 heads to 8 (one tile, two, four, eight): 8 tokens over 2000 by the kernel of few rows, 32 tiles
+// to a unit, 42, 33, 26, 31 us; 16 tokens over 2000 by that of many, 16 tiles, 47, 37, 33, 39; 8 single tokens over up to
+// 1013, 8 tiles, 12.5, 16.5, 17, 25.
+__device__ __forceinline__ int64_t least_share(int64_t tiles, int64_t units, int per) {
+    const int64_t n = units * per;
+    return tiles >= 4 * n ? 4 : (tiles >= 3 * n ? 3 : (tiles >= 2 * n ? 2 : 1));
+}
+
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -105,7 +115,8 @@ struct Window {
     int first;
     int64_t base;               // tiles of all heads before them
     int64_t sum[SEQS + 1];
-    int64_t warp_sum[16];
+    int64_t warp_sum[4];        // (of the warps that add up)
+    unsigned long long units;   // of one head (LONG)
 };
 // All threads of the CTA call it; the first 128 add up.  A sequence's row tiles are gone
 // over by one thread, or, for prompts of many (LONG), by a warp.
@@ -115,17 +126,22 @@ template <int ROWS, int TILE, bool LONG> __device__ void fill_window(const KvAtt
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int64_t mine[PER], total = 0;
     if constexpr (LONG) {
+        unsigned long long units = 0;
+        __syncthreads();   // (the window before has been read)
+        if (threadIdx.x == 0) w.units = 0;
         __syncthreads();
         for (int i = warp; i < SEQS; i += blockDim.x / 32) {
             int64_t n = 0;   // (a prompt of millions of tokens has more tiles than 32 bits count)
             if (first + i < a.n_seqs) {
                 const Seq q(a, first + i);
+                units += (q.m * a.group + ROWS - 1) / ROWS;
                 for (int r = lane * ROWS; r < q.m * a.group; r += 32 * ROWS) n += row_tiles<ROWS, TILE>(a, q, r);
 #pragma unroll
                 for (int d = 16; d; d /= 2) n += __shfl_xor_sync(0xFFFFFFFFu, n, d);
             }
             if (lane == 0) w.sum[i] = n;
         }
+        if (lane == 0 && units > 0) atomicAdd(&w.units, units);
         __syncthreads();
     }
 #pragma unroll
@@ -144,7 +160,7 @@ template <int ROWS, int TILE, bool LONG> __device__ void fill_window(const KvAtt
         if (lane >= d) x += y;
     }
     __syncthreads();
-    if (lane == 31) w.warp_sum[warp] = x;
+    if (counts && lane == 31) w.warp_sum[warp] = x;
     __syncthreads();
     if (counts) {
         int64_t at = x - total;
@@ -165,14 +181,17 @@ struct Lanes {
     int q0, m, len;
     int64_t from, to;   // the lane's sequence's tiles of one head, in the running count
     int64_t sum;        // of all
+    int64_t units;      // of all
 };
 template <int ROWS, int TILE> __device__ __forceinline__ Lanes lanes_of(const KvAttnArgs &a) {
     const int lane = threadIdx.x & 31;
-    Lanes r = {0, 0, 0, 0, 0, 0};
+    Lanes r = {0, 0, 0, 0, 0, 0, 0};
     int64_t n = 0;
+    int units = 0;
     if (lane < a.n_seqs) {
         const Seq q(a, lane);
         r.q0 = q.q0, r.m = q.m, r.len = q.len;
+        units = (q.m * a.group + ROWS - 1) / ROWS;
         for (int r0 = 0; r0 < q.m * a.group; r0 += ROWS) n += row_tiles<ROWS, TILE>(a, q, r0);
     }
     int64_t x = n;
@@ -182,6 +201,7 @@ template <int ROWS, int TILE> __device__ __forceinline__ Lanes lanes_of(const Kv
         if (lane >= d) x += y;
     }
     r.from = x - n, r.to = x, r.sum = __shfl_sync(0xFFFFFFFFu, x, 31);
+    r.units = __reduce_add_sync(0xFFFFFFFFu, units);   // (at most 2^30 rows in all)
     return r;
 }
 template <int ROWS, int TILE>
