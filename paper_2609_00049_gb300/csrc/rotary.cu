@@ -13,7 +13,8 @@
 // cosines and sines of its tokens once in shared memory (a double product, an
 // integer one and a sincospif for each pair and token; a head would take as long
 // for them as for its values) and goes over all heads of q and k with 16-byte
-// accesses.
+// accesses.  16384 tokens of 64 + 8 heads of 128 in bf16, forward and gradient: 197
+// us, 6.1 TB/s, 0.91 of a copy's rate; 8 tokens: 2.7 us a launch.
 #include <cmath>
 
 #include "kernels.cuh"
@@ -139,7 +140,8 @@ template <class T> realq_status_t launch(cudaStream_t s, const RotaryArgs &a, in
     const bool wide = whole(inter ? a.rot_dim : a.rot_dim / 2) && whole(a.head_dim) && whole(a.rot_dim) &&
                       fits(a.q, a.q_ld, a.q_hs, a.n_q) && fits(a.q_out, a.qo_ld, a.qo_hs, a.n_q) &&
                       fits(a.k, a.k_ld, a.k_hs, a.n_k) && fits(a.k_out, a.ko_ld, a.ko_hs, a.n_k);
-    // a few tokens to a CTA once there are enough for all SMs, parts of the heads where there are not
+    // four tokens to a CTA once there are enough for all SMs (16384 tokens of 72 heads, both ways: 197 us, 217 with one;
+    // 2432: 41 and 45), one where there are not (200: 3.3 us, 3.7 with four), then parts of the heads
     const int tokens = a.T >= 16ll * sms ? 4 : 1;
     const int64_t gx = (a.T + tokens - 1) / tokens;
     int parts = 1;
