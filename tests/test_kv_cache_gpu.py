@@ -513,3 +513,22 @@ def test_pages_beyond_32_bits():
     rq.realq_pages_copy(h, i32(list(range(len(at)))), i32([p - 1 for p in at]))
     for name, t in small.items():
         assert torch.equal(getattr(c, name)[:, :len(at)], t) and torch.equal(getattr(c, name)[:, [p - 1 for p in at]], t), name
+
+
+def test_attention_of_many_sequences_with_prompts_among_them():
+    """More sequences than a CTA holds the sums of at a time; prompts, single tokens and rows that wait, in both kernels."""
+    r = random.Random(5)
+    news = [r.choice([0, 0, 1, 1, 2, 9, 20, 70]) for _ in range(1100)]
+    news[510:515], news[1023:1026] = [70, 0, 20, 70, 1], [20, 70, 70]     # (around the sums' ends)
+    lens = [n + r.randint(0, 150) for n in news]
+    c = Cache(17, lens, kv=1, D=32, page=16, block=16, poison=False)
+    attended(c, news, 4, BF16, 1)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("news,lens", [([64], [6000]), ([12, 3], [9000, 2500]), ([8], [2000]), ([2], [3000]), ([300, 9, 1], [700, 3000, 4000])])
+def test_attention_units_of_many_tiles(news, lens, dtype):
+    """One or two sequences, whose tiles are shared out several to a CTA and joined."""
+    c = Cache(18, lens, kv=2, D=128, page=64, block=16)
+    attended(c, news, 8, dtype, 2)
+    attended(c, news, 8, dtype, 3, window=1500, max_new=max(news))
