@@ -21,7 +21,9 @@
 //   running maximum of s + log2 vscale, so that the largest weight is about 2^14
 //   and what fp16 cannot hold is 2^-38 of it.  With bf16 inputs p is rounded to
 //   fp16 (2^-11 relative, an eighth of the output's own rounding); with fp32 ones it
-//   is two fp16 parts.  The softmax's sum adds 2^(s - M) in fp32.
+//   is two fp16 parts.  The softmax's sum adds 2^(s - M - 14) in fp32.  log2 vscale
+//   counts as -96 at least in the maximum, so that 2^31 tokens of zero values, 2^96
+//   each, add up to 2^127.
 // - A warp keeps its own maximum, sum and output; the four are joined at the end
 //   of a CTA's share, and shares of one row tile by the CTA that ends last.
 //
@@ -44,7 +46,7 @@ namespace realq {
 namespace {
 
 constexpr int WARPS = 4, THREADS = 32 * WARPS, GROUP = 16, TILE = GROUP * WARPS;
-constexpr float NEG = -INFINITY;
+constexpr float NEG = -INFINITY, LIFT = 14.f, DOWN = 6.103515625e-05f;   // weights are 2^LIFT times what the sum adds; 2^-LIFT
 
 __device__ __forceinline__ uint32_t transposed8x8(uint32_t x) {
     uint32_t y;
@@ -303,7 +305,7 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
                 }
             }
             float ksc[2] = {scales[g], scales[g + 8]}, vsc[2] = {scales[16 + g], scales[16 + g + 8]};
-            const float lv0 = fmaxf(log2_fast(vsc[0]), -100.f), lv1 = fmaxf(log2_fast(vsc[1]), -100.f);
+            const float lv0 = fmaxf(log2_fast(vsc[0]), -96.f), lv1 = fmaxf(log2_fast(vsc[1]), -96.f);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 s[nt][0] *= ksc[0] * rs[nt][0], s[nt][1] *= ksc[0] * rs[nt][1];
@@ -355,8 +357,8 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float m = mx[nt][e & 1];
-                    const float x = exp2_fast(s[nt][e] - (m == NEG ? 0.f : m - 14.f));
-                    sum[nt][e & 1] += x;
+                    const float x = exp2_fast(s[nt][e] - (m == NEG ? 0.f : m - LIFT));
+                    sum[nt][e & 1] = fmaf(x, DOWN, sum[nt][e & 1]);
                     p[e] = x * vsc[e >> 1];
                     if (masked && s[nt][e] == NEG) p[e] = 0.f;   // whatever the scale of a token that is not seen
                 }
@@ -434,7 +436,7 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
             const int rr = u.r0 + r, qi = rr / a.group;
             const int64_t row = (int64_t)(u.q0 + qi) * a.n_heads + u.head * a.group + rr % a.group;
             const float m = row_m[r], l = row_l[r];
-            const float inv = l == 0.f ? 0.f : 1.f / l;   // (a sum of nothing: the row sees no token)
+            const float inv = l == 0.f ? 0.f : 1.f / l * DOWN;   // (a sum of nothing: the row sees no token)
             const float y[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
             T *o = (T *)a.out + row * D + d;
 #pragma unroll
@@ -444,7 +446,7 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
                 else
                     o[e] = __float2bfloat16_rn(y[e]);
             }
-            if (d == 0 && a.lse != nullptr) a.lse[row] = l == 0.f ? NEG : (m - 14.f + log2f(l)) * 0.6931471805599453f;
+            if (d == 0 && a.lse != nullptr) a.lse[row] = l == 0.f ? NEG : (m + log2f(l)) * 0.6931471805599453f;
         };
         // (a share that saw nothing has maximum -inf, sum 0 and outputs 0; one that saw a NaN a sum of NaN)
         if (threadIdx.x < ROWS) {

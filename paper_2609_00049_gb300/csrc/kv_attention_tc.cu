@@ -17,10 +17,11 @@
 // half a conversion: the block scales enter by the 16 tokens that share them.  With ks, vs a
 // chunk's scales, lv = log2 vs and r the row's own scale (a power of two from
 // scaling q into fp16's range, the softmax scale, log2 e),
-//   p = 2^(S ks r + lv - M + 6),   sum += (sum of p in the chunk) / vs,
+//   p = 2^(S ks r + lv - M + 6),   sum += (sum of p in the chunk) 2^-6 / vs,
 // so p already holds V's scale and O needs no other.  M is at least the running maximum less
 // 8: it moves only when some row's maximum grew by more than that, and only then O is
-// read, scaled and written back (the largest p stays below 2^14).  Scale blocks of fewer than 16
+// read, scaled and written back (the largest p stays below 2^14).  lv is at least -88, so that
+// 2^31 tokens of zero values, 2^(88 + 8) each, add up to 2^127 at most.  Scale blocks of fewer than 16
 // tokens take one scale per token in the same formulas.  bf16 queries are exact in
 // fp16 after scaling (down to 2^-29 of a row's largest value); fp32 queries and their p are two fp16
 // parts each, which doubles the products.
@@ -52,7 +53,7 @@ constexpr int SOFT_WARPS = 16, CONV_WARPS = 4;   // (softmax: eight to a row til
 constexpr int MMA_WARP = SOFT_WARPS + 2 * CONV_WARPS, LOAD_WARP = MMA_WARP + 1, THREADS = 32 * (MMA_WARP + 4);   // (loaders of K and of V; one is idle)
 constexpr int UNIT = 32;                 // tokens whose codes come and are converted together
 constexpr int SLOTS = 4;                 // of block scales
-constexpr float NEG = -INFINITY, LIFT = 6.f, SLACK = 8.f;
+constexpr float NEG = -INFINITY, LIFT = 6.f, DOWN = 0.015625f, SLACK = 8.f;   // (DOWN: 2^-LIFT)
 
 template <int DP, bool F32> struct Shape {
     static constexpr int NM = DP == 256 ? 1 : 2;                                // row tiles
@@ -606,7 +607,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                 }
             };
             const auto put_lse = [&](float mm, float ll) {
-                if (a.lse != nullptr) a.lse[out_row] = ll == 0.f ? NEG : (mm - LIFT + log2f(ll)) * 0.6931471805599453f;
+                if (a.lse != nullptr) a.lse[out_row] = ll == 0.f ? NEG : (mm + log2f(ll)) * 0.6931471805599453f;
             };
             const auto slot_of = [&](int c, bool begins) { return a.part + ((int64_t)(2 * c + (begins ? 1 : 0)) * NM + i) * Sh::PART; };
             float *mine = slot_of(blockIdx.x, begins);
@@ -619,7 +620,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
             bad += swap[half ^ 1][i][row];
             ok = pair(abort_flag) && ok;   // (the next scores' maximum goes there)
             if (!ok) break;
-            const float inv = 1.f / l;
+            const float inv = DOWN / l;
 #pragma unroll 1
             for (int c = 16 * half; c < D; c += 32) {
                 uint32_t v[16];
@@ -668,7 +669,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                 const float mc = __ldcg(s), lc = __ldcg(s + 128);
                 ll += mc == NEG ? lc * 0.f : lc * exp2_fast(mc - mm);   // (a NaN stays one)
             }
-            const float all_inv = ll == 0.f ? 0.f : 1.f / ll;
+            const float all_inv = ll == 0.f ? 0.f : DOWN / ll;
 #pragma unroll 1
             for (int d = 8 * half; d < D; d += 16) {
                 float y[8] = {};
@@ -813,11 +814,11 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                     for (int n0 = 0; n0 < entries; n0 += 32) {
                         const int n = n0 + lane;
                         if (n0 > 0 || fine) scales_of(t, page, n);
-                        // tokens without a page weigh nothing; a scale below 2^-100 counts as that; a NaN's part in the sum
+                        // tokens without a page weigh nothing; a scale below 2^-88 counts as that; a NaN's part in the sum
                         // stays (the scores are not concerned)
                         const bool nan = there_s && vs != vs;
                         const float k = there_s ? ks : 0.f, nv = nan ? vs : 0.f;
-                        const float lv = !there_s ? NEG : (nan ? 0.f : fmaxf(log2_fast(vs), -100.f)), iv = !there_s ? 0.f : exp2_fast(-lv);
+                        const float lv = !there_s ? NEG : (nan ? 0.f : fmaxf(log2_fast(vs), -88.f)), iv = !there_s ? 0.f : exp2_fast(-lv) * DOWN;
                         if (n < entries) {
                             if (fine)
                                 sc[n] = k, sc[KT + n] = lv, sc[2 * KT + n] = nan ? -iv : iv;

@@ -1,0 +1,115 @@
+"""The 8-bit key/value cache's operators at the edges of what their arguments allow,
+against the definitions in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import paper_2609_00049_gb300 as rq
+from kv_reference import gen, i32, starts_of
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def U(t):
+    return torch.finfo(t).eps / 2
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    from paper_2609_00049_gb300 import build as b
+    b.build()
+    rq.lib()
+
+
+def run(q, h, starts, lengths, tables, max_new=None, **kw):
+    """Attention into buffers that hold 9 before: outputs and log sums."""
+    T, H = q.shape[:2]
+    out, lse = torch.full_like(q, 9.0), torch.full((T, H), 9.0, device="cuda")
+    ws = rq.workspace(rq.realq_kv_attention_workspace_size(h, len(lengths), T, H))
+    rq.realq_kv_attention(q, h, 0, starts, lengths, tables, out, lse, max_new=max_new, ws=ws, **kw)
+    rq.realq_workspace_status(ws)
+    return out, lse
+
+
+def one_page(values, D, kv=1, page=256, block=256):
+    """A cache of the given pages: each (k code, k scale, v code, v scale), the same for all tokens and heads."""
+    n = len(values)
+    buf = [torch.empty(1, n, kv, page, D, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    sc = [torch.empty(1, n, kv, page // block, device="cuda") for _ in range(2)]
+    for i, (kc, ks, vc, vs) in enumerate(values):
+        buf[0][:, i], sc[0][:, i], buf[1][:, i], sc[1][:, i] = kc, ks, vc, vs
+    return rq.kv_cache(buf[0], buf[1], sc[0], sc[1])
+
+
+# ------------------------------------------- long contexts of zero values ---
+# Scale 0 and codes 128 are what appending zeros leaves.  The tables name one page again and again.
+# The softmax's sum of n equal weights: fp32 additions, one for every 16 tokens of a share and every joined share.
+def sum_error(n):
+    return (n / 16 + 160) * 2.0 ** -23
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("m,n", [(1, 20000), (1, 3000000), (40, 20000), (40, 5000000)])
+def test_log_sums_over_zero_values(m, n, dtype):
+    """All scores equal, all values zero: the log of the number of tokens seen, and zeros."""
+    h = one_page([(128, 1.0, 128, 0.0)], 16)
+    table = torch.zeros(1, -(-n // 256), dtype=torch.int32, device="cuda")
+    q = torch.randn(m, 2, 16, generator=gen(1), device="cuda").to(dtype)
+    out, lse = run(q, h, starts_of([m]), i32([n]), table)
+    want = torch.log(torch.arange(n - m + 1, n + 1, dtype=torch.float64, device="cuda"))[:, None]
+    assert bool((out == 0).all())
+    assert bool(((lse.double() - want).abs() <= sum_error(n) + 2.0 ** -21 + 4 * U(F32) * want).all()), float(lse.max())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("m", [1, 40])
+def test_log_sums_where_the_maximum_lags(m, dtype):
+    """A first page whose scores are a little below the others', so that a running maximum that moves rarely stays behind
+    by as much; a head to a CTA, so that whole contexts are summed by one."""
+    kv, n, low = 160, 40000, 5.4                         # (5.4 < 8 ln 2)
+    ks = torch.tensor(low / 16, dtype=F32).item()
+    h = one_page([(128, 1.0, 128, 0.0), (127, ks, 128, 0.0)], 16, kv)
+    table = torch.zeros(1, -(-n // 256), dtype=torch.int32, device="cuda")
+    table[0, 0] = 1
+    q = torch.ones(m, kv, 16, device="cuda", dtype=dtype)
+    out, lse = run(q, h, starts_of([m]), i32([n]), table, scale=1.0)
+    seen = torch.arange(n - m + 1, n + 1, dtype=torch.float64, device="cuda")[:, None]
+    want = torch.log(256 * math.exp(-16 * ks) + seen - 256)
+    assert bool((out == 0).all())
+    # (scores within 2^-20 of themselves)
+    assert bool(((lse.double() - want).abs() <= sum_error(n) + 2.0 ** -19 * low + 2.0 ** -21 + 4 * U(F32) * want).all()), float(lse.max())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("m", [1, 12])
+def test_zero_values_before_others(m, dtype):
+    """Many sequences whose values are zero but for the last page's: whole shares see nothing but zeros, and the output
+    is the last page's all the same."""
+    S, kv, G, n = 64, 8, 4, 256 * 157
+    h = one_page([(128, 1.0, 128, 0.0), (128, 1.0, 128, 1.0)], 16, kv)
+    kc, vc = (torch.randint(1, 256, (kv, 256, 16), generator=gen(i), device="cuda").to(torch.uint8) for i in (1, 2))
+    h.tensors[0][0, 1], h.tensors[1][0, 1] = kc, vc
+    h.tensors[2][0, 1] = 0.01
+    table = torch.zeros(S, n // 256, dtype=torch.int32, device="cuda")
+    table[:, -1] = 1
+    T = S * m
+    q = torch.randn(T, kv * G, 16, generator=gen(3), device="cuda").to(dtype)
+    out, lse = run(q, h, starts_of([m] * S), i32([n] * S), table, max_new=m)
+    # the definition: n - 256 tokens of score 0 and value 0, then the last page
+    K, V = (kc.double() - 128).transpose(0, 1) * torch.tensor(0.01, dtype=F32).double().item(), (vc.double() - 128).transpose(0, 1)
+    x = torch.einsum("smkgd,lkd->smkgl", q.double().view(S, m, kv, G, 16), K) * 0.25
+    later = torch.arange(256, device="cuda") > (256 - m + torch.arange(m, device="cuda"))[:, None]
+    w = torch.exp(x.masked_fill(later[None, :, None, None], -math.inf))
+    total = n - 256 + w.sum(-1)
+    y = torch.einsum("smkgl,lkd->smkgd", w, V) / total[..., None]
+    mag = torch.einsum("smkgl,lkd->smkgd", w, V.abs()) / total[..., None]
+    big = (q.double().abs().view(S, m, kv, G, 16).sum(-1) * 1.27 * 0.25).reshape(T, kv * G)
+    y, mag, z = y.reshape(out.shape), mag.reshape(out.shape), torch.log(total).reshape(lse.shape)
+    # as in the attention tests: scores within e, weights by 2.1 e, ex2 and their rounding, sums by additions
+    e = 2.0 ** -20 * big + 2.0 ** -30
+    weight = 2.1 * e + 2.0 ** -20 + (U(torch.float16) if dtype == BF16 else 2.0 ** -21) + sum_error(n)
+    tol = weight[..., None] * mag + U(dtype) * y.abs() + 1e-30
+    assert bool(((out.double() - y).abs() <= tol).all()), float(((out.double() - y).abs() / tol).max())
+    assert bool(((lse.double() - z).abs() <= 1.1 * e + sum_error(n) + 2.0 ** -21 + 4 * U(F32) * z).all()), float(lse.max())
