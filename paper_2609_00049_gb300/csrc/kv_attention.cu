@@ -324,7 +324,7 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
                     }
             }
             // the running maximum of s + log2 vscale over the warp's tokens, by query row
-            float shrink[NT][2];
+            float drop[NT][2];
             bool grew = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -335,19 +335,17 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
                     m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 8));
                     m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
                     m = fmaxf(m, mx[nt][e]);
-                    shrink[nt][e] = m == NEG ? 1.f : exp2_fast(mx[nt][e] - m);
+                    drop[nt][e] = m == NEG ? 0.f : mx[nt][e] - m;
                     grew = grew || m > mx[nt][e];
                     mx[nt][e] = m;
                 }
             if (__any_sync(0xFFFFFFFFu, grew)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    sum[nt][0] *= shrink[nt][0], sum[nt][1] *= shrink[nt][1];
+                    const float f0 = exp2_fast(drop[nt][0]), f1 = exp2_fast(drop[nt][1]);
+                    sum[nt][0] = lowered(sum[nt][0], drop[nt][0]), sum[nt][1] = lowered(sum[nt][1], drop[nt][1]);
 #pragma unroll
-                    for (int d = 0; d < Sh::MT; ++d) {
-                        o[d][nt][0] *= shrink[nt][0], o[d][nt][1] *= shrink[nt][1];
-                        o[d][nt][2] *= shrink[nt][0], o[d][nt][3] *= shrink[nt][1];
-                    }
+                    for (int d = 0; d < Sh::MT; ++d) o[d][nt][0] *= f0, o[d][nt][1] *= f1, o[d][nt][2] *= f0, o[d][nt][3] *= f1;
                 }
             }
             uint32_t pb[NT][Sh::PARTS][2];
@@ -456,9 +454,9 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
             for (int w = 0; w < WARPS; ++w) m = fmaxf(m, join_m[w][r]);
 #pragma unroll
             for (int w = 0; w < WARPS; ++w) {
-                const float f = join_m[w][r] == NEG ? 0.f : exp2_fast(join_m[w][r] - m);
-                l += join_l[w][r] * f;
-                join_m[w][r] = f;
+                const float mw = join_m[w][r];
+                l += mw == NEG ? join_l[w][r] * 0.f : lowered(join_l[w][r], mw - m);
+                join_m[w][r] = mw == NEG ? 0.f : exp2_fast(mw - m);
             }
             row_m[r] = m, row_l[r] = l;
             if (!whole) slot[ROWS * DP + r] = m, slot[ROWS * DP + ROWS + r] = l;
@@ -514,9 +512,9 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
                             if (pass == 1 || parts <= AT_ONCE) {
                                 float some = 0.f;
                                 for (int c = lane; c < n; c += 32) {
-                                    const float mc = ms[c * ROWS + r], f = mc == NEG ? 0.f : exp2_fast(mc - m);
-                                    some += ls[c * ROWS + r] * f;
-                                    ms[c * ROWS + r] = f;
+                                    const float mc = ms[c * ROWS + r], lc = ls[c * ROWS + r];
+                                    some += mc == NEG ? lc * 0.f : lowered(lc, mc - m);
+                                    ms[c * ROWS + r] = mc == NEG ? 0.f : exp2_fast(mc - m);
                                 }
 #pragma unroll
                                 for (int o = 16; o; o /= 2) some += __shfl_xor_sync(0xFFFFFFFFu, some, o);

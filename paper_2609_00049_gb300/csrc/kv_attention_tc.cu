@@ -21,7 +21,9 @@
 // so p already holds V's scale and O needs no other.  M is at least the running maximum less
 // 8: it moves only when some row's maximum grew by more than that, and only then O is
 // read, scaled and written back (the largest p stays below 2^14).  lv is at least -88, so that
-// 2^31 tokens of zero values, 2^(88 + 8) each, add up to 2^127 at most.  Scale blocks of fewer than 16
+// 2^31 tokens of zero values, 2^(88 + 8) each, add up to 2^127 at most.  Beside values of
+// a scale 2^60 larger a chunk's p may be too small for any number while its weights are not:
+// the sum then takes 2^(S ks r - M) by an exponential of its own, in tiles marked by the loader.  Scale blocks of fewer than 16
 // tokens take one scale per token in the same formulas.  bf16 queries are exact in
 // fp16 after scaling (down to 2^-29 of a row's largest value); fp32 queries and their p are two fp16
 // parts each, which doubles the products.
@@ -54,6 +56,8 @@ constexpr int MMA_WARP = SOFT_WARPS + 2 * CONV_WARPS, LOAD_WARP = MMA_WARP + 1, 
 constexpr int UNIT = 32;                 // tokens whose codes come and are converted together
 constexpr int SLOTS = 4;                 // of block scales
 constexpr float NEG = -INFINITY, LIFT = 6.f, DOWN = 0.015625f, SLACK = 8.f;   // (DOWN: 2^-LIFT)
+constexpr int FAR = 60;                  // log2 of two scales' quotient from which on the smaller one's weights are summed by themselves
+constexpr float OWN = 24.f, OWN_DOWN = 5.9604645e-08f;   // (these are 2^OWN times what the sum takes)
 
 template <int DP, bool F32> struct Shape {
     static constexpr int NM = DP == 256 ? 1 : 2;                                // row tiles
@@ -231,6 +235,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
     Window &win = *reinterpret_cast<Window *>(smem + Sh::RAW);   // (before the first codes come)
     __shared__ int last_one[2];
     __shared__ Shares shares;
+    __shared__ int far_scales[SLOTS];   // of the scales' slots: some lies far below others
     __shared__ Walk<ROWS, KT> walks[7];   // row tiles, K's and V's converters, products, loaders
     __shared__ float swap[2][NM][128];   // between the threads of a row
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + Sh::BARS);
@@ -424,7 +429,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                 s_phase ^= 1u;
                 if (!ok) break;
                 tc::fence_after_sync();
-                const bool masked = k0 + COLS > all_hi || k0 < all_lo;
+                const bool masked = k0 + COLS > all_hi || k0 < all_lo || far_scales[slot] != 0;
                 const float *sc = reinterpret_cast<const float *>(smem + Sh::SCALES + slot * Sh::SLOT_BYTES) + half * (fine ? COLS : COLS / 4);
                 const auto seen = [&](int j) { return k0 + j < row_hi && k0 + j >= row_lo; };
                 // the largest S ks r + lv
@@ -472,8 +477,8 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                     top = fmaxf(top, swap[half ^ 1][i][row]);
                     const bool grew = top > (m == NEG ? NEG : m + SLACK);
                     if (__any_sync(FULL, grew)) {
-                        const float now = fmaxf(m, top), f = now == NEG ? 1.f : exp2_fast(m - now);
-                        m = now, l *= f;
+                        const float now = fmaxf(m, top), drop = now == NEG ? 0.f : m - now, f = exp2_fast(drop);
+                        m = now, l = lowered(l, drop);
                         if (t > 0) {   // (the products so far are done: S came behind them)
     #pragma unroll 1
                             for (int c = 16 * half; c < D; c += 32) {
@@ -497,6 +502,14 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                         const float c1 = b.x * factor, c0 = b.y + base;
                         const uint64_t c11 = two(c1, c1), c00 = two(c0, c0);
                         uint64_t part2 = 0;
+                        if constexpr (masks) {
+                            if (b.z == 0.f && b.y > NEG) {   // a scale far below others
+                                float own = 0.f;
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) own += exp2_fast(seen(c + j) ? fmaf(__uint_as_float(v[j]), c1, base + (OWN - LIFT)) : NEG);
+                                l = fmaf(own, OWN_DOWN, l);
+                            }
+                        }
 #pragma unroll
                         for (int j = 0; j < 16; j += 2) {
                             float2 x = halves(fma2(two(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), c11, c00));
@@ -517,16 +530,19 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
 #pragma unroll
                         for (int j = 0; j < 16; j += 4) {
                             const float4 ks = *reinterpret_cast<const float4 *>(sc + c + j), lv = *reinterpret_cast<const float4 *>(sc + KT + c + j);
-                            const float4 iv = *reinterpret_cast<const float4 *>(sc + 2 * KT + c + j);   // below zero: the value is NaN
-                            float x[4] = {fmaf(__uint_as_float(v[j]), ks.x * factor, lv.x + base), fmaf(__uint_as_float(v[j + 1]), ks.y * factor, lv.y + base),
-                                          fmaf(__uint_as_float(v[j + 2]), ks.z * factor, lv.z + base), fmaf(__uint_as_float(v[j + 3]), ks.w * factor, lv.w + base)};
+                            const float4 iv = *reinterpret_cast<const float4 *>(sc + 2 * KT + c + j);   // with a minus: the value is NaN
+                            const float c1[4] = {ks.x * factor, ks.y * factor, ks.z * factor, ks.w * factor}, lvs[4] = {lv.x, lv.y, lv.z, lv.w};
                             const float inv[4] = {iv.x, iv.y, iv.z, iv.w};
+                            float x[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                x[e] = exp2_fast(seen(c + j + e) ? x[e] : NEG);
+                                const float s = __uint_as_float(v[j + e]);
+                                x[e] = exp2_fast(seen(c + j + e) ? fmaf(s, c1[e], lvs[e] + base) : NEG);
                                 const bool some = x[e] != 0.f;
                                 l = fmaf(x[e], some ? fabsf(inv[e]) : 0.f, l);
-                                if (some && inv[e] < 0.f) bad = __uint_as_float(0x7FC00000u);
+                                if (some && signbit(inv[e])) bad = __uint_as_float(0x7FC00000u);
+                                if (inv[e] == 0.f && lvs[e] > NEG && seen(c + j + e))   // a scale far below others
+                                    l = fmaf(exp2_fast(fmaf(s, c1[e], base + (OWN - LIFT))), OWN_DOWN, l);
                             }
                             hi[j / 2] = pack_half(x[0], x[1]), hi[j / 2 + 1] = pack_half(x[2], x[3]);
                             if constexpr (F32) lo[j / 2] = pack_rest(x[0], x[1], hi[j / 2]), lo[j / 2 + 1] = pack_rest(x[2], x[3], hi[j / 2 + 1]);
@@ -667,7 +683,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
             for (int c = 0; c < parts; ++c) {
                 const float *s = slot_of(first_cta + c, c == 0) + 128 * DP + row;
                 const float mc = __ldcg(s), lc = __ldcg(s + 128);
-                ll += mc == NEG ? lc * 0.f : lc * exp2_fast(mc - mm);   // (a NaN stays one)
+                ll += mc == NEG ? lc * 0.f : lowered(lc, mc - mm);   // (a NaN stays one)
             }
             const float all_inv = ll == 0.f ? 0.f : DOWN / ll;
 #pragma unroll 1
@@ -762,6 +778,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
         uint32_t fills = 0;
         int slot = 0;
         while (w.more() && ok) {
+            int top = -128;   // log2 of the largest scale of values so far
             const int count = w.count, lo = w.u.lo, hi = w.u.hi, head = w.u.head;
             const int *table = a.tables + (int64_t)w.u.seq * a.max_pages;
             const int base = (lo / KT + w.from) * KT;
@@ -810,6 +827,18 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                     if (!ok) break;
                     float *sc = reinterpret_cast<float *>(smem + Sh::SCALES + slot * Sh::SLOT_BYTES);
                     const int entries = fine ? KT : KT / 16;
+                    // (a scale that is no number counts for nothing; an infinite one, behind a sequence's end, for 2^127)
+                    const auto largest = [&]() { top = max(top, __reduce_max_sync(FULL, there_s && vs > 0.f ? (int)ceilf(fminf(log2_fast(vs), 127.f)) : -128)); };
+                    if (fine) {
+#pragma unroll 1
+                        for (int n = lane; n < KT; n += 32) {
+                            scales_of(t, page, n);
+                            largest();
+                        }
+                    } else {
+                        largest();
+                    }
+                    bool marked = false;
 #pragma unroll 1
                     for (int n0 = 0; n0 < entries; n0 += 32) {
                         const int n = n0 + lane;
@@ -818,7 +847,10 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                         // stays (the scores are not concerned)
                         const bool nan = there_s && vs != vs;
                         const float k = there_s ? ks : 0.f, nv = nan ? vs : 0.f;
-                        const float lv = !there_s ? NEG : (nan ? 0.f : fmaxf(log2_fast(vs), -88.f)), iv = !there_s ? 0.f : exp2_fast(-lv) * DOWN;
+                        const float lv = !there_s ? NEG : (nan ? 0.f : fmaxf(log2_fast(vs), -88.f));
+                        const bool far = there_s && lv < (float)(top - FAR);
+                        const float iv = !there_s || far ? 0.f : exp2_fast(-lv) * DOWN;
+                        marked = marked || far;
                         if (n < entries) {
                             if (fine)
                                 sc[n] = k, sc[KT + n] = lv, sc[2 * KT + n] = nan ? -iv : iv;
@@ -826,6 +858,8 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                                 reinterpret_cast<float4 *>(sc)[n] = make_float4(k, lv, iv, nv);
                         }
                     }
+                    marked = __any_sync(FULL, marked);
+                    if (lane == 0) far_scales[slot] = marked;
                     __syncwarp();
                     if (lane == 0) tc::mbar_arrive(tc::smem_u32(k_full + kring.s));
                 }

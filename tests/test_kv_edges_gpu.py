@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2609_00049_gb300 as rq
-from kv_reference import gen, i32, starts_of
+from kv_reference import Cache, attention, gen, i32, starts_of
 
 pytestmark = pytest.mark.gpu
 BF16, F32 = torch.bfloat16, torch.float32
@@ -113,3 +113,27 @@ def test_zero_values_before_others(m, dtype):
     tol = weight[..., None] * mag + U(dtype) * y.abs() + 1e-30
     assert bool(((out.double() - y).abs() <= tol).all()), float(((out.double() - y).abs() / tol).max())
     assert bool(((lse.double() - z).abs() <= 1.1 * e + sum_error(n) + 2.0 ** -21 + 4 * U(F32) * z).all()), float(lse.max())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("m", [1, 40])
+@pytest.mark.parametrize("n,block", [(300, 16), (300, 4), (3000, 16)])
+@pytest.mark.parametrize("power", [110, 60, 20, -60])
+def test_values_of_any_size(power, n, block, m, dtype):
+    """Outputs of very large and very small values, with zero and far smaller ones among them: their tokens' weights count
+    all the same, within a tile, over tiles and over shares."""
+    c = Cache(30, [n], kv=1, D=32, page=16, block=block, poison=False)
+    c.v_scale *= 2.0 ** power
+    c.v_scale[0, c.rows[0][3]] = 0.0
+    c.v_scale[0, c.rows[0][5:7]] *= 2.0 ** (-80 if power > 0 else -10)
+    if n > 2000:
+        c.v_scale[0, c.rows[0][40:130]] = 0.0
+    q = torch.randn(m, 4, 32, generator=gen(4), device="cuda").to(dtype)
+    out, lse = run(q, rq.kv_cache(**c.buffers()), starts_of([m]), c.lengths, c.tables)
+    y, z, mag, big = attention(q, c.values("k", 0, 0), c.values("v", 0, 0), n, 0, True, 32 ** -0.5)
+    e = 2.0 ** -20 * big + 2.0 ** -30
+    weight = 2.1 * e + 2.0 ** -20 + (U(torch.float16) if dtype == BF16 else 2.0 ** -21) + sum_error(n)
+    # (a zero value counts as 127 x 2^-88 at most in the kernel of many rows)
+    tol = weight[..., None] * mag + U(dtype) * y.abs() + 2.0 ** -81
+    assert bool(((out.double() - y).abs() <= tol).all()), float(((out.double() - y).abs() / tol).max())
+    assert bool(((lse.double() - z).abs() <= 1.1 * e + sum_error(n) + 2.0 ** -21 + 4 * U(F32) * z.abs()).all())
