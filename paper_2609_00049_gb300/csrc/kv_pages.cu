@@ -68,26 +68,26 @@ __device__ __forceinline__ int block_sum(int v) {
     return __reduce_add_sync(0xFFFFFFFFu, t);
 }
 // exclusive prefix of v over the CTA's threads; *total their sum
-__device__ __forceinline__ int block_scan(int v, int *total) {
-    __shared__ int part[WARPS];
+template <class I> __device__ __forceinline__ I block_scan(I v, I *total) {
+    __shared__ I part[WARPS];
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    int x = v;
+    I x = v;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
-        const int y = __shfl_up_sync(0xFFFFFFFFu, x, d);
+        const I y = __shfl_up_sync(0xFFFFFFFFu, x, d);
         if (lane >= d) x += y;
     }
     __syncthreads();
     if (lane == 31) part[w] = x;
     __syncthreads();
-    int p = part[lane];
+    I p = part[lane];
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
-        const int y = __shfl_up_sync(0xFFFFFFFFu, p, d);
+        const I y = __shfl_up_sync(0xFFFFFFFFu, p, d);
         if (lane >= d) p += y;
     }
     *total = __shfl_sync(0xFFFFFFFFu, p, 31);
-    const int base = w == 0 ? 0 : __shfl_sync(0xFFFFFFFFu, p, w - 1);
+    const I base = w == 0 ? 0 : __shfl_sync(0xFFFFFFFFu, p, w - 1);
     return base + x - v;
 }
 
@@ -179,10 +179,10 @@ reserve_kernel(KvPagesView v, const int *starts, int64_t T, int64_t *positions, 
     // for the sum, the first one notes it.  A shared last page is copied unless the row is the last of its holders.
     bool refused = peek(w.head + 2) != 0;
     const int2 free_pages = counted(w.head + 8);
-    int wanted = 0;
+    int64_t wanted = 0;   // (1024 rows of up to 2^24 pages pass 32 bits)
     for (int base = 0; base < n_rows && !refused; base += THREADS) {
         const int s = base + threadIdx.x;
-        int n = 0;
+        int64_t n = 0;
         bool copy = false;
         if (s < n_rows) {
             const Row r = row_of(v, starts, log_page, s, T);
@@ -190,15 +190,15 @@ reserve_kernel(KvPagesView v, const int *starts, int64_t T, int64_t *positions, 
                 const int held = v.used[r.last];
                 copy = held > 1 && !(peek(w.latest + r.last) == s + 1 && peek(w.writers + r.last) >= held);
             }
-            n = min(r.after - r.first + (copy ? 1 : 0), 1 << 20);   // (a row beyond that is beyond every pool: no sum passes 32 bits)
+            n = r.after - r.first + (copy ? 1 : 0);
         }
-        int total;
-        const int r = block_scan(n, &total);
-        if (s < n_rows && rank() == 0) w.need[s] = wanted + r, w.winner[s] = copy ? 1 : 0;
+        int64_t total;
+        const int64_t r = block_scan(n, &total);
+        if (s < n_rows && rank() == 0) w.need[s] = (int)(wanted + r), w.winner[s] = copy ? 1 : 0;   // (below 2^30 unless refused)
         refused = total > free_pages.y - wanted;
         wanted += total;
     }
-    if (!refused) list_part(part, free_pages.x, wanted, is_free, [&](int r, int p) { w.list[r] = p; });
+    if (!refused) list_part(part, free_pages.x, (int)wanted, is_free, [&](int r, int p) { w.list[r] = p; });
     meet();
     if (refused) {   // (every CTA has counted the same)
         if (tid == 0) atomicOr(w.head, (int)ST_NO_PAGES);

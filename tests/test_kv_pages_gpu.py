@@ -304,3 +304,50 @@ def test_cache_of_many_sequences_lives_through_everything():
             rq.realq_kv_read(p.cache, la, starts_of(counts), pos, p.d_tables, k, v)
             want = torch.stack([t[la] for h in held for t in h])
             assert torch.equal(k, want) and torch.equal(v, -want)
+
+
+def test_reserving_more_than_a_million_pages_at_once():
+    """Rows that need more than 2^20 pages each: refused where the pool has fewer, whatever is left of it, and given
+    what they need where it has them."""
+    n, page = 2 ** 21, 16
+    codes = [torch.empty(1, n, 1, page, 16, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    cache = rq.kv_cache(*codes, *(torch.empty(1, n, 1, 1, device="cuda") for _ in range(2)))
+    used, tables, lengths = i32([0] * n), torch.full((3, n), -1, dtype=torch.int32, device="cuda"), i32([0] * 3)
+    pages = rq.kv_pages(used, tables, lengths)
+    ws = rq.workspace(rq.realq_pages_workspace_size(n, 3, n))
+
+    def reserve(need):      # pages of each row, the last but for 3 places
+        adds = [max(0, page * k - 3) for k in need]
+        before = [t.clone() for t in (used, tables, lengths)]
+        pos = torch.full((sum(adds),), 5, dtype=torch.int64, device="cuda")
+        rq.realq_pages_reserve(pages, starts_of(adds), pos, cache, ws=ws)
+        free = int((before[0] == 0).sum())
+        if sum(need) > free:
+            with pytest.raises(rq.RealqError) as e:
+                rq.realq_workspace_status(ws)
+            assert e.value.status == rq.REALQ_ERR_NO_PAGES
+            assert bool((pos == -1).all())
+            for a, b in zip(before, (used, tables, lengths)):
+                assert torch.equal(a, b)
+            return False
+        rq.realq_workspace_status(ws)
+        at = torch.nonzero(before[0] == 0)[:, 0].to(torch.int32)
+        want = before[1].clone()
+        t = k0 = 0
+        for s, k in enumerate(need):
+            if k:
+                want[s, :k] = at[k0:k0 + k]
+                assert torch.equal(pos[t:t + adds[s]], torch.arange(adds[s], device="cuda"))
+            k0, t = k0 + k, t + adds[s]
+        assert torch.equal(tables, want) and lengths.tolist() == [b + a for b, a in zip(before[2].tolist(), adds)]
+        assert torch.equal(used, before[0].index_fill(0, at[:k0].long(), 1))
+        return True
+    m = 2 ** 20
+    assert not reserve([m + 7, m + 7, 0])
+    assert not reserve([m + 7, m - 7, 1])
+    assert reserve([m - 6, 0, 0])
+    assert not reserve([0, m + 20, 0])          # 2^20 + 6 are left
+    assert reserve([0, m + 6, 0])
+    rq.realq_pages_release(pages, i32([0, 1]))
+    assert int(used.sum()) == 0
+    assert reserve([m + 5, 0, 3])
