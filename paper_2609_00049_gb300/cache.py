@@ -27,7 +27,7 @@ from typing import Optional, Sequence, Union
 
 import torch
 
-from . import (kv_cache, kv_pages, realq_kv_append, realq_kv_attention, realq_kv_attention_workspace_size,
+from . import (REALQ_ERR_TIMEOUT, RealqError, kv_cache, kv_pages, realq_kv_append, realq_kv_attention, realq_kv_attention_workspace_size,
                realq_pages_compact, realq_pages_fork, realq_pages_release, realq_pages_reserve,
                realq_pages_workspace_size, realq_rotary, realq_rotary_frequencies, realq_workspace_status, workspace, _stream)
 
@@ -157,7 +157,17 @@ class Cache8:
         return self.moved_to
 
     def check(self, stream=None) -> None:
-        """Raises RealqError if a step since the last check found too few pages, or a bounded wait gave up (synchronizes)."""
+        """Raises RealqError if a step since the last check found too few pages, or a bounded wait gave up (synchronizes).
+        Where both happened, the latter is raised from the former.  What a wait that gave up left in the cache's
+        workspace is cleared; the outputs since the last check are then unspecified."""
+        error = None
         with self._begin(stream):
             for ws in (self._pages_ws, self._attend_ws):
-                realq_workspace_status(ws)
+                try:
+                    realq_workspace_status(ws)
+                except RealqError as e:
+                    if e.status == REALQ_ERR_TIMEOUT:
+                        ws.zero_()   # (arrival counters stay where the call left them)
+                    e.__cause__, error = error, e
+        if error is not None:
+            raise error

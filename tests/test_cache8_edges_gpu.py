@@ -1,0 +1,65 @@
+"""What Cache8 does with errors, refusals, streams and the host's time."""
+import pytest
+import torch
+
+import paper_2609_00049_gb300 as rq
+from kv_reference import gen
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    from paper_2609_00049_gb300 import build as b
+    b.build()
+    rq.lib()
+
+
+def caches(n, **kw):
+    from paper_2609_00049_gb300.cache import Cache8
+    return [Cache8(2, 40, 3, 300, 2, 64, page_size=16, **kw) for _ in range(n)]
+
+
+def tokens(T, seed, dtype=torch.bfloat16):
+    return [torch.randn(T, n, 64, generator=gen(seed + i), device="cuda").to(dtype) for i, n in enumerate((8, 2, 2))]
+
+
+TIMEOUT_BIT, NO_PAGES_BIT = 4, 8      # of a workspace's status word
+
+
+def test_going_on_after_a_wait_that_gave_up():
+    """A status and arrival counters as a call that gave up leaves them: check raises once, and what follows is as in a
+    cache that never saw it."""
+    bad, good = caches(2)
+    for c in (bad, good):
+        step = c.begin([250, 100, 33])
+        c.attend(step, 0, *tokens(383, 1))
+    torch.cuda.synchronize()
+    # (those of the kernel of few rows begin 256 bytes behind the status)
+    bad._attend_ws.view(torch.int32)[64:128] = 30          # (of a join of some 50 shares)
+    bad._attend_ws.view(torch.int32)[0] = TIMEOUT_BIT
+    with pytest.raises(rq.RealqError) as e:
+        bad.check()
+    assert e.value.status == rq.REALQ_ERR_TIMEOUT
+    bad.check()
+    for i, counts in enumerate([[1, 1, 1], [2, 0, 20], [1, 1, 1]]):
+        got, want = (c.attend(c.begin(counts), 0, *tokens(sum(counts), 10 + i)) for c in (bad, good))
+        assert torch.equal(got, want), counts
+    bad.check()
+
+
+def test_check_reports_both_errors():
+    """Too few pages and a wait that gave up since the last check: both are raised, and nothing is left behind."""
+    c, = caches(1)
+    c._pages_ws.view(torch.int32)[0] = NO_PAGES_BIT
+    c._attend_ws.view(torch.int32)[0] = TIMEOUT_BIT
+    with pytest.raises(rq.RealqError) as e:
+        c.check()
+    assert e.value.status == rq.REALQ_ERR_TIMEOUT and e.value.__cause__.status == rq.REALQ_ERR_NO_PAGES
+    c.check()
+    assert not bool(c._attend_ws.any())
+    c._pages_ws.view(torch.int32)[0] = NO_PAGES_BIT
+    with pytest.raises(rq.RealqError) as e:
+        c.check()
+    assert e.value.status == rq.REALQ_ERR_NO_PAGES
+    c.check()
