@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(32 * WARPS) read_kernel(KvReadArgs a) {
     if (t >= a.T) return;
     const int64_t p = a.positions[t], pi = p >> a.c.log_page;
     const int s = last_at_most(a.n_seqs, t, [&](int q) { return (int64_t)a.starts[q]; });
-    if (a.starts[s] < 0 || t < a.starts[s] || t >= a.starts[s + 1]) return;
+    if (a.starts[s] < 0 || t < a.starts[s] || t >= a.starts[s + 1] || a.starts[s + 1] > a.T) return;
     int pg = -1;
     if (p >= 0 && pi < a.max_pages) pg = a.tables[s * a.max_pages + pi];
     const bool there = pg >= 0 && pg < a.c.n_pages;

@@ -137,3 +137,21 @@ def test_values_of_any_size(power, n, block, m, dtype):
     tol = weight[..., None] * mag + U(dtype) * y.abs() + 2.0 ** -81
     assert bool(((out.double() - y).abs() <= tol).all()), float(((out.double() - y).abs() / tol).max())
     assert bool(((lse.double() - z).abs() <= 1.1 * e + sum_error(n) + 2.0 ** -21 + 4 * U(F32) * z.abs()).all())
+
+
+# ------------------------------------------------------- lists with faults ---
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_reading_beside_a_sequence_that_ends_outside(dtype):
+    """A sequence that ends behind the call's tokens takes no part; those before it are read, and nothing else is written."""
+    c = Cache(31, [40, 40, 40], kv=2, D=32, page=16, block=4, poison=False)
+    h, pos = rq.kv_cache(**c.buffers()), torch.arange(12, device="cuda")
+    for starts, good in (([0, 3, 20, 20], 3), ([0, 3, 7, 13], 7), ([0, 12, 12, 12], 12), ([0, 4, 4, 9], 9), ([0, 0, 0, 13], 0), ([0, 2, 5, 5], 5)):
+        got = [torch.full((12, 2, 32), 7.0, device="cuda", dtype=dtype) for _ in range(2)]
+        rq.realq_kv_read(h, 0, i32(starts), pos, c.tables, *got)
+        for w, t in zip("kv", got):
+            assert bool((t[good:] == 7).all()), starts
+            for s in range(3):
+                a, b = starts[s], min(starts[s + 1], good)
+                if a < b:
+                    want = c.values(w, 0, s)[a:b]
+                    assert bool(((t[a:b].double() - want).abs() <= (U(F32) + U(dtype)) * want.abs()).all()), starts
