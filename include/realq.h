@@ -486,6 +486,7 @@ realq_status_t realq_kv_read(realq_stream_t stream, const realq_kv_cache_t *cach
  * n_seqs at most 2^20, n_heads at most 1024 n_kv, T n_heads / n_kv below 2^30.
  * The block scales are those of realq_kv_append: not negative, or NaN; values'
  * scales below 2^-88 count as that in sequences of many rows.
+ * Tokens beyond the table's row or without a page are not seen; the queries keep their positions.
  * A query that sees no token gets zeros and lse -inf.  Tokens that a query does
  * not see have no influence, whatever the cache holds there.  Rows of q outside
  * every sequence are left as they were in out and lse.  Scores, sums and

@@ -1153,6 +1153,7 @@ realq_status_t realq_kv_attention(realq_stream_t stream, const realq_kv_cache_t 
     REALQ_TRY(check_ws(ws, ws_bytes, kv_attention_ws_bytes(), who));
     a.n_seqs = (int)n_seqs, a.n_heads = (int)n_heads, a.group = (int)(n_heads / a.c.n_kv), a.causal = causal != 0;
     a.T = T, a.q = q, a.q_ld = q_ld, a.q_hs = q_hs, a.max_pages = max_pages, a.window = window;
+    a.room = (int)std::min<int64_t>(max_pages << a.c.log_page, INT32_MAX);
     a.starts = starts, a.lengths = lengths, a.tables = tables, a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.out = out, a.lse = lse;
     // Few rows and many have a kernel each, which take their sequences out of the call's; where the caller has none

@@ -209,6 +209,7 @@ constexpr int KV_MAX_CTAS_PER_SM = 4;
 struct KvAttnArgs {
     KvView c;
     int n_seqs, n_heads, group, causal;   // group: query heads of a key/value head
+    int room;                             // tokens that a table's row has entries for
     int64_t T, q_ld, q_hs, max_pages, window;
     const void *q;
     const int *starts, *lengths, *tables;

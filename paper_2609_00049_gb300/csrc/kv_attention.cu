@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
             if (t == 0) {
                 const int p = u.len - u.m + qi;
                 row_scale[8 * nt + g] = a.scale_log2 * __uint_as_float((uint32_t)(127 - k) << 23);
-                row_hi[8 * nt + g] = !row_in ? 0 : (a.causal ? min(u.len, p + 1) : u.len);
+                row_hi[8 * nt + g] = !row_in ? 0 : min(a.room, a.causal ? p + 1 : u.len);
                 row_lo[8 * nt + g] = a.window > 0 ? (int)max((int64_t)0, (int64_t)p - a.window + 1) : 0;
             }
         }
@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
         for (int nt = 0; nt < NT; ++nt) rs[nt][0] = row_scale[8 * nt + 2 * t], rs[nt][1] = row_scale[8 * nt + 2 * t + 1];
         // tokens that every row sees
         const int p_first = u.len - u.m + u.r0 / a.group, p_last = u.len - u.m + (u.r0 + u.rows - 1) / a.group;
-        const int clear_hi = a.causal ? min(u.len, p_first + 1) : u.len;
+        const int clear_hi = min(a.room, a.causal ? p_first + 1 : u.len);
         const int64_t clear_lo = a.window > 0 ? (int64_t)p_last - a.window + 1 : 0;
 
         float o[Sh::MT][NT][4];

@@ -417,7 +417,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
             int64_t out_row;
             {
                 const int r = w.u.r0 + 128 * i + row, qi = r / a.group, p = w.u.len - w.u.m + qi;
-                if (in) row_hi = a.causal ? min(w.u.len, p + 1) : w.u.len;
+                if (in) row_hi = min(a.room, a.causal ? p + 1 : w.u.len);
                 if (a.window > 0) row_lo = (int)max((int64_t)0, (int64_t)p - a.window + 1);
                 out_row = (int64_t)(w.u.q0 + qi) * a.n_heads + w.u.head * a.group + (r - qi * a.group);
             }

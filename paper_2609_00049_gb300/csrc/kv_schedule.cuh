@@ -78,7 +78,7 @@ __device__ __forceinline__ uint32_t codes23(uint32_t w) { return hsub2(__byte_pe
 struct Unit {        // one sequence, key/value head and row tile
     int seq, head;
     int q0, m;       // the sequence's first query token and their number
-    int len;         // cached tokens
+    int len;         // its tokens (those beyond the table's row, which no one sees, among them)
     int r0, rows;    // rows of the tile: r0 .. r0 + rows - 1 of m x G
     int lo, hi;      // cached tokens that any row sees: [lo, hi)
 };
@@ -87,7 +87,7 @@ struct Unit {        // one sequence, key/value head and row tile
 // are written too).
 __device__ __forceinline__ void span(const KvAttnArgs &a, int m, int len, int r0, int r1, int *lo, int *hi) {
     const int p0 = len - m + r0 / a.group, p1 = len - m + (r1 - 1) / a.group;
-    *hi = a.causal ? max(0, min(len, p1 + 1)) : len;
+    *hi = max(0, min(a.room, a.causal ? p1 + 1 : len));
     *lo = a.window > 0 ? (int)min((int64_t)*hi, max((int64_t)0, (int64_t)p0 - a.window + 1)) : 0;
 }
 template <int TILE> __device__ __forceinline__ int tiles_of(int lo, int hi) {
@@ -100,7 +100,7 @@ struct Seq {
         const int64_t b = a.starts[s], e = a.starts[s + 1];
         const bool ok = b >= 0 && e > b && e <= a.T;
         q0 = ok ? (int)b : 0, m = ok ? (int)(e - b) : 0;
-        len = (int)min((int64_t)max(a.lengths[s], 0), a.max_pages << a.c.log_page);
+        len = max(a.lengths[s], 0);
         if (m > 0 && !a.takes(m)) m = 0;   // another kernel's
     }
 };

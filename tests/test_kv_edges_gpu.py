@@ -155,3 +155,56 @@ def test_reading_beside_a_sequence_that_ends_outside(dtype):
                 if a < b:
                     want = c.values(w, 0, s)[a:b]
                     assert bool(((t[a:b].double() - want).abs() <= (U(F32) + U(dtype)) * want.abs()).all()), starts
+
+
+def expected(q, K, V, there, L, window, causal, scale):
+    """Attention of a sequence of L tokens of which the first len(there) can be in the table and those that `there` names
+    are; as kv_reference.attention."""
+    m, H, D = q.shape
+    kv, n = K.shape[1], len(there)
+    q = q.double().view(m, kv, H // kv, D)
+    at, key = torch.arange(L - m, L, device="cuda")[:, None], torch.arange(n, device="cuda")
+    seen = there.expand(m, n) & ((key <= at) if causal else (key < L))
+    if window:
+        seen = seen & (key > at - window)
+    s = (torch.einsum("mkgd,lkd->mkgl", q, K) * scale).masked_fill(~seen[:, None, None], -math.inf)
+    if n == 0:
+        zero = torch.zeros(m, H, D, dtype=torch.float64, device="cuda")
+        return zero, zero[..., 0] - math.inf, zero, zero[..., 0]
+    lse = torch.logsumexp(s, -1)
+    p = torch.exp(s - lse[..., None]).nan_to_num(0.0)
+    y, mag = torch.einsum("mkgl,lkd->mkgd", p, V), torch.einsum("mkgl,lkd->mkgd", p, V.abs())
+    big = torch.einsum("mkgd,lkd->mkgl", q.abs(), K.abs()).amax(-1) * scale
+    return y.reshape(m, H, D), lse.reshape(m, H), mag.reshape(m, H, D), big.reshape(m, H)
+
+
+def close(out, lse, y, z, mag, big, L):
+    """The attention tests' tolerances."""
+    dtype = out.dtype
+    e, steps = 2.0 ** -20 * big + 2.0 ** -30, (L / 16 + 160) * 2.0 ** -23
+    weight = 2.1 * e + 2.0 ** -20 + (U(torch.float16) if dtype == BF16 else 2.0 ** -21) + steps
+    none = z == -math.inf
+    assert bool((lse[none] == -math.inf).all()) and bool((out[none] == 0).all())
+    err, tol = (out.double() - y).abs(), weight[..., None] * mag + U(dtype) * y.abs() + 1e-30
+    assert bool((err <= tol).all()), float((err / tol).max())
+    err, tol = (lse.double() - z).abs()[~none], (1.1 * e + steps + 2.0 ** -21 + 4 * U(F32) * z.abs())[~none]
+    assert bool((err <= tol).all()), float((err / tol).max())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("kw", [dict(), dict(window=70), dict(causal=False)])
+@pytest.mark.parametrize("news", [[1, 2, 5], [40, 70, 90]])
+def test_attention_of_sequences_beyond_their_table(news, kw, dtype):
+    """lengths that the table's row has no entries for: the queries keep their positions, the tokens behind take no part."""
+    lens, width = [100, 200, 128], 128
+    c = Cache(32, [width] * 3, kv=2, D=64, page=16, block=8, extra_entries=0, poison=False)
+    T, H = sum(news), 8
+    q = torch.randn(T, H, 64, generator=gen(5), device="cuda").to(dtype)
+    out, lse = run(q, rq.kv_cache(**c.buffers()), starts_of(news), i32(lens), c.tables, max_new=max(news), **kw)
+    at = 0
+    for s, m in enumerate(news):
+        n = min(lens[s], width)
+        want = expected(q[at:at + m], c.values("k", 0, s, n), c.values("v", 0, s, n), torch.ones(n, dtype=torch.bool, device="cuda"), lens[s],
+                        kw.get("window", 0), kw.get("causal", True), 64 ** -0.5)
+        close(out[at:at + m], lse[at:at + m], *want, n)
+        at += m
