@@ -146,8 +146,9 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
         // ---- this warp's 16 tokens of every tile ----
         const int *table = a.tables + (int64_t)u.seq * a.max_pages;
         const auto page_of = [&](int i) {   // of the warp's group i, -1 where there is none
-            const int k0 = (tile0 + i) * TILE + warp * GROUP;
-            if (i >= count || k0 >= u.hi || k0 + GROUP <= u.lo) return -1;
+            if (i >= count) return -1;
+            const int k0 = (tile0 + i) * TILE + warp * GROUP;   // (k0 + GROUP may be 2^31)
+            if (k0 >= u.hi || k0 + (GROUP - 1) < u.lo) return -1;
             const int pg = table[k0 >> a.c.log_page];
             return pg >= 0 && pg < a.c.n_pages ? pg : -1;
         };
@@ -311,7 +312,7 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
                 s[nt][0] *= ksc[0] * rs[nt][0], s[nt][1] *= ksc[0] * rs[nt][1];
                 s[nt][2] *= ksc[1] * rs[nt][0], s[nt][3] *= ksc[1] * rs[nt][1];
             }
-            const bool masked = k0 + GROUP > clear_hi || k0 < clear_lo;
+            const bool masked = k0 + (GROUP - 1) >= clear_hi || k0 < clear_lo;
             if (masked) {
                 const int ka = k0 + g, kb = k0 + g + 8;
 #pragma unroll

@@ -429,7 +429,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                 s_phase ^= 1u;
                 if (!ok) break;
                 tc::fence_after_sync();
-                const bool masked = k0 + COLS > all_hi || k0 < all_lo || far_scales[slot] != 0;
+                const bool masked = k0 + (COLS - 1) >= all_hi || k0 < all_lo || far_scales[slot] != 0;
                 const float *sc = reinterpret_cast<const float *>(smem + Sh::SCALES + slot * Sh::SLOT_BYTES) + half * (fine ? COLS : COLS / 4);
                 const auto seen = [&](int j) { return k0 + j < row_hi && k0 + j >= row_lo; };
                 // the largest S ks r + lv
@@ -783,8 +783,9 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
             const int *table = a.tables + (int64_t)w.u.seq * a.max_pages;
             const int base = (lo / KT + w.from) * KT;
             const auto page_of = [&](int t) {   // of the tile's 16 tokens `lane`
-                const int k0 = base + t * KT + 16 * lane;
-                return t < count && lane < KT / 16 && k0 < hi && k0 + 16 > lo ? __ldg(table + (k0 >> a.c.log_page)) : -1;
+                if (t >= count || lane >= KT / 16) return -1;
+                const int k0 = base + t * KT + 16 * lane;   // (k0 + 16 may be 2^31)
+                return k0 < hi && k0 + 15 >= lo ? __ldg(table + (k0 >> a.c.log_page)) : -1;
             };
             float ks = 0.f, vs = 0.f;
             bool there_s = false;
@@ -802,7 +803,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
             for (int t = 0; t < count && ok; ++t, kring.next(), slot = (slot + 1) & (SLOTS - 1)) {
                 const bool good = page >= 0 && page < a.c.n_pages;
                 const uint32_t there = __ballot_sync(FULL, good);
-                const int k0 = base + t * KT + 16 * lane, place = k0 & ((1 << a.c.log_page) - 1);
+                const int k0 = base + t * KT + 16 * (lane & (KT / 16 - 1)), place = k0 & ((1 << a.c.log_page) - 1);
                 const int64_t tile = (int64_t)page * a.c.n_kv + head;
                 const uint8_t *src = codes + ((tile << a.c.log_page) + place) * D;
                 if (!is_v && !fine) scales_of(t, page, lane);   // (under way with the codes)

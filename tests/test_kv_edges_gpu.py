@@ -208,3 +208,20 @@ def test_attention_of_sequences_beyond_their_table(news, kw, dtype):
                         kw.get("window", 0), kw.get("causal", True), 64 ** -0.5)
         close(out[at:at + m], lse[at:at + m], *want, n)
         at += m
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("m", [1, 3, 40])
+@pytest.mark.parametrize("back", [0, 1, 17, 300])
+def test_attention_of_the_last_tokens_that_lengths_can_name(m, back, dtype):
+    """A sequence of 2^31 - 1 tokens (less `back`), whose table names a few pages again and again."""
+    L, page, near, window = 2 ** 31 - 1 - back, 256, 1024, 200
+    c = Cache(33, [7 * page], kv=1, D=16, page=page, block=16, spare=0, extra_entries=0, poison=False)
+    table = (torch.arange(2 ** 31 // page, device="cuda") % 7).to(torch.int32)[None]
+    q = torch.randn(m, 2, 16, generator=gen(6), device="cuda").to(dtype)
+    out, lse = run(q, rq.kv_cache(**c.buffers()), starts_of([m]), i32([L]), table, window=window)
+    at = torch.arange(L - near, L, device="cuda")
+    pg, slot = table[0].long()[at // page], at % page
+    K, V = ((codes[0, pg, :, slot].double() - 128) * scale[0, pg, :, slot // 16].double()[..., None]
+            for codes, scale in ((c.k_codes, c.k_scale), (c.v_codes, c.v_scale)))
+    close(out, lse, *attention(q, K, V, near, window, True, 0.25), near)
