@@ -524,8 +524,8 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                         }
                         const float2 ph = halves(part2);
                         const float part = ph.x + ph.y;
-                        if (!masks || part != 0.f)   // (unseen tokens' scales may be anything)
-                            l = fmaf(part, b.z, l), bad = fmaf(part, b.w, bad);
+                        // (unseen tokens' scales may be anything; a seen NaN counts, however small its weight)
+                        if (!masks || (k0 + c < row_hi && k0 + c + 15 >= row_lo)) l = fmaf(part, b.z, l), bad = fmaf(part, b.w, bad);
                     } else {
 #pragma unroll
                         for (int j = 0; j < 16; j += 4) {
@@ -538,10 +538,10 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                             for (int e = 0; e < 4; ++e) {
                                 const float s = __uint_as_float(v[j + e]);
                                 x[e] = exp2_fast(seen(c + j + e) ? fmaf(s, c1[e], lvs[e] + base) : NEG);
-                                const bool some = x[e] != 0.f;
+                                const bool some = seen(c + j + e);
                                 l = fmaf(x[e], some ? fabsf(inv[e]) : 0.f, l);
                                 if (some && signbit(inv[e])) bad = __uint_as_float(0x7FC00000u);
-                                if (inv[e] == 0.f && lvs[e] > NEG && seen(c + j + e))   // a scale far below others
+                                if (some && inv[e] == 0.f && lvs[e] > NEG)   // a scale far below others
                                     l = fmaf(exp2_fast(fmaf(s, c1[e], base + (OWN - LIFT))), OWN_DOWN, l);
                             }
                             hi[j / 2] = pack_half(x[0], x[1]), hi[j / 2 + 1] = pack_half(x[2], x[3]);

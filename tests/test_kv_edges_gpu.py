@@ -225,3 +225,23 @@ def test_attention_of_the_last_tokens_that_lengths_can_name(m, back, dtype):
     K, V = ((codes[0, pg, :, slot].double() - 128) * scale[0, pg, :, slot // 16].double()[..., None]
             for codes, scale in ((c.k_codes, c.k_scale), (c.v_codes, c.v_scale)))
     close(out, lse, *attention(q, K, V, near, window, True, 0.25), near)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("block", [16, 4])
+@pytest.mark.parametrize("m", [1, 150])
+def test_a_nan_among_values_of_no_weight(m, block, dtype):
+    """Tokens whose weight is too small for any number of fp32, with values that are NaN: the rows that see them are NaN,
+    the log sums are not, whichever tile the rows' last tokens lie in; a window that passes them by leaves numbers."""
+    n = 150
+    c = Cache(34, [n], kv=1, D=64, page=16, block=block, poison=False)
+    first = c.rows[0][0]
+    c.k_codes[0, first], c.k_scale[0, first] = 1, 1.0           # -127 in every channel: a score of -8128 for a q of ones
+    c.v_scale[0, first] = math.nan
+    q = torch.ones(m, 2, 64, device="cuda", dtype=dtype)
+    h = rq.kv_cache(**c.buffers())
+    out, lse = run(q, h, starts_of([m]), c.lengths, c.tables, scale=1.0)
+    p = torch.arange(n - m, n, device="cuda")
+    assert bool(out.isnan().all()) and bool(torch.isfinite(lse).all())
+    out, lse = run(q, h, starts_of([m]), c.lengths, c.tables, scale=1.0, window=20)
+    assert bool(out[p < 35].isnan().all()) and bool(torch.isfinite(out[p >= 35]).all()) and bool(torch.isfinite(lse).all())
