@@ -472,7 +472,7 @@ realq_status_t realq_kv_read(realq_stream_t stream, const realq_kv_cache_t *cach
  * over j <= p when causal != 0 (all j < lengths[s] otherwise), and, with
  * window > 0 (causal only), over the last `window` of them, j > p - window.
  *   q    T x n_heads x head_dim of dtype (head h of token t at t q_ld + h q_hs
- *        elements); n_heads a multiple of n_kv.
+ *        elements); n_heads a multiple of n_kv.  |scale| at most 2^127.
  *   out  T x n_heads x head_dim, dtype.  lse  T x n_heads floats, or NULL:
  *        the natural log of the softmax's sum.
  *   max_new   at least every sequence's number of query tokens, for the choice

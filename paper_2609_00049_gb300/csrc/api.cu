@@ -1140,7 +1140,8 @@ realq_status_t realq_kv_attention(realq_stream_t stream, const realq_kv_cache_t 
     if (!valid_dtype(dtype)) return fail(REALQ_ERR_INVALID_ARG, "kv_attention: bad dtype");
     if (n_heads <= 0 || n_heads % a.c.n_kv) return fail(REALQ_ERR_INVALID_ARG, "kv_attention: n_heads must be a multiple of n_kv");
     if (n_heads / a.c.n_kv > 1024) return fail(REALQ_ERR_UNSUPPORTED, "kv_attention: at most 1024 heads to a key/value head");
-    if (!std::isfinite(scale)) return fail(REALQ_ERR_INVALID_ARG, "kv_attention: scale must be finite");
+    const float scale_log2 = (float)((double)scale * 1.4426950408889634);   // (scores are formed in base 2)
+    if (!std::isfinite(scale_log2)) return fail(REALQ_ERR_INVALID_ARG, "kv_attention: scale log2(e) must be finite");
     if (window < 0 || (window > 0 && !causal)) return fail(REALQ_ERR_INVALID_ARG, "kv_attention: window >= 0, and only with causal != 0");
     if (n_seqs > (1ll << 20)) return fail(REALQ_ERR_UNSUPPORTED, "kv_attention: n_seqs at most 2^20");   // (a bounded wait outlasts a walk over as many)
     if (max_new < 1 && T > 0) return fail(REALQ_ERR_INVALID_ARG, "kv_attention: max_new >= 1 required");
@@ -1154,7 +1155,7 @@ realq_status_t realq_kv_attention(realq_stream_t stream, const realq_kv_cache_t 
     a.n_seqs = (int)n_seqs, a.n_heads = (int)n_heads, a.group = (int)(n_heads / a.c.n_kv), a.causal = causal != 0;
     a.T = T, a.q = q, a.q_ld = q_ld, a.q_hs = q_hs, a.max_pages = max_pages, a.window = window;
     a.room = (int)std::min<int64_t>(max_pages << a.c.log_page, INT32_MAX);
-    a.starts = starts, a.lengths = lengths, a.tables = tables, a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+    a.starts = starts, a.lengths = lengths, a.tables = tables, a.scale_log2 = scale_log2;
     a.out = out, a.lse = lse;
     // Few rows and many have a kernel each, which take their sequences out of the call's; where the caller has none
     // of many rows, one launch takes all (and serves longer ones too, 32 rows at a time).
