@@ -584,6 +584,13 @@ def _on(device: int) -> int:
     return device
 
 
+def _pool(pages: KvPages, cache: KvCache) -> int:
+    """The device of both."""
+    if pages.device != cache.device:
+        raise ValueError(f"cache and pool are on different devices, cuda:{cache.device} and cuda:{pages.device}")
+    return _on(pages.device)
+
+
 def kv_cache(k_codes: torch.Tensor, v_codes: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor) -> KvCache:
     """The 8-bit key/value cache in these buffers: codes uint8 n_layers x n_pages x
     n_kv x page_size x head_dim, scales fp32 n_layers x n_pages x n_kv x
@@ -722,7 +729,7 @@ def realq_pages_reserve(pages: KvPages, starts: torch.Tensor, positions: torch.T
     """Room for starts[s + 1] - starts[s] more tokens in each row; positions (int64)
     receives theirs, or -1 throughout where the pool has too few free pages (then
     realq_workspace_status(ws) raises REALQ_ERR_NO_PAGES and nothing has changed)."""
-    dev, (wp, wb) = _on(pages.device), _ws(ws)
+    dev, (wp, wb) = _pool(pages, cache), _ws(ws)
     T = positions.shape[0]
     _check(lib().realq_pages_reserve(_stream(stream), ctypes.byref(pages), _ints(starts, (pages.n_rows + 1,), "starts", dev), T,
                                      _ints(positions, (T,), "positions", dev, torch.int64), ctypes.byref(cache), wp, wb))
@@ -746,7 +753,7 @@ def realq_pages_compact(pages: KvPages, cache: KvCache, used_out: torch.Tensor, 
                         moved_to: torch.Tensor, ws: Optional[torch.Tensor] = None, stream=None) -> None:
     """The used pages move to the front of the pool: used_out and tables_out
     (which may be the pool's own) follow, moved_to has each page's new number."""
-    dev, (wp, wb) = _on(pages.device), _ws(ws)
+    dev, (wp, wb) = _pool(pages, cache), _ws(ws)
     n = pages.n_pages
     _check(lib().realq_pages_compact(
         _stream(stream), ctypes.byref(pages), ctypes.byref(cache), _ints(used_out, (n,), "used_out", dev),

@@ -25,3 +25,12 @@ def test_a_scale_that_base_two_cannot_hold(L):
         assert call(scale) == INVALID, scale
     for scale in (2.3e38, -2.3e38, 0.0, 1.0):          # (past the scale, the missing workspace)
         assert call(scale) == WORKSPACE, scale
+
+
+def test_a_pool_and_a_cache_on_different_devices():
+    cache, pages = rq.KvCache(2, 10, 2, 64, 64, 16, 0x10000, 0x20000, 0x30000, 0x40000), rq.KvPages(10, 3, 5, 0x10000, 0x20000, 0x30000)
+    cache.device, pages.device = 0, 1
+    i = torch.zeros(4, dtype=torch.int32)
+    for call in (lambda: rq.realq_pages_reserve(pages, i, i.long(), cache), lambda: rq.realq_pages_compact(pages, cache, i, i, i)):
+        with pytest.raises(ValueError, match="cache and pool"):
+            call()
