@@ -29,7 +29,8 @@ import torch
 
 from . import (REALQ_ERR_TIMEOUT, RealqError, kv_cache, kv_pages, realq_kv_append, realq_kv_attention, realq_kv_attention_workspace_size,
                realq_pages_compact, realq_pages_fork, realq_pages_release, realq_pages_reserve,
-               realq_pages_workspace_size, realq_rotary, realq_rotary_frequencies, realq_workspace_status, workspace, _stream)
+               realq_pages_workspace_size, realq_rotary, realq_rotary_frequencies, realq_workspace_status, workspace, _heads,
+               _ints as _buffer, _stream)
 
 Rows = Union[Sequence[int], torch.Tensor]
 _HERE = contextlib.nullcontext()
@@ -67,6 +68,7 @@ class Cache8:
         codes = [torch.full((*shape, head_dim), 128, dtype=torch.uint8, device=device) for _ in range(2)]
         scales = [new(*shape[:3], page_size // scale_block, dtype=torch.float32) for _ in range(2)]
         self.cache = kv_cache(codes[0], codes[1], scales[0], scales[1])
+        self._sizes = layers, n_kv, head_dim, self.cache.device
         max_pages = -(-max_tokens // page_size)
         self.used, self.lengths = new(n_pages, dtype=torch.int32), new(rows, dtype=torch.int32)
         self.tables = torch.full((rows, max_pages), -1, dtype=torch.int32, device=device)
@@ -130,6 +132,7 @@ class Cache8:
         T, H, _ = q.shape
         if T != step.positions.shape[0]:
             raise ValueError(f"q: {step.positions.shape[0]} tokens expected, got {T}")
+        self._refuse(layer, q, k, v, out, lse, window, scale)
         with self._begin(stream, q, k, v, out, lse, step.starts, step.positions):
             if out is None:
                 out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
@@ -139,6 +142,28 @@ class Cache8:
             realq_kv_append(self.cache, layer, k, v, step.starts, step.positions, self.tables)
             return realq_kv_attention(q, self.cache, layer, step.starts, self.lengths, self.tables, out, lse=lse, scale=scale,
                                       window=window, max_new=step.most, ws=self._attend_ws)
+
+    def _refuse(self, layer, q, k, v, out, lse, window, scale) -> None:
+        """What appending and attention would refuse, before q and k are turned."""
+        layers, kv, head_dim, device = self._sizes
+        dt, (T, H, D) = q.dtype, q.shape
+        if not 0 <= layer < layers:
+            raise ValueError(f"layer: one of {layers} expected, got {layer}")
+        if D != head_dim or H % kv or not 0 < H <= 1024 * kv:
+            raise ValueError(f"q: heads of {head_dim} values expected, 1 to 1024 for each of {kv}")
+        if k.dtype is not dt or v.dtype is not dt:
+            raise ValueError("q, k and v have one dtype")
+        for t, name in ((k, "k"), (v, "v")):
+            if t.shape != (T, kv, D) or t.get_device() != device or not t.is_contiguous():
+                _, ld, hs = _heads(t, name, device, (T, kv, D))
+                if min(ld, hs) < D:
+                    raise ValueError(f"{name}: heads or tokens overlap")
+        if out is not None:
+            _buffer(out, q.shape, "out", device, dt)
+        if lse is not None:
+            _buffer(lse, (T, H), "lse", device, torch.float32)
+        if window < 0 or (scale is not None and not abs(scale) <= 2.0 ** 127):
+            raise ValueError("window from 0 on, |scale| up to 2^127 expected")
 
     def fork(self, src: Rows, dst: Rows, stream=None) -> None:
         """Rows dst[i] go on from rows src[i]'s sequences, all at once (a beam search's reordering)."""

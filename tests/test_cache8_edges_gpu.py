@@ -63,3 +63,23 @@ def test_check_reports_both_errors():
         c.check()
     assert e.value.status == rq.REALQ_ERR_NO_PAGES
     c.check()
+
+
+def test_a_refused_attend_changes_nothing():
+    """Whatever attend refuses, q and k are not turned and nothing is cached."""
+    c, = caches(1)
+    step = c.begin([5, 1, 0])
+    q, k, v = tokens(6, 3)
+    before = [t.clone() for t in (q, k, *c.cache.tensors)]
+    out = torch.empty_like(q)
+    for bad in (dict(layer=2), dict(layer=-1), dict(v=v[:5]), dict(v=v.float()), dict(v=v.cpu()), dict(v=v[:, :1].expand(6, 2, 64)), dict(v=v[:, :1]),
+                dict(k=k[:, :1].contiguous()), dict(q=q[:, :7]), dict(out=out[:5]), dict(out=out.float()), dict(out=out.cpu()),
+                dict(lse=torch.empty(6, 7, device="cuda")), dict(lse=torch.empty(6, 8, device="cuda", dtype=torch.float64)),
+                dict(window=-1), dict(scale=float("nan")), dict(scale=float("inf")), dict(q=q[:5])):
+        a = dict(layer=0, q=q, k=k, v=v) | bad
+        with pytest.raises((ValueError, rq.RealqError)):
+            c.attend(step, a.pop("layer"), a.pop("q"), a.pop("k"), a.pop("v"), **a)
+        for t, want in zip((q, k, *c.cache.tensors), before):
+            assert torch.equal(t, want), bad
+    c.attend(step, 0, q, k, v, out=out, lse=torch.empty(6, 8, device="cuda"), window=3, scale=0.2)
+    assert bool(torch.isfinite(out.float()).all())
