@@ -110,7 +110,8 @@ class Cache8:
     def _ints(self, rows: Rows) -> torch.Tensor:
         if isinstance(rows, torch.Tensor):
             return rows
-        return torch.tensor(list(rows), dtype=torch.int32).to(self.used.device)
+        # (from pinned memory, which torch keeps until the copy is done: the host does not wait for the stream)
+        return torch.tensor(list(rows), dtype=torch.int32, pin_memory=True).to(self.used.device, non_blocking=True)
 
     def begin(self, counts: Sequence[int], stream=None) -> Step:
         """Room for counts[s] new tokens in each row."""

@@ -83,3 +83,22 @@ def test_a_refused_attend_changes_nothing():
             assert torch.equal(t, want), bad
     c.attend(step, 0, q, k, v, out=out, lse=torch.empty(6, 8, device="cuda"), window=3, scale=0.2)
     assert bool(torch.isfinite(out.float()).all())
+
+
+def test_steps_do_not_wait_for_the_gpu():
+    """begin, fork and release return while what was enqueued before them is still running."""
+    c, = caches(1)
+    calls = [lambda: c.begin([3, 1, 0]), lambda: c.fork([0], [2]), lambda: c.release([1])]
+    for _ in range(2):                   # (host memory, kernels and streams are there)
+        for f in calls:
+            f()
+    torch.cuda.synchronize()
+    done = torch.cuda.Event()
+    torch.cuda._sleep(2 * 10 ** 9)       # about a second
+    done.record()
+    for f in calls:
+        f()
+    waited = done.query()
+    torch.cuda.synchronize()
+    assert not waited
+    assert c.lengths.tolist() == [9, 0, 9]
