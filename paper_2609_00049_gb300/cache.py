@@ -89,10 +89,10 @@ class Cache8:
         """A call on `stream` (None: the current one) begins: after the caller's work
         and the cache's latest call.  The context that it runs in."""
         handle = _stream(stream)
-        if handle == self._handle and (stream is None or handle == _stream(None)):
-            return _HERE   # (nothing to order; making stream objects would take as long as a small kernel)
-        if stream is None and torch.cuda.is_current_stream_capturing():
-            return _HERE
+        if stream is None or handle == _stream(None):   # the current stream
+            # (nothing to order, or nothing that a capture could; making stream objects would take as long as a small kernel)
+            if handle == self._handle or torch.cuda.is_current_stream_capturing():
+                return _HERE
         caller = torch.cuda.current_stream(self.used.device)
         s = caller if stream is None else stream
         kept = given

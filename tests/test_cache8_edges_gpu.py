@@ -102,3 +102,20 @@ def test_steps_do_not_wait_for_the_gpu():
     torch.cuda.synchronize()
     assert not waited
     assert c.lengths.tolist() == [9, 0, 9]
+
+
+def test_a_captured_token_on_a_stream_given_by_name():
+    """attend captured with `stream` the stream that is being captured."""
+    eager, captured = caches(2)
+    for c in (eager, captured):
+        c.begin([20, 7, 1])
+    steps = [c.begin([1, 1, 1]) for c in (eager, captured)]
+    x = tokens(3, 5)
+    buf, out = [t.clone() for t in x], torch.empty(3, 8, 64, device="cuda", dtype=torch.bfloat16)
+    want = eager.attend(steps[0], 1, *[t.clone() for t in x])
+    g, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=side):
+        captured.attend(steps[1], 1, *buf, out=out, stream=side)
+    g.replay()
+    assert torch.equal(out, want)
