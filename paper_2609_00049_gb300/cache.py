@@ -42,6 +42,7 @@ class Step:
     starts: torch.Tensor      # rows + 1
     positions: torch.Tensor   # tokens
     most: int
+    handle: Optional[int] = None   # of the stream that begin made them on
 
 
 class Cache8:
@@ -121,7 +122,7 @@ class Cache8:
         for n in counts:
             at.append(at[-1] + n)
         with self._begin(stream):
-            step = Step(self._ints(at), torch.empty(at[-1], dtype=torch.int64, device=self.used.device), max(counts))
+            step = Step(self._ints(at), torch.empty(at[-1], dtype=torch.int64, device=self.used.device), max(counts), _stream(None))
             realq_pages_reserve(self.pages, step.starts, step.positions, self.cache, ws=self._pages_ws)
         return step
 
@@ -135,6 +136,9 @@ class Cache8:
             raise ValueError(f"q: {step.positions.shape[0]} tokens expected, got {T}")
         self._refuse(layer, q, k, v, out, lse, window, scale)
         with self._begin(stream, q, k, v, out, lse, step.starts, step.positions):
+            if step.handle not in (None, self._handle) and not torch.cuda.is_current_stream_capturing():
+                for t in (step.starts, step.positions):   # (another step has come between)
+                    t.record_stream(self._latest)
             if out is None:
                 out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
             if T == 0:

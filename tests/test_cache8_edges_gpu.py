@@ -119,3 +119,29 @@ def test_a_captured_token_on_a_stream_given_by_name():
         captured.attend(steps[1], 1, *buf, out=out, stream=side)
     g.replay()
     assert torch.equal(out, want)
+
+
+def test_a_step_of_another_stream_keeps_its_memory():
+    """Two steps at a time, the first from another stream: its lists are not handed on while attention on this one reads them."""
+    c, = caches(1)
+    side = torch.cuda.Stream()
+    c.begin([5, 0, 0])
+    for warm in (True, False):           # (a kernel's first launch waits for the GPU)
+        first = c.begin([3, 0, 0], stream=side)
+        second = c.begin([0, 4, 0])
+        x, y = tokens(3, 1), tokens(4, 9)
+        torch.cuda.synchronize()
+        held, done = {first.starts.data_ptr(), first.positions.data_ptr()}, torch.cuda.Event()
+        if not warm:
+            torch.cuda._sleep(2 * 10 ** 9)           # about a second
+        done.record()
+        c.attend(second, 0, *y)
+        c.attend(first, 0, *x)
+        del first
+        with torch.cuda.stream(side):
+            new = [torch.empty(4, dtype=torch.int32, device="cuda") for _ in range(200)]
+        handed_on, waited = held & {t.data_ptr() for t in new}, done.query()
+        torch.cuda.synchronize()
+        if not warm:
+            assert not waited and not handed_on
+        del new
