@@ -245,3 +245,48 @@ def test_a_nan_among_values_of_no_weight(m, block, dtype):
     assert bool(out.isnan().all()) and bool(torch.isfinite(lse).all())
     out, lse = run(q, h, starts_of([m]), c.lengths, c.tables, scale=1.0, window=20)
     assert bool(out[p < 35].isnan().all()) and bool(torch.isfinite(out[p >= 35]).all()) and bool(torch.isfinite(lse).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("starts,lens", [([45, 90, 0, 45], [90, 77, 60]),               # the second is out of order
+                                         ([0, 45, 200, 200], [90, 77, 60]), ([-3, 45, 90, 90], [90, 95, 60]),
+                                         ([0, 45, 46, 90], [90, -5, 0]), ([0, 3, 5, 6], [90, -2 ** 31, 1])])
+def test_attention_with_faulty_lists(starts, lens, dtype):
+    """Sequences whose starts are not in order or lie outside take no part: their rows stay as they were, the others' are
+    right.  A length below zero is none: such rows see nothing."""
+    c = Cache(35, [96] * 3, kv=2, D=64, page=16, block=16, poison=False)
+    T = 90
+    q = torch.randn(T, 4, 64, generator=gen(7), device="cuda").to(dtype)
+    out, lse = run(q, rq.kv_cache(**c.buffers()), i32(starts), i32(lens), c.tables)
+    touched = torch.zeros(T, dtype=torch.bool, device="cuda")
+    for s in range(3):
+        a, b, L = starts[s], starts[s + 1], max(0, lens[s])
+        if not 0 <= a < b <= T:
+            continue
+        touched[a:b] = True
+        want = expected(q[a:b], c.values("k", 0, s, L), c.values("v", 0, s, L), torch.ones(L, dtype=torch.bool, device="cuda"), L, 0, True, 0.125)
+        close(out[a:b], lse[a:b], *want, 96)
+    assert bool((out[~touched] == 9).all()) and bool((lse[~touched] == 9).all()) and bool(touched.any())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("block", [16, 2])
+@pytest.mark.parametrize("news", [[1, 2], [60, 90]])
+def test_attention_over_missing_pages(news, block, dtype):
+    """Pages outside the pool inside a sequence: their tokens take no part."""
+    lens = [300, 170]
+    c = Cache(36, lens, kv=2, D=64, page=16, block=block, poison=False)
+    gone = [[0, 3, 4, 11, 18], [9, 10]]
+    for s, bad in enumerate([[-1, 10 ** 6, c.n_pages, -2 ** 31, 2 ** 31 - 1], [-7, c.n_pages + 1]]):
+        c.tables[s, gone[s]] = i32(bad)
+    q = torch.randn(sum(news), 4, 64, generator=gen(8), device="cuda").to(dtype)
+    out, lse = run(q, rq.kv_cache(**c.buffers()), starts_of(news), c.lengths, c.tables, max_new=max(news))
+    at = 0
+    for s, (m, L) in enumerate(zip(news, lens)):
+        there = ~torch.isin(torch.arange(L, device="cuda") // 16, torch.tensor(gone[s], device="cuda"))
+        rows = torch.tensor(c.rows[s], device="cuda")[torch.arange(L, device="cuda") // 16]
+        slot = torch.arange(L, device="cuda") % 16
+        K, V = ((codes[0, rows, :, slot].double() - 128) * scale[0, rows, :, slot // block].double()[..., None]
+                for codes, scale in ((c.k_codes, c.k_scale), (c.v_codes, c.v_scale)))
+        close(out[at:at + m], lse[at:at + m], *expected(q[at:at + m], K, V, there, L, 0, True, 0.125), L)
+        at += m
