@@ -90,6 +90,10 @@ __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t *r) {
         : "memory");
 }
 
+__device__ __forceinline__ void tmem_ld_x8(uint32_t taddr, uint32_t (&r)[8]) {   // complete after tmem_wait_ld
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr));
+}
 __device__ __forceinline__ void tmem_st_x8(uint32_t taddr, const uint32_t (&r)[8]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
                  "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
@@ -225,6 +229,25 @@ template <int ROWS, int KT> struct Walk {
         set();
     }
 };
+
+// The sum's part of 2^(S ks r - M) for the tokens among a thread's `cols` whose scale lies far below others (no weight of
+// theirs is in P).  Not inlined: no instruction of the usual tiles makes room for it.
+__device__ __noinline__ float far_weights(uint32_t s_at, const float *sc, int stride, int cols, int step, int lo, int hi, float factor, float lift) {
+    float sum = 0.f;
+#pragma unroll 1
+    for (int c = 0; c < cols; c += 8) {
+        uint32_t v[8];
+        tmem_ld_x8(s_at + c, v);
+        tc::tmem_wait_ld();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float *at = step ? sc + c + j : sc + (c & ~15) / 4;
+            if (c + j >= lo && c + j < hi && at[2 * stride] == 0.f && at[stride] > NEG) sum += exp2_fast(fmaf(__uint_as_float(v[j]), at[0] * factor, lift));
+        }
+        __syncwarp();
+    }
+    return sum * OWN_DOWN;
+}
 
 template <int DP, bool F32, class T>
 __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constant__ KvAttnArgs a, int *err) {
@@ -429,7 +452,8 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                 s_phase ^= 1u;
                 if (!ok) break;
                 tc::fence_after_sync();
-                const bool masked = k0 + (COLS - 1) >= all_hi || k0 < all_lo || far_scales[slot] != 0;
+                const bool masked = k0 + (COLS - 1) >= all_hi || k0 < all_lo;
+                const int far = far_scales[slot];
                 const float *sc = reinterpret_cast<const float *>(smem + Sh::SCALES + slot * Sh::SLOT_BYTES) + half * (fine ? COLS : COLS / 4);
                 const auto seen = [&](int j) { return k0 + j < row_hi && k0 + j >= row_lo; };
                 // the largest S ks r + lv
@@ -475,7 +499,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                     swap[half][i][row] = top;
                     ok = pair(abort_flag) && ok;
                     top = fmaxf(top, swap[half ^ 1][i][row]);
-                    const bool grew = top > (m == NEG ? NEG : m + SLACK);
+                    const bool grew = far != 0 || top > (m == NEG ? NEG : m + SLACK);
                     if (__any_sync(FULL, grew)) {
                         const float now = fmaxf(m, top), drop = now == NEG ? 0.f : m - now, f = exp2_fast(drop);
                         m = now, l = lowered(l, drop);
@@ -490,6 +514,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                                 tmem_st_x16(o_at + c, v);
                             }
                         }
+                        if (far != 0) l += far_weights(s_at, sc, fine ? KT : 1, COLS, fine, row_lo - k0, row_hi - k0, factor, OWN - (m == NEG ? 0.f : m));
                     }
                     base = LIFT - (m == NEG ? 0.f : m);
                 };
@@ -502,14 +527,6 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                         const float c1 = b.x * factor, c0 = b.y + base;
                         const uint64_t c11 = two(c1, c1), c00 = two(c0, c0);
                         uint64_t part2 = 0;
-                        if constexpr (masks) {
-                            if (b.z == 0.f && b.y > NEG) {   // a scale far below others
-                                float own = 0.f;
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) own += exp2_fast(seen(c + j) ? fmaf(__uint_as_float(v[j]), c1, base + (OWN - LIFT)) : NEG);
-                                l = fmaf(own, OWN_DOWN, l);
-                            }
-                        }
 #pragma unroll
                         for (int j = 0; j < 16; j += 2) {
                             float2 x = halves(fma2(two(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), c11, c00));
@@ -531,18 +548,15 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                         for (int j = 0; j < 16; j += 4) {
                             const float4 ks = *reinterpret_cast<const float4 *>(sc + c + j), lv = *reinterpret_cast<const float4 *>(sc + KT + c + j);
                             const float4 iv = *reinterpret_cast<const float4 *>(sc + 2 * KT + c + j);   // with a minus: the value is NaN
-                            const float c1[4] = {ks.x * factor, ks.y * factor, ks.z * factor, ks.w * factor}, lvs[4] = {lv.x, lv.y, lv.z, lv.w};
+                            float x[4] = {fmaf(__uint_as_float(v[j]), ks.x * factor, lv.x + base), fmaf(__uint_as_float(v[j + 1]), ks.y * factor, lv.y + base),
+                                          fmaf(__uint_as_float(v[j + 2]), ks.z * factor, lv.z + base), fmaf(__uint_as_float(v[j + 3]), ks.w * factor, lv.w + base)};
                             const float inv[4] = {iv.x, iv.y, iv.z, iv.w};
-                            float x[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                const float s = __uint_as_float(v[j + e]);
-                                x[e] = exp2_fast(seen(c + j + e) ? fmaf(s, c1[e], lvs[e] + base) : NEG);
+                                x[e] = exp2_fast(seen(c + j + e) ? x[e] : NEG);
                                 const bool some = seen(c + j + e);
                                 l = fmaf(x[e], some ? fabsf(inv[e]) : 0.f, l);
                                 if (some && signbit(inv[e])) bad = __uint_as_float(0x7FC00000u);
-                                if (some && inv[e] == 0.f && lvs[e] > NEG)   // a scale far below others
-                                    l = fmaf(exp2_fast(fmaf(s, c1[e], base + (OWN - LIFT))), OWN_DOWN, l);
                             }
                             hi[j / 2] = pack_half(x[0], x[1]), hi[j / 2 + 1] = pack_half(x[2], x[3]);
                             if constexpr (F32) lo[j / 2] = pack_rest(x[0], x[1], hi[j / 2]), lo[j / 2 + 1] = pack_rest(x[2], x[3], hi[j / 2 + 1]);
