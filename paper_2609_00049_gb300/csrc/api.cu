@@ -1153,7 +1153,8 @@ realq_status_t realq_kv_attention(realq_stream_t stream, const realq_kv_cache_t 
     if (T * (n_heads / a.c.n_kv) >= INT32_MAX / 2) return fail(REALQ_ERR_UNSUPPORTED, "kv_attention: T n_heads / n_kv must be below 2^30");
     REALQ_TRY(check_ws(ws, ws_bytes, kv_attention_ws_bytes(), who));
     a.n_seqs = (int)n_seqs, a.n_heads = (int)n_heads, a.group = (int)(n_heads / a.c.n_kv), a.causal = causal != 0;
-    a.T = T, a.q = q, a.q_ld = q_ld, a.q_hs = q_hs, a.max_pages = max_pages, a.window = window;
+    a.T = T, a.q = q, a.q_ld = q_ld, a.q_hs = q_hs, a.max_pages = max_pages;
+    a.window = std::min<int64_t>(window, 1ll << 32);   // (no sequence is longer; positions below zero less it stay numbers)
     a.room = (int)std::min<int64_t>(max_pages << a.c.log_page, INT32_MAX);
     a.starts = starts, a.lengths = lengths, a.tables = tables, a.scale_log2 = scale_log2;
     a.out = out, a.lse = lse;

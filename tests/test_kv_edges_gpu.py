@@ -290,3 +290,16 @@ def test_attention_over_missing_pages(news, block, dtype):
                 for codes, scale in ((c.k_codes, c.k_scale), (c.v_codes, c.v_scale)))
         close(out[at:at + m], lse[at:at + m], *expected(q[at:at + m], K, V, there, L, 0, True, 0.125), L)
         at += m
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("news", [[5, 9], [60, 90]])
+def test_attention_of_the_largest_window(news, dtype):
+    """A window that no sequence reaches is none, for queries without cached tokens as well."""
+    c = Cache(37, [3, 70], kv=1, D=64, page=16, block=16, poison=False)
+    q = torch.randn(sum(news), 2, 64, generator=gen(9), device="cuda").to(dtype)
+    h = rq.kv_cache(**c.buffers())
+    want = run(q, h, starts_of(news), c.lengths, c.tables, max_new=max(news))
+    for window in (1000, 2 ** 31, 2 ** 40, 2 ** 63 - 1):
+        got = run(q, h, starts_of(news), c.lengths, c.tables, max_new=max(news), window=window)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), window
