@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
             // times 2^k: the largest lies in [2^14, 2^15) after that (a row below 2^-112 a little lower)
-            const int ex = (int)(__float_as_uint(top) >> 23), k = ex == 0 || ex == 255 ? 0 : min(126, 141 - ex);
+            const int ex = (int)(__float_as_uint(top) >> 23), k = ex == 255 ? 0 : min(126, 141 - ex);
             const float up = __uint_as_float((uint32_t)(127 + k) << 23);
 #pragma unroll
             for (int step = 0; step < Sh::STEPS; ++step) {

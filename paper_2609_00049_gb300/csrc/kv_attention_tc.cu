@@ -389,7 +389,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
 #pragma unroll
                     for (int o = 1; o < LANES; o *= 2) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
                     // times 2^k: the largest lies in [2^14, 2^15) after that (a row below 2^-112 a little lower)
-                    const int e = (int)(__float_as_uint(top) >> 23), k = e == 0 || e == 255 ? 0 : min(126, 141 - e);
+                    const int e = (int)(__float_as_uint(top) >> 23), k = e == 255 ? 0 : min(126, 141 - e);
                     float up = __uint_as_float((uint32_t)(127 + k) << 23);
                     const float back = fabsf(a.scale_log2) * __uint_as_float((uint32_t)(127 - k) << 23);
                     if (a.scale_log2 < 0.f) up = -up;   // (the scores' factor is to be positive)

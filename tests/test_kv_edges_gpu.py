@@ -303,3 +303,18 @@ def test_attention_of_the_largest_window(news, dtype):
     for window in (1000, 2 ** 31, 2 ** 40, 2 ** 63 - 1):
         got = run(q, h, starts_of(news), c.lengths, c.tables, max_new=max(news), window=window)
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), window
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("m", [1, 40])
+def test_attention_of_subnormal_queries(m, dtype):
+    """Rows whose largest value is below the smallest normal number, under a scale that makes scores of them; a row of zeros."""
+    c = Cache(38, [200], kv=2, D=64, page=16, block=16, poison=False)
+    q = torch.randn(m, 4, 64, generator=gen(10), device="cuda").clamp(-4, 4) * 2e-39
+    q[0, 1] = 0.0
+    q = q.to(dtype)
+    assert 0.0 < float(q.double().abs().max()) < 2.0 ** -126
+    out, lse = run(q, rq.kv_cache(**c.buffers()), starts_of([m]), c.lengths, c.tables, scale=5e37)
+    sc = torch.tensor(5e37, dtype=F32).double().item()
+    # (values of the scaled rows are held to 2^-25 with a largest of 2^-2 and more: within the tolerance's 2^-20)
+    close(out, lse, *attention(q, c.values("k", 0, 0), c.values("v", 0, 0), 200, 0, True, sc), 200)
