@@ -146,9 +146,8 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
         // ---- this warp's 16 tokens of every tile ----
         const int *table = a.tables + (int64_t)u.seq * a.max_pages;
         const auto page_of = [&](int i) {   // of the warp's group i, -1 where there is none
-            if (i >= count) return -1;
             const int k0 = (tile0 + i) * TILE + warp * GROUP;   // (k0 + GROUP may be 2^31)
-            if (k0 >= u.hi || k0 + (GROUP - 1) < u.lo) return -1;
+            if (i >= count || k0 >= u.hi || k0 + (GROUP - 1) < u.lo) return -1;
             const int pg = table[k0 >> a.c.log_page];
             return pg >= 0 && pg < a.c.n_pages ? pg : -1;
         };
@@ -344,7 +343,7 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     const float f0 = exp2_fast(drop[nt][0]), f1 = exp2_fast(drop[nt][1]);
-                    sum[nt][0] = lowered(sum[nt][0], drop[nt][0]), sum[nt][1] = lowered(sum[nt][1], drop[nt][1]);
+                    sum[nt][0] = lowered(sum[nt][0], drop[nt][0], f0), sum[nt][1] = lowered(sum[nt][1], drop[nt][1], f1);
 #pragma unroll
                     for (int d = 0; d < Sh::MT; ++d) o[d][nt][0] *= f0, o[d][nt][1] *= f1, o[d][nt][2] *= f0, o[d][nt][3] *= f1;
                 }
@@ -455,9 +454,9 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
             for (int w = 0; w < WARPS; ++w) m = fmaxf(m, join_m[w][r]);
 #pragma unroll
             for (int w = 0; w < WARPS; ++w) {
-                const float mw = join_m[w][r];
-                l += mw == NEG ? join_l[w][r] * 0.f : lowered(join_l[w][r], mw - m);
-                join_m[w][r] = mw == NEG ? 0.f : exp2_fast(mw - m);
+                const float mw = join_m[w][r], f = mw == NEG ? 0.f : exp2_fast(mw - m);
+                l += lowered(join_l[w][r], mw - m, f);
+                join_m[w][r] = f;
             }
             row_m[r] = m, row_l[r] = l;
             if (!whole) slot[ROWS * DP + r] = m, slot[ROWS * DP + ROWS + r] = l;
@@ -513,9 +512,9 @@ __global__ void __launch_bounds__(THREADS) decode_kernel(KvAttnArgs a) {
                             if (pass == 1 || parts <= AT_ONCE) {
                                 float some = 0.f;
                                 for (int c = lane; c < n; c += 32) {
-                                    const float mc = ms[c * ROWS + r], lc = ls[c * ROWS + r];
-                                    some += mc == NEG ? lc * 0.f : lowered(lc, mc - m);
-                                    ms[c * ROWS + r] = mc == NEG ? 0.f : exp2_fast(mc - m);
+                                    const float mc = ms[c * ROWS + r], f = mc == NEG ? 0.f : exp2_fast(mc - m);
+                                    some += lowered(ls[c * ROWS + r], mc - m, f);
+                                    ms[c * ROWS + r] = f;
                                 }
 #pragma unroll
                                 for (int o = 16; o; o /= 2) some += __shfl_xor_sync(0xFFFFFFFFu, some, o);

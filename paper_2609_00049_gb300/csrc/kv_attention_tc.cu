@@ -502,7 +502,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
                     const bool grew = far != 0 || top > (m == NEG ? NEG : m + SLACK);
                     if (__any_sync(FULL, grew)) {
                         const float now = fmaxf(m, top), drop = now == NEG ? 0.f : m - now, f = exp2_fast(drop);
-                        m = now, l = lowered(l, drop);
+                        m = now, l = lowered(l, drop, f);
                         if (t > 0) {   // (the products so far are done: S came behind them)
     #pragma unroll 1
                             for (int c = 16 * half; c < D; c += 32) {
@@ -697,7 +697,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_kernel(const __grid_constan
             for (int c = 0; c < parts; ++c) {
                 const float *s = slot_of(first_cta + c, c == 0) + 128 * DP + row;
                 const float mc = __ldcg(s), lc = __ldcg(s + 128);
-                ll += mc == NEG ? lc * 0.f : lowered(lc, mc - mm);   // (a NaN stays one)
+                ll += lowered(lc, mc - mm, mc == NEG ? 0.f : exp2_fast(mc - mm));   // (a NaN stays one)
             }
             const float all_inv = ll == 0.f ? 0.f : DOWN / ll;
 #pragma unroll 1

@@ -45,11 +45,10 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// sum 2^d, d <= 0, in two steps: maxima hold the values' scales too, so that a sum may be 2^96 and belong to a maximum
-// that lies 2^-150 below (zero values beside large ones).  With d above -120 the second step is a multiplication by 1.
-__device__ __forceinline__ float lowered(float sum, float d) {
-    const float first = fmaxf(d, -120.f);
-    return sum * exp2_fast(first) * exp2_fast(d - first);
+// sum 2^d, d <= 0, with f = 2^d: maxima hold the values' scales too, so that a sum may be 2^96 and belong to a maximum
+// that lies 2^-150 below (zero values beside large ones), where f is no number: in two steps there.
+__device__ __forceinline__ float lowered(float sum, float d, float f) {
+    return d < -120.f ? sum * 7.523163845e-37f * exp2_fast(d + 120.f) : sum * f;
 }
 __device__ __forceinline__ float log2_fast(float x) {
     float y;
