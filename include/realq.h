@@ -492,8 +492,11 @@ realq_status_t realq_kv_read(realq_stream_t stream, const realq_kv_cache_t *cach
  * every sequence are left as they were in out and lse.  Scores, sums and
  * outputs are held in fp32; with bf16 inputs the weights of the values are
  * rounded to fp16 (2^-11 of each, an eighth of the output's own rounding), with
- * fp32 inputs queries and weights are taken as two fp16 parts each.  The order of summation is fixed by the
- * lengths and sizes (bitwise repeatable).  T = 0 is a no-op.  Asynchronous. */
+ * fp32 inputs queries and weights (times their values' scales) are taken as two
+ * fp16 parts each: 22 bits of those near their row's largest, 2^-31 of the largest in
+ * all.  In sequences of many rows the values' scales enter through an approximate
+ * log2, off by 2^-22 of itself.  The order of summation is fixed by the lengths and sizes
+ * (bitwise repeatable).  T = 0 is a no-op.  Asynchronous. */
 size_t realq_kv_attention_workspace_size(const realq_kv_cache_t *cache, int64_t n_seqs, int64_t T, int64_t n_heads);
 realq_status_t realq_kv_attention(realq_stream_t stream, const realq_kv_cache_t *cache, int64_t layer, int64_t n_seqs,
                                   int64_t T, int64_t n_heads, const void *q, int64_t q_ld, int64_t q_hs,
@@ -516,7 +519,8 @@ realq_status_t realq_kv_attention(realq_stream_t stream, const realq_kv_cache_t 
  * last row of the call may keep the page where all its holders are in the
  * call): what realq_kv_append writes afterwards is the row's own.  A sequence is
  * put back to fewer tokens by lowering its length: pages behind its end stay
- * with the row until they are replaced here, or the row is released.  All or
+ * with the row until they are replaced here, or the row is released (they do not
+ * count as free before that: in a full pool such a row is refused).  All or
  * nothing: with too few free pages, entries or positions, or starts out of
  * order, nothing changes, all T positions become -1 (so that appending does
  * nothing) and the status becomes REALQ_ERR_NO_PAGES.

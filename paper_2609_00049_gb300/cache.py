@@ -130,7 +130,8 @@ class Cache8:
                out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, window: int = 0,
                scale: Optional[float] = None, stream=None) -> torch.Tensor:
         """The step's tokens through one layer: q and k get their positions (in place),
-        k and v go into the cache, and q attends to all of its row's tokens so far."""
+        k and v go into the cache, and q attends to all of its row's tokens so far.  (By the
+        rows' latest lengths: a row takes part in the next step when all layers are through this one.)"""
         T, H, _ = q.shape
         if T != step.positions.shape[0]:
             raise ValueError(f"q: {step.positions.shape[0]} tokens expected, got {T}")

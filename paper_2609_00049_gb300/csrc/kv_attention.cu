@@ -35,8 +35,8 @@
 // wraps to zero by itself.
 //
 // Measured: one token of each of 64 sequences of up to 16384, 64 heads to 8 of 128
-// (1.24 GB of codes): 222 us, 5.6 TB/s, 0.81 of a copy's rate, with 0.64 of the issue
-// slots used at three CTAs to an SM; one token over 131072: 62 us, of which 40 are
+// (1.24 GB of codes): 224 us, 5.5 TB/s, 0.81 of a copy's rate, with 0.63 of the issue
+// slots used at three CTAs to an SM; one token over 131072: 64 us, of which 40 are
 // the codes; one token over 1013, 16 heads: 10 us in a graph, all of it latency.
 #include <algorithm>
 

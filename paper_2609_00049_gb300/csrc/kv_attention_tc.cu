@@ -26,7 +26,11 @@
 // the sum then takes 2^(S ks r - M) by an exponential of its own, in tiles marked by the loader.  Scale blocks of fewer than 16
 // tokens take one scale per token in the same formulas.  bf16 queries are exact in
 // fp16 after scaling (down to 2^-29 of a row's largest value); fp32 queries and their p are two fp16
-// parts each, which doubles the products.
+// parts each, which doubles the products: 22 bits of a p near the largest, which is 2^6 to 2^14, and
+// to 2^-25 in any (a weight 2^-20 of its row's largest may have only its upper part).  V's scale enters
+// as 2^lv with lv from lg2.approx, off by 2^-22 of itself (the sum takes the same lv out again).
+// Measured for heads of 128 above all; those of 256 have one ring slot (and with fp32 one stage), so
+// that loading, converting and products take turns there.
 //
 // P lies over S in TMEM (its low part, with fp32, has columns of its own), so the next
 // product into S is issued behind the product that reads P; the tensor cores run
@@ -34,11 +38,15 @@
 // joined by the warps that end last.
 //
 // Measured (bf16, 128 channels, 8 heads to a key/value head): a prompt of 8192 tokens
-// 1560 us, 0.70 PFLOP/s, 0.37 of the measured bf16 rate; 5 ragged chunks of up to 1500
-// tokens over up to 12000, 32 heads to 8, 578 us.  Bound by instructions: the
-// schedulers issue in 0.66 of their cycles, some 3500 times for each 256 x 128
-// scores (ALU 0.50, tensor cores 0.39 of their cycles), beside the chain maximum,
-// weights, product of a row tile.  Slower were: tiles of 64 tokens with two parts of
+// 1570 us, 0.70 PFLOP/s, 0.37 of the measured bf16 rate; 5 ragged chunks of up to 1500
+// tokens over up to 12000, 32 heads to 8, 578 us.  No unit is busy throughout: the
+// schedulers issue in 0.66 of their cycles, some 3500 times for each 256 x 128 scores, the
+// ALU works in 0.50 of them, the tensor cores in 0.39, shared memory in 0.55 (0.30 for
+// threads, 0.25 for the tensor cores' operands).  Instructions alone do not bound it: of an
+// earlier version with 20 warps 56 % of them could be taken out for 17 % of the cycles.
+// Scores, maximum, weights and product of a row tile follow one another, as P lies
+// over S; that chain and shared memory are what is left to explain the rest.  Slower
+// were: tiles of 64 tokens with two parts of
 // scores in TMEM (1965 us), one pass with the old maximum and P in registers (1602),
 // more registers for the softmax warps from the others (1595).
 #include <algorithm>
